@@ -298,7 +298,7 @@ def prepare(case, seed):
 def _device(s, head_dim=128, q_heads=8, kv_heads=8, rope=None):
     import paper_2512_16822_b200 as M
     from paper_2512_16822_b200 import runtime as RT
-    max_position = 16 if rope is None else rope.shape[0] - 1
+    max_position = 64 if rope is None else rope.shape[0] - 1
     cfg = M.Config(s["page"] if "page" in s else s["case"]["page"], q_heads, kv_heads, head_dim, s.get("num_pages", 1), max_position, 5e5)
     if "k_scales" in s:
         dev = RT.Device.over(cfg, rope=rope, device=DEV)
