@@ -63,6 +63,8 @@ extern "C" {
 #define MEPIC_DEV_BAD_POSITION  0x4 /* a position fell outside the rope table */
 #define MEPIC_DEV_BAD_SLOT      0x8 /* a new row's logical slot fell outside its request */
 #define MEPIC_DEV_BAD_PLAN      0x10 /* a grouped-decode plan no longer matches kv_len (a request gained or lost a page) */
+#define MEPIC_DEV_BAD_TREE      0x20 /* a drafted row's parent does not precede it, or a request has more rows than the call was told */
+#define MEPIC_DEV_NO_PAGES      0x40 /* mepic_step_tables: the reserve, the tables or the row arrays cannot hold the step; nothing was handed out */
 
 #define MEPIC_SEG_CHUNK  0
 #define MEPIC_SEG_PROMPT 1
@@ -522,6 +524,185 @@ int32_t mepic_attn_decode_grouped_fp8(const mepic_config_t* cfg, const mepic_dec
  */
 int32_t mepic_attn_prefill_fp8(const mepic_config_t* cfg, const mepic_prefill_args_t* args, float* k_scales, float* v_scales,
                                void* cuda_stream);
+
+/* ---------------------------------------------------------------- drafted tokens (device)
+ *
+ * The calls of a step in which every request drafts a TREE of tokens, the model scores all of them in one pass and the
+ * path it agrees with is kept.  (The paper has no counterpart; speculative decoding is one of the serving layers its
+ * pages go under.  Un-rotated pages fit it well: a drafted row's K/V can be written to the slot it ends up in as it is,
+ * with no rotation to undo.)  Drafted rows live OUTSIDE the page pool until they are accepted.  In the order of a step:
+ *   mepic_tree_layout -> (per layer) mepic_attn_tree / _fp8 -> sampling by the caller -> mepic_tree_accept
+ *   -> mepic_step_tables -> (per layer) mepic_rows_commit / _fp8.
+ * mepic_step_tables and mepic_rows_commit know nothing of trees: they serve any append (one token per request of a plain
+ * decode loop, a prompt's rows) and give mepic_attn_decode and mepic_attn_prefill their tables without a host round trip.
+ *
+ * Rows are grouped by request: rows row_offsets[b] .. row_offsets[b+1]-1 of the row arrays belong to request b, which may
+ * have none; row arrays hold total_rows rows and rows that no request owns are neither read nor written.  A row's parent
+ * is the index WITHIN its request of the row it continues, -1 for the request's context, and precedes the row.
+ * Every pointer of the structs below is a DEVICE pointer; int32 arrays are packed.  row_offsets that decrease or leave
+ * [0, total_rows] are clamped and set MEPIC_DEV_BAD_TREE.  Host-side errors: E_INVAL, E_CUDA.  total_rows = 0 (or
+ * max_rows = 0) launches nothing that reads rows.
+ */
+#define MEPIC_TREE_MAX_ROWS 1024   /* drafted rows a request may have */
+
+/*
+ * mepic_tree_layout - what the attention of drafted rows needs beyond the rows: for row i of request b
+ *     row_pos[i]   = position after the request's last context slot + number of i's ancestors among the rows,
+ *     tree_mask[i] = bit j set iff row j of the request is i itself or an ancestor of i (word j / 32, bit j % 32).
+ * The position after the context is pos_base[b][e] + slot % page_size + 1 of its last slot, 0 for an empty context.
+ * A parent that does not precede its row, or lies below -1, sets MEPIC_DEV_BAD_TREE and counts as -1; rows of a request
+ * from index 32 * mask_words on set it too and get the context's next position and an empty mask.  A kv_len outside
+ * [0, table_stride * page_size] sets MEPIC_DEV_BAD_SLOT and is clamped.  mask_words: 1 .. MEPIC_TREE_MAX_ROWS / 32.
+ */
+typedef struct {
+  const int32_t* parent;       /* [total_rows] */
+  const int32_t* row_offsets;  /* [batch+1] */
+  const int32_t* kv_len;       /* [batch] context slots, the drafted rows not included */
+  const int32_t* pos_base;     /* [batch][table_stride] */
+  int32_t*       row_pos;      /* out [total_rows] */
+  int32_t*       tree_mask;    /* out [total_rows][mask_words] */
+  int32_t*       status;
+  int32_t        table_stride, batch, total_rows, mask_words;
+} mepic_tree_layout_args_t;
+int32_t mepic_tree_layout(const mepic_config_t* cfg, const mepic_tree_layout_args_t* args, void* cuda_stream);
+
+/*
+ * mepic_attn_tree - attention of the drafted rows: for row i of request b and query head h
+ *     out[i,h,:] = sum_{t in S(i)} softmax_t( sm_scale * < R(row_pos[i]) q[i,h,:] , R(pos_t) K_t > ) V_t ,
+ * S(i) = all kv_len[b] slots of the request's paged context plus the rows j of the request whose bit is set in
+ * tree_mask[i] (K_j = k_new[j] at position row_pos[j], V_j = v_new[j]).  tree_mask may be any relation, not only a
+ * tree's; a row that sees nothing (empty context, empty mask) gets zeros.  A masked row's K and V have no influence on
+ * the output whatever bits they hold, and slots at or beyond kv_len[b] are ignored whatever bits they hold.  kv_len[b]
+ * may be 0.  bf16 tensor-core products, fp32 accumulation; the rotated q (with sm_scale folded in) and K and the softmax
+ * weights are rounded to bf16 once each.
+ *
+ * q / k_new / v_new rows lie q_stride / kv_stride elements apart (0 = packed; otherwise at least a packed row and a
+ * multiple of 8): the three may be slices of one fused projection.  max_rows: the most rows any request has (launch sizing
+ * and the choice of split; requests with more set MEPIC_DEV_BAD_TREE and their rows from max_rows on are not computed);
+ * max_rows <= 32 * mask_words.  A kv_len outside [0, table_stride * page_size] sets MEPIC_DEV_BAD_SLOT and is clamped.
+ * The work is split over the key axis across the GPU; partials go to the workspace (mepic_attn_tree_workspace bytes,
+ * 16-byte aligned, contents overwritten) and a second kernel merges them.  Two calls that overlap on the GPU must not
+ * share a workspace.  The cut depends on device data only through kv_len and row_offsets: a captured call may be replayed
+ * with other lengths.
+ *
+ * mepic_attn_tree_fp8: the same over 8-bit pools (format above; head_dim 128); the drafted rows stay bf16.
+ */
+typedef struct {
+  const void*    q;            /* bf16 rows of [n_q_heads][head_dim], un-rotated */
+  const void*    k_new;        /* bf16 rows of [n_kv_heads][head_dim], un-rotated */
+  const void*    v_new;
+  const int32_t* row_offsets;  /* [batch+1] */
+  const int32_t* row_pos;      /* [total_rows] */
+  const int32_t* tree_mask;    /* [total_rows][mask_words] */
+  const void*    k_pool;
+  const void*    v_pool;
+  const int32_t* page_ids;     /* [batch][table_stride] */
+  const int32_t* pos_base;     /* [batch][table_stride] */
+  const int32_t* kv_len;       /* [batch] */
+  const float*   rope_table;
+  void*          out;          /* bf16 [total_rows][n_q_heads][head_dim], packed */
+  void*          workspace;
+  size_t         workspace_bytes;
+  int32_t*       status;
+  int32_t        table_stride, batch, total_rows, max_rows, mask_words;
+  int32_t        q_stride, kv_stride;
+  float          sm_scale;
+} mepic_attn_tree_args_t;
+
+/* Bytes of workspace for calls of up to max_rows rows per request on the CURRENT device; 0 on error. */
+size_t  mepic_attn_tree_workspace(const mepic_config_t* cfg, int32_t max_rows);
+int32_t mepic_attn_tree(const mepic_config_t* cfg, const mepic_attn_tree_args_t* args, void* cuda_stream);
+int32_t mepic_attn_tree_fp8(const mepic_config_t* cfg, const mepic_attn_tree_args_t* args, const float* k_scales,
+                            const float* v_scales, void* cuda_stream);
+
+/*
+ * mepic_tree_accept - the path through each request's tree that the model agrees with.  target[i]: the model's choice of
+ * the token after row i; root[b]: its choice after the context.  From the context on, the next row of the path is the
+ * first row (lowest index) whose parent is the path's last row and whose draft equals the choice made there; the path ends
+ * where there is none, or at max_accept rows.
+ *     n_accept[b]       rows on the path,
+ *     accept_rows[b][k] index into the row arrays of its k-th row, -1 from n_accept[b] on,
+ *     next_token[b]     the choice after its last row (root[b] if it is empty).
+ * Rows with a parent that does not precede them, and rows from MEPIC_TREE_MAX_ROWS on, set MEPIC_DEV_BAD_TREE and are
+ * never on a path.
+ */
+typedef struct {
+  const int32_t* parent;       /* [total_rows] */
+  const int32_t* row_offsets;  /* [batch+1] */
+  const int32_t* draft;        /* [total_rows] */
+  const int32_t* target;       /* [total_rows] */
+  const int32_t* root;         /* [batch] */
+  int32_t*       n_accept;     /* out [batch] */
+  int32_t*       accept_rows;  /* out [batch][max_accept] */
+  int32_t*       next_token;   /* out [batch] */
+  int32_t*       status;
+  int32_t        batch, total_rows, max_accept;
+} mepic_tree_accept_args_t;
+int32_t mepic_tree_accept(const mepic_tree_accept_args_t* args, void* cuda_stream);
+
+/*
+ * mepic_step_tables - block tables and slot maps from lengths, on the device: request b has kv_len[b] slots and gains
+ * n_new[b].  Pages it has no table entry for are taken from reserve[*reserve_used ...] (pages of the pool that nobody
+ * else holds: those of a store request built with one prompt segment will do) in request order, entry by entry; a new entry's pos_base continues the entry before
+ * it (0 for the first).  Outputs:
+ *     page_ids, pos_base   the new entries ceil(kv_len/P) .. ceil((kv_len+n_new)/P)-1 are written, nothing else is,
+ *     row_offsets[b]       sum of n_new below b (row_offsets[batch] = all),
+ *     row_slot[r]          logical slot of appended row r (what mepic_attn_prefill calls q_slot),
+ *     slot_map[r]          its physical slot: page id * page_size + in-page slot (what mepic_rows_commit takes),
+ *     kv_len_out[b]        kv_len[b] + n_new[b];   q_pos[b]: position of the last of them (-1 if there is none),
+ *     reserve_used_out     *reserve_used + pages taken.
+ * row_slot and slot_map hold max_rows entries; those past the last row are set to -1.  row_slot, slot_map and q_pos may be
+ * NULL.  Outputs must not overlap inputs, other than the two tables, which are updated in place.
+ * All or nothing: if the reserve, a table row (table_stride) or max_rows cannot hold the step, or a length is negative or
+ * beyond its table row, MEPIC_DEV_NO_PAGES is set and the outputs are those of a step with n_new = 0 for everybody.
+ * A page id outside the pool sets MEPIC_DEV_BAD_PAGE; its rows' slot_map entries become -1.
+ * batch <= MEPIC_STEP_MAX_BATCH.
+ */
+#define MEPIC_STEP_MAX_BATCH 8192
+typedef struct {
+  const int32_t* kv_len;           /* [batch] */
+  const int32_t* n_new;            /* [batch] */
+  int32_t*       page_ids;         /* in/out [batch][table_stride] */
+  int32_t*       pos_base;         /* in/out [batch][table_stride] */
+  const int32_t* reserve;          /* [n_reserve] page ids (NULL when n_reserve = 0) */
+  const int32_t* reserve_used;     /* [1] */
+  int32_t*       row_offsets;      /* out [batch+1] */
+  int32_t*       row_slot;         /* out [max_rows] or NULL */
+  int64_t*       slot_map;         /* out [max_rows] or NULL */
+  int32_t*       kv_len_out;       /* out [batch] */
+  int32_t*       q_pos;            /* out [batch] or NULL */
+  int32_t*       reserve_used_out; /* out [1] */
+  int32_t*       status;
+  int32_t        table_stride, batch, max_rows, n_reserve;
+} mepic_step_tables_args_t;
+int32_t mepic_step_tables(const mepic_config_t* cfg, const mepic_step_tables_args_t* args, void* cuda_stream);
+
+/*
+ * mepic_rows_commit - Section 3.3.2 for rows whose physical slots are known: appended row r (row_offsets[b] <= r <
+ * row_offsets[b+1]) goes, un-rotated, to slot_map[r] of the pools.  Its K/V are row r of k_new / v_new, or, with src_rows
+ * (the accept_rows of mepic_tree_accept), row src_rows[b][r - row_offsets[b]].  Source rows lie kv_stride elements apart
+ * (0 = packed); n_sources of them exist.  A source outside [0, n_sources) sets MEPIC_DEV_BAD_SLOT, a slot outside the pool
+ * MEPIC_DEV_BAD_PAGE; the row is skipped.  max_rows bounds row_offsets[batch] (launch sizing; rows past it are not
+ * committed and set MEPIC_DEV_BAD_SLOT).  Slots must differ from row to row.
+ *
+ * mepic_rows_commit_fp8: into 8-bit pools by the rule of mepic_attn_prefill_fp8: consecutive rows that go to one page are
+ * a run; a run that writes in-page slot 0 starts the page's blocks and sets their scales from its rows, any other run
+ * appends under the scales that stand.  A page's rows must be consecutive, as mepic_step_tables makes them.
+ */
+typedef struct {
+  const void*    k_new;        /* bf16 rows of [n_kv_heads][head_dim] */
+  const void*    v_new;
+  const int32_t* row_offsets;  /* [batch+1] */
+  const int64_t* slot_map;     /* [max_rows] */
+  const int32_t* src_rows;     /* [batch][src_stride] or NULL */
+  void*          k_pool;
+  void*          v_pool;
+  int32_t*       status;
+  int32_t        src_stride, batch, max_rows, n_sources, kv_stride;
+} mepic_rows_commit_args_t;
+int32_t mepic_rows_commit(const mepic_config_t* cfg, const mepic_rows_commit_args_t* args, void* cuda_stream);
+int32_t mepic_rows_commit_fp8(const mepic_config_t* cfg, const mepic_rows_commit_args_t* args, float* k_scales, float* v_scales,
+                              void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -511,3 +511,115 @@ def partial_attention(q: np.ndarray, K: np.ndarray, V: np.ndarray, sm_scale: flo
     m = s.max()
     e = np.exp(s - m)
     return m, e.sum(), e @ V
+
+
+# --------------------------------------------------------------------------- drafted tokens
+# A step in which every request drafts a tree of tokens (the paper has no counterpart; the definitions are this build's).
+
+def tree_layout(parent: Sequence[int], next_pos: int):
+    """One request's rows -> (positions, sees): row i continues row parent[i] (-1: the context), which precedes it.
+
+    A row's position is the context's next position plus its number of ancestors; sees[i, j] iff j is i or an ancestor.
+    """
+    n = len(parent)
+    depth = np.zeros(n, dtype=np.int64)
+    sees = np.zeros((n, n), dtype=bool)
+    for i, p in enumerate(parent):
+        assert -1 <= p < i
+        if p >= 0:
+            depth[i] = depth[p] + 1
+            sees[i] = sees[p]
+        sees[i, i] = True
+    return next_pos + depth, sees
+
+
+def pack_mask(sees: np.ndarray, words: int) -> np.ndarray:
+    """bool [n, m] -> int32 [n, words], bit j of word j // 32."""
+    out = np.zeros((sees.shape[0], words), dtype=np.uint32)
+    for i, j in zip(*np.nonzero(sees)):
+        out[i, j // 32] |= np.uint32(1) << np.uint32(j % 32)
+    return out.view(np.int32)
+
+
+def _values(x: np.ndarray) -> np.ndarray:
+    return bf16_bits_to_f64(x) if x.dtype == np.uint16 else np.asarray(x, dtype=np.float64)
+
+
+def tree_attention_one(q: np.ndarray, k_new: np.ndarray, v_new: np.ndarray, row_pos: Sequence[int], sees: np.ndarray,
+                       k_pool: np.ndarray, v_pool: np.ndarray, page_ids: Sequence[int], pos_base: Sequence[int], kv_len: int,
+                       sm_scale: float, theta: float):
+    """One request's drafted rows -> (out fp64 [n, Hq, D], sigma of the same shape).
+
+    Row i attends to the kv_len context slots and to the rows j with sees[i, j]; a row with nothing to see gets zeros.
+    Masked rows are left out, not weighted by zero.  sigma is the standard deviation of the output's error when the rotated
+    q (scaled) and K, the softmax weights and the output are each rounded once to bf16, relative error of a rounding
+    uniform in +-2^-8: a bound on each rounding's variance is u^2 / 3 with u = 2^-8, and to first order
+        err = sum_i e_i q_i sum_j w_j (v_j - out) k_ji + sum_j w_j (v_j - out) sum_i f_ji q_i k_ji + sum_j w_j g_j v_j + h out
+    with independent e, f, g, h.
+    """
+    P = k_pool.shape[2]
+    K = _values(gather_pages(k_pool, page_ids, kv_len)) if kv_len else np.zeros((0,) + (k_pool.shape[1], k_pool.shape[3]))
+    V = _values(gather_pages(v_pool, page_ids, kv_len)) if kv_len else np.zeros((0,) + (k_pool.shape[1], k_pool.shape[3]))
+    pos = np.concatenate([slot_positions(pos_base, kv_len, P), np.asarray(row_pos, dtype=np.int64)])
+    K = rope_rotate(np.concatenate([K, _values(k_new)]), pos[:, None], theta)
+    V = np.concatenate([V, _values(v_new)])
+    n, Hq, D = q.shape
+    G = Hq // K.shape[1]
+    qr = rope_rotate(_values(q), np.asarray(row_pos, dtype=np.int64)[:, None], theta) * sm_scale
+    out, sigma = np.zeros((n, Hq, D)), np.zeros((n, Hq, D))
+    u2 = 2.0 ** -16 / 3
+    for i in range(n):
+        keys = np.concatenate([np.arange(kv_len), kv_len + np.nonzero(sees[i])[0]])
+        if not len(keys):
+            continue
+        for h in range(Hq):
+            Kh, Vh = K[keys, h // G], V[keys, h // G]
+            w = _softmax_rows((Kh @ qr[i, h])[None])[0]
+            o = w @ Vh
+            off = w[:, None] * (Vh - o)                                            # [keys, D]
+            var = ((qr[i, h][:, None] * (Kh.T @ off)) ** 2).sum(axis=0)            # q's rounding
+            var += (off ** 2 * ((qr[i, h] * Kh) ** 2).sum(axis=1)[:, None]).sum(axis=0)
+            var += ((w[:, None] * Vh) ** 2).sum(axis=0) + o ** 2
+            out[i, h], sigma[i, h] = o, np.sqrt(u2 * var)
+    return out, sigma
+
+
+def tree_accept(parent: Sequence[int], draft: Sequence[int], target: Sequence[int], root: int, max_accept: int):
+    """One request -> (path of row indices, next token): the lowest-index matching child again and again."""
+    path, at, want = [], -1, int(root)
+    while len(path) < max_accept:
+        nxt = [i for i in range(len(parent)) if parent[i] == at and draft[i] == want]
+        if not nxt:
+            break
+        at = nxt[0]
+        path.append(at)
+        want = int(target[at])
+    return path, want
+
+
+def step_tables(kv_len, n_new, page_ids: np.ndarray, pos_base: np.ndarray, reserve, used: int, P: int, max_rows: int):
+    """Lengths and new rows -> dict of everything a step needs; page_ids / pos_base are copied.  The pages a request lacks come
+    from reserve[used:], request by request; a new entry continues the positions of the entry before it."""
+    page_ids, pos_base = page_ids.copy(), pos_base.copy()
+    need = [-(-(k + n) // P) for k, n in zip(kv_len, n_new)]
+    grow = [m - -(-k // P) for m, k in zip(need, kv_len)]
+    rejected = (sum(n_new) > max_rows or used + sum(grow) > len(reserve) or min(list(kv_len) + list(n_new)) < 0
+                or max(need) > page_ids.shape[1])
+    if rejected:
+        n_new, grow = [0] * len(kv_len), [0] * len(kv_len)
+    off = np.concatenate([[0], np.cumsum(n_new)]).astype(np.int64)
+    slot, phys = np.full(max_rows, -1, dtype=np.int64), np.full(max_rows, -1, dtype=np.int64)
+    q_pos = []
+    for b, (k, n) in enumerate(zip(kv_len, n_new)):
+        held = -(-k // P)
+        for e in range(held, held + grow[b]):
+            page_ids[b, e] = reserve[used]
+            used += 1
+            pos_base[b, e] = pos_base[b, e - 1] + P if e else 0
+        for t in range(n):
+            s = k + t
+            slot[off[b] + t], phys[off[b] + t] = s, int(page_ids[b, s // P]) * P + s % P
+        last = k + n - 1
+        q_pos.append(int(pos_base[b, last // P]) + last % P if 0 <= last < page_ids.shape[1] * P else -1)
+    return dict(page_ids=page_ids, pos_base=pos_base, row_offsets=off, row_slot=slot, slot_map=phys,
+                kv_len=np.asarray(kv_len) + np.asarray(n_new), q_pos=np.asarray(q_pos), reserve_used=used, rejected=rejected)

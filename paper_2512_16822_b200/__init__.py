@@ -26,6 +26,8 @@ __all__ = [
     "mepic_attn_decode_workspace", "mepic_attn_decode", "mepic_attn_decode_static",
     "mepic_pages_quantize", "mepic_attn_decode_fp8", "mepic_decode_plan_max_ints", "mepic_decode_plan_build", "mepic_decode_plan_patch", "mepic_attn_decode_grouped_workspace",
     "mepic_attn_decode_grouped", "mepic_attn_decode_grouped_fp8",
+    "mepic_tree_layout", "mepic_attn_tree_workspace", "mepic_attn_tree", "mepic_attn_tree_fp8", "mepic_tree_accept", "mepic_step_tables",
+    "mepic_rows_commit", "mepic_rows_commit_fp8", "MEPIC_TREE_MAX_ROWS", "MEPIC_STEP_MAX_BATCH",
     "MEPIC_DECODE_STATIC_SCRATCH_BYTES", "mepic_attn_prefill_workspace",
     "mepic_attn_prefill", "mepic_attn_prefill_fp8", "mepic_last_error", "mepic_launch_count",
     "MEPIC_OK", "MEPIC_E_INVAL", "MEPIC_E_NOSPACE", "MEPIC_E_NOTFOUND", "MEPIC_E_CAPACITY",
@@ -47,6 +49,10 @@ MEPIC_DEV_WAIT_EXPIRED = 0x2
 MEPIC_DEV_BAD_POSITION = 0x4
 MEPIC_DEV_BAD_SLOT = 0x8
 MEPIC_DEV_BAD_PLAN = 0x10
+MEPIC_DEV_BAD_TREE = 0x20
+MEPIC_DEV_NO_PAGES = 0x40
+MEPIC_TREE_MAX_ROWS = 1024
+MEPIC_STEP_MAX_BATCH = 8192
 
 
 class MepicError(RuntimeError):
@@ -95,6 +101,35 @@ class _DecodeGroupedArgsC(C.Structure):
                 ("plan_host", C.c_void_p), ("kv_len", C.c_void_p), ("q_pos", C.c_void_p), ("rope_table", C.c_void_p),
                 ("out", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
                 ("status", C.c_void_p), ("batch", C.c_int32), ("sm_scale", C.c_float)]
+
+
+class _TreeLayoutArgsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("parent", "row_offsets", "kv_len", "pos_base", "row_pos", "tree_mask", "status")] + \
+               [(n, C.c_int32) for n in ("table_stride", "batch", "total_rows", "mask_words")]
+
+
+class _AttnTreeArgsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k_new", "v_new", "row_offsets", "row_pos", "tree_mask", "k_pool", "v_pool", "page_ids",
+                                          "pos_base", "kv_len", "rope_table", "out", "workspace")] + \
+               [("workspace_bytes", C.c_size_t), ("status", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("table_stride", "batch", "total_rows", "max_rows", "mask_words", "q_stride", "kv_stride")] + \
+               [("sm_scale", C.c_float)]
+
+
+class _TreeAcceptArgsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("parent", "row_offsets", "draft", "target", "root", "n_accept", "accept_rows", "next_token",
+                                          "status")] + [(n, C.c_int32) for n in ("batch", "total_rows", "max_accept")]
+
+
+class _StepTablesArgsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("kv_len", "n_new", "page_ids", "pos_base", "reserve", "reserve_used", "row_offsets", "row_slot",
+                                          "slot_map", "kv_len_out", "q_pos", "reserve_used_out", "status")] + \
+               [(n, C.c_int32) for n in ("table_stride", "batch", "max_rows", "n_reserve")]
+
+
+class _RowsCommitArgsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_new", "v_new", "row_offsets", "slot_map", "src_rows", "k_pool", "v_pool", "status")] + \
+               [(n, C.c_int32) for n in ("src_stride", "batch", "max_rows", "n_sources", "kv_stride")]
 
 
 @dataclass(frozen=True)
@@ -158,6 +193,14 @@ _PROTOTYPES = {
     "mepic_attn_prefill_workspace": (C.c_size_t, [C.POINTER(_ConfigC), C.c_int32, C.c_void_p]),
     "mepic_attn_prefill": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_PrefillArgsC), C.c_void_p]),
     "mepic_attn_prefill_fp8": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_PrefillArgsC), C.c_void_p, C.c_void_p, C.c_void_p]),
+    "mepic_tree_layout": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_TreeLayoutArgsC), C.c_void_p]),
+    "mepic_attn_tree_workspace": (C.c_size_t, [C.POINTER(_ConfigC), C.c_int32]),
+    "mepic_attn_tree": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_AttnTreeArgsC), C.c_void_p]),
+    "mepic_attn_tree_fp8": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_AttnTreeArgsC), C.c_void_p, C.c_void_p, C.c_void_p]),
+    "mepic_tree_accept": (C.c_int32, [C.POINTER(_TreeAcceptArgsC), C.c_void_p]),
+    "mepic_step_tables": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_StepTablesArgsC), C.c_void_p]),
+    "mepic_rows_commit": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_RowsCommitArgsC), C.c_void_p]),
+    "mepic_rows_commit_fp8": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_RowsCommitArgsC), C.c_void_p, C.c_void_p, C.c_void_p]),
 }
 
 
@@ -511,3 +554,76 @@ def mepic_attn_decode_grouped_fp8(cfg: Config, *, q, k_pool, v_pool, k_scales, v
                             batch, sm_scale)
     c = cfg.c()
     _check(lib().mepic_attn_decode_grouped_fp8(C.byref(c), C.byref(a), _ptr(k_scales), _ptr(v_scales), _stream_ptr(stream)))
+
+
+# ------------------------------------------------------------------ drafted tokens (device)
+def mepic_tree_layout(cfg: Config, *, parent, row_offsets, kv_len, pos_base, row_pos, tree_mask, status, table_stride: int, batch: int,
+                      total_rows: int, mask_words: int, stream=None) -> None:
+    a = _TreeLayoutArgsC(_ptr(parent), _ptr(row_offsets), _ptr(kv_len), _ptr(pos_base), _ptr(row_pos), _ptr(tree_mask), _ptr(status),
+                         table_stride, batch, total_rows, mask_words)
+    c = cfg.c()
+    _check(lib().mepic_tree_layout(C.byref(c), C.byref(a), _stream_ptr(stream)))
+
+
+def mepic_attn_tree_workspace(cfg: Config, max_rows: int) -> int:
+    c = cfg.c()
+    n = int(lib().mepic_attn_tree_workspace(C.byref(c), max_rows))
+    if n == 0:
+        raise MepicError(MEPIC_E_INVAL, mepic_last_error())
+    return n
+
+
+def mepic_attn_tree(cfg: Config, *, q, k_new, v_new, row_offsets, row_pos, tree_mask, k_pool, v_pool, page_ids, pos_base, kv_len,
+                    rope_table, out, workspace, workspace_bytes: int, status, table_stride: int, batch: int, total_rows: int,
+                    max_rows: int, mask_words: int, sm_scale: float, q_stride: int = 0, kv_stride: int = 0, stream=None) -> None:
+    a = _AttnTreeArgsC(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(row_offsets), _ptr(row_pos), _ptr(tree_mask), _ptr(k_pool), _ptr(v_pool),
+                       _ptr(page_ids), _ptr(pos_base), _ptr(kv_len), _ptr(rope_table), _ptr(out), _ptr(workspace), workspace_bytes,
+                       _ptr(status), table_stride, batch, total_rows, max_rows, mask_words, q_stride, kv_stride, sm_scale)
+    c = cfg.c()
+    _check(lib().mepic_attn_tree(C.byref(c), C.byref(a), _stream_ptr(stream)))
+
+
+def mepic_attn_tree_fp8(cfg: Config, *, q, k_new, v_new, row_offsets, row_pos, tree_mask, k_pool, v_pool, k_scales, v_scales, page_ids,
+                        pos_base, kv_len, rope_table, out, workspace, workspace_bytes: int, status, table_stride: int, batch: int,
+                        total_rows: int, max_rows: int, mask_words: int, sm_scale: float, q_stride: int = 0, kv_stride: int = 0,
+                        stream=None) -> None:
+    """mepic_attn_tree over 8-bit pools: k_pool / v_pool are e4m3 codes, k_scales / v_scales their scales."""
+    a = _AttnTreeArgsC(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(row_offsets), _ptr(row_pos), _ptr(tree_mask), _ptr(k_pool), _ptr(v_pool),
+                       _ptr(page_ids), _ptr(pos_base), _ptr(kv_len), _ptr(rope_table), _ptr(out), _ptr(workspace), workspace_bytes,
+                       _ptr(status), table_stride, batch, total_rows, max_rows, mask_words, q_stride, kv_stride, sm_scale)
+    c = cfg.c()
+    _check(lib().mepic_attn_tree_fp8(C.byref(c), C.byref(a), _ptr(k_scales), _ptr(v_scales), _stream_ptr(stream)))
+
+
+def mepic_tree_accept(*, parent, row_offsets, draft, target, root, n_accept, accept_rows, next_token, status, batch: int,
+                      total_rows: int, max_accept: int, stream=None) -> None:
+    a = _TreeAcceptArgsC(_ptr(parent), _ptr(row_offsets), _ptr(draft), _ptr(target), _ptr(root), _ptr(n_accept), _ptr(accept_rows),
+                         _ptr(next_token), _ptr(status), batch, total_rows, max_accept)
+    _check(lib().mepic_tree_accept(C.byref(a), _stream_ptr(stream)))
+
+
+def mepic_step_tables(cfg: Config, *, kv_len, n_new, page_ids, pos_base, reserve, reserve_used, row_offsets, kv_len_out, reserve_used_out,
+                      status, table_stride: int, batch: int, max_rows: int, n_reserve: int, row_slot=None, slot_map=None, q_pos=None,
+                      stream=None) -> None:
+    a = _StepTablesArgsC(_ptr(kv_len), _ptr(n_new), _ptr(page_ids), _ptr(pos_base), _ptr(reserve), _ptr(reserve_used), _ptr(row_offsets),
+                         _ptr(row_slot), _ptr(slot_map), _ptr(kv_len_out), _ptr(q_pos), _ptr(reserve_used_out), _ptr(status),
+                         table_stride, batch, max_rows, n_reserve)
+    c = cfg.c()
+    _check(lib().mepic_step_tables(C.byref(c), C.byref(a), _stream_ptr(stream)))
+
+
+def mepic_rows_commit(cfg: Config, *, k_new, v_new, row_offsets, slot_map, k_pool, v_pool, status, batch: int, max_rows: int,
+                      n_sources: int, src_rows=None, src_stride: int = 0, kv_stride: int = 0, stream=None) -> None:
+    a = _RowsCommitArgsC(_ptr(k_new), _ptr(v_new), _ptr(row_offsets), _ptr(slot_map), _ptr(src_rows), _ptr(k_pool), _ptr(v_pool),
+                         _ptr(status), src_stride, batch, max_rows, n_sources, kv_stride)
+    c = cfg.c()
+    _check(lib().mepic_rows_commit(C.byref(c), C.byref(a), _stream_ptr(stream)))
+
+
+def mepic_rows_commit_fp8(cfg: Config, *, k_new, v_new, row_offsets, slot_map, k_pool, v_pool, k_scales, v_scales, status, batch: int,
+                          max_rows: int, n_sources: int, src_rows=None, src_stride: int = 0, kv_stride: int = 0, stream=None) -> None:
+    """mepic_rows_commit into 8-bit pools: k_pool / v_pool are e4m3 codes, k_scales / v_scales their scales (written too)."""
+    a = _RowsCommitArgsC(_ptr(k_new), _ptr(v_new), _ptr(row_offsets), _ptr(slot_map), _ptr(src_rows), _ptr(k_pool), _ptr(v_pool),
+                         _ptr(status), src_stride, batch, max_rows, n_sources, kv_stride)
+    c = cfg.c()
+    _check(lib().mepic_rows_commit_fp8(C.byref(c), C.byref(a), _ptr(k_scales), _ptr(v_scales), _stream_ptr(stream)))

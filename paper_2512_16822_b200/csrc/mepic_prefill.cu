@@ -248,12 +248,6 @@ __global__ void __launch_bounds__(kCommitRows * 32) mepic_prefill_commit(const P
 // it writes there (largest non-NaN magnitude / 448, 1 if zero); otherwise the call appends, the block keeps its scale
 // and the codes saturate.  One CTA per new row; the first row of each run of rows that share a page does the run's work
 // (a request's slots ascend, so a page's rows are neighbours), the others leave at once.
-__device__ __forceinline__ uint32_t e4m3x4_of(float a, float b, float c, float d) {     // byte i = element i
-  uint16_t lo, hi;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
-  return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
-}
 __global__ void __launch_bounds__(256) mepic_prefill_commit_fp8(const PrefillParams p, int head_dim) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int row = blockIdx.x;

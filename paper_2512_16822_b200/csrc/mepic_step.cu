@@ -1,0 +1,459 @@
+// The integer side of a step with drafted tokens, and the commit of its rows: layout of the trees, acceptance, block tables
+// and slot maps from lengths, K/V rows into their physical slots (see "drafted tokens" in mepic.h).
+//
+// The first three move kilobytes: what they cost is launch latency plus one chain of dependent loads, so each is ONE launch,
+// reads its inputs once, side by side, and does everything that depends on them in shared memory.  The commit is a copy.
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "mepic.h"
+#include "mepic_internal.h"
+#include "mepic_ptx.cuh"
+#include "mepic_rows.cuh"
+
+namespace {
+
+using namespace mepic_dev;
+
+// ---------------------------------------------------------------- tree layout
+// One CTA per request.  The parents sit in shared memory; a thread per row walks up its chain of ancestors.  Parents precede
+// their rows, so a walk meets its ancestors in descending order and fills the row's mask words from the last one down, a
+// word at a time, without holding the mask.  The walk is depth x one shared-memory load (~30 cycles).
+constexpr int kLayoutThreads = 256;
+__global__ void __launch_bounds__(kLayoutThreads) mepic_tree_layout_kernel(const mepic_tree_layout_args_t a, int page_shift) {
+  __shared__ int16_t up[MEPIC_TREE_MAX_ROWS];
+  const int b = blockIdx.x, cap = 32 * a.mask_words;
+  const RowRange rr = rows_of(a.row_offsets, b, a.total_rows, 0x7fffffff);
+  const int n = min(rr.n, cap);
+  bool bad = rr.bad || rr.n > cap;
+  int kvl = __ldg(a.kv_len + b);
+  for (int i = threadIdx.x; i < n; i += kLayoutThreads) {
+    int p = __ldg(a.parent + rr.lo + i);
+    if (p < -1 || p >= i) { bad = true; p = -1; }
+    up[i] = static_cast<int16_t>(p);
+  }
+  if (bad) atomicOr(a.status, MEPIC_DEV_BAD_TREE);
+  const long long room = static_cast<long long>(a.table_stride) << page_shift;
+  if (kvl < 0 || kvl > room) {
+    if (threadIdx.x == 0) atomicOr(a.status, MEPIC_DEV_BAD_SLOT);
+    kvl = kvl < 0 ? 0 : static_cast<int>(room);
+  }
+  int next = 0;
+  if (kvl > 0) next = __ldg(a.pos_base + static_cast<size_t>(b) * a.table_stride + ((kvl - 1) >> page_shift)) + ((kvl - 1) & ((1 << page_shift) - 1)) + 1;
+  __syncthreads();
+  for (int i = threadIdx.x; i < rr.n; i += kLayoutThreads) {
+    int32_t* words = a.tree_mask + static_cast<size_t>(rr.lo + i) * a.mask_words;
+    int depth = 0, at = a.mask_words - 1;      // mask word being filled
+    uint32_t acc = 0;
+    if (i < n) {
+      for (int j = i; j >= 0; j = up[j]) {
+        const int w = j >> 5;
+        while (at > w) { words[at--] = static_cast<int32_t>(acc); acc = 0; }
+        acc |= 1u << (j & 31);
+        ++depth;
+      }
+      --depth;
+    }
+    while (at >= 0) { words[at--] = static_cast<int32_t>(acc); acc = 0; }
+    a.row_pos[rr.lo + i] = next + depth;
+  }
+}
+
+// ---------------------------------------------------------------- acceptance
+// One CTA per request.  Whether a row fits (its draft is the choice made at its parent) does not depend on the path, so all
+// rows are tested at once and each parent keeps its first fitting child (a minimum: no order of the atomics changes it);
+// the path is then a walk down those children in shared memory.
+constexpr int kAcceptThreads = 128;
+__global__ void __launch_bounds__(kAcceptThreads) mepic_tree_accept_kernel(const mepic_tree_accept_args_t a) {
+  __shared__ int child[MEPIC_TREE_MAX_ROWS + 1];       // [0]: of the context, [i + 1]: of row i
+  __shared__ int target[MEPIC_TREE_MAX_ROWS];
+  __shared__ int path[MEPIC_TREE_MAX_ROWS];
+  __shared__ int path_n;
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const RowRange rr = rows_of(a.row_offsets, b, a.total_rows, MEPIC_TREE_MAX_ROWS);
+  bool bad = rr.bad;
+  const int root = __ldg(a.root + b);
+  for (int i = tid; i <= rr.n; i += kAcceptThreads) {
+    child[i] = 0x7fffffff;
+    if (i < rr.n) target[i] = __ldg(a.target + rr.lo + i);
+  }
+  __syncthreads();
+  for (int i = tid; i < rr.n; i += kAcceptThreads) {
+    const int p = __ldg(a.parent + rr.lo + i), d = __ldg(a.draft + rr.lo + i);
+    if (p < -1 || p >= i) { bad = true; continue; }
+    if (d == (p < 0 ? root : target[p])) atomicMin(&child[p + 1], i);
+  }
+  if (bad) atomicOr(a.status, MEPIC_DEV_BAD_TREE);
+  __syncthreads();
+  if (tid == 0) {
+    int n = 0, at = child[0];
+    while (at != 0x7fffffff && n < a.max_accept) { path[n++] = at; at = child[at + 1]; }      // children follow their parents: at most rr.n steps
+    path_n = n;
+    a.n_accept[b] = n;
+    a.next_token[b] = n > 0 ? target[path[n - 1]] : root;
+  }
+  __syncthreads();
+  const int n = path_n;
+  for (int k = tid; k < a.max_accept; k += kAcceptThreads)
+    a.accept_rows[static_cast<size_t>(b) * a.max_accept + k] = k < n ? rr.lo + path[k] : -1;
+}
+
+// ---------------------------------------------------------------- step tables
+// Every CTA scans all requests' lengths (a few kilobytes out of L2) and keeps the running sums of rows and new pages in
+// shared memory; it then writes its share of the outputs, which all follow from those sums, by binary search.  No CTA reads
+// what another writes: an appended row's page comes from the table only where the entry existed before the call.
+constexpr int kTablesThreads = 512;
+__device__ __forceinline__ int find_request(const int* off, int batch, int r) {       // the b with off[b] <= r < off[b + 1]
+  int lo = 0, hi = batch;                       // off[lo] <= r < off[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (off[mid] <= r) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+__global__ void __launch_bounds__(kTablesThreads) mepic_step_tables_kernel(const mepic_step_tables_args_t a, int page_shift, int num_pages) {
+  extern __shared__ int sh[];
+  int* row_off = sh;                            // [batch + 1]
+  int* page_off = sh + a.batch + 1;             // [batch + 1]
+  __shared__ long long warp_rows[kTablesThreads / 32], warp_pages[kTablesThreads / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int P = 1 << page_shift;
+  const long long room = static_cast<long long>(a.table_stride) << page_shift;
+  const int used = __ldg(a.reserve_used);
+  // ---- sums: a thread owns `per` consecutive requests
+  const int per = (a.batch + kTablesThreads - 1) / kTablesThreads, b0 = min(tid * per, a.batch), b1 = min(b0 + per, a.batch);
+  long long rows = 0, pages = 0;
+  bool bad = used < 0;
+  for (int b = b0; b < b1; ++b) {
+    const long long kv = __ldg(a.kv_len + b), nn = __ldg(a.n_new + b);
+    if (kv < 0 || nn < 0 || kv + nn > room) { bad = true; continue; }
+    rows += nn;
+    pages += ((kv + nn + P - 1) >> page_shift) - ((kv + P - 1) >> page_shift);
+  }
+  long long r_in = rows, p_in = pages;          // inclusive over the warp
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long r = __shfl_up_sync(kFull, r_in, d), p = __shfl_up_sync(kFull, p_in, d);
+    if (lane >= d) { r_in += r; p_in += p; }
+  }
+  if (lane == 31) { warp_rows[warp] = r_in; warp_pages[warp] = p_in; }
+  bad = __syncthreads_or(bad) != 0;
+  long long r_at = r_in - rows, p_at = p_in - pages, r_all = 0, p_all = 0;
+#pragma unroll
+  for (int w = 0; w < kTablesThreads / 32; ++w) {
+    if (w < warp) { r_at += warp_rows[w]; p_at += warp_pages[w]; }
+    r_all += warp_rows[w]; p_all += warp_pages[w];
+  }
+  bad = bad || r_all > a.max_rows || used + p_all > a.n_reserve;        // the same answer in every thread of every CTA
+  for (int b = b0; b < b1; ++b) {
+    row_off[b] = bad ? 0 : static_cast<int>(r_at);
+    page_off[b] = bad ? 0 : static_cast<int>(p_at);
+    if (bad) continue;
+    const long long kv = __ldg(a.kv_len + b), nn = __ldg(a.n_new + b);
+    r_at += nn;
+    p_at += ((kv + nn + P - 1) >> page_shift) - ((kv + P - 1) >> page_shift);
+  }
+  if (tid == 0) { row_off[a.batch] = bad ? 0 : static_cast<int>(r_all); page_off[a.batch] = bad ? 0 : static_cast<int>(p_all); }
+  __syncthreads();
+  const int n_rows = row_off[a.batch], n_pages = page_off[a.batch];
+  const int gid = blockIdx.x * kTablesThreads + tid, step = gridDim.x * kTablesThreads;
+  if (gid == 0) {
+    if (bad) atomicOr(a.status, MEPIC_DEV_NO_PAGES);
+    *a.reserve_used_out = used + n_pages;
+    a.row_offsets[a.batch] = n_rows;
+  }
+  // ---- per request
+  for (int b = gid; b < a.batch; b += step) {
+    const int kv = __ldg(a.kv_len + b), end = kv + (row_off[b + 1] - row_off[b]);
+    a.row_offsets[b] = row_off[b];
+    a.kv_len_out[b] = end;
+    if (a.q_pos) {
+      int pos = -1;
+      if (end > 0 && end <= room) {
+        const int held = (kv + P - 1) >> page_shift, e = (end - 1) >> page_shift;
+        const int32_t* base = a.pos_base + static_cast<size_t>(b) * a.table_stride;
+        pos = (e < held ? base[e] : (held > 0 ? base[held - 1] + (e - held + 1) * P : e * P)) + ((end - 1) & (P - 1));
+      }
+      a.q_pos[b] = pos;
+    }
+  }
+  // ---- per new table entry
+  for (int t = gid; t < n_pages; t += step) {
+    const int b = find_request(page_off, a.batch, t);
+    const int held = (__ldg(a.kv_len + b) + P - 1) >> page_shift, k = t - page_off[b];
+    const int page = __ldg(a.reserve + used + t);
+    if (static_cast<unsigned>(page) >= static_cast<unsigned>(num_pages)) atomicOr(a.status, MEPIC_DEV_BAD_PAGE);
+    const size_t row = static_cast<size_t>(b) * a.table_stride;
+    a.page_ids[row + held + k] = page;
+    a.pos_base[row + held + k] = held > 0 ? a.pos_base[row + held - 1] + (k + 1) * P : k * P;
+  }
+  // ---- per appended row
+  if (!a.row_slot && !a.slot_map) return;
+  for (int r = gid; r < a.max_rows; r += step) {
+    int slot = -1;
+    long long phys = -1;
+    if (r < n_rows) {
+      const int b = find_request(row_off, a.batch, r);
+      const int kv = __ldg(a.kv_len + b), held = (kv + P - 1) >> page_shift;
+      slot = kv + r - row_off[b];
+      const int e = slot >> page_shift;
+      const int page = e < held ? a.page_ids[static_cast<size_t>(b) * a.table_stride + e] : __ldg(a.reserve + used + page_off[b] + e - held);
+      if (static_cast<unsigned>(page) < static_cast<unsigned>(num_pages)) phys = (static_cast<long long>(page) << page_shift) + (slot & (P - 1));
+      else atomicOr(a.status, MEPIC_DEV_BAD_PAGE);
+    }
+    if (a.row_slot) a.row_slot[r] = slot;
+    if (a.slot_map) a.slot_map[r] = phys;
+  }
+}
+
+// ---------------------------------------------------------------- commit of rows
+struct CommitParams {
+  const uint16_t* src[2];      // K, V
+  void* pool[2];
+  float* scales[2];
+  const int32_t* row_offsets;
+  const int64_t* slot_map;
+  const int32_t* src_rows;
+  int32_t* status;
+  int src_stride, batch, max_rows, n_sources, kv_stride, n_kv_heads, page_size, page_shift;
+  long long n_slots;           // num_pages * page_size
+};
+
+// Where appended row r comes from: the row itself, or the entry of src_rows that belongs to it.  -1: nowhere (reported).
+// Called by a whole warp for one row.  The request is found 32 candidates at a time (the offsets ascend).
+__device__ __forceinline__ int source_of(const CommitParams& p, int r, int lane) {
+  int src = r;
+  if (p.src_rows) {
+    int lo = 0, n = p.batch;                    // the request is in [lo, lo + n)
+    while (n > 1) {
+      const int step = (n + 31) / 32, at = lo + lane * step;
+      const bool below = lane * step < n && __ldg(p.row_offsets + at) <= r;
+      const int k = 31 - __clz(__ballot_sync(kFull, below) | 1u);
+      n = min(step, lo + n - (lo + k * step));
+      lo += k * step;
+    }
+    const int k = r - __ldg(p.row_offsets + lo);
+    src = k >= 0 && k < p.src_stride ? __ldg(p.src_rows + static_cast<size_t>(lo) * p.src_stride + k) : -1;
+  }
+  if (src < 0 || src >= p.n_sources) {
+    if (lane == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
+    return -1;
+  }
+  return src;
+}
+
+constexpr int kCopyRows = 8;         // rows per CTA, one warp each
+template <int D>
+__global__ void __launch_bounds__(kCopyRows * 32) mepic_rows_commit_kernel(const CommitParams p) {
+  constexpr int C = D / 8;           // 16-byte chunks per head row
+  const int lane = threadIdx.x & 31, r = blockIdx.x * kCopyRows + (threadIdx.x >> 5);
+  const int n_rows = __ldg(p.row_offsets + p.batch);
+  if (n_rows > p.max_rows && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
+  if (r >= min(n_rows, p.max_rows)) return;
+  const long long slot = __ldg(reinterpret_cast<const long long*>(p.slot_map) + r);
+  const int src = source_of(p, r, lane);
+  if (src < 0) return;
+  if (slot < 0 || slot >= p.n_slots) { if (lane == 0) atomicOr(p.status, MEPIC_DEV_BAD_PAGE); return; }
+  const int page = static_cast<int>(slot >> p.page_shift), in_page = static_cast<int>(slot) & (p.page_size - 1);
+  const size_t from = static_cast<size_t>(src) * p.kv_stride;
+  for (int c = lane; c < p.n_kv_heads * C; c += 32) {
+    const int h = c / C, cc = c % C;
+    const size_t to = ((static_cast<size_t>(page) * p.n_kv_heads + h) * p.page_size + in_page) * D + 8 * cc;
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.pool[w]) + to) = *reinterpret_cast<const uint4*>(p.src[w] + from + static_cast<size_t>(c) * 8);
+  }
+}
+
+// 8-bit pages.  A CTA looks at kRunRows consecutive rows and does the runs (rows that go to one page) that START among
+// them, whole; each of its warps takes one (pool, kv head) of a run at a time, so a block's maximum, scale and codes stay
+// in one warp.  (A CTA per row left 15 of 16 CTAs of a prompt with nothing to do.)
+constexpr int kRunRows = 16;
+constexpr int kRunWarps = 16;
+__global__ void __launch_bounds__(kRunWarps * 32) mepic_rows_commit_fp8_kernel(const CommitParams p) {
+  constexpr int D = 128;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int r0 = blockIdx.x * kRunRows;
+  const int all = __ldg(p.row_offsets + p.batch), n_rows = min(all, p.max_rows);
+  if (all > p.max_rows && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
+  if (r0 >= n_rows) return;
+  const long long* slots = reinterpret_cast<const long long*>(p.slot_map);
+  auto page_of = [&](int r) -> int {
+    const long long s = __ldg(slots + r);
+    return s < 0 || s >= p.n_slots ? -1 : static_cast<int>(s >> p.page_shift);
+  };
+  // rows of this CTA that start a run
+  bool starts = false;
+  if (lane < kRunRows && r0 + lane < n_rows) {
+    const int mine = page_of(r0 + lane);
+    if (mine < 0) { if (warp == 0) atomicOr(p.status, MEPIC_DEV_BAD_PAGE); }
+    else starts = r0 + lane == 0 || page_of(r0 + lane - 1) != mine;
+  }
+  for (unsigned todo = __ballot_sync(kFull, starts); todo; todo &= todo - 1) {
+    const int first = r0 + __ffs(todo) - 1;
+    const int page = page_of(first);
+    // length of the run and whether it writes in-page slot 0, 32 rows at a time; lane k keeps rows first + k + 32 j
+    int n = 0;
+    bool fresh = false;
+    for (bool more = true; more;) {
+      const int r = first + n + lane;
+      const bool in = r < n_rows && n + lane < p.page_size && page_of(r) == page;
+      const unsigned m = __ballot_sync(kFull, in);
+      const int got = m == kFull ? 32 : __ffs(~m) - 1;
+      fresh = fresh || __any_sync(kFull, lane < got && (__ldg(slots + r) & (p.page_size - 1)) == 0);
+      n += got;
+      more = got == 32;
+    }
+    for (int unit = warp; unit < 2 * p.n_kv_heads; unit += kRunWarps) {
+      const int w = unit & 1, h = unit >> 1;
+      const size_t block = static_cast<size_t>(page) * p.n_kv_heads + h;
+      // half a warp takes a row: lane & 15 is the 16-byte chunk of 8 elements
+      const int half = lane >> 4, cc = lane & 15;
+      float sc;
+      if (fresh) {
+        float amax = 0.f;
+        for (int k = 0; k < n; k += 2) {
+          const int s0 = source_of(p, first + k, lane), s1 = k + 1 < n ? source_of(p, first + k + 1, lane) : -1;
+          const int src = half ? s1 : s0;
+          if (src < 0) continue;
+          const uint4 v = *reinterpret_cast<const uint4*>(p.src[w] + static_cast<size_t>(src) * p.kv_stride + h * D + 8 * cc);
+          const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 f = bf16x2_to_float2(ww[j]);
+            amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));       // fmaxf drops NaN operands: a NaN element does not set the scale
+          }
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(kFull, amax, d));
+        sc = amax > 0.f ? __fdiv_rn(amax, 448.f) : 1.f;
+        if (lane == 0) p.scales[w][block] = sc;
+      } else {
+        sc = p.scales[w][block];
+      }
+      for (int k = 0; k < n; k += 2) {
+        const int s0 = source_of(p, first + k, lane), s1 = k + 1 < n ? source_of(p, first + k + 1, lane) : -1;
+        const int src = half ? s1 : s0;
+        if (src < 0) continue;
+        const uint4 v = *reinterpret_cast<const uint4*>(p.src[w] + static_cast<size_t>(src) * p.kv_stride + h * D + 8 * cc);
+        const float2 f0 = bf16x2_to_float2(v.x), f1 = bf16x2_to_float2(v.y), f2 = bf16x2_to_float2(v.z), f3 = bf16x2_to_float2(v.w);
+        uint2 out;
+        out.x = e4m3x4_of(__fdiv_rn(f0.x, sc), __fdiv_rn(f0.y, sc), __fdiv_rn(f1.x, sc), __fdiv_rn(f1.y, sc));
+        out.y = e4m3x4_of(__fdiv_rn(f2.x, sc), __fdiv_rn(f2.y, sc), __fdiv_rn(f3.x, sc), __fdiv_rn(f3.y, sc));
+        const int in_page = static_cast<int>(__ldg(slots + first + k + half)) & (p.page_size - 1);
+        *reinterpret_cast<uint2*>(static_cast<unsigned char*>(p.pool[w]) + (block * p.page_size + in_page) * D + 8 * cc) = out;
+      }
+    }
+  }
+}
+
+int shift_of(int page_size) {
+  int s = 0;
+  while ((1 << s) < page_size) ++s;
+  return s;
+}
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+int32_t launched(const char* what, int n = 1) {
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) { mepic_set_error("%s: launch: %s", what, cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  mepic_count_launches(n);
+  return MEPIC_OK;
+}
+
+int32_t commit_call(const mepic_config_t* cfg, const mepic_rows_commit_args_t* a, float* k_scales, float* v_scales, bool fp8, void* cuda_stream) {
+  const char* what = fp8 ? "rows_commit_fp8" : "rows_commit";
+  if (!mepic_config_ok(cfg)) return MEPIC_E_INVAL;
+  if (!a) { mepic_set_error("%s: NULL argument", what); return MEPIC_E_INVAL; }
+  if (fp8 && cfg->head_dim != 128) { mepic_set_error("%s: head_dim %d: 8-bit pages are built for head_dim 128", what, cfg->head_dim); return MEPIC_E_INVAL; }
+  if (a->batch < 1 || a->max_rows < 0 || a->n_sources < 0) { mepic_set_error("%s: batch must be positive, max_rows and n_sources not negative", what); return MEPIC_E_INVAL; }
+  const long long packed = static_cast<long long>(cfg->n_kv_heads) * cfg->head_dim;
+  const long long stride = a->kv_stride ? a->kv_stride : packed;
+  if (packed > 0x7fffffffLL || stride < packed || stride % 8) {
+    mepic_set_error("%s: kv_stride %d must be 0 or a multiple of 8 of at least n_kv_heads * head_dim", what, a->kv_stride); return MEPIC_E_INVAL;
+  }
+  if (a->max_rows == 0) return MEPIC_OK;
+  if (!a->k_new || !a->v_new || !a->row_offsets || !a->slot_map || !a->k_pool || !a->v_pool || !a->status) {
+    mepic_set_error("%s: NULL pointer argument", what); return MEPIC_E_INVAL;
+  }
+  if (a->src_rows && a->src_stride < 1) { mepic_set_error("%s: src_stride must be positive", what); return MEPIC_E_INVAL; }
+  if (fp8 && (!k_scales || !v_scales)) { mepic_set_error("%s: NULL scale pointer", what); return MEPIC_E_INVAL; }
+  if (!aligned(a->k_new, 16) || !aligned(a->v_new, 16) || !aligned(a->k_pool, 16) || !aligned(a->v_pool, 16) || !aligned(a->slot_map, 8)) {
+    mepic_set_error("%s: rows and pools must be 16-byte aligned, slot_map 8-byte aligned", what); return MEPIC_E_INVAL;
+  }
+  CommitParams p;
+  p.src[0] = static_cast<const uint16_t*>(a->k_new); p.src[1] = static_cast<const uint16_t*>(a->v_new);
+  p.pool[0] = a->k_pool; p.pool[1] = a->v_pool;
+  p.scales[0] = k_scales; p.scales[1] = v_scales;
+  p.row_offsets = a->row_offsets; p.slot_map = a->slot_map; p.src_rows = a->src_rows; p.status = a->status;
+  p.src_stride = a->src_stride; p.batch = a->batch; p.max_rows = a->max_rows; p.n_sources = a->n_sources;
+  p.kv_stride = static_cast<int>(stride); p.n_kv_heads = cfg->n_kv_heads; p.page_size = cfg->page_size;
+  p.page_shift = shift_of(cfg->page_size);
+  p.n_slots = static_cast<long long>(cfg->num_pages) * cfg->page_size;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (fp8) mepic_rows_commit_fp8_kernel<<<(a->max_rows + kRunRows - 1) / kRunRows, kRunWarps * 32, 0, st>>>(p);
+  else if (cfg->head_dim == 128) mepic_rows_commit_kernel<128><<<(a->max_rows + kCopyRows - 1) / kCopyRows, kCopyRows * 32, 0, st>>>(p);
+  else mepic_rows_commit_kernel<64><<<(a->max_rows + kCopyRows - 1) / kCopyRows, kCopyRows * 32, 0, st>>>(p);
+  return launched(what);
+}
+
+}  // namespace
+
+extern "C" int32_t mepic_tree_layout(const mepic_config_t* cfg, const mepic_tree_layout_args_t* a, void* cuda_stream) {
+  if (!mepic_config_ok(cfg)) return MEPIC_E_INVAL;
+  if (!a) { mepic_set_error("tree_layout: NULL argument"); return MEPIC_E_INVAL; }
+  if (a->batch < 1 || a->table_stride < 1 || a->total_rows < 0) { mepic_set_error("tree_layout: batch and table_stride must be positive, total_rows not negative"); return MEPIC_E_INVAL; }
+  if (a->mask_words < 1 || a->mask_words > MEPIC_TREE_MAX_ROWS / 32) {
+    mepic_set_error("tree_layout: mask_words %d not in 1..%d", a->mask_words, MEPIC_TREE_MAX_ROWS / 32); return MEPIC_E_INVAL;
+  }
+  if (a->total_rows == 0) return MEPIC_OK;
+  if (!a->parent || !a->row_offsets || !a->kv_len || !a->pos_base || !a->row_pos || !a->tree_mask || !a->status) {
+    mepic_set_error("tree_layout: NULL pointer argument"); return MEPIC_E_INVAL;
+  }
+  mepic_tree_layout_kernel<<<a->batch, kLayoutThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(*a, shift_of(cfg->page_size));
+  return launched("tree_layout");
+}
+
+extern "C" int32_t mepic_tree_accept(const mepic_tree_accept_args_t* a, void* cuda_stream) {
+  if (!a) { mepic_set_error("tree_accept: NULL argument"); return MEPIC_E_INVAL; }
+  if (a->batch < 1 || a->total_rows < 0 || a->max_accept < 1) { mepic_set_error("tree_accept: batch and max_accept must be positive, total_rows not negative"); return MEPIC_E_INVAL; }
+  if (!a->row_offsets || !a->root || !a->n_accept || !a->accept_rows || !a->next_token || !a->status ||
+      (a->total_rows > 0 && (!a->parent || !a->draft || !a->target))) {
+    mepic_set_error("tree_accept: NULL pointer argument"); return MEPIC_E_INVAL;
+  }
+  mepic_tree_accept_kernel<<<a->batch, kAcceptThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(*a);
+  return launched("tree_accept");
+}
+
+extern "C" int32_t mepic_step_tables(const mepic_config_t* cfg, const mepic_step_tables_args_t* a, void* cuda_stream) {
+  if (!mepic_config_ok(cfg)) return MEPIC_E_INVAL;
+  if (!a) { mepic_set_error("step_tables: NULL argument"); return MEPIC_E_INVAL; }
+  if (a->batch < 1 || a->batch > MEPIC_STEP_MAX_BATCH) { mepic_set_error("step_tables: batch %d not in 1..%d", a->batch, MEPIC_STEP_MAX_BATCH); return MEPIC_E_INVAL; }
+  if (a->table_stride < 1 || a->max_rows < 0 || a->n_reserve < 0) { mepic_set_error("step_tables: table_stride must be positive, max_rows and n_reserve not negative"); return MEPIC_E_INVAL; }
+  if (!a->kv_len || !a->n_new || !a->page_ids || !a->pos_base || (a->n_reserve > 0 && !a->reserve) || !a->reserve_used || !a->row_offsets ||
+      !a->kv_len_out || !a->reserve_used_out || !a->status) {
+    mepic_set_error("step_tables: NULL pointer argument"); return MEPIC_E_INVAL;
+  }
+  if (a->kv_len_out == a->kv_len || a->kv_len_out == a->n_new || a->reserve_used_out == a->reserve_used) {
+    mepic_set_error("step_tables: outputs must not overlap inputs"); return MEPIC_E_INVAL;
+  }
+  if (a->slot_map && !aligned(a->slot_map, 8)) { mepic_set_error("step_tables: slot_map must be 8-byte aligned"); return MEPIC_E_INVAL; }
+  const size_t smem = 2 * (static_cast<size_t>(a->batch) + 1) * sizeof(int);
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(mepic_step_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) { mepic_set_error("step_tables: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  }
+  const int work = std::max(a->row_slot || a->slot_map ? a->max_rows : 0, a->batch);
+  const int ctas = std::min(std::max(1, (work + 2 * kTablesThreads - 1) / (2 * kTablesThreads)), 296);
+  mepic_step_tables_kernel<<<ctas, kTablesThreads, smem, static_cast<cudaStream_t>(cuda_stream)>>>(*a, shift_of(cfg->page_size), cfg->num_pages);
+  return launched("step_tables");
+}
+
+extern "C" int32_t mepic_rows_commit(const mepic_config_t* cfg, const mepic_rows_commit_args_t* a, void* cuda_stream) {
+  return commit_call(cfg, a, nullptr, nullptr, false, cuda_stream);
+}
+extern "C" int32_t mepic_rows_commit_fp8(const mepic_config_t* cfg, const mepic_rows_commit_args_t* a, float* k_scales, float* v_scales,
+                                         void* cuda_stream) {
+  return commit_call(cfg, a, k_scales, v_scales, true, cuda_stream);
+}

@@ -5,6 +5,7 @@ asks the caller to own, moves host tables to the device and issues the calls.
 """
 from __future__ import annotations
 
+import ctypes as C
 from dataclasses import dataclass
 from typing import List, Optional, Sequence, Tuple
 
@@ -15,7 +16,8 @@ from . import (Config, Segment, Store, MEPIC_SEG_CHUNK, MEPIC_SEG_PROMPT, mepic_
                mepic_decode_plan_build, mepic_decode_plan_patch, mepic_attn_decode_grouped, mepic_attn_decode_grouped_fp8, mepic_attn_decode_grouped_workspace,
                mepic_pages_quantize, mepic_attn_decode_fp8,
                mepic_attn_decode_workspace, mepic_attn_prefill, mepic_attn_prefill_fp8, mepic_attn_prefill_workspace,
-               mepic_rope_table_fill)
+               mepic_rope_table_fill, mepic_attn_tree_workspace, lib, _check, _AttnTreeArgsC, _TreeLayoutArgsC, _TreeAcceptArgsC,
+               _StepTablesArgsC, _RowsCommitArgsC)
 
 
 @dataclass
@@ -99,8 +101,45 @@ class Device:
         self.rope = torch.from_numpy(mepic_rope_table_fill(cfg)).to(self.device)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
 
+    @classmethod
+    def over(cls, cfg: Config, k_pool: Optional[torch.Tensor] = None, v_pool: Optional[torch.Tensor] = None,
+             rope: Optional[torch.Tensor] = None, device: str = "cuda:0") -> "Device":
+        """A device whose pools (and rope table) the caller already holds on the GPU: nothing is copied.  Without a rope table
+        the library's is built."""
+        shape = (cfg.num_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
+        dev = cls.__new__(cls)
+        dev.cfg, dev.device = cfg, torch.device(device)
+        for pool in (k_pool, v_pool):
+            if pool is not None:
+                _expect(pool, "pool", torch.bfloat16, shape, dev.device)
+        dev.k_pool, dev.v_pool = k_pool, v_pool
+        if rope is None:
+            rope = torch.from_numpy(mepic_rope_table_fill(cfg)).to(dev.device)
+        dev.rope = _expect(rope, "rope", torch.float32, (cfg.max_position + 1, cfg.head_dim // 2, 2), dev.device)
+        dev.status = torch.zeros(1, dtype=torch.int32, device=dev.device)
+        return dev
+
     def read_status(self) -> int:
         return int(self.status.item())
+
+
+def _expect(t: torch.Tensor, name: str, dtype: torch.dtype, shape, device: torch.device) -> torch.Tensor:
+    """``t`` if it is a packed tensor of that type, shape and device (-1 in ``shape``: any size); raises ValueError otherwise."""
+    same_device = t.device.type == device.type and (device.index is None or t.device.index == device.index)
+    if t.dtype != dtype or not same_device or t.dim() != len(shape) or any(w >= 0 and g != w for g, w in zip(t.shape, shape)):
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+    return t
+
+
+def _row_stride(t: torch.Tensor, name: str, heads: int, head_dim: int, device: torch.device) -> int:
+    """Row stride in elements of bf16 rows [rows, heads, head_dim] whose rows are packed but may lie apart."""
+    if t.dtype != torch.bfloat16 or t.device.type != device.type or t.dim() != 3 or t.shape[1:] != (heads, head_dim):
+        raise ValueError(f"{name}: expected bfloat16 [rows, {heads}, {head_dim}] on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
+        raise ValueError(f"{name}: the heads of a row must be packed")
+    return t.stride(0) if t.shape[0] > 1 else heads * head_dim
 
 
 class DecodeBatch:
@@ -173,6 +212,16 @@ class Fp8Pools:
         self.v_scales = torch.ones((cfg.num_pages, cfg.n_kv_heads), dtype=torch.float32, device=d)
         if dev.k_pool is not None:                     # pools without a bf16 original start empty: prefill fills them
             self.quantize(np.arange(cfg.num_pages, dtype=np.int32) if pages is None else pages)
+
+    @classmethod
+    def over(cls, dev: Device, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor) -> "Fp8Pools":
+        """8-bit pools the caller already holds: nothing is copied or quantised."""
+        cfg, pools = dev.cfg, cls.__new__(cls)
+        shape = (cfg.num_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
+        pools.dev = dev
+        pools.k_codes, pools.v_codes = (_expect(t, "codes", torch.uint8, shape, dev.device) for t in (k_codes, v_codes))
+        pools.k_scales, pools.v_scales = (_expect(t, "scales", torch.float32, shape[:2], dev.device) for t in (k_scales, v_scales))
+        return pools
 
     def quantize(self, pages: np.ndarray, stream=None) -> None:
         lst = torch.from_numpy(np.ascontiguousarray(pages, dtype=np.int32)).to(self.dev.device)
@@ -324,3 +373,156 @@ class Fp8GroupedDecodeBatch(GroupedDecodeBatch):
                                       workspace_bytes=self.ws_bytes, status=self.dev.status, batch=self.batch,
                                       sm_scale=sm_scale, stream=s)
         return self.out
+
+
+class _StepCall:
+    """One call of a step over buffers that stay in place: the argument struct is filled once, ``run`` only launches, so that a
+    step costs the host a few microseconds and can be captured into a graph.  Inputs are read when the kernels run."""
+
+    def _bind(self, dev: Device, name: str, args, *, with_cfg: bool = True, extra=(), keep=()):
+        self.dev = dev
+        self._index = dev.device.index if dev.device.index is not None else torch.cuda.current_device()
+        self._args, self._cfg, self._keep = args, dev.cfg.c(), keep            # the struct holds raw addresses: keep the tensors alive
+        self._fn = getattr(lib(), name)
+        self._argv = ((C.byref(self._cfg),) if with_cfg else ()) + (C.byref(args),) + tuple(extra)
+
+    def _launch(self, stream=None) -> None:
+        if torch.cuda.current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self._launch(stream)
+        s = stream if stream is not None else torch.cuda.current_stream(self._index)
+        code = self._fn(*self._argv, s if isinstance(s, int) else s.cuda_stream)
+        if code:
+            _check(code)
+
+    def _i32(self, *shape):
+        return torch.empty(shape, dtype=torch.int32, device=self.dev.device)
+
+
+class TreeLayout(_StepCall):
+    """Positions and ancestor masks of drafted rows: run() -> dict(row_pos [rows], tree_mask [rows, mask_words])."""
+
+    def __init__(self, dev: Device, *, parent, row_offsets, kv_len, pos_base, mask_words: int):
+        self.dev, d, i32 = dev, dev.device, torch.int32
+        batch, rows = kv_len.numel(), parent.numel()
+        _expect(parent, "parent", i32, (rows,), d), _expect(row_offsets, "row_offsets", i32, (batch + 1,), d)
+        _expect(kv_len, "kv_len", i32, (batch,), d), _expect(pos_base, "pos_base", i32, (batch, -1), d)
+        self.row_pos, self.tree_mask = self._i32(rows), self._i32(rows, mask_words)
+        self._bind(dev, "mepic_tree_layout",
+                   _TreeLayoutArgsC(parent.data_ptr(), row_offsets.data_ptr(), kv_len.data_ptr(), pos_base.data_ptr(), self.row_pos.data_ptr(),
+                                    self.tree_mask.data_ptr(), dev.status.data_ptr(), pos_base.shape[1], batch, rows, mask_words),
+                   keep=(parent, row_offsets, kv_len, pos_base))
+
+    def run(self, stream=None):
+        self._launch(stream)
+        return dict(row_pos=self.row_pos, tree_mask=self.tree_mask)
+
+
+class TreeBatch(_StepCall):
+    """Attention of drafted rows over the paged context and each other.  q / k_new / v_new are bf16 [rows, heads, head_dim];
+    rows may lie apart (slices of one fused projection).  ``pools``: 8-bit pools to read instead of the device's bf16 ones."""
+
+    def __init__(self, dev: Device, *, q, k_new, v_new, row_offsets, row_pos, tree_mask, page_ids, pos_base, kv_len, max_rows: int,
+                 pools: Optional[Fp8Pools] = None):
+        cfg, d, i32 = dev.cfg, dev.device, torch.int32
+        rows, batch = q.shape[0], kv_len.numel()
+        q_stride = _row_stride(q, "q", cfg.n_q_heads, cfg.head_dim, d)
+        kv_stride = _row_stride(k_new, "k_new", cfg.n_kv_heads, cfg.head_dim, d)
+        if _row_stride(v_new, "v_new", cfg.n_kv_heads, cfg.head_dim, d) != kv_stride or k_new.shape[0] != rows or v_new.shape[0] != rows:
+            raise ValueError("k_new and v_new must have q's rows and one row stride")
+        _expect(row_offsets, "row_offsets", i32, (batch + 1,), d), _expect(row_pos, "row_pos", i32, (rows,), d)
+        _expect(tree_mask, "tree_mask", i32, (rows, -1), d), _expect(page_ids, "page_ids", i32, (batch, -1), d)
+        _expect(pos_base, "pos_base", i32, tuple(page_ids.shape), d), _expect(kv_len, "kv_len", i32, (batch,), d)
+        k_pool, v_pool = (dev.k_pool, dev.v_pool) if pools is None else (pools.k_codes, pools.v_codes)
+        with torch.cuda.device(d):
+            ws = mepic_attn_tree_workspace(cfg, max_rows)
+        self.out = torch.empty((rows, cfg.n_q_heads, cfg.head_dim), dtype=torch.bfloat16, device=d)
+        self.workspace = torch.empty(ws, dtype=torch.uint8, device=d)
+        args = _AttnTreeArgsC(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), row_offsets.data_ptr(), row_pos.data_ptr(),
+                              tree_mask.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), page_ids.data_ptr(), pos_base.data_ptr(),
+                              kv_len.data_ptr(), dev.rope.data_ptr(), self.out.data_ptr(), self.workspace.data_ptr(), ws,
+                              dev.status.data_ptr(), page_ids.shape[1], batch, rows, max_rows, tree_mask.shape[1], q_stride, kv_stride, 0.0)
+        self._bind(dev, "mepic_attn_tree" if pools is None else "mepic_attn_tree_fp8", args,
+                   extra=() if pools is None else (pools.k_scales.data_ptr(), pools.v_scales.data_ptr()),
+                   keep=(q, k_new, v_new, row_offsets, row_pos, tree_mask, page_ids, pos_base, kv_len, k_pool, v_pool, pools))
+
+    def run(self, sm_scale: float, stream=None) -> torch.Tensor:
+        self._args.sm_scale = sm_scale
+        self._launch(stream)
+        return self.out
+
+
+class TreeAccept(_StepCall):
+    """The path the model agrees with: run() -> dict(n_accept [B], accept_rows [B, max_accept], next_token [B])."""
+
+    def __init__(self, dev: Device, *, parent, row_offsets, draft, target, root, max_accept: int):
+        self.dev, d, i32 = dev, dev.device, torch.int32
+        batch, rows = root.numel(), parent.numel()
+        for t, name in ((parent, "parent"), (draft, "draft"), (target, "target")):
+            _expect(t, name, i32, (rows,), d)
+        _expect(row_offsets, "row_offsets", i32, (batch + 1,), d), _expect(root, "root", i32, (batch,), d)
+        self.n_accept, self.accept_rows, self.next_token = self._i32(batch), self._i32(batch, max_accept), self._i32(batch)
+        self._bind(dev, "mepic_tree_accept",
+                   _TreeAcceptArgsC(parent.data_ptr(), row_offsets.data_ptr(), draft.data_ptr(), target.data_ptr(), root.data_ptr(),
+                                    self.n_accept.data_ptr(), self.accept_rows.data_ptr(), self.next_token.data_ptr(),
+                                    dev.status.data_ptr(), batch, rows, max_accept),
+                   with_cfg=False, keep=(parent, row_offsets, draft, target, root))
+
+    def run(self, stream=None):
+        self._launch(stream)
+        return dict(n_accept=self.n_accept, accept_rows=self.accept_rows, next_token=self.next_token)
+
+
+class StepTables(_StepCall):
+    """Block tables and slot maps from lengths: page_ids / pos_base grow in place out of ``reserve``;
+    run() -> dict(row_offsets, row_slot, slot_map, kv_len, q_pos, reserve_used)."""
+
+    def __init__(self, dev: Device, *, kv_len, n_new, page_ids, pos_base, reserve, reserve_used, max_rows: int):
+        self.dev, d, i32 = dev, dev.device, torch.int32
+        batch = kv_len.numel()
+        _expect(kv_len, "kv_len", i32, (batch,), d), _expect(n_new, "n_new", i32, (batch,), d)
+        _expect(page_ids, "page_ids", i32, (batch, -1), d), _expect(pos_base, "pos_base", i32, tuple(page_ids.shape), d)
+        _expect(reserve, "reserve", i32, (-1,), d), _expect(reserve_used, "reserve_used", i32, (1,), d)
+        self.kv_len, self.reserve_used = kv_len, reserve_used
+        self.kv_len_out, self.q_pos, self.reserve_used_out, self.row_offsets = self._i32(batch), self._i32(batch), self._i32(1), self._i32(batch + 1)
+        self.row_slot, self.slot_map = self._i32(max_rows), torch.empty(max_rows, dtype=torch.int64, device=d)
+        self._bind(dev, "mepic_step_tables",
+                   _StepTablesArgsC(kv_len.data_ptr(), n_new.data_ptr(), page_ids.data_ptr(), pos_base.data_ptr(), reserve.data_ptr() or None,
+                                    reserve_used.data_ptr(), self.row_offsets.data_ptr(), self.row_slot.data_ptr() or None,
+                                    self.slot_map.data_ptr() or None, self.kv_len_out.data_ptr(), self.q_pos.data_ptr(),
+                                    self.reserve_used_out.data_ptr(), dev.status.data_ptr(), page_ids.shape[1], batch, max_rows, reserve.numel()),
+                   keep=(kv_len, n_new, page_ids, pos_base, reserve, reserve_used))
+
+    def run(self, stream=None):
+        self._launch(stream)
+        return dict(row_offsets=self.row_offsets, row_slot=self.row_slot, slot_map=self.slot_map, kv_len=self.kv_len_out, q_pos=self.q_pos,
+                    reserve_used=self.reserve_used_out)
+
+    def advance(self) -> None:
+        """The step's lengths and its use of the reserve become the next step's inputs (on the current stream)."""
+        self.kv_len.copy_(self.kv_len_out)
+        self.reserve_used.copy_(self.reserve_used_out)
+
+
+class RowsCommit(_StepCall):
+    """K/V rows into their physical slots.  ``src_rows`` (accept_rows of TreeAccept): which source row each appended row is."""
+
+    def __init__(self, dev: Device, *, k_new, v_new, row_offsets, slot_map, src_rows=None, pools: Optional[Fp8Pools] = None):
+        cfg, d = dev.cfg, dev.device
+        batch, max_rows = row_offsets.numel() - 1, slot_map.numel()
+        kv_stride = _row_stride(k_new, "k_new", cfg.n_kv_heads, cfg.head_dim, d)
+        if _row_stride(v_new, "v_new", cfg.n_kv_heads, cfg.head_dim, d) != kv_stride or v_new.shape[0] != k_new.shape[0]:
+            raise ValueError("k_new and v_new must have the same rows and row stride")
+        _expect(row_offsets, "row_offsets", torch.int32, (batch + 1,), d), _expect(slot_map, "slot_map", torch.int64, (max_rows,), d)
+        if src_rows is not None:
+            _expect(src_rows, "src_rows", torch.int32, (batch, -1), d)
+        k_pool, v_pool = (dev.k_pool, dev.v_pool) if pools is None else (pools.k_codes, pools.v_codes)
+        self._bind(dev, "mepic_rows_commit" if pools is None else "mepic_rows_commit_fp8",
+                   _RowsCommitArgsC(k_new.data_ptr(), v_new.data_ptr(), row_offsets.data_ptr(), slot_map.data_ptr(),
+                                    None if src_rows is None else src_rows.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+                                    dev.status.data_ptr(), 0 if src_rows is None else src_rows.shape[1], batch, max_rows, k_new.shape[0], kv_stride),
+                   extra=() if pools is None else (pools.k_scales.data_ptr(), pools.v_scales.data_ptr()),
+                   keep=(k_new, v_new, row_offsets, slot_map, src_rows, k_pool, v_pool, pools))
+
+    def run(self, stream=None) -> None:
+        self._launch(stream)
