@@ -1,20 +1,69 @@
 // Attention of a tree of drafted tokens over the paged, un-rotated context (see mepic_attn_tree in mepic.h).
 //
-// One warp per (drafted row, query head): a lane holds D / 32 dims of the head as rotation pairs (i, i + D/2), every key
-// is rotated by its row of the table as it is read, and the softmax runs online in fp32.
+// Mathematics.  An item is (request, kv head, tile of 128 / G drafted rows): its 128 query vectors (rows x the G query
+// heads of the kv head) against the request's keys, first the context's slots, then the request's drafted rows under the
+// mask.  Keys are taken 128 at a time: S = Q' K'^T, P = 2^(S - reference), O += P V, with Q' = R(row_pos) q * sm_scale *
+// log2(e) and K' = R(pos) k, a reference per row that only moves when a score lies more than 2^8 above it, and the sum of
+// P in fp32.  Q', K' and P are rounded to bf16 once each, everything else is fp32.
+//
+// What bounds it.  One key tile is 512 D bytes of K and V and 4 * 128 * 128 * D operations: with up to 128 query vectors an
+// item is bound by HBM (a tile's bytes take an SM's share of the bandwidth 1.5 us, its MMAs 0.6), beyond that items share
+// their tiles through L2 and the softmax (16 exponentials a clock) and the MMAs come level.  So one kernel shape serves all
+// sizes: a persistent CTA per SM that never lets the loads stop, and one 128-row MMA tile however few rows are live.
+//
+// Split.  The key tiles of all items lie on a line per LEVEL (level m = the m-th row tile of every request that has one);
+// the CTAs are dealt to the levels in proportion to their lines and each level's line is cut into equal pieces, one per CTA.
+// A request whose rows fill several tiles is thus read by CTAs that walk its keys side by side, which is what lets L2 serve
+// the second reader; a batch with one wide tree in it does not leave the other CTAs idle.  An item that a cut divides leaves
+// partials (reference, sum, unnormalised O), at most two per CTA, and a second kernel merges them.  Every CTA derives the
+// cut from row_offsets and kv_len, so no plan is built or uploaded and a captured call may be replayed with other lengths.
+//
+// Roles (640 threads, one CTA per SM):
+//   softmax warps : a thread per row.  Loads, rotates and stages the row's q; then per key tile the
+//                   row's 128 scores come to registers: maximum, 2^(S - reference), and back as bf16 over the scores' columns,
+//                   where the PV MMA takes P from.
+//   rotator warps : rotate the K tile in place in shared memory, fp32 arithmetic, one rounding.  They also bring the drafted
+//                   K rows (plain loads: one tile per item, at positions of their own).
+//   loader warps  : one for K, one for V; TMA boxes of 16 rows x 64 dims (128-byte swizzle) per 16-slot group, the page ids
+//                   of the tile after next fetched while the ring is full.  The V loader also clears V rows past kv_len,
+//                   brings the drafted V rows and takes non-finite elements out of them: 0 x inf would reach rows that the
+//                   mask hides them from.  The rows that do see such an element get it added in the epilogue.
+//                   Over 8-bit pages the loaders bring the codes into rings of their own (untiled bulk copies) and the
+//                   rotators widen them, K on the way through the rotation and then V; the K scales go into (cos, sin), the V
+//                   scales into P.
+//   MMA warps     : one issues S = Q' K'^T (three score buffers, each of which becomes its tile's P), one O += P V.
+// Every wait is bounded; a lost wait raises a flag that ends every role.
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <cstring>
+
 #include "mepic.h"
 #include "mepic_internal.h"
 #include "mepic_ptx.cuh"
 #include "mepic_rows.cuh"
+#include "mepic_tcgen05.cuh"
 
 namespace {
 
 using namespace mepic_dev;
+
+constexpr int kTileN = 128;                 // keys per tile
+constexpr int kBlockBytes = 128 * 128;      // one [128 rows x 64 bf16] swizzled block
+constexpr int kSoftmaxWarps = 8;             // two warpgroups: one takes the even key tiles, one the odd ones
+constexpr int kRotatorWarp0 = 8, kRotatorWarps = 8;                  // two groups of four, again even and odd tiles
+constexpr int kRotGroupWarps = 4, kRotators = kRotGroupWarps * 32;   // ... threads that share a tile
+constexpr int kKLoaderWarp = 16, kVLoaderWarp = 17, kQkWarp = 18, kPvWarp = 19;
+constexpr int kThreads = 640;
+constexpr int kTmemCols = 512;              // the scores of three tiles at 0, 128, 256 (each becomes its P), O at 384
+constexpr int kSD = 3;                      // score buffers
+constexpr uint32_t kColO = 384;
+constexpr float kRescaleThreshold = 8.f;    // move a row's reference only when a score lies more than 2^8 above it
+constexpr int kMaxLevels = MEPIC_TREE_MAX_ROWS / 16;      // 128 / G >= 16 rows per tile
+constexpr int kSlots = 2;                   // partials a CTA may leave: of the item its piece starts in the middle of, and of the one it ends in
 
 struct TreeParams {
   const uint16_t* q;
@@ -33,108 +82,1004 @@ struct TreeParams {
   const float* rope;
   uint16_t* out;
   int32_t* status;
+  int4* desc;                  // [CTAs] what the merge of the item this CTA begins is (row, rows, kv head, parts; 0 parts: nothing)
+  float2* part_ml;             // [CTAs][kSlots][128] (reference, sum)
+  float* part_o;               // [CTAs][kSlots][128][D]
   int table_stride, batch, total_rows, max_rows, mask_words, q_stride, kv_stride;
-  int n_kv_heads, page_size, page_shift, num_pages, max_position;
+  int n_kv_heads, group, page_size, page_shift, num_pages, max_position;
+  int rows_per_tile, max_levels;
   float scale_log2;
+  int spin_limit, skip_tile;   // test hooks
 };
 
-template <int D, bool FP8>
-__global__ void __launch_bounds__(128) mepic_tree_attn(const TreeParams p, int n_q_heads) {
-  constexpr int N = D / 64;                       // rotation pairs per lane: lane + 32 j
-  const int lane = threadIdx.x & 31;
-  const long long unit = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-  const int row = static_cast<int>(unit / n_q_heads), hq = static_cast<int>(unit % n_q_heads);
-  if (row >= p.total_rows) return;
-  int b = -1;
-  RowRange rr{0, 0, false};
-  for (int i = 0; i < p.batch; ++i) {
-    const RowRange ri = rows_of(p.row_offsets, i, p.total_rows, p.max_rows);
-    if (ri.bad) atomicOr(p.status, MEPIC_DEV_BAD_TREE);
-    if (b < 0 && row >= ri.lo && row < ri.lo + ri.n) { b = i; rr = ri; }
+#define TMEM_LD16(taddr, r)                                                                                          \
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" \
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),      \
+                 "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) \
+               : "r"(taddr) : "memory")
+// The rest of a wait that did not find its phase complete at once: bounded, and over when another role has raised the abort
+// flag.  Not inlined: two dozen waits, each with its loop, were a third of the kernel's code.
+__device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status, int limit) {
+#pragma unroll 1
+  for (int i = 0; i < limit; ++i) {
+    if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
+    if ((i & 255) == 255 && *abort_flag) return false;
   }
-  if (b < 0) return;
-  const int row0 = rr.lo, n_rows = rr.n, h = hq / (n_q_heads / p.n_kv_heads);
-  int kvl = p.kv_len[b];
+  *abort_flag = 1;
+  atomicOr(status, MEPIC_DEV_WAIT_EXPIRED);
+  return false;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+// ---------------------------------------------------------------- the cut
+// What a request contributes: its rows, its key tiles, the row tiles (levels) it has.
+struct Request { int row0, n, kvl, n_ctx, n_all, levels; bool bad_rows, bad_len; };
+__device__ __noinline__ Request request_of(const TreeParams& p, int b) {
+  Request r;
+  const RowRange rr = rows_of(p.row_offsets, b, p.total_rows, p.max_rows);
+  r.row0 = rr.lo; r.n = rr.n; r.bad_rows = rr.bad;
+  const int len = __ldg(p.kv_len + b);
   const long long room = static_cast<long long>(p.table_stride) << p.page_shift;
-  if (kvl < 0 || kvl > room) { atomicOr(p.status, MEPIC_DEV_BAD_SLOT); kvl = kvl < 0 ? 0 : static_cast<int>(room); }
-  auto bounded = [&](int pos) {
-    if (pos < 0 || pos > p.max_position) { atomicOr(p.status, MEPIC_DEV_BAD_POSITION); pos = pos < 0 ? 0 : p.max_position; }
-    return pos;
+  r.kvl = len < 0 ? 0 : (len > room ? static_cast<int>(room) : len);
+  r.bad_len = r.kvl != len;
+  r.n_ctx = static_cast<int>((static_cast<long long>(r.kvl) + kTileN - 1) / kTileN);
+  r.n_all = r.n_ctx + (r.n + kTileN - 1) / kTileN;
+  r.levels = (r.n + p.rows_per_tile - 1) / p.rows_per_tile;
+  return r;
+}
+
+// One CTA's piece: tiles [lo, hi) of its level's line, which has `line` tiles in `pieces` pieces; it starts at key tile t of
+// (request b, kv head h).
+struct Piece { int level, piece, pieces, b, h, t; long long lo, hi, line; };
+struct PlanScratch {
+  unsigned long long hist[kMaxLevels];
+  long long warp_sum[kThreads / 32];
+};
+__device__ __forceinline__ long long cut_at(long long line, int pieces, int k) {
+  return (line / pieces) * k + (line % pieces) * k / pieces;
+}
+// Executed by the whole CTA.
+__device__ __noinline__ void plan_piece(const TreeParams& p, PlanScratch* sh, Piece* out) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  for (int i = tid; i < kMaxLevels; i += kThreads) sh->hist[i] = 0;
+  __syncthreads();
+#pragma unroll 1
+  for (int b = tid; b < p.batch; b += kThreads) {
+    const Request r = request_of(p, b);
+    if (blockIdx.x == 0) {
+      if (r.bad_rows) atomicOr(p.status, MEPIC_DEV_BAD_TREE);
+      if (r.bad_len) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
+    }
+    if (r.levels > 0) atomicAdd(&sh->hist[r.levels - 1], static_cast<unsigned long long>(r.n_all) * p.n_kv_heads);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    long long all = 0, line = 0;
+    int used = 0;
+#pragma unroll 1
+    for (int m = p.max_levels - 1; m >= 0; --m) {
+      line += static_cast<long long>(sh->hist[m]);
+      sh->hist[m] = static_cast<unsigned long long>(line);       // now the length of level m's line
+      all += line;
+      used += line > 0;
+    }
+    Piece c{-1, 0, 0, 0, 0, 0, 0, 0, 0};
+    int cta = blockIdx.x;
+    const long long spare = static_cast<long long>(gridDim.x) - used;      // every level has one CTA, the rest go by length
+#pragma unroll 1
+    for (int m = 0; m < used; ++m) {
+      const long long len = static_cast<long long>(sh->hist[m]);
+      long long n = 1 + spare * len / all;
+      n = n < len ? n : len;                                     // no empty pieces
+      if (cta < n) {
+        c.level = m; c.piece = cta; c.pieces = static_cast<int>(n); c.line = len;
+        c.lo = cut_at(len, c.pieces, c.piece); c.hi = cut_at(len, c.pieces, c.piece + 1);
+        break;
+      }
+      cta -= static_cast<int>(n);
+    }
+    *out = c;
+  }
+  __syncthreads();
+  const int level = (*out).level;
+  const long long lo = (*out).lo;
+  if (level < 0) return;
+  long long before = 0;
+#pragma unroll 1
+  for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
+    const int b = b0 + tid;
+    long long w = 0;
+    int n_all = 1;
+    if (b < p.batch) {
+      const Request r = request_of(p, b);
+      n_all = r.n_all;
+      if (r.levels > level) w = static_cast<long long>(r.n_all) * p.n_kv_heads;
+    }
+    long long incl = w;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long up = __shfl_up_sync(kFull, incl, d);
+      if (lane >= d) incl += up;
+    }
+    if (lane == 31) sh->warp_sum[warp] = incl;
+    __syncthreads();
+    long long at = before + incl - w, chunk = 0;
+#pragma unroll
+    for (int k = 0; k < kThreads / 32; ++k) {
+      if (k < warp) at += sh->warp_sum[k];
+      chunk += sh->warp_sum[k];
+    }
+    if (at <= lo && lo < at + w) {
+      const long long off = lo - at;
+      (*out).b = b; (*out).h = static_cast<int>(off / n_all); (*out).t = static_cast<int>(off % n_all);
+    }
+    before += chunk;
+    __syncthreads();
+    if (before > lo) break;
+  }
+  __syncthreads();
+}
+
+// The segments of a piece, one per item it touches, in order.  Every role walks them for itself; what it reads again lies
+// in the nearest cache.
+struct Walk {
+  Request r;
+  long long left;
+  int b, h, t, level;
+};
+struct Segment { int t0, t1; };        // key tiles of item (walk's request, walk's h)
+__device__ __noinline__ Walk walk_of(const TreeParams& p, const Piece& c) {
+  Walk w;
+  w.level = c.level; w.left = c.hi - c.lo; w.b = c.b; w.h = c.h; w.t = c.t;
+  w.r = request_of(p, c.b);
+  return w;
+}
+__device__ __noinline__ bool next_segment(const TreeParams& p, Walk& w, Segment& s) {
+  if (w.left <= 0) return false;
+  if (w.t >= w.r.n_all) {
+    w.t = 0;
+    if (++w.h >= p.n_kv_heads) {
+      w.h = 0;
+      do {
+        if (++w.b >= p.batch) { w.left = 0; return false; }      // not reached: `left` ends first
+        w.r = request_of(p, w.b);
+      } while (w.r.levels <= w.level);
+    }
+  }
+  const int n = static_cast<int>(w.left < w.r.n_all - w.t ? w.left : w.r.n_all - w.t);
+  s.t0 = w.t; s.t1 = w.t + n;
+  w.t += n; w.left -= n;
+  return true;
+}
+
+// ---------------------------------------------------------------- attention
+// 8-bit pages: the K loader publishes the scales of a tile's blocks beside its K codes.  When it gets to tile i the rotators
+// are through with the K codes of i - 2; that tile's K stage was free, so QK^T of i - 4 was complete, so PV of i - 7 was, so
+// the softmax was through with tile i - 8.
+constexpr int kScaleRing = 8;
+struct Small {
+  float ks[2][8], vs[kScaleRing][8];
+  union {
+    PlanScratch plan;                  // before the roles begin
+    float ref[2][128];                 // [warpgroup][row] the row's reference after that warpgroup's latest tile
   };
-  auto bf = [](uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); };
-  float ql[N], qh[N], ol[N], oh[N], m = -INFINITY, l = 0.f;
-  const float2* cq = reinterpret_cast<const float2*>(p.rope) + static_cast<size_t>(bounded(p.row_pos[row])) * (D / 2);
+  float sum[2][128];                   // [warpgroup][row] its sum at an item's end
+  Piece piece;
+  uint32_t tmem;
+  int abort_flag;
+  int odd_v;                           // a drafted V row of this CTA's holds a non-finite element
+};
+template <int D, bool FP8>
+struct TreeSmem {
+  static constexpr int NB = D / 64;
+  static constexpr int kStage = NB * kBlockBytes;
+  static constexpr int KD = FP8 ? 2 : 3, VD = FP8 ? 2 : 3;       // stages of bf16 K and V tiles
+  static constexpr int CD = 2;                                   // 8-bit pages: stages of K and of V codes
+  static constexpr int kCodes = kTileN * D;
+  static constexpr int kQ = 0;                                   // Q' of the item, as the QK^T MMA reads it
+  static constexpr int kK = kQ + kStage;
+  static constexpr int kV = kK + KD * kStage;
+  static constexpr int kC = kV + VD * kStage;
+  static constexpr int kBars = kC + (FP8 ? 2 * CD * kCodes : 0);
+  static constexpr int kSmall = kBars + 424;                     // Small
+  static constexpr int kBytes = kSmall + sizeof(Small);
+};
+static_assert(TreeSmem<128, false>::kBytes <= 232448 && TreeSmem<128, true>::kBytes <= 232448, "shared memory of an SM");
+
+// barriers
+// A wait names a phase by its parity only, so a waiter must have seen the phase before complete.  Roles that take every second
+// tile have not, where the phase before belongs to the other group: those barriers come one per tile modulo 6, an even number.
+constexpr int kBarKLanded = 0, kBarSFull = 6;                          // [tile % 6]
+constexpr int kBarKReady = 12, kBarKFree = 15;                         // [stage]
+constexpr int kBarVLanded = 18, kBarVReady = 21, kBarVFree = 24;
+constexpr int kBarCFree = 27;                                          // 8-bit pages: [K codes 0, 1, V codes 0, 1]
+constexpr int kBarPFull = 31, kBarPvDone = 34;                         // [score buffer]
+constexpr int kBarQReady = 37, kBarOFree = 38;
+constexpr int kBarRef = 39, kBarItem = 47;                             // [warpgroup * 4 + warp], [warp]
+constexpr int kBarDrain = 51;                                          // [QK, PV] after a lost wait: the MMAs issued so far are done
+constexpr int kNumBars = 53;
+static_assert(kNumBars * 8 <= 424, "barrier block");
+
+// Rotates, scales and rounds half (chunks of wg) of a row's q into row r of the staged tile; a dead row is zeros.
+template <int D>
+__device__ __noinline__ void stage_q(const TreeParams& p, unsigned char* Qs, bool live, int row, int head, int wg, int r) {
+  constexpr int CH = D / 16;
+  int pos = live ? __ldg(p.row_pos + row) : 0;
+  if (pos < 0 || pos > p.max_position) { atomicOr(p.status, MEPIC_DEV_BAD_POSITION); pos = pos < 0 ? 0 : p.max_position; }
+  const uint16_t* src = p.q + static_cast<size_t>(live ? row : 0) * p.q_stride + static_cast<size_t>(head) * D;
+  const float4* cs = reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(pos) * D);
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int i = lane + 32 * j;
-    const uint16_t* q = p.q + static_cast<size_t>(row) * p.q_stride + hq * D;
-    const float lo = bf(q[i]), hi = bf(q[i + D / 2]);
-    const float2 t = cq[i];
-    ql[j] = (lo * t.x - hi * t.y) * p.scale_log2; qh[j] = (lo * t.y + hi * t.x) * p.scale_log2;
-    ol[j] = oh[j] = 0.f;
-  }
-  auto value = [&](const void* base, size_t at, float sc) {
-    if (FP8) {
-      uint32_t two;
-      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(two) : "h"(static_cast<uint16_t>(static_cast<const unsigned char*>(base)[at])));
-      return __half2float(__low2half(*reinterpret_cast<const __half2*>(&two))) * sc;
+  for (int cc = 0; cc < CH / 2; ++cc) {
+    const int c = wg * (CH / 2) + cc, lc = c, hc = CH + c;
+    uint32_t lo_w[4] = {0, 0, 0, 0}, hi_w[4] = {0, 0, 0, 0};
+    if (live) {
+      const uint4 lo = *reinterpret_cast<const uint4*>(src + 8 * c), hi = *reinterpret_cast<const uint4*>(src + D / 2 + 8 * c);
+      const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 t = __ldg(cs + 4 * c + j);              // (cos, sin) of pairs 8c + 2j and 8c + 2j + 1
+        const float2 x = bf16x2_to_float2(lw[j]), y = bf16x2_to_float2(hw[j]);
+        lo_w[j] = pack_bf16x2((x.x * t.x - y.x * t.y) * p.scale_log2, (x.y * t.z - y.y * t.w) * p.scale_log2);
+        hi_w[j] = pack_bf16x2((x.x * t.y + y.x * t.x) * p.scale_log2, (x.y * t.w + y.y * t.z) * p.scale_log2);
+      }
     }
-    return bf(static_cast<const uint16_t*>(base)[at]);
+    *reinterpret_cast<uint4*>(Qs + (lc / 8) * kBlockBytes + sw128(r, lc % 8)) = make_uint4(lo_w[0], lo_w[1], lo_w[2], lo_w[3]);
+    *reinterpret_cast<uint4*>(Qs + (hc / 8) * kBlockBytes + sw128(r, hc % 8)) = make_uint4(hi_w[0], hi_w[1], hi_w[2], hi_w[3]);
+  }
+}
+
+// V of a tile that does not end with its last key, and of drafted rows (whose stage no copy fills): zeros up to the next
+// multiple of 16 keys, which is how far the PV product goes (P is 0 there, but 0 x NaN is NaN), and the drafted rows without
+// their non-finite elements.  Eight 16-byte pieces per thread, `step` apart.
+template <int D>
+__device__ __noinline__ void mend_rows(const TreeParams& p, unsigned char* Vb, int* odd_v, bool draft, int left, int row, int h, int at, int step) {
+  constexpr int CH = D / 16, B = 8;
+  const int end = (left + 15) & ~15;
+  uint4 v[B];
+#pragma unroll
+  for (int u = 0; u < B; ++u) {
+    const int idx = at + u * step, kk = idx / (2 * CH), ch = idx % (2 * CH);
+    v[u] = make_uint4(0, 0, 0, 0);
+    if (draft && kk < left) v[u] = *reinterpret_cast<const uint4*>(p.v_new + static_cast<size_t>(row + kk) * p.kv_stride + static_cast<size_t>(h) * D + 8 * ch);
+  }
+#pragma unroll
+  for (int u = 0; u < B; ++u) {
+    const int idx = at + u * step, kk = idx / (2 * CH), ch = idx % (2 * CH);
+    if (kk >= end) break;
+    uint32_t vw[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if ((vw[j] & 0x7f80u) == 0x7f80u) { vw[j] &= 0xffff0000u; odd = true; }
+      if ((vw[j] & 0x7f800000u) == 0x7f800000u) { vw[j] &= 0x0000ffffu; odd = true; }
+    }
+    if (odd) *reinterpret_cast<volatile int*>(odd_v) = 1;
+    *reinterpret_cast<uint4*>(Vb + (ch / 8) * kBlockBytes + sw128(kk, ch % 8)) = make_uint4(vw[0], vw[1], vw[2], vw[3]);
+  }
+}
+
+template <int D, bool FP8, bool HOOKS>
+__global__ void __launch_bounds__(kThreads, 1)
+mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  using L = TreeSmem<D, FP8>;
+  constexpr int NB = L::NB, KD = L::KD, VD = L::VD, CD = L::CD;
+  constexpr int CH = D / 16;                      // (lo, hi) chunk pairs per row: chunk c pairs dims [8c, 8c+8) with [D/2+8c, ...)
+  constexpr int KPT = kTileN * CH / kRotators;    // consecutive keys a rotator thread takes
+  constexpr uint32_t kIdescQK = instr_desc(128, kTileN, 0, 0);
+  constexpr uint32_t kIdescPV = instr_desc(128, D, 0, 1);
+  constexpr uint32_t kGroupBytes = 16u * D * (FP8 ? 1u : 2u);
+
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* Qs = smem + L::kQ;
+  unsigned char* Ks = smem + L::kK;
+  unsigned char* Vs = smem + L::kV;
+  unsigned char* Kc = smem + L::kC;
+  unsigned char* Vc = Kc + CD * L::kCodes;
+  const uint32_t bar0 = smem_u32(smem + L::kBars);
+  auto BAR = [&](int which, int slot = 0) { return bar0 + static_cast<uint32_t>((which + slot) * 8); };
+  Small* sm = reinterpret_cast<Small*>(smem + L::kSmall);
+  volatile int* abort_flag = &sm->abort_flag;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int spin = HOOKS ? p.spin_limit : kSpinLimit;
+
+  if ((smem_u32(smem) & 1023u) != 0) {            // cannot happen with the alignment requested above; never run misaligned
+    if (tid == 0) atomicOr(p.status, MEPIC_DEV_WAIT_EXPIRED);
+    return;
+  }
+  if (tid == 0) {
+    for (int s = 0; s < 3; ++s) {
+      mbar_init(BAR(kBarKReady, s), kRotGroupWarps); mbar_init(BAR(kBarKFree, s), 1);
+      mbar_init(BAR(kBarVLanded, s), 1); mbar_init(BAR(kBarVReady, s), FP8 ? kRotGroupWarps : 1); mbar_init(BAR(kBarVFree, s), 1);
+      mbar_init(BAR(kBarPFull, s), 4); mbar_init(BAR(kBarPvDone, s), 1);
+    }
+    for (int s = 0; s < 4; ++s) mbar_init(BAR(kBarCFree, s), kRotGroupWarps);
+    for (int s = 0; s < 6; ++s) { mbar_init(BAR(kBarKLanded, s), 1); mbar_init(BAR(kBarSFull, s), 1); }
+    for (int s = 0; s < 8; ++s) mbar_init(BAR(kBarRef, s), 1);
+    for (int s = 0; s < 4; ++s) mbar_init(BAR(kBarItem, s), 2);
+    mbar_init(BAR(kBarQReady), kSoftmaxWarps); mbar_init(BAR(kBarOFree), kSoftmaxWarps); mbar_init(BAR(kBarDrain, 0), 1); mbar_init(BAR(kBarDrain, 1), 1);
+    sm->abort_flag = 0;
+    sm->odd_v = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+  }
+  if (warp == kPvWarp) tmem_alloc(smem_u32(&sm->tmem), kTmemCols);
+  plan_piece(p, &sm->plan, &sm->piece);
+  tc_fence_before();
+  __syncthreads();                                // barriers initialised, tensor memory allocated, the piece known
+  tc_fence_after();
+  const uint32_t tmem = sm->tmem;
+  const Piece piece = sm->piece;
+  const int G = p.group, n_q_heads = p.n_kv_heads * G;
+  const bool has_work = piece.level >= 0;
+  if (!has_work && tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+
+  // Registers by role.  The launch gives 512 x 128; the softmax warps hold a row's 128 scores and take 232, the others leave
+  // that room: 128 x 232 + 384 x 88 = 63,488 of 65,536.
+  // A wait of a whole warp; false ends the role.
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) {
+    return __all_sync(kFull, mbar_try_wait(bar, parity)) || wait_on(bar, parity, abort_flag, p.status, spin);
   };
-  auto key = [&](const float* kl, const float* kh, const float* vl, const float* vh, int pos) {
-    const float2* ck = reinterpret_cast<const float2*>(p.rope) + static_cast<size_t>(bounded(pos)) * (D / 2);
-    float s = 0.f;
+
+  if (has_work && warp < kSoftmaxWarps) {
+    // =============================================================== softmax warps: thread = row (lane of tensor memory)
+    // Warpgroup wg takes the key tiles of parity wg, so that one's exponentials run while the other waits for scores or
+    // barriers.  Both accumulate into one O and so must agree on a row's reference: it is handed from tile to tile (from the
+    // thread of a row to its twin in the other warpgroup), as soon as a tile's maximum is known.
+    const int wg = warp >> 2, wq = warp & 3, r = tid & 127;      // row of the tile: drafted row r / G, query head r % G of the kv head
+    const uint32_t t_row = tmem + (static_cast<uint32_t>(wq * 32) << 16);
+    const int row_in_tile = r / G, g = r % G;
+    Walk w = walk_of(p, piece);
+    Segment seg;
+    bool more = next_segment(p, w, seg);
+    auto put_q = [&](const Walk& a) {
+      const int at = a.level * p.rows_per_tile + row_in_tile;
+      stage_q<D>(p, Qs, row_in_tile < p.rows_per_tile && at < a.r.n, a.r.row0 + at, a.h * G + g, wg, r);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(kBarQReady));
+    };
+    put_q(w);
+    int gi = 0, item = 0;                         // key tiles and items of this CTA so far
+    bool ok = true, begun = false;
+    while (more && ok) {
+      const int n = w.r.n, n_ctx = w.r.n_ctx, n_all = w.r.n_all, kvl = w.r.kvl, h = w.h, row0 = w.r.row0;
+      const int at = w.level * p.rows_per_tile + row_in_tile;            // this thread's drafted row within the request
+      const bool live = row_in_tile < p.rows_per_tile && at < n;
+      const bool warp_live = w.level * p.rows_per_tile + (wq * 32) / G < n;
+      const int t0 = seg.t0, t1 = seg.t1;
+      float m_ref = -INFINITY, l_run = 0.f;       // reference at this warpgroup's latest tile, and its sum under it
+#pragma unroll 1
+      for (int t = t0; t < t1; ++t, ++gi) {
+        if ((gi & 1) != wg) continue;
+        const int sb = gi % kSD;
+        const uint32_t t_S = t_row + static_cast<uint32_t>(sb * 128);
+        if (!wait_warp(BAR(kBarSFull, gi % 6), static_cast<uint32_t>(gi / 6) & 1u)) { ok = false; break; }
+        tc_fence_after();
+        if (warp_live) {
+          const int left = t < n_ctx ? kvl - t * kTileN : n - (t - n_ctx) * kTileN;      // keys that exist
+          const bool masked = t >= n_ctx || left < kTileN;
+          // which of keys 32 q .. 32 q + 31 of the tile this row sees (asked only where masked)
+          auto seen = [&](int q) {
+            uint32_t m = left >= 32 * (q + 1) ? ~0u : (left <= 32 * q ? 0u : (1u << (left - 32 * q)) - 1u);
+            if (t >= n_ctx) {
+              const int wd = (t - n_ctx) * 4 + q;
+              m &= live && wd < p.mask_words ? static_cast<uint32_t>(__ldg(p.tree_mask + static_cast<size_t>(row0 + at) * p.mask_words + wd)) : 0u;
+            }
+            return m;
+          };
+          // ---- pass 1: the maximum of the row's 128 scores.  (Short loop bodies on purpose, here and in the other roles: the
+          // roles that share a scheduler run different code, and unrolled bodies - a row's scores held in registers, say - ran
+          // at a tenth of an instruction a clock out of the instruction cache.)
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            uint32_t sv[32];
+            TMEM_LD32(t_S + 32 * q, sv, 0);
+            tmem_wait_ld();
+            if (masked) {
+              const uint32_t m = seen(q);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float2 t = ck[lane + 32 * j];
-      s += ql[j] * (kl[j] * t.x - kh[j] * t.y) + qh[j] * (kl[j] * t.y + kh[j] * t.x);
+              for (int c = 0; c < 32; ++c) sv[c] = (m >> c) & 1u ? sv[c] : 0xff800000u;      // -inf
+            }
+            float m4[4] = {mx, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < 32; c += 8) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) m4[k] = max3(m4[k], __uint_as_float(sv[c + 2 * k]), __uint_as_float(sv[c + 2 * k + 1]));
+            }
+            mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+          }
+          // ---- the reference: the one the tile before left, raised to this tile's maximum if that lies more than 2^8 above
+          float m_in = -INFINITY;
+          if (t > t0) {
+            if (!wait_warp(BAR(kBarRef, (wg ^ 1) * 4 + wq), static_cast<uint32_t>((gi - 1) >> 1) & 1u)) { ok = false; break; }
+            m_in = *reinterpret_cast<volatile float*>(&sm->ref[wg ^ 1][r]);
+          }
+          const float m_now = mx > m_in + kRescaleThreshold ? mx : m_in;      // always mx on the first tile that shows the row a key
+          *reinterpret_cast<volatile float*>(&sm->ref[wg][r]) = m_now;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(BAR(kBarRef, wg * 4 + wq));
+          if (t > t0 && __any_sync(kFull, m_now != m_in)) {
+            // O holds the earlier tiles' PV: wait for the last of them, then scale the row.  (A barrier per score buffer: that
+            // this tile's scores are here means that PV of three tiles ago has completed, so the parity names one phase.)
+            if (!wait_warp(BAR(kBarPvDone, (gi - 1) % kSD), static_cast<uint32_t>((gi - 1) / kSD) & 1u)) { ok = false; break; }
+            tc_fence_after();
+            const float alpha = m_now != m_in ? ex2(m_in - m_now) : 1.f;      // 2^-inf = 0: nothing has been summed yet
+#pragma unroll 1
+            for (int cb = 0; cb < D; cb += 16) {
+              uint32_t o[16];
+              TMEM_LD16(t_row + kColO + cb, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha);
+              TMEM_ST16(t_row + kColO + cb, o);
+            }
+          }
+          if (m_now != m_ref) {                                    // this warpgroup's sum is still under its own latest reference
+            l_run *= ex2(m_ref - m_now);                           // (0 x 0 before its first tile)
+            m_ref = m_now;
+          }
+          // ---- pass 2: P = 2^(S - reference), bf16, over columns whose scores are consumed
+          const float m_use = m_now == -INFINITY ? 0.f : m_now;    // a row that has seen nothing: every score is -inf, P = 0
+          const float2 ref2 = make_float2(m_use, m_use);
+          float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            uint32_t sv[32], pw[16];
+            TMEM_LD32(t_S + 32 * q, sv, 0);
+            tmem_wait_ld();
+            if (masked) {
+              const uint32_t m = seen(q);
+#pragma unroll
+              for (int c = 0; c < 32; ++c) sv[c] = (m >> c) & 1u ? sv[c] : 0xff800000u;
+            }
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+              const float2 d0 = sub2(make_float2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), ref2);
+              const float2 d1 = sub2(make_float2(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), ref2);
+              float2 p0 = make_float2(ex2(d0.x), ex2(d0.y)), p1 = make_float2(ex2(d1.x), ex2(d1.y));
+              sum2[0] = add2(sum2[0], p0);
+              sum2[1] = add2(sum2[1], p1);
+              if constexpr (FP8) {                                 // the scale of the key's V block (1 for drafted rows)
+                const float s = sm->vs[gi % kScaleRing][2 * q + c / 16];
+                p0 = mul2(p0, make_float2(s, s)); p1 = mul2(p1, make_float2(s, s));
+              }
+              pw[c / 2] = pack_bf16x2(p0.x, p0.y);
+              pw[c / 2 + 1] = pack_bf16x2(p1.x, p1.y);
+            }
+            TMEM_ST16(t_S + 16 * q, pw);
+          }
+          l_run += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
+          tmem_wait_st();
+        } else if (lane == 0) {
+          mbar_arrive(BAR(kBarRef, wg * 4 + wq));                  // no live row: only the phases are kept
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(kBarPFull, sb));
+      }
+      if (!ok) break;
+      // ---- the item's end: the twins exchange their sums
+      const int last = gi - 1;                    // the item's last tile
+      *reinterpret_cast<volatile float*>(&sm->ref[wg][r]) = m_ref;      // (what it holds, or -inf where this warpgroup had no tile)
+      sm->sum[wg][r] = l_run;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(kBarItem, wq));
+      if (!wait_warp(BAR(kBarItem, wq), static_cast<uint32_t>(item) & 1u)) { ok = false; break; }
+      const float m_twin = *reinterpret_cast<volatile float*>(&sm->ref[wg ^ 1][r]), l_twin = *reinterpret_cast<volatile float*>(&sm->sum[wg ^ 1][r]);
+      // the next item's q is staged while this one's last PV runs; the staged q is free once the last QK^T has completed
+      if (!wait_warp(BAR(kBarSFull, last % 6), static_cast<uint32_t>(last / 6) & 1u)) { ok = false; break; }
+      Segment next;
+      const int level = w.level;
+      more = next_segment(p, w, next);
+      if (more) put_q(w);
+      // (a reference only ever rises, so the larger of the two is the one O is under)
+      const float m_end = fmaxf(m_ref, m_twin);
+      const float l_end = (m_ref == m_end ? l_run : l_run * ex2(m_ref - m_end)) + (m_twin == m_end ? l_twin : l_twin * ex2(m_twin - m_end));
+      if (!wait_warp(BAR(kBarPvDone, last % kSD), static_cast<uint32_t>(last / kSD) & 1u)) { ok = false; break; }
+      tc_fence_after();
+      const bool whole = t0 == 0 && t1 == n_all;
+      if (warp_live) {
+        // each of the twins writes half of the row's head dims
+        const size_t part = (static_cast<size_t>(blockIdx.x) * kSlots + (t0 > 0 ? 0 : 1)) * 128 + r;
+        if (!whole && live && wg == 0) p.part_ml[part] = make_float2(m_end, l_end);
+        const float inv = l_end == 0.f ? 0.f : 1.f / l_end;        // nothing seen: zeros
+        uint16_t* dst = p.out + (static_cast<size_t>(row0 + at) * n_q_heads + static_cast<size_t>(h) * G + g) * D;
+        const bool odd = *reinterpret_cast<volatile int*>(&sm->odd_v) != 0 && t1 > n_ctx;
+#pragma unroll 1
+        for (int cb = wg * (D / 2); cb < (wg + 1) * (D / 2); cb += 32) {
+          uint32_t o[32];
+          TMEM_LD32(t_row + kColO + cb, o, 0);
+          tmem_wait_ld();
+          if (odd && live) {
+            // non-finite elements of the drafted V rows this row sees (they were left out of the product): weight > 0
+#pragma unroll 1
+            for (int j = (max(t0, n_ctx) - n_ctx) * kTileN; j < min(n, (t1 - n_ctx) * kTileN); ++j) {
+              if ((j >> 5) >= p.mask_words || !((__ldg(p.tree_mask + static_cast<size_t>(row0 + at) * p.mask_words + (j >> 5)) >> (j & 31)) & 1)) continue;
+              const uint16_t* v = p.v_new + static_cast<size_t>(row0 + j) * p.kv_stride + static_cast<size_t>(h) * D + cb;
+#pragma unroll
+              for (int c = 0; c < 32; ++c) {
+                const uint32_t bits = static_cast<uint32_t>(v[c]) << 16;
+                if ((bits & 0x7f800000u) == 0x7f800000u) o[c] = __float_as_uint(__uint_as_float(o[c]) + __uint_as_float(bits));
+              }
+            }
+          }
+          if (live) {
+            if (whole) {
+#pragma unroll
+              for (int c = 0; c < 32; c += 8) {
+                uint4 x;
+                x.x = pack_bf16x2(__uint_as_float(o[c + 0]) * inv, __uint_as_float(o[c + 1]) * inv);
+                x.y = pack_bf16x2(__uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv);
+                x.z = pack_bf16x2(__uint_as_float(o[c + 4]) * inv, __uint_as_float(o[c + 5]) * inv);
+                x.w = pack_bf16x2(__uint_as_float(o[c + 6]) * inv, __uint_as_float(o[c + 7]) * inv);
+                *reinterpret_cast<uint4*>(dst + cb + c) = x;
+              }
+            } else {
+#pragma unroll
+              for (int c = 0; c < 32; c += 4) *reinterpret_cast<uint4*>(p.part_o + part * D + cb + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+            }
+          }
+        }
+      }
+      if (tid == 0 && t0 == 0 && t1 < n_all) {
+        // this CTA holds the first part of an item that goes on in the next pieces: leave the merge its description
+        const long long end = piece.hi + (n_all - t1);
+        int parts = 1;
+#pragma unroll 1
+        while (cut_at(piece.line, piece.pieces, piece.piece + parts) < end) ++parts;
+        p.desc[blockIdx.x] = make_int4(row0 + level * p.rows_per_tile, min(p.rows_per_tile, n - level * p.rows_per_tile), h, parts);
+        begun = true;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(kBarOFree));
+      ++item;
+      seg = next;
+    }
+    if (tid == 0 && !begun) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+  } else if (has_work && warp < kRotatorWarp0 + kRotatorWarps) {
+    // =============================================================== rotator warps
+    // A group of four warps takes every second tile, so that one group's fixed latencies (barriers, the table row) run behind
+    // the other's arithmetic; the table row of a group's next tile is fetched while it rotates this one.
+    const int group = (warp - kRotatorWarp0) / kRotGroupWarps;
+    const int rt = (tid - kRotatorWarp0 * 32) & (kRotators - 1);
+    const int c = rt % CH;                        // chunk pair
+    const int k0 = (rt / CH) * KPT;               // first of this thread's KPT consecutive keys (within one 16-slot group)
+    const int lc = c, hc = CH + c;
+    // constants: the rotation by the thread's offset in its group, and by one position
+    float2 oc[4], os[4], c1[4], s1[4], ns1[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 a = __ldg(reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(k0 & 15) * D + 16 * c) + j);
+      const float4 b1 = __ldg(reinterpret_cast<const float4*>(p.rope + D + 16 * c) + j);
+      oc[j] = make_float2(a.x, a.z); os[j] = make_float2(a.y, a.w);
+      c1[j] = make_float2(b1.x, b1.z); s1[j] = make_float2(b1.y, b1.w); ns1[j] = make_float2(-b1.y, -b1.w);
+    }
+    Walk w = walk_of(p, piece);
+    Segment seg;
+    int gi = 0;
+    bool ok = true;
+    while (ok && next_segment(p, w, seg)) {
+      const int n = w.r.n, n_ctx = w.r.n_ctx, kvl = w.r.kvl, row0 = w.r.row0, h = w.h;
+      const int32_t* bases = p.pos_base + static_cast<size_t>(w.b) * p.table_stride;
+      // position of the first slot of this thread's 16-slot group of tile t (0 where it has no slots), and its table row
+      auto position = [&](int t) {
+        const long long slot = static_cast<long long>(t) * kTileN + (k0 & ~15);
+        return t < n_ctx && slot < kvl ? __ldg(bases + (slot >> p.page_shift)) + (static_cast<int>(slot) & (p.page_size - 1)) : 0;
+      };
+      float4 base[4];
+      auto fetch_row = [&](int pos) {
+        if (pos < 0 || pos > p.max_position) { atomicOr(p.status, MEPIC_DEV_BAD_POSITION); pos = 0; }
+        const float4* row = reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(pos) * D + 16 * c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) base[j] = __ldg(row + j);
+      };
+      int ahead = position(seg.t0 + ((gi & 1) ^ group));           // this group's first tile of the segment, then two tiles ahead
+      fetch_row(ahead);
+      ahead = position(seg.t0 + ((gi & 1) ^ group) + 2);
+#pragma unroll 1
+      for (int t = seg.t0; t < seg.t1; ++t, ++gi) {
+        if ((gi & 1) != group) continue;
+        const int ks = gi % KD;
+        unsigned char* Kb = Ks + ks * L::kStage;
+        const bool draft = t >= n_ctx;
+        const int left = min(draft ? n - (t - n_ctx) * kTileN : kvl - t * kTileN, kTileN);       // keys that exist
+        const bool have = !draft && (k0 & ~15) < left;
+        float2 cc[4], ss[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 bc = make_float2(base[j].x, base[j].z), bs = make_float2(base[j].y, base[j].w);
+          cc[j] = sub2(mul2(oc[j], bc), mul2(os[j], bs));
+          ss[j] = fma2(os[j], bc, mul2(oc[j], bs));
+        }
+        if (t + 2 < seg.t1) {
+          fetch_row(ahead);
+          ahead = position(t + 4);
+        }
+        if (!wait_warp(BAR(kBarKLanded, gi % 6), static_cast<uint32_t>(gi / 6) & 1u)) { ok = false; break; }
+        if constexpr (FP8) {
+          // (this role fills the bf16 stage itself: every QK^T that read its previous tenant has completed.  With two stages a
+          // group always has the same one.)
+          if (gi >= KD && !wait_warp(BAR(kBarKFree, ks), static_cast<uint32_t>(gi / KD - 1) & 1u)) { ok = false; break; }
+          if (have) {
+            // codes widened exactly, the block's scale folded into (cos, sin): the one-position step is a pure rotation
+            const float sc = *reinterpret_cast<volatile float*>(&sm->ks[gi & 1][k0 >> 4]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { cc[j] = mul2(cc[j], make_float2(sc, sc)); ss[j] = mul2(ss[j], make_float2(sc, sc)); }
+            const unsigned char* codes = Kc + (gi % CD) * L::kCodes + k0 * 128 + 8 * c;
+#pragma unroll 1
+            for (int i = 0; i < KPT; ++i) {
+              const uint2 lo = *reinterpret_cast<const uint2*>(codes + i * 128), hi = *reinterpret_cast<const uint2*>(codes + i * 128 + 64);
+              uint32_t lh[4], hh[4], lo_w[4], hi_w[4];
+              e4m3x4_to_f16x2x2(lo.x, lh[0], lh[1]); e4m3x4_to_f16x2x2(lo.y, lh[2], lh[3]);
+              e4m3x4_to_f16x2x2(hi.x, hh[0], hh[1]); e4m3x4_to_f16x2x2(hi.y, hh[2], hh[3]);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lh[j])), y = __half22float2(*reinterpret_cast<const __half2*>(&hh[j]));
+                const float2 a = sub2(mul2(x, cc[j]), mul2(y, ss[j]));
+                const float2 b = fma2(x, ss[j], mul2(y, cc[j]));
+                lo_w[j] = pack_bf16x2(a.x, a.y);
+                hi_w[j] = pack_bf16x2(b.x, b.y);
+              }
+              *reinterpret_cast<uint4*>(Kb + (lc / 8) * kBlockBytes + sw128(k0 + i, lc % 8)) = make_uint4(lo_w[0], lo_w[1], lo_w[2], lo_w[3]);
+              *reinterpret_cast<uint4*>(Kb + (hc / 8) * kBlockBytes + sw128(k0 + i, hc % 8)) = make_uint4(hi_w[0], hi_w[1], hi_w[2], hi_w[3]);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float2 cn = fma2(ss[j], ns1[j], mul2(cc[j], c1[j]));
+                ss[j] = fma2(ss[j], c1[j], mul2(cc[j], s1[j]));
+                cc[j] = cn;
+              }
+            }
+          }
+        } else if (have) {
+#pragma unroll 2
+          for (int i = 0; i < KPT; ++i) {
+            uint4* plo = reinterpret_cast<uint4*>(Kb + (lc / 8) * kBlockBytes + sw128(k0 + i, lc % 8));
+            uint4* phi = reinterpret_cast<uint4*>(Kb + (hc / 8) * kBlockBytes + sw128(k0 + i, hc % 8));
+            const uint4 lo = *plo, hi = *phi;
+            const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
+            uint32_t lo_w[4], hi_w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float2 x = bf16x2_to_float2(lw[j]), y = bf16x2_to_float2(hw[j]);
+              const float2 a = sub2(mul2(x, cc[j]), mul2(y, ss[j]));                          // lo cos - hi sin
+              const float2 b = fma2(x, ss[j], mul2(y, cc[j]));                                // lo sin + hi cos
+              lo_w[j] = pack_bf16x2(a.x, a.y);
+              hi_w[j] = pack_bf16x2(b.x, b.y);
+            }
+            *plo = make_uint4(lo_w[0], lo_w[1], lo_w[2], lo_w[3]);
+            *phi = make_uint4(hi_w[0], hi_w[1], hi_w[2], hi_w[3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {          // (cos, sin)(pos + 1) = (cos, sin)(pos) x (cos, sin)(1)
+              const float2 cn = fma2(ss[j], ns1[j], mul2(cc[j], c1[j]));
+              ss[j] = fma2(ss[j], c1[j], mul2(cc[j], s1[j]));
+              cc[j] = cn;
+            }
+          }
+        }
+        if (draft) {
+          // ---- drafted rows: brought by plain loads, each at its own position, dealt to the threads one by one.  (Rows past
+          // the last keep whatever the stage holds: their scores are masked.)
+          const int first = row0 + (t - n_ctx) * kTileN;
+#pragma unroll 2
+          for (int kk = rt / CH; kk < left; kk += kRotators / CH) {
+            int at = __ldg(p.row_pos + first + kk);
+            if (at < 0 || at > p.max_position) { atomicOr(p.status, MEPIC_DEV_BAD_POSITION); at = at < 0 ? 0 : p.max_position; }
+            const uint16_t* src = p.k_new + static_cast<size_t>(first + kk) * p.kv_stride + static_cast<size_t>(h) * D + 8 * c;
+            const uint4 lo = *reinterpret_cast<const uint4*>(src), hi = *reinterpret_cast<const uint4*>(src + D / 2);
+            const float4* cs = reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(at) * D + 16 * c);
+            const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
+            uint32_t lo_w[4], hi_w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float4 b = __ldg(cs + j);
+              const float2 x = bf16x2_to_float2(lw[j]), y = bf16x2_to_float2(hw[j]);
+              lo_w[j] = pack_bf16x2(x.x * b.x - y.x * b.y, x.y * b.z - y.y * b.w);
+              hi_w[j] = pack_bf16x2(x.x * b.y + y.x * b.x, x.y * b.w + y.y * b.z);
+            }
+            *reinterpret_cast<uint4*>(Kb + (lc / 8) * kBlockBytes + sw128(kk, lc % 8)) = make_uint4(lo_w[0], lo_w[1], lo_w[2], lo_w[3]);
+            *reinterpret_cast<uint4*>(Kb + (hc / 8) * kBlockBytes + sw128(kk, hc % 8)) = make_uint4(hi_w[0], hi_w[1], hi_w[2], hi_w[3]);
+          }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(kBarKReady, ks));
+        if constexpr (FP8) {
+          // ---- 8-bit pages: the V tile too, codes widened exactly (their scale goes into P)
+          const int vst = gi % VD;
+          unsigned char* Vb = Vs + vst * L::kStage;
+          if (lane == 0) mbar_arrive(BAR(kBarCFree, gi % CD));                  // the K codes have been read
+          if (!wait_warp(BAR(kBarVLanded, gi % CD), static_cast<uint32_t>(gi / CD) & 1u)) { ok = false; break; }
+          if (gi >= VD && !wait_warp(BAR(kBarVFree, vst), static_cast<uint32_t>(gi / VD - 1) & 1u)) { ok = false; break; }
+          if (draft) {
+            for (int i0 = rt & ~31; i0 < ((left + 15) & ~15) * 2 * CH; i0 += kRotators * 8)
+              mend_rows<D>(p, Vb, &sm->odd_v, true, left, row0 + (t - n_ctx) * kTileN, h, i0 + lane, kRotators);
+          } else {
+            const unsigned char* codes = Vc + (gi % CD) * L::kCodes;
+            const int end = (left + 15) & ~15;     // the PV product goes over whole groups of 16 keys
+#pragma unroll 1
+            for (int idx = rt; idx < end * 8; idx += kRotators) {
+              const int kk = idx >> 3, c16 = idx & 7;
+              uint32_t w8[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+              if (kk < left) {
+                const uint4 cd = *reinterpret_cast<const uint4*>(codes + kk * 128 + 16 * c16);
+                const uint32_t cw[4] = {cd.x, cd.y, cd.z, cd.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  uint32_t f0, f1;
+                  e4m3x4_to_f16x2x2(cw[j], f0, f1);
+                  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&f0)), y = __half22float2(*reinterpret_cast<const __half2*>(&f1));
+                  w8[2 * j] = pack_bf16x2(x.x, x.y);
+                  w8[2 * j + 1] = pack_bf16x2(y.x, y.y);
+                }
+              }
+              const int ch = 2 * c16;
+              *reinterpret_cast<uint4*>(Vb + (ch / 8) * kBlockBytes + sw128(kk, ch % 8)) = make_uint4(w8[0], w8[1], w8[2], w8[3]);
+              *reinterpret_cast<uint4*>(Vb + (ch / 8) * kBlockBytes + sw128(kk, ch % 8 + 1)) = make_uint4(w8[4], w8[5], w8[6], w8[7]);
+            }
+          }
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(BAR(kBarVReady, vst));
+            mbar_arrive(BAR(kBarCFree, 2 + gi % CD));
+          }
+        }
+      }
+    }
+  } else if (has_work) {
+    if (warp == kKLoaderWarp || warp == kVLoaderWarp) {
+    // =============================================================== loader warps: lane g < 8 loads 16-slot group g
+    const bool is_k = warp == kKLoaderWarp;
+    const CUtensorMap* map = is_k ? &map_k : &map_v;
+    unsigned char* ring = FP8 ? (is_k ? Kc : Vc) : (is_k ? Ks : Vs);
+    constexpr int kRingStage = FP8 ? L::kCodes : L::kStage;
+    const int depth = FP8 ? CD : (is_k ? KD : VD);
+    Walk w = walk_of(p, piece);
+    Segment seg;
+    struct Next { int page, slot0, h, left, row; bool live, draft, special; float ks, vs; };      // left: keys that exist; row: first drafted row
+    auto look_up = [&](int t) {
+      const bool draft = t >= w.r.n_ctx;
+      const int left = min(draft ? w.r.n - (t - w.r.n_ctx) * kTileN : w.r.kvl - t * kTileN, kTileN);
+      Next x{0, 0, w.h, left, w.r.row0 + (t - w.r.n_ctx) * kTileN, false, draft, draft || left < kTileN, 1.f, 1.f};
+      const long long slot = static_cast<long long>(t) * kTileN + lane * 16;
+      x.live = !x.draft && lane < 8 && slot < w.r.kvl;
+      if (x.live) {
+        const size_t e = static_cast<size_t>(w.b) * p.table_stride + static_cast<size_t>(slot >> p.page_shift);
+        x.slot0 = static_cast<int>(slot) & (p.page_size - 1);
+        x.page = __ldg(p.page_ids + e);
+        if (static_cast<unsigned>(x.page) >= static_cast<unsigned>(p.num_pages)) { atomicOr(p.status, MEPIC_DEV_BAD_PAGE); x.page = 0; }
+        if (FP8 && is_k) {
+          const size_t block = static_cast<size_t>(x.page) * p.n_kv_heads + w.h;
+          x.ks = __ldg(p.k_scales + block);
+          x.vs = __ldg(p.v_scales + block);
+        }
+      }
+      return x;
+    };
+    bool more = next_segment(p, w, seg);
+    int t = seg.t0;
+    Next nx = look_up(t);
+    int gi = 0;
+#pragma unroll 1
+    while (more) {
+      Next x = nx;
+      // the page ids of the tile after this one are on their way while this one waits for room
+      if (++t >= seg.t1) { more = next_segment(p, w, seg); t = seg.t0; }
+      if (more) nx = look_up(t);
+      const int st = gi % depth;
+      if (gi >= depth && !wait_warp(FP8 ? BAR(kBarCFree, is_k ? st : 2 + st) : BAR(is_k ? kBarKFree : kBarVFree, st), static_cast<uint32_t>(gi / depth - 1) & 1u)) break;
+      const uint32_t landed = is_k ? BAR(kBarKLanded, gi % 6) : BAR(kBarVLanded, st);
+      if (FP8 && is_k && lane < 8) { sm->ks[gi & 1][lane] = x.ks; sm->vs[gi % kScaleRing][lane] = x.vs; }
+      const unsigned live = __ballot_sync(kFull, x.live);
+      if (HOOKS && is_k && blockIdx.x == 0 && gi == p.skip_tile) { ++gi; continue; }      // (test hook: a K tile that never comes)
+      if (lane == 0) {
+        if (live) mbar_expect_tx(landed, static_cast<uint32_t>(__popc(live)) * kGroupBytes);
+        else mbar_arrive(landed);                 // drafted rows: the rotators and the V loader bring them into the stage
+      }
+      __syncwarp();
+      if (x.live) {
+        const uint32_t dst = smem_u32(ring + st * kRingStage) + static_cast<uint32_t>(lane * 16 * 128);
+        if constexpr (FP8) {
+          const size_t row = (static_cast<size_t>(x.page) * p.n_kv_heads + x.h) * p.page_size + x.slot0;      // of the pool viewed as [rows][128 bytes]
+          bulk_g2s(dst, static_cast<const unsigned char*>(is_k ? p.k_pool : p.v_pool) + row * 128, kGroupBytes, landed);
+        } else {
+          const int y = (x.page * p.n_kv_heads + x.h) * p.page_size + x.slot0;       // row of the pool viewed as [rows][D]
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) tma_load_2d(dst + nb * kBlockBytes, map, nb * 64, y, landed);
+        }
+      }
+      if (!FP8 && !is_k && x.special) {
+        if (live && !wait_warp(landed, static_cast<uint32_t>(gi / depth) & 1u)) break;
+        const int end = ((x.left + 15) & ~15) * 2 * CH;
+#pragma unroll 1
+        for (int i0 = x.draft ? 0 : x.left * 2 * CH; i0 < end; i0 += 8 * 32) mend_rows<D>(p, Vs + st * L::kStage, &sm->odd_v, x.draft, x.left, x.row, x.h, i0 + lane, 32);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(kBarVReady, st));
+      }
+      ++gi;
+    }
+    // after a lost wait: give the copies started last a bounded chance to land before shared memory is given up
+    if (*abort_flag)
+      for (int j = max(0, gi - depth); j < gi; ++j)
+        for (int i = 0; i < spin && !mbar_try_wait(is_k ? BAR(kBarKLanded, j % 6) : BAR(kBarVLanded, j % depth), static_cast<uint32_t>(is_k ? j / 6 : j / depth) & 1u); ++i) {}
+    } else if (warp == kQkWarp) {
+      // =============================================================== QK^T issuer
+      // S of tile j goes to the buffer that held tile j - 3, once that tile's PV is through with it: the softmax finds the
+      // scores of its next tiles ready.  QK^T and PV are issued by a warp each: one thread's waits, issues and commits for both
+      // took 3,300 cycles a tile and held everything else up.
+      const uint64_t q_desc = smem_desc(smem_u32(Qs), 16, 1024);
+      const uint64_t k_desc0 = smem_desc(smem_u32(Ks), 16, 1024);
+      Walk w = walk_of(p, piece);
+      Segment seg;
+      bool ok = true;
+      int j = 0, items = 0;
+      while (ok && next_segment(p, w, seg)) {
+        if (!wait_warp(BAR(kBarQReady), static_cast<uint32_t>(items++) & 1u)) { ok = false; break; }
+#pragma unroll 1
+        for (int t = seg.t0; t < seg.t1; ++t, ++j) {
+          const int ks = j % KD, sb = j % kSD;
+          if (j >= kSD && !wait_warp(BAR(kBarPvDone, sb), static_cast<uint32_t>(j / kSD - 1) & 1u)) { ok = false; break; }
+          if (!wait_warp(BAR(kBarKReady, ks), static_cast<uint32_t>(j / KD) & 1u)) { ok = false; break; }
+          tc_fence_after();
+          if (lane == 0) {
+            const uint64_t kd = k_desc0 + static_cast<uint64_t>(ks) * (L::kStage >> 4);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+              const uint64_t off = static_cast<uint64_t>(((k / 4) * kBlockBytes + (k % 4) * 32) >> 4);
+              tc_mma(tmem + static_cast<uint32_t>(sb * 128), q_desc + off, kd + off, kIdescQK, k > 0);
+            }
+            tc_commit(BAR(kBarSFull, j % 6));
+            tc_commit(BAR(kBarKFree, ks));
+          }
+          __syncwarp();
+        }
+      }
+      if (!ok && lane == 0) {
+        // a wait was lost: the MMAs issued so far still run; tensor memory may only be released once they are done
+        tc_commit(BAR(kBarDrain, 0));
+        for (int i = 0; i < spin && !mbar_try_wait(BAR(kBarDrain, 0), 0); ++i) {}
+      }
+    } else {
+      // =============================================================== PV issuer
+      const uint64_t v_desc0 = smem_desc(smem_u32(Vs), kBlockBytes, 1024);
+      Walk w = walk_of(p, piece);
+      Segment seg;
+      bool ok = true;
+      int i = 0, items = 0;
+      uint32_t v_parity = 0;                      // bit s: parity of the loader's own work on stage s
+      while (ok && next_segment(p, w, seg)) {
+#pragma unroll 1
+        for (int t = seg.t0; t < seg.t1; ++t, ++i) {
+          const int st = i % VD, sb = i % kSD;
+          const int left = min(t < w.r.n_ctx ? w.r.kvl - t * kTileN : w.r.n - (t - w.r.n_ctx) * kTileN, kTileN);
+          if (FP8) {
+            if (!wait_warp(BAR(kBarVReady, st), static_cast<uint32_t>(i / VD) & 1u)) { ok = false; break; }      // the rotators fill every V stage
+          } else if (!wait_warp(BAR(kBarVLanded, st), static_cast<uint32_t>(i / VD) & 1u)) {
+            ok = false; break;
+          }
+          if (!FP8 && (t >= w.r.n_ctx || left < kTileN)) {
+            if (!wait_warp(BAR(kBarVReady, st), (v_parity >> st) & 1u)) { ok = false; break; }
+            v_parity ^= 1u << st;
+          }
+          if (t == seg.t0 && items++ > 0 && !wait_warp(BAR(kBarOFree), static_cast<uint32_t>(items - 2) & 1u)) { ok = false; break; }      // the item before has left O
+          if (!wait_warp(BAR(kBarPFull, sb), static_cast<uint32_t>(i / kSD) & 1u)) { ok = false; break; }
+          tc_fence_after();
+          if (lane == 0) {
+            const uint64_t vd = v_desc0 + static_cast<uint64_t>(st) * (L::kStage >> 4);
+            const int n_groups = (left + 15) >> 4;
+#pragma unroll
+            for (int k = 0; k < kTileN / 16; ++k)
+              if (k < n_groups)
+                tc_mma_ts(tmem + kColO, tmem + static_cast<uint32_t>(sb * 128 + k * 8), vd + static_cast<uint64_t>((k * 2048) >> 4), kIdescPV,
+                          t > seg.t0 || k > 0 ? 1u : 0u);
+            tc_commit(BAR(kBarVFree, st));
+            tc_commit(BAR(kBarPvDone, sb));
+          }
+          __syncwarp();
+        }
+      }
+      if (!ok && lane == 0) {
+        tc_commit(BAR(kBarDrain, 1));
+        for (int k = 0; k < spin && !mbar_try_wait(BAR(kBarDrain, 1), 0); ++k) {}
+      }
+    }
+  }
+
+  // ---- common exit: nothing of this CTA may still be in flight when tensor memory is released
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kPvWarp) tmem_dealloc(tmem, kTmemCols);
+}
+
+// ---------------------------------------------------------------- merge of the parts of a divided item
+// Block (c, y) combines 16 rows of the item that CTA c began: m* = max m, l* = sum l 2^(m - m*), out = sum o 2^(m - m*) / l*.
+// A warp per row at a time; the parts' (m, l) are read side by side by its lanes, then the outputs four parts at a time.
+constexpr int kMergeRows = 16;
+template <int D>
+__global__ void __launch_bounds__(128) mepic_tree_merge(const TreeParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");               // launched as a programmatic dependent of the attention kernel
+  const int4 d = p.desc[blockIdx.x];
+  const int parts = d.w, G = p.group, lane = threadIdx.x & 31;
+  if (parts == 0) return;
+  for (int r = blockIdx.y * kMergeRows + (threadIdx.x >> 5); r < min(d.y * G, (static_cast<int>(blockIdx.y) + 1) * kMergeRows); r += 4) {
+    auto at = [&](int k) { return ((static_cast<size_t>(blockIdx.x) + k) * kSlots + (k == 0 ? 1 : 0)) * 128 + r; };
+    float m_star = -INFINITY;
+    for (int k = lane; k < parts; k += 32) m_star = fmaxf(m_star, p.part_ml[at(k)].x);
+#pragma unroll
+    for (int s = 16; s; s >>= 1) m_star = fmaxf(m_star, __shfl_xor_sync(kFull, m_star, s));
+    float l_star = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = 0; k0 < parts; k0 += 32) {
+      float wgt = 0.f;
+      if (k0 + lane < parts) {
+        const float2 ml = p.part_ml[at(k0 + lane)];
+        wgt = ml.x == -INFINITY ? 0.f : ex2(ml.x - m_star);        // a part that held nothing this row sees
+        l_star += ml.x == -INFINITY ? ml.y : ml.y * wgt;           // (its sum is 0, or NaN, which must show)
+      }
+      const int n = min(32, parts - k0);
+#pragma unroll 4
+      for (int k = 0; k < n; ++k) {
+        const float wk = __shfl_sync(kFull, wgt, k);
+        if (wk != 0.f && lane < D / 4) {
+          const float4 x = *reinterpret_cast<const float4*>(p.part_o + at(k0 + k) * D + 4 * lane);
+          o.x += x.x * wk; o.y += x.y * wk; o.z += x.z * wk; o.w += x.w * wk;
+        }
+      }
     }
 #pragma unroll
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(kFull, s, d);
-    const float mn = fmaxf(m, s), a = ex2(m - mn), w = ex2(s - mn);
-    l = l * a + w;
-#pragma unroll
-    for (int j = 0; j < N; ++j) { ol[j] = ol[j] * a + w * vl[j]; oh[j] = oh[j] * a + w * vh[j]; }
-    m = mn;
-  };
-  float kl[N], kh[N], vl[N], vh[N];
-  for (int t = 0; t < kvl; ++t) {
-    const int e = t >> p.page_shift, in_page = t & (p.page_size - 1);
-    int page = p.page_ids[static_cast<size_t>(b) * p.table_stride + e];
-    if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) { atomicOr(p.status, MEPIC_DEV_BAD_PAGE); page = 0; }
-    const size_t block = static_cast<size_t>(page) * p.n_kv_heads + h, at = (block * p.page_size + in_page) * D;
-    const float ks = FP8 ? p.k_scales[block] : 1.f, vs = FP8 ? p.v_scales[block] : 1.f;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int i = lane + 32 * j;
-      kl[j] = value(p.k_pool, at + i, ks); kh[j] = value(p.k_pool, at + i + D / 2, ks);
-      vl[j] = value(p.v_pool, at + i, vs); vh[j] = value(p.v_pool, at + i + D / 2, vs);
+    for (int s = 16; s; s >>= 1) l_star += __shfl_xor_sync(kFull, l_star, s);
+    const float inv = l_star == 0.f ? 0.f : 1.f / l_star;
+    if (lane < D / 4) {
+      const size_t to = (static_cast<size_t>(d.x + r / G) * (p.n_kv_heads * G) + static_cast<size_t>(d.z) * G + r % G) * D + 4 * lane;
+      *reinterpret_cast<uint2*>(p.out + to) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
     }
-    key(kl, kh, vl, vh, p.pos_base[static_cast<size_t>(b) * p.table_stride + e] + in_page);
   }
-  for (int t = 0; t < n_rows; ++t) {
-    if (!((p.tree_mask[static_cast<size_t>(row) * p.mask_words + (t >> 5)] >> (t & 31)) & 1)) continue;
-    const size_t at = static_cast<size_t>(row0 + t) * p.kv_stride + h * D;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int i = lane + 32 * j;
-      kl[j] = bf(p.k_new[at + i]); kh[j] = bf(p.k_new[at + i + D / 2]);
-      vl[j] = bf(p.v_new[at + i]); vh[j] = bf(p.v_new[at + i + D / 2]);
-    }
-    key(kl, kh, vl, vh, p.row_pos[row0 + t]);
+}
+
+template <int D, bool FP8, bool HOOKS>
+int32_t launch_tree(const TreeParams& p, int ctas, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t st) {
+  constexpr int smem = TreeSmem<D, FP8>::kBytes;
+  cudaError_t e = cudaFuncSetAttribute(mepic_tree_attn<D, FP8, HOOKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) { mepic_set_error("attn_tree: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  mepic_tree_attn<D, FP8, HOOKS><<<ctas, kThreads, smem, st>>>(p, map_k, map_v);
+  e = cudaGetLastError();
+  if (e == cudaSuccess) {
+    const int live = std::min(p.max_rows, p.rows_per_tile) * p.group;
+    e = launch_dependent(mepic_tree_merge<D>, dim3(ctas, (live + kMergeRows - 1) / kMergeRows), dim3(128), st, p);
   }
-  uint16_t* o = p.out + (static_cast<size_t>(row) * n_q_heads + hq) * D;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int i = lane + 32 * j;
-    o[i] = l > 0.f || l != l ? f32_to_bf16_bits(ol[j] / l) : 0;
-    o[i + D / 2] = l > 0.f || l != l ? f32_to_bf16_bits(oh[j] / l) : 0;
-  }
+  if (e != cudaSuccess) { mepic_set_error("attn_tree: launch: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  mepic_count_launches(2);
+  return MEPIC_OK;
+}
+
+int sm_count() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  return sms;
+}
+int rows_per_tile(const mepic_config_t* cfg) { return 128 / (cfg->n_q_heads / cfg->n_kv_heads); }
+// One CTA per SM, or one per level where there are more levels (row tiles of a request) than SMs.
+int cta_count(const mepic_config_t* cfg, int max_rows, int sms) {
+  const int q = rows_per_tile(cfg);
+  return std::max(sms, (max_rows + q - 1) / q);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-size_t workspace_bytes(const mepic_config_t* cfg, int max_rows) { (void)cfg; (void)max_rows; return 16; }
+size_t workspace_bytes(const mepic_config_t* cfg, int max_rows) {
+  const int sms = sm_count();
+  if (sms <= 0) { mepic_set_error("attn_tree: no CUDA device"); return 0; }
+  const size_t n = static_cast<size_t>(cta_count(cfg, max_rows, sms));
+  return n * (sizeof(int4) + kSlots * 128 * (sizeof(float2) + static_cast<size_t>(cfg->head_dim) * sizeof(float)));
+}
 
 int32_t tree_call(const mepic_config_t* cfg, const mepic_attn_tree_args_t* a, const float* k_scales, const float* v_scales, bool fp8, void* cuda_stream) {
   const char* what = fp8 ? "attn_tree_fp8" : "attn_tree";
@@ -174,16 +1119,28 @@ int32_t tree_call(const mepic_config_t* cfg, const mepic_attn_tree_args_t* a, co
   p.page_shift = 0;
   while ((1 << p.page_shift) < cfg->page_size) ++p.page_shift;
   p.scale_log2 = a->sm_scale * 1.4426950408889634f;
+  p.group = cfg->n_q_heads / cfg->n_kv_heads;
+  p.rows_per_tile = rows_per_tile(cfg);
+  p.max_levels = (a->max_rows + p.rows_per_tile - 1) / p.rows_per_tile;
+  const int ctas = cta_count(cfg, a->max_rows, sm_count());
+  unsigned char* ws = static_cast<unsigned char*>(a->workspace);
+  p.desc = reinterpret_cast<int4*>(ws);
+  p.part_ml = reinterpret_cast<float2*>(ws + sizeof(int4) * ctas);
+  p.part_o = reinterpret_cast<float*>(p.part_ml + static_cast<size_t>(ctas) * kSlots * 128);
+  p.spin_limit = mepic_test_spin_limit(kSpinLimit); p.skip_tile = mepic_test_skip_tile();
+  alignas(64) CUtensorMap map_k, map_v;
+  if (fp8) {
+    memset(&map_k, 0, sizeof(map_k)); memset(&map_v, 0, sizeof(map_v));      // codes come by untiled bulk copies
+  } else {
+    int32_t rc = mepic_make_pool_map(cfg, a->k_pool, &map_k);
+    if (rc == MEPIC_OK) rc = mepic_make_pool_map(cfg, a->v_pool, &map_v);
+    if (rc != MEPIC_OK) return rc;
+  }
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const long long units = static_cast<long long>(a->total_rows) * cfg->n_q_heads;
-  const unsigned grid = static_cast<unsigned>((units + 3) / 4);
-  if (fp8) mepic_tree_attn<128, true><<<grid, 128, 0, st>>>(p, cfg->n_q_heads);
-  else if (cfg->head_dim == 128) mepic_tree_attn<128, false><<<grid, 128, 0, st>>>(p, cfg->n_q_heads);
-  else mepic_tree_attn<64, false><<<grid, 128, 0, st>>>(p, cfg->n_q_heads);
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) { mepic_set_error("%s: launch: %s", what, cudaGetErrorString(e)); return MEPIC_E_CUDA; }
-  mepic_count_launches(1);
-  return MEPIC_OK;
+  const bool hooks = p.spin_limit != kSpinLimit || p.skip_tile >= 0;
+  if (cfg->head_dim == 64) return hooks ? launch_tree<64, false, true>(p, ctas, map_k, map_v, st) : launch_tree<64, false, false>(p, ctas, map_k, map_v, st);
+  if (fp8) return hooks ? launch_tree<128, true, true>(p, ctas, map_k, map_v, st) : launch_tree<128, true, false>(p, ctas, map_k, map_v, st);
+  return hooks ? launch_tree<128, false, true>(p, ctas, map_k, map_v, st) : launch_tree<128, false, false>(p, ctas, map_k, map_v, st);
 }
 
 }  // namespace
