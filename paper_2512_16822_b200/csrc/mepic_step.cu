@@ -18,46 +18,63 @@ namespace {
 using namespace mepic_dev;
 
 // ---------------------------------------------------------------- tree layout
-// One CTA per request.  The parents sit in shared memory; a thread per row walks up its chain of ancestors.  Parents precede
-// their rows, so a walk meets its ancestors in descending order and fills the row's mask words from the last one down, a
-// word at a time, without holding the mask.  The walk is depth x one shared-memory load (~30 cycles).
-constexpr int kLayoutThreads = 256;
+// One CTA per request.  Ancestors by doubling: every row starts with its own bit and a pointer to its parent; in a round it
+// takes over the bits of the row it points to and then points where that row pointed, so after k rounds it holds its 2^k
+// nearest ancestors and log2(depth) rounds do.  (A thread per row walking up its chain took 8 us on trees of 200 rows and
+// depth 45.)  A row may read another's words while those grow: they only ever hold true ancestors, so whatever it reads is
+// right, and the pointers, of which that is not so, are kept twice.  The depth is the number of bits.
+constexpr int kLayoutThreads = 512;
 __global__ void __launch_bounds__(kLayoutThreads) mepic_tree_layout_kernel(const mepic_tree_layout_args_t a, int page_shift) {
-  __shared__ int16_t up[MEPIC_TREE_MAX_ROWS];
-  const int b = blockIdx.x, cap = 32 * a.mask_words;
+  __shared__ int16_t up[2][MEPIC_TREE_MAX_ROWS];
+  extern __shared__ uint32_t bits[];             // [32 mask_words][mask_words]
+  const int b = blockIdx.x, tid = threadIdx.x, W = a.mask_words;
   const RowRange rr = rows_of(a.row_offsets, b, a.total_rows, 0x7fffffff);
-  const int n = min(rr.n, cap);
-  bool bad = rr.bad || rr.n > cap;
   int kvl = __ldg(a.kv_len + b);
-  for (int i = threadIdx.x; i < n; i += kLayoutThreads) {
+  const int n = min(rr.n, 32 * W);
+  bool bad = rr.bad || rr.n > n;
+  const float inv_w = 1.f / static_cast<float>(W);      // k / W = int((k + 1/2) inv_w) for every k below 2^15 here
+  for (int i = tid; i < n; i += kLayoutThreads) {
     int p = __ldg(a.parent + rr.lo + i);
     if (p < -1 || p >= i) { bad = true; p = -1; }
-    up[i] = static_cast<int16_t>(p);
+    up[0][i] = static_cast<int16_t>(p);
+  }
+  for (int k = tid; k < n * W; k += kLayoutThreads) {
+    const int r = static_cast<int>((static_cast<float>(k) + 0.5f) * inv_w);
+    bits[k] = (r >> 5) == k - r * W ? 1u << (r & 31) : 0u;
   }
   if (bad) atomicOr(a.status, MEPIC_DEV_BAD_TREE);
   const long long room = static_cast<long long>(a.table_stride) << page_shift;
   if (kvl < 0 || kvl > room) {
-    if (threadIdx.x == 0) atomicOr(a.status, MEPIC_DEV_BAD_SLOT);
+    if (tid == 0) atomicOr(a.status, MEPIC_DEV_BAD_SLOT);
     kvl = kvl < 0 ? 0 : static_cast<int>(room);
   }
   int next = 0;
   if (kvl > 0) next = __ldg(a.pos_base + static_cast<size_t>(b) * a.table_stride + ((kvl - 1) >> page_shift)) + ((kvl - 1) & ((1 << page_shift) - 1)) + 1;
   __syncthreads();
-  for (int i = threadIdx.x; i < rr.n; i += kLayoutThreads) {
-    int32_t* words = a.tree_mask + static_cast<size_t>(rr.lo + i) * a.mask_words;
-    int depth = 0, at = a.mask_words - 1;      // mask word being filled
-    uint32_t acc = 0;
-    if (i < n) {
-      for (int j = i; j >= 0; j = up[j]) {
-        const int w = j >> 5;
-        while (at > w) { words[at--] = static_cast<int32_t>(acc); acc = 0; }
-        acc |= 1u << (j & 31);
-        ++depth;
-      }
-      --depth;
+  for (int from = 0, more = n > 0; more; from ^= 1) {
+    for (int k = tid; k < n * W; k += kLayoutThreads) {
+      const int r = static_cast<int>((static_cast<float>(k) + 0.5f) * inv_w), w = k - r * W;
+      const int u = up[from][r];
+      if (u >= 0 && w <= (u >> 5)) bits[k] |= *reinterpret_cast<volatile uint32_t*>(bits + u * W + w);      // ancestors of u lie in words up to u's
     }
-    while (at >= 0) { words[at--] = static_cast<int32_t>(acc); acc = 0; }
+    bool left = false;
+    for (int i = tid; i < n; i += kLayoutThreads) {
+      const int u = up[from][i], to = u >= 0 ? up[from][u] : -1;
+      up[from ^ 1][i] = static_cast<int16_t>(to);
+      left = left || to >= 0;
+    }
+    more = __syncthreads_or(left);
+  }
+  int32_t* out = a.tree_mask + static_cast<size_t>(rr.lo) * W;
+  for (int k = tid; k < n * W; k += kLayoutThreads) out[k] = static_cast<int32_t>(bits[k]);
+  for (int i = tid; i < n; i += kLayoutThreads) {
+    int depth = -1;
+    for (int w = 0; w <= (i >> 5); ++w) depth += __popc(bits[i * W + w]);
     a.row_pos[rr.lo + i] = next + depth;
+  }
+  for (int i = n + tid; i < rr.n; i += kLayoutThreads) {      // rows the mask has no room for (reported)
+    for (int w = 0; w < W; ++w) out[static_cast<size_t>(i) * W + w] = 0;
+    a.row_pos[rr.lo + i] = next;
   }
 }
 
@@ -244,9 +261,25 @@ __device__ __forceinline__ int source_of(const CommitParams& p, int r, int lane)
   return src;
 }
 
+// The same for one lane (a row of its own).
+__device__ __forceinline__ int lane_source_of(const CommitParams& p, int r) {
+  int src = r;
+  if (p.src_rows) {
+    int lo = 0, hi = p.batch;                    // row_offsets[lo] <= r < row_offsets[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (__ldg(p.row_offsets + mid) <= r) lo = mid; else hi = mid;
+    }
+    const int k = r - __ldg(p.row_offsets + lo);
+    src = k >= 0 && k < p.src_stride ? __ldg(p.src_rows + static_cast<size_t>(lo) * p.src_stride + k) : -1;
+  }
+  if (src < 0 || src >= p.n_sources) { atomicOr(p.status, MEPIC_DEV_BAD_SLOT); return -1; }
+  return src;
+}
+
 constexpr int kCopyRows = 8;         // rows per CTA, one warp each
 template <int D>
-__global__ void __launch_bounds__(kCopyRows * 32) mepic_rows_commit_kernel(const CommitParams p) {
+__global__ void __launch_bounds__(kCopyRows * 32) mepic_rows_commit_kernel(const __grid_constant__ CommitParams p) {
   constexpr int C = D / 8;           // 16-byte chunks per head row
   const int lane = threadIdx.x & 31, r = blockIdx.x * kCopyRows + (threadIdx.x >> 5);
   const int n_rows = __ldg(p.row_offsets + p.batch);
@@ -271,13 +304,49 @@ __global__ void __launch_bounds__(kCopyRows * 32) mepic_rows_commit_kernel(const
 // them, whole; each of its warps takes one (pool, kv head) of a run at a time, so a block's maximum, scale and codes stay
 // in one warp.  (A CTA per row left 15 of 16 CTAs of a prompt with nothing to do.)
 constexpr int kRunRows = 16;
-constexpr int kRunWarps = 16;
-__global__ void __launch_bounds__(kRunWarps * 32) mepic_rows_commit_fp8_kernel(const CommitParams p) {
+constexpr int kRunWarps = 8;
+// Eight elements -> E4M3(x / sc), the quotient rounded to fp32 first, as the format is defined.  With y = RN(1 / sc) and no
+// overflow or underflow on the way, q <- q + y (x - q sc) in fused arithmetic, begun at q = x y and done twice, ends at the
+// rounded quotient (Markstein's correction): five instructions an element where a division takes a dozen.  For a scale
+// outside [2^-80, 2^80] the division is used.
+__device__ __noinline__ uint2 e4m3x8_by_division(uint4 v, float sc) {
+  const float2 a = bf16x2_to_float2(v.x), b = bf16x2_to_float2(v.y), c = bf16x2_to_float2(v.z), d = bf16x2_to_float2(v.w);
+  return make_uint2(e4m3x4_of(__fdiv_rn(a.x, sc), __fdiv_rn(a.y, sc), __fdiv_rn(b.x, sc), __fdiv_rn(b.y, sc)),
+                    e4m3x4_of(__fdiv_rn(c.x, sc), __fdiv_rn(c.y, sc), __fdiv_rn(d.x, sc), __fdiv_rn(d.y, sc)));
+}
+__device__ __forceinline__ float quotient(float x, float sc, float inv, float most) {
+  x = x > most ? most : (x < -most ? -most : x);      // what saturates anyway must not overflow; NaN stays
+  float q = x * inv;
+  q = fmaf(fmaf(-q, sc, x), inv, q);
+  return copysignf(fmaf(fmaf(-q, sc, x), inv, q), x);      // (a zero's sign is lost on the way)
+}
+__device__ __forceinline__ uint2 e4m3x8_of(const uint4& v, float sc, float inv, float most) {
+  const float2 a = bf16x2_to_float2(v.x), b = bf16x2_to_float2(v.y), c = bf16x2_to_float2(v.z), d = bf16x2_to_float2(v.w);
+  auto q = [&](float x) { return quotient(x, sc, inv, most); };
+  return make_uint2(e4m3x4_of(q(a.x), q(a.y), q(b.x), q(b.y)), e4m3x4_of(q(c.x), q(c.y), q(d.x), q(d.y)));
+}
+// Rows r0 .. r0 + min(n, 16) - 1 of pool w, kv head h: a lane's 16-byte pieces of eight rows (half a warp takes a row), and in
+// lane k < 16 the in-page slot of row k (-1: nothing to write).
+__device__ __forceinline__ void load_block(const CommitParams& p, int w, int r0, int n, int h, int lane, uint4 (&v)[8], int& slot) {
+  int src = -1;
+  slot = -1;
+  if (lane < 16 && lane < n) {
+    src = lane_source_of(p, r0 + lane);
+    slot = src < 0 ? -1 : static_cast<int>(__ldg(reinterpret_cast<const long long*>(p.slot_map) + r0 + lane)) & (p.page_size - 1);
+  }
+  const uint16_t* base = p.src[w] + h * 128 + 8 * (lane & 15);
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    const int s = __shfl_sync(kFull, src, 2 * u + (lane >> 4));
+    v[u] = s < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(base + static_cast<size_t>(s) * p.kv_stride);
+  }
+}
+__global__ void __launch_bounds__(kRunWarps * 32, 3) mepic_rows_commit_fp8_kernel(const __grid_constant__ CommitParams p) {
   constexpr int D = 128;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int r0 = blockIdx.x * kRunRows;
   const int all = __ldg(p.row_offsets + p.batch), n_rows = min(all, p.max_rows);
-  if (all > p.max_rows && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
+  if (all > p.max_rows && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
   if (r0 >= n_rows) return;
   const long long* slots = reinterpret_cast<const long long*>(p.slot_map);
   auto page_of = [&](int r) -> int {
@@ -306,24 +375,27 @@ __global__ void __launch_bounds__(kRunWarps * 32) mepic_rows_commit_fp8_kernel(c
       n += got;
       more = got == 32;
     }
-    for (int unit = warp; unit < 2 * p.n_kv_heads; unit += kRunWarps) {
+    // half a warp takes a row: cc is the 16-byte piece of 8 elements.  A block of 16 rows is 8 pieces per lane, all in flight
+    // at once; a run of one block keeps them in registers between its two passes (maximum, codes).
+    const int half = lane >> 4, cc = lane & 15;
+    for (int unit = blockIdx.y * kRunWarps + warp; unit < 2 * p.n_kv_heads; unit += gridDim.y * kRunWarps) {
       const int w = unit & 1, h = unit >> 1;
       const size_t block = static_cast<size_t>(page) * p.n_kv_heads + h;
-      // half a warp takes a row: lane & 15 is the 16-byte chunk of 8 elements
-      const int half = lane >> 4, cc = lane & 15;
-      float sc;
+      uint4 v[8];
+      int slot = 0;                                // lane k < 16: in-page slot of row k of the block, -1 where there is nothing to write
+      float sc, amax = 0.f;
       if (fresh) {
-        float amax = 0.f;
-        for (int k = 0; k < n; k += 2) {
-          const int s0 = source_of(p, first + k, lane), s1 = k + 1 < n ? source_of(p, first + k + 1, lane) : -1;
-          const int src = half ? s1 : s0;
-          if (src < 0) continue;
-          const uint4 v = *reinterpret_cast<const uint4*>(p.src[w] + static_cast<size_t>(src) * p.kv_stride + h * D + 8 * cc);
-          const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll 1
+        for (int k0 = 0; k0 < n; k0 += 16) {
+          load_block(p, w, first + k0, n - k0, h, lane, v, slot);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 f = bf16x2_to_float2(ww[j]);
-            amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));       // fmaxf drops NaN operands: a NaN element does not set the scale
+          for (int u = 0; u < 8; ++u) {
+            const uint32_t ww[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float2 f = bf16x2_to_float2(ww[j]);
+              amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));       // fmaxf drops NaN operands: a NaN element does not set the scale
+            }
           }
         }
 #pragma unroll
@@ -333,17 +405,17 @@ __global__ void __launch_bounds__(kRunWarps * 32) mepic_rows_commit_fp8_kernel(c
       } else {
         sc = p.scales[w][block];
       }
-      for (int k = 0; k < n; k += 2) {
-        const int s0 = source_of(p, first + k, lane), s1 = k + 1 < n ? source_of(p, first + k + 1, lane) : -1;
-        const int src = half ? s1 : s0;
-        if (src < 0) continue;
-        const uint4 v = *reinterpret_cast<const uint4*>(p.src[w] + static_cast<size_t>(src) * p.kv_stride + h * D + 8 * cc);
-        const float2 f0 = bf16x2_to_float2(v.x), f1 = bf16x2_to_float2(v.y), f2 = bf16x2_to_float2(v.z), f3 = bf16x2_to_float2(v.w);
-        uint2 out;
-        out.x = e4m3x4_of(__fdiv_rn(f0.x, sc), __fdiv_rn(f0.y, sc), __fdiv_rn(f1.x, sc), __fdiv_rn(f1.y, sc));
-        out.y = e4m3x4_of(__fdiv_rn(f2.x, sc), __fdiv_rn(f2.y, sc), __fdiv_rn(f3.x, sc), __fdiv_rn(f3.y, sc));
-        const int in_page = static_cast<int>(__ldg(slots + first + k + half)) & (p.page_size - 1);
-        *reinterpret_cast<uint2*>(static_cast<unsigned char*>(p.pool[w]) + (block * p.page_size + in_page) * D + 8 * cc) = out;
+      const float inv = __frcp_rn(sc), most = 600.f * sc;
+      const bool plain = sc >= 8.2718061e-25f && sc <= 1.2089258e24f;       // 2^-80 .. 2^80
+#pragma unroll 1
+      for (int k0 = 0; k0 < n; k0 += 16) {
+        if (!fresh || n > 16) load_block(p, w, first + k0, n - k0, h, lane, v, slot);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int in_page = __shfl_sync(kFull, slot, 2 * u + half);
+          const uint2 out = plain ? e4m3x8_of(v[u], sc, inv, most) : e4m3x8_by_division(v[u], sc);
+          if (in_page >= 0) *reinterpret_cast<uint2*>(static_cast<unsigned char*>(p.pool[w]) + (block * p.page_size + in_page) * D + 8 * cc) = out;
+        }
       }
     }
   }
@@ -392,7 +464,8 @@ int32_t commit_call(const mepic_config_t* cfg, const mepic_rows_commit_args_t* a
   p.page_shift = shift_of(cfg->page_size);
   p.n_slots = static_cast<long long>(cfg->num_pages) * cfg->page_size;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (fp8) mepic_rows_commit_fp8_kernel<<<(a->max_rows + kRunRows - 1) / kRunRows, kRunWarps * 32, 0, st>>>(p);
+  // a CTA takes up to eight of a run's (pool, kv head) blocks, one per warp: several CTAs fit an SM and hide one another's look-ups
+  if (fp8) mepic_rows_commit_fp8_kernel<<<dim3((a->max_rows + kRunRows - 1) / kRunRows, std::min((2 * cfg->n_kv_heads + kRunWarps - 1) / kRunWarps, 64)), kRunWarps * 32, 0, st>>>(p);
   else if (cfg->head_dim == 128) mepic_rows_commit_kernel<128><<<(a->max_rows + kCopyRows - 1) / kCopyRows, kCopyRows * 32, 0, st>>>(p);
   else mepic_rows_commit_kernel<64><<<(a->max_rows + kCopyRows - 1) / kCopyRows, kCopyRows * 32, 0, st>>>(p);
   return launched(what);
@@ -411,7 +484,12 @@ extern "C" int32_t mepic_tree_layout(const mepic_config_t* cfg, const mepic_tree
   if (!a->parent || !a->row_offsets || !a->kv_len || !a->pos_base || !a->row_pos || !a->tree_mask || !a->status) {
     mepic_set_error("tree_layout: NULL pointer argument"); return MEPIC_E_INVAL;
   }
-  mepic_tree_layout_kernel<<<a->batch, kLayoutThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(*a, shift_of(cfg->page_size));
+  const size_t smem = static_cast<size_t>(32 * a->mask_words) * a->mask_words * sizeof(uint32_t);
+  if (smem > 40 * 1024) {                        // beside the static 4 KB
+    const cudaError_t e = cudaFuncSetAttribute(mepic_tree_layout_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) { mepic_set_error("tree_layout: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  }
+  mepic_tree_layout_kernel<<<a->batch, kLayoutThreads, smem, static_cast<cudaStream_t>(cuda_stream)>>>(*a, shift_of(cfg->page_size));
   return launched("tree_layout");
 }
 
