@@ -97,18 +97,10 @@ struct TreeParams {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),      \
                  "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) \
                : "r"(taddr) : "memory")
-// The rest of a wait that did not find its phase complete at once: bounded, and over when another role has raised the abort
-// flag.  Not inlined: two dozen waits, each with its loop, were a third of the kernel's code.
-__device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status, int limit) {
-#pragma unroll 1
-  for (int i = 0; i < limit; ++i) {
-    if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
-    if ((i & 255) == 255 && *abort_flag) return false;
-  }
-  *abort_flag = 1;
-  atomicOr(status, MEPIC_DEV_WAIT_EXPIRED);
-  return false;
-}
+
+#define TMEM_ST8(taddr, r)                                                                                           \
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"                               \
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory")
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
@@ -119,7 +111,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // ---------------------------------------------------------------- the cut
 // What a request contributes: its rows, its key tiles, the row tiles (levels) it has.
 struct Request { int row0, n, kvl, n_ctx, n_all, levels; bool bad_rows, bad_len; };
-__device__ __noinline__ Request request_of(const TreeParams& p, int b) {
+__device__ __forceinline__ Request request_of(const TreeParams& p, int b) {
   Request r;
   const RowRange rr = rows_of(p.row_offsets, b, p.total_rows, p.max_rows);
   r.row0 = rr.lo; r.n = rr.n; r.bad_rows = rr.bad;
@@ -135,14 +127,16 @@ __device__ __noinline__ Request request_of(const TreeParams& p, int b) {
 
 // One CTA's piece: tiles [lo, hi) of its level's line, which has `line` tiles in `pieces` pieces; it starts at key tile t of
 // (request b, kv head h).
-struct Piece { int level, piece, pieces, b, h, t; long long lo, hi, line; };
+struct Piece { int level, piece, pieces, b, h, t; long long lo, hi, line; Request r; };
 struct PlanScratch {
   unsigned long long hist[kMaxLevels];
   long long warp_sum[kThreads / 32];
 };
-__device__ __forceinline__ long long cut_at(long long line, int pieces, int k) {
-  return (line / pieces) * k + (line % pieces) * k / pieces;
+__device__ __forceinline__ long long mul_div(long long a, int b, long long c) {      // a b / c, b <= 2^11
+  if (a < (1 << 20) && c < (1ll << 31)) return static_cast<uint32_t>(a) * static_cast<uint32_t>(b) / static_cast<uint32_t>(c);
+  return a / c * b + a % c * b / c;
 }
+__device__ __forceinline__ long long cut_at(long long line, int pieces, int k) { return mul_div(line, k, pieces); }
 // Executed by the whole CTA.
 __device__ __noinline__ void plan_piece(const TreeParams& p, PlanScratch* sh, Piece* out) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -168,13 +162,13 @@ __device__ __noinline__ void plan_piece(const TreeParams& p, PlanScratch* sh, Pi
       all += line;
       used += line > 0;
     }
-    Piece c{-1, 0, 0, 0, 0, 0, 0, 0, 0};
+    Piece c{-1, 0, 0, 0, 0, 0, 0, 0, 0, {}};
     int cta = blockIdx.x;
     const long long spare = static_cast<long long>(gridDim.x) - used;      // every level has one CTA, the rest go by length
 #pragma unroll 1
     for (int m = 0; m < used; ++m) {
       const long long len = static_cast<long long>(sh->hist[m]);
-      long long n = 1 + spare * len / all;
+      long long n = 1 + mul_div(len, static_cast<int>(spare), all);
       n = n < len ? n : len;                                     // no empty pieces
       if (cta < n) {
         c.level = m; c.piece = cta; c.pieces = static_cast<int>(n); c.line = len;
@@ -216,7 +210,11 @@ __device__ __noinline__ void plan_piece(const TreeParams& p, PlanScratch* sh, Pi
     }
     if (at <= lo && lo < at + w) {
       const long long off = lo - at;
-      (*out).b = b; (*out).h = static_cast<int>(off / n_all); (*out).t = static_cast<int>(off % n_all);
+      const Request r = request_of(p, b);
+      out->r = r;
+      out->b = b;
+      out->h = off < (1ll << 31) ? static_cast<uint32_t>(off) / static_cast<uint32_t>(n_all) : static_cast<int>(off / n_all);
+      out->t = static_cast<int>(off - static_cast<long long>(out->h) * n_all);
     }
     before += chunk;
     __syncthreads();
@@ -225,36 +223,86 @@ __device__ __noinline__ void plan_piece(const TreeParams& p, PlanScratch* sh, Pi
   __syncthreads();
 }
 
-// The segments of a piece, one per item it touches, in order.  Every role walks them for itself; what it reads again lies
-// in the nearest cache.
+// The same by one warp, a request per lane, for up to 32 requests: no barrier of the CTA on the way.
+__device__ __forceinline__ long long warp_sum64(long long v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(kFull, v, d);
+  return v;
+}
+__device__ __forceinline__ void plan_by_warp(const TreeParams& p, Piece* out, int lane) {
+  Request r{0, 0, 0, 0, 0, 0, false, false};
+  if (lane < p.batch) {
+    r = request_of(p, lane);
+    if (blockIdx.x == 0) {
+      if (r.bad_rows) atomicOr(p.status, MEPIC_DEV_BAD_TREE);
+      if (r.bad_len) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
+    }
+  }
+  const long long w = r.levels > 0 ? static_cast<long long>(r.n_all) * p.n_kv_heads : 0;
+  const long long all = warp_sum64(w * r.levels);
+  const int used = __reduce_max_sync(kFull, r.levels), spare = static_cast<int>(gridDim.x) - used;
+  int cta = blockIdx.x, level = -1, n = 0;
+  long long len = 0;
+#pragma unroll 1
+  for (int m = 0; m < used; ++m) {
+    len = warp_sum64(r.levels > m ? w : 0);
+    const long long share = 1 + mul_div(len, spare, all);
+    n = static_cast<int>(share < len ? share : len);
+    if (cta < n) { level = m; break; }
+    cta -= n;
+  }
+  if (lane == 0) out->level = level;
+  if (level < 0) return;
+  const long long lo = cut_at(len, n, cta), mine = r.levels > level ? w : 0;
+  long long at = mine;                           // inclusive sum, then this request's first place on the line
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long up = __shfl_up_sync(kFull, at, d);
+    if (lane >= d) at += up;
+  }
+  at -= mine;
+  if (at <= lo && lo < at + mine) {              // one lane
+    out->piece = cta; out->pieces = n; out->line = len; out->lo = lo; out->hi = cut_at(len, n, cta + 1);
+    const long long off = lo - at;
+    out->b = lane; out->r = r;
+    out->h = off < (1ll << 31) ? static_cast<uint32_t>(off) / static_cast<uint32_t>(r.n_all) : static_cast<int>(off / r.n_all);
+    out->t = static_cast<int>(off - static_cast<long long>(out->h) * r.n_all);
+  }
+}
+
+// The segments of a piece, one per item it touches, in order.  The K loader walks them and publishes each to the other roles.
 struct Walk {
   Request r;
   long long left;
   int b, h, t, level;
 };
-struct Segment { int t0, t1; };        // key tiles of item (walk's request, walk's h)
-__device__ __noinline__ Walk walk_of(const TreeParams& p, const Piece& c) {
+// Key tiles t0 .. t1 - 1 of item (request b, kv head h); the request's first row, rows, length, context tiles, all tiles.
+// t1 = 0: there are no more.
+struct Segment { int t0, t1, b, h, row0, n, kvl, n_ctx, n_all; };
+__device__ __forceinline__ Walk walk_of(const Piece& c) {
   Walk w;
-  w.level = c.level; w.left = c.hi - c.lo; w.b = c.b; w.h = c.h; w.t = c.t;
-  w.r = request_of(p, c.b);
+  w.level = c.level; w.left = c.hi - c.lo; w.b = c.b; w.h = c.h; w.t = c.t; w.r = c.r;
   return w;
 }
-__device__ __noinline__ bool next_segment(const TreeParams& p, Walk& w, Segment& s) {
-  if (w.left <= 0) return false;
+__device__ __forceinline__ Segment next_segment(const TreeParams& p, Walk& w) {
+  Segment s{0, 0, 0, 0, 0, 0, 0, 0, 0};
+  if (w.left <= 0) return s;
   if (w.t >= w.r.n_all) {
     w.t = 0;
     if (++w.h >= p.n_kv_heads) {
       w.h = 0;
+#pragma unroll 1
       do {
-        if (++w.b >= p.batch) { w.left = 0; return false; }      // not reached: `left` ends first
+        if (++w.b >= p.batch) { w.left = 0; return s; }          // not reached: `left` ends first
         w.r = request_of(p, w.b);
       } while (w.r.levels <= w.level);
     }
   }
   const int n = static_cast<int>(w.left < w.r.n_all - w.t ? w.left : w.r.n_all - w.t);
   s.t0 = w.t; s.t1 = w.t + n;
+  s.b = w.b; s.h = w.h; s.row0 = w.r.row0; s.n = w.r.n; s.kvl = w.r.kvl; s.n_ctx = w.r.n_ctx; s.n_all = w.r.n_all;
   w.t += n; w.left -= n;
-  return true;
+  return s;
 }
 
 // ---------------------------------------------------------------- attention
@@ -262,14 +310,17 @@ __device__ __noinline__ bool next_segment(const TreeParams& p, Walk& w, Segment&
 // are through with the K codes of i - 2; that tile's K stage was free, so QK^T of i - 4 was complete, so PV of i - 7 was, so
 // the softmax was through with tile i - 8.
 constexpr int kScaleRing = 8;
+constexpr int kSegRing = 3;            // segments published and not yet read by everybody
+template <bool FP8>
 struct Small {
-  float ks[2][8], vs[kScaleRing][8];
+  float ks[FP8 ? 2 : 1][8], vs[FP8 ? kScaleRing : 1][8];
   union {
     PlanScratch plan;                  // before the roles begin
     float ref[2][128];                 // [warpgroup][row] the row's reference after that warpgroup's latest tile
   };
   float sum[2][128];                   // [warpgroup][row] its sum at an item's end
   Piece piece;
+  Segment seg[kSegRing];
   uint32_t tmem;
   int abort_flag;
   int odd_v;                           // a drafted V row of this CTA's holds a non-finite element
@@ -286,8 +337,8 @@ struct TreeSmem {
   static constexpr int kV = kK + KD * kStage;
   static constexpr int kC = kV + VD * kStage;
   static constexpr int kBars = kC + (FP8 ? 2 * CD * kCodes : 0);
-  static constexpr int kSmall = kBars + 424;                     // Small
-  static constexpr int kBytes = kSmall + sizeof(Small);
+  static constexpr int kSmall = kBars + 472;                     // Small
+  static constexpr int kBytes = kSmall + sizeof(Small<FP8>);
 };
 static_assert(TreeSmem<128, false>::kBytes <= 232448 && TreeSmem<128, true>::kBytes <= 232448, "shared memory of an SM");
 
@@ -302,27 +353,33 @@ constexpr int kBarPFull = 31, kBarPvDone = 34;                         // [score
 constexpr int kBarQReady = 37, kBarOFree = 38;
 constexpr int kBarRef = 39, kBarItem = 47;                             // [warpgroup * 4 + warp], [warp]
 constexpr int kBarDrain = 51;                                          // [QK, PV] after a lost wait: the MMAs issued so far are done
-constexpr int kNumBars = 53;
-static_assert(kNumBars * 8 <= 424, "barrier block");
+constexpr int kBarSegFull = 53, kBarSegFree = 56;                      // [segment % 3]
+constexpr int kNumBars = 59;
+static_assert(kNumBars * 8 <= 472, "barrier block");
 
-// Rotates, scales and rounds half (chunks of wg) of a row's q into row r of the staged tile; a dead row is zeros.
+// Rotates, scales and rounds the q rows of an item's tile into the staged tile: a thread takes a 16-byte piece and its partner
+// in the other half of a row at a time, neighbours in one row (a thread per row left 32 cache lines per load: 5,000 cycles).
+// Rows without a drafted row are zeros up to the next multiple of 32 and stay as they are beyond: only their own scores
+// come of it.
 template <int D>
-__device__ __noinline__ void stage_q(const TreeParams& p, unsigned char* Qs, bool live, int row, int head, int wg, int r) {
+__device__ __noinline__ void stage_q(const TreeParams& p, unsigned char* Qs, int first, int n_rows, int head0, int tid) {
   constexpr int CH = D / 16;
-  int pos = live ? __ldg(p.row_pos + row) : 0;
-  if (pos < 0 || pos > p.max_position) { atomicOr(p.status, MEPIC_DEV_BAD_POSITION); pos = pos < 0 ? 0 : p.max_position; }
-  const uint16_t* src = p.q + static_cast<size_t>(live ? row : 0) * p.q_stride + static_cast<size_t>(head) * D;
-  const float4* cs = reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(pos) * D);
-#pragma unroll
-  for (int cc = 0; cc < CH / 2; ++cc) {
-    const int c = wg * (CH / 2) + cc, lc = c, hc = CH + c;
+  const int G = p.group, live = n_rows * G;
+#pragma unroll 2
+  for (int idx = tid; idx < ((live + 31) & ~31) * CH; idx += kSoftmaxWarps * 32) {
+    const int r = idx / CH, c = idx % CH, lc = c, hc = CH + c;
     uint32_t lo_w[4] = {0, 0, 0, 0}, hi_w[4] = {0, 0, 0, 0};
-    if (live) {
-      const uint4 lo = *reinterpret_cast<const uint4*>(src + 8 * c), hi = *reinterpret_cast<const uint4*>(src + D / 2 + 8 * c);
+    if (r < live) {
+      const int row = first + r / G;
+      int pos = __ldg(p.row_pos + row);
+      if (pos < 0 || pos > p.max_position) { atomicOr(p.status, MEPIC_DEV_BAD_POSITION); pos = pos < 0 ? 0 : p.max_position; }
+      const uint16_t* src = p.q + static_cast<size_t>(row) * p.q_stride + static_cast<size_t>(head0 + r % G) * D + 8 * c;
+      const float4* cs = reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(pos) * D + 16 * c);
+      const uint4 lo = *reinterpret_cast<const uint4*>(src), hi = *reinterpret_cast<const uint4*>(src + D / 2);
       const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float4 t = __ldg(cs + 4 * c + j);              // (cos, sin) of pairs 8c + 2j and 8c + 2j + 1
+        const float4 t = __ldg(cs + j);                      // (cos, sin) of pairs 8c + 2j and 8c + 2j + 1
         const float2 x = bf16x2_to_float2(lw[j]), y = bf16x2_to_float2(hw[j]);
         lo_w[j] = pack_bf16x2((x.x * t.x - y.x * t.y) * p.scale_log2, (x.y * t.z - y.y * t.w) * p.scale_log2);
         hi_w[j] = pack_bf16x2((x.x * t.y + y.x * t.x) * p.scale_log2, (x.y * t.w + y.y * t.z) * p.scale_log2);
@@ -382,7 +439,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
   unsigned char* Vc = Kc + CD * L::kCodes;
   const uint32_t bar0 = smem_u32(smem + L::kBars);
   auto BAR = [&](int which, int slot = 0) { return bar0 + static_cast<uint32_t>((which + slot) * 8); };
-  Small* sm = reinterpret_cast<Small*>(smem + L::kSmall);
+  Small<FP8>* sm = reinterpret_cast<Small<FP8>*>(smem + L::kSmall);
   volatile int* abort_flag = &sm->abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int spin = HOOKS ? p.spin_limit : kSpinLimit;
@@ -401,6 +458,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
     for (int s = 0; s < 6; ++s) { mbar_init(BAR(kBarKLanded, s), 1); mbar_init(BAR(kBarSFull, s), 1); }
     for (int s = 0; s < 8; ++s) mbar_init(BAR(kBarRef, s), 1);
     for (int s = 0; s < 4; ++s) mbar_init(BAR(kBarItem, s), 2);
+    for (int s = 0; s < kSegRing; ++s) { mbar_init(BAR(kBarSegFull, s), 1); mbar_init(BAR(kBarSegFree, s), kThreads / 32 - 1); }
     mbar_init(BAR(kBarQReady), kSoftmaxWarps); mbar_init(BAR(kBarOFree), kSoftmaxWarps); mbar_init(BAR(kBarDrain, 0), 1); mbar_init(BAR(kBarDrain, 1), 1);
     sm->abort_flag = 0;
     sm->odd_v = 0;
@@ -408,12 +466,14 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
     fence_async_smem();
   }
   if (warp == kPvWarp) tmem_alloc(smem_u32(&sm->tmem), kTmemCols);
-  plan_piece(p, &sm->plan, &sm->piece);
+  if (p.batch > 32) plan_piece(p, &sm->plan, &sm->piece);
+  else if (warp == kKLoaderWarp) plan_by_warp(p, &sm->piece, lane);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the merge may become resident; it waits for this grid's end
   tc_fence_before();
   __syncthreads();                                // barriers initialised, tensor memory allocated, the piece known
   tc_fence_after();
   const uint32_t tmem = sm->tmem;
-  const Piece piece = sm->piece;
+  const Piece& piece = sm->piece;
   const int G = p.group, n_q_heads = p.n_kv_heads * G;
   const bool has_work = piece.level >= 0;
   if (!has_work && tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
@@ -422,8 +482,27 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
   // that room: 128 x 232 + 384 x 88 = 63,488 of 65,536.
   // A wait of a whole warp; false ends the role.
   auto wait_warp = [&](uint32_t bar, uint32_t parity) {
-    return __all_sync(kFull, mbar_try_wait(bar, parity)) || wait_on(bar, parity, abort_flag, p.status, spin);
+#pragma unroll 1
+    for (int i = 0; i < spin; ++i) {
+      if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
+      if ((i & 255) == 255 && *abort_flag) return false;
+    }
+    *abort_flag = 1;
+    atomicOr(p.status, MEPIC_DEV_WAIT_EXPIRED);
+    return false;
   };
+
+  // The k-th segment, for a role other than the K loader; false ends the role (no more segments, or a lost wait).
+  auto take_segment = [&](int k, Segment& s) {
+    const int at = k % kSegRing;
+    if (!wait_warp(BAR(kBarSegFull, at), static_cast<uint32_t>(k / kSegRing) & 1u)) { s.t1 = -1; return false; }
+    const volatile Segment* v = &sm->seg[at];
+    s.t0 = v->t0; s.t1 = v->t1; s.b = v->b; s.h = v->h; s.row0 = v->row0; s.n = v->n; s.kvl = v->kvl; s.n_ctx = v->n_ctx; s.n_all = v->n_all;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(BAR(kBarSegFree, at));
+    return s.t1 > 0;
+  };
+  const int level = piece.level;
 
   if (has_work && warp < kSoftmaxWarps) {
     // =============================================================== softmax warps: thread = row (lane of tensor memory)
@@ -433,24 +512,24 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
     const int wg = warp >> 2, wq = warp & 3, r = tid & 127;      // row of the tile: drafted row r / G, query head r % G of the kv head
     const uint32_t t_row = tmem + (static_cast<uint32_t>(wq * 32) << 16);
     const int row_in_tile = r / G, g = r % G;
-    Walk w = walk_of(p, piece);
     Segment seg;
-    bool more = next_segment(p, w, seg);
-    auto put_q = [&](const Walk& a) {
-      const int at = a.level * p.rows_per_tile + row_in_tile;
-      stage_q<D>(p, Qs, row_in_tile < p.rows_per_tile && at < a.r.n, a.r.row0 + at, a.h * G + g, wg, r);
+    int n_seg = 0;
+    bool more = take_segment(n_seg++, seg);
+    auto put_q = [&](const Segment& a) {
+      const int at = level * p.rows_per_tile;
+      stage_q<D>(p, Qs, a.row0 + at, min(p.rows_per_tile, a.n - at), a.h * G, tid);
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(BAR(kBarQReady));
     };
-    put_q(w);
+    if (more) put_q(seg);
     int gi = 0, item = 0;                         // key tiles and items of this CTA so far
     bool ok = true, begun = false;
     while (more && ok) {
-      const int n = w.r.n, n_ctx = w.r.n_ctx, n_all = w.r.n_all, kvl = w.r.kvl, h = w.h, row0 = w.r.row0;
-      const int at = w.level * p.rows_per_tile + row_in_tile;            // this thread's drafted row within the request
+      const int n = seg.n, n_ctx = seg.n_ctx, n_all = seg.n_all, kvl = seg.kvl, h = seg.h, row0 = seg.row0;
+      const int at = level * p.rows_per_tile + row_in_tile;            // this thread's drafted row within the request
       const bool live = row_in_tile < p.rows_per_tile && at < n;
-      const bool warp_live = w.level * p.rows_per_tile + (wq * 32) / G < n;
+      const bool warp_live = level * p.rows_per_tile + (wq * 32) / G < n;
       const int t0 = seg.t0, t1 = seg.t1;
       float m_ref = -INFINITY, l_run = 0.f;       // reference at this warpgroup's latest tile, and its sum under it
 #pragma unroll 1
@@ -472,20 +551,30 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
             }
             return m;
           };
-          // ---- pass 1: the maximum of the row's 128 scores.  (Short loop bodies on purpose, here and in the other roles: the
-          // roles that share a scheduler run different code, and unrolled bodies - a row's scores held in registers, say - ran
-          // at a tenth of an instruction a clock out of the instruction cache.)
+          // (Short loop bodies, here and in the other roles: the roles that share a scheduler run different code, and what they
+          // wait for first is instructions.  A row's scores held in registers, chunks fetched ahead of their use, unrolled
+          // rotations: each saved latency on paper and lost time.)
+          if (masked) {
+            // hidden scores become -inf where they are, so that the passes below need not know
+#pragma unroll 1
+            for (int q = 0; q < 8; ++q) {
+              uint32_t sv[16];
+              TMEM_LD16(t_S + 16 * q, sv);
+              const uint32_t m = seen(q >> 1) >> (16 * (q & 1));
+              tmem_wait_ld();
+#pragma unroll
+              for (int c = 0; c < 16; ++c) sv[c] = (m >> c) & 1u ? sv[c] : 0xff800000u;
+              TMEM_ST16(t_S + 16 * q, sv);
+            }
+            tmem_wait_st();
+          }
+          // ---- pass 1: the maximum of the row's 128 scores
           float mx = -INFINITY;
 #pragma unroll 1
           for (int q = 0; q < 4; ++q) {
             uint32_t sv[32];
             TMEM_LD32(t_S + 32 * q, sv, 0);
             tmem_wait_ld();
-            if (masked) {
-              const uint32_t m = seen(q);
-#pragma unroll
-              for (int c = 0; c < 32; ++c) sv[c] = (m >> c) & 1u ? sv[c] : 0xff800000u;      // -inf
-            }
             float m4[4] = {mx, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int c = 0; c < 32; c += 8) {
@@ -529,30 +618,23 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
           const float2 ref2 = make_float2(m_use, m_use);
           float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
-          for (int q = 0; q < 4; ++q) {
-            uint32_t sv[32], pw[16];
-            TMEM_LD32(t_S + 32 * q, sv, 0);
+          for (int q = 0; q < 8; ++q) {                            // keys 16 q .. 16 q + 15
+            uint32_t sv[16], pw[8];
+            TMEM_LD16(t_S + 16 * q, sv);
+            const float s = FP8 ? sm->vs[gi % kScaleRing][q] : 1.f;              // the scale of the group's V block (1 for drafted rows)
             tmem_wait_ld();
-            if (masked) {
-              const uint32_t m = seen(q);
 #pragma unroll
-              for (int c = 0; c < 32; ++c) sv[c] = (m >> c) & 1u ? sv[c] : 0xff800000u;
-            }
-#pragma unroll
-            for (int c = 0; c < 32; c += 4) {
+            for (int c = 0; c < 16; c += 4) {
               const float2 d0 = sub2(make_float2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), ref2);
               const float2 d1 = sub2(make_float2(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), ref2);
               float2 p0 = make_float2(ex2(d0.x), ex2(d0.y)), p1 = make_float2(ex2(d1.x), ex2(d1.y));
               sum2[0] = add2(sum2[0], p0);
               sum2[1] = add2(sum2[1], p1);
-              if constexpr (FP8) {                                 // the scale of the key's V block (1 for drafted rows)
-                const float s = sm->vs[gi % kScaleRing][2 * q + c / 16];
-                p0 = mul2(p0, make_float2(s, s)); p1 = mul2(p1, make_float2(s, s));
-              }
+              if constexpr (FP8) { p0 = mul2(p0, make_float2(s, s)); p1 = mul2(p1, make_float2(s, s)); }
               pw[c / 2] = pack_bf16x2(p0.x, p0.y);
               pw[c / 2 + 1] = pack_bf16x2(p1.x, p1.y);
             }
-            TMEM_ST16(t_S + 16 * q, pw);
+            TMEM_ST8(t_S + 8 * q, pw);
           }
           l_run += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
           tmem_wait_st();
@@ -574,10 +656,9 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
       const float m_twin = *reinterpret_cast<volatile float*>(&sm->ref[wg ^ 1][r]), l_twin = *reinterpret_cast<volatile float*>(&sm->sum[wg ^ 1][r]);
       // the next item's q is staged while this one's last PV runs; the staged q is free once the last QK^T has completed
       if (!wait_warp(BAR(kBarSFull, last % 6), static_cast<uint32_t>(last / 6) & 1u)) { ok = false; break; }
-      Segment next;
-      const int level = w.level;
-      more = next_segment(p, w, next);
-      if (more) put_q(w);
+      more = take_segment(n_seg++, seg);
+      if (seg.t1 < 0) { ok = false; break; }
+      if (more) put_q(seg);
       // (a reference only ever rises, so the larger of the two is the one O is under)
       const float m_end = fmaxf(m_ref, m_twin);
       const float l_end = (m_ref == m_end ? l_run : l_run * ex2(m_ref - m_end)) + (m_twin == m_end ? l_twin : l_twin * ex2(m_twin - m_end));
@@ -640,7 +721,6 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
       __syncwarp();
       if (lane == 0) mbar_arrive(BAR(kBarOFree));
       ++item;
-      seg = next;
     }
     if (tid == 0 && !begun) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
   } else if (has_work && warp < kRotatorWarp0 + kRotatorWarps) {
@@ -661,13 +741,12 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
       oc[j] = make_float2(a.x, a.z); os[j] = make_float2(a.y, a.w);
       c1[j] = make_float2(b1.x, b1.z); s1[j] = make_float2(b1.y, b1.w); ns1[j] = make_float2(-b1.y, -b1.w);
     }
-    Walk w = walk_of(p, piece);
     Segment seg;
-    int gi = 0;
+    int gi = 0, n_seg = 0;
     bool ok = true;
-    while (ok && next_segment(p, w, seg)) {
-      const int n = w.r.n, n_ctx = w.r.n_ctx, kvl = w.r.kvl, row0 = w.r.row0, h = w.h;
-      const int32_t* bases = p.pos_base + static_cast<size_t>(w.b) * p.table_stride;
+    while (ok && take_segment(n_seg++, seg)) {
+      const int n = seg.n, n_ctx = seg.n_ctx, kvl = seg.kvl, row0 = seg.row0, h = seg.h;
+      const int32_t* bases = p.pos_base + static_cast<size_t>(seg.b) * p.table_stride;
       // position of the first slot of this thread's 16-slot group of tile t (0 where it has no slots), and its table row
       auto position = [&](int t) {
         const long long slot = static_cast<long long>(t) * kTileN + (k0 & ~15);
@@ -738,7 +817,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
             }
           }
         } else if (have) {
-#pragma unroll 2
+#pragma unroll 1
           for (int i = 0; i < KPT; ++i) {
             uint4* plo = reinterpret_cast<uint4*>(Kb + (lc / 8) * kBlockBytes + sw128(k0 + i, lc % 8));
             uint4* phi = reinterpret_cast<uint4*>(Kb + (hc / 8) * kBlockBytes + sw128(k0 + i, hc % 8));
@@ -841,29 +920,45 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
     unsigned char* ring = FP8 ? (is_k ? Kc : Vc) : (is_k ? Ks : Vs);
     constexpr int kRingStage = FP8 ? L::kCodes : L::kStage;
     const int depth = FP8 ? CD : (is_k ? KD : VD);
-    Walk w = walk_of(p, piece);
+    Walk w;
+    if (is_k) w = walk_of(sm->piece);
     Segment seg;
+    int n_seg = 0;
+    // the K loader finds the segments and publishes them; the V loader is one of those who read them
+    auto advance = [&]() {
+      if (!is_k) return take_segment(n_seg++, seg);
+      seg = next_segment(p, w);
+      const int at = n_seg % kSegRing;
+      if (n_seg >= kSegRing && !wait_warp(BAR(kBarSegFree, at), static_cast<uint32_t>(n_seg / kSegRing - 1) & 1u)) return false;
+      if (lane == 0) {
+        sm->seg[at] = seg;
+        mbar_arrive(BAR(kBarSegFull, at));
+      }
+      ++n_seg;
+      __syncwarp();
+      return seg.t1 > 0;
+    };
     struct Next { int page, slot0, h, left, row; bool live, draft, special; float ks, vs; };      // left: keys that exist; row: first drafted row
     auto look_up = [&](int t) {
-      const bool draft = t >= w.r.n_ctx;
-      const int left = min(draft ? w.r.n - (t - w.r.n_ctx) * kTileN : w.r.kvl - t * kTileN, kTileN);
-      Next x{0, 0, w.h, left, w.r.row0 + (t - w.r.n_ctx) * kTileN, false, draft, draft || left < kTileN, 1.f, 1.f};
+      const bool draft = t >= seg.n_ctx;
+      const int left = min(draft ? seg.n - (t - seg.n_ctx) * kTileN : seg.kvl - t * kTileN, kTileN);
+      Next x{0, 0, seg.h, left, seg.row0 + (t - seg.n_ctx) * kTileN, false, draft, draft || left < kTileN, 1.f, 1.f};
       const long long slot = static_cast<long long>(t) * kTileN + lane * 16;
-      x.live = !x.draft && lane < 8 && slot < w.r.kvl;
+      x.live = !x.draft && lane < 8 && slot < seg.kvl;
       if (x.live) {
-        const size_t e = static_cast<size_t>(w.b) * p.table_stride + static_cast<size_t>(slot >> p.page_shift);
+        const size_t e = static_cast<size_t>(seg.b) * p.table_stride + static_cast<size_t>(slot >> p.page_shift);
         x.slot0 = static_cast<int>(slot) & (p.page_size - 1);
         x.page = __ldg(p.page_ids + e);
         if (static_cast<unsigned>(x.page) >= static_cast<unsigned>(p.num_pages)) { atomicOr(p.status, MEPIC_DEV_BAD_PAGE); x.page = 0; }
         if (FP8 && is_k) {
-          const size_t block = static_cast<size_t>(x.page) * p.n_kv_heads + w.h;
+          const size_t block = static_cast<size_t>(x.page) * p.n_kv_heads + seg.h;
           x.ks = __ldg(p.k_scales + block);
           x.vs = __ldg(p.v_scales + block);
         }
       }
       return x;
     };
-    bool more = next_segment(p, w, seg);
+    bool more = advance();
     int t = seg.t0;
     Next nx = look_up(t);
     int gi = 0;
@@ -871,7 +966,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
     while (more) {
       Next x = nx;
       // the page ids of the tile after this one are on their way while this one waits for room
-      if (++t >= seg.t1) { more = next_segment(p, w, seg); t = seg.t0; }
+      if (++t >= seg.t1) { more = advance(); t = seg.t0; }
       if (more) nx = look_up(t);
       const int st = gi % depth;
       if (gi >= depth && !wait_warp(FP8 ? BAR(kBarCFree, is_k ? st : 2 + st) : BAR(is_k ? kBarKFree : kBarVFree, st), static_cast<uint32_t>(gi / depth - 1) & 1u)) break;
@@ -917,11 +1012,10 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
       // took 3,300 cycles a tile and held everything else up.
       const uint64_t q_desc = smem_desc(smem_u32(Qs), 16, 1024);
       const uint64_t k_desc0 = smem_desc(smem_u32(Ks), 16, 1024);
-      Walk w = walk_of(p, piece);
       Segment seg;
       bool ok = true;
-      int j = 0, items = 0;
-      while (ok && next_segment(p, w, seg)) {
+      int j = 0, items = 0, n_seg = 0;
+      while (ok && take_segment(n_seg++, seg)) {
         if (!wait_warp(BAR(kBarQReady), static_cast<uint32_t>(items++) & 1u)) { ok = false; break; }
 #pragma unroll 1
         for (int t = seg.t0; t < seg.t1; ++t, ++j) {
@@ -942,7 +1036,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
           __syncwarp();
         }
       }
-      if (!ok && lane == 0) {
+      if ((!ok || seg.t1 < 0) && lane == 0) {
         // a wait was lost: the MMAs issued so far still run; tensor memory may only be released once they are done
         tc_commit(BAR(kBarDrain, 0));
         for (int i = 0; i < spin && !mbar_try_wait(BAR(kBarDrain, 0), 0); ++i) {}
@@ -950,22 +1044,21 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
     } else {
       // =============================================================== PV issuer
       const uint64_t v_desc0 = smem_desc(smem_u32(Vs), kBlockBytes, 1024);
-      Walk w = walk_of(p, piece);
       Segment seg;
       bool ok = true;
-      int i = 0, items = 0;
+      int i = 0, items = 0, n_seg = 0;
       uint32_t v_parity = 0;                      // bit s: parity of the loader's own work on stage s
-      while (ok && next_segment(p, w, seg)) {
+      while (ok && take_segment(n_seg++, seg)) {
 #pragma unroll 1
         for (int t = seg.t0; t < seg.t1; ++t, ++i) {
           const int st = i % VD, sb = i % kSD;
-          const int left = min(t < w.r.n_ctx ? w.r.kvl - t * kTileN : w.r.n - (t - w.r.n_ctx) * kTileN, kTileN);
+          const int left = min(t < seg.n_ctx ? seg.kvl - t * kTileN : seg.n - (t - seg.n_ctx) * kTileN, kTileN);
           if (FP8) {
             if (!wait_warp(BAR(kBarVReady, st), static_cast<uint32_t>(i / VD) & 1u)) { ok = false; break; }      // the rotators fill every V stage
           } else if (!wait_warp(BAR(kBarVLanded, st), static_cast<uint32_t>(i / VD) & 1u)) {
             ok = false; break;
           }
-          if (!FP8 && (t >= w.r.n_ctx || left < kTileN)) {
+          if (!FP8 && (t >= seg.n_ctx || left < kTileN)) {
             if (!wait_warp(BAR(kBarVReady, st), (v_parity >> st) & 1u)) { ok = false; break; }
             v_parity ^= 1u << st;
           }
@@ -986,7 +1079,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
           __syncwarp();
         }
       }
-      if (!ok && lane == 0) {
+      if ((!ok || seg.t1 < 0) && lane == 0) {
         tc_commit(BAR(kBarDrain, 1));
         for (int k = 0; k < spin && !mbar_try_wait(BAR(kBarDrain, 1), 0); ++k) {}
       }
@@ -1000,47 +1093,50 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
 }
 
 // ---------------------------------------------------------------- merge of the parts of a divided item
-// Block (c, y) combines 16 rows of the item that CTA c began: m* = max m, l* = sum l 2^(m - m*), out = sum o 2^(m - m*) / l*.
-// A warp per row at a time; the parts' (m, l) are read side by side by its lanes, then the outputs four parts at a time.
-constexpr int kMergeRows = 16;
+// Block (c, y) combines four rows of the item that CTA c began, a warp each: m* = max m, l* = sum l 2^(m - m*),
+// out = sum o 2^(m - m*) / l*.  The parts' (m, l) are read side by side by the lanes, then the outputs eight parts at a time.
+// (Four rows to a warp, one after the other, took 11 us: a chain of a dozen trips to L2.)
+constexpr int kMergeRows = 4;
 template <int D>
-__global__ void __launch_bounds__(128) mepic_tree_merge(const TreeParams p) {
+__global__ void __launch_bounds__(kMergeRows * 32) mepic_tree_merge(const __grid_constant__ TreeParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");               // launched as a programmatic dependent of the attention kernel
   const int4 d = p.desc[blockIdx.x];
-  const int parts = d.w, G = p.group, lane = threadIdx.x & 31;
-  if (parts == 0) return;
-  for (int r = blockIdx.y * kMergeRows + (threadIdx.x >> 5); r < min(d.y * G, (static_cast<int>(blockIdx.y) + 1) * kMergeRows); r += 4) {
-    auto at = [&](int k) { return ((static_cast<size_t>(blockIdx.x) + k) * kSlots + (k == 0 ? 1 : 0)) * 128 + r; };
-    float m_star = -INFINITY;
-    for (int k = lane; k < parts; k += 32) m_star = fmaxf(m_star, p.part_ml[at(k)].x);
+  const int parts = d.w, G = p.group, lane = threadIdx.x & 31, r = blockIdx.y * kMergeRows + (threadIdx.x >> 5);
+  if (parts == 0 || r >= d.y * G) return;
+  auto at = [&](int k) { return ((static_cast<size_t>(blockIdx.x) + k) * kSlots + (k == 0 ? 1 : 0)) * 128 + r; };
+  float m_star = -INFINITY;
+  for (int k = lane; k < parts; k += 32) m_star = fmaxf(m_star, p.part_ml[at(k)].x);
 #pragma unroll
-    for (int s = 16; s; s >>= 1) m_star = fmaxf(m_star, __shfl_xor_sync(kFull, m_star, s));
-    float l_star = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = 0; k0 < parts; k0 += 32) {
-      float wgt = 0.f;
-      if (k0 + lane < parts) {
-        const float2 ml = p.part_ml[at(k0 + lane)];
-        wgt = ml.x == -INFINITY ? 0.f : ex2(ml.x - m_star);        // a part that held nothing this row sees
-        l_star += ml.x == -INFINITY ? ml.y : ml.y * wgt;           // (its sum is 0, or NaN, which must show)
-      }
-      const int n = min(32, parts - k0);
-#pragma unroll 4
-      for (int k = 0; k < n; ++k) {
-        const float wk = __shfl_sync(kFull, wgt, k);
-        if (wk != 0.f && lane < D / 4) {
-          const float4 x = *reinterpret_cast<const float4*>(p.part_o + at(k0 + k) * D + 4 * lane);
-          o.x += x.x * wk; o.y += x.y * wk; o.z += x.z * wk; o.w += x.w * wk;
-        }
-      }
+  for (int s = 16; s; s >>= 1) m_star = fmaxf(m_star, __shfl_xor_sync(kFull, m_star, s));
+  float l_star = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int k0 = 0; k0 < parts; k0 += 8) {
+    float wgt = 0.f;
+    if (lane < 8 && k0 + lane < parts) {
+      const float2 ml = p.part_ml[at(k0 + lane)];
+      wgt = ml.x == -INFINITY ? 0.f : ex2(ml.x - m_star);          // a part that held nothing this row sees
+      l_star += ml.x == -INFINITY ? ml.y : ml.y * wgt;             // (its sum is 0, or NaN, which must show)
+    }
+    float4 x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (k0 + k < parts && lane < D / 4) x[k] = *reinterpret_cast<const float4*>(p.part_o + at(k0 + k) * D + 4 * lane);
     }
 #pragma unroll
-    for (int s = 16; s; s >>= 1) l_star += __shfl_xor_sync(kFull, l_star, s);
-    const float inv = l_star == 0.f ? 0.f : 1.f / l_star;
-    if (lane < D / 4) {
-      const size_t to = (static_cast<size_t>(d.x + r / G) * (p.n_kv_heads * G) + static_cast<size_t>(d.z) * G + r % G) * D + 4 * lane;
-      *reinterpret_cast<uint2*>(p.out + to) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    for (int k = 0; k < 8; ++k) {
+      const float wk = __shfl_sync(kFull, wgt, k);
+      if (wk != 0.f) { o.x += x[k].x * wk; o.y += x[k].y * wk; o.z += x[k].z * wk; o.w += x[k].w * wk; }
     }
+  }
+#pragma unroll
+  for (int s = 4; s; s >>= 1) l_star += __shfl_xor_sync(kFull, l_star, s);
+  l_star = __shfl_sync(kFull, l_star, 0);
+  const float inv = l_star == 0.f ? 0.f : 1.f / l_star;
+  if (lane < D / 4) {
+    const size_t to = (static_cast<size_t>(d.x + r / G) * (p.n_kv_heads * G) + static_cast<size_t>(d.z) * G + r % G) * D + 4 * lane;
+    *reinterpret_cast<uint2*>(p.out + to) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
   }
 }
 
@@ -1053,7 +1149,7 @@ int32_t launch_tree(const TreeParams& p, int ctas, const CUtensorMap& map_k, con
   e = cudaGetLastError();
   if (e == cudaSuccess) {
     const int live = std::min(p.max_rows, p.rows_per_tile) * p.group;
-    e = launch_dependent(mepic_tree_merge<D>, dim3(ctas, (live + kMergeRows - 1) / kMergeRows), dim3(128), st, p);
+    e = launch_dependent(mepic_tree_merge<D>, dim3(ctas, (live + kMergeRows - 1) / kMergeRows), dim3(kMergeRows * 32), st, p);
   }
   if (e != cudaSuccess) { mepic_set_error("attn_tree: launch: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
   mepic_count_launches(2);

@@ -390,8 +390,11 @@ class _StepCall:
         if torch.cuda.current_device() != self._index:
             with torch.cuda.device(self._index):
                 return self._launch(stream)
-        s = stream if stream is not None else torch.cuda.current_stream(self._index)
-        code = self._fn(*self._argv, s if isinstance(s, int) else s.cuda_stream)
+        if stream is None:
+            s = torch._C._cuda_getCurrentRawStream(self._index)      # the current stream's handle without a Stream object around it
+        else:
+            s = stream if isinstance(stream, int) else stream.cuda_stream
+        code = self._fn(*self._argv, s)
         if code:
             _check(code)
 
@@ -412,10 +415,11 @@ class TreeLayout(_StepCall):
                    _TreeLayoutArgsC(parent.data_ptr(), row_offsets.data_ptr(), kv_len.data_ptr(), pos_base.data_ptr(), self.row_pos.data_ptr(),
                                     self.tree_mask.data_ptr(), dev.status.data_ptr(), pos_base.shape[1], batch, rows, mask_words),
                    keep=(parent, row_offsets, kv_len, pos_base))
+        self._result = dict(row_pos=self.row_pos, tree_mask=self.tree_mask)
 
     def run(self, stream=None):
         self._launch(stream)
-        return dict(row_pos=self.row_pos, tree_mask=self.tree_mask)
+        return self._result
 
 
 class TreeBatch(_StepCall):
@@ -467,10 +471,11 @@ class TreeAccept(_StepCall):
                                     self.n_accept.data_ptr(), self.accept_rows.data_ptr(), self.next_token.data_ptr(),
                                     dev.status.data_ptr(), batch, rows, max_accept),
                    with_cfg=False, keep=(parent, row_offsets, draft, target, root))
+        self._result = dict(n_accept=self.n_accept, accept_rows=self.accept_rows, next_token=self.next_token)
 
     def run(self, stream=None):
         self._launch(stream)
-        return dict(n_accept=self.n_accept, accept_rows=self.accept_rows, next_token=self.next_token)
+        return self._result
 
 
 class StepTables(_StepCall):
@@ -492,11 +497,12 @@ class StepTables(_StepCall):
                                     self.slot_map.data_ptr() or None, self.kv_len_out.data_ptr(), self.q_pos.data_ptr(),
                                     self.reserve_used_out.data_ptr(), dev.status.data_ptr(), page_ids.shape[1], batch, max_rows, reserve.numel()),
                    keep=(kv_len, n_new, page_ids, pos_base, reserve, reserve_used))
+        self._result = dict(row_offsets=self.row_offsets, row_slot=self.row_slot, slot_map=self.slot_map, kv_len=self.kv_len_out,
+                            q_pos=self.q_pos, reserve_used=self.reserve_used_out)
 
     def run(self, stream=None):
         self._launch(stream)
-        return dict(row_offsets=self.row_offsets, row_slot=self.row_slot, slot_map=self.slot_map, kv_len=self.kv_len_out, q_pos=self.q_pos,
-                    reserve_used=self.reserve_used_out)
+        return self._result
 
     def advance(self) -> None:
         """The step's lengths and its use of the reserve become the next step's inputs (on the current stream)."""
