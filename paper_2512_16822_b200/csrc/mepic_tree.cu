@@ -537,20 +537,24 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
         if ((gi & 1) != wg) continue;
         const int sb = gi % kSD;
         const uint32_t t_S = t_row + static_cast<uint32_t>(sb * 128);
-        if (!wait_warp(BAR(kBarSFull, gi % 6), static_cast<uint32_t>(gi / 6) & 1u)) { ok = false; break; }
-        tc_fence_after();
-        if (warp_live) {
-          const int left = t < n_ctx ? kvl - t * kTileN : n - (t - n_ctx) * kTileN;      // keys that exist
-          const bool masked = t >= n_ctx || left < kTileN;
-          // which of keys 32 q .. 32 q + 31 of the tile this row sees (asked only where masked)
-          auto seen = [&](int q) {
+        // which of the tile's keys this row sees, where that is not all of them: bit c of word q = key 32 q + c
+        const int left = t < n_ctx ? kvl - t * kTileN : n - (t - n_ctx) * kTileN;        // keys that exist
+        const bool masked = t >= n_ctx || left < kTileN;
+        uint32_t vis[4] = {~0u, ~0u, ~0u, ~0u};
+        if (masked && warp_live) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
             uint32_t m = left >= 32 * (q + 1) ? ~0u : (left <= 32 * q ? 0u : (1u << (left - 32 * q)) - 1u);
             if (t >= n_ctx) {
               const int wd = (t - n_ctx) * 4 + q;
               m &= live && wd < p.mask_words ? static_cast<uint32_t>(__ldg(p.tree_mask + static_cast<size_t>(row0 + at) * p.mask_words + wd)) : 0u;
             }
-            return m;
-          };
+            vis[q] = m;
+          }
+        }
+        if (!wait_warp(BAR(kBarSFull, gi % 6), static_cast<uint32_t>(gi / 6) & 1u)) { ok = false; break; }
+        tc_fence_after();
+        if (warp_live) {
           // (Short loop bodies, here and in the other roles: the roles that share a scheduler run different code, and what they
           // wait for first is instructions.  A row's scores held in registers, chunks fetched ahead of their use, unrolled
           // rotations: each saved latency on paper and lost time.)
@@ -560,7 +564,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
             for (int q = 0; q < 8; ++q) {
               uint32_t sv[16];
               TMEM_LD16(t_S + 16 * q, sv);
-              const uint32_t m = seen(q >> 1) >> (16 * (q & 1));
+              const uint32_t m = (q < 4 ? (q < 2 ? vis[0] : vis[1]) : (q < 6 ? vis[2] : vis[3])) >> (16 * (q & 1));
               tmem_wait_ld();
 #pragma unroll
               for (int c = 0; c < 16; ++c) sv[c] = (m >> c) & 1u ? sv[c] : 0xff800000u;
@@ -964,22 +968,19 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
     int gi = 0;
 #pragma unroll 1
     while (more) {
-      Next x = nx;
-      // the page ids of the tile after this one are on their way while this one waits for room
-      if (++t >= seg.t1) { more = advance(); t = seg.t0; }
-      if (more) nx = look_up(t);
+      const Next x = nx;
       const int st = gi % depth;
       if (gi >= depth && !wait_warp(FP8 ? BAR(kBarCFree, is_k ? st : 2 + st) : BAR(is_k ? kBarKFree : kBarVFree, st), static_cast<uint32_t>(gi / depth - 1) & 1u)) break;
       const uint32_t landed = is_k ? BAR(kBarKLanded, gi % 6) : BAR(kBarVLanded, st);
       if (FP8 && is_k && lane < 8) { sm->ks[gi & 1][lane] = x.ks; sm->vs[gi % kScaleRing][lane] = x.vs; }
       const unsigned live = __ballot_sync(kFull, x.live);
-      if (HOOKS && is_k && blockIdx.x == 0 && gi == p.skip_tile) { ++gi; continue; }      // (test hook: a K tile that never comes)
-      if (lane == 0) {
+      const bool skip = HOOKS && is_k && blockIdx.x == 0 && gi == p.skip_tile;      // (test hook: a K tile that never comes)
+      if (lane == 0 && !skip) {
         if (live) mbar_expect_tx(landed, static_cast<uint32_t>(__popc(live)) * kGroupBytes);
         else mbar_arrive(landed);                 // drafted rows: the rotators and the V loader bring them into the stage
       }
       __syncwarp();
-      if (x.live) {
+      if (x.live && !skip) {
         const uint32_t dst = smem_u32(ring + st * kRingStage) + static_cast<uint32_t>(lane * 16 * 128);
         if constexpr (FP8) {
           const size_t row = (static_cast<size_t>(x.page) * p.n_kv_heads + x.h) * p.page_size + x.slot0;      // of the pool viewed as [rows][128 bytes]
@@ -999,6 +1000,9 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(kBarVReady, st));
       }
+      // the page ids of the next tile are on their way while this role waits for room for it
+      if (++t >= seg.t1) { more = advance(); t = seg.t0; }
+      if (more) nx = look_up(t);
       ++gi;
     }
     // after a lost wait: give the copies started last a bounded chance to land before shared memory is given up
