@@ -39,6 +39,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstring>
 
 #include "mepic.h"
@@ -1145,10 +1146,16 @@ __global__ void __launch_bounds__(kMergeRows * 32) mepic_tree_merge(const __grid
 }
 
 template <int D, bool FP8, bool HOOKS>
-int32_t launch_tree(const TreeParams& p, int ctas, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t st) {
+int32_t launch_tree(const TreeParams& p, int ctas, int device, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t st) {
   constexpr int smem = TreeSmem<D, FP8>::kBytes;
-  cudaError_t e = cudaFuncSetAttribute(mepic_tree_attn<D, FP8, HOOKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) { mepic_set_error("attn_tree: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  static std::atomic<uint64_t> prepared{0};      // bit d: the kernel's shared-memory limit is set on device d
+  cudaError_t e = cudaSuccess;
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (!(prepared.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(mepic_tree_attn<D, FP8, HOOKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) { mepic_set_error("attn_tree: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+    prepared.fetch_or(bit, std::memory_order_relaxed);
+  }
   mepic_tree_attn<D, FP8, HOOKS><<<ctas, kThreads, smem, st>>>(p, map_k, map_v);
   e = cudaGetLastError();
   if (e == cudaSuccess) {
@@ -1160,9 +1167,15 @@ int32_t launch_tree(const TreeParams& p, int ctas, const CUtensorMap& map_k, con
   return MEPIC_OK;
 }
 
-int sm_count() {
+// SM count of the current device (0 without one); *device: its index.
+int sm_count(int* device) {
+  static std::atomic<int> known[64];             // a device's count does not change: asked once
   int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  *device = dev;
+  if (dev < 64 && (sms = known[dev].load(std::memory_order_relaxed)) > 0) return sms;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  if (dev < 64) known[dev].store(sms, std::memory_order_relaxed);
   return sms;
 }
 int rows_per_tile(const mepic_config_t* cfg) { return 128 / (cfg->n_q_heads / cfg->n_kv_heads); }
@@ -1174,9 +1187,10 @@ int cta_count(const mepic_config_t* cfg, int max_rows, int sms) {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-size_t workspace_bytes(const mepic_config_t* cfg, int max_rows) {
-  const int sms = sm_count();
+size_t workspace_bytes(const mepic_config_t* cfg, int max_rows, int* device, int* sms_out) {
+  const int sms = sm_count(device);
   if (sms <= 0) { mepic_set_error("attn_tree: no CUDA device"); return 0; }
+  *sms_out = sms;
   const size_t n = static_cast<size_t>(cta_count(cfg, max_rows, sms));
   return n * (sizeof(int4) + kSlots * 128 * (sizeof(float2) + static_cast<size_t>(cfg->head_dim) * sizeof(float)));
 }
@@ -1204,7 +1218,8 @@ int32_t tree_call(const mepic_config_t* cfg, const mepic_attn_tree_args_t* a, co
   if (q_packed > 0x7fffffffLL || q_stride < q_packed || kv_stride < kv_packed || q_stride % 8 || kv_stride % 8) {
     mepic_set_error("%s: row strides must be 0 or multiples of 8 of at least a packed row", what); return MEPIC_E_INVAL;
   }
-  const size_t need = workspace_bytes(cfg, a->max_rows);
+  int device = 0, sms = 0;
+  const size_t need = workspace_bytes(cfg, a->max_rows, &device, &sms);
   if (need == 0) return MEPIC_E_CUDA;
   if (a->workspace_bytes < need) { mepic_set_error("%s: workspace of %zu bytes, %zu needed", what, a->workspace_bytes, need); return MEPIC_E_INVAL; }
   TreeParams p;
@@ -1222,7 +1237,7 @@ int32_t tree_call(const mepic_config_t* cfg, const mepic_attn_tree_args_t* a, co
   p.group = cfg->n_q_heads / cfg->n_kv_heads;
   p.rows_per_tile = rows_per_tile(cfg);
   p.max_levels = (a->max_rows + p.rows_per_tile - 1) / p.rows_per_tile;
-  const int ctas = cta_count(cfg, a->max_rows, sm_count());
+  const int ctas = cta_count(cfg, a->max_rows, sms);
   unsigned char* ws = static_cast<unsigned char*>(a->workspace);
   p.desc = reinterpret_cast<int4*>(ws);
   p.part_ml = reinterpret_cast<float2*>(ws + sizeof(int4) * ctas);
@@ -1238,9 +1253,9 @@ int32_t tree_call(const mepic_config_t* cfg, const mepic_attn_tree_args_t* a, co
   }
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const bool hooks = p.spin_limit != kSpinLimit || p.skip_tile >= 0;
-  if (cfg->head_dim == 64) return hooks ? launch_tree<64, false, true>(p, ctas, map_k, map_v, st) : launch_tree<64, false, false>(p, ctas, map_k, map_v, st);
-  if (fp8) return hooks ? launch_tree<128, true, true>(p, ctas, map_k, map_v, st) : launch_tree<128, true, false>(p, ctas, map_k, map_v, st);
-  return hooks ? launch_tree<128, false, true>(p, ctas, map_k, map_v, st) : launch_tree<128, false, false>(p, ctas, map_k, map_v, st);
+  if (cfg->head_dim == 64) return hooks ? launch_tree<64, false, true>(p, ctas, device, map_k, map_v, st) : launch_tree<64, false, false>(p, ctas, device, map_k, map_v, st);
+  if (fp8) return hooks ? launch_tree<128, true, true>(p, ctas, device, map_k, map_v, st) : launch_tree<128, true, false>(p, ctas, device, map_k, map_v, st);
+  return hooks ? launch_tree<128, false, true>(p, ctas, device, map_k, map_v, st) : launch_tree<128, false, false>(p, ctas, device, map_k, map_v, st);
 }
 
 }  // namespace
@@ -1248,7 +1263,8 @@ int32_t tree_call(const mepic_config_t* cfg, const mepic_attn_tree_args_t* a, co
 extern "C" size_t mepic_attn_tree_workspace(const mepic_config_t* cfg, int32_t max_rows) {
   if (!mepic_config_ok(cfg)) return 0;
   if (max_rows < 0 || max_rows > MEPIC_TREE_MAX_ROWS) { mepic_set_error("attn_tree_workspace: max_rows %d not in 0..%d", max_rows, MEPIC_TREE_MAX_ROWS); return 0; }
-  return workspace_bytes(cfg, max_rows);
+  int device = 0, sms = 0;
+  return workspace_bytes(cfg, max_rows, &device, &sms);
 }
 extern "C" int32_t mepic_attn_tree(const mepic_config_t* cfg, const mepic_attn_tree_args_t* a, void* cuda_stream) {
   return tree_call(cfg, a, nullptr, nullptr, false, cuda_stream);

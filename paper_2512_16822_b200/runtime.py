@@ -387,11 +387,11 @@ class _StepCall:
         self._argv = ((C.byref(self._cfg),) if with_cfg else ()) + (C.byref(args),) + tuple(extra)
 
     def _launch(self, stream=None) -> None:
-        if torch.cuda.current_device() != self._index:
-            with torch.cuda.device(self._index):
+        if torch._C._cuda_getDevice() != self._index:                # (the private forms of current_device and current_stream: the
+            with torch.cuda.device(self._index):                     # public ones cost as much as the launch)
                 return self._launch(stream)
         if stream is None:
-            s = torch._C._cuda_getCurrentRawStream(self._index)      # the current stream's handle without a Stream object around it
+            s = torch._C._cuda_getCurrentRawStream(self._index)
         else:
             s = stream if isinstance(stream, int) else stream.cuda_stream
         code = self._fn(*self._argv, s)
