@@ -28,9 +28,9 @@
 //                   of the tile after next fetched while the ring is full.  The V loader also clears V rows past kv_len,
 //                   brings the drafted V rows and takes non-finite elements out of them: 0 x inf would reach rows that the
 //                   mask hides them from.  The rows that do see such an element get it added in the epilogue.
-//                   Over 8-bit pages the loaders bring the codes into rings of their own (untiled bulk copies) and the
-//                   rotators widen them, K on the way through the rotation and then V; the K scales go into (cos, sin), the V
-//                   scales into P.
+//                   Over 8-bit pages the loaders bring the codes into rings of their own (untiled bulk copies); the rotators
+//                   widen K on the way through the rotation, the softmax warps V; the K scales go into (cos, sin), the V scales
+//                   into P.
 //   MMA warps     : one issues S = Q' K'^T (three score buffers, each of which becomes its tile's P), one O += P V.
 // Every wait is bounded; a lost wait raises a flag that ends every role.
 #include <cuda.h>
@@ -452,7 +452,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
   if (tid == 0) {
     for (int s = 0; s < 3; ++s) {
       mbar_init(BAR(kBarKReady, s), kRotGroupWarps); mbar_init(BAR(kBarKFree, s), 1);
-      mbar_init(BAR(kBarVLanded, s), 1); mbar_init(BAR(kBarVReady, s), FP8 ? kRotGroupWarps : 1); mbar_init(BAR(kBarVFree, s), 1);
+      mbar_init(BAR(kBarVLanded, s), 1); mbar_init(BAR(kBarVReady, s), FP8 ? 4 : 1); mbar_init(BAR(kBarVFree, s), 1);
       mbar_init(BAR(kBarPFull, s), 4); mbar_init(BAR(kBarPvDone, s), 1);
     }
     for (int s = 0; s < 4; ++s) mbar_init(BAR(kBarCFree, s), kRotGroupWarps);
@@ -523,9 +523,55 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
       __syncwarp();
       if (lane == 0) mbar_arrive(BAR(kBarQReady));
     };
+    // 8-bit pages: key tile t of segment a, this CTA's tile i, from V codes to the bf16 stage the PV product reads (their scale
+    // goes into P).  A warpgroup widens the V of the tile after its own, which the other warpgroup is at: the V stage is free
+    // by then, and the rotators, who have K, are the busier role.  (K and V by the rotators: 520 us on 8 x 65,536 slots.)
+    auto widen_v = [&](int i, int t, const Segment& a) {
+      const int rt = tid & 127, st = i % VD;
+      unsigned char* Vb = Vs + st * L::kStage;
+      if (!wait_warp(BAR(kBarVLanded, i % CD), static_cast<uint32_t>(i / CD) & 1u)) return false;
+      if (i >= VD && !wait_warp(BAR(kBarVFree, st), static_cast<uint32_t>(i / VD - 1) & 1u)) return false;
+      const bool draft = t >= a.n_ctx;
+      const int left = min(draft ? a.n - (t - a.n_ctx) * kTileN : a.kvl - t * kTileN, kTileN);
+      const int end = (left + 15) & ~15;           // the PV product goes over whole groups of 16 keys
+      if (draft) {
+#pragma unroll 1
+        for (int i0 = rt & ~31; i0 < end * 2 * CH; i0 += 128 * 8)
+          mend_rows<D>(p, Vb, &sm->odd_v, true, left, a.row0 + (t - a.n_ctx) * kTileN, a.h, i0 + lane, 128);
+      } else {
+        const unsigned char* codes = Vc + (i % CD) * L::kCodes;
+#pragma unroll 1
+        for (int idx = rt; idx < end * 8; idx += 128) {
+          const int kk = idx >> 3, ch = 2 * (idx & 7);
+          uint32_t w8[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+          if (kk < left) {
+            const uint4 cd = *reinterpret_cast<const uint4*>(codes + kk * 128 + 8 * ch);
+            const uint32_t cw[4] = {cd.x, cd.y, cd.z, cd.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t f0, f1;
+              e4m3x4_to_f16x2x2(cw[j], f0, f1);
+              const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&f0)), y = __half22float2(*reinterpret_cast<const __half2*>(&f1));
+              w8[2 * j] = pack_bf16x2(x.x, x.y);
+              w8[2 * j + 1] = pack_bf16x2(y.x, y.y);
+            }
+          }
+          *reinterpret_cast<uint4*>(Vb + (ch / 8) * kBlockBytes + sw128(kk, ch % 8)) = make_uint4(w8[0], w8[1], w8[2], w8[3]);
+          *reinterpret_cast<uint4*>(Vb + (ch / 8) * kBlockBytes + sw128(kk, ch % 8 + 1)) = make_uint4(w8[4], w8[5], w8[6], w8[7]);
+        }
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(BAR(kBarVReady, st));
+        mbar_arrive(BAR(kBarCFree, 2 + i % CD));
+      }
+      return true;
+    };
     if (more) put_q(seg);
     int gi = 0, item = 0;                         // key tiles and items of this CTA so far
     bool ok = true, begun = false;
+    if (FP8 && more && wg == 1) ok = widen_v(0, seg.t0, seg);
     while (more && ok) {
       const int n = seg.n, n_ctx = seg.n_ctx, n_all = seg.n_all, kvl = seg.kvl, h = seg.h, row0 = seg.row0;
       const int at = level * p.rows_per_tile + row_in_tile;            // this thread's drafted row within the request
@@ -649,6 +695,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(kBarPFull, sb));
+        if (FP8 && t + 1 < t1 && !widen_v(gi + 1, t + 1, seg)) { ok = false; break; }
       }
       if (!ok) break;
       // ---- the item's end: the twins exchange their sums
@@ -664,6 +711,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
       more = take_segment(n_seg++, seg);
       if (seg.t1 < 0) { ok = false; break; }
       if (more) put_q(seg);
+      if (FP8 && more && (last & 1) == wg && !widen_v(gi, seg.t0, seg)) { ok = false; break; }
       // (a reference only ever rises, so the larger of the two is the one O is under)
       const float m_end = fmaxf(m_ref, m_twin);
       const float l_end = (m_ref == m_end ? l_run : l_run * ex2(m_ref - m_end)) + (m_twin == m_end ? l_twin : l_twin * ex2(m_twin - m_end));
@@ -874,47 +922,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(kBarKReady, ks));
-        if constexpr (FP8) {
-          // ---- 8-bit pages: the V tile too, codes widened exactly (their scale goes into P)
-          const int vst = gi % VD;
-          unsigned char* Vb = Vs + vst * L::kStage;
-          if (lane == 0) mbar_arrive(BAR(kBarCFree, gi % CD));                  // the K codes have been read
-          if (!wait_warp(BAR(kBarVLanded, gi % CD), static_cast<uint32_t>(gi / CD) & 1u)) { ok = false; break; }
-          if (gi >= VD && !wait_warp(BAR(kBarVFree, vst), static_cast<uint32_t>(gi / VD - 1) & 1u)) { ok = false; break; }
-          if (draft) {
-            for (int i0 = rt & ~31; i0 < ((left + 15) & ~15) * 2 * CH; i0 += kRotators * 8)
-              mend_rows<D>(p, Vb, &sm->odd_v, true, left, row0 + (t - n_ctx) * kTileN, h, i0 + lane, kRotators);
-          } else {
-            const unsigned char* codes = Vc + (gi % CD) * L::kCodes;
-            const int end = (left + 15) & ~15;     // the PV product goes over whole groups of 16 keys
-#pragma unroll 1
-            for (int idx = rt; idx < end * 8; idx += kRotators) {
-              const int kk = idx >> 3, c16 = idx & 7;
-              uint32_t w8[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-              if (kk < left) {
-                const uint4 cd = *reinterpret_cast<const uint4*>(codes + kk * 128 + 16 * c16);
-                const uint32_t cw[4] = {cd.x, cd.y, cd.z, cd.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  uint32_t f0, f1;
-                  e4m3x4_to_f16x2x2(cw[j], f0, f1);
-                  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&f0)), y = __half22float2(*reinterpret_cast<const __half2*>(&f1));
-                  w8[2 * j] = pack_bf16x2(x.x, x.y);
-                  w8[2 * j + 1] = pack_bf16x2(y.x, y.y);
-                }
-              }
-              const int ch = 2 * c16;
-              *reinterpret_cast<uint4*>(Vb + (ch / 8) * kBlockBytes + sw128(kk, ch % 8)) = make_uint4(w8[0], w8[1], w8[2], w8[3]);
-              *reinterpret_cast<uint4*>(Vb + (ch / 8) * kBlockBytes + sw128(kk, ch % 8 + 1)) = make_uint4(w8[4], w8[5], w8[6], w8[7]);
-            }
-          }
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(BAR(kBarVReady, vst));
-            mbar_arrive(BAR(kBarCFree, 2 + gi % CD));
-          }
-        }
+        if (FP8 && lane == 0) mbar_arrive(BAR(kBarCFree, gi % CD));             // the K codes have been read
       }
     }
   } else if (has_work) {
@@ -1059,7 +1067,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
           const int st = i % VD, sb = i % kSD;
           const int left = min(t < seg.n_ctx ? seg.kvl - t * kTileN : seg.n - (t - seg.n_ctx) * kTileN, kTileN);
           if (FP8) {
-            if (!wait_warp(BAR(kBarVReady, st), static_cast<uint32_t>(i / VD) & 1u)) { ok = false; break; }      // the rotators fill every V stage
+            if (!wait_warp(BAR(kBarVReady, st), static_cast<uint32_t>(i / VD) & 1u)) { ok = false; break; }      // the softmax warps fill every V stage
           } else if (!wait_warp(BAR(kBarVLanded, st), static_cast<uint32_t>(i / VD) & 1u)) {
             ok = false; break;
           }
