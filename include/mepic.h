@@ -240,7 +240,7 @@ int32_t mepic_store_test_hooks(mepic_store_t* store, uint64_t hash_mask, int32_t
  * flight land, releases what it holds and returns; the results of that call are undefined, the GPU and the
  * context stay usable.  spin_limit > 0 replaces the built-in poll limit (about a second) for calls made from now
  * on, 0 restores it.  skip_tile >= 0 makes the first worker of every such call (warp 0 of CTA 0 in the decode
- * kernels, the K loader of CTA 0 in the prefill kernel) leave out the staged copy of its tile with that index, so
+ * kernels, the K loader of CTA 0 in the prefill and tree kernels) leave out the staged copy of its tile with that index, so
  * that the barrier that copy would complete is a flag nothing sets and the wait on it expires; -1 restores normal
  * operation.  Process-wide; not for production use.  Errors: E_INVAL.
  */

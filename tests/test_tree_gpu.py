@@ -328,3 +328,82 @@ def test_no_rows_launch_nothing():
     RT.TreeBatch(case.dev, q=q, k_new=k, v_new=k, row_offsets=dev32([0, 0]), row_pos=dev32([]), tree_mask=torch.empty((0, 1), dtype=torch.int32, device="cuda:0"),
                  page_ids=dev32(case.page_ids), pos_base=dev32(case.pos_base), kv_len=dev32(case.kv_len), max_rows=0).run(0.1)
     assert M.mepic_launch_count() == before
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_pages_whose_elements_lie_past_32_bits(fp8):
+    # pools of 2.6 G elements each; the case's pages are spread over them, the last page included, and the rest is never read.
+    # Committed rows land there too.
+    Hkv, P, D, pages = 8, 64, 128, 40000
+    case = TreeCase(60, Hq=8, Hkv=Hkv, D=D, P=P, specs=[(700, 5), (130, 3)], jitter=False, fp8=fp8)
+    case.device()
+    small = case.dev
+    where = np.linspace(1000, pages - 1, case.num_pages).astype(np.int64)
+    cfg = M.Config(P, 8, Hkv, D, pages, case.max_position, case.theta)
+    src = (small.k_pool, small.v_pool) if not fp8 else (case.pools.k_codes, case.pools.v_codes)
+    big = [torch.empty((pages, Hkv, P, D), dtype=s.dtype, device="cuda:0") for s in src]
+    for b, s in zip(big, src):
+        b[torch.from_numpy(where).cuda()] = s
+    pools = None
+    if fp8:
+        scales = []
+        for s in (case.pools.k_scales, case.pools.v_scales):
+            scales.append(torch.ones((pages, Hkv), dtype=torch.float32, device="cuda:0"))
+            scales[-1][torch.from_numpy(where).cuda()] = s
+    dev = RT.Device.over(cfg, None if fp8 else big[0], None if fp8 else big[1])
+    if fp8:
+        pools = RT.Fp8Pools.over(dev, *big, *scales)
+    ids = np.where(case.page_ids >= 0, where[np.maximum(case.page_ids, 0)], -1)
+    q, k, v = case.fused()
+    out = RT.TreeBatch(dev, q=q, k_new=k, v_new=v, row_offsets=dev32(case.off), row_pos=dev32(np.concatenate(case.row_pos)),
+                       tree_mask=dev32(case.mask()), page_ids=dev32(ids), pos_base=dev32(case.pos_base), kv_len=dev32(case.kv_len),
+                       max_rows=5, pools=pools).run(0.09)
+    torch.cuda.synchronize()
+    assert dev.read_status() == 0
+    case.check(out, 0.09)
+    slots = torch.tensor([(pages - 1) * P + P - 8 + i for i in range(8)], dtype=torch.int64, device="cuda:0")
+    if fp8:
+        scales[0][-1], scales[1][-1] = 0.5, 0.25
+    RT.RowsCommit(dev, k_new=k, v_new=v, row_offsets=dev32([0, 8]), slot_map=slots, pools=pools).run()
+    torch.cuda.synchronize()
+    assert dev.read_status() == 0
+    for b, new, sc in ((big[0], case.kn, 0.5), (big[1], case.vn, 0.25)):
+        got = b[-1, :, P - 8:].transpose(0, 1)
+        if fp8:
+            want = O.e4m3_encode((bf16_bits_to_f64(new).astype(np.float32) / np.float32(sc)))
+            assert np.array_equal(got.cpu().numpy(), want)
+        else:
+            assert np.array_equal(RT.bf16_bits(got.contiguous()), new)
+
+
+def test_use_on_another_stream_than_the_tensors_were_made_on():
+    case = TreeCase(61, Hq=8, Hkv=2, D=128, P=16, specs=[(1500, 9), (40, 3)])
+    case.device()
+    batch = case.batch()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out = batch.run(0.09)                       # no stream named: the current one, which is `side`
+        done = out.clone()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert case.dev.read_status() == 0
+    case.check(done, 0.09)
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_random_shapes(seed):
+    rng = np.random.default_rng(1000 + seed)
+    Hkv = int(rng.choice([1, 2, 3]))
+    G = int(rng.integers(1, 9))
+    fp8 = bool(rng.integers(0, 2))
+    D = 128 if fp8 else int(rng.choice([64, 128]))
+    P = int(rng.choice([16, 32, 64, 256]))
+    specs = [(int(rng.choice([0, 1, 5, int(rng.integers(1, 1500))])), int(rng.choice([0, 1, int(rng.integers(1, 70))]))) for _ in range(int(rng.integers(1, 9)))]
+    if not any(n for _, n in specs):
+        specs[0] = (specs[0][0], 7)
+    case = TreeCase(seed, Hq=Hkv * G, Hkv=Hkv, D=D, P=P, specs=specs, kind=str(rng.choice(["tree", "chain", "star"])), fp8=fp8, theta=float(rng.choice([1e4, 5e5])))
+    for s in case.sees:                             # any relation, not only a tree's
+        if rng.integers(0, 2):
+            s ^= rng.random(s.shape) < 0.2
+    _run(case, 1.0 / np.sqrt(D), max_rows=min(32 * case.words, int(case.rows.max()) + int(rng.integers(0, 5))))

@@ -56,7 +56,7 @@ class TreeCase:
             pos, sees = O.tree_layout(p, nxt)
             self.parents.append(p), self.row_pos.append(pos), self.sees.append(sees)
         self.words = max(1, -(-int(self.rows.max()) // 32))
-        self.max_position = max([int(x) for p in self.row_pos for x in p] + [64]) + 1
+        self.max_position = max([int(x) for p in self.row_pos for x in p] + [64, P]) + 1
         self.cfg = M.Config(P, Hq, Hkv, D, self.num_pages, self.max_position, theta)
 
     def mask(self):
