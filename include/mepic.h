@@ -653,8 +653,8 @@ int32_t mepic_tree_accept(const mepic_tree_accept_args_t* args, void* cuda_strea
  *     reserve_used_out     *reserve_used + pages taken.
  * row_slot and slot_map hold max_rows entries; those past the last row are set to -1.  row_slot, slot_map and q_pos may be
  * NULL.  Outputs must not overlap inputs, other than the two tables, which are updated in place.
- * All or nothing: if the reserve, a table row (table_stride) or max_rows cannot hold the step, or a length is negative or
- * beyond its table row, MEPIC_DEV_NO_PAGES is set and the outputs are those of a step with n_new = 0 for everybody.
+ * All or nothing: if the reserve, a table row (table_stride) or max_rows cannot hold the step, or a length is negative,
+ * beyond its table row or (with n_new) beyond 2^31 - 1, MEPIC_DEV_NO_PAGES is set and the outputs are those of a step with n_new = 0 for everybody.
  * A page id outside the pool sets MEPIC_DEV_BAD_PAGE; its rows' slot_map entries become -1.
  * batch <= MEPIC_STEP_MAX_BATCH.
  */

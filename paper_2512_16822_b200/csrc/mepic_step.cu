@@ -137,7 +137,8 @@ __global__ void __launch_bounds__(kTablesThreads) mepic_step_tables_kernel(const
   __shared__ long long warp_rows[kTablesThreads / 32], warp_pages[kTablesThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int P = 1 << page_shift;
-  const long long room = static_cast<long long>(a.table_stride) << page_shift;
+  const long long room = min(static_cast<long long>(a.table_stride) << page_shift, 0x7fffffffll);       // lengths are int32
+  auto entries = [&](long long len) { return static_cast<int>((len + P - 1) >> page_shift); };        // table entries of `len` slots
   const int used = __ldg(a.reserve_used);
   // ---- sums: a thread owns `per` consecutive requests
   const int per = (a.batch + kTablesThreads - 1) / kTablesThreads, b0 = min(tid * per, a.batch), b1 = min(b0 + per, a.batch);
@@ -147,7 +148,7 @@ __global__ void __launch_bounds__(kTablesThreads) mepic_step_tables_kernel(const
     const long long kv = __ldg(a.kv_len + b), nn = __ldg(a.n_new + b);
     if (kv < 0 || nn < 0 || kv + nn > room) { bad = true; continue; }
     rows += nn;
-    pages += ((kv + nn + P - 1) >> page_shift) - ((kv + P - 1) >> page_shift);
+    pages += entries(kv + nn) - entries(kv);
   }
   long long r_in = rows, p_in = pages;          // inclusive over the warp
 #pragma unroll
@@ -170,7 +171,7 @@ __global__ void __launch_bounds__(kTablesThreads) mepic_step_tables_kernel(const
     if (bad) continue;
     const long long kv = __ldg(a.kv_len + b), nn = __ldg(a.n_new + b);
     r_at += nn;
-    p_at += ((kv + nn + P - 1) >> page_shift) - ((kv + P - 1) >> page_shift);
+    p_at += entries(kv + nn) - entries(kv);
   }
   if (tid == 0) { row_off[a.batch] = bad ? 0 : static_cast<int>(r_all); page_off[a.batch] = bad ? 0 : static_cast<int>(p_all); }
   __syncthreads();
@@ -189,7 +190,7 @@ __global__ void __launch_bounds__(kTablesThreads) mepic_step_tables_kernel(const
     if (a.q_pos) {
       int pos = -1;
       if (end > 0 && end <= room) {
-        const int held = (kv + P - 1) >> page_shift, e = (end - 1) >> page_shift;
+        const int held = entries(kv), e = (end - 1) >> page_shift;
         const int32_t* base = a.pos_base + static_cast<size_t>(b) * a.table_stride;
         pos = (e < held ? base[e] : (held > 0 ? base[held - 1] + (e - held + 1) * P : e * P)) + ((end - 1) & (P - 1));
       }
@@ -199,7 +200,7 @@ __global__ void __launch_bounds__(kTablesThreads) mepic_step_tables_kernel(const
   // ---- per new table entry
   for (int t = gid; t < n_pages; t += step) {
     const int b = find_request(page_off, a.batch, t);
-    const int held = (__ldg(a.kv_len + b) + P - 1) >> page_shift, k = t - page_off[b];
+    const int held = entries(__ldg(a.kv_len + b)), k = t - page_off[b];
     const int page = __ldg(a.reserve + used + t);
     if (static_cast<unsigned>(page) >= static_cast<unsigned>(num_pages)) atomicOr(a.status, MEPIC_DEV_BAD_PAGE);
     const size_t row = static_cast<size_t>(b) * a.table_stride;
@@ -213,7 +214,7 @@ __global__ void __launch_bounds__(kTablesThreads) mepic_step_tables_kernel(const
     long long phys = -1;
     if (r < n_rows) {
       const int b = find_request(row_off, a.batch, r);
-      const int kv = __ldg(a.kv_len + b), held = (kv + P - 1) >> page_shift;
+      const int kv = __ldg(a.kv_len + b), held = entries(kv);
       slot = kv + r - row_off[b];
       const int e = slot >> page_shift;
       const int page = e < held ? a.page_ids[static_cast<size_t>(b) * a.table_stride + e] : __ldg(a.reserve + used + page_off[b] + e - held);
@@ -485,8 +486,8 @@ extern "C" int32_t mepic_tree_layout(const mepic_config_t* cfg, const mepic_tree
     mepic_set_error("tree_layout: NULL pointer argument"); return MEPIC_E_INVAL;
   }
   const size_t smem = static_cast<size_t>(32 * a->mask_words) * a->mask_words * sizeof(uint32_t);
-  if (smem > 40 * 1024) {                        // beside the static 4 KB
-    const cudaError_t e = cudaFuncSetAttribute(mepic_tree_layout_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (smem > 40 * 1024) {                        // beside the static 4 KB.  Always the largest: another thread's call may need more than this one
+    const cudaError_t e = cudaFuncSetAttribute(mepic_tree_layout_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MEPIC_TREE_MAX_ROWS * MEPIC_TREE_MAX_ROWS / 8);
     if (e != cudaSuccess) { mepic_set_error("tree_layout: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
   }
   mepic_tree_layout_kernel<<<a->batch, kLayoutThreads, smem, static_cast<cudaStream_t>(cuda_stream)>>>(*a, shift_of(cfg->page_size));
@@ -518,8 +519,9 @@ extern "C" int32_t mepic_step_tables(const mepic_config_t* cfg, const mepic_step
   }
   if (a->slot_map && !aligned(a->slot_map, 8)) { mepic_set_error("step_tables: slot_map must be 8-byte aligned"); return MEPIC_E_INVAL; }
   const size_t smem = 2 * (static_cast<size_t>(a->batch) + 1) * sizeof(int);
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(mepic_step_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (smem > 40 * 1024) {                        // beside the static sums.  Always the largest, as above
+    const cudaError_t e = cudaFuncSetAttribute(mepic_step_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               2 * (MEPIC_STEP_MAX_BATCH + 1) * static_cast<int>(sizeof(int)));
     if (e != cudaSuccess) { mepic_set_error("step_tables: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
   }
   const int work = std::max(a->row_slot || a->slot_map ? a->max_rows : 0, a->batch);

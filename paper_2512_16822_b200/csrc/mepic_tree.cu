@@ -479,8 +479,6 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
   const bool has_work = piece.level >= 0;
   if (!has_work && tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
 
-  // Registers by role.  The launch gives 512 x 128; the softmax warps hold a row's 128 scores and take 232, the others leave
-  // that room: 128 x 232 + 384 x 88 = 63,488 of 65,536.
   // A wait of a whole warp; false ends the role.
   auto wait_warp = [&](uint32_t bar, uint32_t parity) {
 #pragma unroll 1

@@ -159,6 +159,52 @@ def test_tables_of_a_wide_pool_pass_32_bits():
 
 
 # ------------------------------------------------------------------------------------ commit
+def test_tables_of_lengths_at_the_end_of_32_bits():
+    # table rows longer than an int32 length can name: what ends beyond 2^31 - 1 is refused, what ends there is not
+    P, stride = 1 << 16, 32769
+    dev = RT.Device.over(M.Config(P, 1, 1, 64, 4, P - 1, 1e4))
+    top = 2 ** 31 - 1
+    for kv, new, fits in ((top - 300, 1000, False), (top, 1, False), (top - 5, 5, True), (top, 0, True), (top - P, 3, True)):
+        ids, base = np.zeros((1, stride), dtype=int), np.zeros((1, stride), dtype=int)
+        r = _tables(dev, [kv], [new], ids, base, [1, 2], 0, 1000, check=False)
+        assert dev.read_status() == (0 if fits else M.MEPIC_DEV_NO_PAGES)
+        dev.status.zero_()
+        assert r["kv_len"].item() == kv + (new if fits else 0) and r["row_offsets"].tolist() == [0, new if fits else 0]
+        old, all_ = -(-kv // P), -(-(kv + new) // P)
+        assert r["reserve_used"].item() == (all_ - old if fits else 0)
+        if fits:
+            assert r["row_slot"][:new].tolist() == list(range(kv, kv + new))
+            page = [int(r["page_ids"][0, s // P]) for s in range(kv, kv + new)]
+            assert r["slot_map"][:new].tolist() == [g * P + s % P for g, s in zip(page, range(kv, kv + new))]
+
+
+def test_layouts_and_tables_of_two_sizes_at_once():
+    # two host threads whose calls need different amounts of shared memory
+    import threading
+    rng, dev, failed = np.random.default_rng(9), _dev(16, 64), []
+
+    def work(words, batch):
+        try:
+            n = 32 * words
+            parents = np.arange(n, dtype=np.int32) - 1
+            lay = RT.TreeLayout(dev, parent=dev32(parents), row_offsets=dev32([0, n]), kv_len=dev32([3]), pos_base=dev32([[0]]), mask_words=words)
+            tab = RT.StepTables(dev, kv_len=dev32(np.full(batch, 3)), n_new=dev32(np.ones(batch)), page_ids=dev32(np.ones((batch, 1))),
+                                pos_base=dev32(np.zeros((batch, 1))), reserve=dev32([0]), reserve_used=dev32([0]), max_rows=batch)
+            s = torch.cuda.Stream()
+            s.wait_stream(torch.cuda.default_stream())
+            for _ in range(200):
+                lay.run(s)
+                tab.run(s)
+            s.synchronize()
+            assert lay.row_pos.tolist() == list(range(3, 3 + n)) and tab.slot_map.tolist() == [19] * batch
+        except Exception as e:                       # shown by the test's thread
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=w) for w in ((32, 8192), (20, 5500), (1, 7))]
+    [t.start() for t in threads], [t.join() for t in threads]
+    assert not failed and dev.read_status() == 0
+
+
 @pytest.mark.parametrize("D,P,Hkv", [(128, 16, 8), (64, 16, 1), (128, 64, 3)])
 @pytest.mark.parametrize("gather", [False, True])
 @pytest.mark.parametrize("fp8", [False, True])

@@ -407,3 +407,15 @@ def test_random_shapes(seed):
         if rng.integers(0, 2):
             s ^= rng.random(s.shape) < 0.2
     _run(case, 1.0 / np.sqrt(D), max_rows=min(32 * case.words, int(case.rows.max()) + int(rng.integers(0, 5))))
+
+
+@pytest.mark.parametrize("Hq,Hkv,n", [(8, 1, 1024), (1, 1, 1024), (7, 1, 700)])
+def test_as_many_rows_as_a_request_may_have(Hq, Hkv, n):
+    _run(TreeCase(70 + n, Hq=Hq, Hkv=Hkv, D=64, P=16, specs=[(200, n), (37, 2)]), 0.125)
+
+
+def test_a_batch_of_more_requests_than_the_cut_looks_at_in_one_go():
+    rng = np.random.default_rng(71)
+    specs = [(int(rng.integers(0, 90)), int(rng.integers(0, 4))) for _ in range(1500)]
+    specs[1400] = (700, 90)
+    _run(TreeCase(71, Hq=2, Hkv=1, D=64, P=16, specs=specs), 0.125)
