@@ -12,6 +12,7 @@
 #include "mepic_internal.h"
 #include "mepic_ptx.cuh"
 #include "mepic_rows.cuh"
+#include "mepic_tcgen05.cuh"      // arithmetic on pairs of floats
 
 namespace {
 
@@ -310,29 +311,43 @@ __global__ void __launch_bounds__(kCopyRows * 32) mepic_rows_commit_kernel(const
 // 8-bit pages.  A CTA looks at kRunRows consecutive rows and does the runs (rows that go to one page) that START among
 // them, whole; each of its warps takes one (pool, kv head) of a run at a time, so a block's maximum, scale and codes stay
 // in one warp.  (A CTA per row left 15 of 16 CTAs of a prompt with nothing to do.)  12,000 prompt rows of 8 kv heads (79 MB
-// read and written): 33 us, 2.4 TB/s; a chain of dependent look-ups (slots, sources, rows, maximum, codes) per run, which the
-// CTAs of an SM hide from one another only in part.
+// read and written): 30 us, 2.6 TB/s; about 1,250 instructions per block of 16 rows and a chain of dependent look-ups (slots,
+// sources, rows, maximum, codes), which the CTAs of an SM hide from one another only in part.  (CTAs of 8 warps: 31; of 2: 46;
+// each warp two blocks of a run: 34; rolled loops over a lane's eight pieces: 35.)
 constexpr int kRunRows = 16;
-constexpr int kRunWarps = 8;
+constexpr int kRunWarps = 4;
 // Eight elements -> E4M3(x / sc), the quotient rounded to fp32 first, as the format is defined.  With y = RN(1 / sc) and no
-// overflow or underflow on the way, q <- q + y (x - q sc) in fused arithmetic, begun at q = x y and done twice, ends at the
-// rounded quotient (Markstein's correction): five instructions an element where a division takes a dozen.  For a scale
-// outside [2^-80, 2^80] the division is used.
+// overflow or underflow on the way, q <- q - y (q sc - x) in fused arithmetic, begun at q = x y and done twice, ends at the
+// rounded quotient (Markstein's correction; this order of signs keeps a zero's): two and a half instructions an element, two
+// elements at a time, where a division takes a dozen.  For a scale outside [2^-80, 2^80] the division is used.
 __device__ __noinline__ uint2 e4m3x8_by_division(uint4 v, float sc) {
   const float2 a = bf16x2_to_float2(v.x), b = bf16x2_to_float2(v.y), c = bf16x2_to_float2(v.z), d = bf16x2_to_float2(v.w);
   return make_uint2(e4m3x4_of(__fdiv_rn(a.x, sc), __fdiv_rn(a.y, sc), __fdiv_rn(b.x, sc), __fdiv_rn(b.y, sc)),
                     e4m3x4_of(__fdiv_rn(c.x, sc), __fdiv_rn(c.y, sc), __fdiv_rn(d.x, sc), __fdiv_rn(d.y, sc)));
 }
-__device__ __forceinline__ float quotient(float x, float sc, float inv, float most) {
-  x = x > most ? most : (x < -most ? -most : x);      // what saturates anyway must not overflow; NaN stays
-  float q = x * inv;
-  q = fmaf(fmaf(-q, sc, x), inv, q);
-  return copysignf(fmaf(fmaf(-q, sc, x), inv, q), x);      // (a zero's sign is lost on the way)
-}
+// most: what saturates anyway must not overflow on the way, so |x| is cut to it first; 0: no element is above the block's maximum
+// and none is cut.  NaN stays.
 __device__ __forceinline__ uint2 e4m3x8_of(const uint4& v, float sc, float inv, float most) {
-  const float2 a = bf16x2_to_float2(v.x), b = bf16x2_to_float2(v.y), c = bf16x2_to_float2(v.z), d = bf16x2_to_float2(v.w);
-  auto q = [&](float x) { return quotient(x, sc, inv, most); };
-  return make_uint2(e4m3x4_of(q(a.x), q(a.y), q(b.x), q(b.y)), e4m3x4_of(q(c.x), q(c.y), q(d.x), q(d.y)));
+  const uint32_t w[4] = {v.x ^ 0x80008000u, v.y ^ 0x80008000u, v.z ^ 0x80008000u, v.w ^ 0x80008000u};      // -x
+  const float2 sc2 = make_float2(sc, sc), ninv2 = make_float2(-inv, -inv);
+  float2 q[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float2 nx = bf16x2_to_float2(w[j]);
+    if (most != 0.f) {
+      nx.x = nx.x > most ? most : (nx.x < -most ? -most : nx.x);
+      nx.y = nx.y > most ? most : (nx.y < -most ? -most : nx.y);
+    }
+    q[j] = mul2(nx, ninv2);
+    q[j] = fma2(fma2(q[j], sc2, nx), ninv2, q[j]);
+    q[j] = fma2(fma2(q[j], sc2, nx), ninv2, q[j]);
+  }
+  return make_uint2(e4m3x4_of(q[0].x, q[0].y, q[1].x, q[1].y), e4m3x4_of(q[2].x, q[2].y, q[3].x, q[3].y));
+}
+// Two running maxima of absolute values; a NaN operand is dropped.
+__device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t m, uint32_t x) {
+  asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(x & 0x7fff7fffu));
+  return m;
 }
 // Rows r0 .. r0 + min(n, 16) - 1 of pool w, kv head h: a lane's 16-byte pieces of eight rows (half a warp takes a row), and in
 // lane k < 16 the in-page slot of row k (-1: nothing to write).
@@ -350,7 +365,7 @@ __device__ __forceinline__ void load_block(const CommitParams& p, int w, int r0,
     v[u] = s < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(base + static_cast<size_t>(s) * p.kv_stride);
   }
 }
-__global__ void __launch_bounds__(kRunWarps * 32, 3) mepic_rows_commit_fp8_kernel(const __grid_constant__ CommitParams p) {
+__global__ void __launch_bounds__(kRunWarps * 32, 6) mepic_rows_commit_fp8_kernel(const __grid_constant__ CommitParams p) {
   constexpr int D = 128;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int r0 = blockIdx.x * kRunRows;
@@ -392,21 +407,20 @@ __global__ void __launch_bounds__(kRunWarps * 32, 3) mepic_rows_commit_fp8_kerne
       const size_t block = static_cast<size_t>(page) * p.n_kv_heads + h;
       uint4 v[8];
       int slot = 0;                                // lane k < 16: in-page slot of row k of the block, -1 where there is nothing to write
-      float sc, amax = 0.f;
+      float sc;
       if (fresh) {
+        uint32_t m2[2] = {0, 0};                   // bf16 maxima are exact
 #pragma unroll 1
         for (int k0 = 0; k0 < n; k0 += 16) {
           load_block(p, w, first + k0, n - k0, h, lane, v, slot);
 #pragma unroll
           for (int u = 0; u < 8; ++u) {
-            const uint32_t ww[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float2 f = bf16x2_to_float2(ww[j]);
-              amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));       // fmaxf drops NaN operands: a NaN element does not set the scale
-            }
+            m2[0] = max_abs_bf16x2(max_abs_bf16x2(m2[0], v[u].x), v[u].y);
+            m2[1] = max_abs_bf16x2(max_abs_bf16x2(m2[1], v[u].z), v[u].w);
           }
         }
+        const float2 m = bf16x2_to_float2(max_abs_bf16x2(m2[0], m2[1]));
+        float amax = fmaxf(m.x, m.y);              // a NaN element does not set the scale
 #pragma unroll
         for (int d = 16; d; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(kFull, amax, d));
         sc = amax > 0.f ? __fdiv_rn(amax, 448.f) : 1.f;
@@ -414,7 +428,7 @@ __global__ void __launch_bounds__(kRunWarps * 32, 3) mepic_rows_commit_fp8_kerne
       } else {
         sc = p.scales[w][block];
       }
-      const float inv = __frcp_rn(sc), most = 600.f * sc;
+      const float inv = __frcp_rn(sc), most = fresh ? 0.f : 600.f * sc;
       const bool plain = sc >= 8.2718061e-25f && sc <= 1.2089258e24f;       // 2^-80 .. 2^80
 #pragma unroll 1
       for (int k0 = 0; k0 < n; k0 += 16) {
@@ -473,7 +487,7 @@ int32_t commit_call(const mepic_config_t* cfg, const mepic_rows_commit_args_t* a
   p.page_shift = shift_of(cfg->page_size);
   p.n_slots = static_cast<long long>(cfg->num_pages) * cfg->page_size;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  // a CTA takes up to eight of a run's (pool, kv head) blocks, one per warp: several CTAs fit an SM and hide one another's look-ups
+  // a CTA takes up to four of a run's (pool, kv head) blocks, one per warp: several CTAs fit an SM and hide one another's look-ups
   if (fp8) mepic_rows_commit_fp8_kernel<<<dim3((a->max_rows + kRunRows - 1) / kRunRows, std::min((2 * cfg->n_kv_heads + kRunWarps - 1) / kRunWarps, 64)), kRunWarps * 32, 0, st>>>(p);
   else if (cfg->head_dim == 128) mepic_rows_commit_kernel<128><<<(a->max_rows + kCopyRows - 1) / kCopyRows, kCopyRows * 32, 0, st>>>(p);
   else mepic_rows_commit_kernel<64><<<(a->max_rows + kCopyRows - 1) / kCopyRows, kCopyRows * 32, 0, st>>>(p);

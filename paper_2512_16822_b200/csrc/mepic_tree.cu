@@ -34,11 +34,11 @@
 //   MMA warps     : one issues S = Q' K'^T (three score buffers, each of which becomes its tile's P), one O += P V.
 // Every wait is bounded; a lost wait raises a flag that ends every role.
 //
-// Measured (G = 4, D = 128, 8 kv heads, pages of 16).  32 requests x 16 rows over 8,256 slots: 203 us in a burst of calls, 244
-// in a run of them (the GPU is at its power limit then, and its clock at 1.66 GHz), of it 6 the merge; 986 MB of DRAM traffic,
+// Measured (G = 4, D = 128, 8 kv heads, pages of 16).  32 requests x 16 rows over 8,256 slots: 203 us in a burst of calls, 232
+// to 244 in a run of them (the GPU is at its power limit then, and its clock at 1.66 GHz), of it 6 the merge; 986 MB of DRAM traffic,
 // 55 % of the bandwidth; the tensor pipe is active 30 % of the time, the exponential unit 14, issue slots 40.  8 x 96 rows over
-// 16,640: 328 us (146 GFLOP, 445 TFLOP/s).  8 x 32 rows over 65,536 slots of 8-bit pages: 464 us.  One request of 8 rows over
-// 203 slots: 12.3 us, two launches.  What bounds the large ones is none of the units but the hand-over of a tile from role to
+// 16,640: 317 us (146 GFLOP, 460 TFLOP/s).  8 x 32 rows over 65,536 slots of 8-bit pages: 446 us.  One request of 8 rows over
+// 203 slots: 12.5 us, two launches.  What bounds the large ones is none of the units but the hand-over of a tile from role to
 // role (load, rotate, QK^T, softmax, PV: each waits for latency, and for instructions, which twenty warps with five programs
 // fetch through one cache).
 #include <cuda.h>
