@@ -261,6 +261,52 @@ def test_commit(D, P, Hkv, gather, fp8):
         assert np.array_equal(RT.bf16_bits(dev.k_pool), kp) and np.array_equal(RT.bf16_bits(dev.v_pool), vp)
 
 
+@pytest.mark.parametrize("P", [16, 32])
+def test_commit_of_extreme_values_into_8_bit_pages(P):
+    # a page per magnitude, started (its scale from its rows) or appended to under a scale that stands, from subnormal to infinite
+    rng, Hkv, D = np.random.default_rng(P), 2, 128
+    exps = [-132, -120, -100, -88, -80, -72, -71, -40, 0, 40, 88, 89, 90, 110, 119]
+    standing = np.array([0.0, 1e-44, 2.0 ** -127, 2.0 ** -100, 2.0 ** -81, 2.0 ** -80, 2.0 ** -79, 2.0 ** -3, 2.0 ** 79, 2.0 ** 80, 2.0 ** 81, 2.0 ** 120, 3e38, np.inf, 0.37],
+                        dtype=np.float32)
+    n_pages = 2 * len(exps) + 3
+    rows, slots, off, src = [], [], [0], []
+    def add(page, first, x):
+        rows.append(x), slots.extend(page * P + first + i for i in range(len(x))), off.append(off[-1] + len(x))
+        src.append((page, first))
+    normal = lambda n: rng.standard_normal((n, 2, Hkv, D)).astype(np.float32)
+    with np.errstate(over="ignore", under="ignore"):
+        for i, e in enumerate(exps):
+            add(i, 0, (normal(P).astype(np.float64) * 2.0 ** e).astype(np.float32))
+            x = normal(7)
+            x[..., ::2] *= np.float32(standing[i]) if np.isfinite(standing[i]) else np.float32(1)       # in the scale's range, and far from it
+            x[0, :, :, :4] = [np.inf, -np.inf, np.nan, -0.0]
+            add(len(exps) + i, 5, x)
+    at = 2 * len(exps)
+    x = normal(P); x[3, 0, 0, 5] = np.inf; x[4, 1, 1, 7] = -np.inf
+    add(at, 0, x)
+    x = normal(P); x[:, :, 1] = -0.0; x[2, 0, 0, 0] = np.nan; x[:, 1, 0] = np.nan
+    add(at + 1, 0, x)
+    add(at + 2, 0, np.full((1, 2, Hkv, D), 3.3895e38, dtype=np.float32))
+    kv = f32_to_bf16_bits(np.concatenate(rows))
+    kv[0, 0, 0, :3] = 0x0001, 0x8001, 0x7f
+    dev = RT.Device(M.Config(P, Hkv, Hkv, D, n_pages, P, 1e4))
+    dev.k_pool.zero_(), dev.v_pool.zero_()
+    pools = RT.Fp8Pools(dev)
+    for s in (pools.k_scales, pools.v_scales):
+        s[len(exps):2 * len(exps)] = torch.from_numpy(standing).cuda()[:, None]
+    kc, vc, ks, vs = (_host(t).copy() for t in (pools.k_codes, pools.v_codes, pools.k_scales, pools.v_scales))
+    k, v = (RT.bf16_tensor(np.ascontiguousarray(kv[:, w]), DEV) for w in range(2))
+    RT.RowsCommit(dev, k_new=k, v_new=v, row_offsets=dev32(off), slot_map=torch.tensor(slots, dtype=torch.int64, device=DEV), pools=pools).run()
+    torch.cuda.synchronize()
+    assert dev.read_status() == 0
+    with np.errstate(all="ignore"):
+        for i, (page, first) in enumerate(src):
+            part = kv[off[i]:off[i + 1]]
+            O.commit_rows_fp8(kc, ks, vc, vs, [page], list(first + np.arange(len(part))), part[:, 0], part[:, 1])
+    assert np.array_equal(_host(pools.k_scales), ks, equal_nan=True) and np.array_equal(_host(pools.v_scales), vs, equal_nan=True)
+    assert np.array_equal(_host(pools.k_codes), kc) and np.array_equal(_host(pools.v_codes), vc)
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 def test_commit_reports_and_skips(fp8):
     dev = _dev(num_pages=4, pools=True)
