@@ -53,6 +53,23 @@ def test_layout(kind, counts, words):
         assert np.array_equal(_host(r["tree_mask"])[off[b]:off[b + 1]], O.pack_mask(sees, words)), b
 
 
+def test_layout_of_the_largest_tree_captured_and_replayed():
+    n, dev = 1024, _dev()
+    parents, lens = dev32(np.full(n, -1)), dev32([7])
+    lay = RT.TreeLayout(dev, parent=parents, row_offsets=dev32([0, n]), kv_len=lens, pos_base=dev32([[100]]), mask_words=32)
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=s):
+        lay.run()
+    for p, kv in ((np.arange(n) - 1, 9), (np.full(n, -1), 0), (random_parents(np.random.default_rng(2), n), 16)):
+        parents.copy_(dev32(p)), lens.fill_(kv)
+        g.replay()
+        torch.cuda.synchronize()
+        pos, sees = O.tree_layout(p, 100 + kv if kv else 0)
+        assert dev.read_status() == 0
+        assert lay.row_pos.tolist() == list(pos) and np.array_equal(_host(lay.tree_mask), O.pack_mask(sees, 32))
+
+
 def test_layout_reports_what_makes_no_sense():
     base = dev32(np.zeros((1, 4)))
     def status(parent, off, kv=5, words=1):
