@@ -19,7 +19,7 @@
 // cut from row_offsets and kv_len, so no plan is built or uploaded and a captured call may be replayed with other lengths.
 //
 // Roles (640 threads, one CTA per SM):
-//   softmax warps : a thread per row.  Loads, rotates and stages the row's q; then per key tile the
+//   softmax warps : a thread per row, two warpgroups (even and odd key tiles).  Loads, rotates and stages the row's q; then per key tile the
 //                   row's 128 scores come to registers: maximum, 2^(S - reference), and back as bf16 over the scores' columns,
 //                   where the PV MMA takes P from.
 //   rotator warps : rotate the K tile in place in shared memory, fp32 arithmetic, one rounding.  They also bring the drafted
