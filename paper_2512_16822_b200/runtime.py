@@ -139,7 +139,11 @@ def _row_stride(t: torch.Tensor, name: str, heads: int, head_dim: int, device: t
         raise ValueError(f"{name}: expected bfloat16 [rows, {heads}, {head_dim}] on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     if t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
         raise ValueError(f"{name}: the heads of a row must be packed")
-    return t.stride(0) if t.shape[0] > 1 else heads * head_dim
+    if t.shape[0] <= 1:
+        return heads * head_dim
+    if t.stride(0) < heads * head_dim:           # a broadcast row has stride 0, which the calls read as "packed"
+        raise ValueError(f"{name}: rows must not share memory (row stride {t.stride(0)}, a row has {heads * head_dim} elements)")
+    return t.stride(0)
 
 
 class DecodeBatch:

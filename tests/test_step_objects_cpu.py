@@ -1,0 +1,70 @@
+"""What the objects of a drafted-token step check before they bind a tensor: no GPU is needed to be refused."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+import paper_2512_16822_b200 as M
+from paper_2512_16822_b200 import runtime as RT
+
+CPU = torch.device("cpu")
+CFG = M.Config(page_size=16, n_q_heads=8, n_kv_heads=2, head_dim=128, num_pages=10, max_position=100, rope_theta=1e4)
+ROWS = 5
+
+
+def _dev(cfg=CFG):
+    pool = torch.zeros((cfg.num_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim), dtype=torch.bfloat16)
+    return SimpleNamespace(cfg=cfg, device=CPU, k_pool=pool, v_pool=pool.clone(), rope=None, status=torch.zeros(1, dtype=torch.int32))
+
+
+def _rows(heads, rows=ROWS):
+    return torch.zeros((rows, heads, 128), dtype=torch.bfloat16)
+
+
+def _broadcast(heads):
+    return torch.zeros((1, heads, 128), dtype=torch.bfloat16).expand(ROWS, heads, 128)
+
+
+def _overlapping(heads):
+    return torch.zeros(64 * ROWS + heads * 128, dtype=torch.bfloat16).as_strided((ROWS, heads, 128), (64, 128, 1))
+
+
+def _i32(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def _tree(dev, **over):
+    a = dict(q=_rows(8), k_new=_rows(2), v_new=_rows(2), row_offsets=_i32(2), row_pos=_i32(ROWS), tree_mask=_i32(ROWS, 1), page_ids=_i32(1, 4),
+             pos_base=_i32(1, 4), kv_len=_i32(1), max_rows=ROWS)
+    a.update(over)
+    return RT.TreeBatch(dev, **a)
+
+
+def _commit(dev, **over):
+    a = dict(k_new=_rows(2), v_new=_rows(2), row_offsets=_i32(2), slot_map=torch.zeros(ROWS, dtype=torch.int64))
+    a.update(over)
+    return RT.RowsCommit(dev, **a)
+
+
+@pytest.mark.parametrize("make", [_broadcast, _overlapping])
+def test_rows_that_share_memory_are_refused(make):
+    # a row stride of 0 is the call's word for "packed": a broadcast row bound as it is would be read as ROWS rows
+    with pytest.raises(ValueError, match="q: .*stride"):
+        _tree(_dev(), q=make(8))
+    for name in ("k_new", "v_new"):
+        with pytest.raises(ValueError, match=name + ": .*stride"):
+            _tree(_dev(), **{name: make(2)})
+        with pytest.raises(ValueError, match=name + ": .*stride"):
+            _commit(_dev(), **{name: make(2)})
+    both = make(2)
+    with pytest.raises(ValueError, match="k_new: .*stride"):
+        _commit(_dev(), k_new=both, v_new=both)
+
+
+def test_row_strides_of_rows_that_lie_apart_or_alone():
+    fused = torch.zeros((ROWS, 12 * 128), dtype=torch.bfloat16)
+    q = fused[:, :8 * 128].unflatten(1, (8, 128))
+    assert RT._row_stride(q, "q", 8, 128, CPU) == 12 * 128
+    assert RT._row_stride(_rows(2), "k", 2, 128, CPU) == 2 * 128
+    assert RT._row_stride(_broadcast(2)[:1], "k", 2, 128, CPU) == 2 * 128        # one row has no stride to speak of
+    assert RT._row_stride(_rows(2, 0), "k", 2, 128, CPU) == 2 * 128
