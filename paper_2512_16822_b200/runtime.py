@@ -87,7 +87,7 @@ class Device:
         if not torch.cuda.is_available():
             raise RuntimeError("the MEPIC kernels need a CUDA device; there is no CPU path")
         self.cfg = cfg
-        self.device = torch.device(device)
+        self.device = _cuda_device(device)
         shape = (cfg.num_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
         if not bf16_pools:
             self.k_pool = self.v_pool = None           # a device whose only pools are 8-bit (see Fp8Pools)
@@ -108,7 +108,7 @@ class Device:
         the library's is built."""
         shape = (cfg.num_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
         dev = cls.__new__(cls)
-        dev.cfg, dev.device = cfg, torch.device(device)
+        dev.cfg, dev.device = cfg, _cuda_device(device)
         for pool in (k_pool, v_pool):
             if pool is not None:
                 _expect(pool, "pool", torch.bfloat16, shape, dev.device)
@@ -123,10 +123,19 @@ class Device:
         return int(self.status.item())
 
 
+def _cuda_device(device) -> torch.device:
+    """``device`` with an index: "cuda" is the GPU that is current now."""
+    d = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
+
+
+def _lies_on(t: torch.Tensor, device: torch.device) -> bool:
+    return t.device.type == device.type and (device.index is None or t.device.index == device.index)
+
+
 def _expect(t: torch.Tensor, name: str, dtype: torch.dtype, shape, device: torch.device) -> torch.Tensor:
     """``t`` if it is a packed tensor of that type, shape and device (-1 in ``shape``: any size); raises ValueError otherwise."""
-    same_device = t.device.type == device.type and (device.index is None or t.device.index == device.index)
-    if t.dtype != dtype or not same_device or t.dim() != len(shape) or any(w >= 0 and g != w for g, w in zip(t.shape, shape)):
+    if t.dtype != dtype or not _lies_on(t, device) or t.dim() != len(shape) or any(w >= 0 and g != w for g, w in zip(t.shape, shape)):
         raise ValueError(f"{name}: expected {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     if not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
@@ -135,7 +144,7 @@ def _expect(t: torch.Tensor, name: str, dtype: torch.dtype, shape, device: torch
 
 def _row_stride(t: torch.Tensor, name: str, heads: int, head_dim: int, device: torch.device) -> int:
     """Row stride in elements of bf16 rows [rows, heads, head_dim] whose rows are packed but may lie apart."""
-    if t.dtype != torch.bfloat16 or t.device.type != device.type or t.dim() != 3 or t.shape[1:] != (heads, head_dim):
+    if t.dtype != torch.bfloat16 or not _lies_on(t, device) or t.dim() != 3 or t.shape[1:] != (heads, head_dim):
         raise ValueError(f"{name}: expected bfloat16 [rows, {heads}, {head_dim}] on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     if t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
         raise ValueError(f"{name}: the heads of a row must be packed")
@@ -385,7 +394,7 @@ class _StepCall:
 
     def _bind(self, dev: Device, name: str, args, *, with_cfg: bool = True, extra=(), keep=()):
         self.dev = dev
-        self._index = dev.device.index if dev.device.index is not None else torch.cuda.current_device()
+        self._index = _cuda_device(dev.device).index
         self._args, self._cfg, self._keep = args, dev.cfg.c(), keep            # the struct holds raw addresses: keep the tensors alive
         self._fn = getattr(lib(), name)
         self._argv = ((C.byref(self._cfg),) if with_cfg else ()) + (C.byref(args),) + tuple(extra)

@@ -68,3 +68,31 @@ def test_row_strides_of_rows_that_lie_apart_or_alone():
     assert RT._row_stride(_rows(2), "k", 2, 128, CPU) == 2 * 128
     assert RT._row_stride(_broadcast(2)[:1], "k", 2, 128, CPU) == 2 * 128        # one row has no stride to speak of
     assert RT._row_stride(_rows(2, 0), "k", 2, 128, CPU) == 2 * 128
+
+
+class _Elsewhere:
+    """Stands in for a tensor on a GPU this machine does not have."""
+
+    def __init__(self, like, device):
+        self._like, self.device, self.dtype, self.shape = like, torch.device(device), like.dtype, like.shape
+
+    def __getattr__(self, name):
+        return getattr(self._like, name)
+
+
+def test_tensors_of_another_gpu_are_refused():
+    zero = torch.device("cuda:0")
+    assert RT._row_stride(_Elsewhere(_rows(2), "cuda:0"), "k", 2, 128, zero) == 2 * 128
+    for device in ("cuda:1", "cpu"):
+        with pytest.raises(ValueError, match="on cuda:0"):
+            RT._row_stride(_Elsewhere(_rows(2), device), "k", 2, 128, zero)
+        with pytest.raises(ValueError, match="on cuda:0"):
+            RT._expect(_Elsewhere(_i32(3), device), "kv_len", torch.int32, (3,), zero)
+
+
+def test_a_device_without_an_index_is_the_current_one(monkeypatch):
+    # ... at the time it is made: what is checked against it later may not lie on another GPU
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    assert RT._cuda_device("cuda") == torch.device("cuda:1")
+    assert RT._cuda_device("cuda:0") == torch.device("cuda:0")
+    assert RT._cuda_device(torch.device("cuda:2")) == torch.device("cuda:2")
