@@ -155,6 +155,21 @@ def _row_stride(t: torch.Tensor, name: str, heads: int, head_dim: int, device: t
     return t.stride(0)
 
 
+def _pools_for(dev: Device, pools: Optional["Fp8Pools"]):
+    """The K and V pools a call on ``dev`` uses: those of ``pools`` (8-bit) or the device's bf16 ones.  A page id that is valid
+    for the device's configuration must be valid in them: ValueError otherwise."""
+    cfg = dev.cfg
+    shape = (cfg.num_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
+    if pools is None:
+        if dev.k_pool is None or dev.v_pool is None:
+            raise ValueError("the device has no bf16 pools: name the 8-bit pools to use")
+        return tuple(_expect(t, "pool", torch.bfloat16, shape, dev.device) for t in (dev.k_pool, dev.v_pool))
+    codes = tuple(_expect(t, "codes", torch.uint8, shape, dev.device) for t in (pools.k_codes, pools.v_codes))
+    for t in (pools.k_scales, pools.v_scales):
+        _expect(t, "scales", torch.float32, shape[:2], dev.device)
+    return codes
+
+
 class DecodeBatch:
     """Device copies of one decode batch's tables plus output and workspace."""
 
@@ -229,11 +244,10 @@ class Fp8Pools:
     @classmethod
     def over(cls, dev: Device, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor) -> "Fp8Pools":
         """8-bit pools the caller already holds: nothing is copied or quantised."""
-        cfg, pools = dev.cfg, cls.__new__(cls)
-        shape = (cfg.num_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
+        pools = cls.__new__(cls)
         pools.dev = dev
-        pools.k_codes, pools.v_codes = (_expect(t, "codes", torch.uint8, shape, dev.device) for t in (k_codes, v_codes))
-        pools.k_scales, pools.v_scales = (_expect(t, "scales", torch.float32, shape[:2], dev.device) for t in (k_scales, v_scales))
+        pools.k_codes, pools.v_codes, pools.k_scales, pools.v_scales = k_codes, v_codes, k_scales, v_scales
+        _pools_for(dev, pools)
         return pools
 
     def quantize(self, pages: np.ndarray, stream=None) -> None:
@@ -450,7 +464,7 @@ class TreeBatch(_StepCall):
         _expect(row_offsets, "row_offsets", i32, (batch + 1,), d), _expect(row_pos, "row_pos", i32, (rows,), d)
         _expect(tree_mask, "tree_mask", i32, (rows, -1), d), _expect(page_ids, "page_ids", i32, (batch, -1), d)
         _expect(pos_base, "pos_base", i32, tuple(page_ids.shape), d), _expect(kv_len, "kv_len", i32, (batch,), d)
-        k_pool, v_pool = (dev.k_pool, dev.v_pool) if pools is None else (pools.k_codes, pools.v_codes)
+        k_pool, v_pool = _pools_for(dev, pools)
         with torch.cuda.device(d):
             ws = mepic_attn_tree_workspace(cfg, max_rows)
         self.out = torch.empty((rows, cfg.n_q_heads, cfg.head_dim), dtype=torch.bfloat16, device=d)
@@ -535,7 +549,7 @@ class RowsCommit(_StepCall):
         _expect(row_offsets, "row_offsets", torch.int32, (batch + 1,), d), _expect(slot_map, "slot_map", torch.int64, (max_rows,), d)
         if src_rows is not None:
             _expect(src_rows, "src_rows", torch.int32, (batch, -1), d)
-        k_pool, v_pool = (dev.k_pool, dev.v_pool) if pools is None else (pools.k_codes, pools.v_codes)
+        k_pool, v_pool = _pools_for(dev, pools)
         self._bind(dev, "mepic_rows_commit" if pools is None else "mepic_rows_commit_fp8",
                    _RowsCommitArgsC(k_new.data_ptr(), v_new.data_ptr(), row_offsets.data_ptr(), slot_map.data_ptr(),
                                     None if src_rows is None else src_rows.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),

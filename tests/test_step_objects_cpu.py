@@ -96,3 +96,32 @@ def test_a_device_without_an_index_is_the_current_one(monkeypatch):
     assert RT._cuda_device("cuda") == torch.device("cuda:1")
     assert RT._cuda_device("cuda:0") == torch.device("cuda:0")
     assert RT._cuda_device(torch.device("cuda:2")) == torch.device("cuda:2")
+
+
+def _pools(dev, num_pages=None, device=None):
+    n = dev.cfg.num_pages if num_pages is None else num_pages
+    codes, scales = torch.zeros((n, 2, 16, 128), dtype=torch.uint8), torch.ones((n, 2), dtype=torch.float32)
+    if device is not None:
+        codes, scales = _Elsewhere(codes, device), _Elsewhere(scales, device)
+    return SimpleNamespace(dev=dev, k_codes=codes, v_codes=codes, k_scales=scales, v_scales=scales)
+
+
+def test_pools_that_are_not_the_devices_are_refused():
+    # a page id that is valid for the device's configuration must be valid for the pools it is looked up in
+    dev = _dev()
+    for build in (_tree, _commit):
+        for pools in (_pools(dev, num_pages=9), _pools(dev, device="cuda:1")):
+            with pytest.raises(ValueError, match="codes"):
+                build(dev, pools=pools)
+        short = _pools(dev)
+        short.v_scales = short.v_scales[:9]
+        with pytest.raises(ValueError, match="scales"):
+            build(dev, pools=short)
+        bare = _dev()
+        bare.k_pool = bare.v_pool = None                             # a device whose only pools are 8-bit, and none are given
+        with pytest.raises(ValueError, match="bf16 pools"):
+            build(bare)
+        small = _dev()
+        small.v_pool = small.v_pool[:9]
+        with pytest.raises(ValueError, match="pool"):
+            build(small)
