@@ -404,7 +404,10 @@ class Fp8GroupedDecodeBatch(GroupedDecodeBatch):
 
 class _StepCall:
     """One call of a step over buffers that stay in place: the argument struct is filled once, ``run`` only launches, so that a
-    step costs the host a few microseconds and can be captured into a graph.  Inputs are read when the kernels run."""
+    step costs the host a few microseconds and can be captured into a graph.  Inputs are read when the kernels run.  The results
+    and the workspace are the object's own and the next ``run`` writes them again: runs that may overlap on the GPU need an
+    object each.  An object may be dropped while its kernels still run, on whatever stream, but not before a graph that
+    captured it."""
 
     def _bind(self, dev: Device, name: str, args, *, with_cfg: bool = True, extra=(), keep=()):
         self.dev = dev
@@ -412,6 +415,22 @@ class _StepCall:
         self._args, self._cfg, self._keep = args, dev.cfg.c(), keep            # the struct holds raw addresses: keep the tensors alive
         self._fn = getattr(lib(), name)
         self._argv = ((C.byref(self._cfg),) if with_cfg else ()) + (C.byref(args),) + tuple(extra)
+        self._streams = set()                                                  # raw streams the bound tensors are recorded on
+
+    def _record(self, stream, raw: int) -> None:
+        """Tells the allocator that ``stream`` uses what is bound: memory of a dropped object is handed out again only when
+        its kernels are through."""
+        if stream is None:
+            stream = torch.cuda.current_stream(self._index)
+        elif isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(raw, device=self._index) if raw else torch.cuda.default_stream(self._index)
+        held = list(vars(self).values()) + [self.dev.rope, self.dev.status]
+        for t in self._keep:
+            held += [t.k_codes, t.v_codes, t.k_scales, t.v_scales] if isinstance(t, Fp8Pools) else [t]
+        for t in held:
+            if isinstance(t, torch.Tensor) and t.numel():
+                t.record_stream(stream)
+        self._streams.add(raw)
 
     def _launch(self, stream=None) -> None:
         if torch._C._cuda_getDevice() != self._index:                # (the private forms of current_device and current_stream: the
@@ -421,6 +440,8 @@ class _StepCall:
             s = torch._C._cuda_getCurrentRawStream(self._index)
         else:
             s = stream if isinstance(stream, int) else stream.cuda_stream
+        if s not in self._streams:
+            self._record(stream, s)
         code = self._fn(*self._argv, s)
         if code:
             _check(code)
