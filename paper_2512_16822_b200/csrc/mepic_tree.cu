@@ -990,6 +990,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
       if (FP8 && is_k && lane < 8) { sm->ks[gi & 1][lane] = x.ks; sm->vs[gi % kScaleRing][lane] = x.vs; }
       const unsigned live = __ballot_sync(kFull, x.live);
       const bool skip = HOOKS && is_k && blockIdx.x == 0 && gi == p.skip_tile;      // (test hook: a K tile that never comes)
+      __syncwarp();                               // the scales are written before lane 0's arrival, which publishes them
       if (lane == 0 && !skip) {
         if (live) mbar_expect_tx(landed, static_cast<uint32_t>(__popc(live)) * kGroupBytes);
         else mbar_arrive(landed);                 // drafted rows: the rotators and the V loader bring them into the stage
