@@ -1,10 +1,13 @@
-"""Attention of drafted rows where every CTA takes many key tiles: rings that wrap, and items that follow one another in a CTA."""
+"""Attention of drafted rows where every CTA takes many key tiles: rings that wrap, items that follow one another in a CTA, and
+references that move in the middle of an item."""
 import numpy as np
 import pytest
 import torch
 
+from paper_2512_16822_b200 import runtime as RT
 from paper_2512_16822_b200.build import build_library
 from mepic_inputs import bf16_bits_to_f64, f32_to_bf16_bits
+from oracle import mepic_oracle as O
 from tree_helpers import TreeCase
 
 pytestmark = pytest.mark.gpu
@@ -98,3 +101,74 @@ def test_random_shapes_of_many_tiles(seed):
     order = [int(b) for b in np.argsort(cost) if case.rows[b]]
     run_and_check(case, 1.0 / np.sqrt(D), 4, which=[b for i, b in enumerate(order) if i < 3 or cost[b] < 400_000])
 
+
+# Scores that are whole numbers in base 2: q and K are zero but in one pair of dims that no position here turns by more than
+# 1e-4 rad (its partner is zero, so the rotated element is the element), sm_scale is ln 2, and every K is a value that both
+# bf16 and e4m3 under a power of two hold exactly.  Then Q', K' and P are exact, and what is left is arithmetic in fp32.
+LEVELS = [(0, 9), (11, 20), (22, 32), (36, 48), (52, 64)]
+LN2 = float(np.float32(np.log(2.0)))
+
+
+def staircase(case, rng):
+    """Context scores of every (request, kv head): pairs of tiles, one with all keys at a level, one with a single key 9 to 12
+    above it (so that both count), pair above pair up to a peak that lies elsewhere in every head; low ever after."""
+    D, Hkv, P = case.D, case.Hkv, case.P
+    kp = np.zeros((case.num_pages, Hkv, P, D))
+    for b, n in enumerate(case.kv_len):
+        tiles = -(-int(n) // 128)
+        for h in range(Hkv):
+            level = np.zeros(int(n))
+            start = int(rng.integers(0, max(1, tiles - 2 * len(LEVELS))))
+            for i, (low, high) in enumerate(LEVELS[:int(rng.integers(1, len(LEVELS) + 1))]):
+                lo = (start + 2 * i) * 128
+                level[lo:lo + 128] = low
+                if lo + 128 < n:
+                    level[lo + 128 + int(rng.integers(0, min(128, int(n) - lo - 128)))] = high
+            for t in range(int(n)):
+                kp[case.page_ids[b, t // P], h, t % P, D // 2 - 1] = level[t]
+    case.kp = f32_to_bf16_bits(kp.astype(np.float32))
+    assert np.array_equal(bf16_bits_to_f64(case.kp), kp)
+    sign = rng.choice([1.0, 1.0, -1.0], size=case.q.shape[:2])        # for -1 the staircase goes down
+    q = np.zeros(case.q.shape)
+    q[..., D // 2 - 1] = sign
+    case.q = f32_to_bf16_bits(q.astype(np.float32))
+    kn = np.zeros(case.kn.shape)
+    kn[..., D // 2 - 1] = rng.choice([0.0, 9.0, 20.0, 64.0], size=case.kn.shape[:2])
+    case.kn = f32_to_bf16_bits(kn.astype(np.float32))
+
+
+@pytest.mark.parametrize("D,fp8", [(128, False), (64, False), (128, True)])
+def test_references_that_rise_in_the_middle_of_an_item(D, fp8):
+    rng = np.random.default_rng(110 + D)
+    specs = [(int(n), int(r)) for n, r in zip(rng.integers(1300, 3000, size=8), rng.integers(1, 6, size=8))]
+    case = TreeCase(110 + D, Hq=16, Hkv=8, D=D, P=16, specs=specs, jitter=False, theta=1e12)
+    staircase(case, rng)
+    assert tiles_per_cta(case) >= 5
+    case.device()
+    if fp8:
+        # codes and scales made here, so that they are exact: a power of two per (page, kv head)
+        case.fp8 = True
+        ks = 2.0 ** rng.integers(-1, 3, size=(case.num_pages, case.Hkv))
+        vs = 2.0 ** rng.integers(-4, 4, size=(case.num_pages, case.Hkv))
+        kc = O.e4m3_encode((bf16_bits_to_f64(case.kp) / ks[:, :, None, None]).astype(np.float32))
+        vc = O.e4m3_encode(rng.standard_normal(case.vp.shape).astype(np.float32))
+        assert np.array_equal(O.dequantize_pages(kc, ks.astype(np.float32)), bf16_bits_to_f64(case.kp))
+        up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+        case.pools = RT.Fp8Pools.over(case.dev, up(kc), up(vc), up(ks.astype(np.float32)), up(vs.astype(np.float32)))
+    out = case.batch().run(LN2)
+    torch.cuda.synchronize()
+    assert case.dev.read_status() == 0
+    got = bf16_bits_to_f64(RT.bf16_bits(out))
+    kp, vp = (case.kp, case.vp) if not fp8 else (O.dequantize_pages(kc, ks.astype(np.float32)), O.dequantize_pages(vc, vs.astype(np.float32)))
+    for b in range(len(specs)):
+        r = slice(case.off[b], case.off[b + 1])
+        want, _ = O.tree_attention_one(case.q[r], case.kn[r], case.vn[r], case.row_pos[b], case.sees[b], kp, vp, case.page_ids[b],
+                                       case.pos_base[b], int(case.kv_len[b]), LN2, case.theta)
+        mean, _ = O.tree_attention_one(case.q[r], case.kn[r], f32_to_bf16_bits(np.abs(bf16_bits_to_f64(case.vn[r])).astype(np.float32)), case.row_pos[b], case.sees[b],
+                                       kp, np.abs(vp if fp8 else bf16_bits_to_f64(vp)), case.page_ids[b], case.pos_base[b], int(case.kv_len[b]), LN2, case.theta)
+        # the output's own rounding (2^-8 relative), and fp32 on the way: every weight, sum and product is off by at most 2^-21 of
+        # its value for the exponential and by 2^-23 for each of the n sums it passes through, relative to sum w |v|
+        n = int(case.kv_len[b] + case.rows[b])
+        tol = 2.0 ** -8 * np.abs(want) + (2 * 2.0 ** -21 + 2 * n * 2.0 ** -23) * mean
+        err = np.abs(got[r] - want)
+        assert (err <= tol).all(), (b, float((err / tol).max()), np.argwhere(err > tol)[:4].tolist())
