@@ -32,7 +32,8 @@
 //                   widen K on the way through the rotation, the softmax warps V; the K scales go into (cos, sin), the V scales
 //                   into P.
 //   MMA warps     : one issues S = Q' K'^T (three score buffers, each of which becomes its tile's P), one O += P V.
-// Every wait is bounded; a lost wait raises a flag that ends every role.
+// Every wait is bounded; a lost wait raises a flag that ends every role.  However a role ends, the loaders and the issuers first
+// wait (bounded) for what they have started.
 //
 // Measured (G = 4, D = 128, 8 kv heads, pages of 16).  32 requests x 16 rows over 8,256 slots: 203 us in a burst of calls, 232
 // to 244 in a run of them (the GPU is at its power limit then, and its clock at 1.66 GHz), of it 6 the merge; 986 MB of DRAM traffic,
@@ -361,7 +362,7 @@ constexpr int kBarCFree = 27;                                          // 8-bit 
 constexpr int kBarPFull = 31, kBarPvDone = 34;                         // [score buffer]
 constexpr int kBarQReady = 37, kBarOFree = 38;
 constexpr int kBarRef = 39, kBarItem = 47;                             // [warpgroup * 4 + warp], [warp]
-constexpr int kBarDrain = 51;                                          // [QK, PV] after a lost wait: the MMAs issued so far are done
+constexpr int kBarDrain = 51;                                          // [QK, PV] at the role's end: its MMAs are done
 constexpr int kBarSegFull = 53, kBarSegFree = 56;                      // [segment % 3]
 constexpr int kNumBars = 59;
 static_assert(kNumBars * 8 <= 472, "barrier block");
@@ -980,7 +981,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
     bool more = advance();
     int t = seg.t0;
     Next nx = look_up(t);
-    int gi = 0;
+    int gi = 0, issued = 0;                       // tiles so far; tiles whose copies were started
 #pragma unroll 1
     while (more) {
       const Next x = nx;
@@ -1007,6 +1008,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
           for (int nb = 0; nb < NB; ++nb) tma_load_2d(dst + nb * kBlockBytes, map, nb * 64, y, landed);
         }
       }
+      issued = gi + 1;
       if (!FP8 && !is_k && x.special) {
         if (live && !wait_warp(landed, static_cast<uint32_t>(gi / depth) & 1u)) break;
         const int end = ((x.left + 15) & ~15) * 2 * CH;
@@ -1021,10 +1023,10 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
       if (more) nx = look_up(t);
       ++gi;
     }
-    // after a lost wait: give the copies started last a bounded chance to land before shared memory is given up
-    if (*abort_flag)
-      for (int j = max(0, gi - depth); j < gi; ++j)
-        for (int i = 0; i < spin && !mbar_try_wait(is_k ? BAR(kBarKLanded, j % 6) : BAR(kBarVLanded, j % depth), static_cast<uint32_t>(is_k ? j / 6 : j / depth) & 1u); ++i) {}
+    // The copies started last have landed before shared memory is given up.  Always looked after, not only when this role
+    // itself lost a wait: another may lose one when this role is through.
+    for (int j = max(0, issued - depth); j < issued; ++j)
+      for (int i = 0; i < spin && !mbar_try_wait(is_k ? BAR(kBarKLanded, j % 6) : BAR(kBarVLanded, j % depth), static_cast<uint32_t>(is_k ? j / 6 : j / depth) & 1u); ++i) {}
     } else if (warp == kQkWarp) {
       // =============================================================== QK^T issuer
       // S of tile j goes to the buffer that held tile j - 3, once that tile's PV is through with it: the softmax finds the
@@ -1056,8 +1058,9 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
           __syncwarp();
         }
       }
-      if ((!ok || seg.t1 < 0) && lane == 0) {
-        // a wait was lost: the MMAs issued so far still run; tensor memory may only be released once they are done
+      if (lane == 0) {
+        // tensor memory may only be released once the MMAs issued so far are done: the softmax sees the last of them when all
+        // goes well, nobody does after a lost wait (anybody's)
         tc_commit(BAR(kBarDrain, 0));
         for (int i = 0; i < spin && !mbar_try_wait(BAR(kBarDrain, 0), 0); ++i) {}
       }
@@ -1099,7 +1102,7 @@ mepic_tree_attn(const __grid_constant__ TreeParams p, const __grid_constant__ CU
           __syncwarp();
         }
       }
-      if ((!ok || seg.t1 < 0) && lane == 0) {
+      if (lane == 0) {
         tc_commit(BAR(kBarDrain, 1));
         for (int k = 0; k < spin && !mbar_try_wait(BAR(kBarDrain, 1), 0); ++k) {}
       }
