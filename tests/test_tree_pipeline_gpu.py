@@ -172,3 +172,32 @@ def test_references_that_rise_in_the_middle_of_an_item(D, fp8):
         tol = 2.0 ** -8 * np.abs(want) + (2 * 2.0 ** -21 + 2 * n * 2.0 ** -23) * mean
         err = np.abs(got[r] - want)
         assert (err <= tol).all(), (b, float((err / tol).max()), np.argwhere(err > tol)[:4].tolist())
+
+
+@pytest.mark.parametrize("Hkv", [1, 8])              # a key tile per CTA, and several
+@pytest.mark.parametrize("D", [128, 64])
+def test_what_is_not_finite_shows_however_small_its_weight(D, Hkv):
+    # every row sees every context slot: a NaN or an infinity among their V cannot leave a finite output, also where the weight,
+    # 2^-200 here, is no fp32 number, and whichever CTA meets it.  The same for a drafted row that is seen.
+    case = TreeCase(120 + D, Hq=Hkv, Hkv=Hkv, D=D, P=16, specs=[(3000, 3), (2500, 2)], jitter=False, theta=1e12, kind="star")
+    case.q[:], case.kp[:], case.kn[:] = 0, 0, 0
+    pair = D // 2 - 1
+    case.q[..., pair] = f32_to_bf16_bits(np.float32([1.0]))[0]
+    high = f32_to_bf16_bits(np.float32([200.0]))[0]
+    for b, n in enumerate(case.kv_len):
+        for t in range(600, int(n)):
+            case.kp[case.page_ids[b, t // 16], :, t % 16, pair] = high
+    odd = {3: 0x7fc0, 7: 0x7f80, 40: 0xff80}
+    for d, bits in odd.items():
+        case.vp[case.page_ids[0, 2], :, 5, d] = bits                    # context slot 37 of the first request
+        case.vn[case.off[1], :, d] = bits                               # its first drafted row in the second
+    case.device()
+    out = case.batch().run(LN2)
+    torch.cuda.synchronize()
+    assert case.dev.read_status() == 0
+    got = bf16_bits_to_f64(RT.bf16_bits(out))
+    bad = np.zeros(got.shape, dtype=bool)
+    bad[:case.off[1], :, list(odd)] = True
+    bad[case.off[1], :, list(odd)] = True                               # a star: the other drafted row does not see that one
+    assert np.array_equal(~np.isfinite(got), bad)
+    assert np.isnan(got[:case.off[1] + 1, :, 3]).all()
