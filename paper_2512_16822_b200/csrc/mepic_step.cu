@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(kLayoutThreads) mepic_tree_layout_kernel(const
     for (int w = 0; w <= (i >> 5); ++w) depth += __popc(bits[i * W + w]);
     a.row_pos[rr.lo + i] = next + depth;
   }
-  for (int i = n + tid; i < rr.n; i += kLayoutThreads) {      // rows the mask has no room for (reported)
+  for (long long i = n + tid; i < rr.n; i += kLayoutThreads) {      // rows the mask has no room for (reported)
     for (int w = 0; w < W; ++w) out[static_cast<size_t>(i) * W + w] = 0;
     a.row_pos[rr.lo + i] = next;
   }
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kAcceptThreads) mepic_tree_accept_kernel(const
   }
   __syncthreads();
   const int n = path_n;
-  for (int k = tid; k < a.max_accept; k += kAcceptThreads)
+  for (long long k = tid; k < a.max_accept; k += kAcceptThreads)       // (any int32 length: counters that step past it are 64 bits wide)
     a.accept_rows[static_cast<size_t>(b) * a.max_accept + k] = k < n ? rr.lo + path[k] : -1;
 }
 
@@ -203,7 +203,8 @@ __global__ void __launch_bounds__(kTablesThreads) mepic_step_tables_kernel(const
     }
   }
   // ---- per new table entry
-  for (int t = gid; t < n_pages; t += step) {
+  for (long long at = gid; at < n_pages; at += step) {
+    const int t = static_cast<int>(at);
     const int b = find_request(page_off, a.batch, t);
     const int held = entries(__ldg(a.kv_len + b)), k = t - page_off[b];
     const int page = __ldg(a.reserve + used + t);
@@ -214,7 +215,8 @@ __global__ void __launch_bounds__(kTablesThreads) mepic_step_tables_kernel(const
   }
   // ---- per appended row
   if (!a.row_slot && !a.slot_map) return;
-  for (int r = gid; r < a.max_rows; r += step) {
+  for (long long at = gid; at < a.max_rows; at += step) {
+    const int r = static_cast<int>(at);
     int slot = -1;
     long long phys = -1;
     if (r < n_rows) {
@@ -289,10 +291,12 @@ constexpr int kCopyRows = 8;         // rows per CTA, one warp each
 template <int D>
 __global__ void __launch_bounds__(kCopyRows * 32) mepic_rows_commit_kernel(const __grid_constant__ CommitParams p) {
   constexpr int C = D / 8;           // 16-byte chunks per head row
-  const int lane = threadIdx.x & 31, r = blockIdx.x * kCopyRows + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  const long long at = static_cast<long long>(blockIdx.x) * kCopyRows + (threadIdx.x >> 5);
   const int n_rows = __ldg(p.row_offsets + p.batch);
   if (n_rows > p.max_rows && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
-  if (r >= min(n_rows, p.max_rows)) return;
+  if (at >= min(n_rows, p.max_rows)) return;
+  const int r = static_cast<int>(at);
   const long long slot = __ldg(reinterpret_cast<const long long*>(p.slot_map) + r);
   const int src = source_of(p, r, lane);
   if (src < 0) return;
@@ -392,7 +396,7 @@ __global__ void __launch_bounds__(kRunWarps * 32, 6) mepic_rows_commit_fp8_kerne
     bool fresh = false;
     for (bool more = true; more;) {
       const int r = first + n + lane;
-      const bool in = r < n_rows && n + lane < p.page_size && page_of(r) == page;
+      const bool in = n + lane < min(p.page_size, n_rows - first) && page_of(r) == page;
       const unsigned m = __ballot_sync(kFull, in);
       const int got = m == kFull ? 32 : __ffs(~m) - 1;
       fresh = fresh || __any_sync(kFull, lane < got && (__ldg(slots + r) & (p.page_size - 1)) == 0);
@@ -449,6 +453,7 @@ int shift_of(int page_size) {
   while ((1 << s) < page_size) ++s;
   return s;
 }
+long long ceil_div(long long a, int b) { return (a + b - 1) / b; }
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 int32_t launched(const char* what, int n = 1) {
   const cudaError_t e = cudaGetLastError();
@@ -488,9 +493,10 @@ int32_t commit_call(const mepic_config_t* cfg, const mepic_rows_commit_args_t* a
   p.n_slots = static_cast<long long>(cfg->num_pages) * cfg->page_size;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   // a CTA takes up to four of a run's (pool, kv head) blocks, one per warp: several CTAs fit an SM and hide one another's look-ups
-  if (fp8) mepic_rows_commit_fp8_kernel<<<dim3((a->max_rows + kRunRows - 1) / kRunRows, std::min((2 * cfg->n_kv_heads + kRunWarps - 1) / kRunWarps, 64)), kRunWarps * 32, 0, st>>>(p);
-  else if (cfg->head_dim == 128) mepic_rows_commit_kernel<128><<<(a->max_rows + kCopyRows - 1) / kCopyRows, kCopyRows * 32, 0, st>>>(p);
-  else mepic_rows_commit_kernel<64><<<(a->max_rows + kCopyRows - 1) / kCopyRows, kCopyRows * 32, 0, st>>>(p);
+  const unsigned run_ctas = static_cast<unsigned>(ceil_div(a->max_rows, kRunRows)), copy_ctas = static_cast<unsigned>(ceil_div(a->max_rows, kCopyRows));
+  if (fp8) mepic_rows_commit_fp8_kernel<<<dim3(run_ctas, std::min((2 * cfg->n_kv_heads + kRunWarps - 1) / kRunWarps, 64)), kRunWarps * 32, 0, st>>>(p);
+  else if (cfg->head_dim == 128) mepic_rows_commit_kernel<128><<<copy_ctas, kCopyRows * 32, 0, st>>>(p);
+  else mepic_rows_commit_kernel<64><<<copy_ctas, kCopyRows * 32, 0, st>>>(p);
   return launched(what);
 }
 
@@ -547,7 +553,7 @@ extern "C" int32_t mepic_step_tables(const mepic_config_t* cfg, const mepic_step
     if (e != cudaSuccess) { mepic_set_error("step_tables: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
   }
   const int work = std::max(a->row_slot || a->slot_map ? a->max_rows : 0, a->batch);
-  const int ctas = std::min(std::max(1, (work + 2 * kTablesThreads - 1) / (2 * kTablesThreads)), 296);
+  const int ctas = static_cast<int>(std::min<long long>(ceil_div(work, 2 * kTablesThreads), 296));
   mepic_step_tables_kernel<<<ctas, kTablesThreads, smem, static_cast<cudaStream_t>(cuda_stream)>>>(*a, shift_of(cfg->page_size), cfg->num_pages);
   return launched("step_tables");
 }
