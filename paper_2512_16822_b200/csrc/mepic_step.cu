@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kCopyRows * 32) mepic_rows_commit_kernel(const
   const long long at = static_cast<long long>(blockIdx.x) * kCopyRows + (threadIdx.x >> 5);
   const int n_rows = __ldg(p.row_offsets + p.batch);
   if (n_rows > p.max_rows && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
-  if (at >= min(n_rows, p.max_rows)) return;
+  if (at < __ldg(p.row_offsets) || at >= min(n_rows, p.max_rows)) return;      // (rows before the first request's are nobody's)
   const int r = static_cast<int>(at);
   const long long slot = __ldg(reinterpret_cast<const long long*>(p.slot_map) + r);
   const int src = source_of(p, r, lane);
@@ -376,6 +376,7 @@ __global__ void __launch_bounds__(kRunWarps * 32, 6) mepic_rows_commit_fp8_kerne
   const int all = __ldg(p.row_offsets + p.batch), n_rows = min(all, p.max_rows);
   if (all > p.max_rows && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
   if (r0 >= n_rows) return;
+  const int owned = max(__ldg(p.row_offsets), 0);      // the first row that is anybody's
   const long long* slots = reinterpret_cast<const long long*>(p.slot_map);
   auto page_of = [&](int r) -> int {
     const long long s = __ldg(slots + r);
@@ -383,10 +384,10 @@ __global__ void __launch_bounds__(kRunWarps * 32, 6) mepic_rows_commit_fp8_kerne
   };
   // rows of this CTA that start a run
   bool starts = false;
-  if (lane < kRunRows && r0 + lane < n_rows) {
+  if (lane < kRunRows && r0 + lane >= owned && r0 + lane < n_rows) {
     const int mine = page_of(r0 + lane);
     if (mine < 0) { if (warp == 0) atomicOr(p.status, MEPIC_DEV_BAD_PAGE); }
-    else starts = r0 + lane == 0 || page_of(r0 + lane - 1) != mine;
+    else starts = r0 + lane == owned || page_of(r0 + lane - 1) != mine;
   }
   for (unsigned todo = __ballot_sync(kFull, starts); todo; todo &= todo - 1) {
     const int first = r0 + __ffs(todo) - 1;

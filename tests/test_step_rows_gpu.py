@@ -1,0 +1,56 @@
+"""Which rows the commits of a step take, and steps without any."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_16822_b200 as M
+from paper_2512_16822_b200 import runtime as RT
+from paper_2512_16822_b200.build import build_library
+from tree_helpers import dev32
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build_library()
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+
+
+def _empty_pools(P, num_pages, fp8, Hkv=2, D=128):
+    dev = RT.Device(M.Config(P, Hkv, Hkv, D, num_pages, 4 * P, 1e4))
+    dev.k_pool.zero_(), dev.v_pool.zero_()
+    pools = RT.Fp8Pools(dev) if fp8 else None
+    return dev, pools
+
+
+def _written(dev, pools, w):
+    """[page, slot]: whether anything of the zeroed pool w (0: K, 1: V) was written."""
+    pool = ((pools.k_codes, pools.v_codes) if pools else (dev.k_pool, dev.v_pool))[w]
+    return pool.float().abs().amax(dim=(1, 3)).bool().nonzero().tolist()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("first,n", [(1, 1), (5, 4), (19, 30)])
+def test_rows_before_the_first_request_are_not_committed(fp8, gather, first, n):
+    # row_offsets start at `first`: the rows before it belong to nobody, whatever slots stand beside them (of the same page too)
+    P = 16
+    dev, pools = _empty_pools(P, 12, fp8)
+    total = first + n
+    rows = torch.ones((total, 2, 128), dtype=torch.bfloat16, device=DEV)
+    rows[:first] = 100.0                                                 # would set a page's scale
+    slots = torch.arange(3 * P, 3 * P + total, dtype=torch.int64, device=DEV)
+    src = dev32(np.arange(first, total)[None]) if gather else None
+    RT.RowsCommit(dev, k_new=rows, v_new=rows, row_offsets=dev32([first, total]), slot_map=slots, src_rows=src, pools=pools).run()
+    torch.cuda.synchronize()
+    assert dev.read_status() == 0
+    want = [[(3 * P + r) // P, (3 * P + r) % P] for r in range(first, total)]
+    assert _written(dev, pools, 0) == want and _written(dev, pools, 1) == want
+    if fp8:
+        for s in (pools.k_scales, pools.v_scales):
+            for page in {p for p, _ in want}:
+                started = [page, 0] in want
+                # a run that writes slot 0 sets the scale from its own rows (1 / 448 of their 1.0), any other leaves it
+                assert torch.equal(s[page], torch.full_like(s[page], 1.0) / 448.0 if started else torch.ones_like(s[page]))
