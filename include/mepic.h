@@ -686,8 +686,8 @@ int32_t mepic_step_tables(const mepic_config_t* cfg, const mepic_step_tables_arg
  * committed and set MEPIC_DEV_BAD_SLOT).  Slots must differ from row to row.
  *
  * mepic_rows_commit_fp8: into 8-bit pools by the rule of mepic_attn_prefill_fp8: consecutive rows that go to one page are
- * a run; a run that writes in-page slot 0 starts the page's blocks and sets their scales from its rows, any other run
- * appends under the scales that stand.  A page's rows must be consecutive, as mepic_step_tables makes them.
+ * a run; a run that writes in-page slot 0 starts the page's blocks and sets their scales from the rows it writes, any other
+ * run (one whose row for slot 0 is skipped, too) appends under the scales that stand.  A page's rows must be consecutive, as mepic_step_tables makes them.
  */
 typedef struct {
   const void*    k_new;        /* bf16 rows of [n_kv_heads][head_dim] */

@@ -400,7 +400,8 @@ __global__ void __launch_bounds__(kRunWarps * 32, 6) mepic_rows_commit_fp8_kerne
       const bool in = n + lane < min(p.page_size, n_rows - first) && page_of(r) == page;
       const unsigned m = __ballot_sync(kFull, in);
       const int got = m == kFull ? 32 : __ffs(~m) - 1;
-      fresh = fresh || __any_sync(kFull, lane < got && (__ldg(slots + r) & (p.page_size - 1)) == 0);
+      fresh = fresh || __any_sync(kFull, lane < got && (__ldg(slots + r) & (p.page_size - 1)) == 0 &&
+                                       lane_source_of(p, r) >= 0);       // (a skipped row writes nothing)
       n += got;
       more = got == 32;
     }

@@ -53,4 +53,23 @@ def test_rows_before_the_first_request_are_not_committed(fp8, gather, first, n):
             for page in {p for p, _ in want}:
                 started = [page, 0] in want
                 # a run that writes slot 0 sets the scale from its own rows (1 / 448 of their 1.0), any other leaves it
-                assert torch.equal(s[page], torch.full_like(s[page], 1.0) / 448.0 if started else torch.ones_like(s[page]))
+                assert (s[page] == (float(np.float32(1) / np.float32(448)) if started else 1.0)).all()
+
+
+@pytest.mark.parametrize("P", [16, 64])
+def test_a_skipped_row_does_not_start_a_page(P):
+    # the run's row for in-page slot 0 has no source: the run does not write slot 0, so it appends under the scale that stands
+    dev, pools = _empty_pools(P, 4, True)
+    for s in (pools.k_scales, pools.v_scales):
+        s.fill_(0.5)
+    rows = torch.full((4, 2, 128), 3.0, dtype=torch.bfloat16, device=DEV)
+    slots = torch.tensor([P, P + 1, P + 2, 2 * P, 2 * P + 1, 3 * P, 3 * P + 1], dtype=torch.int64, device=DEV)
+    src = dev32([[-1, 0, 9, 2, 1, -1, -1]])                              # page 1 appended to, page 2 started, page 3 left alone
+    RT.RowsCommit(dev, k_new=rows, v_new=rows, row_offsets=dev32([0, 7]), slot_map=slots, src_rows=src, pools=pools).run()
+    torch.cuda.synchronize()
+    assert dev.read_status() == M.MEPIC_DEV_BAD_SLOT
+    for w, (codes, scales) in enumerate(((pools.k_codes, pools.k_scales), (pools.v_codes, pools.v_scales))):
+        assert _written(dev, pools, w) == [[1, 1], [2, 0], [2, 1]]
+        assert (scales[[0, 1, 3]] == 0.5).all() and (scales[2] == float(np.float32(3) / np.float32(448))).all()
+        value = codes.view(torch.float8_e4m3fn).float()
+        assert (value[1, :, 1] == 6.0).all() and (value[2, :, :2] == 448.0).all()
