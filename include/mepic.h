@@ -681,7 +681,7 @@ int32_t mepic_step_tables(const mepic_config_t* cfg, const mepic_step_tables_arg
  * mepic_rows_commit - Section 3.3.2 for rows whose physical slots are known: appended row r (row_offsets[b] <= r <
  * row_offsets[b+1]) goes, un-rotated, to slot_map[r] of the pools.  Its K/V are row r of k_new / v_new, or, with src_rows
  * (the accept_rows of mepic_tree_accept), row src_rows[b][r - row_offsets[b]].  Source rows lie kv_stride elements apart
- * (0 = packed); n_sources of them exist.  A source outside [0, n_sources) sets MEPIC_DEV_BAD_SLOT, a slot outside the pool
+ * (0 = packed); n_sources of them exist (0: k_new and v_new may be NULL).  A source outside [0, n_sources) sets MEPIC_DEV_BAD_SLOT, a slot outside the pool
  * MEPIC_DEV_BAD_PAGE; the row is skipped.  max_rows bounds row_offsets[batch] (launch sizing; rows past it are not
  * committed and set MEPIC_DEV_BAD_SLOT).  Slots must differ from row to row.
  *

@@ -476,7 +476,7 @@ int32_t commit_call(const mepic_config_t* cfg, const mepic_rows_commit_args_t* a
     mepic_set_error("%s: kv_stride %d must be 0 or a multiple of 8 of at least n_kv_heads * head_dim", what, a->kv_stride); return MEPIC_E_INVAL;
   }
   if (a->max_rows == 0) return MEPIC_OK;
-  if (!a->k_new || !a->v_new || !a->row_offsets || !a->slot_map || !a->k_pool || !a->v_pool || !a->status) {
+  if ((a->n_sources > 0 && (!a->k_new || !a->v_new)) || !a->row_offsets || !a->slot_map || !a->k_pool || !a->v_pool || !a->status) {
     mepic_set_error("%s: NULL pointer argument", what); return MEPIC_E_INVAL;
   }
   if (a->src_rows && a->src_stride < 1) { mepic_set_error("%s: src_stride must be positive", what); return MEPIC_E_INVAL; }

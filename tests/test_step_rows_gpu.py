@@ -73,3 +73,30 @@ def test_a_skipped_row_does_not_start_a_page(P):
         assert (scales[[0, 1, 3]] == 0.5).all() and (scales[2] == float(np.float32(3) / np.float32(448))).all()
         value = codes.view(torch.float8_e4m3fn).float()
         assert (value[1, :, 1] == 6.0).all() and (value[2, :, :2] == 448.0).all()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_step_in_which_nobody_drafts(fp8):
+    # no rows at all in the row arrays: every call of the step is a call without work, and the lengths stay
+    B, P = 3, 16
+    dev, pools = _empty_pools(P, 6, fp8)
+    none = dev32([])
+    off, kv, ids, base = dev32([0] * (B + 1)), dev32([5, 0, 17]), dev32([[0, 1]] * B), dev32([[0, P]] * B)
+    q, k = torch.empty((0, 2, 128), dtype=torch.bfloat16, device=DEV), torch.empty((0, 2, 128), dtype=torch.bfloat16, device=DEV)
+    lay = RT.TreeLayout(dev, parent=none, row_offsets=off, kv_len=kv, pos_base=base, mask_words=1)
+    att = RT.TreeBatch(dev, q=q, k_new=k, v_new=k, row_offsets=off, row_pos=lay.row_pos, tree_mask=lay.tree_mask, page_ids=ids, pos_base=base,
+                       kv_len=kv, max_rows=4, pools=pools)
+    acc = RT.TreeAccept(dev, parent=none, row_offsets=off, draft=none, target=none, root=dev32([7, 8, 9]), max_accept=4)
+    tab = RT.StepTables(dev, kv_len=kv, n_new=acc.n_accept, page_ids=ids, pos_base=base, reserve=dev32([2]), reserve_used=dev32([0]), max_rows=4 * B)
+    com = RT.RowsCommit(dev, k_new=k, v_new=k, row_offsets=tab.row_offsets, slot_map=tab.slot_map, src_rows=acc.accept_rows, pools=pools)
+    for call in (lambda: lay.run(), lambda: att.run(0.1), lambda: acc.run(), lambda: tab.run(), lambda: com.run()):
+        call()
+    torch.cuda.synchronize()
+    assert dev.read_status() == 0
+    assert acc.n_accept.tolist() == [0] * B and acc.next_token.tolist() == [7, 8, 9] and (acc.accept_rows == -1).all()
+    assert tab.kv_len_out.tolist() == [5, 0, 17] and tab.row_offsets.tolist() == [0] * (B + 1) and tab.reserve_used_out.item() == 0
+    assert _written(dev, pools, 0) == [] and _written(dev, pools, 1) == []
+    # rows that are asked for all the same have no source
+    RT.RowsCommit(dev, k_new=k, v_new=k, row_offsets=dev32([0, 2]), slot_map=torch.tensor([3, 4], device=DEV), pools=pools).run()
+    torch.cuda.synchronize()
+    assert dev.read_status() == M.MEPIC_DEV_BAD_SLOT and _written(dev, pools, 0) == []
