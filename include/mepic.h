@@ -534,7 +534,10 @@ int32_t mepic_attn_prefill_fp8(const mepic_config_t* cfg, const mepic_prefill_ar
  *   mepic_tree_layout -> (per layer) mepic_attn_tree / _fp8 -> sampling by the caller -> mepic_tree_accept
  *   -> mepic_step_tables -> (per layer) mepic_rows_commit / _fp8.
  * mepic_step_tables and mepic_rows_commit know nothing of trees: they serve any append (one token per request of a plain
- * decode loop, a prompt's rows) and give mepic_attn_decode and mepic_attn_prefill their tables without a host round trip.
+ * decode loop, a prompt's rows).  mepic_attn_decode takes their tables, kv_len_out and q_pos as they are, with no host round
+ * trip; mepic_attn_prefill takes row_slot, the tables and kv_len_out, and needs row_offsets_host besides, which a caller has
+ * that chose n_new on the host.  A grouped-decode plan is built from tables on the host and does not follow tables that grow
+ * here: patch or rebuild it from a host copy (a call under a plan left behind sets MEPIC_DEV_BAD_PLAN).
  *
  * Rows are grouped by request: rows row_offsets[b] .. row_offsets[b+1]-1 of the row arrays belong to request b, which may
  * have none; row arrays hold total_rows rows and rows that no request owns are neither read nor written.  A row's parent

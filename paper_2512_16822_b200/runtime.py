@@ -528,7 +528,8 @@ class TreeAccept(_StepCall):
 
 class StepTables(_StepCall):
     """Block tables and slot maps from lengths: page_ids / pos_base grow in place out of ``reserve``;
-    run() -> dict(row_offsets, row_slot, slot_map, kv_len, q_pos, reserve_used)."""
+    run() -> dict(row_offsets, row_slot, slot_map, kv_len, q_pos, reserve_used).  The tables may be a DecodeBatch's own
+    (``batch.page_ids``, ``batch.pos_base``); its next run then needs ``kv_len`` and ``q_pos`` copied over."""
 
     def __init__(self, dev: Device, *, kv_len, n_new, page_ids, pos_base, reserve, reserve_used, max_rows: int):
         self.dev, d, i32 = dev, dev.device, torch.int32
