@@ -1151,10 +1151,8 @@ __global__ void __launch_bounds__(kMergeRows * 32) mepic_tree_merge(const __grid
     for (int k = 0; k < 8; ++k) {
       const float wk = __shfl_sync(kFull, wgt, k);
       // (a weight that underflows leaves nothing of what is finite, and NaN of what is not, as 0 x inf does inside a part)
-      o.x += wk != 0.f ? x[k].x * wk : x[k].x - x[k].x;
-      o.y += wk != 0.f ? x[k].y * wk : x[k].y - x[k].y;
-      o.z += wk != 0.f ? x[k].z * wk : x[k].z - x[k].z;
-      o.w += wk != 0.f ? x[k].w * wk : x[k].w - x[k].w;
+      if (wk != 0.f) { o.x += x[k].x * wk; o.y += x[k].y * wk; o.z += x[k].z * wk; o.w += x[k].w * wk; }
+      else if (k0 + k < parts) { o.x += x[k].x - x[k].x; o.y += x[k].y - x[k].y; o.z += x[k].z - x[k].z; o.w += x[k].w - x[k].w; }
     }
   }
 #pragma unroll
