@@ -292,10 +292,10 @@ template <int D>
 __global__ void __launch_bounds__(kCopyRows * 32) mepic_rows_commit_kernel(const __grid_constant__ CommitParams p) {
   constexpr int C = D / 8;           // 16-byte chunks per head row
   const int lane = threadIdx.x & 31;
-  const long long at = static_cast<long long>(blockIdx.x) * kCopyRows + (threadIdx.x >> 5);
-  const int n_rows = __ldg(p.row_offsets + p.batch);
+  const unsigned at = blockIdx.x * kCopyRows + (threadIdx.x >> 5);
+  const int owned = __ldg(p.row_offsets), n_rows = __ldg(p.row_offsets + p.batch);      // rows before the first request's are nobody's
   if (n_rows > p.max_rows && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
-  if (at < __ldg(p.row_offsets) || at >= min(n_rows, p.max_rows)) return;      // (rows before the first request's are nobody's)
+  if (at < static_cast<unsigned>(max(owned, 0)) || at >= static_cast<unsigned>(max(min(n_rows, p.max_rows), 0))) return;
   const int r = static_cast<int>(at);
   const long long slot = __ldg(reinterpret_cast<const long long*>(p.slot_map) + r);
   const int src = source_of(p, r, lane);
@@ -373,10 +373,10 @@ __global__ void __launch_bounds__(kRunWarps * 32, 6) mepic_rows_commit_fp8_kerne
   constexpr int D = 128;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int r0 = blockIdx.x * kRunRows;
+  const int owned = max(__ldg(p.row_offsets), 0);      // the first row that is anybody's
   const int all = __ldg(p.row_offsets + p.batch), n_rows = min(all, p.max_rows);
   if (all > p.max_rows && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
   if (r0 >= n_rows) return;
-  const int owned = max(__ldg(p.row_offsets), 0);      // the first row that is anybody's
   const long long* slots = reinterpret_cast<const long long*>(p.slot_map);
   auto page_of = [&](int r) -> int {
     const long long s = __ldg(slots + r);
