@@ -8,7 +8,7 @@ from paper_2512_16822_b200 import runtime as RT
 from paper_2512_16822_b200.build import build_library
 from mepic_inputs import bf16_bits_to_f64, f32_to_bf16_bits
 from oracle import mepic_oracle as O
-from tree_helpers import TreeCase
+from tree_helpers import TreeCase, dev32
 
 pytestmark = pytest.mark.gpu
 
@@ -201,3 +201,16 @@ def test_what_is_not_finite_shows_however_small_its_weight(D, Hkv):
     bad[case.off[1], :, list(odd)] = True                               # a star: the other drafted row does not see that one
     assert np.array_equal(~np.isfinite(got), bad)
     assert np.isnan(got[:case.off[1] + 1, :, 3]).all()
+
+
+@pytest.mark.parametrize("B", [2, 40])               # the cut by one warp, and by the CTA
+def test_rows_that_no_request_owns_at_all(B):
+    case = TreeCase(130, Hq=4, Hkv=1, D=128, P=16, specs=[(100, 3)] + [(50, 0)] * (B - 1))
+    case.device()
+    q, k, v = (RT.bf16_tensor(x, "cuda:0") for x in (case.q, case.kn, case.vn))
+    batch = RT.TreeBatch(case.dev, q=q, k_new=k, v_new=v, row_offsets=dev32([0] * (B + 1)), row_pos=dev32(np.concatenate(case.row_pos)),
+                         tree_mask=dev32(case.mask()), page_ids=dev32(case.page_ids), pos_base=dev32(case.pos_base), kv_len=dev32(case.kv_len), max_rows=3)
+    batch.out.fill_(7.0)
+    batch.run(0.09)
+    torch.cuda.synchronize()
+    assert case.dev.read_status() == 0 and (batch.out == 7.0).all()
