@@ -269,8 +269,8 @@ __device__ __forceinline__ int source_of(const CommitParams& p, int r, int lane)
   return src;
 }
 
-// The same for one lane (a row of its own).
-__device__ __forceinline__ int lane_source_of(const CommitParams& p, int r) {
+// The same for one lane (a row of its own), and without a word where there is none.
+__device__ __forceinline__ int lane_source_or_none(const CommitParams& p, int r) {
   int src = r;
   if (p.src_rows) {
     int lo = 0, hi = p.batch;                    // row_offsets[lo] <= r < row_offsets[hi]
@@ -281,8 +281,7 @@ __device__ __forceinline__ int lane_source_of(const CommitParams& p, int r) {
     const int k = r - __ldg(p.row_offsets + lo);
     src = k >= 0 && k < p.src_stride ? __ldg(p.src_rows + static_cast<size_t>(lo) * p.src_stride + k) : -1;
   }
-  if (src < 0 || src >= p.n_sources) { atomicOr(p.status, MEPIC_DEV_BAD_SLOT); return -1; }
-  return src;
+  return src < 0 || src >= p.n_sources ? -1 : src;
 }
 
 // bf16 pages: a warp per row, 16 bytes a lane, K and V together.  Bound by latency where it is used most: 128 accepted rows of
@@ -354,12 +353,14 @@ __device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t m, uint32_t x) {
   return m;
 }
 // Rows r0 .. r0 + min(n, 16) - 1 of pool w, kv head h: a lane's 16-byte pieces of eight rows (half a warp takes a row), and in
-// lane k < 16 the in-page slot of row k (-1: nothing to write).
-__device__ __forceinline__ void load_block(const CommitParams& p, int w, int r0, int n, int h, int lane, uint4 (&v)[8], int& slot) {
+// lane k < 16 the in-page slot of row k (-1: nothing to write).  known: in lane k, the source of row cta_r0 + k.
+__device__ __forceinline__ void load_block(const CommitParams& p, int w, int r0, int n, int h, int lane, int cta_r0, int known, uint4 (&v)[8], int& slot) {
+  const int found = p.src_rows ? __shfl_sync(kFull, known, (r0 + lane - cta_r0) & 31) : -1;
   int src = -1;
   slot = -1;
   if (lane < 16 && lane < n) {
-    src = lane_source_of(p, r0 + lane);
+    src = p.src_rows && r0 + lane - cta_r0 < kRunRows ? found : lane_source_or_none(p, r0 + lane);
+    if (src < 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT);
     slot = src < 0 ? -1 : static_cast<int>(__ldg(reinterpret_cast<const long long*>(p.slot_map) + r0 + lane)) & (p.page_size - 1);
   }
   const uint16_t* base = p.src[w] + h * 128 + 8 * (lane & 15);
@@ -382,7 +383,10 @@ __global__ void __launch_bounds__(kRunWarps * 32, 6) mepic_rows_commit_fp8_kerne
     const long long s = __ldg(slots + r);
     return s < 0 || s >= p.n_slots ? -1 : static_cast<int>(s >> p.page_shift);
   };
-  // rows of this CTA that start a run
+  // the sources of this CTA's rows, looked up once, beside their slots (again for each run and block: 2 us more on 32 requests
+  // of 4 rows), and which of the rows start a run
+  const int known = lane < kRunRows && r0 + lane < n_rows ? lane_source_or_none(p, r0 + lane) : -1;
+  const unsigned sourced = __ballot_sync(kFull, known >= 0);
   bool starts = false;
   if (lane < kRunRows && r0 + lane >= owned && r0 + lane < n_rows) {
     const int mine = page_of(r0 + lane);
@@ -400,8 +404,8 @@ __global__ void __launch_bounds__(kRunWarps * 32, 6) mepic_rows_commit_fp8_kerne
       const bool in = n + lane < min(p.page_size, n_rows - first) && page_of(r) == page;
       const unsigned m = __ballot_sync(kFull, in);
       const int got = m == kFull ? 32 : __ffs(~m) - 1;
-      fresh = fresh || __any_sync(kFull, lane < got && (__ldg(slots + r) & (p.page_size - 1)) == 0 &&
-                                       lane_source_of(p, r) >= 0);       // (a skipped row writes nothing)
+      const bool begins = lane < got && (__ldg(slots + r) & (p.page_size - 1)) == 0;      // a skipped row writes nothing, slot 0 neither
+      fresh = fresh || __any_sync(kFull, begins && (r - r0 < kRunRows ? ((sourced >> (r - r0)) & 1) != 0 : lane_source_or_none(p, r) >= 0));
       n += got;
       more = got == 32;
     }
@@ -418,7 +422,7 @@ __global__ void __launch_bounds__(kRunWarps * 32, 6) mepic_rows_commit_fp8_kerne
         uint32_t m2[2] = {0, 0};                   // bf16 maxima are exact
 #pragma unroll 1
         for (int k0 = 0; k0 < n; k0 += 16) {
-          load_block(p, w, first + k0, n - k0, h, lane, v, slot);
+          load_block(p, w, first + k0, n - k0, h, lane, r0, known, v, slot);
 #pragma unroll
           for (int u = 0; u < 8; ++u) {
             m2[0] = max_abs_bf16x2(max_abs_bf16x2(m2[0], v[u].x), v[u].y);
@@ -438,7 +442,7 @@ __global__ void __launch_bounds__(kRunWarps * 32, 6) mepic_rows_commit_fp8_kerne
       const bool plain = sc >= 8.2718061e-25f && sc <= 1.2089258e24f;       // 2^-80 .. 2^80
 #pragma unroll 1
       for (int k0 = 0; k0 < n; k0 += 16) {
-        if (!fresh || n > 16) load_block(p, w, first + k0, n - k0, h, lane, v, slot);
+        if (!fresh || n > 16) load_block(p, w, first + k0, n - k0, h, lane, r0, known, v, slot);
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
           const int in_page = __shfl_sync(kFull, slot, 2 * u + half);
