@@ -690,7 +690,11 @@ int32_t mepic_step_tables(const mepic_config_t* cfg, const mepic_step_tables_arg
  *
  * mepic_rows_commit_fp8: into 8-bit pools by the rule of mepic_attn_prefill_fp8: consecutive rows that go to one page are
  * a run; a run that writes in-page slot 0 starts the page's blocks and sets their scales from the rows it writes, any other
- * run (one whose row for slot 0 is skipped, too) appends under the scales that stand.  A page's rows must be consecutive, as mepic_step_tables makes them.
+ * run (one whose row for slot 0 is skipped, too) appends under the scales that stand.  A page filled a few rows at a time thus
+ * keeps the scale of the rows that came first, and larger elements of later rows saturate.  Pages of 16, rows of one
+ * magnitude: relative error of a page 2.6 % when filled at once, 3.0 / 3.5 / 4.6 % when 4 / 2 / 1 rows come at a time, of the
+ * worst row 4 % against 20 to 26 %.  Rows whose magnitudes vary (log-normal, 0.5): 2.6 % against 14 / 20 / 29 %, the worst row
+ * 4 % against 67 to 89 %.  Where that matters, keep the pages that a step writes in bf16 pools.  A page's rows must be consecutive, as mepic_step_tables makes them.
  */
 typedef struct {
   const void*    k_new;        /* bf16 rows of [n_kv_heads][head_dim] */

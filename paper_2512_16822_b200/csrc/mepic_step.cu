@@ -24,7 +24,7 @@ using namespace mepic_dev;
 // nearest ancestors and log2(depth) rounds do.  (A thread per row walking up its chain took 8 us on trees of 200 rows and
 // depth 45.)  A row may read another's words while those grow: they only ever hold true ancestors, so whatever it reads is
 // right, and the pointers, of which that is not so, are kept twice.  The depth is the number of bits.
-// Bound by latency: 2.5 us for one tree of 8 rows, 5.4 us for 128 trees of 200 rows (device time, calls replayed in a graph).
+// Bound by latency: 2.3 us for one tree of 8 rows, 5.4 us for 128 trees of 200 rows (device time, calls replayed in a graph).
 constexpr int kLayoutThreads = 512;
 __global__ void __launch_bounds__(kLayoutThreads) mepic_tree_layout_kernel(const mepic_tree_layout_args_t a, int page_shift) {
   __shared__ int16_t up[2][MEPIC_TREE_MAX_ROWS];
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kAcceptThreads) mepic_tree_accept_kernel(const
 // shared memory; it then writes its share of the outputs, which all follow from those sums, by binary search.  No CTA reads
 // what another writes: an appended row's page comes from the table only where the entry existed before the call.  (One CTA
 // for the sums and a second launch for the rest would cost a launch, 2 us, to save a scan of a few hundred loads.)  Bound by
-// latency: 4.0 us for 32 requests that gain 4 slots each, 4.9 us for 64 prompts of up to 2,048 rows.
+// latency: 4.0 us for 32 requests that gain 4 slots each, 4.7 us for 64 prompts of up to 2,048 rows.
 constexpr int kTablesThreads = 512;
 __device__ __forceinline__ int find_request(const int* off, int batch, int r) {       // the b with off[b] <= r < off[b + 1]
   int lo = 0, hi = batch;                       // off[lo] <= r < off[hi]
@@ -285,7 +285,8 @@ __device__ __forceinline__ int lane_source_or_none(const CommitParams& p, int r)
 }
 
 // bf16 pages: a warp per row, 16 bytes a lane, K and V together.  Bound by latency where it is used most: 128 accepted rows of
-// 8 kv heads (0.8 MB) take 3.9 us.
+// 8 kv heads (0.8 MB) take 3.7 us, a launch and five dependent loads (row count, offsets search, offset, source, row); 12,900
+// prompt rows (106 MB) 25 us, 4.3 TB/s.
 constexpr int kCopyRows = 8;         // rows per CTA, one warp each
 template <int D>
 __global__ void __launch_bounds__(kCopyRows * 32) mepic_rows_commit_kernel(const __grid_constant__ CommitParams p) {
@@ -313,10 +314,12 @@ __global__ void __launch_bounds__(kCopyRows * 32) mepic_rows_commit_kernel(const
 
 // 8-bit pages.  A CTA looks at kRunRows consecutive rows and does the runs (rows that go to one page) that START among
 // them, whole; each of its warps takes one (pool, kv head) of a run at a time, so a block's maximum, scale and codes stay
-// in one warp.  (A CTA per row left 15 of 16 CTAs of a prompt with nothing to do.)  12,000 prompt rows of 8 kv heads (79 MB
-// read and written): 30 us, 2.6 TB/s; about 1,250 instructions per block of 16 rows and a chain of dependent look-ups (slots,
-// sources, rows, maximum, codes), which the CTAs of an SM hide from one another only in part.  (CTAs of 8 warps: 31; of 2: 46;
-// each warp two blocks of a run: 34; rolled loops over a lane's eight pieces: 35.)
+// in one warp.  (A CTA per row left 15 of 16 CTAs of a prompt with nothing to do.)  12,900 prompt rows of 8 kv heads (79 MB
+// read and written): 39 us (2.0 TB/s), 31 with the inputs in L2; about 1,250 instructions per block of 16 rows and a chain of
+// dependent look-ups (slots, sources, rows, maximum, codes), which the CTAs of an SM hide from one another only in part: issue
+// slots 50 %, DRAM 16.  A few rows per request make many short runs, which a CTA does one after the other: 32 x 4 rows 25 us,
+// 256 x 4 28, 256 x 1 47.  (Prompts, inputs in L2, with CTAs of 8 warps 31; of 2 46; each warp two blocks of a run 34; rolled
+// loops over a lane's eight pieces 35.)
 constexpr int kRunRows = 16;
 constexpr int kRunWarps = 4;
 // Eight elements -> E4M3(x / sc), the quotient rounded to fp32 first, as the format is defined.  With y = RN(1 / sc) and no

@@ -4,7 +4,9 @@
 // heads of the kv head) against the request's keys, first the context's slots, then the request's drafted rows under the
 // mask.  Keys are taken 128 at a time: S = Q' K'^T, P = 2^(S - reference), O += P V, with Q' = R(row_pos) q * sm_scale *
 // log2(e) and K' = R(pos) k, a reference per row that only moves when a score lies more than 2^8 above it, and the sum of
-// P in fp32.  Q', K' and P are rounded to bf16 once each, everything else is fp32.
+// P in fp32.  Q', K' and P are rounded to bf16 once each, because the MMA takes both operands in one 16-bit type and the pages'
+// V is bf16: fp16 would keep three bits more of them, but it ends at 65504, which bf16 pages may pass.  Everything else is fp32,
+// the sum of P too, which takes the weights as they are before their rounding.
 //
 // What bounds it.  One key tile is 512 D bytes of K and V and 4 * 128 * 128 * D operations: with up to 128 query vectors an
 // item is bound by HBM (a tile's bytes take an SM's share of the bandwidth 1.5 us, its MMAs 0.6), beyond that items share
@@ -24,8 +26,8 @@
 //                   where the PV MMA takes P from.
 //   rotator warps : rotate the K tile in place in shared memory, fp32 arithmetic, one rounding.  They also bring the drafted
 //                   K rows (plain loads: one tile per item, at positions of their own).
-//   loader warps  : one for K, one for V; TMA boxes of 16 rows x 64 dims (128-byte swizzle) per 16-slot group, the page ids
-//                   of the tile after next fetched while the ring is full.  The V loader also clears V rows past kv_len,
+//   loader warps  : one for K, one for V; TMA boxes of 16 rows x 64 dims (128-byte swizzle) per 16-slot group, the next
+//                   tile's page ids fetched while the ring is full.  The V loader also clears V rows past kv_len,
 //                   brings the drafted V rows and takes non-finite elements out of them: 0 x inf would reach rows that the
 //                   mask hides them from.  The rows that do see such an element get it added in the epilogue.
 //                   Over 8-bit pages the loaders bring the codes into rings of their own (untiled bulk copies); the rotators
@@ -35,13 +37,15 @@
 // Every wait is bounded; a lost wait raises a flag that ends every role.  However a role ends, the loaders and the issuers first
 // wait (bounded) for what they have started.
 //
-// Measured (G = 4, D = 128, 8 kv heads, pages of 16).  32 requests x 16 rows over 8,256 slots: 203 us in a burst of calls, 232
-// to 244 in a run of them (the GPU is at its power limit then, and its clock at 1.66 GHz), of it 6 the merge; 986 MB of DRAM traffic,
-// 55 % of the bandwidth; the tensor pipe is active 30 % of the time, the exponential unit 14, issue slots 40.  8 x 96 rows over
-// 16,640: 317 us (146 GFLOP, 460 TFLOP/s).  8 x 32 rows over 65,536 slots of 8-bit pages: 446 us.  One request of 8 rows over
-// 203 slots: 12.5 us, two launches.  What bounds the large ones is none of the units but the hand-over of a tile from role to
-// role (load, rotate, QK^T, softmax, PV: each waits for latency, and for instructions, which twenty warps with five programs
-// fetch through one cache).
+// Measured (G = 4, D = 128, 8 kv heads, pages of 16).  32 requests x 16 rows over 8,256 slots: 209 us in a burst of calls, 230
+// to 243 in a run of them (the GPU is at its power limit then, and its clock at 1.66 to 1.76 GHz), of it 6 the merge; 986 MB of
+// DRAM traffic, 55 % of the bandwidth; the tensor pipe is active 30 % of the time, the exponential unit 14, issue slots 40.
+// 8 x 96 rows over 16,640: 295 us in a burst, 314 to 324 in a run (146 GFLOP, 450 TFLOP/s).  8 x 32 rows over 65,536 slots of
+// 8-bit pages: 432 and 448 to 464 us.  One request of 8 rows over 203 slots: 12.3 us, two launches.  A pass (row tile x key
+// tile) takes 2.3 to 2.4 us in all three large ones, whatever its rows, bytes and type: what bounds them is none of the units but
+// the hand-over of a tile from role to role (load, rotate, QK^T, softmax, PV: each waits for latency, and for instructions, which
+// twenty warps with five programs fetch through one cache).  Warp instructions per pass: 5,400, with full row tiles 6,400, over
+// 8-bit pages 9,000 (issue slots 57 %).
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
