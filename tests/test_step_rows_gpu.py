@@ -6,6 +6,8 @@ import torch
 import paper_2512_16822_b200 as M
 from paper_2512_16822_b200 import runtime as RT
 from paper_2512_16822_b200.build import build_library
+from mepic_inputs import f32_to_bf16_bits
+from oracle import mepic_oracle as O
 from tree_helpers import dev32
 
 pytestmark = pytest.mark.gpu
@@ -100,3 +102,42 @@ def test_a_step_in_which_nobody_drafts(fp8):
     RT.RowsCommit(dev, k_new=k, v_new=k, row_offsets=dev32([0, 2]), slot_map=torch.tensor([3, 4], device=DEV), pools=pools).run()
     torch.cuda.synchronize()
     assert dev.read_status() == M.MEPIC_DEV_BAD_SLOT and _written(dev, pools, 0) == []
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("P,Hkv", [(128, 3), (512, 1)])
+def test_commit_into_long_pages_in_any_order_of_slots(fp8, P, Hkv):
+    # runs of hundreds of rows, whole pages among them, whose slots do not ascend; gathered from twice as many sources
+    rng, D, pages = np.random.default_rng(P), 128, 6
+    bits = lambda shape: f32_to_bf16_bits((rng.standard_normal(shape) * 2).astype(np.float32))
+    kp, vp = bits((pages, Hkv, P, D)), bits((pages, Hkv, P, D))
+    dev = RT.Device(M.Config(P, Hkv, Hkv, D, pages, P, 1e4), kp, vp)
+    pools = RT.Fp8Pools(dev) if fp8 else None
+    parts = [(4, rng.permutation(P)), (1, 1 + rng.permutation(P - 1)[:P // 2 + 5]), (5, rng.permutation(P // 2)), (0, np.array([P - 1]))]
+    off = np.array([0, P, P + len(parts[1][1]), P + len(parts[1][1]) + len(parts[2][1]) + 1])       # the third request takes two pages
+    slots = np.concatenate([page * P + t for page, t in parts])
+    total = len(slots)
+    k, v = bits((2 * total, Hkv, D)), bits((2 * total, Hkv, D))
+    src = np.full((3, int(np.diff(off).max())), -1)
+    for b in range(3):
+        src[b, :off[b + 1] - off[b]] = rng.choice(np.arange(2 * total), size=off[b + 1] - off[b], replace=False)
+    flat = np.concatenate([src[b, :off[b + 1] - off[b]] for b in range(3)])
+    RT.RowsCommit(dev, k_new=RT.bf16_tensor(k, DEV), v_new=RT.bf16_tensor(v, DEV), row_offsets=dev32(off),
+                  slot_map=torch.from_numpy(slots.astype(np.int64)).to(DEV), src_rows=dev32(src), pools=pools).run()
+    torch.cuda.synchronize()
+    assert dev.read_status() == 0
+    if fp8:
+        (kc, ks), (vc, vs) = O.quantize_pages(kp), O.quantize_pages(vp)
+    at = 0
+    for page, t in parts:
+        rows = flat[at:at + len(t)]
+        at += len(t)
+        if fp8:
+            O.commit_rows_fp8(kc, ks, vc, vs, [page], list(t), k[rows], v[rows])
+        else:
+            O.commit_rows(kp, vp, [page], list(t), k[rows], v[rows])
+    if fp8:
+        assert np.array_equal(pools.k_scales.cpu().numpy(), ks) and np.array_equal(pools.v_scales.cpu().numpy(), vs)
+        assert np.array_equal(pools.k_codes.cpu().numpy(), kc) and np.array_equal(pools.v_codes.cpu().numpy(), vc)
+    else:
+        assert np.array_equal(RT.bf16_bits(dev.k_pool), kp) and np.array_equal(RT.bf16_bits(dev.v_pool), vp)
