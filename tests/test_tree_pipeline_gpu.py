@@ -214,3 +214,17 @@ def test_rows_that_no_request_owns_at_all(B):
     batch.run(0.09)
     torch.cuda.synchronize()
     assert case.dev.read_status() == 0 and (batch.out == 7.0).all()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_requests_that_alias_long_chunks_at_positions_of_their_own(fp8):
+    # 150 pages that six requests share, in another order and at other positions in each, before pages of their own
+    rng = np.random.default_rng(140)
+    case = TreeCase(140, Hq=16, Hkv=8, D=128, P=16, specs=[(int(n), int(r)) for n, r in zip(rng.integers(2450, 3500, size=6), (1, 5, 2, 9, 1, 3))],
+                    fp8=fp8, theta=5e5)
+    page_amplitudes(case, -3, -3, 3)
+    common = case.page_ids[0, :150].copy()
+    for b in range(1, 6):
+        case.page_ids[b, :150] = rng.permutation(common) if b % 2 else common
+    assert len({tuple(case.pos_base[b, :150]) for b in range(6)}) == 6
+    run_and_check(case, 1.0 / np.sqrt(128), 7)
