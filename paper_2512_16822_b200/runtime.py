@@ -406,8 +406,8 @@ class _StepCall:
     """One call of a step over buffers that stay in place: the argument struct is filled once, ``run`` only launches, so that a
     step costs the host a few microseconds and can be captured into a graph.  Inputs are read when the kernels run.  The results
     and the workspace are the object's own and the next ``run`` writes them again: runs that may overlap on the GPU need an
-    object each.  An object may be dropped while its kernels still run, on whatever stream, but not before a graph that
-    captured it."""
+    object each.  An object may be dropped while its kernels still run on a torch stream; on a stream of the caller's own (a raw
+    handle, an ExternalStream) it has to outlive them, and a graph that captured it always."""
 
     def _bind(self, dev: Device, name: str, args, *, with_cfg: bool = True, extra=(), keep=()):
         self.dev = dev
@@ -419,18 +419,21 @@ class _StepCall:
 
     def _record(self, stream, raw: int) -> None:
         """Tells the allocator that ``stream`` uses what is bound: memory of a dropped object is handed out again only when
-        its kernels are through."""
+        its kernels are through.  Not for a stream of the caller's own: the allocator comes back to the stream when the
+        memory is freed, and such a stream may be gone by then."""
+        if isinstance(stream, int):
+            return
         if stream is None:
             stream = torch.cuda.current_stream(self._index)
-        elif isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(raw, device=self._index) if raw else torch.cuda.default_stream(self._index)
+        self._streams.add(raw)
+        if stream.stream_id and stream.stream_id % 2 == 0:                     # a handle that torch did not make
+            return
         held = list(vars(self).values()) + [self.dev.rope, self.dev.status]
         for t in self._keep:
             held += [t.k_codes, t.v_codes, t.k_scales, t.v_scales] if isinstance(t, Fp8Pools) else [t]
         for t in held:
             if isinstance(t, torch.Tensor) and t.numel():
                 t.record_stream(stream)
-        self._streams.add(raw)
 
     def _launch(self, stream=None) -> None:
         if torch._C._cuda_getDevice() != self._index:                # (the private forms of current_device and current_stream: the
