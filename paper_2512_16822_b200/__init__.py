@@ -103,12 +103,22 @@ class _DecodeGroupedArgsC(C.Structure):
                 ("status", C.c_void_p), ("batch", C.c_int32), ("sm_scale", C.c_float)]
 
 
-class _TreeLayoutArgsC(C.Structure):
+class _StepArgs(C.Structure):
+    """Arguments in the order of the fields.  A count or stride that 32 bits do not hold is refused: ctypes would cut it."""
+
+    def __init__(self, *values):
+        for (name, kind), v in zip(self._fields_, values):
+            if kind is C.c_int32 and not -2 ** 31 <= v < 2 ** 31:
+                raise MepicError(MEPIC_E_INVAL, f"{name} = {v} does not fit in 32 bits")
+        super().__init__(*values)
+
+
+class _TreeLayoutArgsC(_StepArgs):
     _fields_ = [(n, C.c_void_p) for n in ("parent", "row_offsets", "kv_len", "pos_base", "row_pos", "tree_mask", "status")] + \
                [(n, C.c_int32) for n in ("table_stride", "batch", "total_rows", "mask_words")]
 
 
-class _AttnTreeArgsC(C.Structure):
+class _AttnTreeArgsC(_StepArgs):
     _fields_ = [(n, C.c_void_p) for n in ("q", "k_new", "v_new", "row_offsets", "row_pos", "tree_mask", "k_pool", "v_pool", "page_ids",
                                           "pos_base", "kv_len", "rope_table", "out", "workspace")] + \
                [("workspace_bytes", C.c_size_t), ("status", C.c_void_p)] + \
@@ -116,18 +126,18 @@ class _AttnTreeArgsC(C.Structure):
                [("sm_scale", C.c_float)]
 
 
-class _TreeAcceptArgsC(C.Structure):
+class _TreeAcceptArgsC(_StepArgs):
     _fields_ = [(n, C.c_void_p) for n in ("parent", "row_offsets", "draft", "target", "root", "n_accept", "accept_rows", "next_token",
                                           "status")] + [(n, C.c_int32) for n in ("batch", "total_rows", "max_accept")]
 
 
-class _StepTablesArgsC(C.Structure):
+class _StepTablesArgsC(_StepArgs):
     _fields_ = [(n, C.c_void_p) for n in ("kv_len", "n_new", "page_ids", "pos_base", "reserve", "reserve_used", "row_offsets", "row_slot",
                                           "slot_map", "kv_len_out", "q_pos", "reserve_used_out", "status")] + \
                [(n, C.c_int32) for n in ("table_stride", "batch", "max_rows", "n_reserve")]
 
 
-class _RowsCommitArgsC(C.Structure):
+class _RowsCommitArgsC(_StepArgs):
     _fields_ = [(n, C.c_void_p) for n in ("k_new", "v_new", "row_offsets", "slot_map", "src_rows", "k_pool", "v_pool", "status")] + \
                [(n, C.c_int32) for n in ("src_stride", "batch", "max_rows", "n_sources", "kv_stride")]
 

@@ -125,3 +125,25 @@ def test_pools_that_are_not_the_devices_are_refused():
         small.v_pool = small.v_pool[:9]
         with pytest.raises(ValueError, match="pool"):
             build(small)
+
+
+def test_counts_and_strides_that_32_bits_do_not_hold_are_refused():
+    # (ctypes keeps the low 32 bits of a larger number: 2^32 + 3 rows were 3, a row stride of 2^32 was 0, "packed")
+    ptr, big = 1 << 20, 2 ** 32
+    calls = [
+        lambda: M.mepic_step_tables(CFG, kv_len=ptr, n_new=ptr + 64, page_ids=ptr, pos_base=ptr, reserve=ptr, reserve_used=ptr + 128, row_offsets=ptr,
+                                    kv_len_out=ptr + 256, reserve_used_out=ptr + 512, status=ptr, table_stride=4, batch=1, max_rows=big + 3, n_reserve=2),
+        lambda: M.mepic_tree_layout(CFG, parent=ptr, row_offsets=ptr, kv_len=ptr, pos_base=ptr, row_pos=ptr, tree_mask=ptr, status=ptr, table_stride=4,
+                                    batch=1, total_rows=big, mask_words=1),
+        lambda: M.mepic_tree_accept(parent=ptr, row_offsets=ptr, draft=ptr, target=ptr, root=ptr, n_accept=ptr, accept_rows=ptr, next_token=ptr, status=ptr,
+                                    batch=1, total_rows=3, max_accept=2 ** 31),
+        lambda: M.mepic_rows_commit(CFG, k_new=ptr, v_new=ptr, row_offsets=ptr, slot_map=ptr, k_pool=ptr, v_pool=ptr, status=ptr, batch=1, max_rows=0,
+                                    n_sources=3, kv_stride=big),
+        lambda: M.mepic_attn_tree(CFG, q=ptr, k_new=ptr, v_new=ptr, row_offsets=ptr, row_pos=ptr, tree_mask=ptr, k_pool=ptr, v_pool=ptr, page_ids=ptr,
+                                  pos_base=ptr, kv_len=ptr, rope_table=ptr, out=ptr, workspace=ptr, workspace_bytes=0, status=ptr, table_stride=4,
+                                  batch=1, total_rows=0, max_rows=0, mask_words=1, sm_scale=1.0, q_stride=big),
+    ]
+    for call in calls:
+        with pytest.raises(M.MepicError, match="32 bits") as e:
+            call()
+        assert e.value.code == M.MEPIC_E_INVAL
