@@ -64,7 +64,9 @@ extern "C" {
 #define MEPIC_DEV_BAD_SLOT      0x8 /* a new row's logical slot fell outside its request */
 #define MEPIC_DEV_BAD_PLAN      0x10 /* a grouped-decode plan no longer matches kv_len (a request gained or lost a page) */
 #define MEPIC_DEV_BAD_TREE      0x20 /* a drafted row's parent does not precede it, or a request has more rows than the call was told */
-#define MEPIC_DEV_NO_PAGES      0x40 /* mepic_step_tables: the reserve, the tables or the row arrays cannot hold the step; nothing was handed out */
+#define MEPIC_DEV_NO_PAGES      0x40 /* mepic_step_tables, mepic_beam_fork: the reserve, the tables or the row arrays cannot hold the step; nothing was handed out */
+#define MEPIC_DEV_BAD_BEAM      0x80 /* a parent outside its group, or more pages returned than the reserve had handed out */
+#define MEPIC_DEV_BAD_LOGITS    0x100 /* a live beam's logits hold a NaN or +infinity, or its score is one; the beam is given up */
 
 #define MEPIC_SEG_CHUNK  0
 #define MEPIC_SEG_PROMPT 1
@@ -710,6 +712,183 @@ typedef struct {
 int32_t mepic_rows_commit(const mepic_config_t* cfg, const mepic_rows_commit_args_t* args, void* cuda_stream);
 int32_t mepic_rows_commit_fp8(const mepic_config_t* cfg, const mepic_rows_commit_args_t* args, float* k_scales, float* v_scales,
                               void* cuda_stream);
+
+/* ---------------------------------------------------------------- beams (device)
+ *
+ * The calls of a decode with beams: every request (a GROUP) is continued by up to MEPIC_BEAM_MAX_WIDTH beams that share the pages
+ * of their common past.  (The paper has no counterpart; its pages hold un-rotated keys and are reached through tables, so beams
+ * alias them as requests alias a chunk's.)  In the order of a step:
+ *   mepic_step_tables (a slot for each live beam's newest token) -> mepic_beam_plan -> (per layer) mepic_rows_commit / _fp8 and
+ *   mepic_attn_beam / _fp8 -> the model's head -> mepic_beam_select -> mepic_beam_fork -> (per layer) mepic_pages_copy / _fp8.
+ * All of it stays on the device and can be captured once and replayed.  Rows are beams: row group * width + w is beam w of a
+ * group, in the block tables, lengths, queries and logits.  Every pointer of the structs below is a DEVICE pointer; int32 arrays
+ * are packed.  Host-side errors: E_INVAL, E_CUDA.
+ */
+#define MEPIC_BEAM_MAX_WIDTH  32
+#define MEPIC_BEAM_MAX_SELECT 64
+
+/*
+ * mepic_beam_select - the best continuations over the beams and the vocabulary of each group.  With x the logits of beam w's
+ * row, a live beam (done[w] = 0, score[w] > -infinity) offers for every token v the candidate
+ *     score[w] + x[v] - log sum_u exp(x[u]) ,
+ * a finished one (done[w] != 0) the single candidate (pad_token, score[w]), a beam with score -infinity none; a token with
+ * logit -infinity is no candidate.  The n_select best of a group are written in descending order, equal ones in ascending order
+ * of (beam, token):
+ *     parent[g][k]  the beam (0 .. width-1) that is continued, token[g][k], score_out[g][k] (rounded to fp32 once),
+ *     done_out[g][k]  1 if the parent was finished or the token is eos_token, else 0,
+ *     n_new[g][k]     1 if it goes on (what mepic_step_tables takes), 0 if it is finished or there is no such candidate;
+ * where there are fewer candidates: parent = token = -1, score -infinity, done = n_new = 0.  Candidates are compared in 64 bits
+ * (sum of exponentials: terms in fp32, added up in fp32 over at most 64 terms of one thread and in 64 bits beyond).
+ * A row with a NaN or +infinity among its logits, or a score of that kind, sets MEPIC_DEV_BAD_LOGITS and offers nothing.  Rows of
+ * finished beams, and of beams with score -infinity, are not read.
+ * logits: rows of vocab elements, logits_stride elements apart (0 = packed; otherwise at least vocab), any alignment of the type.
+ * eos_token -1: no token ends a beam.  done may be NULL (none is finished).  workspace: mepic_beam_select_workspace bytes,
+ * 16-byte aligned, contents overwritten; two calls that overlap on the GPU must not share one.  Outputs must not overlap inputs.
+ */
+#define MEPIC_LOGITS_BF16 0
+#define MEPIC_LOGITS_FP16 1
+#define MEPIC_LOGITS_FP32 2
+typedef struct {
+  const void*    logits;       /* [groups*width] rows */
+  const float*   score;        /* [groups][width] */
+  const int32_t* done;         /* [groups][width] or NULL */
+  int32_t*       parent;       /* out [groups][n_select] */
+  int32_t*       token;        /* out [groups][n_select] */
+  float*         score_out;    /* out [groups][n_select] */
+  int32_t*       done_out;     /* out [groups][n_select] */
+  int32_t*       n_new;        /* out [groups][n_select] */
+  void*          workspace;
+  size_t         workspace_bytes;
+  int32_t*       status;
+  int64_t        logits_stride;
+  int32_t        logits_type;  /* MEPIC_LOGITS_* */
+  int32_t        groups, width, n_select, vocab, eos_token, pad_token;
+} mepic_beam_select_args_t;
+size_t  mepic_beam_select_workspace(int32_t groups, int32_t width, int32_t n_select, int32_t vocab);   /* 0 on error */
+int32_t mepic_beam_select(const mepic_beam_select_args_t* args, void* cuda_stream);
+
+/*
+ * mepic_beam_fork - block tables of the new beams, from their parents.  New beam k of group g continues beam parent[g][k]
+ * (-1: there is no such beam; its length is 0): it gets that row's length and its ceil(kv_len/P) table entries (page_ids_out,
+ * pos_base_out; the rest of a row is not written).  Pages:
+ *   - owned[page] != 0 marks the pages that belong to the reserve (those mepic_step_tables hands out): they may be written and
+ *     given back.  Others (a chunk's, a prompt's, any page of the store's) are neither.  An owned page is held by beams of one
+ *     group only, at the same table entry in each.
+ *   - Copy on write: a partly filled last page must be its beam's own.  The lowest new beam that holds it keeps it if it is owned and
+ *     no new beam holds it full; every other gets a page out of the reserve in its place, and the copy (copy_src, copy_dst,
+ *     copy_slots = slots of it that are filled) is listed, in order of the new rows.  *n_copies of them are listed, entries from
+ *     there on are -1.  mepic_pages_copy carries them out, layer by layer, before anything is appended.
+ *   - Owned pages that no new beam holds go back: the reserve is a stack, reserve[*reserve_used ..] are free, and in the order
+ *     (group, entry, beam) they are written to the places below *reserve_used; copies take theirs from there upwards.
+ *     *reserve_used_out = *reserve_used - pages returned + copies.  The places of handed-out pages hold nothing of meaning.
+ * width_in beams a group become width_out (1 -> n starts a search).  All or nothing: if the reserve cannot supply the copies,
+ * MEPIC_DEV_NO_PAGES is set, if it would get back more than it handed out (or *reserve_used lies outside [0, n_reserve])
+ * MEPIC_DEV_BAD_BEAM; then every new length is 0, no copy is listed and the reserve stays as it was.  A parent outside
+ * [-1, width_in) sets MEPIC_DEV_BAD_BEAM and counts as -1, a length outside [0, table_stride * P] sets MEPIC_DEV_BAD_SLOT and is
+ * clamped, a page id outside the pool sets MEPIC_DEV_BAD_PAGE and counts as not owned (it is copied, if it has to be, by a
+ * copy that mepic_pages_copy skips).
+ * The tables written must not be the tables read.  workspace: mepic_beam_fork_workspace bytes, 16-byte aligned, contents
+ * overwritten.
+ */
+typedef struct {
+  const int32_t* parent;       /* [groups][width_out] */
+  const int32_t* kv_len;       /* [groups*width_in] */
+  const int32_t* page_ids;     /* [groups*width_in][table_stride] */
+  const int32_t* pos_base;     /* [groups*width_in][table_stride] */
+  const uint8_t* owned;        /* [num_pages] */
+  int32_t*       reserve;      /* in/out [n_reserve] */
+  const int32_t* reserve_used; /* [1] */
+  int32_t*       page_ids_out; /* out [groups*width_out][table_stride] */
+  int32_t*       pos_base_out; /* out [groups*width_out][table_stride] */
+  int32_t*       kv_len_out;   /* out [groups*width_out] */
+  int32_t*       copy_src;     /* out [groups*width_out] */
+  int32_t*       copy_dst;     /* out [groups*width_out] */
+  int32_t*       copy_slots;   /* out [groups*width_out] */
+  int32_t*       n_copies;     /* out [1] */
+  int32_t*       reserve_used_out; /* out [1] */
+  void*          workspace;
+  size_t         workspace_bytes;
+  int32_t*       status;
+  int32_t        table_stride, groups, width_in, width_out, n_reserve;
+} mepic_beam_fork_args_t;
+size_t  mepic_beam_fork_workspace(int32_t groups, int32_t width_in, int32_t width_out, int32_t table_stride);   /* 0 on error */
+int32_t mepic_beam_fork(const mepic_config_t* cfg, const mepic_beam_fork_args_t* args, void* cuda_stream);
+
+/*
+ * mepic_pages_copy - for i < *n_copies: slots 0 .. slots[i]-1 (all heads, K and V) of page src[i] to page dst[i] of the pools.
+ * slots NULL: whole pages; otherwise clamped to [0, page_size].  n_copies NULL: max_copies of them.  *n_copies outside
+ * [0, max_copies] sets MEPIC_DEV_BAD_SLOT and is clamped; a page outside the pool sets MEPIC_DEV_BAD_PAGE and the copy is skipped.
+ * A page may be the source of several copies; destinations differ from one another and from every source.  Nothing else of a
+ * destination is written.  mepic_pages_copy_fp8: 8-bit pools; a copy brings the scales of its page along, for every head.
+ */
+typedef struct {
+  const int32_t* src;          /* [max_copies] */
+  const int32_t* dst;          /* [max_copies] */
+  const int32_t* slots;        /* [max_copies] or NULL */
+  const int32_t* n_copies;     /* [1] or NULL */
+  void*          k_pool;
+  void*          v_pool;
+  int32_t*       status;
+  int32_t        max_copies;
+} mepic_pages_copy_args_t;
+int32_t mepic_pages_copy(const mepic_config_t* cfg, const mepic_pages_copy_args_t* args, void* cuda_stream);
+int32_t mepic_pages_copy_fp8(const mepic_config_t* cfg, const mepic_pages_copy_args_t* args, float* k_scales, float* v_scales,
+                             void* cuda_stream);
+
+/*
+ * mepic_beam_plan - which beams of a group hold which page: once a step, for the attention of all its layers.  Beams that hold
+ * the same page id with the same pos_base and the same number of filled slots at the same table entry share it; nothing needs to
+ * be known of where they parted.  A kv_len outside [0, table_stride * page_size] sets MEPIC_DEV_BAD_SLOT and is clamped, a page id
+ * outside the pool sets MEPIC_DEV_BAD_PAGE and is replaced by 0.  plan: mepic_beam_plan_bytes bytes of device memory, 16-byte
+ * aligned, contents overwritten; it depends on the tables and lengths as they are when the call runs.
+ *
+ * mepic_attn_beam - mepic_attn_decode's formula for every row of the plan (one query, at position q_pos[row], over the row's
+ * kv_len slots), each shared page read once per group (per 32 / G beams of it, where a group has more: the 32 / G beams' G query
+ * heads are the columns of one matrix product).  A row of length 0 gets zeros.  Pages that a beam does not hold and slots at or
+ * beyond its length have no influence on its output whatever bits they hold.  bf16 tensor-core products, fp32 accumulation; the
+ * rotated q (with sm_scale folded in) and K and the softmax weights are rounded to bf16 once each.  q rows lie q_stride elements
+ * apart (0 = packed; otherwise at least a packed row and a multiple of 8).  The plan must be one of the same config, groups,
+ * width and table_stride that ran before on the GPU: another sets MEPIC_DEV_BAD_PLAN and `out` holds zeros.  The work is split over the
+ * key axis across the GPU; partials go to the workspace (mepic_attn_beam_workspace bytes, 16-byte aligned, contents overwritten)
+ * and a second kernel merges them in a fixed order.  Two calls that overlap on the GPU must not share a workspace; they may share a
+ * plan.  A captured call may be replayed with other lengths and tables, after their plan.
+ *
+ * mepic_attn_beam_fp8: over 8-bit pools (head_dim 128); the rotated q and K, the weights and V are carried in fp16 (|q| * sm_scale *
+ * log2(e) must stay below 65504), the pages' V scales beside it in fp32.
+ */
+typedef struct {
+  const int32_t* page_ids;     /* [groups*width][table_stride] */
+  const int32_t* pos_base;     /* [groups*width][table_stride] */
+  const int32_t* kv_len;       /* [groups*width] */
+  void*          plan;         /* out */
+  size_t         plan_bytes;
+  int32_t*       status;
+  int32_t        table_stride, groups, width;
+} mepic_beam_plan_args_t;
+size_t  mepic_beam_plan_bytes(const mepic_config_t* cfg, int32_t groups, int32_t width, int32_t table_stride);   /* 0 on error */
+int32_t mepic_beam_plan(const mepic_config_t* cfg, const mepic_beam_plan_args_t* args, void* cuda_stream);
+
+typedef struct {
+  const void*    q;            /* bf16 rows of [n_q_heads][head_dim], un-rotated */
+  const int32_t* q_pos;        /* [groups*width] */
+  const void*    plan;
+  const void*    k_pool;
+  const void*    v_pool;
+  const float*   rope_table;
+  void*          out;          /* bf16 [groups*width][n_q_heads][head_dim], packed */
+  void*          workspace;
+  size_t         workspace_bytes;
+  int32_t*       status;
+  int32_t        table_stride, groups, width;
+  int32_t        q_stride;
+  float          sm_scale;
+} mepic_attn_beam_args_t;
+
+/* Bytes of workspace on the CURRENT device; 0 on error. */
+size_t  mepic_attn_beam_workspace(const mepic_config_t* cfg, int32_t groups, int32_t width);
+int32_t mepic_attn_beam(const mepic_config_t* cfg, const mepic_attn_beam_args_t* args, void* cuda_stream);
+int32_t mepic_attn_beam_fp8(const mepic_config_t* cfg, const mepic_attn_beam_args_t* args, const float* k_scales,
+                            const float* v_scales, void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -28,6 +28,9 @@ __all__ = [
     "mepic_attn_decode_grouped", "mepic_attn_decode_grouped_fp8",
     "mepic_tree_layout", "mepic_attn_tree_workspace", "mepic_attn_tree", "mepic_attn_tree_fp8", "mepic_tree_accept", "mepic_step_tables",
     "mepic_rows_commit", "mepic_rows_commit_fp8", "MEPIC_TREE_MAX_ROWS", "MEPIC_STEP_MAX_BATCH",
+    "mepic_beam_select_workspace", "mepic_beam_select", "mepic_beam_fork_workspace", "mepic_beam_fork", "mepic_pages_copy", "mepic_pages_copy_fp8",
+    "mepic_beam_plan_bytes", "mepic_beam_plan", "mepic_attn_beam_workspace", "mepic_attn_beam", "mepic_attn_beam_fp8",
+    "MEPIC_BEAM_MAX_WIDTH", "MEPIC_BEAM_MAX_SELECT", "MEPIC_LOGITS_BF16", "MEPIC_LOGITS_FP16", "MEPIC_LOGITS_FP32",
     "MEPIC_DECODE_STATIC_SCRATCH_BYTES", "mepic_attn_prefill_workspace",
     "mepic_attn_prefill", "mepic_attn_prefill_fp8", "mepic_last_error", "mepic_launch_count",
     "MEPIC_OK", "MEPIC_E_INVAL", "MEPIC_E_NOSPACE", "MEPIC_E_NOTFOUND", "MEPIC_E_CAPACITY",
@@ -51,8 +54,15 @@ MEPIC_DEV_BAD_SLOT = 0x8
 MEPIC_DEV_BAD_PLAN = 0x10
 MEPIC_DEV_BAD_TREE = 0x20
 MEPIC_DEV_NO_PAGES = 0x40
+MEPIC_DEV_BAD_BEAM = 0x80
+MEPIC_DEV_BAD_LOGITS = 0x100
 MEPIC_TREE_MAX_ROWS = 1024
 MEPIC_STEP_MAX_BATCH = 8192
+MEPIC_BEAM_MAX_WIDTH = 32
+MEPIC_BEAM_MAX_SELECT = 64
+MEPIC_LOGITS_BF16 = 0
+MEPIC_LOGITS_FP16 = 1
+MEPIC_LOGITS_FP32 = 2
 
 
 class MepicError(RuntimeError):
@@ -142,6 +152,35 @@ class _RowsCommitArgsC(_StepArgs):
                [(n, C.c_int32) for n in ("src_stride", "batch", "max_rows", "n_sources", "kv_stride")]
 
 
+class _BeamSelectArgsC(_StepArgs):
+    _fields_ = [(n, C.c_void_p) for n in ("logits", "score", "done", "parent", "token", "score_out", "done_out", "n_new", "workspace")] + \
+               [("workspace_bytes", C.c_size_t), ("status", C.c_void_p), ("logits_stride", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("logits_type", "groups", "width", "n_select", "vocab", "eos_token", "pad_token")]
+
+
+class _BeamForkArgsC(_StepArgs):
+    _fields_ = [(n, C.c_void_p) for n in ("parent", "kv_len", "page_ids", "pos_base", "owned", "reserve", "reserve_used", "page_ids_out",
+                                          "pos_base_out", "kv_len_out", "copy_src", "copy_dst", "copy_slots", "n_copies", "reserve_used_out",
+                                          "workspace")] + \
+               [("workspace_bytes", C.c_size_t), ("status", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("table_stride", "groups", "width_in", "width_out", "n_reserve")]
+
+
+class _PagesCopyArgsC(_StepArgs):
+    _fields_ = [(n, C.c_void_p) for n in ("src", "dst", "slots", "n_copies", "k_pool", "v_pool", "status")] + [("max_copies", C.c_int32)]
+
+
+class _BeamPlanArgsC(_StepArgs):
+    _fields_ = [(n, C.c_void_p) for n in ("page_ids", "pos_base", "kv_len", "plan")] + \
+               [("plan_bytes", C.c_size_t), ("status", C.c_void_p)] + [(n, C.c_int32) for n in ("table_stride", "groups", "width")]
+
+
+class _AttnBeamArgsC(_StepArgs):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "q_pos", "plan", "k_pool", "v_pool", "rope_table", "out", "workspace")] + \
+               [("workspace_bytes", C.c_size_t), ("status", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("table_stride", "groups", "width", "q_stride")] + [("sm_scale", C.c_float)]
+
+
 @dataclass(frozen=True)
 class Config:
     page_size: int
@@ -211,6 +250,17 @@ _PROTOTYPES = {
     "mepic_step_tables": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_StepTablesArgsC), C.c_void_p]),
     "mepic_rows_commit": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_RowsCommitArgsC), C.c_void_p]),
     "mepic_rows_commit_fp8": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_RowsCommitArgsC), C.c_void_p, C.c_void_p, C.c_void_p]),
+    "mepic_beam_select_workspace": (C.c_size_t, [C.c_int32] * 4),
+    "mepic_beam_select": (C.c_int32, [C.POINTER(_BeamSelectArgsC), C.c_void_p]),
+    "mepic_beam_fork_workspace": (C.c_size_t, [C.c_int32] * 4),
+    "mepic_beam_fork": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_BeamForkArgsC), C.c_void_p]),
+    "mepic_pages_copy": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_PagesCopyArgsC), C.c_void_p]),
+    "mepic_pages_copy_fp8": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_PagesCopyArgsC), C.c_void_p, C.c_void_p, C.c_void_p]),
+    "mepic_beam_plan_bytes": (C.c_size_t, [C.POINTER(_ConfigC), C.c_int32, C.c_int32, C.c_int32]),
+    "mepic_beam_plan": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_BeamPlanArgsC), C.c_void_p]),
+    "mepic_attn_beam_workspace": (C.c_size_t, [C.POINTER(_ConfigC), C.c_int32, C.c_int32]),
+    "mepic_attn_beam": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_AttnBeamArgsC), C.c_void_p]),
+    "mepic_attn_beam_fp8": (C.c_int32, [C.POINTER(_ConfigC), C.POINTER(_AttnBeamArgsC), C.c_void_p, C.c_void_p, C.c_void_p]),
 }
 
 
@@ -637,3 +687,97 @@ def mepic_rows_commit_fp8(cfg: Config, *, k_new, v_new, row_offsets, slot_map, k
                          _ptr(status), src_stride, batch, max_rows, n_sources, kv_stride)
     c = cfg.c()
     _check(lib().mepic_rows_commit_fp8(C.byref(c), C.byref(a), _ptr(k_scales), _ptr(v_scales), _stream_ptr(stream)))
+
+
+# ------------------------------------------------------------------ beams (device)
+def _counted(n: int) -> int:
+    if n == 0:
+        raise MepicError(MEPIC_E_INVAL, mepic_last_error())
+    return n
+
+
+def _int32s(**values: int) -> None:
+    for name, v in values.items():
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise MepicError(MEPIC_E_INVAL, f"{name} = {v} does not fit in 32 bits")
+
+
+def mepic_beam_select_workspace(groups: int, width: int, n_select: int, vocab: int) -> int:
+    _int32s(groups=groups, width=width, n_select=n_select, vocab=vocab)
+    return _counted(int(lib().mepic_beam_select_workspace(groups, width, n_select, vocab)))
+
+
+def mepic_beam_select(*, logits, score, parent, token, score_out, done_out, n_new, workspace, workspace_bytes: int, status, logits_type: int,
+                      groups: int, width: int, n_select: int, vocab: int, eos_token: int, pad_token: int, done=None, logits_stride: int = 0,
+                      stream=None) -> None:
+    a = _BeamSelectArgsC(_ptr(logits), _ptr(score), _ptr(done), _ptr(parent), _ptr(token), _ptr(score_out), _ptr(done_out), _ptr(n_new),
+                         _ptr(workspace), workspace_bytes, _ptr(status), logits_stride, logits_type, groups, width, n_select, vocab,
+                         eos_token, pad_token)
+    _check(lib().mepic_beam_select(C.byref(a), _stream_ptr(stream)))
+
+
+def mepic_beam_fork_workspace(groups: int, width_in: int, width_out: int, table_stride: int) -> int:
+    _int32s(groups=groups, width_in=width_in, width_out=width_out, table_stride=table_stride)
+    return _counted(int(lib().mepic_beam_fork_workspace(groups, width_in, width_out, table_stride)))
+
+
+def mepic_beam_fork(cfg: Config, *, parent, kv_len, page_ids, pos_base, owned, reserve, reserve_used, page_ids_out, pos_base_out, kv_len_out,
+                    copy_src, copy_dst, copy_slots, n_copies, reserve_used_out, workspace, workspace_bytes: int, status, table_stride: int,
+                    groups: int, width_in: int, width_out: int, n_reserve: int, stream=None) -> None:
+    a = _BeamForkArgsC(_ptr(parent), _ptr(kv_len), _ptr(page_ids), _ptr(pos_base), _ptr(owned), _ptr(reserve), _ptr(reserve_used),
+                       _ptr(page_ids_out), _ptr(pos_base_out), _ptr(kv_len_out), _ptr(copy_src), _ptr(copy_dst), _ptr(copy_slots),
+                       _ptr(n_copies), _ptr(reserve_used_out), _ptr(workspace), workspace_bytes, _ptr(status), table_stride, groups,
+                       width_in, width_out, n_reserve)
+    c = cfg.c()
+    _check(lib().mepic_beam_fork(C.byref(c), C.byref(a), _stream_ptr(stream)))
+
+
+def mepic_pages_copy(cfg: Config, *, src, dst, k_pool, v_pool, status, max_copies: int, slots=None, n_copies=None, stream=None) -> None:
+    a = _PagesCopyArgsC(_ptr(src), _ptr(dst), _ptr(slots), _ptr(n_copies), _ptr(k_pool), _ptr(v_pool), _ptr(status), max_copies)
+    c = cfg.c()
+    _check(lib().mepic_pages_copy(C.byref(c), C.byref(a), _stream_ptr(stream)))
+
+
+def mepic_pages_copy_fp8(cfg: Config, *, src, dst, k_pool, v_pool, k_scales, v_scales, status, max_copies: int, slots=None, n_copies=None,
+                         stream=None) -> None:
+    """mepic_pages_copy in 8-bit pools: k_pool / v_pool are e4m3 codes, k_scales / v_scales their scales (written too)."""
+    a = _PagesCopyArgsC(_ptr(src), _ptr(dst), _ptr(slots), _ptr(n_copies), _ptr(k_pool), _ptr(v_pool), _ptr(status), max_copies)
+    c = cfg.c()
+    _check(lib().mepic_pages_copy_fp8(C.byref(c), C.byref(a), _ptr(k_scales), _ptr(v_scales), _stream_ptr(stream)))
+
+
+def mepic_beam_plan_bytes(cfg: Config, groups: int, width: int, table_stride: int) -> int:
+    _int32s(groups=groups, width=width, table_stride=table_stride)
+    c = cfg.c()
+    return _counted(int(lib().mepic_beam_plan_bytes(C.byref(c), groups, width, table_stride)))
+
+
+def mepic_beam_plan(cfg: Config, *, page_ids, pos_base, kv_len, plan, plan_bytes: int, status, table_stride: int, groups: int, width: int,
+                    stream=None) -> None:
+    a = _BeamPlanArgsC(_ptr(page_ids), _ptr(pos_base), _ptr(kv_len), _ptr(plan), plan_bytes, _ptr(status), table_stride, groups, width)
+    c = cfg.c()
+    _check(lib().mepic_beam_plan(C.byref(c), C.byref(a), _stream_ptr(stream)))
+
+
+def mepic_attn_beam_workspace(cfg: Config, groups: int, width: int) -> int:
+    _int32s(groups=groups, width=width)
+    c = cfg.c()
+    return _counted(int(lib().mepic_attn_beam_workspace(C.byref(c), groups, width)))
+
+
+def mepic_attn_beam(cfg: Config, *, q, q_pos, plan, k_pool, v_pool, rope_table, out, workspace, workspace_bytes: int, status,
+                    table_stride: int, groups: int, width: int, sm_scale: float, q_stride: int = 0, stream=None) -> None:
+    a = _AttnBeamArgsC(_ptr(q), _ptr(q_pos), _ptr(plan), _ptr(k_pool), _ptr(v_pool), _ptr(rope_table), _ptr(out), _ptr(workspace),
+                       workspace_bytes, _ptr(status), table_stride, groups, width, q_stride, sm_scale)
+    c = cfg.c()
+    _check(lib().mepic_attn_beam(C.byref(c), C.byref(a), _stream_ptr(stream)))
+
+
+def mepic_attn_beam_fp8(cfg: Config, *, q, q_pos, plan, k_pool, v_pool, k_scales, v_scales, rope_table, out, workspace,
+                        workspace_bytes: int, status, table_stride: int, groups: int, width: int, sm_scale: float, q_stride: int = 0,
+                        stream=None) -> None:
+    """mepic_attn_beam over 8-bit pools: k_pool / v_pool are e4m3 codes, k_scales / v_scales their scales."""
+    a = _AttnBeamArgsC(_ptr(q), _ptr(q_pos), _ptr(plan), _ptr(k_pool), _ptr(v_pool), _ptr(rope_table), _ptr(out), _ptr(workspace),
+                       workspace_bytes, _ptr(status), table_stride, groups, width, q_stride, sm_scale)
+    c = cfg.c()
+    _check(lib().mepic_attn_beam_fp8(C.byref(c), C.byref(a), _ptr(k_scales), _ptr(v_scales), _stream_ptr(stream)))

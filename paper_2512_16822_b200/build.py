@@ -18,7 +18,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libmepic.so")
 
 SOURCES = ["mepic_store.cpp", "mepic_tensor_map.cu", "mepic_decode.cu", "mepic_decode_fp8.cu", "mepic_decode_grouped.cu", "mepic_plan.cpp",
-           "mepic_prefill.cu", "mepic_step.cu", "mepic_tree.cu"]
+           "mepic_prefill.cu", "mepic_step.cu", "mepic_tree.cu", "mepic_beam.cu", "mepic_attn_beam.cu"]
 
 
 def _nvcc() -> str:

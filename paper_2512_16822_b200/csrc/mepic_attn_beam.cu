@@ -1,0 +1,860 @@
+// Attention of the newest token of every beam over the paged, un-rotated context, each page that beams of a request share read
+// once (see mepic_beam_plan and mepic_attn_beam in mepic.h).
+//
+// Bound: HBM.  A request's W beams of G query heads are up to 32 columns of one matrix product per kv head, so a page's K and V
+// serve W G query vectors for one read.  As in the per-request decode the keys are the M rows of both products
+// (S^T = K' Q^T, O^T = V^T P^T on mma.sync m16n8k16) and the columns are the N side: 8 columns a tile of the instruction, up to
+// four such tiles (NT).  The (column block, kv head, 16-key tile) triples of the batch form one line, cut into equal pieces, one
+// per warp of a persistent grid, each with a ring of TMA stages of its own; pieces that end inside a column block leave partials
+// (reference, sum, unnormalised output) that a second kernel joins in a fixed order.
+//
+// Rotation.  <R(qpos) q, R(pos) k> = <R(qpos - a) q, R(pos - a) k> for any anchor a.  A warp keeps its queries rotated for an anchor
+// and turns each key by pos - a, 0 <= pos - a < 64, from a table of 64 positions in shared memory; the anchor moves, and the
+// queries are rotated anew from what the caller gave, once in 64 consecutive positions.  So the keys are rotated once for all
+// columns, and the work that grows with the columns (rotating queries) is done for every fourth tile only.
+//
+// Who sees what.  A record of the plan is one page of one column block: page, position, the beams that hold it, its filled slots.
+// Where every beam of the block holds it, nothing is masked.  Where only some do, the other columns' scores are -infinity and
+// their outputs are left as they are (not "plus 0 x V": V may hold anything that is not finite).
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <float.h>
+#include <limits.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "mepic.h"
+#include "mepic_internal.h"
+#include "mepic_ptx.cuh"
+#include "mepic_tcgen05.cuh"      // arithmetic on pairs of floats
+
+namespace {
+
+using namespace mepic_dev;
+
+constexpr int kTile = 16;            // keys per staged tile
+constexpr int kStages = 2;
+constexpr int kMinPiece = 4;         // the line is never cut into pieces shorter than this many tiles
+constexpr int kAngles = 64;          // positions of the shared-memory table
+constexpr int kMaxColumns = 32;      // columns of a column block
+constexpr int kSeg = 256;            // table entries a CTA of the plan looks at
+
+// ---------------------------------------------------------------- the plan's layout
+// ints: [0, kHead) header, then the running sums of records per (column block, segment), then the rows' lengths, then (16-byte
+// aligned) the records {page, pos_base, beams, filled slots}, kSeg * beams of a block for each (column block, segment).
+constexpr int kHead = 16;
+constexpr int kPlanMagic = 0x4d424d31;
+enum { kHMagic, kHGroups, kHWidth, kHStride, kHPage, kHGroupSize, kHKvHeads, kHBeams, kHSegments, kHPages };
+
+struct PlanShape {
+  int groups, width, blocks, beams, segments;      // column blocks of a group, beams of a block, segments of a row
+  size_t off_len, off_rec, bytes;                  // in ints, in ints, in bytes
+};
+// A group's beams are dealt evenly to as few column blocks of at most 32 columns as hold them.
+bool plan_shape(const mepic_config_t* cfg, int groups, int width, int stride, const char* what, PlanShape* s) {
+  if (groups < 1 || width < 1 || width > MEPIC_BEAM_MAX_WIDTH) { mepic_set_error("%s: groups must be positive, width in 1..%d", what, MEPIC_BEAM_MAX_WIDTH); return false; }
+  if (stride < 1 || static_cast<long long>(groups) * width * stride > 0x40000000LL || static_cast<long long>(groups) * width > 0xffffLL * 16) {
+    mepic_set_error("%s: table_stride must be positive and the tables below 2^30 entries", what); return false;
+  }
+  const int most = kMaxColumns / (cfg->n_q_heads / cfg->n_kv_heads);
+  s->groups = groups; s->width = width;
+  s->blocks = (width + most - 1) / most;
+  s->beams = (width + s->blocks - 1) / s->blocks;
+  s->segments = (stride + kSeg - 1) / kSeg;
+  const size_t n = static_cast<size_t>(groups) * s->blocks * s->segments;
+  if (n * kSeg * s->beams > 0x7fffffffULL) { mepic_set_error("%s: the plan would have more than 2^31 records", what); return false; }
+  s->off_len = kHead + n + 1;
+  s->off_rec = (s->off_len + static_cast<size_t>(groups) * width + 3) & ~static_cast<size_t>(3);
+  s->bytes = s->off_rec * 4 + n * kSeg * s->beams * 16;
+  return true;
+}
+
+struct PlanParams {
+  const int32_t* page_ids;
+  const int32_t* pos_base;
+  const int32_t* kv_len;
+  int32_t* sums;         // running sums; the first launch leaves the counts here
+  int32_t* lens;
+  int4* records;
+  int32_t* head;
+  int32_t* status;
+  int stride, groups, width, blocks, beams, segments, page_shift, num_pages, group_size, n_kv_heads;
+};
+
+// ---------------------------------------------------------------- plan
+// A CTA per (column block, segment of 256 table entries), a thread per entry: the block's beams fall into classes that hold the
+// same page at the same position with the same number of slots.  Counted, summed up over the CTA, written.
+__global__ void __launch_bounds__(kSeg) mepic_beam_plan_classes(const __grid_constant__ PlanParams p) {
+  __shared__ int len[MEPIC_BEAM_MAX_WIDTH];
+  __shared__ int warp_n[kSeg / 32];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int block = blockIdx.x, seg = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int group = block / p.blocks, first = (block - group * p.blocks) * p.beams, nb = min(p.beams, p.width - first);
+  const int P = 1 << p.page_shift;
+  const size_t row0 = static_cast<size_t>(group) * p.width + first;
+  if (tid < nb) {
+    const long long room = min(static_cast<long long>(p.stride) << p.page_shift, 0x7fffffffll);
+    int n = __ldg(p.kv_len + row0 + tid);
+    if (n < 0 || n > room) { if (seg == 0) atomicOr(p.status, MEPIC_DEV_BAD_SLOT); n = n < 0 ? 0 : static_cast<int>(room); }
+    len[tid] = n;
+    if (seg == 0) p.lens[row0 + tid] = n;
+  }
+  __syncthreads();
+  const int e = seg * kSeg + tid;
+  const long long from = static_cast<long long>(e) << p.page_shift;
+  unsigned held = 0;
+  if (e < p.stride)
+    for (int i = 0; i < nb; ++i) if (len[i] > from) held |= 1u << i;
+  const int32_t* ids = p.page_ids + row0 * p.stride + e;
+  const int32_t* base = p.pos_base + row0 * p.stride + e;
+  auto fill = [&](int i) { return static_cast<int>(min(static_cast<long long>(P), len[i] - from)); };
+  auto each_class = [&](auto use) {
+    for (unsigned left = held; left;) {
+      const int i = __ffs(left) - 1;
+      const int page = __ldg(ids + static_cast<size_t>(i) * p.stride), pos = __ldg(base + static_cast<size_t>(i) * p.stride), n = fill(i);
+      unsigned same = 0;
+      for (unsigned m = left; m; m &= m - 1) {
+        const int j = __ffs(m) - 1;
+        if (__ldg(ids + static_cast<size_t>(j) * p.stride) == page && __ldg(base + static_cast<size_t>(j) * p.stride) == pos && fill(j) == n) same |= 1u << j;
+      }
+      left &= ~same;
+      use(page, pos, same, n);
+    }
+  };
+  int n = 0;
+  each_class([&](int, int, unsigned, int) { ++n; });
+  int incl = n;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) { const int y = __shfl_up_sync(kFull, incl, d); if (lane >= d) incl += y; }
+  if (lane == 31) warp_n[warp] = incl;
+  __syncthreads();
+  int at = incl - n, total = 0;
+  for (int w = 0; w < kSeg / 32; ++w) {
+    if (w < warp) at += warp_n[w];
+    total += warp_n[w];
+  }
+  const size_t part = static_cast<size_t>(block) * p.segments + seg;
+  if (tid == 0) p.sums[part] = total;
+  int4* out = p.records + part * kSeg * p.beams;
+  each_class([&](int page, int pos, unsigned same, int slots) {
+    if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) { atomicOr(p.status, MEPIC_DEV_BAD_PAGE); page = 0; }
+    out[at++] = make_int4(page, pos, static_cast<int>(same), slots);
+  });
+}
+
+// One CTA: counts -> running sums, and the header.
+constexpr int kScanThreads = 1024;
+__global__ void __launch_bounds__(kScanThreads) mepic_beam_plan_sums(const __grid_constant__ PlanParams p) {
+  __shared__ int warp_n[kScanThreads / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int n = p.groups * p.blocks * p.segments;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  int before = 0;
+  for (int i0 = 0; i0 < n; i0 += kScanThreads) {
+    const int c = i0 + tid < n ? p.sums[i0 + tid] : 0;
+    int incl = c;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) { const int y = __shfl_up_sync(kFull, incl, d); if (lane >= d) incl += y; }
+    if (lane == 31) warp_n[warp] = incl;
+    __syncthreads();
+    int w = warp_n[lane];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) { const int y = __shfl_up_sync(kFull, w, d); if (lane >= d) w += y; }
+    const int mine = __shfl_sync(kFull, w, max(warp - 1, 0)), all = __shfl_sync(kFull, w, 31);
+    if (i0 + tid < n) p.sums[i0 + tid] = before + (warp ? mine : 0) + incl - c;
+    before += all;
+    __syncthreads();
+  }
+  if (tid == 0) {
+    p.sums[n] = before;
+    p.head[kHMagic] = kPlanMagic; p.head[kHGroups] = p.groups; p.head[kHWidth] = p.width; p.head[kHStride] = p.stride;
+    p.head[kHPage] = 1 << p.page_shift; p.head[kHGroupSize] = p.group_size; p.head[kHKvHeads] = p.n_kv_heads;
+    p.head[kHBeams] = p.beams; p.head[kHSegments] = p.segments; p.head[kHPages] = p.num_pages;
+  }
+}
+
+// ---------------------------------------------------------------- attention
+struct BeamParams {
+  const uint16_t* q;
+  const int32_t* q_pos;
+  const int32_t* head;
+  const int32_t* sums;
+  const int32_t* lens;
+  const int4* records;
+  const float* rope;
+  const float* k_scales;   // 8-bit pools only: [num_pages][n_kv_heads]
+  const float* v_scales;
+  float* part_o;           // [slots][columns][D]
+  float2* part_ml;         // [slots][columns] (reference in log2 units, sum)
+  uint16_t* out;
+  int32_t* status;
+  int groups, width, stride, blocks, beams, segments, group_size, columns;
+  int n_kv_heads, page_size, log2_tpp, num_pages, max_position, q_stride, workers;
+  int spin_limit, skip_tile;
+  float scale_log2;
+};
+
+// The plan is one of this call's shape, and its sums are ones that its shape allows.
+__device__ __forceinline__ bool plan_fits(const BeamParams& p) {
+  const int32_t* h = p.head;
+  const long long n = static_cast<long long>(p.groups) * p.blocks * p.segments, total = __ldg(p.sums + n);
+  return __ldg(h + kHMagic) == kPlanMagic && __ldg(h + kHGroups) == p.groups && __ldg(h + kHWidth) == p.width && __ldg(h + kHStride) == p.stride &&
+         __ldg(h + kHPage) == p.page_size && __ldg(h + kHGroupSize) == p.group_size && __ldg(h + kHKvHeads) == p.n_kv_heads &&
+         __ldg(h + kHBeams) == p.beams && __ldg(h + kHSegments) == p.segments && __ldg(h + kHPages) == p.num_pages &&
+         total >= 0 && total <= n * kSeg * p.beams;
+}
+struct Cut { long long total, piece; };
+__device__ __forceinline__ Cut cut_of_line(const BeamParams& p) {
+  Cut c;
+  c.total = (static_cast<long long>(__ldg(p.sums + static_cast<size_t>(p.groups) * p.blocks * p.segments)) << p.log2_tpp) * p.n_kv_heads;
+  c.piece = max((c.total + p.workers - 1) / p.workers, static_cast<long long>(kMinPiece));
+  return c;
+}
+// A unit of the line: a column block under one kv head, records r0 .. r1-1 of the plan.
+struct Unit { int block, head, r0, r1; };
+__device__ __forceinline__ void bounds_of(const BeamParams& p, Unit& u) {
+  u.r0 = __ldg(p.sums + static_cast<size_t>(u.block) * p.segments);
+  u.r1 = __ldg(p.sums + static_cast<size_t>(u.block + 1) * p.segments);
+}
+__device__ __forceinline__ void next_unit(const BeamParams& p, Unit& u) {
+  if (++u.head < p.n_kv_heads) return;
+  u.head = 0;
+  do {
+    if (++u.block >= p.groups * p.blocks) { u.r0 = u.r1 = 0; return; }
+    bounds_of(p, u);
+  } while (u.r0 >= u.r1);
+}
+// The column block that place x of the line falls into, 32 candidates at a time (by a whole warp).
+__device__ __forceinline__ Unit unit_at(const BeamParams& p, long long x, int lane) {
+  int lo = 0, n = p.groups * p.blocks;                  // in [lo, lo + n): the last block whose begin is <= x
+  while (n > 1) {
+    const int step = (n + 31) / 32, at = lo + lane * step;
+    const bool below = lane * step < n && (static_cast<long long>(__ldg(p.sums + static_cast<size_t>(min(at, p.groups * p.blocks)) * p.segments)) << p.log2_tpp) * p.n_kv_heads <= x;
+    const int k = 31 - __clz(__ballot_sync(kFull, below) | 1u);
+    n = min(step, lo + n - (lo + k * step));
+    lo += k * step;
+  }
+  Unit u{lo, 0, 0, 0};
+  bounds_of(p, u);
+  return u;
+}
+
+template <int D, bool FP8> constexpr int stage_bytes = 2 * kTile * D * (FP8 ? 1 : 2);
+// per position of the table: 64 (cos, sin) pairs, fp32 (c0, c1, s0, s1 of two pairs) or fp16 (the same four)
+template <int D, bool FP8> constexpr int angle_bytes = D / 2 * (FP8 ? 4 : 8);
+template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (kStages * stage_bytes<D, FP8> + 128) + kAngles * angle_bytes<D, FP8> + 1024;
+
+// NT: tiles of 8 columns; W: warps of a CTA.
+template <int D, int NT, bool FP8, int W>
+__global__ void __launch_bounds__(W * 32, 1)
+mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  constexpr int NB = D / 64;                 // 64-dim blocks (128-byte swizzled rows) per K or V row
+  constexpr int KS = D / 16, KH = KS / 2;    // k-steps of the QK^T product; step j pairs with step j + KH
+  constexpr int NV = D / 16;                 // 16-dim blocks of the output
+  constexpr int KB = FP8 ? 1 : NB;
+  constexpr int kBlockBytes = kTile * 128;
+  constexpr int kStageBytes = stage_bytes<D, FP8>;
+  constexpr int kAngleBytes = angle_bytes<D, FP8>;
+
+  extern __shared__ unsigned char smem_dyn[];
+  // 1024-byte alignment: the swizzle pattern is a function of the address bits
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~static_cast<uintptr_t>(1023));
+  const int lane = threadIdx.x & 31, wic = threadIdx.x >> 5;
+  unsigned char* stage0 = smem + static_cast<size_t>(wic) * kStages * kStageBytes;
+  unsigned char* angles = smem + static_cast<size_t>(W) * kStages * kStageBytes;
+  unsigned char* misc = angles + kAngles * kAngleBytes + wic * 128;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(misc);                          // kStages x 8 bytes
+  volatile int* meta = reinterpret_cast<volatile int*>(misc + 16);             // per stage: position, beams, valid slots of the tile
+  volatile float* scl = reinterpret_cast<volatile float*>(misc + 16 + kStages * 16);      // per stage: K and V scale of the page
+
+  const int g = lane >> 2, t = lane & 3;     // fragment row (key, dim, or column of Q) and column group
+  // 8-bit pages: ldmatrix on bytes hands a lane four consecutive dims of a key, its transposing form four consecutive keys of a
+  // dim; which dim or key stands at which place of the contraction is free as long as both operands agree.
+  auto pair_of = [&](int j, int r) { return FP8 ? 16 * j + 4 * t + 2 * r : 16 * j + 2 * t + 8 * r; };
+  const int keyA = FP8 ? 4 * (g >> 1) + (g & 1) : g, keyB = FP8 ? keyA + 2 : g + 8;      // keys of the lane's two rows
+
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the merge kernel may move in as CTAs of this one retire
+  if (!plan_fits(p)) return;                                         // (reported by the merge kernel)
+  const Cut cut = cut_of_line(p);
+  if (static_cast<long long>(blockIdx.x) * W * cut.piece >= cut.total) return;
+
+  // ---- the table of angles: for position a and pairs 2u, 2u+1 the quadruple (c, c', s, s'), rows swizzled so that the eight lanes
+  // that load together (two keys, four column groups) meet all banks
+  for (int i = threadIdx.x; i < kAngles * (D / 4); i += W * 32) {
+    const int a = i / (D / 4), u = i % (D / 4);
+    const float4 cs = __ldg(reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(min(a, p.max_position)) * D + 4 * u));      // c, s, c', s'
+    if constexpr (FP8) {
+      // a key's row and the next key's row meet in the same 8-lane phase: 32 bytes a lane pair of quadruples
+      unsigned char* at = angles + a * kAngleBytes + ((u * 8) ^ ((a & 1) << 6));
+      *reinterpret_cast<uint2*>(at) = make_uint2(pack_f16x2(cs.x, cs.z), pack_f16x2(cs.y, cs.w));
+    } else {
+      unsigned char* at = angles + a * kAngleBytes + ((u * 16) ^ ((a & 1) << 6));
+      *reinterpret_cast<float4*>(at) = make_float4(cs.x, cs.z, cs.y, cs.w);
+    }
+  }
+  if (lane == 0) {
+#pragma unroll
+    for (int s = 0; s < kStages; ++s) mbar_init(smem_u32(&bars[s]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncthreads();
+
+  const long long w = static_cast<long long>(blockIdx.x) * W + wic;
+  const long long x0 = w * cut.piece;
+  if (x0 >= cut.total) return;
+  const long long x1 = min(x0 + cut.piece, cut.total);
+  const int G = p.group_size, tpp_mask = (1 << p.log2_tpp) - 1;
+
+  // ---- producer: the next tile to stage
+  Unit pu = unit_at(p, x0, lane);
+  int pr, pt;
+  {
+    const long long in = x0 - (static_cast<long long>(pu.r0) << p.log2_tpp) * p.n_kv_heads, per = static_cast<long long>(pu.r1 - pu.r0) << p.log2_tpp;
+    pu.head = static_cast<int>(in / per);
+    const long long in_head = in - pu.head * per;
+    pr = pu.r0 + static_cast<int>(in_head >> p.log2_tpp);
+    pt = static_cast<int>(in_head) & tpp_mask;
+  }
+  Unit cu = pu;                                                        // consumer: its unit, and the unit's tiles still to come
+  long long c_left = (static_cast<long long>(cu.r1 - pr) << p.log2_tpp) - pt;
+  int pseg = pu.block * p.segments;                                    // segment of the producer's record
+  int win0 = 0, win_n = 0;                                             // records win0 .. win0 + win_n - 1, one per lane
+  int4 win = make_int4(0, 0, 0, 0);
+  float win_ks = 0.f, win_vs = 0.f;
+  long long issued = x0;
+  auto issue = [&](int stage) {
+    if (pr < win0 || pr >= win0 + win_n) {
+      while (pseg + 1 < p.groups * p.blocks * p.segments && __ldg(p.sums + pseg + 1) <= pr) ++pseg;
+      const int s0 = __ldg(p.sums + pseg);
+      const int at = pr - s0 + lane;
+      win0 = pr;
+      win_n = min(32, __ldg(p.sums + pseg + 1) - pr);
+      const bool in = lane < win_n && at >= 0 && at < kSeg * p.beams;
+      win = in ? __ldg(p.records + static_cast<size_t>(pseg) * kSeg * p.beams + at) : make_int4(0, 0, 0, 0);
+      if (static_cast<unsigned>(win.x) >= static_cast<unsigned>(p.num_pages)) win.x = 0;
+      if constexpr (FP8) {
+        win_ks = __ldg(p.k_scales + static_cast<size_t>(win.x) * p.n_kv_heads + pu.head);
+        win_vs = __ldg(p.v_scales + static_cast<size_t>(win.x) * p.n_kv_heads + pu.head);
+      }
+    }
+    const int src = pr - win0;
+    const int page = __shfl_sync(kFull, win.x, src), pos = __shfl_sync(kFull, win.y, src), beams = __shfl_sync(kFull, win.z, src), slots = __shfl_sync(kFull, win.w, src);
+    float ks = 0.f, vs = 0.f;
+    if constexpr (FP8) { ks = __shfl_sync(kFull, win_ks, src); vs = __shfl_sync(kFull, win_vs, src); }
+    const int n_valid = min(slots - pt * kTile, kTile);
+    if (lane == 0) {
+      meta[stage * 4] = pos + pt * kTile; meta[stage * 4 + 1] = beams; meta[stage * 4 + 2] = n_valid;
+      if constexpr (FP8) { scl[stage * 2] = ks; scl[stage * 2 + 1] = vs; }
+      if (!(w == 0 && issued - x0 == p.skip_tile)) {        // (test hook: one copy that never comes)
+        const uint32_t bar = smem_u32(&bars[stage]), dst = smem_u32(stage0 + stage * kStageBytes);
+        if (n_valid <= 0) {
+          mbar_expect_tx(bar, 0);                           // a tile of the page that holds no slot
+        } else {
+          const int y = (page * p.n_kv_heads + pu.head) * p.page_size + pt * kTile;      // row of the pool viewed as [rows][D]
+          mbar_expect_tx(bar, kStageBytes);
+#pragma unroll
+          for (int nb = 0; nb < KB; ++nb) {
+            tma_load_2d(dst + nb * kBlockBytes, &map_k, nb * 64, y, bar);
+            tma_load_2d(dst + (KB + nb) * kBlockBytes, &map_v, nb * 64, y, bar);
+          }
+        }
+      }
+    }
+    ++issued;
+    if (pt < tpp_mask) { ++pt; return; }
+    pt = 0;
+    if (++pr < pu.r1) return;
+    next_unit(p, pu);
+    pr = pu.r0;
+    pseg = min(pu.block, p.groups * p.blocks - 1) * p.segments;
+    win_n = 0;                                              // another head: its scales, another block: its records
+  };
+  for (int s = 0; s < kStages && issued < x1; ++s) issue(s);
+  __syncwarp();
+
+  // ---- state of the unit
+  int u_block = -1, u_head = -1;
+  unsigned all_beams = 0;
+  int anchor = INT_MIN;
+  unsigned see[NT][2];                       // beam bit of the columns 8 nt + 2 t, + 1 of this lane (0: no such column)
+  uint32_t qf[NT][KS][2];                    // B fragments of Q'^T, column 8 nt + g
+  float m_run[NT][2], l_run[NT][2];          // reference and this lane's share of the sum of columns 2 t, 2 t + 1
+  float acc[NT][NV][4];                      // O^T: [dim g: column 2t, 2t+1 | dim g + 8: the same]
+  float v_ref = 0.f;                         // 8-bit pages: acc is in units of this V scale times 2^-12
+
+  auto flush = [&]() {
+    if (u_block < 0) return;
+    const long long slot = static_cast<long long>(u_block) * p.n_kv_heads + u_head + w;
+    const float unit = FP8 ? v_ref * 0x1p-12f : 1.f;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float l = l_run[nt][c];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(kFull, l, o);
+        const int col = 8 * nt + 2 * t + c;
+        if (col < p.columns) {
+          float* dst = p.part_o + (slot * p.columns + col) * D;
+#pragma unroll
+          for (int db = 0; db < NV; ++db) { dst[16 * db + g] = acc[nt][db][c] * unit; dst[16 * db + 8 + g] = acc[nt][db][2 + c] * unit; }
+          if (g == 0) p.part_ml[slot * p.columns + col] = make_float2(m_run[nt][c], l);
+        }
+      }
+  };
+  // The queries of the unit, rotated by their position less the anchor.
+  auto rotate_queries = [&]() {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int col = 8 * nt + g, beam = col / G, group = u_block / p.blocks, at = (u_block - group * p.blocks) * p.beams + beam;
+      const bool live = beam < p.beams && at < p.width;
+      const int row = live ? group * p.width + at : 0;
+      const int rel = live ? __ldg(p.q_pos + row) - anchor : 0;
+      int arel = rel < 0 ? -rel : rel;
+      if (static_cast<unsigned>(arel) > static_cast<unsigned>(p.max_position)) { atomicOr(p.status, MEPIC_DEV_BAD_POSITION); arel = p.max_position; }
+      const float sc = live ? p.scale_log2 : 0.f, sn = rel < 0 ? -sc : sc;
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + static_cast<size_t>(row) * p.q_stride + (static_cast<size_t>(u_head) * G + (live ? col - beam * G : 0)) * D);
+      const float* turn = p.rope + static_cast<size_t>(arel) * D;
+#pragma unroll
+      for (int j = 0; j < KH; ++j)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int pair = pair_of(j, r);
+          const float2 lo = bf16x2_to_float2(__ldg(src + pair / 2)), hi = bf16x2_to_float2(__ldg(src + (pair + D / 2) / 2));
+          const float4 cs = __ldg(reinterpret_cast<const float4*>(turn + 2 * pair));
+          const float c0 = cs.x * sc, s0 = cs.y * sn, c1 = cs.z * sc, s1 = cs.w * sn;
+          const float a0 = lo.x * c0 - hi.x * s0, a1 = lo.y * c1 - hi.y * s1, b0 = lo.x * s0 + hi.x * c0, b1 = lo.y * s1 + hi.y * c1;
+          qf[nt][j][r] = FP8 ? pack_f16x2(a0, a1) : pack_bf16x2(a0, a1);
+          qf[nt][j + KH][r] = FP8 ? pack_f16x2(b0, b1) : pack_bf16x2(b0, b1);
+        }
+    }
+  };
+
+  int stage = 0;
+  uint32_t parity = 0;
+  for (long long x = x0; x < x1; ++x) {
+    if (cu.block != u_block || cu.head != u_head) {
+      flush();
+      u_block = cu.block; u_head = cu.head;
+      anchor = INT_MIN; v_ref = 0.f;
+      const int first = (u_block % p.blocks) * p.beams, nb = min(p.beams, p.width - first);
+      all_beams = nb == 32 ? ~0u : (1u << nb) - 1;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int beam = (8 * nt + 2 * t + c) / G;
+          see[nt][c] = beam < nb ? 1u << beam : 0u;
+          m_run[nt][c] = -FLT_MAX; l_run[nt][c] = 0.f;
+        }
+#pragma unroll
+        for (int db = 0; db < NV; ++db) { acc[nt][db][0] = 0.f; acc[nt][db][1] = 0.f; acc[nt][db][2] = 0.f; acc[nt][db][3] = 0.f; }
+      }
+    }
+    const int pos = meta[stage * 4], n_valid = meta[stage * 4 + 2];
+    const unsigned beams = static_cast<unsigned>(meta[stage * 4 + 1]);
+    if (n_valid > 0 && (anchor == INT_MIN || static_cast<unsigned>(pos - anchor) > kAngles - kTile)) { anchor = pos; rotate_queries(); }
+    if (!mbar_wait_bounded(smem_u32(&bars[stage]), parity, p.spin_limit)) {
+      // Give the copies still in flight a last bounded chance to land, then leave cleanly.
+      if (lane == 0) atomicOr(p.status, MEPIC_DEV_WAIT_EXPIRED);
+      for (int s = 0; s < kStages; ++s) mbar_wait_bounded(smem_u32(&bars[s]), s == stage ? parity : (s < stage ? parity ^ 1u : parity), p.spin_limit);
+      return;
+    }
+    if (n_valid > 0) {
+      const uint32_t ks_addr = smem_u32(stage0 + stage * kStageBytes), vs_addr = ks_addr + KB * kBlockBytes;
+      // slots past the filled ones may hold anything: their P is 0, but 0 x NaN is NaN, so V must be finite there
+      if (n_valid < kTile) {
+        for (int idx = n_valid * 8 * KB + lane; idx < kTile * 8 * KB; idx += 32) {
+          const int key = idx / (8 * KB), chk = idx % (8 * KB);
+          const uint32_t a = vs_addr + (chk / 8) * kBlockBytes + key * 128 + (((chk % 8) ^ (key & 7)) << 4);
+          asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0) : "memory");
+        }
+        // these generic-proxy stores must be ordered before the TMA (async proxy) write that refills this stage
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      }
+      // ---- S^T = K' Q'^T
+      float sc[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) { sc[nt][0] = 0.f; sc[nt][1] = 0.f; sc[nt][2] = 0.f; sc[nt][3] = 0.f; }
+      const int offA = pos - anchor + keyA, offB = pos - anchor + keyB;
+#pragma unroll
+      for (int j = 0; j < KH; ++j) {
+        uint32_t lo[4], hi[4];      // A fragments of k-steps j, j + KH: [key A, key B | key A, key B (second column half)]
+        if constexpr (FP8) {
+          uint32_t raw[4];          // [key A, key B of chunk j | of chunk j + KH], four dims each
+          {
+            const int mi = lane >> 3, rr = lane & 7, key = 4 * (rr >> 1) + (rr & 1) + 2 * (mi & 1), chk = j + KH * (mi >> 1);
+            ldmatrix_x4(raw, ks_addr + key * 128 + ((chk ^ (key & 7)) << 4));
+          }
+          e4m3x4_to_f16x2x2(raw[0], lo[0], lo[2]);
+          e4m3x4_to_f16x2x2(raw[1], lo[1], lo[3]);
+          e4m3x4_to_f16x2x2(raw[2], hi[0], hi[2]);
+          e4m3x4_to_f16x2x2(raw[3], hi[1], hi[3]);
+          const int u8 = (16 * j + 4 * t) * 4;      // byte of the quadruple of pairs 16 j + 4 t
+          const uint4 ca = *reinterpret_cast<const uint4*>(angles + offA * kAngleBytes + (u8 ^ ((offA & 1) << 6)));
+          const uint4 cb = *reinterpret_cast<const uint4*>(angles + offB * kAngleBytes + (u8 ^ ((offB & 1) << 6)));
+          const uint32_t cc[4] = {ca.x, cb.x, ca.z, cb.z}, ss[4] = {ca.y, cb.y, ca.w, cb.w};
+#pragma unroll
+          for (int f = 0; f < 4; ++f) {
+            const uint32_t a = lo[f], b = hi[f];
+            lo[f] = f16x2_fma(a, cc[f], f16x2_neg(f16x2_mul(b, ss[f])));
+            hi[f] = f16x2_fma(a, ss[f], f16x2_mul(b, cc[f]));
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            mma_f16(sc[nt], lo[0], lo[1], lo[2], lo[3], qf[nt][j][0], qf[nt][j][1]);
+            mma_f16(sc[nt], hi[0], hi[1], hi[2], hi[3], qf[nt][j + KH][0], qf[nt][j + KH][1]);
+          }
+        } else {
+          {
+            // lane -> (matrix mi = lane / 8, row = lane % 8): key = 8 (mi & 1) + row, 16-byte chunk 2 j + (mi >> 1)
+            const int mi = lane >> 3, key = ((mi & 1) << 3) + (lane & 7);
+            const int cl = 2 * j + (mi >> 1), chh = 2 * (j + KH) + (mi >> 1);
+            ldmatrix_x4(lo, ks_addr + (cl / 8) * kBlockBytes + key * 128 + (((cl % 8) ^ (key & 7)) << 4));
+            ldmatrix_x4(hi, ks_addr + (chh / 8) * kBlockBytes + key * 128 + (((chh % 8) ^ (key & 7)) << 4));
+          }
+#pragma unroll
+          for (int f = 0; f < 4; ++f) {
+            const int off = (f & 1) ? offB : offA, r = f >> 1;
+            const float4 cs = *reinterpret_cast<const float4*>(angles + off * kAngleBytes + (((16 * j + 2 * t + 8 * r) * 8) ^ ((off & 1) << 6)));
+            const float2 c = make_float2(cs.x, cs.y), s = make_float2(cs.z, cs.w), ns = make_float2(-cs.z, -cs.w);
+            const float2 a = bf16x2_to_float2(lo[f]), b = bf16x2_to_float2(hi[f]);
+            const float2 x = fma2(a, c, mul2(b, ns)), y = fma2(a, s, mul2(b, c));
+            lo[f] = pack_bf16x2(x.x, x.y); hi[f] = pack_bf16x2(y.x, y.y);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            mma_bf16(sc[nt], lo[0], lo[1], lo[2], lo[3], qf[nt][j][0], qf[nt][j][1]);
+            mma_bf16(sc[nt], hi[0], hi[1], hi[2], hi[3], qf[nt][j + KH][0], qf[nt][j + KH][1]);
+          }
+        }
+      }
+      // ---- online softmax (log2 domain): keys A (0, 1) and B (2, 3) of columns 2t (0, 2) and 2t + 1 (1, 3)
+      const bool some = (beams & all_beams) != all_beams;
+      float v_scale = 0.f;
+      if constexpr (FP8) {
+        const float k_scale = scl[stage * 2], vs = scl[stage * 2 + 1];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) { sc[nt][0] *= k_scale; sc[nt][1] *= k_scale; sc[nt][2] *= k_scale; sc[nt][3] *= k_scale; }
+        // P carries the page's V scale relative to the largest met so far, and 2^12 so that small weights stay normal in fp16
+        const bool finite = vs <= FLT_MAX;      // a page's scale may be infinite or NaN: that is for the columns that see the page, not for the others
+        if (finite && vs > v_ref) {
+          const float f = v_ref / vs;
+          v_ref = vs;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int db = 0; db < NV; ++db) { acc[nt][db][0] *= f; acc[nt][db][1] *= f; acc[nt][db][2] *= f; acc[nt][db][3] *= f; }
+        }
+        v_scale = !finite ? __int_as_float(0x7fffffff) : v_ref > 0.f ? vs / v_ref * 0x1p12f : 0.f;
+      }
+      if (n_valid < kTile) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          if (keyA >= n_valid) { sc[nt][0] = -INFINITY; sc[nt][1] = -INFINITY; }
+          if (keyB >= n_valid) { sc[nt][2] = -INFINITY; sc[nt][3] = -INFINITY; }
+        }
+      }
+      if (some) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          if (!(see[nt][0] & beams)) { sc[nt][0] = -INFINITY; sc[nt][2] = -INFINITY; }
+          if (!(see[nt][1] & beams)) { sc[nt][1] = -INFINITY; sc[nt][3] = -INFINITY; }
+        }
+      }
+      bool higher = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) higher = higher || fmaxf(sc[nt][0], sc[nt][2]) > m_run[nt][0] || fmaxf(sc[nt][1], sc[nt][3]) > m_run[nt][1];
+      // the references move only if some lane saw a larger score
+      if (__any_sync(kFull, higher)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float mx0 = fmaxf(sc[nt][0], sc[nt][2]), mx1 = fmaxf(sc[nt][1], sc[nt][3]);
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) { mx0 = fmaxf(mx0, __shfl_xor_sync(kFull, mx0, o)); mx1 = fmaxf(mx1, __shfl_xor_sync(kFull, mx1, o)); }
+          const float n0 = fmaxf(m_run[nt][0], mx0), n1 = fmaxf(m_run[nt][1], mx1);
+          const float a0 = ex2(m_run[nt][0] - n0), a1 = ex2(m_run[nt][1] - n1);
+          m_run[nt][0] = n0; m_run[nt][1] = n1;
+          l_run[nt][0] *= a0; l_run[nt][1] *= a1;
+#pragma unroll
+          for (int db = 0; db < NV; ++db) { acc[nt][db][0] *= a0; acc[nt][db][1] *= a1; acc[nt][db][2] *= a0; acc[nt][db][3] *= a1; }
+        }
+      }
+      uint32_t pb[NT][2];                    // B fragments of P^T: the transposes of the two 8 x 8 blocks (key row, columns)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p0 = ex2(sc[nt][0] - m_run[nt][0]), p1 = ex2(sc[nt][1] - m_run[nt][1]), p2 = ex2(sc[nt][2] - m_run[nt][0]), p3 = ex2(sc[nt][3] - m_run[nt][1]);
+        l_run[nt][0] += p0 + p2; l_run[nt][1] += p1 + p3;
+        if constexpr (FP8) {
+          pb[nt][0] = movmatrix_trans(pack_f16x2(p0 * v_scale, p1 * v_scale));
+          pb[nt][1] = movmatrix_trans(pack_f16x2(p2 * v_scale, p3 * v_scale));
+        } else {
+          pb[nt][0] = movmatrix_trans(pack_bf16x2(p0, p1));
+          pb[nt][1] = movmatrix_trans(pack_bf16x2(p2, p3));
+        }
+      }
+      // ---- O^T += V^T P^T
+      auto add_block = [&](int db, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          if (!some) {
+            if constexpr (FP8) mma_f16(acc[nt][db], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+            else mma_bf16(acc[nt][db], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+          } else {
+            float x[4] = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (FP8) mma_f16(x, a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+            else mma_bf16(x, a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+            if (see[nt][0] & beams) { acc[nt][db][0] += x[0]; acc[nt][db][2] += x[2]; }
+            if (see[nt][1] & beams) { acc[nt][db][1] += x[1]; acc[nt][db][3] += x[3]; }
+          }
+        }
+      };
+      if constexpr (FP8) {
+#pragma unroll
+        for (int c = 0; c < NV; c += 2) {
+          uint32_t raw[4];          // [block c: dim g, dim g + 8 | block c + 1: the same], keys 4t .. 4t+3 each
+          {
+            const int key = lane & 15, chk = c + (lane >> 4);
+            ldmatrix_b8_trans_x2(raw, vs_addr + key * 128 + ((chk ^ (key & 7)) << 4));
+          }
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            uint32_t a0, a1, a2, a3;
+            e4m3x4_to_f16x2x2(raw[2 * m], a0, a2);
+            e4m3x4_to_f16x2x2(raw[2 * m + 1], a1, a3);
+            add_block(c + m, a0, a1, a2, a3);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int db = 0; db < NV; ++db) {
+          uint32_t va[4];             // a0 dims g x keys 0-7, a1 dims g+8 x keys 0-7, a2 dims g x keys 8-15, a3 dims g+8 x keys 8-15
+          {
+            const int mi = lane >> 3, key = ((mi >> 1) << 3) + (lane & 7), ch = 2 * db + (mi & 1);
+            ldmatrix_x4_trans(va, vs_addr + (ch / 8) * kBlockBytes + key * 128 + (((ch % 8) ^ (key & 7)) << 4));
+          }
+          add_block(db, va[0], va[1], va[2], va[3]);
+        }
+      }
+    }
+    __syncwarp();   // every lane is done with this stage
+    if (issued < x1) issue(stage);
+    __syncwarp();
+    if (--c_left == 0) {
+      next_unit(p, cu);
+      c_left = static_cast<long long>(cu.r1 - cu.r0) << p.log2_tpp;
+    }
+    if (++stage == kStages) { stage = 0; parity ^= 1u; }
+  }
+  flush();
+}
+
+// ---------------------------------------------------------------- merge
+// A CTA of four warps per (unit, column): its partials are dealt round to the warps, a lane owns D / 32 output dims.
+template <int D>
+__global__ void __launch_bounds__(128) mepic_beam_merge(const __grid_constant__ BeamParams p) {
+  constexpr int E = D / 32;
+  const int unit = blockIdx.x, col = blockIdx.y, wv = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __shared__ float sh_m[4], sh_l[4];
+  __shared__ float sh_o[4][D];
+  const int block = unit / p.n_kv_heads, head = unit - block * p.n_kv_heads, group = block / p.blocks;
+  const int beam = (block - group * p.blocks) * p.beams + col / p.group_size;
+  if (beam >= p.width) return;
+  const size_t row = static_cast<size_t>(group) * p.width + beam;
+  const bool fits = plan_fits(p);
+  if (!fits && unit == 0 && col == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_PLAN);
+  long long w0 = 0, w1 = -1;
+  bool sees = false;
+  if (fits) {
+    const Cut cut = cut_of_line(p);
+    Unit u{block, head, 0, 0};
+    bounds_of(p, u);
+    const long long per = static_cast<long long>(u.r1 - u.r0) << p.log2_tpp, begin = (static_cast<long long>(u.r0) << p.log2_tpp) * p.n_kv_heads + head * per;
+    if (per > 0) { w0 = begin / cut.piece; w1 = (begin + per - 1) / cut.piece; }
+    sees = __ldg(p.lens + row) > 0;
+  }
+  // launched as a programmatic dependent of the attention kernel: its partials are complete and visible after this
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  float m = -FLT_MAX;
+  for (long long k = w0 + wv; k <= w1; k += 4) m = fmaxf(m, p.part_ml[(unit + k) * p.columns + col].x);
+  if (lane == 0) sh_m[wv] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
+  float l = 0.f, o[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) o[i] = 0.f;
+#pragma unroll 2
+  for (long long k = w0 + wv; k <= w1; k += 4) {
+    const float2 ml = p.part_ml[(unit + k) * p.columns + col];
+    const float wgt = ex2(ml.x - m);
+    l += ml.y * wgt;
+    const float* src = p.part_o + ((unit + k) * p.columns + col) * D + E * lane;
+#pragma unroll
+    for (int i = 0; i < E; ++i) o[i] += src[i] * wgt;
+  }
+  if (lane == 0) sh_l[wv] = l;
+#pragma unroll
+  for (int i = 0; i < E; ++i) sh_o[wv][E * lane + i] = o[i];
+  __syncthreads();
+  if (wv != 0) return;
+  l = (sh_l[0] + sh_l[1]) + (sh_l[2] + sh_l[3]);
+  uint16_t* dst = p.out + (row * p.n_kv_heads * p.group_size + static_cast<size_t>(head) * p.group_size + col % p.group_size) * D + E * lane;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const float x = (sh_o[0][E * lane + i] + sh_o[1][E * lane + i]) + (sh_o[2][E * lane + i] + sh_o[3][E * lane + i]);
+    dst[i] = f32_to_bf16_bits(sees ? x / l : 0.f);      // l = 0 where the row sees slots: every score is -infinity, 0 / 0
+  }
+}
+
+// ---------------------------------------------------------------- host side
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+int sm_count(int* device) {
+  static std::atomic<int> known[64];             // a device's count does not change: asked once
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  *device = dev;
+  if (dev < 64 && (sms = known[dev].load(std::memory_order_relaxed)) > 0) return sms;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  if (dev < 64) known[dev].store(sms, std::memory_order_relaxed);
+  return sms;
+}
+constexpr int kMaxWarps = 12;
+constexpr int warps_of(int, bool) { return 8; }
+size_t slots_of(const PlanShape& s, int n_kv_heads, int sms) { return static_cast<size_t>(s.groups) * s.blocks * n_kv_heads + static_cast<size_t>(sms) * kMaxWarps; }
+size_t workspace_bytes(const mepic_config_t* cfg, const PlanShape& s, int sms) {
+  const size_t columns = static_cast<size_t>(s.beams) * (cfg->n_q_heads / cfg->n_kv_heads);
+  return slots_of(s, cfg->n_kv_heads, sms) * columns * (cfg->head_dim + 2) * sizeof(float);
+}
+
+template <int D, int NT, bool FP8>
+int32_t launch_beam(BeamParams& p, int sms, int device, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t st) {
+  constexpr int W = warps_of(NT, FP8);
+  constexpr size_t smem = smem_bytes<D, FP8, W>;
+  static_assert(smem <= 232448, "shared memory of a CTA");
+  static std::atomic<unsigned long long> prepared{0};      // devices on which the limit is raised
+  const unsigned long long bit = device < 64 ? 1ull << device : 0;
+  cudaError_t e = cudaSuccess;
+  if (!(prepared.load(std::memory_order_relaxed) & bit) || !bit) {
+    e = cudaFuncSetAttribute(mepic_beam_attn<D, NT, FP8, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) { mepic_set_error("attn_beam: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+    prepared.fetch_or(bit, std::memory_order_relaxed);
+  }
+  p.workers = sms * W;
+  mepic_beam_attn<D, NT, FP8, W><<<sms, W * 32, smem, st>>>(p, map_k, map_v);
+  e = cudaGetLastError();
+  if (e == cudaSuccess) e = launch_dependent(mepic_beam_merge<D>, dim3(static_cast<unsigned>(p.groups) * p.blocks * p.n_kv_heads, p.columns), dim3(128), st, p);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  if (e != cudaSuccess) { mepic_set_error("attn_beam: launch: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  mepic_count_launches(2);
+  return MEPIC_OK;
+}
+
+int32_t beam_call(const mepic_config_t* cfg, const mepic_attn_beam_args_t* a, const float* k_scales, const float* v_scales, bool fp8, void* cuda_stream) {
+  const char* what = fp8 ? "attn_beam_fp8" : "attn_beam";
+  if (!mepic_config_ok(cfg)) return MEPIC_E_INVAL;
+  if (!a) { mepic_set_error("%s: NULL argument", what); return MEPIC_E_INVAL; }
+  if (fp8 && cfg->head_dim != 128) { mepic_set_error("%s: head_dim %d: 8-bit pages are built for head_dim 128", what, cfg->head_dim); return MEPIC_E_INVAL; }
+  PlanShape s;
+  if (!plan_shape(cfg, a->groups, a->width, a->table_stride, what, &s)) return MEPIC_E_INVAL;
+  if (!a->q || !a->q_pos || !a->plan || !a->k_pool || !a->v_pool || !a->rope_table || !a->out || !a->workspace || !a->status) {
+    mepic_set_error("%s: NULL pointer argument", what); return MEPIC_E_INVAL;
+  }
+  if (fp8 && (!k_scales || !v_scales)) { mepic_set_error("%s: NULL scale pointer", what); return MEPIC_E_INVAL; }
+  if (!aligned16(a->q) || !aligned16(a->plan) || !aligned16(a->k_pool) || !aligned16(a->v_pool) || !aligned16(a->rope_table) || !aligned16(a->out) || !aligned16(a->workspace)) {
+    mepic_set_error("%s: pointers must be 16-byte aligned", what); return MEPIC_E_INVAL;
+  }
+  const long long packed = static_cast<long long>(cfg->n_q_heads) * cfg->head_dim, q_stride = a->q_stride ? a->q_stride : packed;
+  if (packed > 0x7fffffffLL || q_stride < packed || q_stride % 8) { mepic_set_error("%s: q_stride %d must be 0 or a multiple of 8 of at least a packed row", what, a->q_stride); return MEPIC_E_INVAL; }
+  if (static_cast<long long>(s.groups) * s.blocks * cfg->n_kv_heads > 0x7fffffffLL) { mepic_set_error("%s: too many beams and heads", what); return MEPIC_E_INVAL; }
+  int device = 0;
+  const int sms = sm_count(&device);
+  if (sms <= 0) { mepic_set_error("%s: no CUDA device", what); return MEPIC_E_CUDA; }
+  const size_t need = workspace_bytes(cfg, s, sms);
+  if (a->workspace_bytes < need) { mepic_set_error("%s: workspace of %zu bytes, %zu needed", what, a->workspace_bytes, need); return MEPIC_E_INVAL; }
+  BeamParams p;
+  p.q = static_cast<const uint16_t*>(a->q); p.q_pos = a->q_pos;
+  p.head = static_cast<const int32_t*>(a->plan);
+  p.sums = p.head + kHead; p.lens = p.head + s.off_len;
+  p.records = reinterpret_cast<const int4*>(p.head + s.off_rec);
+  p.rope = a->rope_table; p.k_scales = k_scales; p.v_scales = v_scales;
+  p.out = static_cast<uint16_t*>(a->out); p.status = a->status;
+  p.groups = s.groups; p.width = s.width; p.stride = a->table_stride; p.blocks = s.blocks; p.beams = s.beams; p.segments = s.segments;
+  p.group_size = cfg->n_q_heads / cfg->n_kv_heads; p.columns = s.beams * p.group_size;
+  p.n_kv_heads = cfg->n_kv_heads; p.page_size = cfg->page_size; p.num_pages = cfg->num_pages; p.max_position = cfg->max_position;
+  p.log2_tpp = 0;
+  while ((kTile << p.log2_tpp) < cfg->page_size) ++p.log2_tpp;
+  p.q_stride = static_cast<int>(q_stride);
+  p.scale_log2 = a->sm_scale * 1.4426950408889634f;
+  p.spin_limit = mepic_test_spin_limit(kSpinLimit); p.skip_tile = mepic_test_skip_tile();
+  p.part_o = static_cast<float*>(a->workspace);
+  p.part_ml = reinterpret_cast<float2*>(p.part_o + slots_of(s, cfg->n_kv_heads, sms) * p.columns * cfg->head_dim);
+  alignas(64) CUtensorMap map_k, map_v;
+  int32_t rc = fp8 ? mepic_make_pool_map_u8(cfg, a->k_pool, &map_k) : mepic_make_pool_map(cfg, a->k_pool, &map_k);
+  if (rc == MEPIC_OK) rc = fp8 ? mepic_make_pool_map_u8(cfg, a->v_pool, &map_v) : mepic_make_pool_map(cfg, a->v_pool, &map_v);
+  if (rc != MEPIC_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const int nt = (p.columns + 7) / 8;
+#define MEPIC_BEAM_CASE(NT)                                                                                     \
+  if (nt == NT) return fp8 ? launch_beam<128, NT, true>(p, sms, device, map_k, map_v, st)                        \
+                           : cfg->head_dim == 128 ? launch_beam<128, NT, false>(p, sms, device, map_k, map_v, st) \
+                                                  : launch_beam<64, NT, false>(p, sms, device, map_k, map_v, st);
+  MEPIC_BEAM_CASE(1) MEPIC_BEAM_CASE(2) MEPIC_BEAM_CASE(3) MEPIC_BEAM_CASE(4)
+#undef MEPIC_BEAM_CASE
+  mepic_set_error("%s: %d columns", what, p.columns);
+  return MEPIC_E_INVAL;
+}
+
+}  // namespace
+
+extern "C" size_t mepic_beam_plan_bytes(const mepic_config_t* cfg, int32_t groups, int32_t width, int32_t table_stride) {
+  PlanShape s;
+  return mepic_config_ok(cfg) && plan_shape(cfg, groups, width, table_stride, "beam_plan", &s) ? s.bytes : 0;
+}
+
+extern "C" int32_t mepic_beam_plan(const mepic_config_t* cfg, const mepic_beam_plan_args_t* a, void* cuda_stream) {
+  if (!mepic_config_ok(cfg)) return MEPIC_E_INVAL;
+  if (!a) { mepic_set_error("beam_plan: NULL argument"); return MEPIC_E_INVAL; }
+  PlanShape s;
+  if (!plan_shape(cfg, a->groups, a->width, a->table_stride, "beam_plan", &s)) return MEPIC_E_INVAL;
+  if (!a->page_ids || !a->pos_base || !a->kv_len || !a->plan || !a->status) { mepic_set_error("beam_plan: NULL pointer argument"); return MEPIC_E_INVAL; }
+  if (!aligned16(a->plan)) { mepic_set_error("beam_plan: the plan must be 16-byte aligned"); return MEPIC_E_INVAL; }
+  if (a->plan_bytes < s.bytes) { mepic_set_error("beam_plan: a plan of %zu bytes, %zu needed", a->plan_bytes, s.bytes); return MEPIC_E_INVAL; }
+  if (s.segments > 65535) { mepic_set_error("beam_plan: table_stride %d is too large", a->table_stride); return MEPIC_E_INVAL; }
+  PlanParams p;
+  p.page_ids = a->page_ids; p.pos_base = a->pos_base; p.kv_len = a->kv_len; p.status = a->status;
+  p.head = static_cast<int32_t*>(a->plan);
+  p.sums = p.head + kHead; p.lens = p.head + s.off_len;
+  p.records = reinterpret_cast<int4*>(p.head + s.off_rec);
+  p.stride = a->table_stride; p.groups = s.groups; p.width = s.width; p.blocks = s.blocks; p.beams = s.beams; p.segments = s.segments;
+  p.page_shift = 0;
+  while ((1 << p.page_shift) < cfg->page_size) ++p.page_shift;
+  p.num_pages = cfg->num_pages; p.group_size = cfg->n_q_heads / cfg->n_kv_heads; p.n_kv_heads = cfg->n_kv_heads;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  mepic_beam_plan_classes<<<dim3(static_cast<unsigned>(s.groups) * s.blocks, s.segments), kSeg, 0, st>>>(p);
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess) e = launch_dependent(mepic_beam_plan_sums, dim3(1), dim3(kScanThreads), st, p);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  if (e != cudaSuccess) { mepic_set_error("beam_plan: launch: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  mepic_count_launches(2);
+  return MEPIC_OK;
+}
+
+extern "C" size_t mepic_attn_beam_workspace(const mepic_config_t* cfg, int32_t groups, int32_t width) {
+  PlanShape s;
+  if (!mepic_config_ok(cfg) || !plan_shape(cfg, groups, width, 1, "attn_beam_workspace", &s)) return 0;
+  int device = 0;
+  const int sms = sm_count(&device);
+  if (sms <= 0) { mepic_set_error("attn_beam_workspace: no CUDA device"); return 0; }
+  return workspace_bytes(cfg, s, sms);
+}
+extern "C" int32_t mepic_attn_beam(const mepic_config_t* cfg, const mepic_attn_beam_args_t* args, void* cuda_stream) {
+  return beam_call(cfg, args, nullptr, nullptr, false, cuda_stream);
+}
+extern "C" int32_t mepic_attn_beam_fp8(const mepic_config_t* cfg, const mepic_attn_beam_args_t* args, const float* k_scales, const float* v_scales,
+                                       void* cuda_stream) {
+  return beam_call(cfg, args, k_scales, v_scales, true, cuda_stream);
+}

@@ -1,0 +1,667 @@
+// A decode with beams, apart from its attention: selection over beams and vocabulary, block tables of the new beams, page copies
+// (see "beams" in mepic.h).
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "mepic.h"
+#include "mepic_internal.h"
+#include "mepic_ptx.cuh"
+
+namespace {
+
+using namespace mepic_dev;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWidth = MEPIC_BEAM_MAX_WIDTH;
+
+// ---------------------------------------------------------------- selection
+// Two launches.  The first cuts every row of logits into segments, one CTA each: a segment is read once, into registers, and
+// leaves its maximum, its sum of exponentials and its n_select best tokens in order.  The second joins a group's segments: the
+// n_select best of a row are among its segments' best, and those of a group among its rows'.
+constexpr int kSelThreads = 256;
+constexpr int kSelWarps = kSelThreads / 32;
+constexpr int kSelChunks = 8;                  // 16-byte pieces a thread holds
+
+template <typename T> struct Vec { static constexpr int n = 16 / sizeof(T); };
+
+template <typename T> __device__ __forceinline__ void widen(const uint4& c, float (&x)[Vec<T>::n]);
+template <> __device__ __forceinline__ void widen<float>(const uint4& c, float (&x)[4]) {
+  x[0] = __uint_as_float(c.x); x[1] = __uint_as_float(c.y); x[2] = __uint_as_float(c.z); x[3] = __uint_as_float(c.w);
+}
+template <> __device__ __forceinline__ void widen<__nv_bfloat16>(const uint4& c, float (&x)[8]) {
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const float2 f = bf16x2_to_float2(w[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
+}
+template <> __device__ __forceinline__ void widen<__half>(const uint4& c, float (&x)[8]) {
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i])); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
+}
+template <typename T> __device__ __forceinline__ T minus_infinity();
+template <> __device__ __forceinline__ float minus_infinity<float>() { return -INFINITY; }
+template <> __device__ __forceinline__ __nv_bfloat16 minus_infinity<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80); }
+template <> __device__ __forceinline__ __half minus_infinity<__half>() { return __ushort_as_half(0xfc00); }
+
+// Key of a token: the larger logit first, the lower index among equals (-0 counts as 0); 0 where there is no candidate
+// (-infinity; a NaN's row is given up as a whole).
+__device__ __forceinline__ uint64_t token_key(float x, int at) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  const uint32_t s = u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+  return x > -INFINITY ? static_cast<uint64_t>(s) << 32 | (0xffffffffu - static_cast<uint32_t>(at)) : 0;
+}
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const uint32_t s = static_cast<uint32_t>(k >> 32);
+  return __uint_as_float(s ^ ((s >> 31) ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ int key_token(uint64_t k) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(k)); }
+__device__ __forceinline__ uint64_t warp_max_key(uint64_t k) {
+  const uint32_t hi = static_cast<uint32_t>(k >> 32), top = __reduce_max_sync(kFull, hi);
+  return static_cast<uint64_t>(top) << 32 | __reduce_max_sync(kFull, hi == top ? static_cast<uint32_t>(k) : 0u);
+}
+
+struct SegmentSum { double sum; float top; float pad; };      // sum of exp(x - top) over the segment; NaN: the row is to be given up
+
+struct SelectParams {
+  mepic_beam_select_args_t a;
+  SegmentSum* sums;      // [rows][segments]
+  uint64_t* best;        // [rows][segments][n_select], descending, 0 where there are fewer
+  int segments;
+  long long stride;
+};
+
+// One segment of one row.
+template <typename T>
+__global__ void __launch_bounds__(kSelThreads) mepic_beam_segments(const __grid_constant__ SelectParams p) {
+  constexpr int N = Vec<T>::n;
+  __shared__ uint64_t round_best[2][kSelWarps];
+  __shared__ double warp_sums[kSelWarps];
+  __shared__ float warp_tops[kSelWarps];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int row = blockIdx.y, seg = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const float score = __ldg(p.a.score + row);
+  if (score == -INFINITY || (p.a.done && __ldg(p.a.done + row) != 0)) return;        // nobody reads what such a row leaves
+  const T* x = static_cast<const T*>(p.a.logits) + row * p.stride;
+  // pieces of 16 bytes by address: the row may begin and end inside one
+  const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
+  const int V = p.a.vocab;
+  uint4 c[kSelChunks];
+  long long at0[kSelChunks];       // token of a piece's first element (negative in the row's first piece)
+#pragma unroll
+  for (int k = 0; k < kSelChunks; ++k) {
+    at0[k] = (static_cast<long long>(seg) * kSelChunks * kSelThreads + k * kSelThreads + tid) * N - lead;
+    if (at0[k] >= 0 && at0[k] + N <= V) c[k] = __ldcs(reinterpret_cast<const uint4*>(x + at0[k]));
+    else {
+      alignas(16) T e[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) e[i] = at0[k] + i >= 0 && at0[k] + i < V ? x[at0[k] + i] : minus_infinity<T>();
+      c[k] = *reinterpret_cast<const uint4*>(e);
+    }
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kSelChunks; ++k) {
+    float v[N];
+    widen<T>(c[k], v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fmaxf(top, v[i]);
+  }
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < kSelChunks; ++k) {
+    float v[N];
+    widen<T>(c[k], v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum += ex2((v[i] - ref) * kLog2e);      // +infinity - +infinity and NaN - anything: NaN
+  }
+  // ---- maximum and sum of the segment
+  float wtop = top;
+#pragma unroll
+  for (int d = 16; d; d >>= 1) wtop = fmaxf(wtop, __shfl_xor_sync(kFull, wtop, d));
+  double s = static_cast<double>(sum) * (top == -INFINITY ? 1.0 : static_cast<double>(ex2((top - wtop) * kLog2e)));
+#pragma unroll
+  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(kFull, s, d);
+  if (lane == 0) { warp_sums[warp] = s; warp_tops[warp] = wtop; }
+  // ---- the n_select best, one a round
+  const int K = p.a.n_select;
+  uint64_t last = ~0ull, mine = 0;
+  auto rescan = [&]() {
+    mine = 0;
+#pragma unroll
+    for (int k = 0; k < kSelChunks; ++k) {
+      float v[N];
+      widen<T>(c[k], v);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint64_t key = token_key(v[i], static_cast<int>(at0[k] + i));
+        if (key < last && key > mine) mine = key;
+      }
+    }
+  };
+  rescan();
+  uint64_t* out = p.best + (static_cast<size_t>(row) * p.segments + seg) * K;
+  for (int k = 0; k < K; ++k) {
+    const uint64_t w = warp_max_key(mine);
+    if (lane == 0) round_best[k & 1][warp] = w;
+    __syncthreads();
+    uint64_t b = round_best[k & 1][0];
+#pragma unroll
+    for (int i = 1; i < kSelWarps; ++i) b = max(b, round_best[k & 1][i]);
+    if (tid == 0) out[k] = b;
+    if (mine == b && b) { last = b; rescan(); }
+  }
+  if (tid == 0) {
+    float t = warp_tops[0];
+    for (int i = 1; i < kSelWarps; ++i) t = fmaxf(t, warp_tops[i]);
+    double all = 0.0;
+    for (int i = 0; i < kSelWarps; ++i) all += warp_sums[i] * (warp_tops[i] == -INFINITY ? 1.0 : static_cast<double>(ex2((warp_tops[i] - t) * kLog2e)));
+    p.sums[static_cast<size_t>(row) * p.segments + seg] = SegmentSum{all, t, 0.f};
+  }
+}
+
+struct Best { double score; long long flat; };       // flat: beam * vocab + token, -1: none
+__device__ __forceinline__ bool better(const Best& x, const Best& y) {
+  if (x.flat < 0 || y.flat < 0) return x.flat >= 0;
+  return x.score > y.score || (x.score == y.score && x.flat < y.flat);
+}
+
+// One group: log-sum-exp of its rows, then its n_select best, one a round, off the heads of the segments' ordered lists.
+__global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_constant__ SelectParams p) {
+  __shared__ double lse[kWidth];
+  __shared__ int kind[kWidth];                    // 0: offers nothing, 1: live, 2: finished
+  __shared__ Best round_best[2][kSelWarps];
+  extern __shared__ unsigned char head[];         // [width * segments]: candidates of a list that are gone
+  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int W = p.a.width, S = p.segments, K = p.a.n_select, lists = W * S;
+  for (int l = tid; l < lists; l += kSelThreads) head[l] = 0;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  for (int w = warp; w < W; w += kSelWarps) {
+    const int row = g * W + w;
+    const float score = __ldg(p.a.score + row);
+    int what = 1;
+    bool bad = !(score < INFINITY);
+    double l = 0.0;
+    if (p.a.done && __ldg(p.a.done + row) != 0) what = 2;
+    else if (score > -INFINITY) {
+      const SegmentSum* seg = p.sums + static_cast<size_t>(row) * S;
+      float top = -INFINITY;
+      for (int i = lane; i < S; i += 32) top = fmaxf(top, seg[i].top);
+#pragma unroll
+      for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+      double sum = 0.0;
+      for (int i = lane; i < S; i += 32) sum += seg[i].top == -INFINITY ? seg[i].sum : seg[i].sum * exp(static_cast<double>(seg[i].top) - static_cast<double>(top));
+#pragma unroll
+      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
+      bad = bad || !(sum < INFINITY);              // NaN
+      if (!(sum > 0.0)) what = 0;                  // every token is masked
+      else l = static_cast<double>(top) + log(sum);
+    }
+    if (score == -INFINITY) what = 0;
+    if (bad) what = 0;
+    if (lane == 0) {
+      lse[w] = l; kind[w] = what;
+      if (bad) atomicOr(p.a.status, MEPIC_DEV_BAD_LOGITS);
+    }
+  }
+  __syncthreads();
+  auto head_of = [&](int l) {
+    const int w = l / S, s = l - w * S, h = head[l];
+    Best b{0.0, -1};
+    if (kind[w] == 0 || h >= K) return b;
+    const double score = static_cast<double>(__ldg(p.a.score + g * W + w));
+    if (kind[w] == 2) {
+      if (s == 0 && h == 0) b = Best{score, static_cast<long long>(w) * p.a.vocab + p.a.pad_token};
+      return b;
+    }
+    const uint64_t key = p.best[(static_cast<size_t>(g * W + w) * S + s) * K + h];
+    if (key) b = Best{score + (static_cast<double>(key_value(key)) - lse[w]), static_cast<long long>(w) * p.a.vocab + key_token(key)};
+    return b;
+  };
+  Best mine{0.0, -1};
+  int mine_list = -1;
+  auto rescan = [&]() {
+    mine = Best{0.0, -1};
+    for (int l = tid; l < lists; l += kSelThreads) {
+      const Best b = head_of(l);
+      if (better(b, mine)) { mine = b; mine_list = l; }
+    }
+  };
+  rescan();
+  for (int k = 0; k < K; ++k) {
+    Best b = mine;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+      const Best o{__shfl_xor_sync(kFull, b.score, d), __shfl_xor_sync(kFull, b.flat, d)};
+      if (better(o, b)) b = o;
+    }
+    if (lane == 0) round_best[k & 1][warp] = b;
+    __syncthreads();
+    b = round_best[k & 1][0];
+#pragma unroll
+    for (int i = 1; i < kSelWarps; ++i) if (better(round_best[k & 1][i], b)) b = round_best[k & 1][i];
+    if (tid == 0) {
+      const size_t at = static_cast<size_t>(g) * K + k;
+      const bool any = b.flat >= 0;
+      const int w = any ? static_cast<int>(b.flat / p.a.vocab) : -1, v = any ? static_cast<int>(b.flat - static_cast<long long>(w) * p.a.vocab) : -1;
+      const bool ended = any && (kind[w] == 2 || v == p.a.eos_token);
+      p.a.parent[at] = w; p.a.token[at] = v;
+      p.a.score_out[at] = any ? static_cast<float>(b.score) : -INFINITY;
+      p.a.done_out[at] = ended; p.a.n_new[at] = any && !ended;
+    }
+    if (b.flat >= 0 && mine.flat == b.flat) { ++head[mine_list]; rescan(); }
+  }
+}
+
+// ---------------------------------------------------------------- fork
+// Two launches: the first finds, a CTA per group and stretch of entries, which pages nobody holds any more and how many copies a
+// group needs; in the second every CTA sums those counts up for itself and writes its share of the new tables, the reserve and
+// the copy list.
+constexpr int kForkThreads = 256;
+struct ForkParams {
+  mepic_beam_fork_args_t a;
+  int* n_freed;          // [groups][stretches]
+  int* n_copies;         // [groups]
+  int* freed;            // [groups][stretches][width_in * stretch]
+  int page_shift, num_pages, stretches, stretch;
+};
+
+// What a group's CTA knows of it: parents, lengths, and which new beams need a copy of their last page.
+struct Group {
+  int parent[kWidth], len[kWidth];       // new beam -> beam (-1: none); beam -> slots
+  unsigned copies;                       // new beams that copy
+};
+__device__ void load_group(const ForkParams& p, int g, Group& s, bool report) {
+  const int tid = threadIdx.x, Wi = p.a.width_in, Wo = p.a.width_out;
+  const long long room = min(static_cast<long long>(p.a.table_stride) << p.page_shift, 0x7fffffffll);
+  if (tid == 0) s.copies = 0;
+  if (tid < Wi) {
+    int n = __ldg(p.a.kv_len + static_cast<size_t>(g) * Wi + tid);
+    if (n < 0 || n > room) { if (report) atomicOr(p.a.status, MEPIC_DEV_BAD_SLOT); n = n < 0 ? 0 : static_cast<int>(room); }
+    s.len[tid] = n;
+  }
+  if (tid >= 32 && tid - 32 < Wo) {
+    int q = __ldg(p.a.parent + static_cast<size_t>(g) * Wo + tid - 32);
+    if (q < -1 || q >= Wi) { if (report) atomicOr(p.a.status, MEPIC_DEV_BAD_BEAM); q = -1; }
+    s.parent[tid - 32] = q;
+  }
+  __syncthreads();
+  if (tid < Wo && s.parent[tid] >= 0) {
+    const int32_t* ids = p.a.page_ids + static_cast<size_t>(g) * Wi * p.a.table_stride;
+    const int n = s.len[s.parent[tid]], P = 1 << p.page_shift;
+    if (n & (P - 1)) {
+      const int e = n >> p.page_shift, page = __ldg(ids + static_cast<size_t>(s.parent[tid]) * p.a.table_stride + e);
+      const long long from = static_cast<long long>(e) << p.page_shift;
+      bool keeps = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages) && __ldg(p.a.owned + page) != 0;
+      for (int j = 0; j < Wo && keeps; ++j) {
+        if (j == tid || s.parent[j] < 0) continue;
+        const int m = s.len[s.parent[j]];
+        if (m <= from || __ldg(ids + static_cast<size_t>(s.parent[j]) * p.a.table_stride + e) != page) continue;
+        keeps = j > tid && m < from + P;
+      }
+      if (!keeps) atomicOr(&s.copies, 1u << tid);
+    }
+  }
+  __syncthreads();
+}
+
+__global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_count(const __grid_constant__ ForkParams p) {
+  __shared__ Group s;
+  __shared__ int warp_n[kForkThreads / 32];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int g = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int Wi = p.a.width_in, Wo = p.a.width_out, stride = p.a.table_stride;
+  load_group(p, g, s, part == 0);
+  if (part == 0 && tid == 0) p.n_copies[g] = __popc(s.copies);
+  unsigned kept = 0;
+  for (int k = 0; k < Wo; ++k) if (s.parent[k] >= 0) kept |= 1u << s.parent[k];
+  const unsigned dropped = ~kept & (Wi == 32 ? ~0u : (1u << Wi) - 1);
+  const int32_t* ids = p.a.page_ids + static_cast<size_t>(g) * Wi * stride;
+  int* out = p.freed + (static_cast<size_t>(g) * p.stretches + part) * p.stretch * Wi;
+  int longest = 0;
+  for (unsigned m = dropped; m; m &= m - 1) longest = max(longest, s.len[__ffs(m) - 1]);
+  const int e_end = min(min(stride, (part + 1) * p.stretch), (longest + (1 << p.page_shift) - 1) >> p.page_shift);
+  int total = 0;
+  for (int e0 = part * p.stretch; e0 < e_end; e0 += kForkThreads) {
+    const int e = e0 + tid;
+    unsigned back = 0;
+    if (e < e_end) {
+      const long long from = static_cast<long long>(e) << p.page_shift;
+      for (unsigned m = dropped; m; m &= m - 1) {
+        const int r = __ffs(m) - 1;
+        if (s.len[r] <= from) continue;
+        const int page = __ldg(ids + static_cast<size_t>(r) * stride + e);
+        if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) { atomicOr(p.a.status, MEPIC_DEV_BAD_PAGE); continue; }
+        bool held = false;                          // by a beam that goes on, or by an earlier one that does not
+        for (unsigned o = kept | (dropped & ((1u << r) - 1)); o && !held; o &= o - 1) {
+          const int q = __ffs(o) - 1;
+          held = s.len[q] > from && __ldg(ids + static_cast<size_t>(q) * stride + e) == page;
+        }
+        if (!held && __ldg(p.a.owned + page) != 0) back |= 1u << r;
+      }
+    }
+    const int n = __popc(back);
+    int incl = n;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) { const int y = __shfl_up_sync(kFull, incl, d); if (lane >= d) incl += y; }
+    if (lane == 31) warp_n[warp] = incl;
+    __syncthreads();
+    int at = total + incl - n;
+    for (int w = 0; w < kForkThreads / 32; ++w) {
+      if (w < warp) at += warp_n[w];
+      total += warp_n[w];
+    }
+    for (; back; back &= back - 1) out[at++] = __ldg(ids + static_cast<size_t>(__ffs(back) - 1) * stride + e);
+    __syncthreads();
+  }
+  if (tid == 0) p.n_freed[g * p.stretches + part] = total;
+}
+
+// Exclusive running sums of n counts into sums[0 .. n] (shared memory).
+__device__ void running_sums(const int* counts, int n, int* sums) {
+  __shared__ int warp_n[kForkThreads / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (n + kForkThreads - 1) / kForkThreads, i0 = min(tid * per, n), i1 = min(i0 + per, n);
+  int mine = 0;
+  for (int i = i0; i < i1; ++i) mine += counts[i];
+  int incl = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) { const int y = __shfl_up_sync(kFull, incl, d); if (lane >= d) incl += y; }
+  __syncthreads();
+  if (lane == 31) warp_n[warp] = incl;
+  __syncthreads();
+  int at = incl - mine;
+  for (int w = 0; w < warp; ++w) at += warp_n[w];
+  for (int i = i0; i < i1; ++i) { sums[i] = at; at += counts[i]; }
+  if (i1 == n && i0 < n) sums[n] = at;
+  __syncthreads();
+}
+
+__global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_write(const __grid_constant__ ForkParams p) {
+  __shared__ Group s;
+  __shared__ int fresh[kWidth];
+  extern __shared__ int sums[];
+  const int g = blockIdx.x, tid = threadIdx.x;
+  const int Wi = p.a.width_in, Wo = p.a.width_out, stride = p.a.table_stride, groups = p.a.groups, S = p.stretches;
+  int* freed_at = sums;                              // [groups * stretches + 1]
+  int* copies_at = sums + groups * S + 1;            // [groups + 1]
+  load_group(p, g, s, false);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  running_sums(p.n_freed, groups * S, freed_at);
+  running_sums(p.n_copies, groups, copies_at);
+  const long long used = __ldg(p.a.reserve_used), n_freed = freed_at[groups * S], n_copies = copies_at[groups];
+  const bool bad = used < 0 || used > p.a.n_reserve || n_freed > used, full = !bad && used - n_freed + n_copies > p.a.n_reserve;
+  const bool ok = !bad && !full;
+  const int part = blockIdx.y, parts = gridDim.y;
+  // ---- the counts, and the unused end of the copy list
+  if (g == 0 && part == 0 && tid == 0) {
+    if (bad) atomicOr(p.a.status, MEPIC_DEV_BAD_BEAM);
+    if (full) atomicOr(p.a.status, MEPIC_DEV_NO_PAGES);
+    *p.a.n_copies = ok ? static_cast<int>(n_copies) : 0;
+    *p.a.reserve_used_out = static_cast<int>(ok ? used - n_freed + n_copies : used);
+  }
+  const long long rows = static_cast<long long>(groups) * Wo;
+  for (long long i = (ok ? n_copies : 0) + (static_cast<long long>(g) * parts + part) * kForkThreads + tid; i < rows; i += static_cast<long long>(groups) * parts * kForkThreads) {
+    p.a.copy_src[i] = -1; p.a.copy_dst[i] = -1; p.a.copy_slots[i] = -1;
+  }
+  if (part == 0 && tid < Wo) p.a.kv_len_out[static_cast<size_t>(g) * Wo + tid] = ok && s.parent[tid] >= 0 ? s.len[s.parent[tid]] : 0;
+  if (!ok) return;
+  // ---- pages that go back
+  for (int q = part; q < S; q += parts) {
+    const int* list = p.freed + (static_cast<size_t>(g) * S + q) * p.stretch * Wi;
+    const int n = freed_at[g * S + q + 1] - freed_at[g * S + q];
+    for (int i = tid; i < n; i += kForkThreads) p.a.reserve[used - n_freed + freed_at[g * S + q] + i] = list[i];
+  }
+  // ---- copies of this group: their pages come from the top of the reserve as it is with the returned ones on it
+  if (tid < Wo) {
+    fresh[tid] = -1;
+    if (s.copies >> tid & 1) {
+      const int rank = copies_at[g] + __popc(s.copies & ((1u << tid) - 1));
+      int page;
+      if (rank < n_freed) {
+        int lo = 0, hi = groups * S;                 // freed_at[lo] <= rank < freed_at[hi]
+        while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (freed_at[mid] <= rank) lo = mid; else hi = mid; }
+        page = p.freed[static_cast<size_t>(lo) * p.stretch * Wi + rank - freed_at[lo]];
+      } else {
+        page = p.a.reserve[used + rank - n_freed];
+      }
+      fresh[tid] = page;
+      if (part == 0) {
+        const int n = s.len[s.parent[tid]];
+        const int src = __ldg(p.a.page_ids + (static_cast<size_t>(g) * Wi + s.parent[tid]) * stride + (n >> p.page_shift));
+        if (static_cast<unsigned>(src) >= static_cast<unsigned>(p.num_pages) || static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages))
+          atomicOr(p.a.status, MEPIC_DEV_BAD_PAGE);
+        p.a.copy_src[rank] = src; p.a.copy_dst[rank] = page; p.a.copy_slots[rank] = n & ((1 << p.page_shift) - 1);
+      }
+    }
+  }
+  __syncthreads();
+  // ---- tables
+  for (int k = 0; k < Wo; ++k) {
+    if (s.parent[k] < 0) continue;
+    const int n = s.len[s.parent[k]], ents = static_cast<int>((static_cast<long long>(n) + (1 << p.page_shift) - 1) >> p.page_shift);
+    const size_t from = (static_cast<size_t>(g) * Wi + s.parent[k]) * stride, to = (static_cast<size_t>(g) * Wo + k) * stride;
+    const bool swap = s.copies >> k & 1;
+    for (int e = part * kForkThreads + tid; e < ents; e += parts * kForkThreads) {
+      const int page = __ldg(p.a.page_ids + from + e);
+      p.a.page_ids_out[to + e] = swap && e == ents - 1 ? fresh[k] : page;
+      p.a.pos_base_out[to + e] = __ldg(p.a.pos_base + from + e);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- page copies
+// A warp per (copy, pool, kv head): its filled slots are one contiguous stretch on both sides.
+constexpr int kCopyWarps = 8;
+struct CopyParams {
+  mepic_pages_copy_args_t a;
+  float* scales[2];
+  int n_kv_heads, page_size, num_pages, row_bytes;
+};
+__global__ void __launch_bounds__(kCopyWarps * 32) mepic_pages_copy_kernel(const __grid_constant__ CopyParams p) {
+  const int lane = threadIdx.x & 31;
+  const long long unit = static_cast<long long>(blockIdx.x) * kCopyWarps + (threadIdx.x >> 5);
+  int n = p.a.n_copies ? __ldg(p.a.n_copies) : p.a.max_copies;
+  if (n < 0 || n > p.a.max_copies) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.a.status, MEPIC_DEV_BAD_SLOT);
+    n = n < 0 ? 0 : p.a.max_copies;
+  }
+  const int units = 2 * p.n_kv_heads;
+  const long long i = unit / units;
+  if (i >= n) return;
+  const int u = static_cast<int>(unit - i * units), w = u / p.n_kv_heads, h = u - w * p.n_kv_heads;
+  const int src = __ldg(p.a.src + i), dst = __ldg(p.a.dst + i);
+  const int slots = p.a.slots ? min(max(__ldg(p.a.slots + i), 0), p.page_size) : p.page_size;
+  if (static_cast<unsigned>(src) >= static_cast<unsigned>(p.num_pages) || static_cast<unsigned>(dst) >= static_cast<unsigned>(p.num_pages)) {
+    if (lane == 0) atomicOr(p.a.status, MEPIC_DEV_BAD_PAGE);
+    return;
+  }
+  unsigned char* pool = static_cast<unsigned char*>(w ? p.a.v_pool : p.a.k_pool);
+  const size_t block = static_cast<size_t>(p.page_size) * p.row_bytes;
+  const uint4* from = reinterpret_cast<const uint4*>(pool + (static_cast<size_t>(src) * p.n_kv_heads + h) * block);
+  uint4* to = reinterpret_cast<uint4*>(pool + (static_cast<size_t>(dst) * p.n_kv_heads + h) * block);
+  const int chunks = slots * (p.row_bytes / 16);
+  for (int c0 = lane; c0 < chunks; c0 += 8 * 32) {
+    uint4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) if (c0 + 32 * k < chunks) v[k] = from[c0 + 32 * k];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) if (c0 + 32 * k < chunks) to[c0 + 32 * k] = v[k];
+  }
+  if (p.scales[w] && lane == 0) p.scales[w][static_cast<size_t>(dst) * p.n_kv_heads + h] = p.scales[w][static_cast<size_t>(src) * p.n_kv_heads + h];
+}
+
+// ---------------------------------------------------------------- host side
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+int shift_of(int page_size) {
+  int s = 0;
+  while ((1 << s) < page_size) ++s;
+  return s;
+}
+int32_t launched(const char* what, cudaError_t e, int n) {
+  if (e == cudaSuccess) e = cudaGetLastError();
+  if (e != cudaSuccess) { mepic_set_error("%s: launch: %s", what, cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  mepic_count_launches(n);
+  return MEPIC_OK;
+}
+size_t up16(size_t n) { return (n + 15) & ~static_cast<size_t>(15); }
+
+int elements_per_segment(int type) { return kSelThreads * kSelChunks * (type == MEPIC_LOGITS_FP32 ? 4 : 8); }
+// a row that begins inside a 16-byte piece may need one segment more
+int segments_of(long long vocab, int type) { return static_cast<int>((vocab + 7 + elements_per_segment(type) - 1) / elements_per_segment(type)); }
+bool select_shape_ok(int32_t groups, int32_t width, int32_t n_select, int32_t vocab) {
+  if (groups < 1 || width < 1 || width > MEPIC_BEAM_MAX_WIDTH) { mepic_set_error("beam_select: groups must be positive, width in 1..%d", MEPIC_BEAM_MAX_WIDTH); return false; }
+  if (n_select < 1 || n_select > MEPIC_BEAM_MAX_SELECT) { mepic_set_error("beam_select: n_select %d not in 1..%d", n_select, MEPIC_BEAM_MAX_SELECT); return false; }
+  if (vocab < 1 || vocab > (1 << 24)) { mepic_set_error("beam_select: vocab %d not in 1..2^24", vocab); return false; }
+  if (static_cast<long long>(groups) * width > 65535) { mepic_set_error("beam_select: more than 65535 beams"); return false; }
+  return true;
+}
+size_t select_bytes(int32_t groups, int32_t width, int32_t n_select, int segments) {
+  const size_t rows = static_cast<size_t>(groups) * width;
+  return up16(rows * segments * sizeof(SegmentSum)) + up16(rows * segments * n_select * sizeof(uint64_t));
+}
+
+// how the entries of a group are cut for the first launch of a fork: enough CTAs to fill the GPU, few enough counts to sum up
+void fork_cut(int groups, int table_stride, int* stretches, int* stretch) {
+  int n = std::max(1, std::min((table_stride + 511) / 512, 1024 / std::max(1, groups)));
+  int len = (table_stride + n - 1) / n;
+  len = (len + kForkThreads - 1) / kForkThreads * kForkThreads;
+  *stretch = len;
+  *stretches = (table_stride + len - 1) / len;
+}
+bool fork_shape_ok(int32_t groups, int32_t width_in, int32_t width_out, int32_t table_stride) {
+  if (groups < 1 || groups > MEPIC_STEP_MAX_BATCH) { mepic_set_error("beam_fork: groups %d not in 1..%d", groups, MEPIC_STEP_MAX_BATCH); return false; }
+  if (width_in < 1 || width_in > MEPIC_BEAM_MAX_WIDTH || width_out < 1 || width_out > MEPIC_BEAM_MAX_WIDTH) {
+    mepic_set_error("beam_fork: widths must be in 1..%d", MEPIC_BEAM_MAX_WIDTH); return false;
+  }
+  if (table_stride < 1 || table_stride > (1 << 24) || static_cast<long long>(groups) * std::max(width_in, width_out) * table_stride > 0x7fffffffLL) {
+    mepic_set_error("beam_fork: table_stride must be in 1..2^24 and the tables below 2^31 entries"); return false;
+  }
+  return true;
+}
+size_t fork_bytes(int32_t groups, int32_t width_in, int32_t table_stride) {
+  int n, len;
+  fork_cut(groups, table_stride, &n, &len);
+  return up16(static_cast<size_t>(groups) * n * 4) + up16(static_cast<size_t>(groups) * 4) + static_cast<size_t>(groups) * n * len * width_in * 4;
+}
+
+int32_t copy_call(const mepic_config_t* cfg, const mepic_pages_copy_args_t* a, float* k_scales, float* v_scales, bool fp8, void* cuda_stream) {
+  const char* what = fp8 ? "pages_copy_fp8" : "pages_copy";
+  if (!mepic_config_ok(cfg)) return MEPIC_E_INVAL;
+  if (!a) { mepic_set_error("%s: NULL argument", what); return MEPIC_E_INVAL; }
+  if (fp8 && cfg->head_dim != 128) { mepic_set_error("%s: head_dim %d: 8-bit pages are built for head_dim 128", what, cfg->head_dim); return MEPIC_E_INVAL; }
+  if (a->max_copies < 0) { mepic_set_error("%s: max_copies must not be negative", what); return MEPIC_E_INVAL; }
+  if (a->max_copies == 0) return MEPIC_OK;
+  if (!a->src || !a->dst || !a->k_pool || !a->v_pool || !a->status) { mepic_set_error("%s: NULL pointer argument", what); return MEPIC_E_INVAL; }
+  if (fp8 && (!k_scales || !v_scales)) { mepic_set_error("%s: NULL scale pointer", what); return MEPIC_E_INVAL; }
+  if (!aligned(a->k_pool, 16) || !aligned(a->v_pool, 16)) { mepic_set_error("%s: pools must be 16-byte aligned", what); return MEPIC_E_INVAL; }
+  CopyParams p;
+  p.a = *a;
+  p.scales[0] = k_scales; p.scales[1] = v_scales;
+  p.n_kv_heads = cfg->n_kv_heads; p.page_size = cfg->page_size; p.num_pages = cfg->num_pages;
+  p.row_bytes = cfg->head_dim * (fp8 ? 1 : 2);
+  const long long warps = 2LL * cfg->n_kv_heads * a->max_copies, ctas = (warps + kCopyWarps - 1) / kCopyWarps;
+  if (ctas > 0x7fffffffLL) { mepic_set_error("%s: max_copies %d is too large", what, a->max_copies); return MEPIC_E_INVAL; }
+  mepic_pages_copy_kernel<<<static_cast<unsigned>(ctas), kCopyWarps * 32, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
+  return launched(what, cudaSuccess, 1);
+}
+
+}  // namespace
+
+extern "C" size_t mepic_beam_select_workspace(int32_t groups, int32_t width, int32_t n_select, int32_t vocab) {
+  if (!select_shape_ok(groups, width, n_select, vocab)) return 0;
+  return select_bytes(groups, width, n_select, segments_of(vocab, MEPIC_LOGITS_FP32));       // enough for every type
+}
+
+extern "C" int32_t mepic_beam_select(const mepic_beam_select_args_t* a, void* cuda_stream) {
+  if (!a) { mepic_set_error("beam_select: NULL argument"); return MEPIC_E_INVAL; }
+  if (!select_shape_ok(a->groups, a->width, a->n_select, a->vocab)) return MEPIC_E_INVAL;
+  if (a->logits_type < MEPIC_LOGITS_BF16 || a->logits_type > MEPIC_LOGITS_FP32) { mepic_set_error("beam_select: logits_type %d is none of MEPIC_LOGITS_*", a->logits_type); return MEPIC_E_INVAL; }
+  if (!a->logits || !a->score || !a->parent || !a->token || !a->score_out || !a->done_out || !a->n_new || !a->workspace || !a->status) {
+    mepic_set_error("beam_select: NULL pointer argument"); return MEPIC_E_INVAL;
+  }
+  const long long stride = a->logits_stride ? a->logits_stride : a->vocab;
+  if (stride < a->vocab || stride > (1LL << 40)) { mepic_set_error("beam_select: logits_stride %lld must be 0 or at least vocab", static_cast<long long>(a->logits_stride)); return MEPIC_E_INVAL; }
+  if (a->eos_token < -1 || a->eos_token >= a->vocab || a->pad_token < 0 || a->pad_token >= a->vocab) {
+    mepic_set_error("beam_select: eos_token must be -1 or a token, pad_token a token of the vocabulary"); return MEPIC_E_INVAL;
+  }
+  if (!aligned(a->logits, a->logits_type == MEPIC_LOGITS_FP32 ? 4 : 2) || !aligned(a->workspace, 16)) {
+    mepic_set_error("beam_select: logits must be aligned to their type, the workspace to 16 bytes"); return MEPIC_E_INVAL;
+  }
+  if (a->score_out == a->score || (a->done && a->done_out == a->done)) { mepic_set_error("beam_select: outputs must not overlap inputs"); return MEPIC_E_INVAL; }
+  SelectParams p;
+  p.a = *a;
+  p.segments = segments_of(a->vocab, a->logits_type);
+  p.stride = stride;
+  const size_t need = select_bytes(a->groups, a->width, a->n_select, p.segments), rows = static_cast<size_t>(a->groups) * a->width;
+  if (a->workspace_bytes < need) { mepic_set_error("beam_select: workspace of %zu bytes, %zu needed", a->workspace_bytes, need); return MEPIC_E_INVAL; }
+  p.sums = static_cast<SegmentSum*>(a->workspace);
+  p.best = reinterpret_cast<uint64_t*>(static_cast<unsigned char*>(a->workspace) + up16(rows * p.segments * sizeof(SegmentSum)));
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const dim3 grid(p.segments, static_cast<unsigned>(rows));
+  if (a->logits_type == MEPIC_LOGITS_BF16) mepic_beam_segments<__nv_bfloat16><<<grid, kSelThreads, 0, st>>>(p);
+  else if (a->logits_type == MEPIC_LOGITS_FP16) mepic_beam_segments<__half><<<grid, kSelThreads, 0, st>>>(p);
+  else mepic_beam_segments<float><<<grid, kSelThreads, 0, st>>>(p);
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess) {
+    const size_t smem = static_cast<size_t>(a->width) * p.segments;
+    if (smem > 40 * 1024) e = cudaFuncSetAttribute(mepic_beam_join, cudaFuncAttributeMaxDynamicSharedMemorySize, kWidth * segments_of(1 << 24, MEPIC_LOGITS_FP32));
+    if (e == cudaSuccess) e = launch_dependent(mepic_beam_join, dim3(a->groups), dim3(kSelThreads), smem, st, p);
+  }
+  return launched("beam_select", e, 2);
+}
+
+extern "C" size_t mepic_beam_fork_workspace(int32_t groups, int32_t width_in, int32_t width_out, int32_t table_stride) {
+  if (!fork_shape_ok(groups, width_in, width_out, table_stride)) return 0;
+  return fork_bytes(groups, width_in, table_stride);
+}
+
+extern "C" int32_t mepic_beam_fork(const mepic_config_t* cfg, const mepic_beam_fork_args_t* a, void* cuda_stream) {
+  if (!mepic_config_ok(cfg)) return MEPIC_E_INVAL;
+  if (!a) { mepic_set_error("beam_fork: NULL argument"); return MEPIC_E_INVAL; }
+  if (!fork_shape_ok(a->groups, a->width_in, a->width_out, a->table_stride)) return MEPIC_E_INVAL;
+  if (a->n_reserve < 0) { mepic_set_error("beam_fork: n_reserve must not be negative"); return MEPIC_E_INVAL; }
+  if (!a->parent || !a->kv_len || !a->page_ids || !a->pos_base || !a->owned || (a->n_reserve > 0 && !a->reserve) || !a->reserve_used || !a->page_ids_out ||
+      !a->pos_base_out || !a->kv_len_out || !a->copy_src || !a->copy_dst || !a->copy_slots || !a->n_copies || !a->reserve_used_out || !a->workspace || !a->status) {
+    mepic_set_error("beam_fork: NULL pointer argument"); return MEPIC_E_INVAL;
+  }
+  if (a->page_ids_out == a->page_ids || a->pos_base_out == a->pos_base || a->kv_len_out == a->kv_len || a->reserve_used_out == a->reserve_used) {
+    mepic_set_error("beam_fork: outputs must not overlap inputs"); return MEPIC_E_INVAL;
+  }
+  if (!aligned(a->workspace, 16)) { mepic_set_error("beam_fork: the workspace must be 16-byte aligned"); return MEPIC_E_INVAL; }
+  const size_t need = fork_bytes(a->groups, a->width_in, a->table_stride);
+  if (a->workspace_bytes < need) { mepic_set_error("beam_fork: workspace of %zu bytes, %zu needed", a->workspace_bytes, need); return MEPIC_E_INVAL; }
+  ForkParams p;
+  p.a = *a;
+  p.page_shift = shift_of(cfg->page_size); p.num_pages = cfg->num_pages;
+  fork_cut(a->groups, a->table_stride, &p.stretches, &p.stretch);
+  unsigned char* ws = static_cast<unsigned char*>(a->workspace);
+  p.n_freed = reinterpret_cast<int*>(ws);
+  ws += up16(static_cast<size_t>(a->groups) * p.stretches * 4);
+  p.n_copies = reinterpret_cast<int*>(ws);
+  ws += up16(static_cast<size_t>(a->groups) * 4);
+  p.freed = reinterpret_cast<int*>(ws);
+  const size_t smem = (static_cast<size_t>(a->groups) * (p.stretches + 1) + 2) * sizeof(int);
+  cudaError_t e = cudaSuccess;
+  if (smem > 40 * 1024) e = cudaFuncSetAttribute(mepic_beam_fork_write, cudaFuncAttributeMaxDynamicSharedMemorySize, (2 * MEPIC_STEP_MAX_BATCH + 2) * static_cast<int>(sizeof(int)));
+  if (e != cudaSuccess) { mepic_set_error("beam_fork: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  mepic_beam_fork_count<<<dim3(a->groups, p.stretches), kForkThreads, 0, st>>>(p);
+  e = cudaGetLastError();
+  // entries of a group's tables: a few per thread
+  const int parts = std::max(1, std::min((a->table_stride + kForkThreads - 1) / kForkThreads, std::max(1, 592 / a->groups)));
+  if (e == cudaSuccess) e = launch_dependent(mepic_beam_fork_write, dim3(a->groups, parts), dim3(kForkThreads), smem, st, p);
+  return launched("beam_fork", e, 2);
+}
+
+extern "C" int32_t mepic_pages_copy(const mepic_config_t* cfg, const mepic_pages_copy_args_t* a, void* cuda_stream) {
+  return copy_call(cfg, a, nullptr, nullptr, false, cuda_stream);
+}
+extern "C" int32_t mepic_pages_copy_fp8(const mepic_config_t* cfg, const mepic_pages_copy_args_t* a, float* k_scales, float* v_scales,
+                                        void* cuda_stream) {
+  return copy_call(cfg, a, k_scales, v_scales, true, cuda_stream);
+}

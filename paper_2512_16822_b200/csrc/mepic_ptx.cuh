@@ -128,14 +128,18 @@ __device__ __forceinline__ void ldmatrix_b8_trans_x2(uint32_t (&r)[4], uint32_t 
 // Launches `kernel` so that it may become resident while the previous kernel on the stream is still running
 // (programmatic dependent launch); the kernel itself waits with griddepcontrol.wait before touching that kernel's output.
 template <typename Kernel, typename... Args>
-cudaError_t launch_dependent(Kernel kernel, dim3 grid, dim3 block, cudaStream_t stream, Args... args) {
+cudaError_t launch_dependent(Kernel kernel, dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = 0; cfg.stream = stream;
+  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+template <typename Kernel, typename... Args>
+cudaError_t launch_dependent(Kernel kernel, dim3 grid, dim3 block, cudaStream_t stream, Args... args) {
+  return launch_dependent(kernel, grid, block, size_t{0}, stream, args...);
 }
 
 }  // namespace mepic_dev

@@ -17,7 +17,9 @@ from . import (Config, Segment, Store, MEPIC_SEG_CHUNK, MEPIC_SEG_PROMPT, mepic_
                mepic_pages_quantize, mepic_attn_decode_fp8,
                mepic_attn_decode_workspace, mepic_attn_prefill, mepic_attn_prefill_fp8, mepic_attn_prefill_workspace,
                mepic_rope_table_fill, mepic_attn_tree_workspace, lib, _check, _AttnTreeArgsC, _TreeLayoutArgsC, _TreeAcceptArgsC,
-               _StepTablesArgsC, _RowsCommitArgsC)
+               _StepTablesArgsC, _RowsCommitArgsC, mepic_beam_select_workspace, mepic_beam_fork_workspace, mepic_beam_plan_bytes,
+               mepic_attn_beam_workspace, MEPIC_LOGITS_BF16, MEPIC_LOGITS_FP16, MEPIC_LOGITS_FP32, _BeamSelectArgsC, _BeamForkArgsC,
+               _PagesCopyArgsC, _BeamPlanArgsC, _AttnBeamArgsC)
 
 
 @dataclass
@@ -584,3 +586,163 @@ class RowsCommit(_StepCall):
 
     def run(self, stream=None) -> None:
         self._launch(stream)
+
+
+class BeamSelect(_StepCall):
+    """The best continuations over the beams and the vocabulary of each group.  logits: bf16, fp16 or fp32 [groups * width, vocab]
+    (rows may lie apart), scores: fp32 [groups, width], done: int32 [groups, width] or None (no beam is finished);
+    run() -> dict(parent, token, score, done, n_new), each [groups, n_select]."""
+
+    _TYPES = {torch.bfloat16: MEPIC_LOGITS_BF16, torch.float16: MEPIC_LOGITS_FP16, torch.float32: MEPIC_LOGITS_FP32}
+
+    def __init__(self, dev: Device, *, logits, scores, done=None, n_select: Optional[int] = None, eos_token: Optional[int] = None, pad_token: int = 0):
+        self.dev, d, i32 = dev, dev.device, torch.int32
+        _expect(scores, "scores", torch.float32, (-1, -1), d)
+        groups, width = scores.shape
+        n_select = width if n_select is None else n_select
+        if done is not None:
+            _expect(done, "done", i32, (groups, width), d)
+        if logits.dtype not in self._TYPES or not _lies_on(logits, d) or logits.dim() != 2 or logits.shape[0] != groups * width:
+            raise ValueError(f"logits: expected bfloat16, float16 or float32 ({groups * width}, vocab) on {d}, got {logits.dtype} {tuple(logits.shape)} on {logits.device}")
+        vocab = logits.shape[1]
+        if vocab > 1 and logits.stride(1) != 1:
+            raise ValueError("logits: the elements of a row must be packed")
+        if logits.shape[0] > 1 and logits.stride(0) < vocab:
+            raise ValueError(f"logits: rows must not share memory (row stride {logits.stride(0)}, a row has {vocab} elements)")
+        ws = mepic_beam_select_workspace(groups, width, n_select, vocab)
+        self.parent, self.token, self.done_out, self.n_new = (self._i32(groups, n_select) for _ in range(4))
+        self.score = torch.empty((groups, n_select), dtype=torch.float32, device=d)
+        self.workspace = torch.empty(ws, dtype=torch.uint8, device=d)
+        self._bind(dev, "mepic_beam_select",
+                   _BeamSelectArgsC(logits.data_ptr(), scores.data_ptr(), None if done is None else done.data_ptr(), self.parent.data_ptr(),
+                                    self.token.data_ptr(), self.score.data_ptr(), self.done_out.data_ptr(), self.n_new.data_ptr(),
+                                    self.workspace.data_ptr(), ws, dev.status.data_ptr(), logits.stride(0) if logits.shape[0] > 1 else vocab,
+                                    self._TYPES[logits.dtype], groups, width, n_select, vocab, -1 if eos_token is None else eos_token, pad_token),
+                   with_cfg=False, keep=(logits, scores, done))
+        self._result = dict(parent=self.parent, token=self.token, score=self.score, done=self.done_out, n_new=self.n_new)
+
+    def run(self, stream=None):
+        self._launch(stream)
+        return self._result
+
+
+class BeamFork(_StepCall):
+    """Block tables of the new beams from their parents.  parent: [groups, width_out]; kv_len, page_ids, pos_base: the rows of the
+    beams that are continued, [groups * width_in ...]; page_ids_out, pos_base_out: where the new rows go, [groups * width_out,
+    entries].  owned: uint8 [num_pages], 1 for the pages of the reserve.  Pages come out of ``reserve`` and go back to it, in place;
+    run() -> dict(kv_len, reserve_used, copy_src, copy_dst, copy_slots, n_copies): the last four are what PagesCopy takes."""
+
+    def __init__(self, dev: Device, *, parent, kv_len, page_ids, pos_base, page_ids_out, pos_base_out, owned, reserve, reserve_used):
+        self.dev, d, i32 = dev, dev.device, torch.int32
+        _expect(parent, "parent", i32, (-1, -1), d)
+        groups, width_out = parent.shape
+        _expect(kv_len, "kv_len", i32, (-1,), d)
+        rows_in, rows_out = kv_len.numel(), groups * width_out
+        if groups == 0 or rows_in == 0 or rows_in % groups:
+            raise ValueError(f"kv_len: {rows_in} beams are no whole number for each of {groups} groups")
+        _expect(page_ids, "page_ids", i32, (rows_in, -1), d), _expect(pos_base, "pos_base", i32, tuple(page_ids.shape), d)
+        stride = page_ids.shape[1]
+        _expect(page_ids_out, "page_ids_out", i32, (rows_out, stride), d), _expect(pos_base_out, "pos_base_out", i32, (rows_out, stride), d)
+        _expect(owned, "owned", torch.uint8, (dev.cfg.num_pages,), d)
+        _expect(reserve, "reserve", i32, (-1,), d), _expect(reserve_used, "reserve_used", i32, (1,), d)
+        read = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in (parent, kv_len, page_ids, pos_base, owned, reserve, reserve_used)]
+        for name, t in (("page_ids_out", page_ids_out), ("pos_base_out", pos_base_out)):
+            if any(t.data_ptr() < hi and lo < t.data_ptr() + 4 * t.numel() for lo, hi in read):
+                raise ValueError(f"{name}: must not overlap what the call reads")
+        ws = mepic_beam_fork_workspace(groups, rows_in // groups, width_out, stride)
+        self.reserve_used = reserve_used
+        self.kv_len_out, self.reserve_used_out, self.n_copies = self._i32(rows_out), self._i32(1), self._i32(1)
+        self.copy_src, self.copy_dst, self.copy_slots = (self._i32(rows_out) for _ in range(3))
+        self.workspace = torch.empty(ws, dtype=torch.uint8, device=d)
+        self._bind(dev, "mepic_beam_fork",
+                   _BeamForkArgsC(parent.data_ptr(), kv_len.data_ptr(), page_ids.data_ptr(), pos_base.data_ptr(), owned.data_ptr(),
+                                  reserve.data_ptr() or None, reserve_used.data_ptr(), page_ids_out.data_ptr(), pos_base_out.data_ptr(),
+                                  self.kv_len_out.data_ptr(), self.copy_src.data_ptr(), self.copy_dst.data_ptr(), self.copy_slots.data_ptr(),
+                                  self.n_copies.data_ptr(), self.reserve_used_out.data_ptr(), self.workspace.data_ptr(), ws,
+                                  dev.status.data_ptr(), stride, groups, rows_in // groups, width_out, reserve.numel()),
+                   keep=(parent, kv_len, page_ids, pos_base, owned, reserve, reserve_used, page_ids_out, pos_base_out))
+        self._result = dict(kv_len=self.kv_len_out, reserve_used=self.reserve_used_out, copy_src=self.copy_src, copy_dst=self.copy_dst,
+                            copy_slots=self.copy_slots, n_copies=self.n_copies)
+
+    def run(self, stream=None):
+        self._launch(stream)
+        return self._result
+
+
+class PagesCopy(_StepCall):
+    """Pages ``src`` to pages ``dst`` of the pools, K and V, the first ``slots`` of each (None: whole pages), ``n_copies`` of the
+    list (int32 [1] on the device; None: all).  ``pools``: 8-bit pools instead of the device's bf16 ones; scales come along."""
+
+    def __init__(self, dev: Device, *, src, dst, slots=None, n_copies=None, pools: Optional[Fp8Pools] = None):
+        d, i32 = dev.device, torch.int32
+        _expect(src, "src", i32, (-1,), d)
+        n = src.numel()
+        _expect(dst, "dst", i32, (n,), d)
+        if slots is not None:
+            _expect(slots, "slots", i32, (n,), d)
+        if n_copies is not None:
+            _expect(n_copies, "n_copies", i32, (1,), d)
+        k_pool, v_pool = _pools_for(dev, pools)
+        self._bind(dev, "mepic_pages_copy" if pools is None else "mepic_pages_copy_fp8",
+                   _PagesCopyArgsC(src.data_ptr(), dst.data_ptr(), None if slots is None else slots.data_ptr(),
+                                   None if n_copies is None else n_copies.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), dev.status.data_ptr(), n),
+                   extra=() if pools is None else (pools.k_scales.data_ptr(), pools.v_scales.data_ptr()),
+                   keep=(src, dst, slots, n_copies, k_pool, v_pool, pools))
+
+    def run(self, stream=None) -> None:
+        self._launch(stream)
+
+
+class BeamPlan(_StepCall):
+    """Which beams of a group share which page: run once a step, then the BeamBatch of every layer.  Rows group * width + w of the
+    tables are the beams of a group."""
+
+    def __init__(self, dev: Device, *, page_ids, pos_base, kv_len, width: int):
+        self.dev, d, i32 = dev, dev.device, torch.int32
+        _expect(kv_len, "kv_len", i32, (-1,), d)
+        rows = kv_len.numel()
+        _expect(page_ids, "page_ids", i32, (rows, -1), d), _expect(pos_base, "pos_base", i32, tuple(page_ids.shape), d)
+        if width < 1 or rows == 0 or rows % width:
+            raise ValueError(f"width: {rows} rows are no whole number of groups of {width} beams")
+        self.groups, self.width, self.stride = rows // width, width, page_ids.shape[1]
+        n = mepic_beam_plan_bytes(dev.cfg, self.groups, width, self.stride)
+        self.plan = torch.zeros(n, dtype=torch.uint8, device=d)
+        self._bind(dev, "mepic_beam_plan",
+                   _BeamPlanArgsC(page_ids.data_ptr(), pos_base.data_ptr(), kv_len.data_ptr(), self.plan.data_ptr(), n, dev.status.data_ptr(),
+                                  self.stride, self.groups, width),
+                   keep=(page_ids, pos_base, kv_len))
+
+    def run(self, stream=None) -> None:
+        self._launch(stream)
+
+
+class BeamBatch(_StepCall):
+    """Attention of every beam's newest token (its K/V is in the cache already) under a plan.  q: bf16 [rows, heads, head_dim], rows
+    may lie apart; q_pos: int32 [rows].  ``dev`` may be another than the plan's (another layer's pools) of the same configuration.
+    ``pools``: 8-bit pools to read instead of the device's bf16 ones."""
+
+    def __init__(self, dev: Device, *, q, q_pos, plan: BeamPlan, pools: Optional[Fp8Pools] = None):
+        cfg, d = dev.cfg, dev.device
+        rows = plan.groups * plan.width
+        if plan.dev.cfg != cfg or plan.dev.device != d:
+            raise ValueError("plan: made for another configuration or device")
+        q_stride = _row_stride(q, "q", cfg.n_q_heads, cfg.head_dim, d)
+        if q.shape[0] != rows:
+            raise ValueError(f"q: {q.shape[0]} rows, the plan has {rows}")
+        _expect(q_pos, "q_pos", torch.int32, (rows,), d)
+        k_pool, v_pool = _pools_for(dev, pools)
+        with torch.cuda.device(d):
+            ws = mepic_attn_beam_workspace(cfg, plan.groups, plan.width)
+        self.out = torch.empty((rows, cfg.n_q_heads, cfg.head_dim), dtype=torch.bfloat16, device=d)
+        self.workspace = torch.empty(ws, dtype=torch.uint8, device=d)
+        args = _AttnBeamArgsC(q.data_ptr(), q_pos.data_ptr(), plan.plan.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), dev.rope.data_ptr(),
+                              self.out.data_ptr(), self.workspace.data_ptr(), ws, dev.status.data_ptr(), plan.stride, plan.groups, plan.width,
+                              q_stride, 0.0)
+        self._bind(dev, "mepic_attn_beam" if pools is None else "mepic_attn_beam_fp8", args,
+                   extra=() if pools is None else (pools.k_scales.data_ptr(), pools.v_scales.data_ptr()),
+                   keep=(q, q_pos, plan.plan, k_pool, v_pool, pools))
+
+    def run(self, sm_scale: float, stream=None) -> torch.Tensor:
+        self._args.sm_scale = sm_scale
+        self._launch(stream)
+        return self.out
