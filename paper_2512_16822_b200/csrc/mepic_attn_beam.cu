@@ -37,8 +37,9 @@ using namespace mepic_dev;
 constexpr int kTile = 16;            // keys per staged tile
 constexpr int kStages = 2;
 constexpr int kMinPiece = 4;         // the line is never cut into pieces shorter than this many tiles
-constexpr int kAngles = 64;          // positions of the shared-memory table
+constexpr int kAngles = 128;         // positions of the shared-memory table
 constexpr int kMaxColumns = 32;      // columns of a column block
+constexpr float kSmallScale = 0x1p-100f;      // 8-bit pages: V scales are taken relative to the largest met, at least to this one
 constexpr int kSeg = 256;            // table entries a CTA of the plan looks at
 
 // ---------------------------------------------------------------- the plan's layout
@@ -242,11 +243,22 @@ __device__ __forceinline__ Unit unit_at(const BeamParams& p, long long x, int la
 }
 
 template <int D, bool FP8> constexpr int stage_bytes = 2 * kTile * D * (FP8 ? 1 : 2);
-// per position of the table: 64 (cos, sin) pairs, fp32 (c0, c1, s0, s1 of two pairs) or fp16 (the same four)
-template <int D, bool FP8> constexpr int angle_bytes = D / 2 * (FP8 ? 4 : 8);
+// Per position of the table, for every two pairs of dims: (c, c', s, s') and, for fp32, (-s, -s') behind all of those.
+template <int D, bool FP8> constexpr int angle_bytes = D / 2 * (FP8 ? 4 : 12);
 template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (kStages * stage_bytes<D, FP8> + 128) + kAngles * angle_bytes<D, FP8> + 1024;
 
 // NT: tiles of 8 columns; W: warps of a CTA.
+__device__ __forceinline__ float4 lds128(uint32_t addr) {
+  float4 v;
+  asm("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ float2 lds64(uint32_t addr) {
+  float2 v;
+  asm("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
+  return v;
+}
+
 template <int D, int NT, bool FP8, int W>
 __global__ void __launch_bounds__(W * 32, 1)
 mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
@@ -261,13 +273,13 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   extern __shared__ unsigned char smem_dyn[];
   // 1024-byte alignment: the swizzle pattern is a function of the address bits
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~static_cast<uintptr_t>(1023));
-  const int lane = threadIdx.x & 31, wic = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, wic = __shfl_sync(kFull, static_cast<int>(threadIdx.x >> 5), 0);      // (known to be the same in a warp)
   unsigned char* stage0 = smem + static_cast<size_t>(wic) * kStages * kStageBytes;
   unsigned char* angles = smem + static_cast<size_t>(W) * kStages * kStageBytes;
   unsigned char* misc = angles + kAngles * kAngleBytes + wic * 128;
   uint64_t* bars = reinterpret_cast<uint64_t*>(misc);                          // kStages x 8 bytes
-  volatile int* meta = reinterpret_cast<volatile int*>(misc + 16);             // per stage: position, beams, valid slots of the tile
-  volatile float* scl = reinterpret_cast<volatile float*>(misc + 16 + kStages * 16);      // per stage: K and V scale of the page
+  const uint32_t meta = smem_u32(misc + 16);             // per stage: position, beams, valid slots of the tile
+  const uint32_t scl = meta + kStages * 16;              // per stage: K and V scale of the page
 
   const int g = lane >> 2, t = lane & 3;     // fragment row (key, dim, or column of Q) and column group
   // 8-bit pages: ldmatrix on bytes hands a lane four consecutive dims of a key, its transposing form four consecutive keys of a
@@ -280,32 +292,17 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   const Cut cut = cut_of_line(p);
   if (static_cast<long long>(blockIdx.x) * W * cut.piece >= cut.total) return;
 
-  // ---- the table of angles: for position a and pairs 2u, 2u+1 the quadruple (c, c', s, s'), rows swizzled so that the eight lanes
-  // that load together (two keys, four column groups) meet all banks
-  for (int i = threadIdx.x; i < kAngles * (D / 4); i += W * 32) {
-    const int a = i / (D / 4), u = i % (D / 4);
-    const float4 cs = __ldg(reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(min(a, p.max_position)) * D + 4 * u));      // c, s, c', s'
-    if constexpr (FP8) {
-      // a key's row and the next key's row meet in the same 8-lane phase: 32 bytes a lane pair of quadruples
-      unsigned char* at = angles + a * kAngleBytes + ((u * 8) ^ ((a & 1) << 6));
-      *reinterpret_cast<uint2*>(at) = make_uint2(pack_f16x2(cs.x, cs.z), pack_f16x2(cs.y, cs.w));
-    } else {
-      unsigned char* at = angles + a * kAngleBytes + ((u * 16) ^ ((a & 1) << 6));
-      *reinterpret_cast<float4*>(at) = make_float4(cs.x, cs.z, cs.y, cs.w);
-    }
-  }
   if (lane == 0) {
 #pragma unroll
     for (int s = 0; s < kStages; ++s) mbar_init(smem_u32(&bars[s]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  __syncthreads();
+  __syncwarp();
 
   const long long w = static_cast<long long>(blockIdx.x) * W + wic;
-  const long long x0 = w * cut.piece;
-  if (x0 >= cut.total) return;
-  const long long x1 = min(x0 + cut.piece, cut.total);
+  const int n_tiles = static_cast<int>(max(min(cut.piece, cut.total - w * cut.piece), 0ll));      // 0: the line ends before this warp
+  const long long x0 = min(w * cut.piece, cut.total - 1);
   const int G = p.group_size, tpp_mask = (1 << p.log2_tpp) - 1;
 
   // ---- producer: the next tile to stage
@@ -319,12 +316,12 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     pt = static_cast<int>(in_head) & tpp_mask;
   }
   Unit cu = pu;                                                        // consumer: its unit, and the unit's tiles still to come
-  long long c_left = (static_cast<long long>(cu.r1 - pr) << p.log2_tpp) - pt;
+  int c_left = static_cast<int>(min((static_cast<long long>(cu.r1 - pr) << p.log2_tpp) - pt, static_cast<long long>(INT_MAX)));
   int pseg = pu.block * p.segments;                                    // segment of the producer's record
   int win0 = 0, win_n = 0;                                             // records win0 .. win0 + win_n - 1, one per lane
   int4 win = make_int4(0, 0, 0, 0);
   float win_ks = 0.f, win_vs = 0.f;
-  long long issued = x0;
+  int issued = 0;                                                      // tiles handed to the ring
   auto issue = [&](int stage) {
     if (pr < win0 || pr >= win0 + win_n) {
       while (pseg + 1 < p.groups * p.blocks * p.segments && __ldg(p.sums + pseg + 1) <= pr) ++pseg;
@@ -346,19 +343,21 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     if constexpr (FP8) { ks = __shfl_sync(kFull, win_ks, src); vs = __shfl_sync(kFull, win_vs, src); }
     const int n_valid = min(slots - pt * kTile, kTile);
     if (lane == 0) {
-      meta[stage * 4] = pos + pt * kTile; meta[stage * 4 + 1] = beams; meta[stage * 4 + 2] = n_valid;
-      if constexpr (FP8) { scl[stage * 2] = ks; scl[stage * 2 + 1] = vs; }
-      if (!(w == 0 && issued - x0 == p.skip_tile)) {        // (test hook: one copy that never comes)
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%3};" ::"r"(meta + stage * 16), "r"(pos + pt * kTile), "r"(beams), "r"(n_valid) : "memory");
+      if constexpr (FP8) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(scl + stage * 8), "f"(ks), "f"(vs) : "memory");
+      if (!(w == 0 && issued == p.skip_tile)) {        // (test hook: one copy that never comes)
         const uint32_t bar = smem_u32(&bars[stage]), dst = smem_u32(stage0 + stage * kStageBytes);
         if (n_valid <= 0) {
           mbar_expect_tx(bar, 0);                           // a tile of the page that holds no slot
         } else {
           const int y = (page * p.n_kv_heads + pu.head) * p.page_size + pt * kTile;      // row of the pool viewed as [rows][D]
           mbar_expect_tx(bar, kStageBytes);
-#pragma unroll
-          for (int nb = 0; nb < KB; ++nb) {
-            tma_load_2d(dst + nb * kBlockBytes, &map_k, nb * 64, y, bar);
-            tma_load_2d(dst + (KB + nb) * kBlockBytes, &map_v, nb * 64, y, bar);
+          if constexpr (FP8) {
+            tma_load_2d(dst, &map_k, 0, y, bar);
+            tma_load_2d(dst + kBlockBytes, &map_v, 0, y, bar);
+          } else {
+            tma_load_3d(dst, &map_k, 0, y, 0, bar);
+            tma_load_3d(dst + NB * kBlockBytes, &map_v, 0, y, 0, bar);
           }
         }
       }
@@ -372,18 +371,38 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     pseg = min(pu.block, p.groups * p.blocks - 1) * p.segments;
     win_n = 0;                                              // another head: its scales, another block: its records
   };
-  for (int s = 0; s < kStages && issued < x1; ++s) issue(s);
-  __syncwarp();
+  for (int s = 0; s < kStages && issued < n_tiles; ++s) issue(s);
+
+  // positions the table has to reach: those of a piece, where it is short
+  const int span = static_cast<int>(min(static_cast<long long>(kAngles), max(cut.piece, 1ll) * kTile));
+  // ---- the table of angles: for position a and pairs 2u, 2u+1 the quadruple (c, c', s, s'), rows swizzled so that the eight lanes
+  // that load together (two keys, four column groups) meet all banks
+  for (int i = threadIdx.x; i < span * (D / 4); i += W * 32) {
+    const int a = i / (D / 4), u = i % (D / 4);
+    const float4 cs = __ldg(reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(min(a, p.max_position)) * D + 4 * u));      // c, s, c', s'
+    if constexpr (FP8) {
+      unsigned char* at = angles + a * kAngleBytes + ((u * 8) ^ ((a & 1) << 6));
+      *reinterpret_cast<uint2*>(at) = make_uint2(pack_f16x2(cs.x, cs.z), pack_f16x2(cs.y, cs.w));
+    } else {
+      unsigned char* at = angles + a * kAngleBytes;
+      *reinterpret_cast<float4*>(at + ((u * 16) ^ ((a & 1) << 6))) = make_float4(cs.x, cs.z, cs.y, cs.w);
+      *reinterpret_cast<float2*>(at + D * 4 + ((u * 8) ^ ((a & 3) << 5))) = make_float2(-cs.y, -cs.w);
+    }
+  }
+  __syncthreads();
+  const uint32_t angles_addr = smem_u32(angles);
 
   // ---- state of the unit
   int u_block = -1, u_head = -1;
   unsigned all_beams = 0;
   int anchor = INT_MIN;
   unsigned see[NT][2];                       // beam bit of the columns 8 nt + 2 t, + 1 of this lane (0: no such column)
+  int q_at[NT];                              // position and un-rotated query of column 8 nt + g
+  const uint16_t* q_src[NT];
   uint32_t qf[NT][KS][2];                    // B fragments of Q'^T, column 8 nt + g
   float m_run[NT][2], l_run[NT][2];          // reference and this lane's share of the sum of columns 2 t, 2 t + 1
   float acc[NT][NV][4];                      // O^T: [dim g: column 2t, 2t+1 | dim g + 8: the same]
-  float v_ref = 0.f;                         // 8-bit pages: acc is in units of this V scale times 2^-12
+  float v_ref = kSmallScale, v_inv = 0x1p12f / kSmallScale;      // 8-bit pages: acc is in units of v_ref 2^-12; 2^12 / v_ref
 
   auto flush = [&]() {
     if (u_block < 0) return;
@@ -405,43 +424,65 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         }
       }
   };
-  // The queries of the unit, rotated by their position less the anchor.
+  // The queries of the unit, rotated by their position less the anchor.  One table row does for all columns where their positions are
+  // the same, as they are but for beams that have ended.
   auto rotate_queries = [&]() {
+    const float* turn[NT];
+    float sign[NT];
+    const int q0 = __shfl_sync(kFull, q_at[0], 0);
+    bool same = true;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int col = 8 * nt + g, beam = col / G, group = u_block / p.blocks, at = (u_block - group * p.blocks) * p.beams + beam;
-      const bool live = beam < p.beams && at < p.width;
-      const int row = live ? group * p.width + at : 0;
-      const int rel = live ? __ldg(p.q_pos + row) - anchor : 0;
+      const int rel = q_at[nt] - anchor;
       int arel = rel < 0 ? -rel : rel;
       if (static_cast<unsigned>(arel) > static_cast<unsigned>(p.max_position)) { atomicOr(p.status, MEPIC_DEV_BAD_POSITION); arel = p.max_position; }
-      const float sc = live ? p.scale_log2 : 0.f, sn = rel < 0 ? -sc : sc;
-      const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + static_cast<size_t>(row) * p.q_stride + (static_cast<size_t>(u_head) * G + (live ? col - beam * G : 0)) * D);
-      const float* turn = p.rope + static_cast<size_t>(arel) * D;
+      turn[nt] = p.rope + static_cast<size_t>(arel) * D;
+      sign[nt] = rel < 0 ? -1.f : 1.f;
+      same = same && q_at[nt] == q0;
+    }
+    auto rotate = [&](int nt, int j, int r, const float4& cs, float sn) {
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(q_src[nt] + pair_of(j, r));
+      const float2 lo = bf16x2_to_float2(__ldg(src)), hi = bf16x2_to_float2(__ldg(src + D / 4));
+      const float2 c = make_float2(cs.x, cs.z), sp = make_float2(cs.y * sn, cs.w * sn), sm = make_float2(-sp.x, -sp.y);
+      const float2 a = fma2(lo, c, mul2(hi, sm)), b = fma2(lo, sp, mul2(hi, c));
+      qf[nt][j][r] = FP8 ? pack_f16x2(a.x, a.y) : pack_bf16x2(a.x, a.y);
+      qf[nt][j + KH][r] = FP8 ? pack_f16x2(b.x, b.y) : pack_bf16x2(b.x, b.y);
+    };
+    if (__all_sync(kFull, same)) {
 #pragma unroll
       for (int j = 0; j < KH; ++j)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const int pair = pair_of(j, r);
-          const float2 lo = bf16x2_to_float2(__ldg(src + pair / 2)), hi = bf16x2_to_float2(__ldg(src + (pair + D / 2) / 2));
-          const float4 cs = __ldg(reinterpret_cast<const float4*>(turn + 2 * pair));
-          const float c0 = cs.x * sc, s0 = cs.y * sn, c1 = cs.z * sc, s1 = cs.w * sn;
-          const float a0 = lo.x * c0 - hi.x * s0, a1 = lo.y * c1 - hi.y * s1, b0 = lo.x * s0 + hi.x * c0, b1 = lo.y * s1 + hi.y * c1;
-          qf[nt][j][r] = FP8 ? pack_f16x2(a0, a1) : pack_bf16x2(a0, a1);
-          qf[nt][j + KH][r] = FP8 ? pack_f16x2(b0, b1) : pack_bf16x2(b0, b1);
+          const float4 cs = __ldg(reinterpret_cast<const float4*>(turn[0] + 2 * pair_of(j, r)));
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) rotate(nt, j, r, cs, sign[0]);
         }
+    } else {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < KH; ++j)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) rotate(nt, j, r, __ldg(reinterpret_cast<const float4*>(turn[nt] + 2 * pair_of(j, r))), sign[nt]);
     }
   };
 
   int stage = 0;
   uint32_t parity = 0;
-  for (long long x = x0; x < x1; ++x) {
+  for (int it = 0; it < n_tiles; ++it) {
     if (cu.block != u_block || cu.head != u_head) {
       flush();
       u_block = cu.block; u_head = cu.head;
-      anchor = INT_MIN; v_ref = 0.f;
+      anchor = INT_MIN; v_ref = kSmallScale; v_inv = 0x1p12f / kSmallScale;
       const int first = (u_block % p.blocks) * p.beams, nb = min(p.beams, p.width - first);
       all_beams = nb == 32 ? ~0u : (1u << nb) - 1;
+      const int row0 = u_block / p.blocks * p.width + first;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {                       // a column that is none repeats the first: nobody looks at it
+        const int col = 8 * nt + g < nb * G ? 8 * nt + g : 0, row = row0 + col / G;
+        q_at[nt] = __ldg(p.q_pos + row);
+        q_src[nt] = p.q + static_cast<size_t>(row) * p.q_stride + (static_cast<size_t>(u_head) * G + col % G) * D;
+      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -454,199 +495,217 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         for (int db = 0; db < NV; ++db) { acc[nt][db][0] = 0.f; acc[nt][db][1] = 0.f; acc[nt][db][2] = 0.f; acc[nt][db][3] = 0.f; }
       }
     }
-    const int pos = meta[stage * 4], n_valid = meta[stage * 4 + 2];
-    const unsigned beams = static_cast<unsigned>(meta[stage * 4 + 1]);
-    if (n_valid > 0 && (anchor == INT_MIN || static_cast<unsigned>(pos - anchor) > kAngles - kTile)) { anchor = pos; rotate_queries(); }
+    int pos, n_valid, unused;
+    unsigned beams;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(pos), "=r"(beams), "=r"(n_valid), "=r"(unused) : "r"(meta + stage * 16) : "memory");
+    if (anchor == INT_MIN || static_cast<unsigned>(pos - anchor) > static_cast<unsigned>(span - kTile)) { anchor = pos; rotate_queries(); }
     if (!mbar_wait_bounded(smem_u32(&bars[stage]), parity, p.spin_limit)) {
       // Give the copies still in flight a last bounded chance to land, then leave cleanly.
       if (lane == 0) atomicOr(p.status, MEPIC_DEV_WAIT_EXPIRED);
       for (int s = 0; s < kStages; ++s) mbar_wait_bounded(smem_u32(&bars[s]), s == stage ? parity : (s < stage ? parity ^ 1u : parity), p.spin_limit);
       return;
     }
-    if (n_valid > 0) {
-      const uint32_t ks_addr = smem_u32(stage0 + stage * kStageBytes), vs_addr = ks_addr + KB * kBlockBytes;
-      // slots past the filled ones may hold anything: their P is 0, but 0 x NaN is NaN, so V must be finite there
-      if (n_valid < kTile) {
-        for (int idx = n_valid * 8 * KB + lane; idx < kTile * 8 * KB; idx += 32) {
-          const int key = idx / (8 * KB), chk = idx % (8 * KB);
-          const uint32_t a = vs_addr + (chk / 8) * kBlockBytes + key * 128 + (((chk % 8) ^ (key & 7)) << 4);
-          asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0) : "memory");
-        }
-        // these generic-proxy stores must be ordered before the TMA (async proxy) write that refills this stage
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
+    const uint32_t ks_addr = smem_u32(stage0 + stage * kStageBytes), vs_addr = ks_addr + KB * kBlockBytes;
+    // slots past the filled ones may hold anything: their P is 0, but 0 x NaN is NaN, so V must be finite there
+    if (n_valid < kTile) {
+      for (int idx = max(n_valid, 0) * 8 * KB + lane; idx < kTile * 8 * KB; idx += 32) {
+        const int key = idx / (8 * KB), chk = idx % (8 * KB);
+        const uint32_t a = vs_addr + (chk / 8) * kBlockBytes + key * 128 + (((chk % 8) ^ (key & 7)) << 4);
+        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0) : "memory");
       }
-      // ---- S^T = K' Q'^T
-      float sc[NT][4];
+      // these generic-proxy stores must be ordered before the TMA (async proxy) write that refills this stage
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+    }
+    // ---- S^T = K' Q'^T
+    float sc[NT][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) { sc[nt][0] = 0.f; sc[nt][1] = 0.f; sc[nt][2] = 0.f; sc[nt][3] = 0.f; }
-      const int offA = pos - anchor + keyA, offB = pos - anchor + keyB;
+    for (int nt = 0; nt < NT; ++nt) { sc[nt][0] = 0.f; sc[nt][1] = 0.f; sc[nt][2] = 0.f; sc[nt][3] = 0.f; }
+    const int offA = pos - anchor + keyA, offB = pos - anchor + keyB;
+    const uint32_t row_a = angles_addr + offA * kAngleBytes, row_b = angles_addr + offB * kAngleBytes;
+    uint32_t cs_a[2], cs_b[2], ns_a[4], ns_b[4];      // addresses of the lane's quadruples (column half r) and of its negated sines
+    if constexpr (!FP8) {
 #pragma unroll
-      for (int j = 0; j < KH; ++j) {
-        uint32_t lo[4], hi[4];      // A fragments of k-steps j, j + KH: [key A, key B | key A, key B (second column half)]
-        if constexpr (FP8) {
-          uint32_t raw[4];          // [key A, key B of chunk j | of chunk j + KH], four dims each
-          {
-            const int mi = lane >> 3, rr = lane & 7, key = 4 * (rr >> 1) + (rr & 1) + 2 * (mi & 1), chk = j + KH * (mi >> 1);
-            ldmatrix_x4(raw, ks_addr + key * 128 + ((chk ^ (key & 7)) << 4));
-          }
-          e4m3x4_to_f16x2x2(raw[0], lo[0], lo[2]);
-          e4m3x4_to_f16x2x2(raw[1], lo[1], lo[3]);
-          e4m3x4_to_f16x2x2(raw[2], hi[0], hi[2]);
-          e4m3x4_to_f16x2x2(raw[3], hi[1], hi[3]);
-          const int u8 = (16 * j + 4 * t) * 4;      // byte of the quadruple of pairs 16 j + 4 t
-          const uint4 ca = *reinterpret_cast<const uint4*>(angles + offA * kAngleBytes + (u8 ^ ((offA & 1) << 6)));
-          const uint4 cb = *reinterpret_cast<const uint4*>(angles + offB * kAngleBytes + (u8 ^ ((offB & 1) << 6)));
-          const uint32_t cc[4] = {ca.x, cb.x, ca.z, cb.z}, ss[4] = {ca.y, cb.y, ca.w, cb.w};
-#pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            const uint32_t a = lo[f], b = hi[f];
-            lo[f] = f16x2_fma(a, cc[f], f16x2_neg(f16x2_mul(b, ss[f])));
-            hi[f] = f16x2_fma(a, ss[f], f16x2_mul(b, cc[f]));
-          }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            mma_f16(sc[nt], lo[0], lo[1], lo[2], lo[3], qf[nt][j][0], qf[nt][j][1]);
-            mma_f16(sc[nt], hi[0], hi[1], hi[2], hi[3], qf[nt][j + KH][0], qf[nt][j + KH][1]);
-          }
-        } else {
-          {
-            // lane -> (matrix mi = lane / 8, row = lane % 8): key = 8 (mi & 1) + row, 16-byte chunk 2 j + (mi >> 1)
-            const int mi = lane >> 3, key = ((mi & 1) << 3) + (lane & 7);
-            const int cl = 2 * j + (mi >> 1), chh = 2 * (j + KH) + (mi >> 1);
-            ldmatrix_x4(lo, ks_addr + (cl / 8) * kBlockBytes + key * 128 + (((cl % 8) ^ (key & 7)) << 4));
-            ldmatrix_x4(hi, ks_addr + (chh / 8) * kBlockBytes + key * 128 + (((chh % 8) ^ (key & 7)) << 4));
-          }
-#pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            const int off = (f & 1) ? offB : offA, r = f >> 1;
-            const float4 cs = *reinterpret_cast<const float4*>(angles + off * kAngleBytes + (((16 * j + 2 * t + 8 * r) * 8) ^ ((off & 1) << 6)));
-            const float2 c = make_float2(cs.x, cs.y), s = make_float2(cs.z, cs.w), ns = make_float2(-cs.z, -cs.w);
-            const float2 a = bf16x2_to_float2(lo[f]), b = bf16x2_to_float2(hi[f]);
-            const float2 x = fma2(a, c, mul2(b, ns)), y = fma2(a, s, mul2(b, c));
-            lo[f] = pack_bf16x2(x.x, x.y); hi[f] = pack_bf16x2(y.x, y.y);
-          }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            mma_bf16(sc[nt], lo[0], lo[1], lo[2], lo[3], qf[nt][j][0], qf[nt][j][1]);
-            mma_bf16(sc[nt], hi[0], hi[1], hi[2], hi[3], qf[nt][j + KH][0], qf[nt][j + KH][1]);
-          }
-        }
+      for (int r = 0; r < 2; ++r) {
+        cs_a[r] = row_a + ((16 * t + 64 * r) ^ ((offA & 1) << 6));
+        cs_b[r] = row_b + ((16 * t + 64 * r) ^ ((offB & 1) << 6));
       }
-      // ---- online softmax (log2 domain): keys A (0, 1) and B (2, 3) of columns 2t (0, 2) and 2t + 1 (1, 3)
-      const bool some = (beams & all_beams) != all_beams;
-      float v_scale = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        ns_a[k] = row_a + D * 4 + ((8 * t + 32 * k) ^ ((offA & 3) << 5));
+        ns_b[k] = row_b + D * 4 + ((8 * t + 32 * k) ^ ((offB & 3) << 5));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < KH; ++j) {
+      uint32_t lo[4], hi[4];      // A fragments of k-steps j, j + KH: [key A, key B | key A, key B (second column half)]
       if constexpr (FP8) {
-        const float k_scale = scl[stage * 2], vs = scl[stage * 2 + 1];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) { sc[nt][0] *= k_scale; sc[nt][1] *= k_scale; sc[nt][2] *= k_scale; sc[nt][3] *= k_scale; }
-        // P carries the page's V scale relative to the largest met so far, and 2^12 so that small weights stay normal in fp16
-        const bool finite = vs <= FLT_MAX;      // a page's scale may be infinite or NaN: that is for the columns that see the page, not for the others
-        if (finite && vs > v_ref) {
-          const float f = v_ref / vs;
-          v_ref = vs;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int db = 0; db < NV; ++db) { acc[nt][db][0] *= f; acc[nt][db][1] *= f; acc[nt][db][2] *= f; acc[nt][db][3] *= f; }
+        uint32_t raw[4];          // [key A, key B of chunk j | of chunk j + KH], four dims each
+        {
+          const int mi = lane >> 3, rr = lane & 7, key = 4 * (rr >> 1) + (rr & 1) + 2 * (mi & 1), chk = j + KH * (mi >> 1);
+          ldmatrix_x4(raw, ks_addr + key * 128 + ((chk ^ (key & 7)) << 4));
         }
-        v_scale = !finite ? __int_as_float(0x7fffffff) : v_ref > 0.f ? vs / v_ref * 0x1p12f : 0.f;
-      }
-      if (n_valid < kTile) {
+        e4m3x4_to_f16x2x2(raw[0], lo[0], lo[2]);
+        e4m3x4_to_f16x2x2(raw[1], lo[1], lo[3]);
+        e4m3x4_to_f16x2x2(raw[2], hi[0], hi[2]);
+        e4m3x4_to_f16x2x2(raw[3], hi[1], hi[3]);
+        const int u8 = (16 * j + 4 * t) * 4;      // byte of the quadruple of pairs 16 j + 4 t
+        const float4 ca = lds128(row_a + (u8 ^ ((offA & 1) << 6))), cb = lds128(row_b + (u8 ^ ((offB & 1) << 6)));
+        const uint32_t cc[4] = {__float_as_uint(ca.x), __float_as_uint(cb.x), __float_as_uint(ca.z), __float_as_uint(cb.z)};
+        const uint32_t ss[4] = {__float_as_uint(ca.y), __float_as_uint(cb.y), __float_as_uint(ca.w), __float_as_uint(cb.w)};
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+          const uint32_t a = lo[f], b = hi[f];
+          lo[f] = f16x2_fma(a, cc[f], f16x2_neg(f16x2_mul(b, ss[f])));
+          hi[f] = f16x2_fma(a, ss[f], f16x2_mul(b, cc[f]));
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          if (keyA >= n_valid) { sc[nt][0] = -INFINITY; sc[nt][1] = -INFINITY; }
-          if (keyB >= n_valid) { sc[nt][2] = -INFINITY; sc[nt][3] = -INFINITY; }
-        }
-      }
-      if (some) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          if (!(see[nt][0] & beams)) { sc[nt][0] = -INFINITY; sc[nt][2] = -INFINITY; }
-          if (!(see[nt][1] & beams)) { sc[nt][1] = -INFINITY; sc[nt][3] = -INFINITY; }
-        }
-      }
-      bool higher = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) higher = higher || fmaxf(sc[nt][0], sc[nt][2]) > m_run[nt][0] || fmaxf(sc[nt][1], sc[nt][3]) > m_run[nt][1];
-      // the references move only if some lane saw a larger score
-      if (__any_sync(kFull, higher)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float mx0 = fmaxf(sc[nt][0], sc[nt][2]), mx1 = fmaxf(sc[nt][1], sc[nt][3]);
-#pragma unroll
-          for (int o = 4; o < 32; o <<= 1) { mx0 = fmaxf(mx0, __shfl_xor_sync(kFull, mx0, o)); mx1 = fmaxf(mx1, __shfl_xor_sync(kFull, mx1, o)); }
-          const float n0 = fmaxf(m_run[nt][0], mx0), n1 = fmaxf(m_run[nt][1], mx1);
-          const float a0 = ex2(m_run[nt][0] - n0), a1 = ex2(m_run[nt][1] - n1);
-          m_run[nt][0] = n0; m_run[nt][1] = n1;
-          l_run[nt][0] *= a0; l_run[nt][1] *= a1;
-#pragma unroll
-          for (int db = 0; db < NV; ++db) { acc[nt][db][0] *= a0; acc[nt][db][1] *= a1; acc[nt][db][2] *= a0; acc[nt][db][3] *= a1; }
-        }
-      }
-      uint32_t pb[NT][2];                    // B fragments of P^T: the transposes of the two 8 x 8 blocks (key row, columns)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p0 = ex2(sc[nt][0] - m_run[nt][0]), p1 = ex2(sc[nt][1] - m_run[nt][1]), p2 = ex2(sc[nt][2] - m_run[nt][0]), p3 = ex2(sc[nt][3] - m_run[nt][1]);
-        l_run[nt][0] += p0 + p2; l_run[nt][1] += p1 + p3;
-        if constexpr (FP8) {
-          pb[nt][0] = movmatrix_trans(pack_f16x2(p0 * v_scale, p1 * v_scale));
-          pb[nt][1] = movmatrix_trans(pack_f16x2(p2 * v_scale, p3 * v_scale));
-        } else {
-          pb[nt][0] = movmatrix_trans(pack_bf16x2(p0, p1));
-          pb[nt][1] = movmatrix_trans(pack_bf16x2(p2, p3));
-        }
-      }
-      // ---- O^T += V^T P^T
-      auto add_block = [&](int db, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          if (!some) {
-            if constexpr (FP8) mma_f16(acc[nt][db], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
-            else mma_bf16(acc[nt][db], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
-          } else {
-            float x[4] = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (FP8) mma_f16(x, a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
-            else mma_bf16(x, a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
-            if (see[nt][0] & beams) { acc[nt][db][0] += x[0]; acc[nt][db][2] += x[2]; }
-            if (see[nt][1] & beams) { acc[nt][db][1] += x[1]; acc[nt][db][3] += x[3]; }
-          }
-        }
-      };
-      if constexpr (FP8) {
-#pragma unroll
-        for (int c = 0; c < NV; c += 2) {
-          uint32_t raw[4];          // [block c: dim g, dim g + 8 | block c + 1: the same], keys 4t .. 4t+3 each
-          {
-            const int key = lane & 15, chk = c + (lane >> 4);
-            ldmatrix_b8_trans_x2(raw, vs_addr + key * 128 + ((chk ^ (key & 7)) << 4));
-          }
-#pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            uint32_t a0, a1, a2, a3;
-            e4m3x4_to_f16x2x2(raw[2 * m], a0, a2);
-            e4m3x4_to_f16x2x2(raw[2 * m + 1], a1, a3);
-            add_block(c + m, a0, a1, a2, a3);
-          }
+          mma_f16(sc[nt], lo[0], lo[1], lo[2], lo[3], qf[nt][j][0], qf[nt][j][1]);
+          mma_f16(sc[nt], hi[0], hi[1], hi[2], hi[3], qf[nt][j + KH][0], qf[nt][j + KH][1]);
         }
       } else {
+        {
+          // lane -> (matrix mi = lane / 8, row = lane % 8): key = 8 (mi & 1) + row, 16-byte chunk 2 j + (mi >> 1)
+          const int mi = lane >> 3, key = ((mi & 1) << 3) + (lane & 7);
+          const int cl = 2 * j + (mi >> 1), chh = 2 * (j + KH) + (mi >> 1);
+          ldmatrix_x4(lo, ks_addr + (cl / 8) * kBlockBytes + key * 128 + (((cl % 8) ^ (key & 7)) << 4));
+          ldmatrix_x4(hi, ks_addr + (chh / 8) * kBlockBytes + key * 128 + (((chh % 8) ^ (key & 7)) << 4));
+        }
 #pragma unroll
-        for (int db = 0; db < NV; ++db) {
-          uint32_t va[4];             // a0 dims g x keys 0-7, a1 dims g+8 x keys 0-7, a2 dims g x keys 8-15, a3 dims g+8 x keys 8-15
-          {
-            const int mi = lane >> 3, key = ((mi >> 1) << 3) + (lane & 7), ch = 2 * db + (mi & 1);
-            ldmatrix_x4_trans(va, vs_addr + (ch / 8) * kBlockBytes + key * 128 + (((ch % 8) ^ (key & 7)) << 4));
-          }
-          add_block(db, va[0], va[1], va[2], va[3]);
+        for (int f = 0; f < 4; ++f) {
+          const int r = f >> 1;
+          const float4 cs = lds128(((f & 1) ? cs_b : cs_a)[r] + 128 * j);
+          const float2 c = make_float2(cs.x, cs.y), s = make_float2(cs.z, cs.w), ns = lds64(((f & 1) ? ns_b : ns_a)[(2 * j + r) & 3] + 128 * (j >> 1));
+          const float2 a = bf16x2_to_float2(lo[f]), b = bf16x2_to_float2(hi[f]);
+          const float2 x = fma2(a, c, mul2(b, ns)), y = fma2(a, s, mul2(b, c));
+          lo[f] = pack_bf16x2(x.x, x.y); hi[f] = pack_bf16x2(y.x, y.y);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma_bf16(sc[nt], lo[0], lo[1], lo[2], lo[3], qf[nt][j][0], qf[nt][j][1]);
+          mma_bf16(sc[nt], hi[0], hi[1], hi[2], hi[3], qf[nt][j + KH][0], qf[nt][j + KH][1]);
         }
       }
     }
+    // ---- online softmax (log2 domain): keys A (0, 1) and B (2, 3) of columns 2t (0, 2) and 2t + 1 (1, 3)
+    const bool some = __any_sync(kFull, (beams & all_beams) != all_beams);      // (the same in every lane: the vote says so to the compiler)
+    float v_scale = 0.f, s_scale = p.scale_log2;
+    if constexpr (FP8) {
+      float ks, vs;
+      asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(ks), "=f"(vs) : "r"(scl + stage * 8) : "memory");
+      s_scale *= ks;
+      // P carries the page's V scale relative to the largest met so far, and 2^12 so that small weights stay normal in fp16
+      const bool finite = vs <= FLT_MAX;      // a page's scale may be infinite or NaN: that is for the columns that see the page, not for the others
+      if (finite && vs > v_ref) {
+        const float f = v_ref / vs;
+        v_ref = vs;
+        v_inv = 0x1p12f / vs;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int db = 0; db < NV; ++db) { acc[nt][db][0] *= f; acc[nt][db][1] *= f; acc[nt][db][2] *= f; acc[nt][db][3] *= f; }
+      }
+      v_scale = finite ? vs * v_inv : __int_as_float(0x7fffffff);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) { sc[nt][0] *= s_scale; sc[nt][1] *= s_scale; sc[nt][2] *= s_scale; sc[nt][3] *= s_scale; }
+    if (n_valid < kTile) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        if (keyA >= n_valid) { sc[nt][0] = -INFINITY; sc[nt][1] = -INFINITY; }
+        if (keyB >= n_valid) { sc[nt][2] = -INFINITY; sc[nt][3] = -INFINITY; }
+      }
+    }
+    if (some) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        if (!(see[nt][0] & beams)) { sc[nt][0] = -INFINITY; sc[nt][2] = -INFINITY; }
+        if (!(see[nt][1] & beams)) { sc[nt][1] = -INFINITY; sc[nt][3] = -INFINITY; }
+      }
+    }
+    bool higher = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) higher = higher || fmaxf(sc[nt][0], sc[nt][2]) > m_run[nt][0] || fmaxf(sc[nt][1], sc[nt][3]) > m_run[nt][1];
+    // the references move only if some lane saw a larger score
+    if (__any_sync(kFull, higher)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float mx0 = fmaxf(sc[nt][0], sc[nt][2]), mx1 = fmaxf(sc[nt][1], sc[nt][3]);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) { mx0 = fmaxf(mx0, __shfl_xor_sync(kFull, mx0, o)); mx1 = fmaxf(mx1, __shfl_xor_sync(kFull, mx1, o)); }
+        const float n0 = fmaxf(m_run[nt][0], mx0), n1 = fmaxf(m_run[nt][1], mx1);
+        const float a0 = ex2(m_run[nt][0] - n0), a1 = ex2(m_run[nt][1] - n1);
+        m_run[nt][0] = n0; m_run[nt][1] = n1;
+        l_run[nt][0] *= a0; l_run[nt][1] *= a1;
+#pragma unroll
+        for (int db = 0; db < NV; ++db) { acc[nt][db][0] *= a0; acc[nt][db][1] *= a1; acc[nt][db][2] *= a0; acc[nt][db][3] *= a1; }
+      }
+    }
+    uint32_t pb[NT][2];                    // B fragments of P^T: the transposes of the two 8 x 8 blocks (key row, columns)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float p0 = ex2(sc[nt][0] - m_run[nt][0]), p1 = ex2(sc[nt][1] - m_run[nt][1]), p2 = ex2(sc[nt][2] - m_run[nt][0]), p3 = ex2(sc[nt][3] - m_run[nt][1]);
+      l_run[nt][0] += p0 + p2; l_run[nt][1] += p1 + p3;
+      if constexpr (FP8) {
+        pb[nt][0] = movmatrix_trans(pack_f16x2(p0 * v_scale, p1 * v_scale));
+        pb[nt][1] = movmatrix_trans(pack_f16x2(p2 * v_scale, p3 * v_scale));
+      } else {
+        pb[nt][0] = movmatrix_trans(pack_bf16x2(p0, p1));
+        pb[nt][1] = movmatrix_trans(pack_bf16x2(p2, p3));
+      }
+    }
+    // ---- O^T += V^T P^T
+    auto v_block = [&](int db, uint32_t (&va)[4]) {      // a0 dims g x keys 0-7, a1 dims g+8 x keys 0-7, a2 dims g x keys 8-15, a3 dims g+8 x keys 8-15
+      const int mi = lane >> 3, key = ((mi >> 1) << 3) + (lane & 7), ch = 2 * db + (mi & 1);
+      ldmatrix_x4_trans(va, vs_addr + (ch / 8) * kBlockBytes + key * 128 + (((ch % 8) ^ (key & 7)) << 4));
+    };
+    auto v_blocks = [&](int c, uint32_t (&va)[2][4]) {      // 8-bit pages: dim blocks c and c + 1, keys 4t .. 4t+3 a lane
+      uint32_t raw[4];          // [block c: dim g, dim g + 8 | block c + 1: the same]
+      const int key = lane & 15, chk = c + (lane >> 4);
+      ldmatrix_b8_trans_x2(raw, vs_addr + key * 128 + ((chk ^ (key & 7)) << 4));
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        e4m3x4_to_f16x2x2(raw[2 * m], va[m][0], va[m][2]);
+        e4m3x4_to_f16x2x2(raw[2 * m + 1], va[m][1], va[m][3]);
+      }
+    };
+    auto mma = [&](float (&d)[4], const uint32_t (&va)[4], const uint32_t (&b)[2]) {
+      if constexpr (FP8) mma_f16(d, va[0], va[1], va[2], va[3], b[0], b[1]);
+      else mma_bf16(d, va[0], va[1], va[2], va[3], b[0], b[1]);
+    };
+    auto each_block = [&](auto use) {
+#pragma unroll
+      for (int db = 0; db < NV; db += 2) {
+        uint32_t va[2][4];
+        if constexpr (FP8) v_blocks(db, va);
+        else { v_block(db, va[0]); v_block(db + 1, va[1]); }
+        use(db, va[0]);
+        use(db + 1, va[1]);
+      }
+    };
+    if (!some) {
+      each_block([&](int db, const uint32_t (&va)[4]) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) mma(acc[nt][db], va, pb[nt]);
+      });
+    } else {
+      each_block([&](int db, const uint32_t (&va)[4]) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float x[4] = {0.f, 0.f, 0.f, 0.f};
+          mma(x, va, pb[nt]);
+          if (see[nt][0] & beams) { acc[nt][db][0] += x[0]; acc[nt][db][2] += x[2]; }
+          if (see[nt][1] & beams) { acc[nt][db][1] += x[1]; acc[nt][db][3] += x[3]; }
+        }
+      });
+    }
     __syncwarp();   // every lane is done with this stage
-    if (issued < x1) issue(stage);
+    if (issued < n_tiles) issue(stage);
     __syncwarp();
     if (--c_left == 0) {
       next_unit(p, cu);
-      c_left = static_cast<long long>(cu.r1 - cu.r0) << p.log2_tpp;
+      c_left = static_cast<int>(min(static_cast<long long>(cu.r1 - cu.r0) << p.log2_tpp, static_cast<long long>(INT_MAX)));
     }
     if (++stage == kStages) { stage = 0; parity ^= 1u; }
   }
@@ -793,8 +852,8 @@ int32_t beam_call(const mepic_config_t* cfg, const mepic_attn_beam_args_t* a, co
   p.part_o = static_cast<float*>(a->workspace);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + slots_of(s, cfg->n_kv_heads, sms) * p.columns * cfg->head_dim);
   alignas(64) CUtensorMap map_k, map_v;
-  int32_t rc = fp8 ? mepic_make_pool_map_u8(cfg, a->k_pool, &map_k) : mepic_make_pool_map(cfg, a->k_pool, &map_k);
-  if (rc == MEPIC_OK) rc = fp8 ? mepic_make_pool_map_u8(cfg, a->v_pool, &map_v) : mepic_make_pool_map(cfg, a->v_pool, &map_v);
+  int32_t rc = fp8 ? mepic_make_pool_map_u8(cfg, a->k_pool, &map_k) : mepic_make_pool_map_halves(cfg, a->k_pool, &map_k);
+  if (rc == MEPIC_OK) rc = fp8 ? mepic_make_pool_map_u8(cfg, a->v_pool, &map_v) : mepic_make_pool_map_halves(cfg, a->v_pool, &map_v);
   if (rc != MEPIC_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int nt = (p.columns + 7) / 8;

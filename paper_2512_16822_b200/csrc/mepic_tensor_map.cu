@@ -52,6 +52,25 @@ int32_t mepic_make_pool_map(const mepic_config_t* cfg, const void* pool, void* o
   return MEPIC_OK;
 }
 
+// The same pool seen as [head_dim / 64 halves][rows][64 dims], so that one box brings every half of a 16-token group, one after the
+// other, each as above: one copy a tile instead of one per half.
+int32_t mepic_make_pool_map_halves(const mepic_config_t* cfg, const void* pool, void* out_map) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) { mepic_set_error("cuTensorMapEncodeTiled is not available from the driver"); return MEPIC_E_CUDA; }
+  const cuuint64_t rows = static_cast<cuuint64_t>(cfg->num_pages) * cfg->n_kv_heads * cfg->page_size;
+  if (rows > 0x7fffffffull) { mepic_set_error("pool has too many rows for 32-bit tensor coordinates"); return MEPIC_E_INVAL; }
+  const cuuint32_t halves = static_cast<cuuint32_t>(cfg->head_dim / 64);
+  const cuuint64_t dims[3] = {64, rows, halves};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(cfg->head_dim) * 2, 128};
+  const cuuint32_t box[3] = {64, 16, halves};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = fn(static_cast<CUtensorMap*>(out_map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(pool), dims, strides,
+                        box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) { mepic_set_error("cuTensorMapEncodeTiled failed with code %d", static_cast<int>(r)); return MEPIC_E_CUDA; }
+  return MEPIC_OK;
+}
+
 // The same for a pool of 8-bit elements (fp8 pages, head_dim = 128): rows of 128 bytes, one box = a whole
 // 16-token group (16 rows x 128 bytes).
 int32_t mepic_make_pool_map_u8(const mepic_config_t* cfg, const void* pool, void* out_map) {
