@@ -39,6 +39,9 @@ constexpr int kStages = 2;
 constexpr int kMinPiece = 4;         // the line is never cut into pieces shorter than this many tiles
 constexpr int kAngles = 128;         // positions of the shared-memory table
 constexpr int kMaxColumns = 32;      // columns of a column block
+// Cutting a number off after ten bits of mantissa makes it smaller, by 2^-11 of its power of two in the mean and by 2^-11 / (2 ln 2) of
+// itself where mantissas are spread as those of products are; the scores are made larger by as much.
+constexpr float kTf32Cut = 1.f + 0x1p-11f * 0.7213475f;
 constexpr float kSmallScale = 0x1p-100f;      // 8-bit pages: V scales are taken relative to the largest met, at least to this one
 constexpr int kSeg = 256;            // table entries a CTA of the plan looks at
 
@@ -243,19 +246,14 @@ __device__ __forceinline__ Unit unit_at(const BeamParams& p, long long x, int la
 }
 
 template <int D, bool FP8> constexpr int stage_bytes = 2 * kTile * D * (FP8 ? 1 : 2);
-// Per position of the table, for every two pairs of dims: (c, c', s, s') and, for fp32, (-s, -s') behind all of those.
-template <int D, bool FP8> constexpr int angle_bytes = D / 2 * (FP8 ? 4 : 12);
+// Per position of the table, for every two pairs of dims: (c, c', s, s') in fp32 or fp16.
+template <int D, bool FP8> constexpr int angle_bytes = D / 2 * (FP8 ? 4 : 8);
 template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (kStages * stage_bytes<D, FP8> + 128) + kAngles * angle_bytes<D, FP8> + 1024;
 
 // NT: tiles of 8 columns; W: warps of a CTA.
 __device__ __forceinline__ float4 lds128(uint32_t addr) {
   float4 v;
   asm("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-  return v;
-}
-__device__ __forceinline__ float2 lds64(uint32_t addr) {
-  float2 v;
-  asm("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
   return v;
 }
 
@@ -386,7 +384,6 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     } else {
       unsigned char* at = angles + a * kAngleBytes;
       *reinterpret_cast<float4*>(at + ((u * 16) ^ ((a & 1) << 6))) = make_float4(cs.x, cs.z, cs.y, cs.w);
-      *reinterpret_cast<float2*>(at + D * 4 + ((u * 8) ^ ((a & 3) << 5))) = make_float2(-cs.y, -cs.w);
     }
   }
   __syncthreads();
@@ -399,6 +396,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   unsigned see[NT][2];                       // beam bit of the columns 8 nt + 2 t, + 1 of this lane (0: no such column)
   int q_at[NT];                              // position and un-rotated query of column 8 nt + g
   const uint16_t* q_src[NT];
+  constexpr bool TF32 = !FP8 && NT <= 2;     // QK^T in tf32 where the registers allow it
+  float qt[TF32 ? NT : 1][KS][4];            // B fragments of Q'^T in tf32: dims of the k-step's two column halves, pairs
   uint32_t qf[NT][KS][2];                    // B fragments of Q'^T, column 8 nt + g
   float m_run[NT][2], l_run[NT][2];          // reference and this lane's share of the sum of columns 2 t, 2 t + 1
   float acc[NT][NV][4];                      // O^T: [dim g: column 2t, 2t+1 | dim g + 8: the same]
@@ -445,8 +444,13 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       const float2 lo = bf16x2_to_float2(__ldg(src)), hi = bf16x2_to_float2(__ldg(src + D / 4));
       const float2 c = make_float2(cs.x, cs.z), sp = make_float2(cs.y * sn, cs.w * sn), sm = make_float2(-sp.x, -sp.y);
       const float2 a = fma2(lo, c, mul2(hi, sm)), b = fma2(lo, sp, mul2(hi, c));
-      qf[nt][j][r] = FP8 ? pack_f16x2(a.x, a.y) : pack_bf16x2(a.x, a.y);
-      qf[nt][j + KH][r] = FP8 ? pack_f16x2(b.x, b.y) : pack_bf16x2(b.x, b.y);
+      if constexpr (TF32) {
+        qt[nt][j][2 * r] = round_tf32(a.x); qt[nt][j][2 * r + 1] = round_tf32(a.y);
+        qt[nt][j + KH][2 * r] = round_tf32(b.x); qt[nt][j + KH][2 * r + 1] = round_tf32(b.y);
+      } else {
+        qf[nt][j][r] = FP8 ? pack_f16x2(a.x, a.y) : pack_bf16x2(a.x, a.y);
+        qf[nt][j + KH][r] = FP8 ? pack_f16x2(b.x, b.y) : pack_bf16x2(b.x, b.y);
+      }
     };
     if (__all_sync(kFull, same)) {
 #pragma unroll
@@ -523,21 +527,17 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     for (int nt = 0; nt < NT; ++nt) { sc[nt][0] = 0.f; sc[nt][1] = 0.f; sc[nt][2] = 0.f; sc[nt][3] = 0.f; }
     const int offA = pos - anchor + keyA, offB = pos - anchor + keyB;
     const uint32_t row_a = angles_addr + offA * kAngleBytes, row_b = angles_addr + offB * kAngleBytes;
-    uint32_t cs_a[2], cs_b[2], ns_a[4], ns_b[4];      // addresses of the lane's quadruples (column half r) and of its negated sines
+    uint32_t cs_a[2], cs_b[2];      // addresses of the lane's quadruples, by column half r
     if constexpr (!FP8) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         cs_a[r] = row_a + ((16 * t + 64 * r) ^ ((offA & 1) << 6));
         cs_b[r] = row_b + ((16 * t + 64 * r) ^ ((offB & 1) << 6));
       }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        ns_a[k] = row_a + D * 4 + ((8 * t + 32 * k) ^ ((offA & 3) << 5));
-        ns_b[k] = row_b + D * 4 + ((8 * t + 32 * k) ^ ((offB & 3) << 5));
-      }
     }
 #pragma unroll
     for (int j = 0; j < KH; ++j) {
+      float2 kx[TF32 ? 4 : 1], ky[TF32 ? 4 : 1];
       uint32_t lo[4], hi[4];      // A fragments of k-steps j, j + KH: [key A, key B | key A, key B (second column half)]
       if constexpr (FP8) {
         uint32_t raw[4];          // [key A, key B of chunk j | of chunk j + KH], four dims each
@@ -575,12 +575,23 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
           const int r = f >> 1;
-          const float4 cs = lds128(((f & 1) ? cs_b : cs_a)[r] + 128 * j);
-          const float2 c = make_float2(cs.x, cs.y), s = make_float2(cs.z, cs.w), ns = lds64(((f & 1) ? ns_b : ns_a)[(2 * j + r) & 3] + 128 * (j >> 1));
+          const float4 cs = lds128(((f & 1) ? cs_b : cs_a)[r] + 128 * j);      // c, c', s, s'
           const float2 a = bf16x2_to_float2(lo[f]), b = bf16x2_to_float2(hi[f]);
-          const float2 x = fma2(a, c, mul2(b, ns)), y = fma2(a, s, mul2(b, c));
-          lo[f] = pack_bf16x2(x.x, x.y); hi[f] = pack_bf16x2(y.x, y.y);
+          const float2 x = make_float2(fmaf(a.x, cs.x, -(b.x * cs.z)), fmaf(a.y, cs.y, -(b.y * cs.w)));
+          const float2 y = make_float2(fmaf(a.x, cs.z, b.x * cs.x), fmaf(a.y, cs.w, b.y * cs.y));
+          if constexpr (TF32) { kx[f] = x; ky[f] = y; }
+          else { lo[f] = pack_bf16x2(x.x, x.y); hi[f] = pack_bf16x2(y.x, y.y); }
         }
+        if constexpr (TF32) {
+          // one k-step of 16 dims is two of eight: a lane's two neighbouring dims stand at places t and t + 4
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              mma_tf32(sc[nt], kx[2 * r].x, kx[2 * r + 1].x, kx[2 * r].y, kx[2 * r + 1].y, qt[nt][j][2 * r], qt[nt][j][2 * r + 1]);
+              mma_tf32(sc[nt], ky[2 * r].x, ky[2 * r + 1].x, ky[2 * r].y, ky[2 * r + 1].y, qt[nt][j + KH][2 * r], qt[nt][j + KH][2 * r + 1]);
+            }
+        } else
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           mma_bf16(sc[nt], lo[0], lo[1], lo[2], lo[3], qf[nt][j][0], qf[nt][j][1]);
@@ -590,7 +601,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     }
     // ---- online softmax (log2 domain): keys A (0, 1) and B (2, 3) of columns 2t (0, 2) and 2t + 1 (1, 3)
     const bool some = __any_sync(kFull, (beams & all_beams) != all_beams);      // (the same in every lane: the vote says so to the compiler)
-    float v_scale = 0.f, s_scale = p.scale_log2;
+    float v_scale = 0.f, s_scale = TF32 ? p.scale_log2 * kTf32Cut : p.scale_log2;
     if constexpr (FP8) {
       float ks, vs;
       asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(ks), "=f"(vs) : "r"(scl + stage * 8) : "memory");
