@@ -35,13 +35,12 @@ namespace {
 using namespace mepic_dev;
 
 constexpr int kTile = 16;            // keys per staged tile
-constexpr int kStages = 2;
 constexpr int kMinPiece = 4;         // the line is never cut into pieces shorter than this many tiles
-constexpr int kAngles = 128;         // positions of the shared-memory table
 constexpr int kMaxColumns = 32;      // columns of a column block
 // Cutting a number off after ten bits of mantissa makes it smaller, by 2^-11 of its power of two in the mean and by 2^-11 / (2 ln 2) of
 // itself where mantissas are spread as those of products are; the scores are made larger by as much.
 constexpr float kTf32Cut = 1.f + 0x1p-11f * 0.7213475f;
+constexpr float kLag = 8.f;                      // weights may reach 2^8
 constexpr float kSmallScale = 0x1p-100f;      // 8-bit pages: V scales are taken relative to the largest met, at least to this one
 constexpr int kSeg = 256;            // table entries a CTA of the plan looks at
 
@@ -248,7 +247,12 @@ __device__ __forceinline__ Unit unit_at(const BeamParams& p, long long x, int la
 template <int D, bool FP8> constexpr int stage_bytes = 2 * kTile * D * (FP8 ? 1 : 2);
 // Per position of the table, for every two pairs of dims: (c, c', s, s') in fp32 or fp16.
 template <int D, bool FP8> constexpr int angle_bytes = D / 2 * (FP8 ? 4 : 8);
-template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (kStages * stage_bytes<D, FP8> + 128) + kAngles * angle_bytes<D, FP8> + 1024;
+// Stages of a warp's ring.  8-bit tiles are half as large: twice as many keep the same bytes in flight.
+template <bool FP8> constexpr int stages_of = FP8 ? 4 : 2;
+constexpr int kWarpWords = 128;      // bytes a warp has beside its ring: per stage 16 of tile data, 8 of scales and a barrier of 8
+// Positions of the table: as many as fit beside the rings.
+template <bool FP8, int W> constexpr int angles_of = !FP8 && W > 10 ? 64 : 128;
+template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (stages_of<FP8> * stage_bytes<D, FP8> + kWarpWords) + angles_of<FP8, W> * angle_bytes<D, FP8> + 1024;
 
 // NT: tiles of 8 columns; W: warps of a CTA.
 __device__ __forceinline__ float4 lds128(uint32_t addr) {
@@ -266,7 +270,9 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   constexpr int KB = FP8 ? 1 : NB;
   constexpr int kBlockBytes = kTile * 128;
   constexpr int kStageBytes = stage_bytes<D, FP8>;
-  constexpr int kAngleBytes = angle_bytes<D, FP8>;
+  constexpr int kStages = stages_of<FP8>;
+  static_assert(kStages * 32 <= kWarpWords, "tile data, scales and barriers of the ring");
+  constexpr int kAngleBytes = angle_bytes<D, FP8>, kAngles = angles_of<FP8, W>;
 
   extern __shared__ unsigned char smem_dyn[];
   // 1024-byte alignment: the swizzle pattern is a function of the address bits
@@ -274,10 +280,10 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   const int lane = threadIdx.x & 31, wic = __shfl_sync(kFull, static_cast<int>(threadIdx.x >> 5), 0);      // (known to be the same in a warp)
   unsigned char* stage0 = smem + static_cast<size_t>(wic) * kStages * kStageBytes;
   unsigned char* angles = smem + static_cast<size_t>(W) * kStages * kStageBytes;
-  unsigned char* misc = angles + kAngles * kAngleBytes + wic * 128;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(misc);                          // kStages x 8 bytes
-  const uint32_t meta = smem_u32(misc + 16);             // per stage: position, beams, valid slots of the tile
+  unsigned char* words = angles + kAngles * kAngleBytes + wic * kWarpWords;
+  const uint32_t meta = smem_u32(words);                 // per stage: position, beams, valid slots of the tile
   const uint32_t scl = meta + kStages * 16;              // per stage: K and V scale of the page
+  uint64_t* bars = reinterpret_cast<uint64_t*>(words + kStages * 24);
 
   const int g = lane >> 2, t = lane & 3;     // fragment row (key, dim, or column of Q) and column group
   // 8-bit pages: ldmatrix on bytes hands a lane four consecutive dims of a key, its transposing form four consecutive keys of a
@@ -335,20 +341,17 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         win_vs = __ldg(p.v_scales + static_cast<size_t>(win.x) * p.n_kv_heads + pu.head);
       }
     }
-    const int src = pr - win0;
-    const int page = __shfl_sync(kFull, win.x, src), pos = __shfl_sync(kFull, win.y, src), beams = __shfl_sync(kFull, win.z, src), slots = __shfl_sync(kFull, win.w, src);
-    float ks = 0.f, vs = 0.f;
-    if constexpr (FP8) { ks = __shfl_sync(kFull, win_ks, src); vs = __shfl_sync(kFull, win_vs, src); }
-    const int n_valid = min(slots - pt * kTile, kTile);
-    if (lane == 0) {
-      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%3};" ::"r"(meta + stage * 16), "r"(pos + pt * kTile), "r"(beams), "r"(n_valid) : "memory");
-      if constexpr (FP8) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(scl + stage * 8), "f"(ks), "f"(vs) : "memory");
+    // the lane that holds the record issues the copies
+    if (lane == pr - win0) {
+      const int n_valid = min(win.w - pt * kTile, kTile);
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%3};" ::"r"(meta + stage * 16), "r"(win.y + pt * kTile), "r"(win.z), "r"(n_valid) : "memory");
+      if constexpr (FP8) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(scl + stage * 8), "f"(win_ks), "f"(win_vs) : "memory");
       if (!(w == 0 && issued == p.skip_tile)) {        // (test hook: one copy that never comes)
         const uint32_t bar = smem_u32(&bars[stage]), dst = smem_u32(stage0 + stage * kStageBytes);
         if (n_valid <= 0) {
           mbar_expect_tx(bar, 0);                           // a tile of the page that holds no slot
         } else {
-          const int y = (page * p.n_kv_heads + pu.head) * p.page_size + pt * kTile;      // row of the pool viewed as [rows][D]
+          const int y = (win.x * p.n_kv_heads + pu.head) * p.page_size + pt * kTile;      // row of the pool viewed as [rows][D]
           mbar_expect_tx(bar, kStageBytes);
           if constexpr (FP8) {
             tma_load_2d(dst, &map_k, 0, y, bar);
@@ -401,12 +404,12 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   uint32_t qf[NT][KS][2];                    // B fragments of Q'^T, column 8 nt + g
   float m_run[NT][2], l_run[NT][2];          // reference and this lane's share of the sum of columns 2 t, 2 t + 1
   float acc[NT][NV][4];                      // O^T: [dim g: column 2t, 2t+1 | dim g + 8: the same]
-  float v_ref = kSmallScale, v_inv = 0x1p12f / kSmallScale;      // 8-bit pages: acc is in units of v_ref 2^-12; 2^12 / v_ref
+  float v_ref = kSmallScale, v_inv = 0x1p6f / kSmallScale;      // 8-bit pages: acc is in units of v_ref 2^-6; 2^6 / v_ref
 
   auto flush = [&]() {
     if (u_block < 0) return;
     const long long slot = static_cast<long long>(u_block) * p.n_kv_heads + u_head + w;
-    const float unit = FP8 ? v_ref * 0x1p-12f : 1.f;
+    const float unit = FP8 ? v_ref * 0x1p-6f : 1.f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -477,7 +480,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     if (cu.block != u_block || cu.head != u_head) {
       flush();
       u_block = cu.block; u_head = cu.head;
-      anchor = INT_MIN; v_ref = kSmallScale; v_inv = 0x1p12f / kSmallScale;
+      anchor = INT_MIN; v_ref = kSmallScale; v_inv = 0x1p6f / kSmallScale;
       const int first = (u_block % p.blocks) * p.beams, nb = min(p.beams, p.width - first);
       all_beams = nb == 32 ? ~0u : (1u << nb) - 1;
       const int row0 = u_block / p.blocks * p.width + first;
@@ -606,12 +609,12 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       float ks, vs;
       asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(ks), "=f"(vs) : "r"(scl + stage * 8) : "memory");
       s_scale *= ks;
-      // P carries the page's V scale relative to the largest met so far, and 2^12 so that small weights stay normal in fp16
+      // P carries the page's V scale relative to the largest met so far, and 2^6 so that small weights stay normal in fp16 (the largest reach 2^14)
       const bool finite = vs <= FLT_MAX;      // a page's scale may be infinite or NaN: that is for the columns that see the page, not for the others
       if (finite && vs > v_ref) {
         const float f = v_ref / vs;
         v_ref = vs;
-        v_inv = 0x1p12f / vs;
+        v_inv = 0x1p6f / vs;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -637,8 +640,9 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     }
     bool higher = false;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) higher = higher || fmaxf(sc[nt][0], sc[nt][2]) > m_run[nt][0] || fmaxf(sc[nt][1], sc[nt][3]) > m_run[nt][1];
-    // the references move only if some lane saw a larger score
+    for (int nt = 0; nt < NT; ++nt) higher = higher || fmaxf(sc[nt][0], sc[nt][2]) > m_run[nt][0] + kLag || fmaxf(sc[nt][1], sc[nt][3]) > m_run[nt][1] + kLag;
+    // the references move only if some lane saw a score well above: any reference gives the same softmax as long as no weight
+    // overflows (with 16 columns some column's largest score moves in two tiles of five, by little)
     if (__any_sync(kFull, higher)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -793,7 +797,7 @@ int sm_count(int* device) {
   return sms;
 }
 constexpr int kMaxWarps = 12;
-constexpr int warps_of(int, bool) { return 8; }
+constexpr int warps_of(int nt, bool fp8) { return fp8 && nt <= 2 ? 12 : 8; }
 size_t slots_of(const PlanShape& s, int n_kv_heads, int sms) { return static_cast<size_t>(s.groups) * s.blocks * n_kv_heads + static_cast<size_t>(sms) * kMaxWarps; }
 size_t workspace_bytes(const mepic_config_t* cfg, const PlanShape& s, int sms) {
   const size_t columns = static_cast<size_t>(s.beams) * (cfg->n_q_heads / cfg->n_kv_heads);
