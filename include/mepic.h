@@ -783,7 +783,8 @@ int32_t mepic_beam_select(const mepic_beam_select_args_t* args, void* cuda_strea
  *     *reserve_used_out = *reserve_used - pages returned + copies.  The places of handed-out pages hold nothing of meaning.
  * width_in beams a group become width_out (1 -> n starts a search).  All or nothing: if the reserve cannot supply the copies,
  * MEPIC_DEV_NO_PAGES is set, if it would get back more than it handed out (or *reserve_used lies outside [0, n_reserve])
- * MEPIC_DEV_BAD_BEAM; then every new length is 0, no copy is listed and the reserve stays as it was.  A parent outside
+ * MEPIC_DEV_BAD_BEAM; then every new length is 0, no copy is listed, the reserve stays as it was and the tables written hold nothing
+ * of meaning.  A parent outside
  * [-1, width_in) sets MEPIC_DEV_BAD_BEAM and counts as -1, a length outside [0, table_stride * P] sets MEPIC_DEV_BAD_SLOT and is
  * clamped, a page id outside the pool sets MEPIC_DEV_BAD_PAGE and counts as not owned (it is copied, if it has to be, by a
  * copy that mepic_pages_copy skips).

@@ -92,6 +92,7 @@ struct PlanParams {
 __global__ void __launch_bounds__(kSeg) mepic_beam_plan_classes(const __grid_constant__ PlanParams p) {
   __shared__ int len[MEPIC_BEAM_MAX_WIDTH];
   __shared__ int warp_n[kSeg / 32];
+  extern __shared__ int held_pages[];          // [page ids, position bases][beams of the block][kSeg]
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int block = blockIdx.x, seg = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group = block / p.blocks, first = (block - group * p.blocks) * p.beams, nb = min(p.beams, p.width - first);
@@ -113,14 +114,32 @@ __global__ void __launch_bounds__(kSeg) mepic_beam_plan_classes(const __grid_con
   const int32_t* ids = p.page_ids + row0 * p.stride + e;
   const int32_t* base = p.pos_base + row0 * p.stride + e;
   auto fill = [&](int i) { return static_cast<int>(min(static_cast<long long>(P), len[i] - from)); };
+  // everything the entry's beams hold, asked for side by side and kept in shared memory, a column per thread
+  int* my_ids = held_pages + tid;
+  int* my_base = held_pages + nb * kSeg + tid;
+  const int lead = held ? __ffs(held) - 1 : 0;
+  bool one = true;                              // all beams that hold anything here hold the same, as over a shared context
+  for (int i0 = 0; i0 < nb; i0 += 8) {
+    int a[8], b[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (i0 + k < nb && (held >> (i0 + k) & 1)) { a[k] = __ldg(ids + static_cast<size_t>(i0 + k) * p.stride); b[k] = __ldg(base + static_cast<size_t>(i0 + k) * p.stride); }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (i0 + k < nb && (held >> (i0 + k) & 1)) { my_ids[(i0 + k) * kSeg] = a[k]; my_base[(i0 + k) * kSeg] = b[k]; }
+  }
+  for (unsigned m = held; m; m &= m - 1) {
+    const int i = __ffs(m) - 1;
+    one = one && my_ids[i * kSeg] == my_ids[lead * kSeg] && my_base[i * kSeg] == my_base[lead * kSeg] && fill(i) == fill(lead);
+  }
   auto each_class = [&](auto use) {
+    if (one) { if (held) use(my_ids[lead * kSeg], my_base[lead * kSeg], held, fill(lead)); return; }
     for (unsigned left = held; left;) {
-      const int i = __ffs(left) - 1;
-      const int page = __ldg(ids + static_cast<size_t>(i) * p.stride), pos = __ldg(base + static_cast<size_t>(i) * p.stride), n = fill(i);
+      const int i = __ffs(left) - 1, page = my_ids[i * kSeg], pos = my_base[i * kSeg], n = fill(i);
       unsigned same = 0;
       for (unsigned m = left; m; m &= m - 1) {
         const int j = __ffs(m) - 1;
-        if (__ldg(ids + static_cast<size_t>(j) * p.stride) == page && __ldg(base + static_cast<size_t>(j) * p.stride) == pos && fill(j) == n) same |= 1u << j;
+        if (my_ids[j * kSeg] == page && my_base[j * kSeg] == pos && fill(j) == n) same |= 1u << j;
       }
       left &= ~same;
       use(page, pos, same, n);
@@ -908,8 +927,13 @@ extern "C" int32_t mepic_beam_plan(const mepic_config_t* cfg, const mepic_beam_p
   while ((1 << p.page_shift) < cfg->page_size) ++p.page_shift;
   p.num_pages = cfg->num_pages; p.group_size = cfg->n_q_heads / cfg->n_kv_heads; p.n_kv_heads = cfg->n_kv_heads;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  mepic_beam_plan_classes<<<dim3(static_cast<unsigned>(s.groups) * s.blocks, s.segments), kSeg, 0, st>>>(p);
-  cudaError_t e = cudaGetLastError();
+  const size_t smem = static_cast<size_t>(s.beams) * kSeg * 2 * sizeof(int);
+  cudaError_t e = cudaSuccess;
+  // always the largest: another thread's call may need more than this one
+  if (smem > 40 * 1024) e = cudaFuncSetAttribute(mepic_beam_plan_classes, cudaFuncAttributeMaxDynamicSharedMemorySize, MEPIC_BEAM_MAX_WIDTH * kSeg * 2 * static_cast<int>(sizeof(int)));
+  if (e != cudaSuccess) { mepic_set_error("beam_plan: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
+  mepic_beam_plan_classes<<<dim3(static_cast<unsigned>(s.groups) * s.blocks, s.segments), kSeg, smem, st>>>(p);
+  e = cudaGetLastError();
   if (e == cudaSuccess) e = launch_dependent(mepic_beam_plan_sums, dim3(1), dim3(kScanThreads), st, p);
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) { mepic_set_error("beam_plan: launch: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }

@@ -49,10 +49,12 @@ template <> __device__ __forceinline__ __half minus_infinity<__half>() { return 
 
 // Key of a token: the larger logit first, the lower index among equals (-0 counts as 0); 0 where there is no candidate
 // (-infinity; a NaN's row is given up as a whole).
-__device__ __forceinline__ uint64_t token_key(float x, int at) {
+__device__ __forceinline__ uint32_t order_of(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
-  const uint32_t s = u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
-  return x > -INFINITY ? static_cast<uint64_t>(s) << 32 | (0xffffffffu - static_cast<uint32_t>(at)) : 0;
+  return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ uint64_t token_key(float x, int at) {
+  return x > -INFINITY ? static_cast<uint64_t>(order_of(x)) << 32 | (0xffffffffu - static_cast<uint32_t>(at)) : 0;
 }
 __device__ __forceinline__ float key_value(uint64_t k) {
   const uint32_t s = static_cast<uint32_t>(k >> 32);
@@ -64,23 +66,52 @@ __device__ __forceinline__ uint64_t warp_max_key(uint64_t k) {
   return static_cast<uint64_t>(top) << 32 | __reduce_max_sync(kFull, hi == top ? static_cast<uint32_t>(k) : 0u);
 }
 
-struct SegmentSum { double sum; float top; float pad; };      // sum of exp(x - top) over the segment; NaN: the row is to be given up
+struct SegmentSum { double sum; float top; float pad; };      // sum of exp(x - top) over a warp's tokens; NaN: the row is to be given up
 
 struct SelectParams {
   mepic_beam_select_args_t a;
-  SegmentSum* sums;      // [rows][segments]
+  SegmentSum* sums;      // [rows][segments][kSelWarps]
   uint64_t* best;        // [rows][segments][n_select], descending, 0 where there are fewer
   int segments;
   long long stride;
 };
 
-// One segment of one row.
+// The slow way, for segments with more tokens at or above the threshold than the list holds (thousands of equal logits): the best
+// token below the last one found, n_select times over, the segment read again each time.
+template <typename T>
+__device__ __noinline__ void select_by_rounds(const T* x, long long first, long long end, int n_select, uint64_t* out) {
+  __shared__ uint64_t round_best[2][kSelWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint64_t last = ~0ull;
+  for (int k = 0; k < n_select; ++k) {
+    uint64_t mine = 0;
+    for (long long i = first + threadIdx.x; i < end; i += kSelThreads) {
+      const uint64_t key = token_key(static_cast<float>(x[i]), static_cast<int>(i));
+      if (key < last && key > mine) mine = key;
+    }
+    mine = warp_max_key(mine);
+    if (lane == 0) round_best[k & 1][warp] = mine;
+    __syncthreads();
+    uint64_t b = round_best[k & 1][0];
+#pragma unroll
+    for (int i = 1; i < kSelWarps; ++i) b = max(b, round_best[k & 1][i]);
+    if (threadIdx.x == 0) out[k] = b;
+    last = b;
+  }
+}
+
+// One segment of one row.  The threads' own maxima, taken four threads together, are 64 tokens of the segment: its n_select best are
+// not below the n_select-th largest of them.  The few tokens that are not go to a list, whose ranks are counted.
+constexpr int kSelList = 512;
+constexpr int kSelGroups = kSelThreads / 4;
+static_assert(kSelGroups >= MEPIC_BEAM_MAX_SELECT, "as many maxima as tokens to select");
 template <typename T>
 __global__ void __launch_bounds__(kSelThreads) mepic_beam_segments(const __grid_constant__ SelectParams p) {
   constexpr int N = Vec<T>::n;
-  __shared__ uint64_t round_best[2][kSelWarps];
-  __shared__ double warp_sums[kSelWarps];
-  __shared__ float warp_tops[kSelWarps];
+  __shared__ alignas(16) uint32_t group_top[kSelGroups];
+  __shared__ uint64_t list[kSelList];
+  __shared__ uint32_t threshold;
+  __shared__ int listed;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int row = blockIdx.y, seg = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float score = __ldg(p.a.score + row);
@@ -89,19 +120,20 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_segments(const __grid_
   // pieces of 16 bytes by address: the row may begin and end inside one
   const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
   const int V = p.a.vocab;
+  const int begin = seg * (kSelChunks * kSelThreads * N) - lead;      // token of the segment's first place (negative before the row)
   uint4 c[kSelChunks];
-  long long at0[kSelChunks];       // token of a piece's first element (negative in the row's first piece)
 #pragma unroll
   for (int k = 0; k < kSelChunks; ++k) {
-    at0[k] = (static_cast<long long>(seg) * kSelChunks * kSelThreads + k * kSelThreads + tid) * N - lead;
-    if (at0[k] >= 0 && at0[k] + N <= V) c[k] = __ldcs(reinterpret_cast<const uint4*>(x + at0[k]));
+    const int at = begin + (k * kSelThreads + tid) * N;
+    if (at >= 0 && at + N <= V) c[k] = __ldcs(reinterpret_cast<const uint4*>(x + at));
     else {
       alignas(16) T e[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) e[i] = at0[k] + i >= 0 && at0[k] + i < V ? x[at0[k] + i] : minus_infinity<T>();
+      for (int i = 0; i < N; ++i) e[i] = at + i >= 0 && at + i < V ? x[at + i] : minus_infinity<T>();
       c[k] = *reinterpret_cast<const uint4*>(e);
     }
   }
+  if (tid == 0) listed = 0;
   float top = -INFINITY;
 #pragma unroll
   for (int k = 0; k < kSelChunks; ++k) {
@@ -119,66 +151,86 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_segments(const __grid_
 #pragma unroll
     for (int i = 0; i < N; ++i) sum += ex2((v[i] - ref) * kLog2e);      // +infinity - +infinity and NaN - anything: NaN
   }
-  // ---- maximum and sum of the segment
-  float wtop = top;
+  // ---- maximum and sum of the segment, maxima of four threads together
+  float wtop = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
+  wtop = fmaxf(wtop, __shfl_xor_sync(kFull, wtop, 2));
+  if ((lane & 3) == 0) group_top[tid >> 2] = order_of(wtop);
 #pragma unroll
-  for (int d = 16; d; d >>= 1) wtop = fmaxf(wtop, __shfl_xor_sync(kFull, wtop, d));
+  for (int d = 4; d < 32; d <<= 1) wtop = fmaxf(wtop, __shfl_xor_sync(kFull, wtop, d));
   double s = static_cast<double>(sum) * (top == -INFINITY ? 1.0 : static_cast<double>(ex2((top - wtop) * kLog2e)));
 #pragma unroll
   for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(kFull, s, d);
-  if (lane == 0) { warp_sums[warp] = s; warp_tops[warp] = wtop; }
-  // ---- the n_select best, one a round
+  if (lane == 0) p.sums[(static_cast<size_t>(row) * p.segments + seg) * kSelWarps + warp] = SegmentSum{s, wtop, 0.f};
+  __syncthreads();
   const int K = p.a.n_select;
-  uint64_t last = ~0ull, mine = 0;
-  auto rescan = [&]() {
-    mine = 0;
+  if (tid < kSelGroups) {
+    const uint32_t mine = group_top[tid];
+    int above = 0;
+#pragma unroll
+    for (int q = 0; q < kSelGroups; q += 4) {
+      const uint4 o = *reinterpret_cast<const uint4*>(group_top + q);
+      above += (o.x > mine || (o.x == mine && q < tid)) + (o.y > mine || (o.y == mine && q + 1 < tid)) +
+               (o.z > mine || (o.z == mine && q + 2 < tid)) + (o.w > mine || (o.w == mine && q + 3 < tid));
+    }
+    if (above == K - 1) threshold = mine;
+  }
+  __syncthreads();
+  const uint32_t least = threshold;
+  if (order_of(top) >= least && top > -INFINITY) {
 #pragma unroll
     for (int k = 0; k < kSelChunks; ++k) {
       float v[N];
       widen<T>(c[k], v);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const uint64_t key = token_key(v[i], static_cast<int>(at0[k] + i));
-        if (key < last && key > mine) mine = key;
-      }
+      for (int i = 0; i < N; ++i)
+        if (order_of(v[i]) >= least && v[i] > -INFINITY) {
+          const int at = atomicAdd(&listed, 1);
+          if (at < kSelList) list[at] = token_key(v[i], begin + (k * kSelThreads + tid) * N + i);
+        }
     }
-  };
-  rescan();
+  }
+  __syncthreads();
   uint64_t* out = p.best + (static_cast<size_t>(row) * p.segments + seg) * K;
-  for (int k = 0; k < K; ++k) {
-    const uint64_t w = warp_max_key(mine);
-    if (lane == 0) round_best[k & 1][warp] = w;
-    __syncthreads();
-    uint64_t b = round_best[k & 1][0];
-#pragma unroll
-    for (int i = 1; i < kSelWarps; ++i) b = max(b, round_best[k & 1][i]);
-    if (tid == 0) out[k] = b;
-    if (mine == b && b) { last = b; rescan(); }
+  const int n = listed;
+  if (n > kSelList) {
+    const long long first = max(begin, 0), end = min(static_cast<long long>(begin) + kSelChunks * kSelThreads * N, static_cast<long long>(V));
+    select_by_rounds<T>(x, first, end, K, out);
+    return;
   }
-  if (tid == 0) {
-    float t = warp_tops[0];
-    for (int i = 1; i < kSelWarps; ++i) t = fmaxf(t, warp_tops[i]);
-    double all = 0.0;
-    for (int i = 0; i < kSelWarps; ++i) all += warp_sums[i] * (warp_tops[i] == -INFINITY ? 1.0 : static_cast<double>(ex2((warp_tops[i] - t) * kLog2e)));
-    p.sums[static_cast<size_t>(row) * p.segments + seg] = SegmentSum{all, t, 0.f};
+  for (int i = tid; i < n; i += kSelThreads) {
+    const uint64_t mine = list[i];
+    int above = 0;
+    for (int q = 0; q < n; ++q) above += list[q] > mine;
+    if (above < K) out[above] = mine;
   }
+  for (int i = n + tid; i < K; i += kSelThreads) out[i] = 0;
 }
 
-struct Best { double score; long long flat; };       // flat: beam * vocab + token, -1: none
-__device__ __forceinline__ bool better(const Best& x, const Best& y) {
-  if (x.flat < 0 || y.flat < 0) return x.flat >= 0;
-  return x.score > y.score || (x.score == y.score && x.flat < y.flat);
+// A candidate of the join: its score in 64 bits, ordered as an unsigned number (0: none), and where it stands, beam * vocab + token.
+struct Candidate { uint64_t order; long long flat; };
+__device__ __forceinline__ bool better(const Candidate& x, const Candidate& y) { return x.order > y.order || (x.order == y.order && x.order && x.flat < y.flat); }
+__device__ __forceinline__ uint64_t order_of(double x) {
+  const uint64_t u = static_cast<uint64_t>(__double_as_longlong(x + 0.0));
+  return u ^ ((u >> 63) ? ~0ull : 0x8000000000000000ull);
+}
+__device__ __forceinline__ double score_of(uint64_t order) {
+  return __longlong_as_double(static_cast<long long>(order ^ ((order >> 63) ? 0x8000000000000000ull : ~0ull)));
 }
 
-// One group: log-sum-exp of its rows, then its n_select best, one a round, off the heads of the segments' ordered lists.
+// One group: log-sum-exp of its rows, then the n_select best of its segments' candidates, found as in the segments: a threshold from
+// the best of every four threads, a list of what is not below it, ranks counted in the list.
+constexpr int kJoinList = 512;
 __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_constant__ SelectParams p) {
-  __shared__ double lse[kWidth];
+  __shared__ double lse[kWidth], base[kWidth];
   __shared__ int kind[kWidth];                    // 0: offers nothing, 1: live, 2: finished
-  __shared__ Best round_best[2][kSelWarps];
-  extern __shared__ unsigned char head[];         // [width * segments]: candidates of a list that are gone
+  __shared__ uint64_t group_top[kSelGroups];
+  __shared__ Candidate list[kJoinList];
+  __shared__ Candidate round_best[2][kSelWarps];
+  __shared__ uint64_t threshold;
+  __shared__ int listed;
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int W = p.a.width, S = p.segments, K = p.a.n_select, lists = W * S;
-  for (int l = tid; l < lists; l += kSelThreads) head[l] = 0;
+  const int W = p.a.width, S = p.segments, K = p.a.n_select;
+  if (tid == 0) listed = 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   for (int w = warp; w < W; w += kSelWarps) {
     const int row = g * W + w;
@@ -188,13 +240,14 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
     double l = 0.0;
     if (p.a.done && __ldg(p.a.done + row) != 0) what = 2;
     else if (score > -INFINITY) {
-      const SegmentSum* seg = p.sums + static_cast<size_t>(row) * S;
+      const int parts = S * kSelWarps;
+      const SegmentSum* part = p.sums + static_cast<size_t>(row) * parts;
       float top = -INFINITY;
-      for (int i = lane; i < S; i += 32) top = fmaxf(top, seg[i].top);
+      for (int i = lane; i < parts; i += 32) top = fmaxf(top, part[i].top);
 #pragma unroll
       for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
       double sum = 0.0;
-      for (int i = lane; i < S; i += 32) sum += seg[i].top == -INFINITY ? seg[i].sum : seg[i].sum * exp(static_cast<double>(seg[i].top) - static_cast<double>(top));
+      for (int i = lane; i < parts; i += 32) sum += part[i].top == -INFINITY ? part[i].sum : part[i].sum * exp(static_cast<double>(part[i].top) - static_cast<double>(top));
 #pragma unroll
       for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
       bad = bad || !(sum < INFINITY);              // NaN
@@ -204,39 +257,81 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
     if (score == -INFINITY) what = 0;
     if (bad) what = 0;
     if (lane == 0) {
-      lse[w] = l; kind[w] = what;
+      lse[w] = l; base[w] = score; kind[w] = what;
       if (bad) atomicOr(p.a.status, MEPIC_DEV_BAD_LOGITS);
     }
   }
   __syncthreads();
-  auto head_of = [&](int l) {
-    const int w = l / S, s = l - w * S, h = head[l];
-    Best b{0.0, -1};
-    if (kind[w] == 0 || h >= K) return b;
-    const double score = static_cast<double>(__ldg(p.a.score + g * W + w));
-    if (kind[w] == 2) {
-      if (s == 0 && h == 0) b = Best{score, static_cast<long long>(w) * p.a.vocab + p.a.pad_token};
-      return b;
+  const uint64_t* keys = p.best + static_cast<size_t>(g) * W * S * K;
+  const int n = W * S * K, per = S * K;
+  auto candidate = [&](int i) {
+    const int w = i / per;
+    Candidate c{0, 0};
+    if (kind[w] == 1) {
+      const uint64_t key = keys[i];
+      if (key) c = Candidate{order_of(base[w] + (static_cast<double>(key_value(key)) - lse[w])), static_cast<long long>(w) * p.a.vocab + key_token(key)};
+    } else if (kind[w] == 2 && i == w * per) {
+      c = Candidate{order_of(base[w]), static_cast<long long>(w) * p.a.vocab + p.a.pad_token};
     }
-    const uint64_t key = p.best[(static_cast<size_t>(g * W + w) * S + s) * K + h];
-    if (key) b = Best{score + (static_cast<double>(key_value(key)) - lse[w]), static_cast<long long>(w) * p.a.vocab + key_token(key)};
-    return b;
+    return c;
   };
-  Best mine{0.0, -1};
-  int mine_list = -1;
-  auto rescan = [&]() {
-    mine = Best{0.0, -1};
-    for (int l = tid; l < lists; l += kSelThreads) {
-      const Best b = head_of(l);
-      if (better(b, mine)) { mine = b; mine_list = l; }
+  uint64_t top = 0;
+#pragma unroll 4
+  for (int i = tid; i < n; i += kSelThreads) top = max(top, candidate(i).order);
+  uint64_t wtop = max(top, __shfl_xor_sync(kFull, top, 1));
+  wtop = max(wtop, __shfl_xor_sync(kFull, wtop, 2));
+  if ((lane & 3) == 0) group_top[tid >> 2] = wtop;
+  __syncthreads();
+  if (tid < kSelGroups) {
+    const uint64_t mine = group_top[tid];
+    int above = 0;
+#pragma unroll 16
+    for (int q = 0; q < kSelGroups; ++q) above += group_top[q] > mine || (group_top[q] == mine && q < tid);
+    if (above == K - 1) threshold = mine;
+  }
+  __syncthreads();
+  const uint64_t least = threshold;
+  if (top >= least && top) {
+    for (int i = tid; i < n; i += kSelThreads) {
+      const Candidate c = candidate(i);
+      if (c.order >= least && c.order) {
+        const int at = atomicAdd(&listed, 1);
+        if (at < kJoinList) list[at] = c;
+      }
     }
+  }
+  __syncthreads();
+  auto write = [&](int k, const Candidate& c) {
+    const size_t at = static_cast<size_t>(g) * K + k;
+    const bool any = c.order != 0;
+    const int w = any ? static_cast<int>(c.flat / p.a.vocab) : -1, v = any ? static_cast<int>(c.flat - static_cast<long long>(w) * p.a.vocab) : -1;
+    const bool ended = any && (kind[w] == 2 || v == p.a.eos_token);
+    p.a.parent[at] = w; p.a.token[at] = v;
+    p.a.score_out[at] = any ? static_cast<float>(score_of(c.order)) : -INFINITY;
+    p.a.done_out[at] = ended; p.a.n_new[at] = any && !ended;
   };
-  rescan();
+  const int m = listed;
+  if (m <= kJoinList) {
+    for (int i = tid; i < m; i += kSelThreads) {
+      const Candidate mine = list[i];
+      int above = 0;
+      for (int q = 0; q < m; ++q) above += better(list[q], mine);
+      if (above < K) write(above, mine);
+    }
+    for (int k = m + tid; k < K; k += kSelThreads) write(k, Candidate{0, 0});
+    return;
+  }
+  // more candidates at one score than the list holds: one a round
+  Candidate last{~0ull, -1};
   for (int k = 0; k < K; ++k) {
-    Best b = mine;
+    Candidate b{0, 0};
+    for (int i = tid; i < n; i += kSelThreads) {
+      const Candidate c = candidate(i);
+      if (better(last, c) && better(c, b)) b = c;
+    }
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
-      const Best o{__shfl_xor_sync(kFull, b.score, d), __shfl_xor_sync(kFull, b.flat, d)};
+      const Candidate o{__shfl_xor_sync(kFull, b.order, d), __shfl_xor_sync(kFull, b.flat, d)};
       if (better(o, b)) b = o;
     }
     if (lane == 0) round_best[k & 1][warp] = b;
@@ -244,23 +339,16 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
     b = round_best[k & 1][0];
 #pragma unroll
     for (int i = 1; i < kSelWarps; ++i) if (better(round_best[k & 1][i], b)) b = round_best[k & 1][i];
-    if (tid == 0) {
-      const size_t at = static_cast<size_t>(g) * K + k;
-      const bool any = b.flat >= 0;
-      const int w = any ? static_cast<int>(b.flat / p.a.vocab) : -1, v = any ? static_cast<int>(b.flat - static_cast<long long>(w) * p.a.vocab) : -1;
-      const bool ended = any && (kind[w] == 2 || v == p.a.eos_token);
-      p.a.parent[at] = w; p.a.token[at] = v;
-      p.a.score_out[at] = any ? static_cast<float>(b.score) : -INFINITY;
-      p.a.done_out[at] = ended; p.a.n_new[at] = any && !ended;
-    }
-    if (b.flat >= 0 && mine.flat == b.flat) { ++head[mine_list]; rescan(); }
+    if (tid == 0) write(k, b);
+    last = b;
+    if (b.order == 0) last = Candidate{0, -1};      // nothing is below nothing
   }
 }
 
 // ---------------------------------------------------------------- fork
 // Two launches: the first finds, a CTA per group and stretch of entries, which pages nobody holds any more and how many copies a
-// group needs; in the second every CTA sums those counts up for itself and writes its share of the new tables, the reserve and
-// the copy list.
+// group needs.  The second copies the tables meanwhile (it is a programmatic dependent), and then every CTA sums the counts up for
+// itself and writes its share of the reserve and the copy list.
 constexpr int kForkThreads = 256;
 struct ForkParams {
   mepic_beam_fork_args_t a;
@@ -276,7 +364,7 @@ struct Group {
   unsigned copies;                       // new beams that copy
 };
 __device__ void load_group(const ForkParams& p, int g, Group& s, bool report) {
-  const int tid = threadIdx.x, Wi = p.a.width_in, Wo = p.a.width_out;
+  const int tid = threadIdx.x, Wi = p.a.width_in, Wo = p.a.width_out, P = 1 << p.page_shift;
   const long long room = min(static_cast<long long>(p.a.table_stride) << p.page_shift, 0x7fffffffll);
   if (tid == 0) s.copies = 0;
   if (tid < Wi) {
@@ -290,21 +378,19 @@ __device__ void load_group(const ForkParams& p, int g, Group& s, bool report) {
     s.parent[tid - 32] = q;
   }
   __syncthreads();
-  if (tid < Wo && s.parent[tid] >= 0) {
-    const int32_t* ids = p.a.page_ids + static_cast<size_t>(g) * Wi * p.a.table_stride;
-    const int n = s.len[s.parent[tid]], P = 1 << p.page_shift;
-    if (n & (P - 1)) {
-      const int e = n >> p.page_shift, page = __ldg(ids + static_cast<size_t>(s.parent[tid]) * p.a.table_stride + e);
-      const long long from = static_cast<long long>(e) << p.page_shift;
-      bool keeps = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages) && __ldg(p.a.owned + page) != 0;
-      for (int j = 0; j < Wo && keeps; ++j) {
-        if (j == tid || s.parent[j] < 0) continue;
-        const int m = s.len[s.parent[j]];
-        if (m <= from || __ldg(ids + static_cast<size_t>(s.parent[j]) * p.a.table_stride + e) != page) continue;
-        keeps = j > tid && m < from + P;
-      }
-      if (!keeps) atomicOr(&s.copies, 1u << tid);
-    }
+  // every pair of new beams side by side: does j keep k from keeping its partly filled last page?
+  const int32_t* ids = p.a.page_ids + static_cast<size_t>(g) * Wi * p.a.table_stride;
+  for (int i = tid; i < Wo * Wo; i += kForkThreads) {
+    const int k = i / Wo, j = i - k * Wo;
+    if (s.parent[k] < 0 || s.parent[j] < 0) continue;
+    const int n = s.len[s.parent[k]], e = n >> p.page_shift;
+    if ((n & (P - 1)) == 0) continue;
+    const int page = __ldg(ids + static_cast<size_t>(s.parent[k]) * p.a.table_stride + e);
+    const long long from = static_cast<long long>(e) << p.page_shift, m = s.len[s.parent[j]];
+    bool lost;
+    if (j == k) lost = static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages) || __ldg(p.a.owned + page) == 0;
+    else lost = m > from && (j < k || m >= from + P) && __ldg(ids + static_cast<size_t>(s.parent[j]) * p.a.table_stride + e) == page;
+    if (lost) atomicOr(&s.copies, 1u << k);
   }
   __syncthreads();
 }
@@ -312,6 +398,7 @@ __device__ void load_group(const ForkParams& p, int g, Group& s, bool report) {
 __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_count(const __grid_constant__ ForkParams p) {
   __shared__ Group s;
   __shared__ int warp_n[kForkThreads / 32];
+  extern __shared__ int at_entry[];              // [width_in][kForkThreads]: what the beams hold at a thread's entry
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int g = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int Wi = p.a.width_in, Wo = p.a.width_out, stride = p.a.table_stride;
@@ -331,15 +418,23 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_count(const __gr
     unsigned back = 0;
     if (e < e_end) {
       const long long from = static_cast<long long>(e) << p.page_shift;
+      // what all beams hold here, asked for side by side
+      for (int q0 = 0; q0 < Wi; q0 += 8) {
+        int page[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) page[q] = q0 + q < Wi && s.len[q0 + q] > from ? __ldg(ids + static_cast<size_t>(q0 + q) * stride + e) : -1;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) if (q0 + q < Wi) at_entry[(q0 + q) * kForkThreads + tid] = page[q];
+      }
       for (unsigned m = dropped; m; m &= m - 1) {
         const int r = __ffs(m) - 1;
         if (s.len[r] <= from) continue;
-        const int page = __ldg(ids + static_cast<size_t>(r) * stride + e);
+        const int page = at_entry[r * kForkThreads + tid];
         if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) { atomicOr(p.a.status, MEPIC_DEV_BAD_PAGE); continue; }
         bool held = false;                          // by a beam that goes on, or by an earlier one that does not
-        for (unsigned o = kept | (dropped & ((1u << r) - 1)); o && !held; o &= o - 1) {
+        for (unsigned o = kept | (dropped & ((1u << r) - 1)); o; o &= o - 1) {
           const int q = __ffs(o) - 1;
-          held = s.len[q] > from && __ldg(ids + static_cast<size_t>(q) * stride + e) == page;
+          held = held || (s.len[q] > from && at_entry[q * kForkThreads + tid] == page);
         }
         if (!held && __ldg(p.a.owned + page) != 0) back |= 1u << r;
       }
@@ -355,7 +450,7 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_count(const __gr
       if (w < warp) at += warp_n[w];
       total += warp_n[w];
     }
-    for (; back; back &= back - 1) out[at++] = __ldg(ids + static_cast<size_t>(__ffs(back) - 1) * stride + e);
+    for (; back; back &= back - 1) out[at++] = at_entry[(__ffs(back) - 1) * kForkThreads + tid];
     __syncthreads();
   }
   if (tid == 0) p.n_freed[g * p.stretches + part] = total;
@@ -389,14 +484,38 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_write(const __gr
   const int Wi = p.a.width_in, Wo = p.a.width_out, stride = p.a.table_stride, groups = p.a.groups, S = p.stretches;
   int* freed_at = sums;                              // [groups * stretches + 1]
   int* copies_at = sums + groups * S + 1;            // [groups + 1]
+  const int part = blockIdx.y, parts = gridDim.y;
   load_group(p, g, s, false);
+  // ---- tables: they do not depend on the counts, but for the pages of the copies; four rows side by side
+  for (int k0 = 0; k0 < Wo; k0 += 4) {
+    int ents[4], most = 0;
+    size_t from[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int parent = k0 + k < Wo ? s.parent[k0 + k] : -1;
+      ents[k] = parent >= 0 ? static_cast<int>((static_cast<long long>(s.len[parent]) + (1 << p.page_shift) - 1) >> p.page_shift) : 0;
+      from[k] = (static_cast<size_t>(g) * Wi + max(parent, 0)) * stride;
+      most = max(most, ents[k]);
+    }
+    for (int e = part * kForkThreads + tid; e < most; e += parts * kForkThreads) {
+      int page[4], pos[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) if (e < ents[k]) { page[k] = __ldg(p.a.page_ids + from[k] + e); pos[k] = __ldg(p.a.pos_base + from[k] + e); }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (e < ents[k]) {
+          const size_t to = (static_cast<size_t>(g) * Wo + k0 + k) * stride + e;
+          p.a.page_ids_out[to] = page[k]; p.a.pos_base_out[to] = pos[k];
+        }
+    }
+  }
+  __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   running_sums(p.n_freed, groups * S, freed_at);
   running_sums(p.n_copies, groups, copies_at);
   const long long used = __ldg(p.a.reserve_used), n_freed = freed_at[groups * S], n_copies = copies_at[groups];
   const bool bad = used < 0 || used > p.a.n_reserve || n_freed > used, full = !bad && used - n_freed + n_copies > p.a.n_reserve;
   const bool ok = !bad && !full;
-  const int part = blockIdx.y, parts = gridDim.y;
   // ---- the counts, and the unused end of the copy list
   if (g == 0 && part == 0 && tid == 0) {
     if (bad) atomicOr(p.a.status, MEPIC_DEV_BAD_BEAM);
@@ -440,17 +559,10 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_write(const __gr
     }
   }
   __syncthreads();
-  // ---- tables
-  for (int k = 0; k < Wo; ++k) {
-    if (s.parent[k] < 0) continue;
-    const int n = s.len[s.parent[k]], ents = static_cast<int>((static_cast<long long>(n) + (1 << p.page_shift) - 1) >> p.page_shift);
-    const size_t from = (static_cast<size_t>(g) * Wi + s.parent[k]) * stride, to = (static_cast<size_t>(g) * Wo + k) * stride;
-    const bool swap = s.copies >> k & 1;
-    for (int e = part * kForkThreads + tid; e < ents; e += parts * kForkThreads) {
-      const int page = __ldg(p.a.page_ids + from + e);
-      p.a.page_ids_out[to + e] = swap && e == ents - 1 ? fresh[k] : page;
-      p.a.pos_base_out[to + e] = __ldg(p.a.pos_base + from + e);
-    }
+  // ---- the copies' places in the tables (this CTA wrote them above with the parents' pages)
+  if (tid < Wo && (s.copies >> tid & 1)) {
+    const int last = s.len[s.parent[tid]] >> p.page_shift;
+    if (last / kForkThreads % parts == part) p.a.page_ids_out[(static_cast<size_t>(g) * Wo + tid) * stride + last] = fresh[tid];
   }
 }
 
@@ -522,7 +634,7 @@ bool select_shape_ok(int32_t groups, int32_t width, int32_t n_select, int32_t vo
 }
 size_t select_bytes(int32_t groups, int32_t width, int32_t n_select, int segments) {
   const size_t rows = static_cast<size_t>(groups) * width;
-  return up16(rows * segments * sizeof(SegmentSum)) + up16(rows * segments * n_select * sizeof(uint64_t));
+  return up16(rows * segments * kSelWarps * sizeof(SegmentSum)) + up16(rows * segments * n_select * sizeof(uint64_t));
 }
 
 // how the entries of a group are cut for the first launch of a fork: enough CTAs to fill the GPU, few enough counts to sum up
@@ -600,18 +712,14 @@ extern "C" int32_t mepic_beam_select(const mepic_beam_select_args_t* a, void* cu
   const size_t need = select_bytes(a->groups, a->width, a->n_select, p.segments), rows = static_cast<size_t>(a->groups) * a->width;
   if (a->workspace_bytes < need) { mepic_set_error("beam_select: workspace of %zu bytes, %zu needed", a->workspace_bytes, need); return MEPIC_E_INVAL; }
   p.sums = static_cast<SegmentSum*>(a->workspace);
-  p.best = reinterpret_cast<uint64_t*>(static_cast<unsigned char*>(a->workspace) + up16(rows * p.segments * sizeof(SegmentSum)));
+  p.best = reinterpret_cast<uint64_t*>(static_cast<unsigned char*>(a->workspace) + up16(rows * p.segments * kSelWarps * sizeof(SegmentSum)));
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const dim3 grid(p.segments, static_cast<unsigned>(rows));
   if (a->logits_type == MEPIC_LOGITS_BF16) mepic_beam_segments<__nv_bfloat16><<<grid, kSelThreads, 0, st>>>(p);
   else if (a->logits_type == MEPIC_LOGITS_FP16) mepic_beam_segments<__half><<<grid, kSelThreads, 0, st>>>(p);
   else mepic_beam_segments<float><<<grid, kSelThreads, 0, st>>>(p);
   cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess) {
-    const size_t smem = static_cast<size_t>(a->width) * p.segments;
-    if (smem > 40 * 1024) e = cudaFuncSetAttribute(mepic_beam_join, cudaFuncAttributeMaxDynamicSharedMemorySize, kWidth * segments_of(1 << 24, MEPIC_LOGITS_FP32));
-    if (e == cudaSuccess) e = launch_dependent(mepic_beam_join, dim3(a->groups), dim3(kSelThreads), smem, st, p);
-  }
+  if (e == cudaSuccess) e = launch_dependent(mepic_beam_join, dim3(a->groups), dim3(kSelThreads), st, p);
   return launched("beam_select", e, 2);
 }
 
@@ -650,7 +758,7 @@ extern "C" int32_t mepic_beam_fork(const mepic_config_t* cfg, const mepic_beam_f
   if (smem > 40 * 1024) e = cudaFuncSetAttribute(mepic_beam_fork_write, cudaFuncAttributeMaxDynamicSharedMemorySize, (2 * MEPIC_STEP_MAX_BATCH + 2) * static_cast<int>(sizeof(int)));
   if (e != cudaSuccess) { mepic_set_error("beam_fork: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  mepic_beam_fork_count<<<dim3(a->groups, p.stretches), kForkThreads, 0, st>>>(p);
+  mepic_beam_fork_count<<<dim3(a->groups, p.stretches), kForkThreads, static_cast<size_t>(a->width_in) * kForkThreads * sizeof(int), st>>>(p);
   e = cudaGetLastError();
   // entries of a group's tables: a few per thread
   const int parts = std::max(1, std::min((a->table_stride + kForkThreads - 1) / kForkThreads, std::max(1, 592 / a->groups)));

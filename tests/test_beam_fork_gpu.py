@@ -76,7 +76,7 @@ class Tables:
         rows = parent.size
         if want["status"]:
             assert (got["kv_len"] == 0).all() and got["n_copies"][0] == 0 and got["reserve_used"][0] == self.used
-            assert (ids == -9).all() and (base == -9).all() and (got["copy_src"] == -1).all() and (got["copy_dst"] == -1).all()
+            assert (got["copy_src"] == -1).all() and (got["copy_dst"] == -1).all() and (got["copy_slots"] == -1).all()
             assert (self.d["reserve"].cpu().numpy() == self.reserve).all()
             return want
         for r, (p, b, n) in enumerate(want["rows"]):
