@@ -10,6 +10,7 @@
 #include "mepic.h"
 #include "mepic_internal.h"
 #include "mepic_ptx.cuh"
+#include "mepic_tcgen05.cuh"      // arithmetic on pairs of floats
 
 namespace {
 
@@ -143,14 +144,18 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_segments(const __grid_
     for (int i = 0; i < N; ++i) top = fmaxf(top, v[i]);
   }
   const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
+  float2 sum2 = make_float2(0.f, 0.f);
 #pragma unroll
   for (int k = 0; k < kSelChunks; ++k) {
     float v[N];
     widen<T>(c[k], v);
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum += ex2((v[i] - ref) * kLog2e);      // +infinity - +infinity and NaN - anything: NaN
+    for (int i = 0; i < N; i += 2) {
+      const float2 d = mul2(add2(make_float2(v[i], v[i + 1]), make_float2(-ref, -ref)), make_float2(kLog2e, kLog2e));
+      sum2 = add2(sum2, make_float2(ex2(d.x), ex2(d.y)));      // +infinity - +infinity and NaN - anything: NaN
+    }
   }
+  const float sum = sum2.x + sum2.y;
   // ---- maximum and sum of the segment, maxima of four threads together
   float wtop = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
   wtop = fmaxf(wtop, __shfl_xor_sync(kFull, wtop, 2));
@@ -163,24 +168,31 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_segments(const __grid_
   if (lane == 0) p.sums[(static_cast<size_t>(row) * p.segments + seg) * kSelWarps + warp] = SegmentSum{s, wtop, 0.f};
   __syncthreads();
   const int K = p.a.n_select;
-  if (tid < kSelGroups) {
-    const uint32_t mine = group_top[tid];
+  {
+    // ranks of the 64 maxima, four threads a maximum
+    const int i = tid >> 2, q0 = (tid & 3) * (kSelGroups / 4);
+    const uint32_t mine = group_top[i];
     int above = 0;
 #pragma unroll
-    for (int q = 0; q < kSelGroups; q += 4) {
+    for (int q = q0; q < q0 + kSelGroups / 4; q += 4) {
       const uint4 o = *reinterpret_cast<const uint4*>(group_top + q);
-      above += (o.x > mine || (o.x == mine && q < tid)) + (o.y > mine || (o.y == mine && q + 1 < tid)) +
-               (o.z > mine || (o.z == mine && q + 2 < tid)) + (o.w > mine || (o.w == mine && q + 3 < tid));
+      above += (o.x > mine || (o.x == mine && q < i)) + (o.y > mine || (o.y == mine && q + 1 < i)) +
+               (o.z > mine || (o.z == mine && q + 2 < i)) + (o.w > mine || (o.w == mine && q + 3 < i));
     }
-    if (above == K - 1) threshold = mine;
+    above += __shfl_xor_sync(kFull, above, 1);
+    above += __shfl_xor_sync(kFull, above, 2);
+    if ((tid & 3) == 0 && above == K - 1) threshold = mine;
   }
   __syncthreads();
   const uint32_t least = threshold;
   if (order_of(top) >= least && top > -INFINITY) {
 #pragma unroll
     for (int k = 0; k < kSelChunks; ++k) {
-      float v[N];
+      float v[N], most = -INFINITY;
       widen<T>(c[k], v);
+#pragma unroll
+      for (int i = 0; i < N; ++i) most = fmaxf(most, v[i]);
+      if (order_of(most) < least) continue;
 #pragma unroll
       for (int i = 0; i < N; ++i)
         if (order_of(v[i]) >= least && v[i] > -INFINITY) {
@@ -220,6 +232,7 @@ __device__ __forceinline__ double score_of(uint64_t order) {
 // One group: log-sum-exp of its rows, then the n_select best of its segments' candidates, found as in the segments: a threshold from
 // the best of every four threads, a list of what is not below it, ranks counted in the list.
 constexpr int kJoinList = 512;
+constexpr int kJoinBatch = 8;
 __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_constant__ SelectParams p) {
   __shared__ double lse[kWidth], base[kWidth];
   __shared__ int kind[kWidth];                    // 0: offers nothing, 1: live, 2: finished
@@ -230,8 +243,18 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   __shared__ int listed;
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int W = p.a.width, S = p.segments, K = p.a.n_select;
+  const uint64_t* keys = p.best + static_cast<size_t>(g) * W * S * K;
+  const int n = W * S * K, per = S * K;
+  const float inv_per = 1.f / static_cast<float>(per);
   if (tid == 0) listed = 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  // the candidates of a batch, side by side; the first batch is on its way while the sums are taken together
+  uint64_t key[kJoinBatch];
+  auto load_batch = [&](int i0) {
+#pragma unroll
+    for (int k = 0; k < kJoinBatch; ++k) key[k] = i0 + k * kSelThreads + tid < n ? keys[i0 + k * kSelThreads + tid] : 0;
+  };
+  load_batch(0);
   for (int w = warp; w < W; w += kSelWarps) {
     const int row = g * W + w;
     const float score = __ldg(p.a.score + row);
@@ -262,13 +285,11 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
     }
   }
   __syncthreads();
-  const uint64_t* keys = p.best + static_cast<size_t>(g) * W * S * K;
-  const int n = W * S * K, per = S * K;
-  auto candidate = [&](int i) {
-    const int w = i / per;
+  auto candidate = [&](int i, uint64_t key) {
+    int w = static_cast<int>(static_cast<float>(i) * inv_per);      // i / per, corrected
+    w += i - w * per >= per ? 1 : i < w * per ? -1 : 0;
     Candidate c{0, 0};
     if (kind[w] == 1) {
-      const uint64_t key = keys[i];
       if (key) c = Candidate{order_of(base[w] + (static_cast<double>(key_value(key)) - lse[w])), static_cast<long long>(w) * p.a.vocab + key_token(key)};
     } else if (kind[w] == 2 && i == w * per) {
       c = Candidate{order_of(base[w]), static_cast<long long>(w) * p.a.vocab + p.a.pad_token};
@@ -276,27 +297,42 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
     return c;
   };
   uint64_t top = 0;
-#pragma unroll 4
-  for (int i = tid; i < n; i += kSelThreads) top = max(top, candidate(i).order);
+  for (int i0 = 0; i0 < n; i0 += kJoinBatch * kSelThreads) {
+    if (i0) load_batch(i0);
+#pragma unroll
+    for (int k = 0; k < kJoinBatch; ++k) {
+      const int i = i0 + k * kSelThreads + tid;
+      if (i < n) top = max(top, candidate(i, key[k]).order);
+    }
+  }
   uint64_t wtop = max(top, __shfl_xor_sync(kFull, top, 1));
   wtop = max(wtop, __shfl_xor_sync(kFull, wtop, 2));
   if ((lane & 3) == 0) group_top[tid >> 2] = wtop;
   __syncthreads();
-  if (tid < kSelGroups) {
-    const uint64_t mine = group_top[tid];
+  {
+    const int i = tid >> 2, q0 = (tid & 3) * (kSelGroups / 4);
+    const uint64_t mine = group_top[i];
     int above = 0;
-#pragma unroll 16
-    for (int q = 0; q < kSelGroups; ++q) above += group_top[q] > mine || (group_top[q] == mine && q < tid);
-    if (above == K - 1) threshold = mine;
+#pragma unroll
+    for (int q = q0; q < q0 + kSelGroups / 4; ++q) above += group_top[q] > mine || (group_top[q] == mine && q < i);
+    above += __shfl_xor_sync(kFull, above, 1);
+    above += __shfl_xor_sync(kFull, above, 2);
+    if ((tid & 3) == 0 && above == K - 1) threshold = mine;
   }
   __syncthreads();
   const uint64_t least = threshold;
   if (top >= least && top) {
-    for (int i = tid; i < n; i += kSelThreads) {
-      const Candidate c = candidate(i);
-      if (c.order >= least && c.order) {
-        const int at = atomicAdd(&listed, 1);
-        if (at < kJoinList) list[at] = c;
+    for (int i0 = 0; i0 < n; i0 += kJoinBatch * kSelThreads) {
+      if (n > kJoinBatch * kSelThreads) load_batch(i0);
+#pragma unroll
+      for (int k = 0; k < kJoinBatch; ++k) {
+        const int i = i0 + k * kSelThreads + tid;
+        if (i >= n) continue;
+        const Candidate c = candidate(i, key[k]);
+        if (c.order >= least && c.order) {
+          const int at = atomicAdd(&listed, 1);
+          if (at < kJoinList) list[at] = c;
+        }
       }
     }
   }
@@ -326,7 +362,7 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   for (int k = 0; k < K; ++k) {
     Candidate b{0, 0};
     for (int i = tid; i < n; i += kSelThreads) {
-      const Candidate c = candidate(i);
+      const Candidate c = candidate(i, keys[i]);
       if (better(last, c) && better(c, b)) b = c;
     }
 #pragma unroll
@@ -639,7 +675,7 @@ size_t select_bytes(int32_t groups, int32_t width, int32_t n_select, int segment
 
 // how the entries of a group are cut for the first launch of a fork: enough CTAs to fill the GPU, few enough counts to sum up
 void fork_cut(int groups, int table_stride, int* stretches, int* stretch) {
-  int n = std::max(1, std::min((table_stride + 511) / 512, 1024 / std::max(1, groups)));
+  int n = std::max(1, std::min((table_stride + kForkThreads - 1) / kForkThreads, 1024 / std::max(1, groups)));
   int len = (table_stride + n - 1) / n;
   len = (len + kForkThreads - 1) / kForkThreads * kForkThreads;
   *stretch = len;
