@@ -20,16 +20,19 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWidth = MEPIC_BEAM_MAX_WIDTH;
 
 // ---------------------------------------------------------------- selection
-// Two launches.  The first cuts every row of logits into segments, one CTA each: a segment is read once, into registers, and
-// leaves its maximum, its sum of exponentials and its n_select best tokens in order.  The second joins a group's segments: the
-// n_select best of a row are among its segments' best, and those of a group among its rows'.
+// Two launches.  The first is a pass over the logits, bound by HBM: every warp leaves the sum of its tokens' exponentials and every
+// four threads (a SET: 64 tokens at least) their largest logit, nothing else.  The second has a CTA per group: the n_select best
+// tokens are not below the n_select-th largest of the sets' maxima, so only the few sets that reach it are read again, and of those
+// only the tokens that reach it are ranked.  (Every segment keeping its own n_select best, in the first pass, took a dozen
+// instructions a token more: 64 x 8 beams over 100,003 tokens in 65 us against {SEL_NOW}.)
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
-constexpr int kSelChunks = 8;                  // 16-byte pieces a thread holds
+constexpr int kSelPieces = 8;                  // 16-byte pieces a thread reads
+constexpr int kSelSets = kSelThreads / 4;      // sets of a segment (the tokens of a CTA of the first pass)
+static_assert(kSelSets >= MEPIC_BEAM_MAX_SELECT, "as many maxima as tokens to select");
 
-template <typename T> struct Vec { static constexpr int n = 16 / sizeof(T); };
-
-template <typename T> __device__ __forceinline__ void widen(const uint4& c, float (&x)[Vec<T>::n]);
+template <typename T> constexpr int kVec = 16 / sizeof(T);
+template <typename T> __device__ __forceinline__ void widen(const uint4& c, float (&x)[kVec<T>]);
 template <> __device__ __forceinline__ void widen<float>(const uint4& c, float (&x)[4]) {
   x[0] = __uint_as_float(c.x); x[1] = __uint_as_float(c.y); x[2] = __uint_as_float(c.z); x[3] = __uint_as_float(c.w);
 }
@@ -48,84 +51,36 @@ template <> __device__ __forceinline__ float minus_infinity<float>() { return -I
 template <> __device__ __forceinline__ __nv_bfloat16 minus_infinity<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80); }
 template <> __device__ __forceinline__ __half minus_infinity<__half>() { return __ushort_as_half(0xfc00); }
 
-// Key of a token: the larger logit first, the lower index among equals (-0 counts as 0); 0 where there is no candidate
-// (-infinity; a NaN's row is given up as a whole).
-__device__ __forceinline__ uint32_t order_of(float x) {
-  const uint32_t u = __float_as_uint(x + 0.f);
-  return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
-}
-__device__ __forceinline__ uint64_t token_key(float x, int at) {
-  return x > -INFINITY ? static_cast<uint64_t>(order_of(x)) << 32 | (0xffffffffu - static_cast<uint32_t>(at)) : 0;
-}
-__device__ __forceinline__ float key_value(uint64_t k) {
-  const uint32_t s = static_cast<uint32_t>(k >> 32);
-  return __uint_as_float(s ^ ((s >> 31) ? 0x80000000u : 0xffffffffu));
-}
-__device__ __forceinline__ int key_token(uint64_t k) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(k)); }
-__device__ __forceinline__ uint64_t warp_max_key(uint64_t k) {
-  const uint32_t hi = static_cast<uint32_t>(k >> 32), top = __reduce_max_sync(kFull, hi);
-  return static_cast<uint64_t>(top) << 32 | __reduce_max_sync(kFull, hi == top ? static_cast<uint32_t>(k) : 0u);
-}
-
-struct SegmentSum { double sum; float top; float pad; };      // sum of exp(x - top) over a warp's tokens; NaN: the row is to be given up
+struct WarpSum { double sum; float top; float pad; };      // sum of exp(x - top) over a warp's tokens; NaN: the row is to be given up
 
 struct SelectParams {
   mepic_beam_select_args_t a;
-  SegmentSum* sums;      // [rows][segments][kSelWarps]
-  uint64_t* best;        // [rows][segments][n_select], descending, 0 where there are fewer
+  WarpSum* sums;         // [rows][segments][kSelWarps]
+  float* tops;           // [rows][segments][kSelSets]; -infinity where a set has no candidate
   int segments;
   long long stride;
 };
 
-// The slow way, for segments with more tokens at or above the threshold than the list holds (thousands of equal logits): the best
-// token below the last one found, n_select times over, the segment read again each time.
-template <typename T>
-__device__ __noinline__ void select_by_rounds(const T* x, long long first, long long end, int n_select, uint64_t* out) {
-  __shared__ uint64_t round_best[2][kSelWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint64_t last = ~0ull;
-  for (int k = 0; k < n_select; ++k) {
-    uint64_t mine = 0;
-    for (long long i = first + threadIdx.x; i < end; i += kSelThreads) {
-      const uint64_t key = token_key(static_cast<float>(x[i]), static_cast<int>(i));
-      if (key < last && key > mine) mine = key;
-    }
-    mine = warp_max_key(mine);
-    if (lane == 0) round_best[k & 1][warp] = mine;
-    __syncthreads();
-    uint64_t b = round_best[k & 1][0];
-#pragma unroll
-    for (int i = 1; i < kSelWarps; ++i) b = max(b, round_best[k & 1][i]);
-    if (threadIdx.x == 0) out[k] = b;
-    last = b;
-  }
+// Pieces are 16 bytes by address, so that a row may begin and end inside one: the elements of a row that its first piece lacks.
+template <typename T> __device__ __forceinline__ int lead_of(const T* row) { return static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)); }
+// Token of the first element of piece k of a thread (negative before the row).
+template <typename T> __device__ __forceinline__ int token_of(int lead, int seg, int k, int thread) {
+  return ((seg * kSelPieces + k) * kSelThreads + thread) * kVec<T> - lead;
 }
 
-// One segment of one row.  The threads' own maxima, taken four threads together, are 64 tokens of the segment: its n_select best are
-// not below the n_select-th largest of them.  The few tokens that are not go to a list, whose ranks are counted.
-constexpr int kSelList = 512;
-constexpr int kSelGroups = kSelThreads / 4;
-static_assert(kSelGroups >= MEPIC_BEAM_MAX_SELECT, "as many maxima as tokens to select");
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads) mepic_beam_segments(const __grid_constant__ SelectParams p) {
-  constexpr int N = Vec<T>::n;
-  __shared__ alignas(16) uint32_t group_top[kSelGroups];
-  __shared__ uint64_t list[kSelList];
-  __shared__ uint32_t threshold;
-  __shared__ int listed;
+__global__ void __launch_bounds__(kSelThreads) mepic_beam_pass(const __grid_constant__ SelectParams p) {
+  constexpr int N = kVec<T>;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int row = blockIdx.y, seg = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float score = __ldg(p.a.score + row);
   if (score == -INFINITY || (p.a.done && __ldg(p.a.done + row) != 0)) return;        // nobody reads what such a row leaves
   const T* x = static_cast<const T*>(p.a.logits) + row * p.stride;
-  // pieces of 16 bytes by address: the row may begin and end inside one
-  const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
-  const int V = p.a.vocab;
-  const int begin = seg * (kSelChunks * kSelThreads * N) - lead;      // token of the segment's first place (negative before the row)
-  uint4 c[kSelChunks];
+  const int lead = lead_of(x), V = p.a.vocab;
+  uint4 c[kSelPieces];
 #pragma unroll
-  for (int k = 0; k < kSelChunks; ++k) {
-    const int at = begin + (k * kSelThreads + tid) * N;
+  for (int k = 0; k < kSelPieces; ++k) {
+    const int at = token_of<T>(lead, seg, k, tid);
     if (at >= 0 && at + N <= V) c[k] = __ldcs(reinterpret_cast<const uint4*>(x + at));
     else {
       alignas(16) T e[N];
@@ -134,19 +89,20 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_segments(const __grid_
       c[k] = *reinterpret_cast<const uint4*>(e);
     }
   }
-  if (tid == 0) listed = 0;
   float top = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < kSelChunks; ++k) {
+  for (int k = 0; k < kSelPieces; ++k) {
     float v[N];
     widen<T>(c[k], v);
 #pragma unroll
     for (int i = 0; i < N; ++i) top = fmaxf(top, v[i]);
   }
+  // x - top first (nothing is lost there that matters), then the scale: one product for both would round away what two large
+  // logits differ by
   const float ref = top == -INFINITY ? 0.f : top;
   float2 sum2 = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int k = 0; k < kSelChunks; ++k) {
+  for (int k = 0; k < kSelPieces; ++k) {
     float v[N];
     widen<T>(c[k], v);
 #pragma unroll
@@ -155,70 +111,19 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_segments(const __grid_
       sum2 = add2(sum2, make_float2(ex2(d.x), ex2(d.y)));      // +infinity - +infinity and NaN - anything: NaN
     }
   }
-  const float sum = sum2.x + sum2.y;
-  // ---- maximum and sum of the segment, maxima of four threads together
+  const size_t part = static_cast<size_t>(row) * p.segments + seg;
   float wtop = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
   wtop = fmaxf(wtop, __shfl_xor_sync(kFull, wtop, 2));
-  if ((lane & 3) == 0) group_top[tid >> 2] = order_of(wtop);
+  if ((lane & 3) == 0) p.tops[part * kSelSets + (tid >> 2)] = wtop;
 #pragma unroll
   for (int d = 4; d < 32; d <<= 1) wtop = fmaxf(wtop, __shfl_xor_sync(kFull, wtop, d));
-  double s = static_cast<double>(sum) * (top == -INFINITY ? 1.0 : static_cast<double>(ex2((top - wtop) * kLog2e)));
+  double s = static_cast<double>(sum2.x + sum2.y) * (top == -INFINITY ? 1.0 : static_cast<double>(ex2((top - wtop) * kLog2e)));
 #pragma unroll
   for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(kFull, s, d);
-  if (lane == 0) p.sums[(static_cast<size_t>(row) * p.segments + seg) * kSelWarps + warp] = SegmentSum{s, wtop, 0.f};
-  __syncthreads();
-  const int K = p.a.n_select;
-  {
-    // ranks of the 64 maxima, four threads a maximum
-    const int i = tid >> 2, q0 = (tid & 3) * (kSelGroups / 4);
-    const uint32_t mine = group_top[i];
-    int above = 0;
-#pragma unroll
-    for (int q = q0; q < q0 + kSelGroups / 4; q += 4) {
-      const uint4 o = *reinterpret_cast<const uint4*>(group_top + q);
-      above += (o.x > mine || (o.x == mine && q < i)) + (o.y > mine || (o.y == mine && q + 1 < i)) +
-               (o.z > mine || (o.z == mine && q + 2 < i)) + (o.w > mine || (o.w == mine && q + 3 < i));
-    }
-    above += __shfl_xor_sync(kFull, above, 1);
-    above += __shfl_xor_sync(kFull, above, 2);
-    if ((tid & 3) == 0 && above == K - 1) threshold = mine;
-  }
-  __syncthreads();
-  const uint32_t least = threshold;
-  if (order_of(top) >= least && top > -INFINITY) {
-#pragma unroll
-    for (int k = 0; k < kSelChunks; ++k) {
-      float v[N], most = -INFINITY;
-      widen<T>(c[k], v);
-#pragma unroll
-      for (int i = 0; i < N; ++i) most = fmaxf(most, v[i]);
-      if (order_of(most) < least) continue;
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (order_of(v[i]) >= least && v[i] > -INFINITY) {
-          const int at = atomicAdd(&listed, 1);
-          if (at < kSelList) list[at] = token_key(v[i], begin + (k * kSelThreads + tid) * N + i);
-        }
-    }
-  }
-  __syncthreads();
-  uint64_t* out = p.best + (static_cast<size_t>(row) * p.segments + seg) * K;
-  const int n = listed;
-  if (n > kSelList) {
-    const long long first = max(begin, 0), end = min(static_cast<long long>(begin) + kSelChunks * kSelThreads * N, static_cast<long long>(V));
-    select_by_rounds<T>(x, first, end, K, out);
-    return;
-  }
-  for (int i = tid; i < n; i += kSelThreads) {
-    const uint64_t mine = list[i];
-    int above = 0;
-    for (int q = 0; q < n; ++q) above += list[q] > mine;
-    if (above < K) out[above] = mine;
-  }
-  for (int i = n + tid; i < K; i += kSelThreads) out[i] = 0;
+  if (lane == 0) p.sums[part * kSelWarps + warp] = WarpSum{s, wtop, 0.f};
 }
 
-// A candidate of the join: its score in 64 bits, ordered as an unsigned number (0: none), and where it stands, beam * vocab + token.
+// A candidate: its score in 64 bits, ordered as an unsigned number (0: none), and where it stands, beam * vocab + token.
 struct Candidate { uint64_t order; long long flat; };
 __device__ __forceinline__ bool better(const Candidate& x, const Candidate& y) { return x.order > y.order || (x.order == y.order && x.order && x.flat < y.flat); }
 __device__ __forceinline__ uint64_t order_of(double x) {
@@ -229,32 +134,46 @@ __device__ __forceinline__ double score_of(uint64_t order) {
   return __longlong_as_double(static_cast<long long>(order ^ ((order >> 63) ? 0x8000000000000000ull : ~0ull)));
 }
 
-// One group: log-sum-exp of its rows, then the n_select best of its segments' candidates, found as in the segments: a threshold from
-// the best of every four threads, a list of what is not below it, ranks counted in the list.
-constexpr int kJoinList = 512;
-constexpr int kJoinBatch = 8;
+// The same order for floats.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float float_of(uint32_t order) { return __uint_as_float(order ^ ((order >> 31) ? 0x80000000u : 0xffffffffu)); }
+
+constexpr int kJoinSets = 512;           // sets that are read again
+constexpr int kJoinList = 1536;          // tokens that are ranked
+constexpr int kJoinBatch = 8;            // pieces of four maxima a thread has under way
+template <typename T>
 __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_constant__ SelectParams p) {
   __shared__ double lse[kWidth], base[kWidth];
+  __shared__ float off[kWidth];                   // base - lse in fp32; -infinity where a beam offers no tokens
   __shared__ int kind[kWidth];                    // 0: offers nothing, 1: live, 2: finished
-  __shared__ uint64_t group_top[kSelGroups];
+  __shared__ alignas(16) uint32_t quad_top[kSelSets];
+  __shared__ uint64_t set_order[kJoinSets];
+  __shared__ int sets[kJoinSets];
   __shared__ Candidate list[kJoinList];
   __shared__ Candidate round_best[2][kSelWarps];
   __shared__ uint64_t threshold;
-  __shared__ int listed;
+  __shared__ uint32_t threshold0;
+  __shared__ int n_sets, n_listed;
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int W = p.a.width, S = p.segments, K = p.a.n_select;
-  const uint64_t* keys = p.best + static_cast<size_t>(g) * W * S * K;
-  const int n = W * S * K, per = S * K;
+  const int W = p.a.width, S = p.segments, K = p.a.n_select, V = p.a.vocab;
+  const float* tops = p.tops + static_cast<size_t>(g) * W * S * kSelSets;
+  const int n = W * S * kSelSets, per = S * kSelSets;
   const float inv_per = 1.f / static_cast<float>(per);
-  if (tid == 0) listed = 0;
+  if (tid == 0) { n_sets = 0; n_listed = 0; threshold = 0; }
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  // the candidates of a batch, side by side; the first batch is on its way while the sums are taken together
-  uint64_t key[kJoinBatch];
+  // the maxima of a batch, side by side; the first batch is on its way while the sums are taken together
+  float4 top[kJoinBatch];
+  auto place = [&](int i0, int k) { return i0 + 4 * (k * kSelThreads + tid); };
   auto load_batch = [&](int i0) {
 #pragma unroll
-    for (int k = 0; k < kJoinBatch; ++k) key[k] = i0 + k * kSelThreads + tid < n ? keys[i0 + k * kSelThreads + tid] : 0;
+    for (int k = 0; k < kJoinBatch; ++k)
+      top[k] = place(i0, k) < n ? *reinterpret_cast<const float4*>(tops + place(i0, k)) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
   };
   load_batch(0);
+  // ---- log-sum-exp of the rows
   for (int w = warp; w < W; w += kSelWarps) {
     const int row = g * W + w;
     const float score = __ldg(p.a.score + row);
@@ -264,107 +183,157 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
     if (p.a.done && __ldg(p.a.done + row) != 0) what = 2;
     else if (score > -INFINITY) {
       const int parts = S * kSelWarps;
-      const SegmentSum* part = p.sums + static_cast<size_t>(row) * parts;
-      float top = -INFINITY;
-      for (int i = lane; i < parts; i += 32) top = fmaxf(top, part[i].top);
+      const WarpSum* part = p.sums + static_cast<size_t>(row) * parts;
+      float most = -INFINITY;
+#pragma unroll 4
+      for (int i = lane; i < parts; i += 32) most = fmaxf(most, part[i].top);
 #pragma unroll
-      for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+      for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(kFull, most, d));
       double sum = 0.0;
-      for (int i = lane; i < parts; i += 32) sum += part[i].top == -INFINITY ? part[i].sum : part[i].sum * exp(static_cast<double>(part[i].top) - static_cast<double>(top));
+#pragma unroll 4
+      for (int i = lane; i < parts; i += 32) sum += part[i].top == -INFINITY ? part[i].sum : part[i].sum * static_cast<double>(ex2((part[i].top - most) * kLog2e));
 #pragma unroll
       for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
       bad = bad || !(sum < INFINITY);              // NaN
       if (!(sum > 0.0)) what = 0;                  // every token is masked
-      else l = static_cast<double>(top) + log(sum);
+      else l = static_cast<double>(most) + log(sum);
     }
     if (score == -INFINITY) what = 0;
     if (bad) what = 0;
     if (lane == 0) {
       lse[w] = l; base[w] = score; kind[w] = what;
+      off[w] = what == 1 ? static_cast<float>(static_cast<double>(score) - l) : -INFINITY;
       if (bad) atomicOr(p.a.status, MEPIC_DEV_BAD_LOGITS);
     }
   }
   __syncthreads();
-  auto candidate = [&](int i, uint64_t key) {
-    int w = static_cast<int>(static_cast<float>(i) * inv_per);      // i / per, corrected
-    w += i - w * per >= per ? 1 : i < w * per ? -1 : 0;
-    Candidate c{0, 0};
-    if (kind[w] == 1) {
-      if (key) c = Candidate{order_of(base[w] + (static_cast<double>(key_value(key)) - lse[w])), static_cast<long long>(w) * p.a.vocab + key_token(key)};
-    } else if (kind[w] == 2 && i == w * per) {
-      c = Candidate{order_of(base[w]), static_cast<long long>(w) * p.a.vocab + p.a.pad_token};
-    }
-    return c;
+  auto order_at = [&](int w, float x) -> uint64_t { return x > -INFINITY ? order_of(base[w] + (static_cast<double>(x) - lse[w])) : 0; };
+  auto beam_of = [&](int i) {                      // i / per
+    int w = static_cast<int>(static_cast<float>(i) * inv_per);
+    return w + (i - w * per >= per ? 1 : i < w * per ? -1 : 0);
   };
-  uint64_t top = 0;
-  for (int i0 = 0; i0 < n; i0 += kJoinBatch * kSelThreads) {
+  const uint64_t ended = tid < W && kind[tid] == 2 ? order_of(base[tid]) : 0;      // a finished beam's one candidate
+  // Scores in fp32 do to leave out what cannot be among the best: x + off is off by 2^-24 of off and of itself at most.
+  float most_off = 0.f;
+  for (int w = 0; w < W; ++w) if (off[w] > -INFINITY) most_off = fmaxf(most_off, fabsf(off[w]));
+  auto lowered = [&](float x) { return x - 0x1p-21f * (most_off + fabsf(x)); };
+  // ---- a first threshold, from the best of every four threads (no two equal: a number of their own in the last bits)
+  float mine = ended ? static_cast<float>(base[tid]) : -INFINITY;
+  for (int i0 = 0; i0 < n; i0 += 4 * kJoinBatch * kSelThreads) {
     if (i0) load_batch(i0);
 #pragma unroll
-    for (int k = 0; k < kJoinBatch; ++k) {
-      const int i = i0 + k * kSelThreads + tid;
-      if (i < n) top = max(top, candidate(i, key[k]).order);
-    }
+    for (int k = 0; k < kJoinBatch; ++k)
+      if (place(i0, k) < n) mine = fmaxf(mine, fmaxf(fmaxf(top[k].x, top[k].y), fmaxf(top[k].z, top[k].w)) + off[beam_of(place(i0, k))]);
   }
-  uint64_t wtop = max(top, __shfl_xor_sync(kFull, top, 1));
-  wtop = max(wtop, __shfl_xor_sync(kFull, wtop, 2));
-  if ((lane & 3) == 0) group_top[tid >> 2] = wtop;
+  float quad = fmaxf(mine, __shfl_xor_sync(kFull, mine, 1));
+  quad = fmaxf(quad, __shfl_xor_sync(kFull, quad, 2));
+  if ((lane & 3) == 0) quad_top[tid >> 2] = (order_of(quad) & ~(kSelSets - 1u)) | (tid >> 2);
   __syncthreads();
   {
-    const int i = tid >> 2, q0 = (tid & 3) * (kSelGroups / 4);
-    const uint64_t mine = group_top[i];
+    const int i = tid >> 2, q0 = (tid & 3) * (kSelSets / 4);
+    const uint32_t me = quad_top[i];
     int above = 0;
 #pragma unroll
-    for (int q = q0; q < q0 + kSelGroups / 4; ++q) above += group_top[q] > mine || (group_top[q] == mine && q < i);
+    for (int q = q0; q < q0 + kSelSets / 4; q += 4) {
+      const uint4 o = *reinterpret_cast<const uint4*>(quad_top + q);
+      above += (o.x > me) + (o.y > me) + (o.z > me) + (o.w > me);
+    }
     above += __shfl_xor_sync(kFull, above, 1);
     above += __shfl_xor_sync(kFull, above, 2);
-    if ((tid & 3) == 0 && above == K - 1) threshold = mine;
+    if ((tid & 3) == 0 && above == K - 1) threshold0 = me & ~(kSelSets - 1u);
   }
   __syncthreads();
-  const uint64_t least = threshold;
-  if (top >= least && top) {
-    for (int i0 = 0; i0 < n; i0 += kJoinBatch * kSelThreads) {
-      if (n > kJoinBatch * kSelThreads) load_batch(i0);
+  // ---- the sets that may reach it; the threshold proper is the n_select-th largest among them, in 64 bits
+  const float least0 = threshold0 > order_of(-INFINITY) ? lowered(float_of(threshold0)) : -INFINITY;
+  if (mine >= least0) {
+    for (int i0 = 0; i0 < n; i0 += 4 * kJoinBatch * kSelThreads) {
+      if (n > 4 * kJoinBatch * kSelThreads) load_batch(i0);
 #pragma unroll
       for (int k = 0; k < kJoinBatch; ++k) {
-        const int i = i0 + k * kSelThreads + tid;
-        if (i >= n) continue;
-        const Candidate c = candidate(i, key[k]);
-        if (c.order >= least && c.order) {
-          const int at = atomicAdd(&listed, 1);
-          if (at < kJoinList) list[at] = c;
-        }
+        if (place(i0, k) >= n) continue;
+        const int w = beam_of(place(i0, k));
+        if (!(fmaxf(fmaxf(top[k].x, top[k].y), fmaxf(top[k].z, top[k].w)) + off[w] >= least0)) continue;
+        const float x[4] = {top[k].x, top[k].y, top[k].z, top[k].w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (x[c] + off[w] >= least0 && x[c] + off[w] > -INFINITY) {
+            const int at = atomicAdd(&n_sets, 1);
+            if (at < kJoinSets) { sets[at] = place(i0, k) + c; set_order[at] = order_at(w, x[c]); }
+          }
       }
     }
+  }
+  __syncthreads();
+  const int m = min(n_sets, kJoinSets);
+  const bool all_sets = n_sets <= kJoinSets;
+  for (int i = tid; i < m; i += kSelThreads) {
+    const uint64_t me = set_order[i];
+    int above = 0;
+    for (int q = 0; q < m; ++q) above += set_order[q] > me || (set_order[q] == me && q < i);
+    if (above == K - 1) threshold = me;            // (never below what it was)
+  }
+  __syncthreads();
+  // (fewer sets than that: the others that reached the first threshold are finished beams, and it holds)
+  const uint64_t least = max(threshold, least0 > -INFINITY ? order_of(static_cast<double>(least0)) : static_cast<uint64_t>(1));
+  const float least_f = least > 1 ? lowered(static_cast<float>(score_of(least))) : -INFINITY;
+  // ---- the tokens that reach it, a set a warp
+  const T* logits = static_cast<const T*>(p.a.logits) + static_cast<long long>(g) * W * p.stride;
+  auto each_token = [&](int set, auto use) {       // by a whole warp: the tokens of a set
+    const int w = beam_of(set), seg = (set - w * per) / kSelSets, quad0 = (set % kSelSets) * 4;
+    const T* x = logits + w * p.stride;
+    const int lead = lead_of(x);
+    constexpr int kRun = 4 * kVec<T>;              // consecutive tokens of a set's piece
+#pragma unroll 4
+    for (int i = lane; i < kSelPieces * kRun; i += 32) {
+      const int v = token_of<T>(lead, seg, i / kRun, quad0) + i % kRun;
+      if (v < 0 || v >= V) continue;
+      const float y = static_cast<float>(x[v]);
+      if (y + off[w] >= least_f) use(Candidate{order_at(w, y), static_cast<long long>(w) * V + v});
+    }
+  };
+  if (all_sets) {
+    if (ended >= least) {
+      const int at = atomicAdd(&n_listed, 1);
+      if (at < kJoinList) list[at] = Candidate{ended, static_cast<long long>(tid) * V + p.a.pad_token};
+    }
+    for (int q = warp; q < m; q += kSelWarps)
+      if (set_order[q] >= least)
+        each_token(sets[q], [&](const Candidate& c) {
+          if (c.order >= least) {
+            const int at = atomicAdd(&n_listed, 1);
+            if (at < kJoinList) list[at] = c;
+          }
+        });
   }
   __syncthreads();
   auto write = [&](int k, const Candidate& c) {
     const size_t at = static_cast<size_t>(g) * K + k;
     const bool any = c.order != 0;
-    const int w = any ? static_cast<int>(c.flat / p.a.vocab) : -1, v = any ? static_cast<int>(c.flat - static_cast<long long>(w) * p.a.vocab) : -1;
-    const bool ended = any && (kind[w] == 2 || v == p.a.eos_token);
+    const int w = any ? static_cast<int>(c.flat / V) : -1, v = any ? static_cast<int>(c.flat - static_cast<long long>(w) * V) : -1;
+    const bool stops = any && (kind[w] == 2 || v == p.a.eos_token);
     p.a.parent[at] = w; p.a.token[at] = v;
     p.a.score_out[at] = any ? static_cast<float>(score_of(c.order)) : -INFINITY;
-    p.a.done_out[at] = ended; p.a.n_new[at] = any && !ended;
+    p.a.done_out[at] = stops; p.a.n_new[at] = any && !stops;
   };
-  const int m = listed;
-  if (m <= kJoinList) {
-    for (int i = tid; i < m; i += kSelThreads) {
-      const Candidate mine = list[i];
+  const int listed = n_listed;
+  if (all_sets && listed <= kJoinList) {
+    for (int i = tid; i < listed; i += kSelThreads) {
+      const Candidate me = list[i];
       int above = 0;
-      for (int q = 0; q < m; ++q) above += better(list[q], mine);
-      if (above < K) write(above, mine);
+      for (int q = 0; q < listed; ++q) above += better(list[q], me);
+      if (above < K) write(above, me);
     }
-    for (int k = m + tid; k < K; k += kSelThreads) write(k, Candidate{0, 0});
+    for (int k = listed + tid; k < K; k += kSelThreads) write(k, Candidate{0, 0});
     return;
   }
-  // more candidates at one score than the list holds: one a round
+  // ---- more of them than the lists hold (thousands of equal logits): the best below the last one found, n_select times over
   Candidate last{~0ull, -1};
   for (int k = 0; k < K; ++k) {
     Candidate b{0, 0};
-    for (int i = tid; i < n; i += kSelThreads) {
-      const Candidate c = candidate(i, keys[i]);
-      if (better(last, c) && better(c, b)) b = c;
-    }
+    auto look = [&](const Candidate& c) { if (c.order >= least && better(last, c) && better(c, b)) b = c; };
+    if (ended) look(Candidate{ended, static_cast<long long>(tid) * V + p.a.pad_token});
+    for (int i = warp; i < n; i += kSelWarps)
+      if (tops[i] + off[beam_of(i)] >= least_f) each_token(i, look);
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
       const Candidate o{__shfl_xor_sync(kFull, b.order, d), __shfl_xor_sync(kFull, b.flat, d)};
@@ -376,8 +345,7 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
 #pragma unroll
     for (int i = 1; i < kSelWarps; ++i) if (better(round_best[k & 1][i], b)) b = round_best[k & 1][i];
     if (tid == 0) write(k, b);
-    last = b;
-    if (b.order == 0) last = Candidate{0, -1};      // nothing is below nothing
+    last = b.order ? b : Candidate{0, -1};         // nothing is below nothing
   }
 }
 
@@ -658,9 +626,11 @@ int32_t launched(const char* what, cudaError_t e, int n) {
 }
 size_t up16(size_t n) { return (n + 15) & ~static_cast<size_t>(15); }
 
-int elements_per_segment(int type) { return kSelThreads * kSelChunks * (type == MEPIC_LOGITS_FP32 ? 4 : 8); }
 // a row that begins inside a 16-byte piece may need one segment more
-int segments_of(long long vocab, int type) { return static_cast<int>((vocab + 7 + elements_per_segment(type) - 1) / elements_per_segment(type)); }
+int segments_of(long long vocab, int type) {
+  const int n = kSelThreads * kSelPieces * (type == MEPIC_LOGITS_FP32 ? 4 : 8);
+  return static_cast<int>((vocab + 7 + n - 1) / n);
+}
 bool select_shape_ok(int32_t groups, int32_t width, int32_t n_select, int32_t vocab) {
   if (groups < 1 || width < 1 || width > MEPIC_BEAM_MAX_WIDTH) { mepic_set_error("beam_select: groups must be positive, width in 1..%d", MEPIC_BEAM_MAX_WIDTH); return false; }
   if (n_select < 1 || n_select > MEPIC_BEAM_MAX_SELECT) { mepic_set_error("beam_select: n_select %d not in 1..%d", n_select, MEPIC_BEAM_MAX_SELECT); return false; }
@@ -668,9 +638,8 @@ bool select_shape_ok(int32_t groups, int32_t width, int32_t n_select, int32_t vo
   if (static_cast<long long>(groups) * width > 65535) { mepic_set_error("beam_select: more than 65535 beams"); return false; }
   return true;
 }
-size_t select_bytes(int32_t groups, int32_t width, int32_t n_select, int segments) {
-  const size_t rows = static_cast<size_t>(groups) * width;
-  return up16(rows * segments * kSelWarps * sizeof(SegmentSum)) + up16(rows * segments * n_select * sizeof(uint64_t));
+size_t select_bytes(int32_t groups, int32_t width, int segments) {
+  return static_cast<size_t>(groups) * width * segments * (kSelWarps * sizeof(WarpSum) + kSelSets * sizeof(float));
 }
 
 // how the entries of a group are cut for the first launch of a fork: enough CTAs to fill the GPU, few enough counts to sum up
@@ -722,7 +691,7 @@ int32_t copy_call(const mepic_config_t* cfg, const mepic_pages_copy_args_t* a, f
 
 extern "C" size_t mepic_beam_select_workspace(int32_t groups, int32_t width, int32_t n_select, int32_t vocab) {
   if (!select_shape_ok(groups, width, n_select, vocab)) return 0;
-  return select_bytes(groups, width, n_select, segments_of(vocab, MEPIC_LOGITS_FP32));       // enough for every type
+  return select_bytes(groups, width, segments_of(vocab, MEPIC_LOGITS_FP32));       // enough for every type
 }
 
 extern "C" int32_t mepic_beam_select(const mepic_beam_select_args_t* a, void* cuda_stream) {
@@ -745,17 +714,23 @@ extern "C" int32_t mepic_beam_select(const mepic_beam_select_args_t* a, void* cu
   p.a = *a;
   p.segments = segments_of(a->vocab, a->logits_type);
   p.stride = stride;
-  const size_t need = select_bytes(a->groups, a->width, a->n_select, p.segments), rows = static_cast<size_t>(a->groups) * a->width;
+  const size_t need = select_bytes(a->groups, a->width, p.segments), rows = static_cast<size_t>(a->groups) * a->width;
   if (a->workspace_bytes < need) { mepic_set_error("beam_select: workspace of %zu bytes, %zu needed", a->workspace_bytes, need); return MEPIC_E_INVAL; }
-  p.sums = static_cast<SegmentSum*>(a->workspace);
-  p.best = reinterpret_cast<uint64_t*>(static_cast<unsigned char*>(a->workspace) + up16(rows * p.segments * kSelWarps * sizeof(SegmentSum)));
+  p.sums = static_cast<WarpSum*>(a->workspace);
+  p.tops = reinterpret_cast<float*>(p.sums + rows * p.segments * kSelWarps);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const dim3 grid(p.segments, static_cast<unsigned>(rows));
-  if (a->logits_type == MEPIC_LOGITS_BF16) mepic_beam_segments<__nv_bfloat16><<<grid, kSelThreads, 0, st>>>(p);
-  else if (a->logits_type == MEPIC_LOGITS_FP16) mepic_beam_segments<__half><<<grid, kSelThreads, 0, st>>>(p);
-  else mepic_beam_segments<float><<<grid, kSelThreads, 0, st>>>(p);
-  cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess) e = launch_dependent(mepic_beam_join, dim3(a->groups), dim3(kSelThreads), st, p);
+  const dim3 grid(p.segments, static_cast<unsigned>(rows)), groups(a->groups);
+  cudaError_t e;
+  if (a->logits_type == MEPIC_LOGITS_BF16) {
+    mepic_beam_pass<__nv_bfloat16><<<grid, kSelThreads, 0, st>>>(p);
+    if ((e = cudaGetLastError()) == cudaSuccess) e = launch_dependent(mepic_beam_join<__nv_bfloat16>, groups, dim3(kSelThreads), st, p);
+  } else if (a->logits_type == MEPIC_LOGITS_FP16) {
+    mepic_beam_pass<__half><<<grid, kSelThreads, 0, st>>>(p);
+    if ((e = cudaGetLastError()) == cudaSuccess) e = launch_dependent(mepic_beam_join<__half>, groups, dim3(kSelThreads), st, p);
+  } else {
+    mepic_beam_pass<float><<<grid, kSelThreads, 0, st>>>(p);
+    if ((e = cudaGetLastError()) == cudaSuccess) e = launch_dependent(mepic_beam_join<float>, groups, dim3(kSelThreads), st, p);
+  }
   return launched("beam_select", e, 2);
 }
 
