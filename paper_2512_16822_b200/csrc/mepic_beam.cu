@@ -153,7 +153,6 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   __shared__ uint64_t set_order[kJoinSets];
   __shared__ int sets[kJoinSets];
   __shared__ Candidate list[kJoinList];
-  __shared__ Candidate round_best[2][kSelWarps];
   __shared__ uint64_t threshold;
   __shared__ uint32_t threshold0;
   __shared__ int n_sets, n_listed;
@@ -175,23 +174,28 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   load_batch(0);
   // ---- log-sum-exp of the rows
   for (int w = warp; w < W; w += kSelWarps) {
-    const int row = g * W + w;
+    const int row = g * W + w, parts = S * kSelWarps;
+    const WarpSum* part = p.sums + static_cast<size_t>(row) * parts;
+    auto part_at = [&](int i) { return i < parts ? part[i] : WarpSum{0.0, -INFINITY, 0.f}; };
+    // (asked for before it is known whether the row counts: one that does not left nothing, and nothing is made of it)
+    WarpSum first[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) first[k] = part_at(lane + 32 * k);
     const float score = __ldg(p.a.score + row);
     int what = 1;
     bool bad = !(score < INFINITY);
     double l = 0.0;
     if (p.a.done && __ldg(p.a.done + row) != 0) what = 2;
     else if (score > -INFINITY) {
-      const int parts = S * kSelWarps;
-      const WarpSum* part = p.sums + static_cast<size_t>(row) * parts;
-      float most = -INFINITY;
-#pragma unroll 4
-      for (int i = lane; i < parts; i += 32) most = fmaxf(most, part[i].top);
+      float most = fmaxf(fmaxf(first[0].top, first[1].top), fmaxf(first[2].top, first[3].top));
+      for (int i = lane + 128; i < parts; i += 32) most = fmaxf(most, part[i].top);
 #pragma unroll
       for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(kFull, most, d));
       double sum = 0.0;
-#pragma unroll 4
-      for (int i = lane; i < parts; i += 32) sum += part[i].top == -INFINITY ? part[i].sum : part[i].sum * static_cast<double>(ex2((part[i].top - most) * kLog2e));
+      auto add = [&](const WarpSum& v) { sum += v.top == -INFINITY ? v.sum : v.sum * static_cast<double>(ex2((v.top - most) * kLog2e)); };
+#pragma unroll
+      for (int k = 0; k < 4; ++k) add(first[k]);
+      for (int i = lane + 128; i < parts; i += 32) add(part[i]);
 #pragma unroll
       for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
       bad = bad || !(sum < INFINITY);              // NaN
@@ -274,36 +278,36 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   }
   __syncthreads();
   // (fewer sets than that: the others that reached the first threshold are finished beams, and it holds)
-  const uint64_t least = max(threshold, least0 > -INFINITY ? order_of(static_cast<double>(least0)) : static_cast<uint64_t>(1));
-  const float least_f = least > 1 ? lowered(static_cast<float>(score_of(least))) : -INFINITY;
-  // ---- the tokens that reach it, a set a warp
+  uint64_t least = max(threshold, least0 > -INFINITY ? order_of(static_cast<double>(least0)) : static_cast<uint64_t>(1));
+  // ---- the tokens that reach it: a set a warp, the warp's loads side by side
   const T* logits = static_cast<const T*>(p.a.logits) + static_cast<long long>(g) * W * p.stride;
-  auto each_token = [&](int set, auto use) {       // by a whole warp: the tokens of a set
-    const int w = beam_of(set), seg = (set - w * per) / kSelSets, quad0 = (set % kSelSets) * 4;
+  constexpr int kRun = 4 * kVec<T>, kLoads = kSelPieces * kRun / 32;      // consecutive tokens of a set's piece; tokens of a set a lane has
+  auto each_token = [&](int set, uint64_t from, auto use) {               // those whose order is `from` or more
+    const float from_f = from > 1 ? lowered(static_cast<float>(score_of(from))) : -INFINITY;
+    const int w = beam_of(set);
     const T* x = logits + w * p.stride;
-    const int lead = lead_of(x);
-    constexpr int kRun = 4 * kVec<T>;              // consecutive tokens of a set's piece
-#pragma unroll 4
-    for (int i = lane; i < kSelPieces * kRun; i += 32) {
-      const int v = token_of<T>(lead, seg, i / kRun, quad0) + i % kRun;
-      if (v < 0 || v >= V) continue;
-      const float y = static_cast<float>(x[v]);
-      if (y + off[w] >= least_f) use(Candidate{order_at(w, y), static_cast<long long>(w) * V + v});
+    const int first = token_of<T>(lead_of(x), (set - w * per) / kSelSets, lane / kRun, (set % kSelSets) * 4) + lane % kRun;
+    float y[kLoads];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int v = first + k * (32 / kRun) * kSelThreads * kVec<T>;      // (a warp covers 32 / kRun pieces at a time)
+      y[k] = v >= 0 && v < V ? static_cast<float>(x[v]) : -INFINITY;
     }
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      if (y[k] + off[w] >= from_f && y[k] > -INFINITY) {
+        const Candidate c{order_at(w, y[k]), static_cast<long long>(w) * V + first + k * (32 / kRun) * kSelThreads * kVec<T>};
+        if (c.order >= from) use(c);
+      }
+  };
+  auto append = [&](const Candidate& c) {
+    const int at = atomicAdd(&n_listed, 1);
+    if (at < kJoinList) list[at] = c;
   };
   if (all_sets) {
-    if (ended >= least) {
-      const int at = atomicAdd(&n_listed, 1);
-      if (at < kJoinList) list[at] = Candidate{ended, static_cast<long long>(tid) * V + p.a.pad_token};
-    }
+    if (ended >= least) append(Candidate{ended, static_cast<long long>(tid) * V + p.a.pad_token});
     for (int q = warp; q < m; q += kSelWarps)
-      if (set_order[q] >= least)
-        each_token(sets[q], [&](const Candidate& c) {
-          if (c.order >= least) {
-            const int at = atomicAdd(&n_listed, 1);
-            if (at < kJoinList) list[at] = c;
-          }
-        });
+      if (set_order[q] >= least) each_token(sets[q], least, append);
   }
   __syncthreads();
   auto write = [&](int k, const Candidate& c) {
@@ -315,38 +319,92 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
     p.a.score_out[at] = any ? static_cast<float>(score_of(c.order)) : -INFINITY;
     p.a.done_out[at] = stops; p.a.n_new[at] = any && !stops;
   };
-  const int listed = n_listed;
-  if (all_sets && listed <= kJoinList) {
-    for (int i = tid; i < listed; i += kSelThreads) {
+  auto write_list = [&](int n_of) {                // the list's best, by their ranks
+    for (int i = tid; i < n_of; i += kSelThreads) {
       const Candidate me = list[i];
       int above = 0;
-      for (int q = 0; q < listed; ++q) above += better(list[q], me);
+      for (int q = 0; q < n_of; ++q) above += better(list[q], me);
       if (above < K) write(above, me);
     }
-    for (int k = listed + tid; k < K; k += kSelThreads) write(k, Candidate{0, 0});
+  };
+  if (all_sets && n_listed <= kJoinList) {
+    write_list(n_listed);
+    for (int k = n_listed + tid; k < K; k += kSelThreads) write(k, Candidate{0, 0});
     return;
   }
-  // ---- more of them than the lists hold (thousands of equal logits): the best below the last one found, n_select times over
-  Candidate last{~0ull, -1};
-  for (int k = 0; k < K; ++k) {
-    Candidate b{0, 0};
-    auto look = [&](const Candidate& c) { if (c.order >= least && better(last, c) && better(c, b)) b = c; };
-    if (ended) look(Candidate{ended, static_cast<long long>(tid) * V + p.a.pad_token});
-    for (int i = warp; i < n; i += kSelWarps)
-      if (tops[i] + off[beam_of(i)] >= least_f) each_token(i, look);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) {
-      const Candidate o{__shfl_xor_sync(kFull, b.order, d), __shfl_xor_sync(kFull, b.flat, d)};
-      if (better(o, b)) b = o;
-    }
-    if (lane == 0) round_best[k & 1][warp] = b;
+  // ---- More of them than the lists hold: thousands of equal logits, or of neighbours above the threshold.  What lies above the
+  // threshold is listed without what equals it; where that is too much, the threshold rises to the n_select-th largest of what the
+  // list got hold of.  (So does every round; two or three are the most that was seen.)
+  for (;;) {
     __syncthreads();
-    b = round_best[k & 1][0];
-#pragma unroll
-    for (int i = 1; i < kSelWarps; ++i) if (better(round_best[k & 1][i], b)) b = round_best[k & 1][i];
-    if (tid == 0) write(k, b);
-    last = b.order ? b : Candidate{0, -1};         // nothing is below nothing
+    if (tid == 0) n_sets = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kSelThreads) {
+      const int w = beam_of(i);
+      const uint64_t o = kind[w] == 1 ? order_at(w, tops[i]) : 0;
+      if (o > least) {
+        const int at = atomicAdd(&n_sets, 1);
+        if (at < kJoinSets) { sets[at] = i; set_order[at] = o; }
+      }
+    }
+    __syncthreads();
+    if (n_sets <= kJoinSets) break;
+    for (int i = tid; i < kJoinSets; i += kSelThreads) {
+      int above = 0;
+      for (int q = 0; q < kJoinSets; ++q) above += set_order[q] > set_order[i] || (set_order[q] == set_order[i] && q < i);
+      if (above == K - 1) threshold = set_order[i];
+    }
+    __syncthreads();
+    least = threshold;
   }
+  const int m2 = n_sets;
+  for (;;) {
+    __syncthreads();
+    if (tid == 0) n_listed = 0;
+    __syncthreads();
+    if (ended > least) append(Candidate{ended, static_cast<long long>(tid) * V + p.a.pad_token});
+    for (int q = warp; q < m2; q += kSelWarps)
+      if (set_order[q] > least) each_token(sets[q], least + 1, append);
+    __syncthreads();
+    if (n_listed <= kJoinList) break;
+    for (int i = tid; i < kJoinList; i += kSelThreads) {
+      int above = 0;
+      for (int q = 0; q < kJoinList; ++q) above += list[q].order > list[i].order || (list[q].order == list[i].order && q < i);
+      if (above == K - 1) threshold = list[i].order;
+    }
+    __syncthreads();
+    least = threshold;
+  }
+  write_list(n_listed);
+  // ... and what equals it in order of beam and token, until there is enough
+  int found = n_listed;
+  for (int w = 0; w < W && found < K && least > 1; ++w) {
+    if (kind[w] == 2) {
+      if (order_of(base[w]) == least) { if (tid == 0) write(found, Candidate{least, static_cast<long long>(w) * V + p.a.pad_token}); ++found; }
+      continue;
+    }
+    if (kind[w] == 0) continue;
+    for (int v0 = 0; v0 < V && found < K; v0 += 8 * kSelThreads) {
+      const T* x = logits + w * p.stride + v0 + 8 * tid;       // eight consecutive tokens a thread
+      unsigned hit = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) if (v0 + 8 * tid + i < V && order_at(w, static_cast<float>(x[i])) == least) hit |= 1u << i;
+      if (!__syncthreads_or(hit != 0)) continue;
+      int incl = __popc(hit);
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) { const int y = __shfl_up_sync(kFull, incl, d); if (lane >= d) incl += y; }
+      if (lane == 31) sets[warp] = incl;
+      __syncthreads();
+      int at = found + incl - __popc(hit);
+      for (int q = 0; q < kSelWarps; ++q) {
+        if (q < warp) at += sets[q];
+        found += sets[q];
+      }
+      for (; hit && at < K; hit &= hit - 1, ++at) write(at, Candidate{least, static_cast<long long>(w) * V + v0 + 8 * tid + __ffs(hit) - 1});
+      __syncthreads();
+    }
+  }
+  for (int k = found + tid; k < K; k += kSelThreads) write(k, Candidate{0, 0});
 }
 
 // ---------------------------------------------------------------- fork
