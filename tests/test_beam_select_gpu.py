@@ -115,6 +115,28 @@ def test_sorted_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("every,of", [(4, 16), (1, 16), (2, 5)])
+def test_the_best_in_a_few_stretches_of_a_large_vocabulary(dtype, every, of):
+    # whole stretches of 8,192 or 16,384 tokens stand above the rest of all rows: hundreds of neighbours are candidates
+    V = 120000
+    x = _logits(8, V, dtype, 15)
+    stretch = 8192 if dtype == "fp32" else 16384
+    lift = (torch.arange(V, device="cuda:0") // stretch)[None, :] + -(-V // stretch) * torch.arange(8, device="cuda:0")[:, None]
+    x = (x.float() + 30.0 * (lift % of < every)).to(TYPES[dtype])
+    _run(x, _scores(1, 8, 15), K=16)
+    _run(x, _scores(1, 8, 16), K=64, done=np.array([[0, 0, 1, 0, 0, 0, 1, 1]]))
+    x[:, ::3] = x[:, 1:2]                           # ... many of them equal
+    _run(x, np.zeros((1, 8)), K=64)
+
+
+def test_finished_beams_among_the_best_and_more_candidates_than_live_beams():
+    # half of the beams are finished and lead: fewer sets of tokens reach the threshold than candidates are asked for
+    x = _logits(64, 60001, "fp32", 16)
+    done = np.tile([1, 0], 32).reshape(2, 32)
+    _run(x, np.where(done == 1, -0.5, -3.0) - np.arange(32) * 0.01, K=40, done=done)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_masked_tokens(dtype):
     x = _logits(8, 20000, dtype, 7)
     x[0] = -np.inf                                  # nothing is allowed
