@@ -38,8 +38,8 @@ constexpr int kTile = 16;            // keys per staged tile
 constexpr int kMinPiece = 4;         // the line is never cut into pieces shorter than this many tiles
 constexpr int kMaxColumns = 32;      // columns of a column block
 // Cutting a number off after ten bits of mantissa makes it smaller, by 2^-11 of its power of two in the mean and by 2^-11 / (2 ln 2) of
-// itself where mantissas are spread as those of products are; the scores are made larger by as much.
-constexpr float kTf32Cut = 1.f + 0x1p-11f * 0.7213475f;
+// itself where mantissas are spread as those of products are; the scores are made larger by as much for either factor.
+constexpr float kTf32Cut = 1.f + 2.f * 0x1p-11f * 0.7213475f;
 constexpr float kLag = 8.f;                      // weights may reach 2^8
 constexpr float kSmallScale = 0x1p-100f;      // 8-bit pages: V scales are taken relative to the largest met, at least to this one
 constexpr int kSeg = 256;            // table entries a CTA of the plan looks at
@@ -270,8 +270,8 @@ template <int D, bool FP8> constexpr int angle_bytes = D / 2 * (FP8 ? 4 : 8);
 template <bool FP8> constexpr int stages_of = FP8 ? 4 : 2;
 constexpr int kWarpWords = 128;      // bytes a warp has beside its ring: per stage 16 of tile data, 8 of scales and a barrier of 8
 // Positions of the table: as many as fit beside the rings.
-template <bool FP8, int W> constexpr int angles_of = !FP8 && W > 10 ? 64 : 128;
-template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (stages_of<FP8> * stage_bytes<D, FP8> + kWarpWords) + angles_of<FP8, W> * angle_bytes<D, FP8> + 1024;
+template <bool FP8> constexpr int angles_of = FP8 ? 384 : 192;
+template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (stages_of<FP8> * stage_bytes<D, FP8> + kWarpWords) + (angles_of<FP8> + 1) * angle_bytes<D, FP8> + 1024;
 
 // NT: tiles of 8 columns; W: warps of a CTA.
 __device__ __forceinline__ float4 lds128(uint32_t addr) {
@@ -291,7 +291,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   constexpr int kStageBytes = stage_bytes<D, FP8>;
   constexpr int kStages = stages_of<FP8>;
   static_assert(kStages * 32 <= kWarpWords, "tile data, scales and barriers of the ring");
-  constexpr int kAngleBytes = angle_bytes<D, FP8>, kAngles = angles_of<FP8, W>;
+  constexpr int kAngleBytes = angle_bytes<D, FP8>, kAngles = angles_of<FP8>;
 
   extern __shared__ unsigned char smem_dyn[];
   // 1024-byte alignment: the swizzle pattern is a function of the address bits
@@ -299,7 +299,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   const int lane = threadIdx.x & 31, wic = __shfl_sync(kFull, static_cast<int>(threadIdx.x >> 5), 0);      // (known to be the same in a warp)
   unsigned char* stage0 = smem + static_cast<size_t>(wic) * kStages * kStageBytes;
   unsigned char* angles = smem + static_cast<size_t>(W) * kStages * kStageBytes;
-  unsigned char* words = angles + kAngles * kAngleBytes + wic * kWarpWords;
+  unsigned char* words = angles + (kAngles + 1) * kAngleBytes + wic * kWarpWords;
   const uint32_t meta = smem_u32(words);                 // per stage: position, beams, valid slots of the tile
   const uint32_t scl = meta + kStages * 16;              // per stage: K and V scale of the page
   uint64_t* bars = reinterpret_cast<uint64_t*>(words + kStages * 24);
@@ -397,15 +397,14 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   const int span = static_cast<int>(min(static_cast<long long>(kAngles), max(cut.piece, 1ll) * kTile));
   // ---- the table of angles: for position a and pairs 2u, 2u+1 the quadruple (c, c', s, s'), rows swizzled so that the eight lanes
   // that load together (two keys, four column groups) meet all banks
-  for (int i = threadIdx.x; i < span * (D / 4); i += W * 32) {
-    const int a = i / (D / 4), u = i % (D / 4);
-    const float4 cs = __ldg(reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(min(a, p.max_position)) * D + 4 * u));      // c, s, c', s'
+  // (the last row is that of `span` positions, by which an anchor moves)
+  for (int i = threadIdx.x; i < (span + 1) * (D / 4); i += W * 32) {
+    const int at = i / (D / 4), a = at < span ? at : kAngles, u = i % (D / 4);
+    const float4 cs = __ldg(reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(min(at, p.max_position)) * D + 4 * u));      // c, s, c', s'
     if constexpr (FP8) {
-      unsigned char* at = angles + a * kAngleBytes + ((u * 8) ^ ((a & 1) << 6));
-      *reinterpret_cast<uint2*>(at) = make_uint2(pack_f16x2(cs.x, cs.z), pack_f16x2(cs.y, cs.w));
+      *reinterpret_cast<uint2*>(angles + a * kAngleBytes + ((u * 8) ^ ((a & 1) << 6))) = make_uint2(pack_f16x2(cs.x, cs.z), pack_f16x2(cs.y, cs.w));
     } else {
-      unsigned char* at = angles + a * kAngleBytes;
-      *reinterpret_cast<float4*>(at + ((u * 16) ^ ((a & 1) << 6))) = make_float4(cs.x, cs.z, cs.y, cs.w);
+      *reinterpret_cast<float4*>(angles + a * kAngleBytes + ((u * 16) ^ ((a & 1) << 6))) = make_float4(cs.x, cs.z, cs.y, cs.w);
     }
   }
   __syncthreads();
@@ -467,8 +466,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       const float2 c = make_float2(cs.x, cs.z), sp = make_float2(cs.y * sn, cs.w * sn), sm = make_float2(-sp.x, -sp.y);
       const float2 a = fma2(lo, c, mul2(hi, sm)), b = fma2(lo, sp, mul2(hi, c));
       if constexpr (TF32) {
-        qt[nt][j][2 * r] = round_tf32(a.x); qt[nt][j][2 * r + 1] = round_tf32(a.y);
-        qt[nt][j + KH][2 * r] = round_tf32(b.x); qt[nt][j + KH][2 * r + 1] = round_tf32(b.y);
+        qt[nt][j][2 * r] = a.x; qt[nt][j][2 * r + 1] = a.y;
+        qt[nt][j + KH][2 * r] = b.x; qt[nt][j + KH][2 * r + 1] = b.y;
       } else {
         qf[nt][j][r] = FP8 ? pack_f16x2(a.x, a.y) : pack_bf16x2(a.x, a.y);
         qf[nt][j + KH][r] = FP8 ? pack_f16x2(b.x, b.y) : pack_bf16x2(b.x, b.y);
@@ -491,6 +490,22 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
 #pragma unroll
           for (int r = 0; r < 2; ++r) rotate(nt, j, r, __ldg(reinterpret_cast<const float4*>(turn[nt] + 2 * pair_of(j, r))), sign[nt]);
     }
+  };
+
+  // The anchor moves on by `span`: queries held in fp32 are turned back by as much where they are.
+  auto advance_queries = [&]() {
+#pragma unroll
+    for (int j = 0; j < KH; ++j)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float4 cs = lds128(angles_addr + kAngles * kAngleBytes + (16 * j + 2 * t + 8 * r) * 8);      // c, c', s, s'  (an even row)
+#pragma unroll
+        for (int nt = 0; nt < (TF32 ? NT : 0); ++nt) {
+          float &l0 = qt[nt][j][2 * r], &l1 = qt[nt][j][2 * r + 1], &h0 = qt[nt][j + KH][2 * r], &h1 = qt[nt][j + KH][2 * r + 1];
+          const float a0 = fmaf(l0, cs.x, h0 * cs.z), b0 = fmaf(h0, cs.x, -(l0 * cs.z)), a1 = fmaf(l1, cs.y, h1 * cs.w), b1 = fmaf(h1, cs.y, -(l1 * cs.w));
+          l0 = a0; h0 = b0; l1 = a1; h1 = b1;
+        }
+      }
   };
 
   int stage = 0;
@@ -524,7 +539,12 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     int pos, n_valid, unused;
     unsigned beams;
     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(pos), "=r"(beams), "=r"(n_valid), "=r"(unused) : "r"(meta + stage * 16) : "memory");
-    if (anchor == INT_MIN || static_cast<unsigned>(pos - anchor) > static_cast<unsigned>(span - kTile)) { anchor = pos; rotate_queries(); }
+    if (anchor == INT_MIN || static_cast<unsigned>(pos - anchor) > static_cast<unsigned>(span - kTile)) {
+      const bool on = TF32 && anchor != INT_MIN && pos - anchor == span && span <= p.max_position;
+      anchor = pos;
+      if (on) advance_queries();
+      else rotate_queries();
+    }
     if (!mbar_wait_bounded(smem_u32(&bars[stage]), parity, p.spin_limit)) {
       // Give the copies still in flight a last bounded chance to land, then leave cleanly.
       if (lane == 0) atomicOr(p.status, MEPIC_DEV_WAIT_EXPIRED);
@@ -815,9 +835,8 @@ int sm_count(int* device) {
   if (dev < 64) known[dev].store(sms, std::memory_order_relaxed);
   return sms;
 }
-constexpr int kMaxWarps = 12;
-constexpr int warps_of(int nt, bool fp8) { return fp8 && nt <= 2 ? 12 : 8; }
-size_t slots_of(const PlanShape& s, int n_kv_heads, int sms) { return static_cast<size_t>(s.groups) * s.blocks * n_kv_heads + static_cast<size_t>(sms) * kMaxWarps; }
+constexpr int kWarps = 8;
+size_t slots_of(const PlanShape& s, int n_kv_heads, int sms) { return static_cast<size_t>(s.groups) * s.blocks * n_kv_heads + static_cast<size_t>(sms) * kWarps; }
 size_t workspace_bytes(const mepic_config_t* cfg, const PlanShape& s, int sms) {
   const size_t columns = static_cast<size_t>(s.beams) * (cfg->n_q_heads / cfg->n_kv_heads);
   return slots_of(s, cfg->n_kv_heads, sms) * columns * (cfg->head_dim + 2) * sizeof(float);
@@ -825,7 +844,7 @@ size_t workspace_bytes(const mepic_config_t* cfg, const PlanShape& s, int sms) {
 
 template <int D, int NT, bool FP8>
 int32_t launch_beam(BeamParams& p, int sms, int device, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t st) {
-  constexpr int W = warps_of(NT, FP8);
+  constexpr int W = kWarps;
   constexpr size_t smem = smem_bytes<D, FP8, W>;
   static_assert(smem <= 232448, "shared memory of a CTA");
   static std::atomic<unsigned long long> prepared{0};      // devices on which the limit is raised
