@@ -92,7 +92,9 @@ struct PlanParams {
 __global__ void __launch_bounds__(kSeg) mepic_beam_plan_classes(const __grid_constant__ PlanParams p) {
   __shared__ int len[MEPIC_BEAM_MAX_WIDTH];
   __shared__ int warp_n[kSeg / 32];
-  extern __shared__ int held_pages[];          // [page ids, position bases][beams of the block][kSeg]
+  __shared__ int mixed[kSeg], n_mixed;         // entries that not all of their beams hold alike
+  __shared__ unsigned mixed_held[kSeg];
+  extern __shared__ int held_pages[];          // [page ids, position bases, beams that hold the same][beams of the block][kSeg]
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int block = blockIdx.x, seg = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group = block / p.blocks, first = (block - group * p.blocks) * p.beams, nb = min(p.beams, p.width - first);
@@ -105,6 +107,7 @@ __global__ void __launch_bounds__(kSeg) mepic_beam_plan_classes(const __grid_con
     len[tid] = n;
     if (seg == 0) p.lens[row0 + tid] = n;
   }
+  if (tid == 0) n_mixed = 0;
   __syncthreads();
   const int e = seg * kSeg + tid;
   const long long from = static_cast<long long>(e) << p.page_shift;
@@ -132,17 +135,34 @@ __global__ void __launch_bounds__(kSeg) mepic_beam_plan_classes(const __grid_con
     const int i = __ffs(m) - 1;
     one = one && my_ids[i * kSeg] == my_ids[lead * kSeg] && my_base[i * kSeg] == my_base[lead * kSeg] && fill(i) == fill(lead);
   }
+  // where they do not, every (entry, beam) pair of the CTA finds the beams that hold the same, a pair a thread
+  int* my_same = held_pages + 2 * nb * kSeg + tid;
+  mixed_held[tid] = one ? 0 : held;
+  if (!one) mixed[atomicAdd(&n_mixed, 1)] = tid;         // (in any order: what is found for an entry is kept at the entry)
+  __syncthreads();
+  for (int q = tid; q < n_mixed * nb; q += kSeg) {
+    const int at = mixed[q / nb], i = q % nb;
+    const unsigned those = mixed_held[at];
+    if (!(those >> i & 1)) continue;
+    const int* col_ids = held_pages + at;
+    const int* col_base = held_pages + nb * kSeg + at;
+    const long long start = static_cast<long long>(seg * kSeg + at) << p.page_shift;
+    auto slots = [&](int b) { return min(static_cast<long long>(P), len[b] - start); };
+    unsigned same = 0;
+    for (unsigned m = those; m; m &= m - 1) {
+      const int b = __ffs(m) - 1;
+      if (col_ids[b * kSeg] == col_ids[i * kSeg] && col_base[b * kSeg] == col_base[i * kSeg] && slots(b) == slots(i)) same |= 1u << b;
+    }
+    held_pages[(2 * nb + i) * kSeg + at] = static_cast<int>(same);
+  }
+  __syncthreads();
   auto each_class = [&](auto use) {
     if (one) { if (held) use(my_ids[lead * kSeg], my_base[lead * kSeg], held, fill(lead)); return; }
     for (unsigned left = held; left;) {
-      const int i = __ffs(left) - 1, page = my_ids[i * kSeg], pos = my_base[i * kSeg], n = fill(i);
-      unsigned same = 0;
-      for (unsigned m = left; m; m &= m - 1) {
-        const int j = __ffs(m) - 1;
-        if (my_ids[j * kSeg] == page && my_base[j * kSeg] == pos && fill(j) == n) same |= 1u << j;
-      }
+      const int i = __ffs(left) - 1;
+      const unsigned same = static_cast<unsigned>(my_same[i * kSeg]);
       left &= ~same;
-      use(page, pos, same, n);
+      use(my_ids[i * kSeg], my_base[i * kSeg], same, fill(i));
     }
   };
   int n = 0;
@@ -236,17 +256,19 @@ __device__ __forceinline__ Cut cut_of_line(const BeamParams& p) {
 }
 // A unit of the line: a column block under one kv head, records r0 .. r1-1 of the plan.
 struct Unit { int block, head, r0, r1; };
+__device__ __forceinline__ int begin_of(const BeamParams& p, int block) { return __ldg(p.sums + static_cast<size_t>(block) * p.segments); }
 __device__ __forceinline__ void bounds_of(const BeamParams& p, Unit& u) {
   u.r0 = __ldg(p.sums + static_cast<size_t>(u.block) * p.segments);
   u.r1 = __ldg(p.sums + static_cast<size_t>(u.block + 1) * p.segments);
 }
-__device__ __forceinline__ void next_unit(const BeamParams& p, Unit& u) {
-  if (++u.head < p.n_kv_heads) return;
-  u.head = 0;
+// The unit after (block, head); false: there is none.
+__device__ __forceinline__ bool next_unit(const BeamParams& p, int& block, int& head) {
+  if (++head < p.n_kv_heads) return true;
+  head = 0;
   do {
-    if (++u.block >= p.groups * p.blocks) { u.r0 = u.r1 = 0; return; }
-    bounds_of(p, u);
-  } while (u.r0 >= u.r1);
+    if (++block >= p.groups * p.blocks) return false;
+  } while (begin_of(p, block) >= begin_of(p, block + 1));
+  return true;
 }
 // The column block that place x of the line falls into, 32 candidates at a time (by a whole warp).
 __device__ __forceinline__ Unit unit_at(const BeamParams& p, long long x, int lane) {
@@ -329,18 +351,20 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   const int G = p.group_size, tpp_mask = (1 << p.log2_tpp) - 1;
 
   // ---- producer: the next tile to stage
-  Unit pu = unit_at(p, x0, lane);
-  int pr, pt;
+  int p_block, p_head, pr, pr_end, pt;                                 // column block, kv head, record, the block's last one, tile of the page
+  int c_block, c_head, c_left;                                         // consumer: its unit, and the unit's tiles still to come
   {
-    const long long in = x0 - (static_cast<long long>(pu.r0) << p.log2_tpp) * p.n_kv_heads, per = static_cast<long long>(pu.r1 - pu.r0) << p.log2_tpp;
-    pu.head = static_cast<int>(in / per);
-    const long long in_head = in - pu.head * per;
-    pr = pu.r0 + static_cast<int>(in_head >> p.log2_tpp);
+    const Unit u = unit_at(p, x0, lane);
+    const long long in = x0 - (static_cast<long long>(u.r0) << p.log2_tpp) * p.n_kv_heads, per = static_cast<long long>(u.r1 - u.r0) << p.log2_tpp;
+    const int head = static_cast<int>(in / per);
+    const long long in_head = in - head * per;
+    p_block = c_block = u.block; p_head = c_head = head;
+    pr = u.r0 + static_cast<int>(in_head >> p.log2_tpp);
+    pr_end = u.r1;
     pt = static_cast<int>(in_head) & tpp_mask;
+    c_left = static_cast<int>(min(per - in_head, static_cast<long long>(INT_MAX)));
   }
-  Unit cu = pu;                                                        // consumer: its unit, and the unit's tiles still to come
-  int c_left = static_cast<int>(min((static_cast<long long>(cu.r1 - pr) << p.log2_tpp) - pt, static_cast<long long>(INT_MAX)));
-  int pseg = pu.block * p.segments;                                    // segment of the producer's record
+  int pseg = p_block * p.segments;                                    // segment of the producer's record
   int win0 = 0, win_n = 0;                                             // records win0 .. win0 + win_n - 1, one per lane
   int4 win = make_int4(0, 0, 0, 0);
   float win_ks = 0.f, win_vs = 0.f;
@@ -356,8 +380,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       win = in ? __ldg(p.records + static_cast<size_t>(pseg) * kSeg * p.beams + at) : make_int4(0, 0, 0, 0);
       if (static_cast<unsigned>(win.x) >= static_cast<unsigned>(p.num_pages)) win.x = 0;
       if constexpr (FP8) {
-        win_ks = __ldg(p.k_scales + static_cast<size_t>(win.x) * p.n_kv_heads + pu.head);
-        win_vs = __ldg(p.v_scales + static_cast<size_t>(win.x) * p.n_kv_heads + pu.head);
+        win_ks = __ldg(p.k_scales + static_cast<size_t>(win.x) * p.n_kv_heads + p_head);
+        win_vs = __ldg(p.v_scales + static_cast<size_t>(win.x) * p.n_kv_heads + p_head);
       }
     }
     // the lane that holds the record issues the copies
@@ -370,7 +394,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         if (n_valid <= 0) {
           mbar_expect_tx(bar, 0);                           // a tile of the page that holds no slot
         } else {
-          const int y = (win.x * p.n_kv_heads + pu.head) * p.page_size + pt * kTile;      // row of the pool viewed as [rows][D]
+          const int y = (win.x * p.n_kv_heads + p_head) * p.page_size + pt * kTile;      // row of the pool viewed as [rows][D]
           mbar_expect_tx(bar, kStageBytes);
           if constexpr (FP8) {
             tma_load_2d(dst, &map_k, 0, y, bar);
@@ -385,10 +409,11 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     ++issued;
     if (pt < tpp_mask) { ++pt; return; }
     pt = 0;
-    if (++pr < pu.r1) return;
-    next_unit(p, pu);
-    pr = pu.r0;
-    pseg = min(pu.block, p.groups * p.blocks - 1) * p.segments;
+    if (++pr < pr_end) return;
+    if (!next_unit(p, p_block, p_head)) return;            // (the line's end: nothing is issued any more)
+    pr = begin_of(p, p_block);
+    pr_end = begin_of(p, p_block + 1);
+    pseg = p_block * p.segments;
     win_n = 0;                                              // another head: its scales, another block: its records
   };
   for (int s = 0; s < kStages && issued < n_tiles; ++s) issue(s);
@@ -414,9 +439,9 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   int u_block = -1, u_head = -1;
   unsigned all_beams = 0;
   int anchor = INT_MIN;
-  unsigned see[NT][2];                       // beam bit of the columns 8 nt + 2 t, + 1 of this lane (0: no such column)
-  int q_at[NT];                              // position and un-rotated query of column 8 nt + g
-  const uint16_t* q_src[NT];
+  uint32_t beam_of[(NT + 1) / 2];            // beams of the columns 8 nt + 2 t, + 1 of this lane, a byte each
+  auto sees = [&](int nt, int c, unsigned beams) { return (beams >> (beam_of[nt / 2] >> (16 * (nt % 2) + 8 * c) & 31) & 1) != 0; };
+  int q_at[NT];                              // position of column 8 nt + g
   constexpr bool TF32 = !FP8 && NT <= 2;     // QK^T in tf32 where the registers allow it
   float qt[TF32 ? NT : 1][KS][4];            // B fragments of Q'^T in tf32: dims of the k-step's two column halves, pairs
   uint32_t qf[NT][KS][2];                    // B fragments of Q'^T, column 8 nt + g
@@ -447,12 +472,16 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   // The queries of the unit, rotated by their position less the anchor.  One table row does for all columns where their positions are
   // the same, as they are but for beams that have ended.
   auto rotate_queries = [&]() {
+    const int first = (u_block % p.blocks) * p.beams, nb = min(p.beams, p.width - first), row0 = u_block / p.blocks * p.width + first;
+    const uint16_t* q_src[NT];
     const float* turn[NT];
     float sign[NT];
     const int q0 = __shfl_sync(kFull, q_at[0], 0);
     bool same = true;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+      const int col = 8 * nt + g < nb * G ? 8 * nt + g : 0;
+      q_src[nt] = p.q + static_cast<size_t>(row0 + col / G) * p.q_stride + (static_cast<size_t>(u_head) * G + col % G) * D;
       const int rel = q_at[nt] - anchor;
       int arel = rel < 0 ? -rel : rel;
       if (static_cast<unsigned>(arel) > static_cast<unsigned>(p.max_position)) { atomicOr(p.status, MEPIC_DEV_BAD_POSITION); arel = p.max_position; }
@@ -511,9 +540,9 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   int stage = 0;
   uint32_t parity = 0;
   for (int it = 0; it < n_tiles; ++it) {
-    if (cu.block != u_block || cu.head != u_head) {
+    if (c_block != u_block || c_head != u_head) {
       flush();
-      u_block = cu.block; u_head = cu.head;
+      u_block = c_block; u_head = c_head;
       anchor = INT_MIN; v_ref = kSmallScale; v_inv = 0x1p6f / kSmallScale;
       const int first = (u_block % p.blocks) * p.beams, nb = min(p.beams, p.width - first);
       all_beams = nb == 32 ? ~0u : (1u << nb) - 1;
@@ -522,14 +551,14 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       for (int nt = 0; nt < NT; ++nt) {                       // a column that is none repeats the first: nobody looks at it
         const int col = 8 * nt + g < nb * G ? 8 * nt + g : 0, row = row0 + col / G;
         q_at[nt] = __ldg(p.q_pos + row);
-        q_src[nt] = p.q + static_cast<size_t>(row) * p.q_stride + (static_cast<size_t>(u_head) * G + col % G) * D;
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const int beam = (8 * nt + 2 * t + c) / G;
-          see[nt][c] = beam < nb ? 1u << beam : 0u;
+          // a column that is none belongs to beam 31: no page does (with 32 beams of one head there is no such column)
+          const uint32_t beam = min((8 * nt + 2 * t + c) / G < nb ? (8 * nt + 2 * t + c) / G : 31, 31);
+          beam_of[nt / 2] = nt % 2 == 0 && c == 0 ? beam : beam_of[nt / 2] | beam << (16 * (nt % 2) + 8 * c);
           m_run[nt][c] = -FLT_MAX; l_run[nt][c] = 0.f;
         }
 #pragma unroll
@@ -673,8 +702,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     if (some) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        if (!(see[nt][0] & beams)) { sc[nt][0] = -INFINITY; sc[nt][2] = -INFINITY; }
-        if (!(see[nt][1] & beams)) { sc[nt][1] = -INFINITY; sc[nt][3] = -INFINITY; }
+        if (!sees(nt, 0, beams)) { sc[nt][0] = -INFINITY; sc[nt][2] = -INFINITY; }
+        if (!sees(nt, 1, beams)) { sc[nt][1] = -INFINITY; sc[nt][3] = -INFINITY; }
       }
     }
     bool higher = false;
@@ -749,8 +778,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         for (int nt = 0; nt < NT; ++nt) {
           float x[4] = {0.f, 0.f, 0.f, 0.f};
           mma(x, va, pb[nt]);
-          if (see[nt][0] & beams) { acc[nt][db][0] += x[0]; acc[nt][db][2] += x[2]; }
-          if (see[nt][1] & beams) { acc[nt][db][1] += x[1]; acc[nt][db][3] += x[3]; }
+          if (sees(nt, 0, beams)) { acc[nt][db][0] += x[0]; acc[nt][db][2] += x[2]; }
+          if (sees(nt, 1, beams)) { acc[nt][db][1] += x[1]; acc[nt][db][3] += x[3]; }
         }
       });
     }
@@ -758,8 +787,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     if (issued < n_tiles) issue(stage);
     __syncwarp();
     if (--c_left == 0) {
-      next_unit(p, cu);
-      c_left = static_cast<int>(min(static_cast<long long>(cu.r1 - cu.r0) << p.log2_tpp, static_cast<long long>(INT_MAX)));
+      if (next_unit(p, c_block, c_head))
+        c_left = static_cast<int>(min(static_cast<long long>(begin_of(p, c_block + 1) - begin_of(p, c_block)) << p.log2_tpp, static_cast<long long>(INT_MAX)));
     }
     if (++stage == kStages) { stage = 0; parity ^= 1u; }
   }
@@ -946,10 +975,10 @@ extern "C" int32_t mepic_beam_plan(const mepic_config_t* cfg, const mepic_beam_p
   while ((1 << p.page_shift) < cfg->page_size) ++p.page_shift;
   p.num_pages = cfg->num_pages; p.group_size = cfg->n_q_heads / cfg->n_kv_heads; p.n_kv_heads = cfg->n_kv_heads;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const size_t smem = static_cast<size_t>(s.beams) * kSeg * 2 * sizeof(int);
+  const size_t smem = static_cast<size_t>(s.beams) * kSeg * 3 * sizeof(int);
   cudaError_t e = cudaSuccess;
   // always the largest: another thread's call may need more than this one
-  if (smem > 40 * 1024) e = cudaFuncSetAttribute(mepic_beam_plan_classes, cudaFuncAttributeMaxDynamicSharedMemorySize, MEPIC_BEAM_MAX_WIDTH * kSeg * 2 * static_cast<int>(sizeof(int)));
+  if (smem > 40 * 1024) e = cudaFuncSetAttribute(mepic_beam_plan_classes, cudaFuncAttributeMaxDynamicSharedMemorySize, MEPIC_BEAM_MAX_WIDTH * kSeg * 3 * static_cast<int>(sizeof(int)));
   if (e != cudaSuccess) { mepic_set_error("beam_plan: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
   mepic_beam_plan_classes<<<dim3(static_cast<unsigned>(s.groups) * s.blocks, s.segments), kSeg, smem, st>>>(p);
   e = cudaGetLastError();
