@@ -796,60 +796,97 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
 }
 
 // ---------------------------------------------------------------- merge
-// A CTA of four warps per (unit, column): its partials are dealt round to the warps, a lane owns D / 32 output dims.
-template <int D>
-__global__ void __launch_bounds__(128) mepic_beam_merge(const __grid_constant__ BeamParams p) {
+// PER warps a (unit, column): the column's partials are dealt round to them, a lane owns D / 32 output dims.  Each warp joins its
+// own partials against the largest reference among them, and the PER results are joined in order.  Few partials a unit (a batch):
+// one warp, 2 us less than four; many (one long request): four.
+constexpr int kMergeWarps = 8;
+template <int D, int PER>
+__global__ void __launch_bounds__(kMergeWarps * 32) mepic_beam_merge(const __grid_constant__ BeamParams p) {
   constexpr int E = D / 32;
-  const int unit = blockIdx.x, col = blockIdx.y, wv = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  __shared__ float sh_m[4], sh_l[4];
-  __shared__ float sh_o[4][D];
+  const int unit = blockIdx.x, wv = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = wv % PER;
+  const int col = blockIdx.y * (kMergeWarps / PER) + wv / PER;
+  __shared__ float sh_m[kMergeWarps], sh_l[kMergeWarps];
+  __shared__ float sh_o[kMergeWarps][D];
   const int block = unit / p.n_kv_heads, head = unit - block * p.n_kv_heads, group = block / p.blocks;
   const int beam = (block - group * p.blocks) * p.beams + col / p.group_size;
-  if (beam >= p.width) return;
-  const size_t row = static_cast<size_t>(group) * p.width + beam;
+  const bool live = col < p.columns && beam < p.width;
+  const size_t row = static_cast<size_t>(group) * p.width + (live ? beam : 0);
   const bool fits = plan_fits(p);
-  if (!fits && unit == 0 && col == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_PLAN);
+  if (!fits && unit == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(p.status, MEPIC_DEV_BAD_PLAN);
   long long w0 = 0, w1 = -1;
-  bool sees = false;
-  if (fits) {
+  bool shows = false;
+  if (fits && live) {
     const Cut cut = cut_of_line(p);
     Unit u{block, head, 0, 0};
     bounds_of(p, u);
     const long long per = static_cast<long long>(u.r1 - u.r0) << p.log2_tpp, begin = (static_cast<long long>(u.r0) << p.log2_tpp) * p.n_kv_heads + head * per;
     if (per > 0) { w0 = begin / cut.piece; w1 = (begin + per - 1) / cut.piece; }
-    sees = __ldg(p.lens + row) > 0;
+    shows = __ldg(p.lens + row) > 0;
   }
   // launched as a programmatic dependent of the attention kernel: its partials are complete and visible after this
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  float m = -FLT_MAX;
-  for (long long k = w0 + wv; k <= w1; k += 4) m = fmaxf(m, p.part_ml[(unit + k) * p.columns + col].x);
-  if (lane == 0) sh_m[wv] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
-  float l = 0.f, o[E];
+  float m = -FLT_MAX, l = 0.f, o[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) o[i] = 0.f;
-#pragma unroll 2
-  for (long long k = w0 + wv; k <= w1; k += 4) {
-    const float2 ml = p.part_ml[(unit + k) * p.columns + col];
-    const float wgt = ex2(ml.x - m);
-    l += ml.y * wgt;
-    const float* src = p.part_o + ((unit + k) * p.columns + col) * D + E * lane;
+  // 32 partials at a time, a lane each for their references and sums
+  for (long long k0 = w0 + sub; k0 <= w1; k0 += 32 * PER) {
+    const long long mine = k0 + static_cast<long long>(lane) * PER;
+    const float2 ml = mine <= w1 ? p.part_ml[(unit + mine) * p.columns + col] : make_float2(-FLT_MAX, 0.f);
+    float top = fmaxf(ml.x, m);
 #pragma unroll
-    for (int i = 0; i < E; ++i) o[i] += src[i] * wgt;
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+    const float wgt = mine <= w1 ? ex2(ml.x - top) : 0.f, was = ex2(m - top);
+    float add = mine <= w1 ? ml.y * wgt : 0.f;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) add += __shfl_xor_sync(kFull, add, d);
+    l = l * was + add;
+    m = top;
+#pragma unroll
+    for (int i = 0; i < E; ++i) o[i] *= was;
+    const int n = static_cast<int>(min((w1 - k0) / PER + 1, 32ll));
+#pragma unroll 4
+    for (int q = 0; q < n; ++q) {
+      const float w = __shfl_sync(kFull, wgt, q);
+      const float* src = p.part_o + ((unit + k0 + static_cast<long long>(q) * PER) * p.columns + col) * D + E * lane;
+      if constexpr (E == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(src);
+        o[0] += x.x * w; o[1] += x.y * w; o[2] += x.z * w; o[3] += x.w * w;
+      } else {
+        const float2 x = *reinterpret_cast<const float2*>(src);
+        o[0] += x.x * w; o[1] += x.y * w;
+      }
+    }
   }
-  if (lane == 0) sh_l[wv] = l;
+  if constexpr (PER > 1) {
+    if (lane == 0) { sh_m[wv] = m; sh_l[wv] = l; }
 #pragma unroll
-  for (int i = 0; i < E; ++i) sh_o[wv][E * lane + i] = o[i];
-  __syncthreads();
-  if (wv != 0) return;
-  l = (sh_l[0] + sh_l[1]) + (sh_l[2] + sh_l[3]);
+    for (int i = 0; i < E; ++i) sh_o[wv][E * lane + i] = o[i];
+    __syncthreads();
+    if (sub != 0) return;
+    float top = m;
+#pragma unroll
+    for (int q = 1; q < PER; ++q) top = fmaxf(top, sh_m[wv + q]);
+    float f = ex2(m - top);
+    l *= f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) o[i] *= f;
+#pragma unroll
+    for (int q = 1; q < PER; ++q) {
+      f = ex2(sh_m[wv + q] - top);
+      l += sh_l[wv + q] * f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) o[i] += sh_o[wv + q][E * lane + i] * f;
+    }
+  }
+  if (!live) return;
+  // l = 0 where the row has slots: every score is -infinity, 0 / 0
+  uint32_t bits[E / 2];
+#pragma unroll
+  for (int i = 0; i < E; i += 2)
+    bits[i / 2] = static_cast<uint32_t>(f32_to_bf16_bits(shows ? o[i] / l : 0.f)) | static_cast<uint32_t>(f32_to_bf16_bits(shows ? o[i + 1] / l : 0.f)) << 16;
   uint16_t* dst = p.out + (row * p.n_kv_heads * p.group_size + static_cast<size_t>(head) * p.group_size + col % p.group_size) * D + E * lane;
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const float x = (sh_o[0][E * lane + i] + sh_o[1][E * lane + i]) + (sh_o[2][E * lane + i] + sh_o[3][E * lane + i]);
-    dst[i] = f32_to_bf16_bits(sees ? x / l : 0.f);      // l = 0 where the row sees slots: every score is -infinity, 0 / 0
-  }
+  if constexpr (E == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(bits[0], bits[1]);
+  else *reinterpret_cast<uint32_t*>(dst) = bits[0];
 }
 
 // ---------------------------------------------------------------- host side
@@ -887,7 +924,11 @@ int32_t launch_beam(BeamParams& p, int sms, int device, const CUtensorMap& map_k
   p.workers = sms * W;
   mepic_beam_attn<D, NT, FP8, W><<<sms, W * 32, smem, st>>>(p, map_k, map_v);
   e = cudaGetLastError();
-  if (e == cudaSuccess) e = launch_dependent(mepic_beam_merge<D>, dim3(static_cast<unsigned>(p.groups) * p.blocks * p.n_kv_heads, p.columns), dim3(128), st, p);
+  const int units = p.groups * p.blocks * p.n_kv_heads;
+  if (e == cudaSuccess) {
+    if (p.workers <= 16LL * units) e = launch_dependent(mepic_beam_merge<D, 1>, dim3(units, (p.columns + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), st, p);
+    else e = launch_dependent(mepic_beam_merge<D, 4>, dim3(units, (p.columns + kMergeWarps / 4 - 1) / (kMergeWarps / 4)), dim3(kMergeWarps * 32), st, p);
+  }
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) { mepic_set_error("attn_beam: launch: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
   mepic_count_launches(2);
