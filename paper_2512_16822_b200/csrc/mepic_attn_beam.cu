@@ -35,7 +35,6 @@ namespace {
 using namespace mepic_dev;
 
 constexpr int kTile = 16;            // keys per staged tile
-constexpr int kMinPiece = 4;         // the line is never cut into pieces shorter than this many tiles
 constexpr int kMaxColumns = 32;      // columns of a column block
 // Cutting a number off after ten bits of mantissa makes it smaller, by 2^-11 of its power of two in the mean and by 2^-11 / (2 ln 2) of
 // itself where mantissas are spread as those of products are; the scores are made larger by as much for either factor.
@@ -85,6 +84,12 @@ struct PlanParams {
   int32_t* status;
   int stride, groups, width, blocks, beams, segments, page_shift, num_pages, group_size, n_kv_heads;
 };
+
+__device__ __forceinline__ void write_header(const PlanParams& p) {
+  p.head[kHMagic] = kPlanMagic; p.head[kHGroups] = p.groups; p.head[kHWidth] = p.width; p.head[kHStride] = p.stride;
+  p.head[kHPage] = 1 << p.page_shift; p.head[kHGroupSize] = p.group_size; p.head[kHKvHeads] = p.n_kv_heads;
+  p.head[kHBeams] = p.beams; p.head[kHSegments] = p.segments; p.head[kHPages] = p.num_pages;
+}
 
 // ---------------------------------------------------------------- plan
 // A CTA per (column block, segment of 256 table entries), a thread per entry: the block's beams fall into classes that hold the
@@ -178,7 +183,10 @@ __global__ void __launch_bounds__(kSeg) mepic_beam_plan_classes(const __grid_con
     total += warp_n[w];
   }
   const size_t part = static_cast<size_t>(block) * p.segments + seg;
-  if (tid == 0) p.sums[part] = total;
+  if (tid == 0) {
+    if (gridDim.x * gridDim.y > 1) p.sums[part] = total;
+    else { p.sums[0] = 0; p.sums[1] = total; write_header(p); }      // the only part: its sums are known
+  }
   int4* out = p.records + part * kSeg * p.beams;
   each_class([&](int page, int pos, unsigned same, int slots) {
     if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) { atomicOr(p.status, MEPIC_DEV_BAD_PAGE); page = 0; }
@@ -211,9 +219,7 @@ __global__ void __launch_bounds__(kScanThreads) mepic_beam_plan_sums(const __gri
   }
   if (tid == 0) {
     p.sums[n] = before;
-    p.head[kHMagic] = kPlanMagic; p.head[kHGroups] = p.groups; p.head[kHWidth] = p.width; p.head[kHStride] = p.stride;
-    p.head[kHPage] = 1 << p.page_shift; p.head[kHGroupSize] = p.group_size; p.head[kHKvHeads] = p.n_kv_heads;
-    p.head[kHBeams] = p.beams; p.head[kHSegments] = p.segments; p.head[kHPages] = p.num_pages;
+    write_header(p);
   }
 }
 
@@ -251,7 +257,7 @@ struct Cut { long long total, piece; };
 __device__ __forceinline__ Cut cut_of_line(const BeamParams& p) {
   Cut c;
   c.total = (static_cast<long long>(__ldg(p.sums + static_cast<size_t>(p.groups) * p.blocks * p.segments)) << p.log2_tpp) * p.n_kv_heads;
-  c.piece = max((c.total + p.workers - 1) / p.workers, static_cast<long long>(kMinPiece));
+  c.piece = max((c.total + p.workers - 1) / p.workers, 1ll);
   return c;
 }
 // A unit of the line: a column block under one kv head, records r0 .. r1-1 of the plan.
@@ -288,12 +294,11 @@ __device__ __forceinline__ Unit unit_at(const BeamParams& p, long long x, int la
 template <int D, bool FP8> constexpr int stage_bytes = 2 * kTile * D * (FP8 ? 1 : 2);
 // Per position of the table, for every two pairs of dims: (c, c', s, s') in fp32 or fp16.
 template <int D, bool FP8> constexpr int angle_bytes = D / 2 * (FP8 ? 4 : 8);
-// Stages of a warp's ring.  8-bit tiles are half as large: twice as many keep the same bytes in flight.
-template <bool FP8> constexpr int stages_of = FP8 ? 4 : 2;
+// Stages of a warp's ring, and positions of the table: as many as fit beside the rings (an anchor lasts as long).
+template <bool FP8, int W> constexpr int stages_of = FP8 && W <= 8 ? 4 : 2;
+template <bool FP8, int W> constexpr int angles_of = FP8 ? (W <= 8 ? 384 : 512) : 192;
 constexpr int kWarpWords = 128;      // bytes a warp has beside its ring: per stage 16 of tile data, 8 of scales and a barrier of 8
-// Positions of the table: as many as fit beside the rings.
-template <bool FP8> constexpr int angles_of = FP8 ? 384 : 192;
-template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (stages_of<FP8> * stage_bytes<D, FP8> + kWarpWords) + (angles_of<FP8> + 1) * angle_bytes<D, FP8> + 1024;
+template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (stages_of<FP8, W> * stage_bytes<D, FP8> + kWarpWords) + (angles_of<FP8, W> + 1) * angle_bytes<D, FP8> + 1024;
 
 // NT: tiles of 8 columns; W: warps of a CTA.
 __device__ __forceinline__ float4 lds128(uint32_t addr) {
@@ -311,9 +316,9 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   constexpr int KB = FP8 ? 1 : NB;
   constexpr int kBlockBytes = kTile * 128;
   constexpr int kStageBytes = stage_bytes<D, FP8>;
-  constexpr int kStages = stages_of<FP8>;
+  constexpr int kStages = stages_of<FP8, W>;
   static_assert(kStages * 32 <= kWarpWords, "tile data, scales and barriers of the ring");
-  constexpr int kAngleBytes = angle_bytes<D, FP8>, kAngles = angles_of<FP8>;
+  constexpr int kAngleBytes = angle_bytes<D, FP8>, kAngles = angles_of<FP8, W>;
 
   extern __shared__ unsigned char smem_dyn[];
   // 1024-byte alignment: the swizzle pattern is a function of the address bits
@@ -335,7 +340,10 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the merge kernel may move in as CTAs of this one retire
   if (!plan_fits(p)) return;                                         // (reported by the merge kernel)
   const Cut cut = cut_of_line(p);
-  if (static_cast<long long>(blockIdx.x) * W * cut.piece >= cut.total) return;
+  // Pieces of one tile each (fewer tiles than warps) are dealt round to the SMs, longer ones to the warps of a CTA in a row: they
+  // mostly share a unit, and its queries in the first-level cache.
+  const bool spread = cut.piece == 1;
+  if ((spread ? static_cast<long long>(blockIdx.x) : static_cast<long long>(blockIdx.x) * W * cut.piece) >= cut.total) return;
 
   if (lane == 0) {
 #pragma unroll
@@ -345,7 +353,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   }
   __syncwarp();
 
-  const long long w = static_cast<long long>(blockIdx.x) * W + wic;
+  const long long w = spread ? static_cast<long long>(wic) * gridDim.x + blockIdx.x : static_cast<long long>(blockIdx.x) * W + wic;
   const int n_tiles = static_cast<int>(max(min(cut.piece, cut.total - w * cut.piece), 0ll));      // 0: the line ends before this warp
   const long long x0 = min(w * cut.piece, cut.total - 1);
   const int G = p.group_size, tpp_mask = (1 << p.log2_tpp) - 1;
@@ -901,8 +909,12 @@ int sm_count(int* device) {
   if (dev < 64) known[dev].store(sms, std::memory_order_relaxed);
   return sms;
 }
-constexpr int kWarps = 8;
-size_t slots_of(const PlanShape& s, int n_kv_heads, int sms) { return static_cast<size_t>(s.groups) * s.blocks * n_kv_heads + static_cast<size_t>(sms) * kWarps; }
+// Warps of a CTA.  bf16 pages: HBM is the bound, and more tiles under way than those of eight warps make it slower (12 warps: 226 us
+// against 181 on 32 x 4 beams over 8,300 slots).  8-bit pages are bound by instructions and their latency: twelve, where registers
+// allow them (122 us against 130 on 8 x 4 beams over 33,000 slots).
+constexpr int kMaxWarps = 12;
+template <int NT, bool FP8> constexpr int warps_of = FP8 && NT <= 2 ? 12 : 8;
+size_t slots_of(const PlanShape& s, int n_kv_heads, int sms) { return static_cast<size_t>(s.groups) * s.blocks * n_kv_heads + static_cast<size_t>(sms) * kMaxWarps; }
 size_t workspace_bytes(const mepic_config_t* cfg, const PlanShape& s, int sms) {
   const size_t columns = static_cast<size_t>(s.beams) * (cfg->n_q_heads / cfg->n_kv_heads);
   return slots_of(s, cfg->n_kv_heads, sms) * columns * (cfg->head_dim + 2) * sizeof(float);
@@ -910,7 +922,7 @@ size_t workspace_bytes(const mepic_config_t* cfg, const PlanShape& s, int sms) {
 
 template <int D, int NT, bool FP8>
 int32_t launch_beam(BeamParams& p, int sms, int device, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t st) {
-  constexpr int W = kWarps;
+  constexpr int W = warps_of<NT, FP8>;
   constexpr size_t smem = smem_bytes<D, FP8, W>;
   static_assert(smem <= 232448, "shared memory of a CTA");
   static std::atomic<unsigned long long> prepared{0};      // devices on which the limit is raised
@@ -1023,10 +1035,11 @@ extern "C" int32_t mepic_beam_plan(const mepic_config_t* cfg, const mepic_beam_p
   if (e != cudaSuccess) { mepic_set_error("beam_plan: cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
   mepic_beam_plan_classes<<<dim3(static_cast<unsigned>(s.groups) * s.blocks, s.segments), kSeg, smem, st>>>(p);
   e = cudaGetLastError();
-  if (e == cudaSuccess) e = launch_dependent(mepic_beam_plan_sums, dim3(1), dim3(kScanThreads), st, p);
+  const bool sums = static_cast<long long>(s.groups) * s.blocks * s.segments > 1;
+  if (e == cudaSuccess && sums) e = launch_dependent(mepic_beam_plan_sums, dim3(1), dim3(kScanThreads), st, p);
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) { mepic_set_error("beam_plan: launch: %s", cudaGetErrorString(e)); return MEPIC_E_CUDA; }
-  mepic_count_launches(2);
+  mepic_count_launches(sums ? 2 : 1);
   return MEPIC_OK;
 }
 

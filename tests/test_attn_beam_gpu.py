@@ -271,7 +271,7 @@ def test_bad_lengths_pages_and_positions_are_reported_and_harmless():
 
 
 def test_a_copy_that_never_comes():
-    case = BeamCase(25, Hq=4, Hkv=1, D=128, P=16, width=3, specs=[(2000, 40)])
+    case = BeamCase(25, Hq=2, Hkv=1, D=128, P=16, width=3, specs=[(70000, 40)], theta=5e5)      # several tiles a worker
     case.device()
     case.batch()
     for tile in (0, 2):
