@@ -4,7 +4,7 @@
 // Bound: HBM.  A request's W beams of G query heads are up to 32 columns of one matrix product per kv head, so a page's K and V
 // serve W G query vectors for one read.  As in the per-request decode the keys are the M rows of both products
 // (S^T = K' Q^T, O^T = V^T P^T on mma.sync m16n8k16) and the columns are the N side: 8 columns a tile of the instruction, up to
-// four such tiles (NT).  The (column block, kv head, 16-key tile) triples of the batch form one line, cut into equal pieces, one
+// two such tiles (NT).  The (column block, kv head, 16-key tile) triples of the batch form one line, cut into equal pieces, one
 // per warp of a persistent grid, each with a ring of TMA stages of its own; pieces that end inside a column block leave partials
 // (reference, sum, unnormalised output) that a second kernel joins in a fixed order.
 //
@@ -35,7 +35,7 @@ namespace {
 using namespace mepic_dev;
 
 constexpr int kTile = 16;            // keys per staged tile
-constexpr int kMaxColumns = 32;      // columns of a column block
+constexpr int kMaxColumns = 16;      // columns of a column block
 // Cutting a number off after ten bits of mantissa makes it smaller, by 2^-11 of its power of two in the mean and by 2^-11 / (2 ln 2) of
 // itself where mantissas are spread as those of products are; the scores are made larger by as much for either factor.
 constexpr float kTf32Cut = 1.f + 2.f * 0x1p-11f * 0.7213475f;
@@ -294,11 +294,11 @@ __device__ __forceinline__ Unit unit_at(const BeamParams& p, long long x, int la
 template <int D, bool FP8> constexpr int stage_bytes = 2 * kTile * D * (FP8 ? 1 : 2);
 // Per position of the table, for every two pairs of dims: (c, c', s, s') in fp32 or fp16.
 template <int D, bool FP8> constexpr int angle_bytes = D / 2 * (FP8 ? 4 : 8);
-// Stages of a warp's ring, and positions of the table: as many as fit beside the rings (an anchor lasts as long).
-template <bool FP8, int W> constexpr int stages_of = FP8 && W <= 8 ? 4 : 2;
-template <bool FP8, int W> constexpr int angles_of = FP8 ? (W <= 8 ? 384 : 512) : 192;
+// Stages of a warp's ring; positions of the table, as many as fit beside the rings (an anchor lasts as long).
+constexpr int kStages = 2;
+template <bool FP8> constexpr int angles_of = FP8 ? 512 : 192;
 constexpr int kWarpWords = 128;      // bytes a warp has beside its ring: per stage 16 of tile data, 8 of scales and a barrier of 8
-template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (stages_of<FP8, W> * stage_bytes<D, FP8> + kWarpWords) + (angles_of<FP8, W> + 1) * angle_bytes<D, FP8> + 1024;
+template <int D, bool FP8, int W> constexpr size_t smem_bytes = static_cast<size_t>(W) * (kStages * stage_bytes<D, FP8> + kWarpWords) + (angles_of<FP8> + 1) * angle_bytes<D, FP8> + 1024;
 
 // NT: tiles of 8 columns; W: warps of a CTA.
 __device__ __forceinline__ float4 lds128(uint32_t addr) {
@@ -316,9 +316,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   constexpr int KB = FP8 ? 1 : NB;
   constexpr int kBlockBytes = kTile * 128;
   constexpr int kStageBytes = stage_bytes<D, FP8>;
-  constexpr int kStages = stages_of<FP8, W>;
   static_assert(kStages * 32 <= kWarpWords, "tile data, scales and barriers of the ring");
-  constexpr int kAngleBytes = angle_bytes<D, FP8>, kAngles = angles_of<FP8, W>;
+  constexpr int kAngleBytes = angle_bytes<D, FP8>, kAngles = angles_of<FP8>;
 
   extern __shared__ unsigned char smem_dyn[];
   // 1024-byte alignment: the swizzle pattern is a function of the address bits
@@ -447,12 +446,11 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   int u_block = -1, u_head = -1;
   unsigned all_beams = 0;
   int anchor = INT_MIN;
-  uint32_t beam_of[(NT + 1) / 2];            // beams of the columns 8 nt + 2 t, + 1 of this lane, a byte each
-  auto sees = [&](int nt, int c, unsigned beams) { return (beams >> (beam_of[nt / 2] >> (16 * (nt % 2) + 8 * c) & 31) & 1) != 0; };
+  unsigned see[NT][2];                       // beam bit of the columns 8 nt + 2 t, + 1 of this lane (0: no such column)
   int q_at[NT];                              // position of column 8 nt + g
-  constexpr bool TF32 = !FP8 && NT <= 2;     // QK^T in tf32 where the registers allow it
-  float qt[TF32 ? NT : 1][KS][4];            // B fragments of Q'^T in tf32: dims of the k-step's two column halves, pairs
-  uint32_t qf[NT][KS][2];                    // B fragments of Q'^T, column 8 nt + g
+  // B fragments of Q'^T, column 8 nt + g: bf16 pages in fp32 (the product takes them as tf32), 8-bit pages in fp16
+  float qt[FP8 ? 1 : NT][KS][4];             // dims of the k-step's two column halves, pairs
+  uint32_t qf[FP8 ? NT : 1][KS][2];
   float m_run[NT][2], l_run[NT][2];          // reference and this lane's share of the sum of columns 2 t, 2 t + 1
   float acc[NT][NV][4];                      // O^T: [dim g: column 2t, 2t+1 | dim g + 8: the same]
   float v_ref = kSmallScale, v_inv = 0x1p6f / kSmallScale;      // 8-bit pages: acc is in units of v_ref 2^-6; 2^6 / v_ref
@@ -502,12 +500,12 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       const float2 lo = bf16x2_to_float2(__ldg(src)), hi = bf16x2_to_float2(__ldg(src + D / 4));
       const float2 c = make_float2(cs.x, cs.z), sp = make_float2(cs.y * sn, cs.w * sn), sm = make_float2(-sp.x, -sp.y);
       const float2 a = fma2(lo, c, mul2(hi, sm)), b = fma2(lo, sp, mul2(hi, c));
-      if constexpr (TF32) {
+      if constexpr (!FP8) {
         qt[nt][j][2 * r] = a.x; qt[nt][j][2 * r + 1] = a.y;
         qt[nt][j + KH][2 * r] = b.x; qt[nt][j + KH][2 * r + 1] = b.y;
       } else {
-        qf[nt][j][r] = FP8 ? pack_f16x2(a.x, a.y) : pack_bf16x2(a.x, a.y);
-        qf[nt][j + KH][r] = FP8 ? pack_f16x2(b.x, b.y) : pack_bf16x2(b.x, b.y);
+        qf[nt][j][r] = pack_f16x2(a.x, a.y);
+        qf[nt][j + KH][r] = pack_f16x2(b.x, b.y);
       }
     };
     if (__all_sync(kFull, same)) {
@@ -537,7 +535,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       for (int r = 0; r < 2; ++r) {
         const float4 cs = lds128(angles_addr + kAngles * kAngleBytes + (16 * j + 2 * t + 8 * r) * 8);      // c, c', s, s'  (an even row)
 #pragma unroll
-        for (int nt = 0; nt < (TF32 ? NT : 0); ++nt) {
+        for (int nt = 0; nt < (FP8 ? 0 : NT); ++nt) {
           float &l0 = qt[nt][j][2 * r], &l1 = qt[nt][j][2 * r + 1], &h0 = qt[nt][j + KH][2 * r], &h1 = qt[nt][j + KH][2 * r + 1];
           const float a0 = fmaf(l0, cs.x, h0 * cs.z), b0 = fmaf(h0, cs.x, -(l0 * cs.z)), a1 = fmaf(l1, cs.y, h1 * cs.w), b1 = fmaf(h1, cs.y, -(l1 * cs.w));
           l0 = a0; h0 = b0; l1 = a1; h1 = b1;
@@ -564,9 +562,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          // a column that is none belongs to beam 31: no page does (with 32 beams of one head there is no such column)
-          const uint32_t beam = min((8 * nt + 2 * t + c) / G < nb ? (8 * nt + 2 * t + c) / G : 31, 31);
-          beam_of[nt / 2] = nt % 2 == 0 && c == 0 ? beam : beam_of[nt / 2] | beam << (16 * (nt % 2) + 8 * c);
+          const int beam = (8 * nt + 2 * t + c) / G;
+          see[nt][c] = beam < nb ? 1u << beam : 0u;
           m_run[nt][c] = -FLT_MAX; l_run[nt][c] = 0.f;
         }
 #pragma unroll
@@ -577,7 +574,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     unsigned beams;
     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(pos), "=r"(beams), "=r"(n_valid), "=r"(unused) : "r"(meta + stage * 16) : "memory");
     if (anchor == INT_MIN || static_cast<unsigned>(pos - anchor) > static_cast<unsigned>(span - kTile)) {
-      const bool on = TF32 && anchor != INT_MIN && pos - anchor == span && span <= p.max_position;
+      const bool on = !FP8 && anchor != INT_MIN && pos - anchor == span && span <= p.max_position;
       anchor = pos;
       if (on) advance_queries();
       else rotate_queries();
@@ -616,7 +613,6 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     }
 #pragma unroll
     for (int j = 0; j < KH; ++j) {
-      float2 kx[TF32 ? 4 : 1], ky[TF32 ? 4 : 1];
       uint32_t lo[4], hi[4];      // A fragments of k-steps j, j + KH: [key A, key B | key A, key B (second column half)]
       if constexpr (FP8) {
         uint32_t raw[4];          // [key A, key B of chunk j | of chunk j + KH], four dims each
@@ -644,6 +640,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
           mma_f16(sc[nt], hi[0], hi[1], hi[2], hi[3], qf[nt][j + KH][0], qf[nt][j + KH][1]);
         }
       } else {
+        float2 kx[4], ky[4];      // the same four places of either k-step, rotated, in fp32
         {
           // lane -> (matrix mi = lane / 8, row = lane % 8): key = 8 (mi & 1) + row, 16-byte chunk 2 j + (mi >> 1)
           const int mi = lane >> 3, key = ((mi & 1) << 3) + (lane & 7);
@@ -658,29 +655,21 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
           const float2 a = bf16x2_to_float2(lo[f]), b = bf16x2_to_float2(hi[f]);
           const float2 x = make_float2(fmaf(a.x, cs.x, -(b.x * cs.z)), fmaf(a.y, cs.y, -(b.y * cs.w)));
           const float2 y = make_float2(fmaf(a.x, cs.z, b.x * cs.x), fmaf(a.y, cs.w, b.y * cs.y));
-          if constexpr (TF32) { kx[f] = x; ky[f] = y; }
-          else { lo[f] = pack_bf16x2(x.x, x.y); hi[f] = pack_bf16x2(y.x, y.y); }
+          kx[f] = x; ky[f] = y;
         }
-        if constexpr (TF32) {
-          // one k-step of 16 dims is two of eight: a lane's two neighbouring dims stand at places t and t + 4
+        // one k-step of 16 dims is two of eight: a lane's two neighbouring dims stand at places t and t + 4
 #pragma unroll
-          for (int r = 0; r < 2; ++r)
+        for (int r = 0; r < 2; ++r)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              mma_tf32(sc[nt], kx[2 * r].x, kx[2 * r + 1].x, kx[2 * r].y, kx[2 * r + 1].y, qt[nt][j][2 * r], qt[nt][j][2 * r + 1]);
-              mma_tf32(sc[nt], ky[2 * r].x, ky[2 * r + 1].x, ky[2 * r].y, ky[2 * r + 1].y, qt[nt][j + KH][2 * r], qt[nt][j + KH][2 * r + 1]);
-            }
-        } else
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          mma_bf16(sc[nt], lo[0], lo[1], lo[2], lo[3], qf[nt][j][0], qf[nt][j][1]);
-          mma_bf16(sc[nt], hi[0], hi[1], hi[2], hi[3], qf[nt][j + KH][0], qf[nt][j + KH][1]);
-        }
+          for (int nt = 0; nt < NT; ++nt) {
+            mma_tf32(sc[nt], kx[2 * r].x, kx[2 * r + 1].x, kx[2 * r].y, kx[2 * r + 1].y, qt[nt][j][2 * r], qt[nt][j][2 * r + 1]);
+            mma_tf32(sc[nt], ky[2 * r].x, ky[2 * r + 1].x, ky[2 * r].y, ky[2 * r + 1].y, qt[nt][j + KH][2 * r], qt[nt][j + KH][2 * r + 1]);
+          }
       }
     }
     // ---- online softmax (log2 domain): keys A (0, 1) and B (2, 3) of columns 2t (0, 2) and 2t + 1 (1, 3)
     const bool some = __any_sync(kFull, (beams & all_beams) != all_beams);      // (the same in every lane: the vote says so to the compiler)
-    float v_scale = 0.f, s_scale = TF32 ? p.scale_log2 * kTf32Cut : p.scale_log2;
+    float v_scale = 0.f, s_scale = FP8 ? p.scale_log2 : p.scale_log2 * kTf32Cut;
     if constexpr (FP8) {
       float ks, vs;
       asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(ks), "=f"(vs) : "r"(scl + stage * 8) : "memory");
@@ -710,8 +699,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     if (some) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        if (!sees(nt, 0, beams)) { sc[nt][0] = -INFINITY; sc[nt][2] = -INFINITY; }
-        if (!sees(nt, 1, beams)) { sc[nt][1] = -INFINITY; sc[nt][3] = -INFINITY; }
+        if (!(see[nt][0] & beams)) { sc[nt][0] = -INFINITY; sc[nt][2] = -INFINITY; }
+        if (!(see[nt][1] & beams)) { sc[nt][1] = -INFINITY; sc[nt][3] = -INFINITY; }
       }
     }
     bool higher = false;
@@ -786,8 +775,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         for (int nt = 0; nt < NT; ++nt) {
           float x[4] = {0.f, 0.f, 0.f, 0.f};
           mma(x, va, pb[nt]);
-          if (sees(nt, 0, beams)) { acc[nt][db][0] += x[0]; acc[nt][db][2] += x[2]; }
-          if (sees(nt, 1, beams)) { acc[nt][db][1] += x[1]; acc[nt][db][3] += x[3]; }
+          if (see[nt][0] & beams) { acc[nt][db][0] += x[0]; acc[nt][db][2] += x[2]; }
+          if (see[nt][1] & beams) { acc[nt][db][1] += x[1]; acc[nt][db][3] += x[3]; }
         }
       });
     }
@@ -910,10 +899,10 @@ int sm_count(int* device) {
   return sms;
 }
 // Warps of a CTA.  bf16 pages: HBM is the bound, and more tiles under way than those of eight warps make it slower (12 warps: 226 us
-// against 181 on 32 x 4 beams over 8,300 slots).  8-bit pages are bound by instructions and their latency: twelve, where registers
-// allow them (122 us against 130 on 8 x 4 beams over 33,000 slots).
+// against 181 on 32 x 4 beams over 8,300 slots).  8-bit pages are bound by instructions and their latency: twelve (122 us against 130
+// on 8 x 4 beams over 33,000 slots).
 constexpr int kMaxWarps = 12;
-template <int NT, bool FP8> constexpr int warps_of = FP8 && NT <= 2 ? 12 : 8;
+template <bool FP8> constexpr int warps_of = FP8 ? kMaxWarps : 8;
 size_t slots_of(const PlanShape& s, int n_kv_heads, int sms) { return static_cast<size_t>(s.groups) * s.blocks * n_kv_heads + static_cast<size_t>(sms) * kMaxWarps; }
 size_t workspace_bytes(const mepic_config_t* cfg, const PlanShape& s, int sms) {
   const size_t columns = static_cast<size_t>(s.beams) * (cfg->n_q_heads / cfg->n_kv_heads);
@@ -922,7 +911,7 @@ size_t workspace_bytes(const mepic_config_t* cfg, const PlanShape& s, int sms) {
 
 template <int D, int NT, bool FP8>
 int32_t launch_beam(BeamParams& p, int sms, int device, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t st) {
-  constexpr int W = warps_of<NT, FP8>;
+  constexpr int W = warps_of<FP8>;
   constexpr size_t smem = smem_bytes<D, FP8, W>;
   static_assert(smem <= 232448, "shared memory of a CTA");
   static std::atomic<unsigned long long> prepared{0};      // devices on which the limit is raised
@@ -991,15 +980,10 @@ int32_t beam_call(const mepic_config_t* cfg, const mepic_attn_beam_args_t* a, co
   if (rc == MEPIC_OK) rc = fp8 ? mepic_make_pool_map_u8(cfg, a->v_pool, &map_v) : mepic_make_pool_map_halves(cfg, a->v_pool, &map_v);
   if (rc != MEPIC_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int nt = (p.columns + 7) / 8;
-#define MEPIC_BEAM_CASE(NT)                                                                                     \
-  if (nt == NT) return fp8 ? launch_beam<128, NT, true>(p, sms, device, map_k, map_v, st)                        \
-                           : cfg->head_dim == 128 ? launch_beam<128, NT, false>(p, sms, device, map_k, map_v, st) \
-                                                  : launch_beam<64, NT, false>(p, sms, device, map_k, map_v, st);
-  MEPIC_BEAM_CASE(1) MEPIC_BEAM_CASE(2) MEPIC_BEAM_CASE(3) MEPIC_BEAM_CASE(4)
-#undef MEPIC_BEAM_CASE
-  mepic_set_error("%s: %d columns", what, p.columns);
-  return MEPIC_E_INVAL;
+  const bool two = p.columns > 8;      // tiles of eight columns
+  if (fp8) return two ? launch_beam<128, 2, true>(p, sms, device, map_k, map_v, st) : launch_beam<128, 1, true>(p, sms, device, map_k, map_v, st);
+  if (cfg->head_dim == 128) return two ? launch_beam<128, 2, false>(p, sms, device, map_k, map_v, st) : launch_beam<128, 1, false>(p, sms, device, map_k, map_v, st);
+  return two ? launch_beam<64, 2, false>(p, sms, device, map_k, map_v, st) : launch_beam<64, 1, false>(p, sms, device, map_k, map_v, st);
 }
 
 }  // namespace
