@@ -732,14 +732,15 @@ int32_t mepic_rows_commit_fp8(const mepic_config_t* cfg, const mepic_rows_commit
  * row, a live beam (done[w] = 0, score[w] > -infinity) offers for every token v the candidate
  *     score[w] + x[v] - log sum_u exp(x[u]) ,
  * a finished one (done[w] != 0) the single candidate (pad_token, score[w]), a beam with score -infinity none; a token with
- * logit -infinity is no candidate.  The n_select best of a group are written in descending order, equal ones in ascending order
+ * logit -infinity, or with a score below -FLT_MAX, is no candidate.  The n_select best of a group are written in descending order, equal ones in ascending order
  * of (beam, token):
  *     parent[g][k]  the beam (0 .. width-1) that is continued, token[g][k], score_out[g][k] (rounded to fp32 once),
  *     done_out[g][k]  1 if the parent was finished or the token is eos_token, else 0,
  *     n_new[g][k]     1 if it goes on (what mepic_step_tables takes), 0 if it is finished or there is no such candidate;
  * where there are fewer candidates: parent = token = -1, score -infinity, done = n_new = 0.  Candidates are compared in 64 bits
  * (sum of exponentials: terms in fp32, added up in fp32 over at most 64 terms of one thread and in 64 bits beyond).
- * A row with a NaN or +infinity among its logits, or a score of that kind, sets MEPIC_DEV_BAD_LOGITS and offers nothing.  Rows of
+ * A row with a NaN or +infinity among its logits, a score of that kind, or a score whose difference from the logarithm exceeds
+ * FLT_MAX sets MEPIC_DEV_BAD_LOGITS and offers nothing.  Rows of
  * finished beams, and of beams with score -infinity, are not read.
  * logits: rows of vocab elements, logits_stride elements apart (0 = packed; otherwise at least vocab), any alignment of the type.
  * eos_token -1: no token ends a beam.  done may be NULL (none is finished).  workspace: mepic_beam_select_workspace bytes,
@@ -844,18 +845,19 @@ int32_t mepic_pages_copy_fp8(const mepic_config_t* cfg, const mepic_pages_copy_a
  * aligned, contents overwritten; it depends on the tables and lengths as they are when the call runs.
  *
  * mepic_attn_beam - mepic_attn_decode's formula for every row of the plan (one query, at position q_pos[row], over the row's
- * kv_len slots), each shared page read once per group (per 32 / G beams of it, where a group has more: the 32 / G beams' G query
- * heads are the columns of one matrix product).  A row of length 0 gets zeros.  Pages that a beam does not hold and slots at or
- * beyond its length have no influence on its output whatever bits they hold.  bf16 tensor-core products, fp32 accumulation; the
- * rotated q (with sm_scale folded in) and K and the softmax weights are rounded to bf16 once each.  q rows lie q_stride elements
- * apart (0 = packed; otherwise at least a packed row and a multiple of 8).  The plan must be one of the same config, groups,
- * width and table_stride that ran before on the GPU: another sets MEPIC_DEV_BAD_PLAN and `out` holds zeros.  The work is split over the
- * key axis across the GPU; partials go to the workspace (mepic_attn_beam_workspace bytes, 16-byte aligned, contents overwritten)
+ * kv_len slots), each shared page read once per group (where a group has more than 16 query heads per kv head, its beams together:
+ * once per 16 of them).  A row of length 0 gets zeros.  Pages that a beam does not hold and slots at or beyond its length have no
+ * influence on its output whatever bits they hold.  Tensor-core products, fp32 accumulation: the rotated q and K are taken as tf32
+ * (cut off after ten bits of mantissa; the mean of what that takes from a product is put back into the scores), the softmax weights
+ * are rounded to bf16.  Positions may be negative: only the distance of a row's q_pos from the positions of its group's pages has to
+ * stay within max_position.  q rows lie q_stride elements apart (0 = packed; otherwise at least a packed row and a multiple of 8).  The
+ * plan must be one of the same config, groups, width and table_stride that ran before on the GPU: another sets MEPIC_DEV_BAD_PLAN and
+ * `out` holds zeros.  The work is split over the key axis across the GPU; partials go to the workspace (mepic_attn_beam_workspace bytes, 16-byte aligned, contents overwritten)
  * and a second kernel merges them in a fixed order.  Two calls that overlap on the GPU must not share a workspace; they may share a
  * plan.  A captured call may be replayed with other lengths and tables, after their plan.
  *
- * mepic_attn_beam_fp8: over 8-bit pools (head_dim 128); the rotated q and K, the weights and V are carried in fp16 (|q| * sm_scale *
- * log2(e) must stay below 65504), the pages' V scales beside it in fp32.
+ * mepic_attn_beam_fp8: over 8-bit pools (head_dim 128); the rotated q and K, the weights and V are carried in fp16 (the rotated q must
+ * stay below 65504), the pages' K and V scales, of either sign, beside it in fp32.
  */
 typedef struct {
   const int32_t* page_ids;     /* [groups*width][table_stride] */

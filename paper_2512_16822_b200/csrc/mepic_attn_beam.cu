@@ -1,17 +1,28 @@
 // Attention of the newest token of every beam over the paged, un-rotated context, each page that beams of a request share read
 // once (see mepic_beam_plan and mepic_attn_beam in mepic.h).
 //
-// Bound: HBM.  A request's W beams of G query heads are up to 32 columns of one matrix product per kv head, so a page's K and V
-// serve W G query vectors for one read.  As in the per-request decode the keys are the M rows of both products
-// (S^T = K' Q^T, O^T = V^T P^T on mma.sync m16n8k16) and the columns are the N side: 8 columns a tile of the instruction, up to
-// two such tiles (NT).  The (column block, kv head, 16-key tile) triples of the batch form one line, cut into equal pieces, one
-// per warp of a persistent grid, each with a ring of TMA stages of its own; pieces that end inside a column block leave partials
-// (reference, sum, unnormalised output) that a second kernel joins in a fixed order.
+// Bound: HBM, for bf16 pages.  A request's W beams of G query heads are columns of one matrix product per kv head, so a page's K and
+// V serve them all for one read.  As in the per-request decode the keys are the M rows of both products (S^T = K' Q^T, O^T = V^T P^T
+// on mma.sync) and the columns are the N side: 8 columns a tile of the instruction, one or two such tiles (NT), which is what fits in
+// registers with 32 bits an element of Q and of O.  More columns are more blocks, and a page is read once for each: of 8 x 8 beams of
+// 4 heads (two blocks) half the second reads come from L2.  (Blocks that walk a page together, so that all of them do, halve the HBM
+// traffic and take as long, 160 us against 162: by then instructions are the bound; 32-column blocks spill.)  The (column block, kv
+// head, 16-key tile) triples of the batch form one line, cut into equal pieces, one per warp of a persistent grid, each with a ring
+// of TMA stages of its own; pieces that end inside a column block leave partials (reference, sum, unnormalised output) that a second
+// kernel joins in a fixed order.
+//
+// Measured: 32 x 4 beams of 4 heads, 8 kv heads, over 8,300 slots 167 us (5.9 TB/s of what has to be read); 8 x 8 beams with 700 slots of
+// their own 162 us; 8 x 4 beams over 33,000 slots of 8-bit pages 120 us (3.7 TB/s; bound by instructions and their latency); one
+// request of 3 beams 10 us, the chain plan -> line -> page -> merge.
 //
 // Rotation.  <R(qpos) q, R(pos) k> = <R(qpos - a) q, R(pos - a) k> for any anchor a.  A warp keeps its queries rotated for an anchor
-// and turns each key by pos - a, 0 <= pos - a < 64, from a table of 64 positions in shared memory; the anchor moves, and the
-// queries are rotated anew from what the caller gave, once in 64 consecutive positions.  So the keys are rotated once for all
-// columns, and the work that grows with the columns (rotating queries) is done for every fourth tile only.
+// and turns each key by pos - a from a table of angles in shared memory, 192 positions of it (8-bit pages: 512); the anchor moves once
+// in as many consecutive positions.  So the keys are rotated once for all columns, and the work that grows with the columns is done
+// for one tile in twelve.  Queries held in fp32 move on with the anchor where they are; others are rotated anew from the caller's.
+//
+// Precision.  bf16 pages: rotated q and K stay fp32 and enter tf32 products (ten bits of mantissa, cut off), which costs no time that
+// rounding them to bf16 would save (twice the products, but no packing) and halves the error; the softmax weights are rounded to bf16,
+// the type of V.  8-bit pages: codes are exact in fp16, where q, K and the weights are rounded once each.  All sums are fp32.
 //
 // Who sees what.  A record of the plan is one page of one column block: page, position, the beams that hold it, its filled slots.
 // Where every beam of the block holds it, nothing is masked.  Where only some do, the other columns' scores are -infinity and
@@ -54,7 +65,7 @@ struct PlanShape {
   int groups, width, blocks, beams, segments;      // column blocks of a group, beams of a block, segments of a row
   size_t off_len, off_rec, bytes;                  // in ints, in ints, in bytes
 };
-// A group's beams are dealt evenly to as few column blocks of at most 32 columns as hold them.
+// A group's beams are dealt evenly to as few column blocks of at most kMaxColumns columns as hold them.
 bool plan_shape(const mepic_config_t* cfg, int groups, int width, int stride, const char* what, PlanShape* s) {
   if (groups < 1 || width < 1 || width > MEPIC_BEAM_MAX_WIDTH) { mepic_set_error("%s: groups must be positive, width in 1..%d", what, MEPIC_BEAM_MAX_WIDTH); return false; }
   if (stride < 1 || static_cast<long long>(groups) * width * stride > 0x40000000LL || static_cast<long long>(groups) * width > 0xffffLL * 16) {
@@ -334,6 +345,15 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   // 8-bit pages: ldmatrix on bytes hands a lane four consecutive dims of a key, its transposing form four consecutive keys of a
   // dim; which dim or key stands at which place of the contraction is free as long as both operands agree.
   auto pair_of = [&](int j, int r) { return FP8 ? 16 * j + 4 * t + 2 * r : 16 * j + 2 * t + 8 * r; };
+  // what ldmatrix wants of this lane: the row (key) that it names of a tile, and its first 16-byte chunk under the swizzle
+  uint32_t k_lane, v_lane;
+  {
+    const int mi = lane >> 3, rr = lane & 7;
+    const int kk = FP8 ? 4 * (rr >> 1) + (rr & 1) + 2 * (mi & 1) : ((mi & 1) << 3) + rr, kc = FP8 ? KH * (mi >> 1) : mi >> 1;
+    const int vk = FP8 ? lane & 15 : ((mi >> 1) << 3) + rr, vc = FP8 ? lane >> 4 : mi & 1;
+    k_lane = kk * 128 + ((kc ^ (kk & 7)) << 4);
+    v_lane = vk * 128 + ((vc ^ (vk & 7)) << 4);
+  }
   const int keyA = FP8 ? 4 * (g >> 1) + (g & 1) : g, keyB = FP8 ? keyA + 2 : g + 8;      // keys of the lane's two rows
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the merge kernel may move in as CTAs of this one retire
@@ -425,8 +445,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   };
   for (int s = 0; s < kStages && issued < n_tiles; ++s) issue(s);
 
-  // positions the table has to reach: those of a piece, where it is short
-  const int span = static_cast<int>(min(static_cast<long long>(kAngles), max(cut.piece, 1ll) * kTile));
+  // positions the table has to reach: those of a piece, where it is short; no more than the caller's table has
+  const int span = static_cast<int>(min(static_cast<long long>(min(kAngles, max((p.max_position + 1) / kTile, 1) * kTile)), max(cut.piece, 1ll) * kTile));
   // ---- the table of angles: for position a and pairs 2u, 2u+1 the quadruple (c, c', s, s'), rows swizzled so that the eight lanes
   // that load together (two keys, four column groups) meet all banks
   // (the last row is that of `span` positions, by which an anchor moves)
@@ -601,31 +621,24 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     float sc[NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) { sc[nt][0] = 0.f; sc[nt][1] = 0.f; sc[nt][2] = 0.f; sc[nt][3] = 0.f; }
-    const int offA = pos - anchor + keyA, offB = pos - anchor + keyB;
-    const uint32_t row_a = angles_addr + offA * kAngleBytes, row_b = angles_addr + offB * kAngleBytes;
-    uint32_t cs_a[2], cs_b[2];      // addresses of the lane's quadruples, by column half r
-    if constexpr (!FP8) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        cs_a[r] = row_a + ((16 * t + 64 * r) ^ ((offA & 1) << 6));
-        cs_b[r] = row_b + ((16 * t + 64 * r) ^ ((offB & 1) << 6));
-      }
-    }
+    // Addresses: stages and rows of angles begin at multiples of 128 bytes, so that a chunk's place under the swizzle is the first
+    // chunk's with its number XORed in, and the second key's row of angles a fixed distance from the first's.
+    const int at = pos - anchor + keyA;
+    const uint32_t cs0 = angles_addr + at * kAngleBytes + ((16 * t) ^ ((at & 1) << 6)), cs1 = cs0 ^ 64;
+    constexpr int kRowB = (FP8 ? 2 : 8) * kAngleBytes;
+    const uint32_t k0 = ks_addr + k_lane, v0 = vs_addr + v_lane;
 #pragma unroll
     for (int j = 0; j < KH; ++j) {
       uint32_t lo[4], hi[4];      // A fragments of k-steps j, j + KH: [key A, key B | key A, key B (second column half)]
       if constexpr (FP8) {
         uint32_t raw[4];          // [key A, key B of chunk j | of chunk j + KH], four dims each
-        {
-          const int mi = lane >> 3, rr = lane & 7, key = 4 * (rr >> 1) + (rr & 1) + 2 * (mi & 1), chk = j + KH * (mi >> 1);
-          ldmatrix_x4(raw, ks_addr + key * 128 + ((chk ^ (key & 7)) << 4));
-        }
+        ldmatrix_x4(raw, k0 ^ (j << 4));
         e4m3x4_to_f16x2x2(raw[0], lo[0], lo[2]);
         e4m3x4_to_f16x2x2(raw[1], lo[1], lo[3]);
         e4m3x4_to_f16x2x2(raw[2], hi[0], hi[2]);
         e4m3x4_to_f16x2x2(raw[3], hi[1], hi[3]);
-        const int u8 = (16 * j + 4 * t) * 4;      // byte of the quadruple of pairs 16 j + 4 t
-        const float4 ca = lds128(row_a + (u8 ^ ((offA & 1) << 6))), cb = lds128(row_b + (u8 ^ ((offB & 1) << 6)));
+        const uint32_t cs_at = (j & 1 ? cs1 : cs0) + 128 * (j >> 1);
+        const float4 ca = lds128(cs_at), cb = lds128(cs_at + kRowB);
         const uint32_t cc[4] = {__float_as_uint(ca.x), __float_as_uint(cb.x), __float_as_uint(ca.z), __float_as_uint(cb.z)};
         const uint32_t ss[4] = {__float_as_uint(ca.y), __float_as_uint(cb.y), __float_as_uint(ca.w), __float_as_uint(cb.w)};
 #pragma unroll
@@ -641,17 +654,12 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         }
       } else {
         float2 kx[4], ky[4];      // the same four places of either k-step, rotated, in fp32
-        {
-          // lane -> (matrix mi = lane / 8, row = lane % 8): key = 8 (mi & 1) + row, 16-byte chunk 2 j + (mi >> 1)
-          const int mi = lane >> 3, key = ((mi & 1) << 3) + (lane & 7);
-          const int cl = 2 * j + (mi >> 1), chh = 2 * (j + KH) + (mi >> 1);
-          ldmatrix_x4(lo, ks_addr + (cl / 8) * kBlockBytes + key * 128 + (((cl % 8) ^ (key & 7)) << 4));
-          ldmatrix_x4(hi, ks_addr + (chh / 8) * kBlockBytes + key * 128 + (((chh % 8) ^ (key & 7)) << 4));
-        }
+        ldmatrix_x4(lo, k0 ^ (j % 4 << 5));      // chunks 2 j and 2 j + 1 of the lower half of the dims, and of the upper
+        ldmatrix_x4(hi, D == 128 ? (k0 ^ (j << 5)) + kBlockBytes : k0 ^ ((j + KH) << 5));
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
           const int r = f >> 1;
-          const float4 cs = lds128(((f & 1) ? cs_b : cs_a)[r] + 128 * j);      // c, c', s, s'
+          const float4 cs = lds128((r ? cs1 : cs0) + 128 * j + (f & 1) * kRowB);      // c, c', s, s'
           const float2 a = bf16x2_to_float2(lo[f]), b = bf16x2_to_float2(hi[f]);
           const float2 x = make_float2(fmaf(a.x, cs.x, -(b.x * cs.z)), fmaf(a.y, cs.y, -(b.y * cs.w)));
           const float2 y = make_float2(fmaf(a.x, cs.z, b.x * cs.x), fmaf(a.y, cs.w, b.y * cs.y));
@@ -675,11 +683,12 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(ks), "=f"(vs) : "r"(scl + stage * 8) : "memory");
       s_scale *= ks;
       // P carries the page's V scale relative to the largest met so far, and 2^6 so that small weights stay normal in fp16 (the largest reach 2^14)
-      const bool finite = vs <= FLT_MAX;      // a page's scale may be infinite or NaN: that is for the columns that see the page, not for the others
-      if (finite && vs > v_ref) {
-        const float f = v_ref / vs;
-        v_ref = vs;
-        v_inv = 0x1p6f / vs;
+      const float size = fabsf(vs);
+      const bool finite = size <= FLT_MAX;      // a page's scale may be infinite or NaN: that is for the columns that see the page, not for the others
+      if (finite && size > v_ref) {
+        const float f = v_ref / size;
+        v_ref = size;
+        v_inv = 0x1p6f / size;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -737,13 +746,11 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     }
     // ---- O^T += V^T P^T
     auto v_block = [&](int db, uint32_t (&va)[4]) {      // a0 dims g x keys 0-7, a1 dims g+8 x keys 0-7, a2 dims g x keys 8-15, a3 dims g+8 x keys 8-15
-      const int mi = lane >> 3, key = ((mi >> 1) << 3) + (lane & 7), ch = 2 * db + (mi & 1);
-      ldmatrix_x4_trans(va, vs_addr + (ch / 8) * kBlockBytes + key * 128 + (((ch % 8) ^ (key & 7)) << 4));
+      ldmatrix_x4_trans(va, (v0 ^ (db % 4 << 5)) + db / 4 * kBlockBytes);
     };
     auto v_blocks = [&](int c, uint32_t (&va)[2][4]) {      // 8-bit pages: dim blocks c and c + 1, keys 4t .. 4t+3 a lane
       uint32_t raw[4];          // [block c: dim g, dim g + 8 | block c + 1: the same]
-      const int key = lane & 15, chk = c + (lane >> 4);
-      ldmatrix_b8_trans_x2(raw, vs_addr + key * 128 + ((chk ^ (key & 7)) << 4));
+      ldmatrix_b8_trans_x2(raw, v0 ^ (c << 4));
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         e4m3x4_to_f16x2x2(raw[2 * m], va[m][0], va[m][2]);
@@ -795,7 +802,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
 // ---------------------------------------------------------------- merge
 // PER warps a (unit, column): the column's partials are dealt round to them, a lane owns D / 32 output dims.  Each warp joins its
 // own partials against the largest reference among them, and the PER results are joined in order.  Few partials a unit (a batch):
-// one warp, 2 us less than four; many (one long request): four.
+// one warp (32 x 4 beams, attention and merge: 168 us against 170 with four); many (one long request): four.
 constexpr int kMergeWarps = 8;
 template <int D, int PER>
 __global__ void __launch_bounds__(kMergeWarps * 32) mepic_beam_merge(const __grid_constant__ BeamParams p) {
@@ -898,9 +905,9 @@ int sm_count(int* device) {
   if (dev < 64) known[dev].store(sms, std::memory_order_relaxed);
   return sms;
 }
-// Warps of a CTA.  bf16 pages: HBM is the bound, and more tiles under way than those of eight warps make it slower (12 warps: 226 us
-// against 181 on 32 x 4 beams over 8,300 slots).  8-bit pages are bound by instructions and their latency: twelve (122 us against 130
-// on 8 x 4 beams over 33,000 slots).
+// Warps of a CTA.  bf16 pages: HBM is the bound, and more tiles under way than those of eight warps make it slower (12 warps, which
+// spill besides: 226 us against 181 on 32 x 4 beams over 8,300 slots).  8-bit pages are bound by instructions and their latency: twelve
+// (122 us against 130 on 8 x 4 beams over 33,000 slots).
 constexpr int kMaxWarps = 12;
 template <bool FP8> constexpr int warps_of = FP8 ? kMaxWarps : 8;
 size_t slots_of(const PlanShape& s, int n_kv_heads, int sms) { return static_cast<size_t>(s.groups) * s.blocks * n_kv_heads + static_cast<size_t>(sms) * kMaxWarps; }

@@ -154,6 +154,62 @@ def test_8_bit_pages_whose_values_are_tiny():
         assert (np.abs(got[r] - want) <= 7 * sigma + 1e-16).all()
 
 
+def test_scales_of_either_sign():
+    # the oracle takes a page's values as code x scale, whatever its sign
+    case = BeamCase(25, Hq=4, Hkv=2, D=128, P=16, width=3, specs=[(200, 30)], fp8=True)
+    case.device()
+    rng = np.random.default_rng(25)
+    for scales in (case.pools.k_scales, case.pools.v_scales):
+        scales.mul_(torch.from_numpy(rng.choice([-1.0, 1.0], size=tuple(scales.shape)).astype(np.float32)).cuda())
+    case.pools.v_scales.neg_()
+    case.pools.v_scales[int(case.page_ids[0, 0])].abs_().neg_()            # the first page met has a negative one
+    case.batch()
+    out = case.run(0.09)
+    torch.cuda.synchronize()
+    assert case.dev.read_status() == 0
+    case.check(out, 0.09)
+
+
+@pytest.mark.parametrize("D,fp8", [(64, False), (128, False), (128, True)])
+def test_negative_positions_and_a_rope_table_shorter_than_the_context(D, fp8):
+    # positions -176 .. 176, the query at 0: a key may be further from the first than the table reaches
+    case = BeamCase(26, Hq=4, Hkv=2, D=D, P=16, width=2, specs=[(320, 30)], fp8=fp8)
+    case.pos_base[:] = np.arange(case.pos_base.shape[1]) * 16 - 176
+    case.q_pos[:] = 0
+    case.max_position = 176
+    case.cfg = M.Config(16, 4, 2, D, case.num_pages, 176, case.theta)
+    case.device()
+    case.batch()
+    out = case.run(0.09)
+    torch.cuda.synchronize()
+    assert case.dev.read_status() == 0
+    case.check(out, 0.09)
+
+
+def test_what_a_dropped_call_holds_is_not_handed_out_while_it_runs():
+    case = BeamCase(27, Hq=8, Hkv=2, D=128, P=16, width=4, specs=[(700, 100), (90, 33)])
+    case.device()
+    side = torch.cuda.Stream()
+    case.batch()
+    case.plan.run(side), case.attn.run(0.09, side)                  # what happens once is not waited for below
+    torch.cuda.synchronize()
+    case.batch()
+    held = {t.data_ptr(): t.numel() for t in (case.plan.plan, case.attn.workspace)}
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(1_000_000_000)                            # half a second: the calls are still in the queue when their objects go
+        case.plan.run()
+        out = case.attn.run(0.09)
+    del case.plan, case.attn
+    early = not side.query()
+    others = [torch.empty(n, dtype=torch.uint8, device="cuda:0") for n in held.values()]
+    torch.cuda.synchronize()
+    assert early, "the kernels were through before the memory was asked for"
+    assert not {t.data_ptr() for t in others} & set(held)
+    assert case.dev.read_status() == 0
+    case.check(out, 0.09)
+
+
 def test_scores_whose_exponentials_do_not_fit():
     # scores of some thousands: only differences from the largest count
     case = BeamCase(18, Hq=8, Hkv=2, D=128, P=16, width=4, specs=[(200, 30)])
