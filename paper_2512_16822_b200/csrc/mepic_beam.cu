@@ -3,6 +3,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <stdint.h>
 
 #include <algorithm>
@@ -24,7 +25,8 @@ constexpr int kWidth = MEPIC_BEAM_MAX_WIDTH;
 // four threads (a SET: 64 tokens at least) their largest logit, nothing else.  The second has a CTA per group: the n_select best
 // tokens are not below the n_select-th largest of the sets' maxima, so only the few sets that reach it are read again, and of those
 // only the tokens that reach it are ranked.  (Every segment keeping its own n_select best, in the first pass, took a dozen
-// instructions a token more: 64 x 8 beams over 100,003 tokens in 65 us against {SEL_NOW}.)
+// instructions a token more: 64 x 8 beams over 100,003 fp32 tokens in 65 us against 41.)  The pass alone
+// takes 33 of them (6.2 TB/s); the join is a chain of five dependent round trips.
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelPieces = 8;                  // 16-byte pieces a thread reads
@@ -229,6 +231,7 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
       bad = bad || !(sum < INFINITY);              // NaN
       if (!(sum > 0.0)) what = 0;                  // every token is masked
       else l = static_cast<double>(most) + log(sum);
+      bad = bad || !(fabs(static_cast<double>(score) - l) <= FLT_MAX);      // what is added to every logit
     }
     if (score == -INFINITY) what = 0;
     if (bad) what = 0;
@@ -239,7 +242,10 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
     }
   }
   __syncthreads();
-  auto order_at = [&](int w, float x) -> uint64_t { return x > -INFINITY ? order_of(base[w] + (static_cast<double>(x) - lse[w])) : 0; };
+  auto order_at = [&](int w, float x) -> uint64_t {
+    const double d = base[w] + (static_cast<double>(x) - lse[w]);
+    return d >= -FLT_MAX ? order_of(d) : 0;          // (x = -infinity, or a score that fp32 does not hold: no candidate)
+  };
   auto beam_of = [&](int i) {                      // i / per
     int w = static_cast<int>(static_cast<float>(i) * inv_per);
     return w + (i - w * per >= per ? 1 : i < w * per ? -1 : 0);

@@ -150,6 +150,11 @@ def test_long_tables_and_many_groups():
     _run(t, t.rng.integers(-1, 3, size=(900, 3)))
 
 
+def test_the_most_groups_there_may_be():
+    t = Tables(21, G=M.MEPIC_STEP_MAX_BATCH, W=2, P=16, context=20, grown=20)
+    _run(t, t.rng.integers(-1, 2, size=(M.MEPIC_STEP_MAX_BATCH, 2)))
+
+
 def test_a_reserve_that_cannot_supply_the_copies():
     t = Tables(13, G=2, W=1, P=16, context=0, grown=40, spare=5, ragged=False)
     parent = np.zeros((2, 4), dtype=np.int64)

@@ -59,6 +59,11 @@ def _run(logits, scores, done=None, K=None, eos=None, pad=0):
     return op, dev
 
 
+def _op(logits, scores, K):
+    dev = RT.Device(CFG)
+    return RT.BeamSelect(dev, logits=logits, scores=torch.from_numpy(np.asarray(scores, dtype=np.float32)).cuda(), n_select=K), dev
+
+
 def _logits(rows, V, dtype, seed, std=2.5):
     g = torch.Generator(device="cuda:0").manual_seed(seed)
     return (torch.randn((rows, V), generator=g, device="cuda:0") * std).to(TYPES[dtype])
@@ -159,6 +164,29 @@ def test_the_types_lowest_value_is_a_candidate():
         x[:, 3] = 1.0
         x[:, 699] = torch.finfo(dtype).max if dtype != torch.float16 else 100.0
         _run(x, np.zeros((1, 2)), K=1)
+
+
+def test_scores_that_fp32_does_not_hold():
+    big = torch.finfo(torch.float32).max
+    # logits at either end: the lowest have scores of twice the lowest number, and are no candidates
+    x = torch.full((2, 900), -big, device="cuda:0")
+    x[:, 5], x[:, 700] = 1.0, big
+    op, dev = _op(x, np.array([[0.0, -1.0]]), 4)
+    got = op.run()
+    torch.cuda.synchronize()
+    assert dev.read_status() == 0
+    # (700: score less nothing; 5: 1 - big; the others -2 big)
+    assert got["token"].tolist() == [[700, 700, 5, 5]] and got["parent"].tolist() == [[0, 1, 0, 1]]
+    assert got["score"].tolist() == [[0.0, -1.0, -big, -big]]
+    op, dev = _op(x, np.array([[0.0, -1.0]]), 7)
+    got = op.run()
+    torch.cuda.synchronize()
+    assert dev.read_status() == 0 and got["token"].tolist() == [[700, 700, 5, 5, -1, -1, -1]] and got["n_new"].tolist() == [[1, 1, 1, 1, 0, 0, 0]]
+    # a score that less the logarithm fits no more
+    op, dev = _op(x, np.array([[-1e38, 0.0]]), 2)
+    got = op.run()
+    torch.cuda.synchronize()
+    assert dev.read_status() == M.MEPIC_DEV_BAD_LOGITS and got["token"].tolist() == [[700, 5]] and got["parent"].tolist() == [[1, 1]]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
