@@ -6,14 +6,14 @@
 // on mma.sync) and the columns are the N side: 8 columns a tile of the instruction, one or two such tiles (NT), which is what fits in
 // registers with 32 bits an element of Q and of O.  More columns are more blocks, and a page is read once for each: of 8 x 8 beams of
 // 4 heads (two blocks) half the second reads come from L2.  (Blocks that walk a page together, so that all of them do, halve the HBM
-// traffic and take as long, 160 us against 162: by then instructions are the bound; 32-column blocks spill.)  The (column block, kv
+// traffic and took as long, 160 us against 162: by then instructions are the bound; 32-column blocks spill.)  The (column block, kv
 // head, 16-key tile) triples of the batch form one line, cut into equal pieces, one per warp of a persistent grid, each with a ring
 // of TMA stages of its own; pieces that end inside a column block leave partials (reference, sum, unnormalised output) that a second
 // kernel joins in a fixed order.
 //
-// Measured: 32 x 4 beams of 4 heads, 8 kv heads, over 8,300 slots 167 us (5.9 TB/s of what has to be read); 8 x 8 beams with 700 slots of
-// their own 162 us; 8 x 4 beams over 33,000 slots of 8-bit pages 120 us (3.7 TB/s; bound by instructions and their latency); one
-// request of 3 beams 10 us, the chain plan -> line -> page -> merge.
+// Measured: 32 x 4 beams of 4 heads, 8 kv heads, over 8,300 slots 164 us (6 TB/s of what has to be read); 8 x 8 beams over 17,300 slots,
+// 700 of them their own, 158 us; 8 x 4 beams over 33,000 slots of 8-bit pages 113 us (3.9 TB/s; bound by instructions and their
+// latency); one request of 4 beams over 224 slots 11 us: launch, then the chain plan -> line -> page -> partials -> merge.
 //
 // Rotation.  <R(qpos) q, R(pos) k> = <R(qpos - a) q, R(pos - a) k> for any anchor a.  A warp keeps its queries rotated for an anchor
 // and turns each key by pos - a from a table of angles in shared memory, 192 positions of it (8-bit pages: 512); the anchor moves once
@@ -264,20 +264,21 @@ __device__ __forceinline__ bool plan_fits(const BeamParams& p) {
          __ldg(h + kHBeams) == p.beams && __ldg(h + kHSegments) == p.segments && __ldg(h + kHPages) == p.num_pages &&
          total >= 0 && total <= n * kSeg * p.beams;
 }
+// a / b where both are positive, in 32 bits where they fit (a tenth of the instructions).
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+  return a / b;
+}
 struct Cut { long long total, piece; };
 __device__ __forceinline__ Cut cut_of_line(const BeamParams& p) {
   Cut c;
   c.total = (static_cast<long long>(__ldg(p.sums + static_cast<size_t>(p.groups) * p.blocks * p.segments)) << p.log2_tpp) * p.n_kv_heads;
-  c.piece = max((c.total + p.workers - 1) / p.workers, 1ll);
+  c.piece = max(quotient(c.total + p.workers - 1, p.workers), 1ll);
   return c;
 }
 // A unit of the line: a column block under one kv head, records r0 .. r1-1 of the plan.
 struct Unit { int block, head, r0, r1; };
 __device__ __forceinline__ int begin_of(const BeamParams& p, int block) { return __ldg(p.sums + static_cast<size_t>(block) * p.segments); }
-__device__ __forceinline__ void bounds_of(const BeamParams& p, Unit& u) {
-  u.r0 = __ldg(p.sums + static_cast<size_t>(u.block) * p.segments);
-  u.r1 = __ldg(p.sums + static_cast<size_t>(u.block + 1) * p.segments);
-}
 // The unit after (block, head); false: there is none.
 __device__ __forceinline__ bool next_unit(const BeamParams& p, int& block, int& head) {
   if (++head < p.n_kv_heads) return true;
@@ -287,19 +288,28 @@ __device__ __forceinline__ bool next_unit(const BeamParams& p, int& block, int& 
   } while (begin_of(p, block) >= begin_of(p, block + 1));
   return true;
 }
-// The column block that place x of the line falls into, 32 candidates at a time (by a whole warp).
-__device__ __forceinline__ Unit unit_at(const BeamParams& p, long long x, int lane) {
-  int lo = 0, n = p.groups * p.blocks;                  // in [lo, lo + n): the last block whose begin is <= x
-  while (n > 1) {
-    const int step = (n + 31) / 32, at = lo + lane * step;
-    const bool below = lane * step < n && (static_cast<long long>(__ldg(p.sums + static_cast<size_t>(min(at, p.groups * p.blocks)) * p.segments)) << p.log2_tpp) * p.n_kv_heads <= x;
+// The column block that place x of the line falls into, 32 candidates at a time (by a whole warp).  candidate_of: a lane's first one,
+// which does not depend on x.
+__device__ __forceinline__ int candidate_of(const BeamParams& p, int lane) {
+  const int n = p.groups * p.blocks;
+  return begin_of(p, min(lane * ((n + 31) / 32), n));
+}
+__device__ __forceinline__ Unit unit_at(const BeamParams& p, long long x, int lane, int candidate) {
+  const int all = p.groups * p.blocks;
+  int lo = 0, n = all, begin = candidate;               // in [lo, lo + n): the last block whose begin is <= x
+  for (;;) {
+    const int step = (n + 31) / 32;
+    const bool below = lane * step < n && (static_cast<long long>(begin) << p.log2_tpp) * p.n_kv_heads <= x;
     const int k = 31 - __clz(__ballot_sync(kFull, below) | 1u);
-    n = min(step, lo + n - (lo + k * step));
+    if (step == 1) {
+      Unit u{lo + k, 0, __shfl_sync(kFull, begin, k), __shfl_sync(kFull, begin, min(k + 1, 31))};
+      if (k == 31) u.r1 = begin_of(p, u.block + 1);
+      return u;
+    }
+    n = min(step, n - k * step);
     lo += k * step;
+    begin = begin_of(p, min(lo + lane * ((n + 31) / 32), all));
   }
-  Unit u{lo, 0, 0, 0};
-  bounds_of(p, u);
-  return u;
 }
 
 template <int D, bool FP8> constexpr int stage_bytes = 2 * kTile * D * (FP8 ? 1 : 2);
@@ -357,12 +367,26 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   const int keyA = FP8 ? 4 * (g >> 1) + (g & 1) : g, keyB = FP8 ? keyA + 2 : g + 8;      // keys of the lane's two rows
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the merge kernel may move in as CTAs of this one retire
+  const int candidate = candidate_of(p, lane);
   if (!plan_fits(p)) return;                                         // (reported by the merge kernel)
   const Cut cut = cut_of_line(p);
   // Pieces of one tile each (fewer tiles than warps) are dealt round to the SMs, longer ones to the warps of a CTA in a row: they
   // mostly share a unit, and its queries in the first-level cache.
   const bool spread = cut.piece == 1;
   if ((spread ? static_cast<long long>(blockIdx.x) : static_cast<long long>(blockIdx.x) * W * cut.piece) >= cut.total) return;
+
+  // The table of angles is made of products, R(16 k + f) = R(16 k) R(f): only these 16 + kAngles / 16 rows of the caller's table are read
+  // (all 192 or 512 of them, by every SM at once, took 4.7 and 6.9 us; this takes 1.6 and 2).  A warp has the rows k = warp, warp + W
+  // ..., a lane two pairs of dims; asked for here, used once the first tiles are under way.
+  constexpr int kCoarse = (kAngles / kTile + W) / W;            // rows 16 k of a warp, that of kAngles among them
+  auto row_of = [&](int at) { return lane < D / 4 ? __ldg(reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(min(at, p.max_position)) * D + 4 * lane)) : make_float4(0.f, 0.f, 0.f, 0.f); };
+  float4 coarse[kCoarse], fine[kTile / 2];                      // c, s, c', s'
+  if (!spread) {
+#pragma unroll
+    for (int k = 0; k < kCoarse; ++k) coarse[k] = row_of(kTile * (wic + W * k));
+#pragma unroll
+    for (int f = 0; f < kTile / 2; ++f) fine[f] = row_of(f);
+  }
 
   if (lane == 0) {
 #pragma unroll
@@ -381,9 +405,9 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   int p_block, p_head, pr, pr_end, pt;                                 // column block, kv head, record, the block's last one, tile of the page
   int c_block, c_head, c_left;                                         // consumer: its unit, and the unit's tiles still to come
   {
-    const Unit u = unit_at(p, x0, lane);
+    const Unit u = unit_at(p, x0, lane, candidate);
     const long long in = x0 - (static_cast<long long>(u.r0) << p.log2_tpp) * p.n_kv_heads, per = static_cast<long long>(u.r1 - u.r0) << p.log2_tpp;
-    const int head = static_cast<int>(in / per);
+    const int head = static_cast<int>(quotient(in, per));
     const long long in_head = in - head * per;
     p_block = c_block = u.block; p_head = c_head = head;
     pr = u.r0 + static_cast<int>(in_head >> p.log2_tpp);
@@ -398,7 +422,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   int issued = 0;                                                      // tiles handed to the ring
   auto issue = [&](int stage) {
     if (pr < win0 || pr >= win0 + win_n) {
-      while (pseg + 1 < p.groups * p.blocks * p.segments && __ldg(p.sums + pseg + 1) <= pr) ++pseg;
+      for (unsigned past = kFull; past == kFull; pseg += __popc(past))      // the segment that record pr lies in
+        past = __ballot_sync(kFull, pseg + 1 + lane < p.groups * p.blocks * p.segments && __ldg(p.sums + pseg + 1 + lane) <= pr);
       const int s0 = __ldg(p.sums + pseg);
       const int at = pr - s0 + lane;
       win0 = pr;
@@ -450,13 +475,33 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   // ---- the table of angles: for position a and pairs 2u, 2u+1 the quadruple (c, c', s, s'), rows swizzled so that the eight lanes
   // that load together (two keys, four column groups) meet all banks
   // (the last row is that of `span` positions, by which an anchor moves)
-  for (int i = threadIdx.x; i < (span + 1) * (D / 4); i += W * 32) {
-    const int at = i / (D / 4), a = at < span ? at : kAngles, u = i % (D / 4);
-    const float4 cs = __ldg(reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(min(at, p.max_position)) * D + 4 * u));      // c, s, c', s'
+  auto put_row = [&](int at, const float4& cs) {      // c, s, c', s'
+    const int a = at < span ? at : kAngles;
+    if (at > span || lane >= D / 4) return;
     if constexpr (FP8) {
-      *reinterpret_cast<uint2*>(angles + a * kAngleBytes + ((u * 8) ^ ((a & 1) << 6))) = make_uint2(pack_f16x2(cs.x, cs.z), pack_f16x2(cs.y, cs.w));
+      *reinterpret_cast<uint2*>(angles + a * kAngleBytes + ((lane * 8) ^ ((a & 1) << 6))) = make_uint2(pack_f16x2(cs.x, cs.z), pack_f16x2(cs.y, cs.w));
     } else {
-      *reinterpret_cast<float4*>(angles + a * kAngleBytes + ((u * 16) ^ ((a & 1) << 6))) = make_float4(cs.x, cs.z, cs.y, cs.w);
+      *reinterpret_cast<float4*>(angles + a * kAngleBytes + ((lane * 16) ^ ((a & 1) << 6))) = make_float4(cs.x, cs.z, cs.y, cs.w);
+    }
+  };
+  if (spread) {                                        // pieces of a tile: no more than 17 rows
+    for (int at = wic; at <= span; at += W) put_row(at, row_of(at));
+  } else {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int k = 0; k < kCoarse; ++k) {
+        const float4 b = coarse[k];
+#pragma unroll
+        for (int f = 0; f < kTile / 2; ++f) {
+          const float4 x = fine[f];
+          put_row(kTile * (wic + W * k) + half * (kTile / 2) + f,
+                  make_float4(fmaf(b.x, x.x, -(b.y * x.y)), fmaf(b.x, x.y, b.y * x.x), fmaf(b.z, x.z, -(b.w * x.w)), fmaf(b.z, x.w, b.w * x.z)));
+        }
+      }
+      if (half == 0)
+#pragma unroll
+        for (int f = 0; f < kTile / 2; ++f) fine[f] = row_of(kTile / 2 + f);
     }
   }
   __syncthreads();
@@ -515,9 +560,9 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       sign[nt] = rel < 0 ? -1.f : 1.f;
       same = same && q_at[nt] == q0;
     }
-    auto rotate = [&](int nt, int j, int r, const float4& cs, float sn) {
-      const uint32_t* src = reinterpret_cast<const uint32_t*>(q_src[nt] + pair_of(j, r));
-      const float2 lo = bf16x2_to_float2(__ldg(src)), hi = bf16x2_to_float2(__ldg(src + D / 4));
+    // (8-bit pages: the two pairs of a k-step are neighbours, one load: 8 x 4 beams over 33,000 slots 115 -> 113 us)
+    auto rotate = [&](int nt, int j, int r, const uint2& raw, const float4& cs, float sn) {
+      const float2 lo = bf16x2_to_float2(raw.x), hi = bf16x2_to_float2(raw.y);
       const float2 c = make_float2(cs.x, cs.z), sp = make_float2(cs.y * sn, cs.w * sn), sm = make_float2(-sp.x, -sp.y);
       const float2 a = fma2(lo, c, mul2(hi, sm)), b = fma2(lo, sp, mul2(hi, c));
       if constexpr (!FP8) {
@@ -528,22 +573,37 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         qf[nt][j + KH][r] = pack_f16x2(b.x, b.y);
       }
     };
-    if (__all_sync(kFull, same)) {
-#pragma unroll
-      for (int j = 0; j < KH; ++j)
+    auto rotate_step = [&](int nt, int j, const float4 (&cs)[2], float sn) {
+      uint2 raw[2];
+      if constexpr (FP8) {
+        const uint2* src = reinterpret_cast<const uint2*>(q_src[nt] + pair_of(j, 0));
+        const uint2 lo = __ldg(src), hi = __ldg(src + D / 8);
+        raw[0] = make_uint2(lo.x, hi.x); raw[1] = make_uint2(lo.y, hi.y);
+      } else {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float4 cs = __ldg(reinterpret_cast<const float4*>(turn[0] + 2 * pair_of(j, r)));
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) rotate(nt, j, r, cs, sign[0]);
+          const uint32_t* src = reinterpret_cast<const uint32_t*>(q_src[nt] + pair_of(j, r));
+          raw[r] = make_uint2(__ldg(src), __ldg(src + D / 4));
         }
-    } else {
+      }
+      rotate(nt, j, 0, raw[0], cs[0], sn);
+      rotate(nt, j, 1, raw[1], cs[1], sn);
+    };
+    auto angles_of_step = [&](int nt, int j, float4 (&cs)[2]) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int r = 0; r < 2; ++r) cs[r] = __ldg(reinterpret_cast<const float4*>(turn[nt] + 2 * pair_of(j, r)));
+    };
+    const bool one_turn = __all_sync(kFull, same);
 #pragma unroll
-        for (int j = 0; j < KH; ++j)
+    for (int j = 0; j < KH; ++j) {
+      float4 cs[2];
+      angles_of_step(0, j, cs);
+      rotate_step(0, j, cs, sign[0]);
 #pragma unroll
-          for (int r = 0; r < 2; ++r) rotate(nt, j, r, __ldg(reinterpret_cast<const float4*>(turn[nt] + 2 * pair_of(j, r))), sign[nt]);
+      for (int nt = 1; nt < NT; ++nt) {
+        if (!one_turn) angles_of_step(nt, j, cs);
+        rotate_step(nt, j, cs, sign[nt]);
+      }
     }
   };
 
@@ -821,10 +881,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32) mepic_beam_merge(const __gri
   bool shows = false;
   if (fits && live) {
     const Cut cut = cut_of_line(p);
-    Unit u{block, head, 0, 0};
-    bounds_of(p, u);
-    const long long per = static_cast<long long>(u.r1 - u.r0) << p.log2_tpp, begin = (static_cast<long long>(u.r0) << p.log2_tpp) * p.n_kv_heads + head * per;
-    if (per > 0) { w0 = begin / cut.piece; w1 = (begin + per - 1) / cut.piece; }
+    const int r0 = begin_of(p, block);
+    const long long per = static_cast<long long>(begin_of(p, block + 1) - r0) << p.log2_tpp, begin = (static_cast<long long>(r0) << p.log2_tpp) * p.n_kv_heads + head * per;
+    if (per > 0) { w0 = quotient(begin, cut.piece); w1 = quotient(begin + per - 1, cut.piece); }
     shows = __ldg(p.lens + row) > 0;
   }
   // launched as a programmatic dependent of the attention kernel: its partials are complete and visible after this
