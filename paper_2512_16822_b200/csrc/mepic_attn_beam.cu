@@ -12,7 +12,7 @@
 // kernel joins in a fixed order.
 //
 // Measured: 32 x 4 beams of 4 heads, 8 kv heads, over 8,300 slots 164 us (6 TB/s of what has to be read); 8 x 8 beams over 17,300 slots,
-// 700 of them their own, 158 us; 8 x 4 beams over 33,000 slots of 8-bit pages 113 us (3.9 TB/s; bound by instructions and their
+// 700 of them their own, 155 us; 8 x 4 beams over 33,000 slots of 8-bit pages 108 us (4.1 TB/s; bound by instructions and their
 // latency); one request of 4 beams over 224 slots 11 us: launch, then the chain plan -> line -> page -> partials -> merge.
 //
 // Rotation.  <R(qpos) q, R(pos) k> = <R(qpos - a) q, R(pos - a) k> for any anchor a.  A warp keeps its queries rotated for an anchor
@@ -328,6 +328,12 @@ __device__ __forceinline__ float4 lds128(uint32_t addr) {
   return v;
 }
 
+__device__ __forceinline__ bool elect_one() {
+  uint32_t is;
+  asm volatile("{ .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p; }" : "=r"(is));
+  return is != 0;
+}
+
 template <int D, int NT, bool FP8, int W>
 __global__ void __launch_bounds__(W * 32, 1)
 mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
@@ -436,27 +442,31 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         win_vs = __ldg(p.v_scales + static_cast<size_t>(win.x) * p.n_kv_heads + p_head);
       }
     }
-    // the lane that holds the record issues the copies
-    if (lane == pr - win0) {
+    auto copy = [&](int page) {
+      if (w == 0 && issued == p.skip_tile) return;          // (test hook: one copy that never comes)
+      const uint32_t bar = smem_u32(&bars[stage]), dst = smem_u32(stage0 + stage * kStageBytes);
+      const int y = (page * p.n_kv_heads + p_head) * p.page_size + pt * kTile;      // row of the pool viewed as [rows][D]
+      mbar_expect_tx(bar, kStageBytes);
+      if constexpr (FP8) {
+        tma_load_2d(dst, &map_k, 0, y, bar);
+        tma_load_2d(dst + kBlockBytes, &map_v, 0, y, bar);
+      } else {
+        tma_load_3d(dst, &map_k, 0, y, 0, bar);
+        tma_load_3d(dst + NB * kBlockBytes, &map_v, 0, y, 0, bar);
+      }
+    };
+    // The lane that holds the record leaves what the tile's consumer needs.  bf16 pages: it also issues the copies (no registers for
+    // another way: 8 x 8 beams 157 us against 164); 8-bit pages: an elected one does, which takes fewer instructions (108 us against 111).
+    const int holds = pr - win0;
+    if (lane == holds) {
       const int n_valid = min(win.w - pt * kTile, kTile);
       asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%3};" ::"r"(meta + stage * 16), "r"(win.y + pt * kTile), "r"(win.z), "r"(n_valid) : "memory");
       if constexpr (FP8) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(scl + stage * 8), "f"(win_ks), "f"(win_vs) : "memory");
-      if (!(w == 0 && issued == p.skip_tile)) {        // (test hook: one copy that never comes)
-        const uint32_t bar = smem_u32(&bars[stage]), dst = smem_u32(stage0 + stage * kStageBytes);
-        if (n_valid <= 0) {
-          mbar_expect_tx(bar, 0);                           // a tile of the page that holds no slot
-        } else {
-          const int y = (win.x * p.n_kv_heads + p_head) * p.page_size + pt * kTile;      // row of the pool viewed as [rows][D]
-          mbar_expect_tx(bar, kStageBytes);
-          if constexpr (FP8) {
-            tma_load_2d(dst, &map_k, 0, y, bar);
-            tma_load_2d(dst + kBlockBytes, &map_v, 0, y, bar);
-          } else {
-            tma_load_3d(dst, &map_k, 0, y, 0, bar);
-            tma_load_3d(dst + NB * kBlockBytes, &map_v, 0, y, 0, bar);
-          }
-        }
-      }
+      else copy(win.x);
+    }
+    if constexpr (FP8) {
+      const int page = __shfl_sync(kFull, win.x, holds);
+      if (elect_one()) copy(page);
     }
     ++issued;
     if (pt < tpp_mask) { ++pt; return; }
@@ -516,7 +526,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   // B fragments of Q'^T, column 8 nt + g: bf16 pages in fp32 (the product takes them as tf32), 8-bit pages in fp16
   float qt[FP8 ? 1 : NT][KS][4];             // dims of the k-step's two column halves, pairs
   uint32_t qf[FP8 ? NT : 1][KS][2];
-  float m_run[NT][2], l_run[NT][2];          // reference and this lane's share of the sum of columns 2 t, 2 t + 1
+  float2 m_neg[NT], l_run[NT];               // the negative of the reference, and this lane's share of the sum, of columns 2 t, 2 t + 1
   float acc[NT][NV][4];                      // O^T: [dim g: column 2t, 2t+1 | dim g + 8: the same]
   float v_ref = kSmallScale, v_inv = 0x1p6f / kSmallScale;      // 8-bit pages: acc is in units of v_ref 2^-6; 2^6 / v_ref
 
@@ -528,7 +538,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float l = l_run[nt][c];
+        float l = c ? l_run[nt].y : l_run[nt].x;
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(kFull, l, o);
         const int col = 8 * nt + 2 * t + c;
@@ -536,7 +546,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
           float* dst = p.part_o + (slot * p.columns + col) * D;
 #pragma unroll
           for (int db = 0; db < NV; ++db) { dst[16 * db + g] = acc[nt][db][c] * unit; dst[16 * db + 8 + g] = acc[nt][db][2 + c] * unit; }
-          if (g == 0) p.part_ml[slot * p.columns + col] = make_float2(m_run[nt][c], l);
+          if (g == 0) p.part_ml[slot * p.columns + col] = make_float2(-(c ? m_neg[nt].y : m_neg[nt].x), l);
         }
       }
   };
@@ -644,8 +654,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         for (int c = 0; c < 2; ++c) {
           const int beam = (8 * nt + 2 * t + c) / G;
           see[nt][c] = beam < nb ? 1u << beam : 0u;
-          m_run[nt][c] = -FLT_MAX; l_run[nt][c] = 0.f;
         }
+        m_neg[nt] = make_float2(FLT_MAX, FLT_MAX); l_run[nt] = make_float2(0.f, 0.f);
 #pragma unroll
         for (int db = 0; db < NV; ++db) { acc[nt][db][0] = 0.f; acc[nt][db][1] = 0.f; acc[nt][db][2] = 0.f; acc[nt][db][3] = 0.f; }
       }
@@ -756,52 +766,65 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       }
       v_scale = finite ? vs * v_inv : __int_as_float(0x7fffffff);
     }
+    // d: the scores less the reference, of keys A (0) and B (1)
+    float2 d[NT][2];
+    const float2 s_scale2 = make_float2(s_scale, s_scale);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) { sc[nt][0] *= s_scale; sc[nt][1] *= s_scale; sc[nt][2] *= s_scale; sc[nt][3] *= s_scale; }
+    for (int nt = 0; nt < NT; ++nt) {
+      d[nt][0] = fma2(make_float2(sc[nt][0], sc[nt][1]), s_scale2, m_neg[nt]);
+      d[nt][1] = fma2(make_float2(sc[nt][2], sc[nt][3]), s_scale2, m_neg[nt]);
+    }
     if (n_valid < kTile) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        if (keyA >= n_valid) { sc[nt][0] = -INFINITY; sc[nt][1] = -INFINITY; }
-        if (keyB >= n_valid) { sc[nt][2] = -INFINITY; sc[nt][3] = -INFINITY; }
+        if (keyA >= n_valid) d[nt][0] = make_float2(-INFINITY, -INFINITY);
+        if (keyB >= n_valid) d[nt][1] = make_float2(-INFINITY, -INFINITY);
       }
     }
     if (some) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        if (!(see[nt][0] & beams)) { sc[nt][0] = -INFINITY; sc[nt][2] = -INFINITY; }
-        if (!(see[nt][1] & beams)) { sc[nt][1] = -INFINITY; sc[nt][3] = -INFINITY; }
+        if (!(see[nt][0] & beams)) { d[nt][0].x = -INFINITY; d[nt][1].x = -INFINITY; }
+        if (!(see[nt][1] & beams)) { d[nt][0].y = -INFINITY; d[nt][1].y = -INFINITY; }
       }
     }
-    bool higher = false;
+    float top = -INFINITY;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) higher = higher || fmaxf(sc[nt][0], sc[nt][2]) > m_run[nt][0] + kLag || fmaxf(sc[nt][1], sc[nt][3]) > m_run[nt][1] + kLag;
+    for (int nt = 0; nt < NT; ++nt) top = fmaxf(fmaxf(fmaxf(top, d[nt][0].x), fmaxf(d[nt][0].y, d[nt][1].x)), d[nt][1].y);
     // the references move only if some lane saw a score well above: any reference gives the same softmax as long as no weight
     // overflows (with 16 columns some column's largest score moves in two tiles of five, by little)
-    if (__any_sync(kFull, higher)) {
+    if (__any_sync(kFull, top > kLag)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float mx0 = fmaxf(sc[nt][0], sc[nt][2]), mx1 = fmaxf(sc[nt][1], sc[nt][3]);
+        // (once more from the scores: less a reference of -FLT_MAX nothing is left of them)
+        auto score = [&](float less, float x) { return less == -INFINITY ? less : x * s_scale; };
+        float mx0 = fmaxf(score(d[nt][0].x, sc[nt][0]), score(d[nt][1].x, sc[nt][2])), mx1 = fmaxf(score(d[nt][0].y, sc[nt][1]), score(d[nt][1].y, sc[nt][3]));
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) { mx0 = fmaxf(mx0, __shfl_xor_sync(kFull, mx0, o)); mx1 = fmaxf(mx1, __shfl_xor_sync(kFull, mx1, o)); }
-        const float n0 = fmaxf(m_run[nt][0], mx0), n1 = fmaxf(m_run[nt][1], mx1);
-        const float a0 = ex2(m_run[nt][0] - n0), a1 = ex2(m_run[nt][1] - n1);
-        m_run[nt][0] = n0; m_run[nt][1] = n1;
-        l_run[nt][0] *= a0; l_run[nt][1] *= a1;
+        const float2 n = make_float2(fminf(m_neg[nt].x, -mx0), fminf(m_neg[nt].y, -mx1));
+        const float a0 = ex2(n.x - m_neg[nt].x), a1 = ex2(n.y - m_neg[nt].y);
+        m_neg[nt] = n;
+        l_run[nt] = mul2(l_run[nt], make_float2(a0, a1));
 #pragma unroll
         for (int db = 0; db < NV; ++db) { acc[nt][db][0] *= a0; acc[nt][db][1] *= a1; acc[nt][db][2] *= a0; acc[nt][db][3] *= a1; }
+        auto less = [&](float was, float x, float m) { return was == -INFINITY ? was : fmaf(x, s_scale, m); };
+        d[nt][0] = make_float2(less(d[nt][0].x, sc[nt][0], n.x), less(d[nt][0].y, sc[nt][1], n.y));
+        d[nt][1] = make_float2(less(d[nt][1].x, sc[nt][2], n.x), less(d[nt][1].y, sc[nt][3], n.y));
       }
     }
     uint32_t pb[NT][2];                    // B fragments of P^T: the transposes of the two 8 x 8 blocks (key row, columns)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float p0 = ex2(sc[nt][0] - m_run[nt][0]), p1 = ex2(sc[nt][1] - m_run[nt][1]), p2 = ex2(sc[nt][2] - m_run[nt][0]), p3 = ex2(sc[nt][3] - m_run[nt][1]);
-      l_run[nt][0] += p0 + p2; l_run[nt][1] += p1 + p3;
+      float2 pa = make_float2(ex2(d[nt][0].x), ex2(d[nt][0].y)), pc = make_float2(ex2(d[nt][1].x), ex2(d[nt][1].y));
+      l_run[nt] = add2(l_run[nt], add2(pa, pc));
       if constexpr (FP8) {
-        pb[nt][0] = movmatrix_trans(pack_f16x2(p0 * v_scale, p1 * v_scale));
-        pb[nt][1] = movmatrix_trans(pack_f16x2(p2 * v_scale, p3 * v_scale));
+        const float2 v2 = make_float2(v_scale, v_scale);
+        pa = mul2(pa, v2); pc = mul2(pc, v2);
+        pb[nt][0] = movmatrix_trans(pack_f16x2(pa.x, pa.y));
+        pb[nt][1] = movmatrix_trans(pack_f16x2(pc.x, pc.y));
       } else {
-        pb[nt][0] = movmatrix_trans(pack_bf16x2(p0, p1));
-        pb[nt][1] = movmatrix_trans(pack_bf16x2(p2, p3));
+        pb[nt][0] = movmatrix_trans(pack_bf16x2(pa.x, pa.y));
+        pb[nt][1] = movmatrix_trans(pack_bf16x2(pc.x, pc.y));
       }
     }
     // ---- O^T += V^T P^T
