@@ -885,7 +885,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
 // ---------------------------------------------------------------- merge
 // PER warps a (unit, column): the column's partials are dealt round to them, a lane owns D / 32 output dims.  Each warp joins its
 // own partials against the largest reference among them, and the PER results are joined in order.  Few partials a unit (a batch):
-// one warp (32 x 4 beams, attention and merge: 168 us against 170 with four); many (one long request): four.
+// one warp (32 x 4 beams, attention and merge: 165 us against 167 with four); many (one long request): four.
 constexpr int kMergeWarps = 8;
 template <int D, int PER>
 __global__ void __launch_bounds__(kMergeWarps * 32) mepic_beam_merge(const __grid_constant__ BeamParams p) {
@@ -930,16 +930,22 @@ __global__ void __launch_bounds__(kMergeWarps * 32) mepic_beam_merge(const __gri
 #pragma unroll
     for (int i = 0; i < E; ++i) o[i] *= was;
     const int n = static_cast<int>(min((w1 - k0) / PER + 1, 32ll));
-#pragma unroll 4
-    for (int q = 0; q < n; ++q) {
-      const float w = __shfl_sync(kFull, wgt, q);
-      const float* src = p.part_o + ((unit + k0 + static_cast<long long>(q) * PER) * p.columns + col) * D + E * lane;
-      if constexpr (E == 4) {
-        const float4 x = *reinterpret_cast<const float4*>(src);
-        o[0] += x.x * w; o[1] += x.y * w; o[2] += x.z * w; o[3] += x.w * w;
-      } else {
-        const float2 x = *reinterpret_cast<const float2*>(src);
-        o[0] += x.x * w; o[1] += x.y * w;
+    for (int q = 0; q < n; q += 4) {      // four of them side by side; eight take registers that keep CTAs out: 32 x 4 beams 167 us against 165
+      float x[4][E] = {};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (q + k < n) {
+          const float* src = p.part_o + ((unit + k0 + static_cast<long long>(q + k) * PER) * p.columns + col) * D + E * lane;
+          if constexpr (E == 4) *reinterpret_cast<float4*>(x[k]) = *reinterpret_cast<const float4*>(src);
+          else *reinterpret_cast<float2*>(x[k]) = *reinterpret_cast<const float2*>(src);
+        }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float w = __shfl_sync(kFull, wgt, (q + k) & 31);      // (0 past the last)
+        if (q + k < n) {
+#pragma unroll
+          for (int i = 0; i < E; ++i) o[i] += x[k][i] * w;
+        }
       }
     }
   }
