@@ -5,8 +5,8 @@
 // V serve them all for one read.  As in the per-request decode the keys are the M rows of both products (S^T = K' Q^T, O^T = V^T P^T
 // on mma.sync) and the columns are the N side: 8 columns a tile of the instruction, one or two such tiles (NT), which is what fits in
 // registers with 32 bits an element of Q and of O.  More columns are more blocks, and a page is read once for each: of 8 x 8 beams of
-// 4 heads (two blocks) half the second reads come from L2.  (Blocks that walk a page together, so that all of them do, halve the HBM
-// traffic and took as long, 160 us against 162: by then instructions are the bound; 32-column blocks spill.)  The (column block, kv
+// 4 heads, two blocks, 0.92 GB come from HBM where 0.50 would do.  (Blocks that walk a page together halved that and took as long, 160
+// us against 162 then: the bound becomes the latency of a tile's instructions; 32-column blocks spill.)  The (column block, kv
 // head, 16-key tile) triples of the batch form one line, cut into equal pieces, one per warp of a persistent grid, each with a ring
 // of TMA stages of its own; pieces that end inside a column block leave partials (reference, sum, unnormalised output) that a second
 // kernel joins in a fixed order.
@@ -22,7 +22,8 @@
 //
 // Precision.  bf16 pages: rotated q and K stay fp32 and enter tf32 products (ten bits of mantissa, cut off), which costs no time that
 // rounding them to bf16 would save (twice the products, but no packing) and halves the error; the softmax weights are rounded to bf16,
-// the type of V.  8-bit pages: codes are exact in fp16, where q, K and the weights are rounded once each.  All sums are fp32.
+// the type of V.  8-bit pages: codes are exact in fp16; angles, rotated q and K and the weights are rounded to it.  All sums are
+// fp32.
 //
 // Who sees what.  A record of the plan is one page of one column block: page, position, the beams that hold it, its filled slots.
 // Where every beam of the block holds it, nothing is masked.  Where only some do, the other columns' scores are -infinity and
