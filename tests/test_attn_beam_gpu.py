@@ -90,6 +90,27 @@ def test_rows_longer_than_a_segment_of_the_plan():
     _run(BeamCase(13, Hq=8, Hkv=2, D=64, P=16, width=4, specs=[(4100, 3000), (10, 0), (8000, 500)], theta=5e5))
 
 
+def test_more_groups_than_are_looked_through_in_two_rounds():
+    # 32 column blocks are told apart at a time: 1,200 take three rounds; many of the groups have nothing
+    rng = np.random.default_rng(28)
+    specs = [(int(rng.integers(0, 40)) * int(rng.integers(0, 2)), int(rng.integers(0, 20)) * int(rng.integers(0, 2))) for _ in range(1200)]
+    case = BeamCase(28, Hq=4, Hkv=2, D=64, P=16, width=2, specs=specs)
+    _run(case, which=list(range(0, 2400, 41)) + [2398, 2399])
+
+
+def test_a_row_of_more_segments_than_are_looked_through_at_a_time():
+    # 33 stretches of 256 table entries and a part of one
+    case = BeamCase(29, Hq=2, Hkv=1, D=64, P=16, width=2, specs=[(136_000, 40)], theta=5e5)
+    case.pos_base = (case.pos_base // 8).astype(np.int32)             # (positions run into one another: the rope table need not reach as far)
+    case.finish()
+    _run(case)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_large_pages(fp8):
+    _run(BeamCase(30, Hq=4, Hkv=2, D=128, P=512, width=3, specs=[(1024, 700), (0, 1), (300, 212)], fp8=fp8))
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 def test_what_a_beam_does_not_hold_has_no_influence(fp8):
     case = BeamCase(14, Hq=8, Hkv=2, D=128, P=16, width=4, specs=[(64, 20), (0, 9)], fp8=fp8)

@@ -165,6 +165,15 @@ def test_a_reserve_that_cannot_supply_the_copies():
     assert want["used"] == len(t.reserve)
 
 
+def test_no_reserve_at_all():
+    t = Tables(22, G=2, W=2, P=16, context=64, grown=0, spare=0)       # whole pages of the store's: nothing to copy, nothing to give back
+    assert t.reserve.size == 0
+    _run(t, np.array([[1, 0], [0, 0]]))
+    t.kv[:] = 60
+    want, _ = _run(t, np.array([[1, 0], [0, 0]]))                      # a copy each
+    assert want["status"] == M.MEPIC_DEV_NO_PAGES
+
+
 def test_a_reserve_that_would_get_back_more_than_it_gave():
     t = Tables(14, G=2, W=4, P=16, context=30, grown=90)
     t.used = 1

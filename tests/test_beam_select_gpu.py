@@ -200,6 +200,10 @@ def test_a_row_with_nan_or_infinity_offers_nothing(dtype, what, at):
     _run(x, _scores(2, 3, 9), K=3)
 
 
+def test_the_most_beams_there_may_be():
+    _run(_logits(65535, 6, "bf16", 12), _scores(13107, 5, 12), K=3)
+
+
 def test_scores_that_are_no_numbers():
     x = _logits(6, 3000, "bf16", 10)
     _run(x, np.array([[0.0, -np.inf, -1.0], [-np.inf, -np.inf, -np.inf]]), K=4)
