@@ -5,8 +5,9 @@
 // V serve them all for one read.  As in the per-request decode the keys are the M rows of both products (S^T = K' Q^T, O^T = V^T P^T
 // on mma.sync) and the columns are the N side: 8 columns a tile of the instruction, one or two such tiles (NT), which is what fits in
 // registers with 32 bits an element of Q and of O.  More columns are more blocks, and a page is read once for each: of 8 x 8 beams of
-// 4 heads, two blocks, 0.92 GB come from HBM where 0.50 would do.  (Blocks that walk a page together halved that and took as long, 160
-// us against 162 then: the bound becomes the latency of a tile's instructions; 32-column blocks spill.)  The (column block, kv
+// 4 heads, two blocks, 0.92 GB come from HBM where 0.50 would do.  (Blocks that walk a page together halved that: 151
+// us against 155, the bound being the latency of a tile's instructions by then, but 5 x 5 heads took 39 us against 37 and 8-bit pages,
+// out of registers, 123 against 107; 32-column blocks spill.)  The (column block, kv
 // head, 16-key tile) triples of the batch form one line, cut into equal pieces, one per warp of a persistent grid, each with a ring
 // of TMA stages of its own; pieces that end inside a column block leave partials (reference, sum, unnormalised output) that a second
 // kernel joins in a fixed order.
