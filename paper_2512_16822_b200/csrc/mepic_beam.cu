@@ -459,8 +459,8 @@ struct Group {
   int parent[kWidth], len[kWidth];       // new beam -> beam (-1: none); beam -> slots
   unsigned copies;                       // new beams that copy
 };
-__device__ void load_group(const ForkParams& p, int g, Group& s, bool report) {
-  const int tid = threadIdx.x, Wi = p.a.width_in, Wo = p.a.width_out, P = 1 << p.page_shift;
+__device__ void load_lengths(const ForkParams& p, int g, Group& s, bool report) {
+  const int tid = threadIdx.x, Wi = p.a.width_in, Wo = p.a.width_out;
   const long long room = min(static_cast<long long>(p.a.table_stride) << p.page_shift, 0x7fffffffll);
   if (tid == 0) s.copies = 0;
   if (tid < Wi) {
@@ -474,19 +474,35 @@ __device__ void load_group(const ForkParams& p, int g, Group& s, bool report) {
     s.parent[tid - 32] = q;
   }
   __syncthreads();
-  // every pair of new beams side by side: does j keep k from keeping its partly filled last page?
-  const int32_t* ids = p.a.page_ids + static_cast<size_t>(g) * Wi * p.a.table_stride;
-  for (int i = tid; i < Wo * Wo; i += kForkThreads) {
-    const int k = i / Wo, j = i - k * Wo;
-    if (s.parent[k] < 0 || s.parent[j] < 0) continue;
-    const int n = s.len[s.parent[k]], e = n >> p.page_shift;
-    if ((n & (P - 1)) == 0) continue;
-    const int page = __ldg(ids + static_cast<size_t>(s.parent[k]) * p.a.table_stride + e);
-    const long long from = static_cast<long long>(e) << p.page_shift, m = s.len[s.parent[j]];
-    bool lost;
-    if (j == k) lost = static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages) || __ldg(p.a.owned + page) == 0;
-    else lost = m > from && (j < k || m >= from + P) && __ldg(ids + static_cast<size_t>(s.parent[j]) * p.a.table_stride + e) == page;
-    if (lost) atomicOr(&s.copies, 1u << k);
+}
+// Every pair (k, j) of new beams side by side: does j keep k from keeping its partly filled last page?
+struct Pair { int page, other; bool asks; };      // k's last page, what j holds there, whether there is such a page
+__device__ __forceinline__ Pair load_pair(const ForkParams& p, int g, const Group& s, int i) {
+  const int Wo = p.a.width_out, k = i / Wo, j = i - k * Wo, stride = p.a.table_stride;
+  Pair r{-1, -1, false};
+  if (i >= Wo * Wo || s.parent[k] < 0 || s.parent[j] < 0) return r;
+  const int n = s.len[s.parent[k]], e = n >> p.page_shift;
+  r.asks = (n & ((1 << p.page_shift) - 1)) != 0;
+  if (!r.asks) return r;
+  const int32_t* ids = p.a.page_ids + static_cast<size_t>(g) * p.a.width_in * stride + e;
+  r.page = __ldg(ids + static_cast<size_t>(s.parent[k]) * stride);
+  if (s.len[s.parent[j]] > (static_cast<long long>(e) << p.page_shift)) r.other = __ldg(ids + static_cast<size_t>(s.parent[j]) * stride);
+  return r;
+}
+__device__ __forceinline__ void judge_pair(const ForkParams& p, Group& s, int i, const Pair& r) {
+  if (!r.asks) return;
+  const int Wo = p.a.width_out, k = i / Wo, j = i - k * Wo;
+  const long long from = static_cast<long long>(s.len[s.parent[k]] >> p.page_shift) << p.page_shift, m = s.len[s.parent[j]];
+  bool lost;
+  if (j == k) lost = static_cast<unsigned>(r.page) >= static_cast<unsigned>(p.num_pages) || __ldg(p.a.owned + r.page) == 0;
+  else lost = m > from && (j < k || m >= from + (1 << p.page_shift)) && r.other == r.page;
+  if (lost) atomicOr(&s.copies, 1u << k);
+}
+__device__ void find_copies(const ForkParams& p, int g, Group& s, Pair first) {      // first: the thread's first pair
+  const int pairs = p.a.width_out * p.a.width_out;
+  for (int i = threadIdx.x; i < pairs; i += kForkThreads) {
+    judge_pair(p, s, i, first);
+    first = load_pair(p, g, s, i + kForkThreads);
   }
   __syncthreads();
 }
@@ -498,8 +514,8 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_count(const __gr
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int g = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int Wi = p.a.width_in, Wo = p.a.width_out, stride = p.a.table_stride;
-  load_group(p, g, s, part == 0);
-  if (part == 0 && tid == 0) p.n_copies[g] = __popc(s.copies);
+  load_lengths(p, g, s, part == 0);
+  const Pair first = load_pair(p, g, s, tid);
   unsigned kept = 0;
   for (int k = 0; k < Wo; ++k) if (s.parent[k] >= 0) kept |= 1u << s.parent[k];
   const unsigned dropped = ~kept & (Wi == 32 ? ~0u : (1u << Wi) - 1);
@@ -507,21 +523,31 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_count(const __gr
   int* out = p.freed + (static_cast<size_t>(g) * p.stretches + part) * p.stretch * Wi;
   int longest = 0;
   for (unsigned m = dropped; m; m &= m - 1) longest = max(longest, s.len[__ffs(m) - 1]);
-  const int e_end = min(min(stride, (part + 1) * p.stretch), (longest + (1 << p.page_shift) - 1) >> p.page_shift);
+  const int e_end = min(min(stride, (part + 1) * p.stretch), static_cast<int>((longest + (1ll << p.page_shift) - 1) >> p.page_shift));
+  // what all beams hold at entry e, asked for side by side
+  auto fetch = [&](int e) {
+    if (e >= e_end) return;
+    const long long from = static_cast<long long>(e) << p.page_shift;
+    for (int q0 = 0; q0 < Wi; q0 += 8) {
+      int page[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) page[q] = q0 + q < Wi && s.len[q0 + q] > from ? __ldg(ids + static_cast<size_t>(q0 + q) * stride + e) : -1;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) if (q0 + q < Wi) at_entry[(q0 + q) * kForkThreads + tid] = page[q];
+    }
+  };
+  fetch(part * p.stretch + tid);                   // (beside the pairs' pages)
+  if (part == 0) {
+    find_copies(p, g, s, first);
+    if (tid == 0) p.n_copies[g] = __popc(s.copies);
+  }
   int total = 0;
   for (int e0 = part * p.stretch; e0 < e_end; e0 += kForkThreads) {
     const int e = e0 + tid;
     unsigned back = 0;
+    if (e0 > part * p.stretch) fetch(e);
     if (e < e_end) {
       const long long from = static_cast<long long>(e) << p.page_shift;
-      // what all beams hold here, asked for side by side
-      for (int q0 = 0; q0 < Wi; q0 += 8) {
-        int page[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) page[q] = q0 + q < Wi && s.len[q0 + q] > from ? __ldg(ids + static_cast<size_t>(q0 + q) * stride + e) : -1;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) if (q0 + q < Wi) at_entry[(q0 + q) * kForkThreads + tid] = page[q];
-      }
       for (unsigned m = dropped; m; m &= m - 1) {
         const int r = __ffs(m) - 1;
         if (s.len[r] <= from) continue;
@@ -552,23 +578,28 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_count(const __gr
   if (tid == 0) p.n_freed[g * p.stretches + part] = total;
 }
 
-// Exclusive running sums of n counts into sums[0 .. n] (shared memory).
-__device__ void running_sums(const int* counts, int n, int* sums) {
-  __shared__ int warp_n[kForkThreads / 32];
+// Exclusive running sums of na counts into sa[0 .. na] and of nb into sb[0 .. nb] (shared memory), both in one scan.
+__device__ void running_sums(const int* ca, int na, int* sa, const int* cb, int nb, int* sb) {
+  __shared__ long long warp_n[kForkThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (n + kForkThreads - 1) / kForkThreads, i0 = min(tid * per, n), i1 = min(i0 + per, n);
-  int mine = 0;
-  for (int i = i0; i < i1; ++i) mine += counts[i];
-  int incl = mine;
+  const int pa = (na + kForkThreads - 1) / kForkThreads, a0 = min(tid * pa, na), a1 = min(a0 + pa, na);
+  const int pb = (nb + kForkThreads - 1) / kForkThreads, b0 = min(tid * pb, nb), b1 = min(b0 + pb, nb);
+  int in_a = 0, in_b = 0;
+  for (int i = a0; i < a1; ++i) in_a += ca[i];
+  for (int i = b0; i < b1; ++i) in_b += cb[i];
+  const long long mine = static_cast<long long>(in_b) << 32 | static_cast<unsigned>(in_a);      // (counts: neither half reaches 2^31)
+  long long incl = mine;
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) { const int y = __shfl_up_sync(kFull, incl, d); if (lane >= d) incl += y; }
-  __syncthreads();
+  for (int d = 1; d < 32; d <<= 1) { const long long y = __shfl_up_sync(kFull, incl, d); if (lane >= d) incl += y; }
   if (lane == 31) warp_n[warp] = incl;
   __syncthreads();
-  int at = incl - mine;
-  for (int w = 0; w < warp; ++w) at += warp_n[w];
-  for (int i = i0; i < i1; ++i) { sums[i] = at; at += counts[i]; }
-  if (i1 == n && i0 < n) sums[n] = at;
+  long long before = incl - mine;
+  for (int w = 0; w < warp; ++w) before += warp_n[w];
+  int at_a = static_cast<int>(before), at_b = static_cast<int>(before >> 32);
+  for (int i = a0; i < a1; ++i) { sa[i] = at_a; at_a += ca[i]; }
+  for (int i = b0; i < b1; ++i) { sb[i] = at_b; at_b += cb[i]; }
+  if (a1 == na && a0 < na) sa[na] = at_a;
+  if (b1 == nb && b0 < nb) sb[nb] = at_b;
   __syncthreads();
 }
 
@@ -581,7 +612,8 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_write(const __gr
   int* freed_at = sums;                              // [groups * stretches + 1]
   int* copies_at = sums + groups * S + 1;            // [groups + 1]
   const int part = blockIdx.y, parts = gridDim.y;
-  load_group(p, g, s, false);
+  load_lengths(p, g, s, false);
+  find_copies(p, g, s, load_pair(p, g, s, tid));
   // ---- tables: they do not depend on the counts, but for the pages of the copies; four rows side by side
   for (int k0 = 0; k0 < Wo; k0 += 4) {
     int ents[4], most = 0;
@@ -605,11 +637,11 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_write(const __gr
         }
     }
   }
+  const long long used = __ldg(p.a.reserve_used);
   __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  running_sums(p.n_freed, groups * S, freed_at);
-  running_sums(p.n_copies, groups, copies_at);
-  const long long used = __ldg(p.a.reserve_used), n_freed = freed_at[groups * S], n_copies = copies_at[groups];
+  running_sums(p.n_freed, groups * S, freed_at, p.n_copies, groups, copies_at);
+  const long long n_freed = freed_at[groups * S], n_copies = copies_at[groups];
   const bool bad = used < 0 || used > p.a.n_reserve || n_freed > used, full = !bad && used - n_freed + n_copies > p.a.n_reserve;
   const bool ok = !bad && !full;
   // ---- the counts, and the unused end of the copy list
