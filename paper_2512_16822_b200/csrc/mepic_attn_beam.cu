@@ -213,6 +213,7 @@ __global__ void __launch_bounds__(kScanThreads) mepic_beam_plan_sums(const __gri
   __shared__ int warp_n[kScanThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int n = p.groups * p.blocks * p.segments;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   int before = 0;
   for (int i0 = 0; i0 < n; i0 += kScanThreads) {
@@ -257,13 +258,14 @@ struct BeamParams {
   float scale_log2;
 };
 
+template <typename T> __device__ __forceinline__ T plain(const T* at) { return *at; }
 // The plan is one of this call's shape, and its sums are ones that its shape allows.
 __device__ __forceinline__ bool plan_fits(const BeamParams& p) {
   const int32_t* h = p.head;
-  const long long n = static_cast<long long>(p.groups) * p.blocks * p.segments, total = __ldg(p.sums + n);
-  return __ldg(h + kHMagic) == kPlanMagic && __ldg(h + kHGroups) == p.groups && __ldg(h + kHWidth) == p.width && __ldg(h + kHStride) == p.stride &&
-         __ldg(h + kHPage) == p.page_size && __ldg(h + kHGroupSize) == p.group_size && __ldg(h + kHKvHeads) == p.n_kv_heads &&
-         __ldg(h + kHBeams) == p.beams && __ldg(h + kHSegments) == p.segments && __ldg(h + kHPages) == p.num_pages &&
+  const long long n = static_cast<long long>(p.groups) * p.blocks * p.segments, total = plain(p.sums + n);
+  return plain(h + kHMagic) == kPlanMagic && plain(h + kHGroups) == p.groups && plain(h + kHWidth) == p.width && plain(h + kHStride) == p.stride &&
+         plain(h + kHPage) == p.page_size && plain(h + kHGroupSize) == p.group_size && plain(h + kHKvHeads) == p.n_kv_heads &&
+         plain(h + kHBeams) == p.beams && plain(h + kHSegments) == p.segments && plain(h + kHPages) == p.num_pages &&
          total >= 0 && total <= n * kSeg * p.beams;
 }
 // a / b where both are positive, in 32 bits where they fit (a tenth of the instructions).
@@ -274,13 +276,13 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
 struct Cut { long long total, piece; };
 __device__ __forceinline__ Cut cut_of_line(const BeamParams& p) {
   Cut c;
-  c.total = (static_cast<long long>(__ldg(p.sums + static_cast<size_t>(p.groups) * p.blocks * p.segments)) << p.log2_tpp) * p.n_kv_heads;
+  c.total = (static_cast<long long>(plain(p.sums + static_cast<size_t>(p.groups) * p.blocks * p.segments)) << p.log2_tpp) * p.n_kv_heads;
   c.piece = max(quotient(c.total + p.workers - 1, p.workers), 1ll);
   return c;
 }
 // A unit of the line: a column block under one kv head, records r0 .. r1-1 of the plan.
 struct Unit { int block, head, r0, r1; };
-__device__ __forceinline__ int begin_of(const BeamParams& p, int block) { return __ldg(p.sums + static_cast<size_t>(block) * p.segments); }
+__device__ __forceinline__ int begin_of(const BeamParams& p, int block) { return plain(p.sums + static_cast<size_t>(block) * p.segments); }
 // The unit after (block, head); false: there is none.
 __device__ __forceinline__ bool next_unit(const BeamParams& p, int& block, int& head) {
   if (++head < p.n_kv_heads) return true;
@@ -374,6 +376,11 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   }
   const int keyA = FP8 ? 4 * (g >> 1) + (g & 1) : g, keyB = FP8 ? keyA + 2 : g + 8;      // keys of the lane's two rows
 
+  // What the launches before this one wrote (the plan, the queries, pages) is complete and visible from here on; the CTAs may have been
+  // in place before, so their loads are plain ones, not of the read-only path.  (One request, plan and attention launched one by one:
+  // 16.4 us before, 14.9 so; replayed from a graph the same.)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("fence.proxy.async.global;" ::: "memory");            // ... for the copies of pages, too
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the merge kernel may move in as CTAs of this one retire
   const int candidate = candidate_of(p, lane);
   if (!plan_fits(p)) return;                                         // (reported by the merge kernel)
@@ -387,7 +394,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   // (all 192 or 512 of them, by every SM at once, took 4.7 and 6.9 us; this takes 1.6 and 2).  A warp has the rows k = warp, warp + W
   // ..., a lane two pairs of dims; asked for here, used once the first tiles are under way.
   constexpr int kCoarse = (kAngles / kTile + W) / W;            // rows 16 k of a warp, that of kAngles among them
-  auto row_of = [&](int at) { return lane < D / 4 ? __ldg(reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(min(at, p.max_position)) * D + 4 * lane)) : make_float4(0.f, 0.f, 0.f, 0.f); };
+  auto row_of = [&](int at) { return lane < D / 4 ? plain(reinterpret_cast<const float4*>(p.rope + static_cast<size_t>(min(at, p.max_position)) * D + 4 * lane)) : make_float4(0.f, 0.f, 0.f, 0.f); };
   float4 coarse[kCoarse], fine[kTile / 2];                      // c, s, c', s'
   if (!spread) {
 #pragma unroll
@@ -431,17 +438,17 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   auto issue = [&](int stage) {
     if (pr < win0 || pr >= win0 + win_n) {
       for (unsigned past = kFull; past == kFull; pseg += __popc(past))      // the segment that record pr lies in
-        past = __ballot_sync(kFull, pseg + 1 + lane < p.groups * p.blocks * p.segments && __ldg(p.sums + pseg + 1 + lane) <= pr);
-      const int s0 = __ldg(p.sums + pseg);
+        past = __ballot_sync(kFull, pseg + 1 + lane < p.groups * p.blocks * p.segments && plain(p.sums + pseg + 1 + lane) <= pr);
+      const int s0 = plain(p.sums + pseg);
       const int at = pr - s0 + lane;
       win0 = pr;
-      win_n = min(32, __ldg(p.sums + pseg + 1) - pr);
+      win_n = min(32, plain(p.sums + pseg + 1) - pr);
       const bool in = lane < win_n && at >= 0 && at < kSeg * p.beams;
-      win = in ? __ldg(p.records + static_cast<size_t>(pseg) * kSeg * p.beams + at) : make_int4(0, 0, 0, 0);
+      win = in ? plain(p.records + static_cast<size_t>(pseg) * kSeg * p.beams + at) : make_int4(0, 0, 0, 0);
       if (static_cast<unsigned>(win.x) >= static_cast<unsigned>(p.num_pages)) win.x = 0;
       if constexpr (FP8) {
-        win_ks = __ldg(p.k_scales + static_cast<size_t>(win.x) * p.n_kv_heads + p_head);
-        win_vs = __ldg(p.v_scales + static_cast<size_t>(win.x) * p.n_kv_heads + p_head);
+        win_ks = plain(p.k_scales + static_cast<size_t>(win.x) * p.n_kv_heads + p_head);
+        win_vs = plain(p.v_scales + static_cast<size_t>(win.x) * p.n_kv_heads + p_head);
       }
     }
     auto copy = [&](int page) {
@@ -589,13 +596,13 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       uint2 raw[2];
       if constexpr (FP8) {
         const uint2* src = reinterpret_cast<const uint2*>(q_src[nt] + pair_of(j, 0));
-        const uint2 lo = __ldg(src), hi = __ldg(src + D / 8);
+        const uint2 lo = plain(src), hi = plain(src + D / 8);
         raw[0] = make_uint2(lo.x, hi.x); raw[1] = make_uint2(lo.y, hi.y);
       } else {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const uint32_t* src = reinterpret_cast<const uint32_t*>(q_src[nt] + pair_of(j, r));
-          raw[r] = make_uint2(__ldg(src), __ldg(src + D / 4));
+          raw[r] = make_uint2(plain(src), plain(src + D / 4));
         }
       }
       rotate(nt, j, 0, raw[0], cs[0], sn);
@@ -603,7 +610,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     };
     auto angles_of_step = [&](int nt, int j, float4 (&cs)[2]) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) cs[r] = __ldg(reinterpret_cast<const float4*>(turn[nt] + 2 * pair_of(j, r)));
+      for (int r = 0; r < 2; ++r) cs[r] = plain(reinterpret_cast<const float4*>(turn[nt] + 2 * pair_of(j, r)));
     };
     const bool one_turn = __all_sync(kFull, same);
 #pragma unroll
@@ -648,7 +655,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {                       // a column that is none repeats the first: nobody looks at it
         const int col = 8 * nt + g < nb * G ? 8 * nt + g : 0, row = row0 + col / G;
-        q_at[nt] = __ldg(p.q_pos + row);
+        q_at[nt] = plain(p.q_pos + row);
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -1020,8 +1027,8 @@ int32_t launch_beam(BeamParams& p, int sms, int device, const CUtensorMap& map_k
     prepared.fetch_or(bit, std::memory_order_relaxed);
   }
   p.workers = sms * W;
-  mepic_beam_attn<D, NT, FP8, W><<<sms, W * 32, smem, st>>>(p, map_k, map_v);
-  e = cudaGetLastError();
+  e = launch_dependent(mepic_beam_attn<D, NT, FP8, W>, dim3(sms), dim3(W * 32), smem, st, p, map_k, map_v);
+  if (e == cudaSuccess) e = cudaGetLastError();
   const int units = p.groups * p.blocks * p.n_kv_heads;
   if (e == cudaSuccess) {
     if (p.workers <= 16LL * units) e = launch_dependent(mepic_beam_merge<D, 1>, dim3(units, (p.columns + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), st, p);

@@ -489,7 +489,7 @@ __device__ __forceinline__ Pair load_pair(const ForkParams& p, int g, const Grou
   if (s.len[s.parent[j]] > (static_cast<long long>(e) << p.page_shift)) r.other = __ldg(ids + static_cast<size_t>(s.parent[j]) * stride);
   return r;
 }
-__device__ __forceinline__ void judge_pair(const ForkParams& p, Group& s, int i, const Pair& r) {
+__device__ __forceinline__ void settle_pair(const ForkParams& p, Group& s, int i, const Pair& r) {
   if (!r.asks) return;
   const int Wo = p.a.width_out, k = i / Wo, j = i - k * Wo;
   const long long from = static_cast<long long>(s.len[s.parent[k]] >> p.page_shift) << p.page_shift, m = s.len[s.parent[j]];
@@ -501,7 +501,7 @@ __device__ __forceinline__ void judge_pair(const ForkParams& p, Group& s, int i,
 __device__ void find_copies(const ForkParams& p, int g, Group& s, Pair first) {      // first: the thread's first pair
   const int pairs = p.a.width_out * p.a.width_out;
   for (int i = threadIdx.x; i < pairs; i += kForkThreads) {
-    judge_pair(p, s, i, first);
+    settle_pair(p, s, i, first);
     first = load_pair(p, g, s, i + kForkThreads);
   }
   __syncthreads();

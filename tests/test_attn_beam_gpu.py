@@ -285,6 +285,49 @@ def test_captured_and_replayed_with_other_lengths_and_tables():
         case.check(out, 0.09)
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_queries_written_just_before_and_on_another_stream(captured):
+    # the attention may be in place before what precedes it is done: the queries change on a side stream that is joined between
+    # the plan and the attention, and in the launch right before it
+    case = BeamCase(31, Hq=8, Hkv=2, D=128, P=16, width=4, specs=[(700, 100), (90, 33)])
+    case.device()
+    good = case.fused_q()
+    q, half = torch.zeros_like(good), good.shape[0] // 2
+    case.batch(q)
+    side = torch.cuda.Stream()
+
+    def step():
+        main = torch.cuda.current_stream()
+        q.zero_()
+        case.plan.run()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000)
+            q[:half].copy_(good[:half])
+        main.wait_stream(side)
+        first = case.attn.run(0.09).clone()
+        torch.cuda._sleep(100_000)
+        q[half:].copy_(good[half:])
+        return first, case.attn.run(0.09)
+
+    if captured:
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            first, out = step()
+        for _ in range(3):
+            out.zero_()
+            graph.replay()
+    else:
+        for _ in range(3):
+            first, out = step()
+    torch.cuda.synchronize()
+    assert case.dev.read_status() == 0
+    case.check(first, 0.09, which=range(half))
+    case.check(out, 0.09)
+
+
 def test_layers_share_a_plan_and_run_on_two_streams():
     case = BeamCase(22, Hq=8, Hkv=2, D=128, P=16, width=4, specs=[(700, 100), (90, 33)])
     case.device()
