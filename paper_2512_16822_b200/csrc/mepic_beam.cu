@@ -317,7 +317,8 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   const T* logits = static_cast<const T*>(p.a.logits) + static_cast<long long>(g) * W * p.stride;
   constexpr int kRun = 4 * kVec<T>, kLoads = kSelPieces * kRun / 32;      // consecutive tokens of a set's piece; tokens of a set a lane has
   auto each_token = [&](int set, uint64_t from, auto use) {               // those whose order is `from` or more
-    const float from_f = from > 1 ? lowered(static_cast<float>(score_of(from))) : -INFINITY;
+    // (below the lowest score's order there is no number to compare with: 1 and 2 would be read as NaN)
+    const float from_f = from >= order_of(static_cast<double>(-FLT_MAX)) ? lowered(static_cast<float>(score_of(from))) : -INFINITY;
     const int w = beam_of(set);
     const T* x = logits + w * p.stride;
     const int first = token_of<T>(lead_of(x), (set - w * per) / kSelSets, lane / kRun, (set % kSelSets) * 4) + lane % kRun;
