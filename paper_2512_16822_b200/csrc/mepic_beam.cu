@@ -29,6 +29,7 @@ constexpr int kWidth = MEPIC_BEAM_MAX_WIDTH;
 // takes 33 of them (6.2 TB/s); the join is a chain of five dependent round trips.
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
+constexpr float kFusedRef = 65536.f;           // largest magnitude of a maximum that the fused form of its exponentials is for
 constexpr int kSelPieces = 8;                  // 16-byte pieces a thread reads
 constexpr int kSelSets = kSelThreads / 4;      // sets of a segment (the tokens of a CTA of the first pass)
 static_assert(kSelSets >= MEPIC_BEAM_MAX_SELECT, "as many maxima as tokens to select");
@@ -132,12 +133,13 @@ __global__ void __launch_bounds__(kSelThreads, 5) mepic_beam_pass(const __grid_c
   };
   const float2 l2 = make_float2(kLog2e, kLog2e);
   float sum;
-  if (fabsf(ref) < 1e30f) {
-    // 2^(x log2e - c) with c = ref log2e as rounded, in one fused step an element; what the rounding of c took comes back as a factor
+  if (fabsf(ref) <= kFusedRef) {
+    // 2^(x log2e - c) with c = ref log2e as rounded, in one fused step an element; what the rounding of c took (2^-8 at most: 2^16 log2e
+    // is below 2^17) comes back as a factor
     const float c0 = ref * kLog2e;
     add_all([&](float2 v) { return fma2(v, l2, make_float2(-c0, -c0)); });
     sum = (sum2.x + sum2.y) * ex2(-fmaf(ref, kLog2e, -c0));
-  } else {                                        // ref log2e may not fit (or ref is infinite)
+  } else {                                        // ref log2e would be rounded by more than a factor can give back (or ref is infinite)
     add_all([&](float2 v) { return mul2(add2(v, make_float2(-ref, -ref)), l2); });
     sum = sum2.x + sum2.y;
   }
