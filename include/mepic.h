@@ -858,7 +858,8 @@ int32_t mepic_pages_copy_fp8(const mepic_config_t* cfg, const mepic_pages_copy_a
  * plan.  A captured call may be replayed with other lengths and tables, after their plan.
  *
  * mepic_attn_beam_fp8: over 8-bit pools (head_dim 128); the rotated q and K, the weights and V are carried in fp16 (the rotated q must
- * stay below 65504), the pages' K and V scales, of either sign, beside it in fp32.
+ * stay below 65504), the pages' K and V scales, of either sign and any size, beside it in fp32.  (A weight below about 2^-17 of a row's
+ * largest is rounded to a multiple of 2^-27 of it or finer.)
  */
 typedef struct {
   const int32_t* page_ids;     /* [groups*width][table_stride] */

@@ -53,7 +53,10 @@ constexpr int kMaxColumns = 16;      // columns of a column block
 // itself where mantissas are spread as those of products are; the scores are made larger by as much for either factor.
 constexpr float kTf32Cut = 1.f + 2.f * 0x1p-11f * 0.7213475f;
 constexpr float kLag = 8.f;                      // weights may reach 2^8
-constexpr float kSmallScale = 0x1p-100f;      // 8-bit pages: V scales are taken relative to the largest met, at least to this one
+// 8-bit pages: O is kept in units of a power of two, which starts as the first one and follows the V scales of pages that all columns
+// hold, down to 2^-60 of the largest scale met (so that what a page with a large one left does not overflow).
+constexpr float kFirstUnit = 0x1p-7f, kLeastUnit = 0x1p-60f, kMostUnit = 0x1p126f, kBelowTop = 0x1p-60f;
+constexpr float kWeight = 0x1p5f;             // weights (2^8 at most) are carried as 2^5 of them, times at most 4: below 65504, and normal in fp16 from 2^-17 on
 constexpr int kSeg = 256;            // table entries a CTA of the plan looks at
 
 // ---------------------------------------------------------------- the plan's layout
@@ -537,12 +540,12 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   uint32_t qf[FP8 ? NT : 1][KS][2];
   float2 m_neg[NT], l_run[NT];               // the negative of the reference, and this lane's share of the sum, of columns 2 t, 2 t + 1
   float acc[NT][NV][4];                      // O^T: [dim g: column 2t, 2t+1 | dim g + 8: the same]
-  float v_ref = kSmallScale, v_inv = 0x1p6f / kSmallScale;      // 8-bit pages: acc is in units of v_ref 2^-6; 2^6 / v_ref
+  float v_unit = kFirstUnit, v_least = kLeastUnit;      // 8-bit pages: acc is in units of v_unit / kWeight; the least that it may be
 
   auto flush = [&]() {
     if (u_block < 0) return;
     const long long slot = static_cast<long long>(u_block) * p.n_kv_heads + u_head + w;
-    const float unit = FP8 ? v_ref * 0x1p-6f : 1.f;
+    const float unit = FP8 ? v_unit * (1.f / kWeight) : 1.f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -648,7 +651,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     if (c_block != u_block || c_head != u_head) {
       flush();
       u_block = c_block; u_head = c_head;
-      anchor = INT_MIN; v_ref = kSmallScale; v_inv = 0x1p6f / kSmallScale;
+      anchor = INT_MIN; v_unit = kFirstUnit; v_least = kLeastUnit;
       const int first = (u_block % p.blocks) * p.beams, nb = min(p.beams, p.width - first);
       all_beams = nb == 32 ? ~0u : (1u << nb) - 1;
       const int row0 = u_block / p.blocks * p.width + first;
@@ -755,26 +758,39 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       }
     }
     // ---- online softmax (log2 domain): keys A (0, 1) and B (2, 3) of columns 2t (0, 2) and 2t + 1 (1, 3)
-    const bool some = __any_sync(kFull, (beams & all_beams) != all_beams);      // (the same in every lane: the vote says so to the compiler)
-    float v_scale = 0.f, s_scale = FP8 ? p.scale_log2 : p.scale_log2 * kTf32Cut;
+    // (`some`: not all columns hold the page, or their weights cannot carry its V scale.  The same in every lane: the vote says so to the
+    // compiler)
+    bool some = (beams & all_beams) != all_beams;
+    float v_rel = 1.f, s_scale = FP8 ? p.scale_log2 : p.scale_log2 * kTf32Cut;
     if constexpr (FP8) {
       float ks, vs;
       asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(ks), "=f"(vs) : "r"(scl + stage * 8) : "memory");
       s_scale *= ks;
-      // P carries the page's V scale relative to the largest met so far, and 2^6 so that small weights stay normal in fp16 (the largest reach 2^14)
+      // A page that all columns hold, with a V scale near the unit: the weights carry it into the product.  Any other: the product is made
+      // with the weights alone and multiplied by the scale in fp32, where it is added.  So no page has a say in the precision of
+      // columns that do not hold it, nor one of little weight in that of the others: it moves the unit at most, by a power of two.
+      // (One reference for all weights, the largest scale met, left of a weight of 0.01 nothing behind a page with a scale 1e10 times
+      // the others'.)
+      auto over = [](float unit) { return __int_as_float(0x7f000000 - __float_as_int(unit)); };      // 1 / a power of two
       const float size = fabsf(vs);
-      const bool finite = size <= FLT_MAX;      // a page's scale may be infinite or NaN: that is for the columns that see the page, not for the others
-      if (finite && size > v_ref) {
-        const float f = v_ref / size;
-        v_ref = size;
-        v_inv = 0x1p6f / size;
+      v_rel = vs * over(v_unit);
+      if (!(size < 4.f * v_unit && size >= 0.25f * v_unit)) {
+        const float order = fminf(__int_as_float(__float_as_int(size) & 0x7f800000), kMostUnit);      // (infinity, NaN: no unit follows them)
+        if (size <= FLT_MAX) v_least = fmaxf(v_least, order * kBelowTop);
+        const float unit = fmaxf(some || !(size <= FLT_MAX) ? v_unit : order, v_least);
+        if (unit != v_unit) {
+          const float f = v_unit * over(unit);
+          v_unit = unit;
+          v_rel = vs * over(unit);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int db = 0; db < NV; ++db) { acc[nt][db][0] *= f; acc[nt][db][1] *= f; acc[nt][db][2] *= f; acc[nt][db][3] *= f; }
+            for (int db = 0; db < NV; ++db) { acc[nt][db][0] *= f; acc[nt][db][1] *= f; acc[nt][db][2] *= f; acc[nt][db][3] *= f; }
+        }
+        some = some || !(size < 4.f * v_unit && size >= 0.25f * v_unit);
       }
-      v_scale = finite ? vs * v_inv : __int_as_float(0x7fffffff);
     }
+    some = __any_sync(kFull, some);
     // d: the scores less the reference, of keys A (0) and B (1)
     float2 d[NT][2];
     const float2 s_scale2 = make_float2(s_scale, s_scale);
@@ -827,7 +843,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
       float2 pa = make_float2(ex2(d[nt][0].x), ex2(d[nt][0].y)), pc = make_float2(ex2(d[nt][1].x), ex2(d[nt][1].y));
       l_run[nt] = add2(l_run[nt], add2(pa, pc));
       if constexpr (FP8) {
-        const float2 v2 = make_float2(v_scale, v_scale);
+        const float v = some ? kWeight : v_rel * kWeight;
+        const float2 v2 = make_float2(v, v);
         pa = mul2(pa, v2); pc = mul2(pc, v2);
         pb[nt][0] = movmatrix_trans(pack_f16x2(pa.x, pa.y));
         pb[nt][1] = movmatrix_trans(pack_f16x2(pc.x, pc.y));
@@ -874,8 +891,13 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
         for (int nt = 0; nt < NT; ++nt) {
           float x[4] = {0.f, 0.f, 0.f, 0.f};
           mma(x, va, pb[nt]);
-          if (see[nt][0] & beams) { acc[nt][db][0] += x[0]; acc[nt][db][2] += x[2]; }
-          if (see[nt][1] & beams) { acc[nt][db][1] += x[1]; acc[nt][db][3] += x[3]; }
+          if constexpr (FP8) {
+            if (see[nt][0] & beams) { acc[nt][db][0] = fmaf(x[0], v_rel, acc[nt][db][0]); acc[nt][db][2] = fmaf(x[2], v_rel, acc[nt][db][2]); }
+            if (see[nt][1] & beams) { acc[nt][db][1] = fmaf(x[1], v_rel, acc[nt][db][1]); acc[nt][db][3] = fmaf(x[3], v_rel, acc[nt][db][3]); }
+          } else {
+            if (see[nt][0] & beams) { acc[nt][db][0] += x[0]; acc[nt][db][2] += x[2]; }
+            if (see[nt][1] & beams) { acc[nt][db][1] += x[1]; acc[nt][db][3] += x[3]; }
+          }
         }
       });
     }
