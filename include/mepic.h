@@ -788,8 +788,8 @@ int32_t mepic_beam_select(const mepic_beam_select_args_t* args, void* cuda_strea
  * MEPIC_DEV_BAD_BEAM; then every new length is 0, no copy is listed, the reserve stays as it was and the tables written hold nothing
  * of meaning.  A parent outside
  * [-1, width_in) sets MEPIC_DEV_BAD_BEAM and counts as -1, a length outside [0, table_stride * P] sets MEPIC_DEV_BAD_SLOT and is
- * clamped, a page id outside the pool sets MEPIC_DEV_BAD_PAGE and counts as not owned (it is copied, if it has to be, by a
- * copy that mepic_pages_copy skips).
+ * clamped, a page id outside the pool within a beam's length sets MEPIC_DEV_BAD_PAGE and counts as not owned (it goes into the new
+ * tables as it is, and is copied, if it has to be, by a copy that mepic_pages_copy skips).
  * The tables written must not be the tables read.  workspace: mepic_beam_fork_workspace bytes, 16-byte aligned, contents
  * overwritten.
  */

@@ -618,6 +618,7 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_write(const __gr
   load_lengths(p, g, s, false);
   find_copies(p, g, s, load_pair(p, g, s, tid));
   // ---- tables: they do not depend on the counts, but for the pages of the copies; four rows side by side
+  bool none = false;                                 // a page outside the pool, in a beam that goes on (others: by the first launch)
   for (int k0 = 0; k0 < Wo; k0 += 4) {
     int ents[4], most = 0;
     size_t from[4];
@@ -637,9 +638,11 @@ __global__ void __launch_bounds__(kForkThreads) mepic_beam_fork_write(const __gr
         if (e < ents[k]) {
           const size_t to = (static_cast<size_t>(g) * Wo + k0 + k) * stride + e;
           p.a.page_ids_out[to] = page[k]; p.a.pos_base_out[to] = pos[k];
+          none = none || static_cast<unsigned>(page[k]) >= static_cast<unsigned>(p.num_pages);
         }
     }
   }
+  if (none) atomicOr(p.a.status, MEPIC_DEV_BAD_PAGE);
   const long long used = __ldg(p.a.reserve_used);
   __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
