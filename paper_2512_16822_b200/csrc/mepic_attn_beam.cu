@@ -438,6 +438,10 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
   int4 win = make_int4(0, 0, 0, 0);
   float win_ks = 0.f, win_vs = 0.f;
   int issued = 0;                                                      // tiles handed to the ring
+  // A tile behind its page's filled slots goes by the position of the page's last tile that has any: its keys are masked, but an anchor
+  // has to be where a key is, within reach of the rope table.  How far that one is from a tile with n_valid filled slots (0 or fewer: none).
+  // (bf16 pages: where the tile is issued, 8-bit pages: where it moves the anchor; the other way takes 8-bit pages 2 % and bf16 pages 1 %.)
+  auto last_filled = [](int n_valid) { return (n_valid - 1) & -kTile; };
   auto issue = [&](int stage) {
     if (pr < win0 || pr >= win0 + win_n) {
       for (unsigned past = kFull; past == kFull; pseg += __popc(past))      // the segment that record pr lies in
@@ -472,7 +476,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     const int holds = pr - win0;
     if (lane == holds) {
       const int n_valid = min(win.w - pt * kTile, kTile);
-      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%3};" ::"r"(meta + stage * 16), "r"(win.y + pt * kTile), "r"(win.z), "r"(n_valid) : "memory");
+      const int pos = win.y + pt * kTile + (FP8 ? 0 : last_filled(n_valid));
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%3};" ::"r"(meta + stage * 16), "r"(pos), "r"(win.z), "r"(n_valid) : "memory");
       if constexpr (FP8) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(scl + stage * 8), "f"(win_ks), "f"(win_vs) : "memory");
       else copy(win.x);
     }
@@ -675,7 +680,12 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     int pos, n_valid, unused;
     unsigned beams;
     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(pos), "=r"(beams), "=r"(n_valid), "=r"(unused) : "r"(meta + stage * 16) : "memory");
-    if (anchor == INT_MIN || static_cast<unsigned>(pos - anchor) > static_cast<unsigned>(span - kTile)) {
+    auto beyond = [&]() { return anchor == INT_MIN || static_cast<unsigned>(pos - anchor) > static_cast<unsigned>(span - kTile); };
+    bool moves = beyond();
+    if constexpr (FP8) {
+      if (moves) { pos += last_filled(n_valid); moves = beyond(); }
+    }
+    if (moves) {
       const bool on = !FP8 && anchor != INT_MIN && pos - anchor == span && span <= p.max_position;
       anchor = pos;
       if (on) advance_queries();
