@@ -847,11 +847,11 @@ int32_t mepic_pages_copy_fp8(const mepic_config_t* cfg, const mepic_pages_copy_a
  *
  * mepic_attn_beam - mepic_attn_decode's formula for every row of the plan (one query, at position q_pos[row], over the row's
  * kv_len slots), each shared page read once per group (where a group has more than 16 query heads per kv head, its beams together:
- * once per 16 of them).  A row of length 0 gets zeros.  Pages that a beam does not hold and slots at or beyond its length have no
- * influence on its output whatever bits they hold.  Tensor-core products, fp32 accumulation: the rotated q and K are taken as tf32
- * (cut off after ten bits of mantissa; the mean of what that takes from a product is put back into the scores), the softmax weights
- * are rounded to bf16.  Positions may be negative: only the distance of a row's q_pos from the positions of its group's pages has to
- * stay within max_position.  q rows lie q_stride elements apart (0 = packed; otherwise at least a packed row and a multiple of 8).  The
+ * once per 16 of them).  A row of length 0 gets zeros, whatever its q and q_pos are.  Pages that a beam does not hold and slots at or
+ * beyond its length have no influence on its output whatever bits they hold.  Tensor-core products, fp32 accumulation: the rotated q
+ * and K are taken as tf32 (cut off after ten bits of mantissa; the mean of what that takes from a product is put back into the scores),
+ * the softmax weights are rounded to bf16.  Positions may be negative: only the distance of a row's q_pos from the positions of its
+ * group's pages has to stay within max_position.  q rows lie q_stride elements apart (0 = packed; otherwise at least a packed row and a multiple of 8).  The
  * plan must be one of the same config, groups, width and table_stride that ran before on the GPU: another sets MEPIC_DEV_BAD_PLAN and
  * `out` holds zeros.  The work is split over the key axis across the GPU; partials go to the workspace (mepic_attn_beam_workspace bytes, 16-byte aligned, contents overwritten)
  * and a second kernel merges them in a fixed order.  Two calls that overlap on the GPU must not share a workspace; they may share a

@@ -58,6 +58,7 @@ constexpr float kLag = 8.f;                      // weights may reach 2^8
 constexpr float kFirstUnit = 0x1p-7f, kLeastUnit = 0x1p-60f, kMostUnit = 0x1p126f, kBelowTop = 0x1p-60f;
 constexpr float kWeight = 0x1p5f;             // weights (2^8 at most) are carried as 2^5 of them, times at most 4: below 65504, and normal in fp16 from 2^-17 on
 constexpr int kSeg = 256;            // table entries a CTA of the plan looks at
+constexpr int kNowhere = INT_MIN;    // position of a query that sees nothing
 
 // ---------------------------------------------------------------- the plan's layout
 // ints: [0, kHead) header, then the running sums of records per (column block, segment), then the rows' lengths, then (16-byte
@@ -580,7 +581,7 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
     for (int nt = 0; nt < NT; ++nt) {
       const int col = 8 * nt + g < nb * G ? 8 * nt + g : 0;
       q_src[nt] = p.q + static_cast<size_t>(row0 + col / G) * p.q_stride + (static_cast<size_t>(u_head) * G + col % G) * D;
-      const int rel = q_at[nt] - anchor;
+      const int rel = q_at[nt] == kNowhere ? 0 : q_at[nt] - anchor;
       int arel = rel < 0 ? -rel : rel;
       if (static_cast<unsigned>(arel) > static_cast<unsigned>(p.max_position)) { atomicOr(p.status, MEPIC_DEV_BAD_POSITION); arel = p.max_position; }
       turn[nt] = p.rope + static_cast<size_t>(arel) * D;
@@ -663,7 +664,8 @@ mepic_beam_attn(const __grid_constant__ BeamParams p, const __grid_constant__ CU
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {                       // a column that is none repeats the first: nobody looks at it
         const int col = 8 * nt + g < nb * G ? 8 * nt + g : 0, row = row0 + col / G;
-        q_at[nt] = plain(p.q_pos + row);
+        const int at = max(plain(p.q_pos + row), kNowhere + 1);
+        q_at[nt] = plain(p.lens + row) > 0 ? at : kNowhere;     // a row without slots: nobody's position
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
