@@ -739,7 +739,8 @@ int32_t mepic_rows_commit_fp8(const mepic_config_t* cfg, const mepic_rows_commit
  *     n_new[g][k]     1 if it goes on (what mepic_step_tables takes), 0 if it is finished or there is no such candidate;
  * where there are fewer candidates: parent = token = -1, score -infinity, done = n_new = 0.  Candidates are compared in 64 bits
  * (sum of exponentials: terms in fp32, added up in fp32 over at most 64 terms of one thread and in 64 bits beyond; the logarithm is off
- * by 2^-53 of itself besides, which shows where every logit of a row is a number like -1e15).  Finite logits may be of any magnitude.
+ * by 2^-53 of itself besides, which shows where every logit of a row is a number like -1e15; logarithms of a group's beams that are
+ * within 2^-18 of one another count as equal, so that beams with the same logits and score tie).  Finite logits may be of any magnitude.
  * A row with a NaN or +infinity among its logits, a score of that kind, or a score whose difference from the logarithm exceeds
  * FLT_MAX sets MEPIC_DEV_BAD_LOGITS and offers nothing.  Rows of
  * finished beams, and of beams with score -infinity, are not read.

@@ -173,6 +173,9 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 __device__ __forceinline__ float float_of(uint32_t order) { return __uint_as_float(order ^ ((order >> 31) ? 0x80000000u : 0xffffffffu)); }
 
+// Two sums of the same terms, relative to one another: each term is off by 2^-22 (ex2) and 2^-23 (its argument), the 31 additions of a
+// thread's terms by 2^-25 each; both sums at most by 1.3e-6 therefore.  (A logarithm taken for another's is off by this much at most.)
+constexpr double kSame = 0x1p-18;
 constexpr int kJoinSets = 512;           // sets that are read again
 constexpr int kJoinList = 1536;          // tokens that are ranked
 constexpr int kJoinBatch = 8;            // pieces of four maxima a thread has under way
@@ -181,6 +184,7 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   __shared__ double lse[kWidth], base[kWidth];
   __shared__ float off[kWidth];                   // base - lse in fp32; -infinity where a beam offers no tokens
   __shared__ int kind[kWidth];                    // 0: offers nothing, 1: live, 2: finished
+  __shared__ int like[kWidth];                    // the first beam with the same logarithm
   __shared__ alignas(16) uint32_t quad_top[kSelSets];
   __shared__ uint64_t set_order[kJoinSets];
   __shared__ int sets[kJoinSets];
@@ -194,6 +198,7 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   const int n = W * S * kSelSets, per = S * kSelSets;
   const float inv_per = 1.f / static_cast<float>(per);
   if (tid == 0) { n_sets = 0; n_listed = 0; threshold = 0; }
+  if (tid < W) like[tid] = tid;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // the maxima of a batch, side by side; the first batch is on its way while the sums are taken together
   float4 top[kJoinBatch];
@@ -244,6 +249,20 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
     }
   }
   __syncthreads();
+  // Beams with the same logits have the same logarithm.  The sums of two such rows are rounded differently where the rows begin
+  // at different places of their 16 bytes, by less than kSame: one that near to an earlier beam's is taken to be the same.
+  bool alike = false;
+  for (int i = tid; i < W * W; i += kSelThreads) {
+    const int w = i / W, v = i - w * W;
+    if (v < w && kind[w] == 1 && kind[v] == 1 && fabs(lse[w] - lse[v]) <= kSame + fabs(lse[w]) * 0x1p-51) { atomicMin(&like[w], v); alike = true; }
+  }
+  if (__syncthreads_or(alike)) {
+    const bool mine = tid < W && like[tid] != tid;
+    const double l = mine ? lse[like[tid]] : 0.0;
+    __syncthreads();
+    if (mine) { lse[tid] = l; off[tid] = static_cast<float>(base[tid] - l); }
+    __syncthreads();
+  }
   auto order_at = [&](int w, float x) -> uint64_t {
     const double d = base[w] + (static_cast<double>(x) - lse[w]);
     return d >= -FLT_MAX ? order_of(d) : 0;          // (x = -infinity, or a score that fp32 does not hold: no candidate)
