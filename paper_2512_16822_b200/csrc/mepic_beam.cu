@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   bool alike = false;
   for (int i = tid; i < W * W; i += kSelThreads) {
     const int w = i / W, v = i - w * W;
-    if (v < w && kind[w] == 1 && kind[v] == 1 && fabs(lse[w] - lse[v]) <= kSame + fabs(lse[w]) * 0x1p-51) { atomicMin(&like[w], v); alike = true; }
+    if (v < w && kind[w] == 1 && kind[v] == 1 && fabs(lse[w] - lse[v]) <= kSame + fabs(lse[w]) * 0x1p-52) { atomicMin(&like[w], v); alike = true; }
   }
   if (__syncthreads_or(alike)) {
     const bool mine = tid < W && like[tid] != tid;
