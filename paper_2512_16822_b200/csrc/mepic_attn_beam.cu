@@ -12,8 +12,8 @@
 // of TMA stages of its own; pieces that end inside a column block leave partials (reference, sum, unnormalised output) that a second
 // kernel joins in a fixed order.
 //
-// Measured: 32 x 4 beams of 4 heads, 8 kv heads, over 8,300 slots 164 us (6 TB/s of what has to be read); 8 x 8 beams over 17,300 slots,
-// 700 of them their own, 155 us; 8 x 4 beams over 33,000 slots of 8-bit pages 108 us (4.1 TB/s; bound by instructions and their
+// Measured, without the plan: 32 x 4 beams of 4 heads, 8 kv heads, over 8,300 slots 164 us (6 TB/s of what has to be read); 8 x 8 beams over 17,300 slots,
+// 700 of them their own, 154 us; 8 x 4 beams over 33,000 slots of 8-bit pages 106 us (4.2 TB/s; bound by instructions and their
 // latency); one request of 4 beams over 224 slots 11 us: launch, then the chain plan -> line -> page -> partials -> merge.
 //
 // Rotation.  <R(qpos) q, R(pos) k> = <R(qpos - a) q, R(pos - a) k> for any anchor a.  A warp keeps its queries rotated for an anchor
@@ -50,7 +50,9 @@ using namespace mepic_dev;
 constexpr int kTile = 16;            // keys per staged tile
 constexpr int kMaxColumns = 16;      // columns of a column block
 // Cutting a number off after ten bits of mantissa makes it smaller, by 2^-11 of its power of two in the mean and by 2^-11 / (2 ln 2) of
-// itself where mantissas are spread as those of products are; the scores are made larger by as much for either factor.
+// itself where mantissas are spread as those of products are; the scores are made larger by as much for either factor.  (Scores of 30,
+// 320 of them: off by 3e-5 of themselves in the mean.  Where nothing is cut it is too much: by half of it, 3.5e-4 of the score, for a key
+// at its anchor, whose angle is 0.)
 constexpr float kTf32Cut = 1.f + 2.f * 0x1p-11f * 0.7213475f;
 constexpr float kLag = 8.f;                      // weights may reach 2^8
 // 8-bit pages: O is kept in units of a power of two, which starts as the first one and follows the V scales of pages that all columns

@@ -22,7 +22,7 @@ constexpr int kWidth = MEPIC_BEAM_MAX_WIDTH;
 
 // ---------------------------------------------------------------- selection
 // Two launches.  The first is a pass over the logits, bound by HBM: every warp leaves the sum of its tokens' exponentials and every
-// four threads (a SET: 64 tokens at least) their largest logit, nothing else.  The second has a CTA per group: the n_select best
+// four threads (a SET: 128 fp32 or 256 16-bit tokens) their largest logit, nothing else.  The second has a CTA per group: the n_select best
 // tokens are not below the n_select-th largest of the sets' maxima, so only the few sets that reach it are read again, and of those
 // only the tokens that reach it are ranked.  (Every segment keeping its own n_select best, in the first pass, took a dozen
 // instructions a token more: 64 x 8 beams over 100,003 fp32 tokens in 65 us against 41.)  The pass alone
@@ -922,8 +922,9 @@ extern "C" int32_t mepic_beam_fork(const mepic_config_t* cfg, const mepic_beam_f
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   mepic_beam_fork_count<<<dim3(a->groups, p.stretches), kForkThreads, static_cast<size_t>(a->width_in) * kForkThreads * sizeof(int), st>>>(p);
   e = cudaGetLastError();
-  // entries of a group's tables: a few per thread
-  const int parts = std::max(1, std::min((a->table_stride + kForkThreads - 1) / kForkThreads, std::max(1, 592 / a->groups)));
+  // entries of a group's tables: one a thread, but no more CTAs than give each of 148 SMs four; every CTA sums the counts up for itself
+  constexpr int kCtas = 4 * 148;
+  const int parts = std::max(1, std::min((a->table_stride + kForkThreads - 1) / kForkThreads, std::max(1, kCtas / a->groups)));
   if (e == cudaSuccess) e = launch_dependent(mepic_beam_fork_write, dim3(a->groups, parts), dim3(kForkThreads), smem, st, p);
   return launched("beam_fork", e, 2);
 }
