@@ -181,8 +181,9 @@ constexpr double kSame = 0x1p-18;
 constexpr int kJoinSets = 512;           // sets that are read again
 constexpr int kJoinList = 1536;          // tokens that are ranked
 constexpr int kJoinBatch = 8;            // pieces of four maxima a thread has under way
+// (three CTAs an SM: the compiler keeps to 64 registers otherwise and spills, 64 x 8 beams over 100,003 bf16 tokens 35 us against 33)
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_constant__ SelectParams p) {
+__global__ void __launch_bounds__(kSelThreads, 3) mepic_beam_join(const __grid_constant__ SelectParams p) {
   __shared__ double lse[kWidth], base[kWidth];
   __shared__ float off[kWidth];                   // base - lse in fp32; -infinity where a beam offers no tokens
   __shared__ int kind[kWidth];                    // 0: offers nothing, 1: live, 2: finished
@@ -200,7 +201,6 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   const int n = W * S * kSelSets, per = S * kSelSets;
   const float inv_per = 1.f / static_cast<float>(per);
   if (tid == 0) { n_sets = 0; n_listed = 0; threshold = 0; }
-  if (tid < W) like[tid] = tid;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // the maxima of a batch, side by side; the first batch is on its way while the sums are taken together
   float4 top[kJoinBatch];
@@ -251,20 +251,6 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
     }
   }
   __syncthreads();
-  // Beams with the same logits have the same logarithm.  The sums of two such rows are rounded differently where the rows begin
-  // at different places of their 16 bytes, by less than kSame: one that near to an earlier beam's is taken to be the same.
-  bool alike = false;
-  for (int i = tid; i < W * W; i += kSelThreads) {
-    const int w = i / W, v = i - w * W;
-    if (v < w && kind[w] == 1 && kind[v] == 1 && fabs(lse[w] - lse[v]) <= kSame + fabs(lse[w]) * 0x1p-52) { atomicMin(&like[w], v); alike = true; }
-  }
-  if (__syncthreads_or(alike)) {
-    const bool mine = tid < W && like[tid] != tid;
-    const double l = mine ? lse[like[tid]] : 0.0;
-    __syncthreads();
-    if (mine) { lse[tid] = l; off[tid] = static_cast<float>(base[tid] - l); }
-    __syncthreads();
-  }
   auto order_at = [&](int w, float x) -> uint64_t {
     const double d = base[w] + (static_cast<double>(x) - lse[w]);
     return d >= -FLT_MAX ? order_of(d) : 0;          // (x = -infinity, or a score that fp32 does not hold: no candidate)
@@ -277,7 +263,15 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   // Scores in fp32 do to leave out what cannot be among the best: x + off is off by 2^-24 of off and of itself at most.
   float most_off = 0.f;
   for (int w = 0; w < W; ++w) if (off[w] > -INFINITY) most_off = fmaxf(most_off, fabsf(off[w]));
-  auto lowered = [&](float x) { return x - 0x1p-21f * (most_off + fabsf(x)); };
+  auto lowered = [&](float x) { return x - 0x1p-21f * (most_off + fabsf(x)) - static_cast<float>(kSame); };      // (off is that of the sums as they are)
+  // Beams with the same logits have the same logarithm.  The sums of two such rows are rounded differently where the rows begin
+  // at different places of their 16 bytes, by less than kSame: one that near to an earlier beam's is taken to be the same.  (Found here, put
+  // in place behind the next barrier and used behind the one after it: nothing is compared in 64 bits before.)
+  for (int w = warp; w < W; w += kSelWarps) {
+    const bool same = lane < w && kind[w] == 1 && kind[lane] == 1 && fabs(lse[w] - lse[lane]) <= kSame + fabs(lse[w]) * 0x1p-52;
+    const unsigned those = __ballot_sync(kFull, same);
+    if (lane == 0) like[w] = those ? __ffs(those) - 1 : w;
+  }
   // ---- a first threshold, from the best of every four threads (no two equal: a number of their own in the last bits)
   float mine = ended ? static_cast<float>(base[tid]) : -INFINITY;
   for (int i0 = 0; i0 < n; i0 += 4 * kJoinBatch * kSelThreads) {
@@ -290,6 +284,11 @@ __global__ void __launch_bounds__(kSelThreads) mepic_beam_join(const __grid_cons
   quad = fmaxf(quad, __shfl_xor_sync(kFull, quad, 2));
   if ((lane & 3) == 0) quad_top[tid >> 2] = (order_of(quad) & ~(kSelSets - 1u)) | (tid >> 2);
   __syncthreads();
+  if (warp == 0) {                                 // a lane a beam: all are read before any is written
+    const double l = lane < W ? lse[like[lane]] : 0.0;
+    __syncwarp();
+    if (lane < W) lse[lane] = l;
+  }
   {
     const int i = tid >> 2, q0 = (tid & 3) * (kSelSets / 4);
     const uint32_t me = quad_top[i];
